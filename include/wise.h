@@ -9,7 +9,8 @@
  *              kv-head, query-block) list of key blocks (Eq. 6);
  *   reuse      late steps recompute Q, K, V and the softmax, restricted to
  *              that fixed block support (Eqs. 7-8).
- * Each entry point below is one hand-written CUDA kernel.
+ * Each entry point below is one hand-written CUDA kernel (two for some of
+ * the serving calls).
  *
  * Conventions shared by all entry points
  *  - Tensors are dense, contiguous, row-major device buffers owned by the
@@ -34,13 +35,15 @@
  *    the end of the preceding attention call on the same stream, whose other
  *    effects they wait for.  So idx and counts must not share memory with the
  *    O or blockmass of the preceding attention call.
- *  - Inputs are never written.  The library keeps one lazily allocated
- *    scratch buffer per device for the block-mass epilogue (see
- *    wise_full_attn_accumulate); no other call allocates device memory.
+ *  - Inputs are never written (a cache is input and output).  The library
+ *    keeps one lazily allocated scratch buffer per device for the block-mass
+ *    epilogue (see wise_full_attn_accumulate); no other call allocates device
+ *    memory.
  */
 #ifndef WISE_H_
 #define WISE_H_
 
+#include <stddef.h>
 #include <stdint.h>
 #include <cuda_runtime_api.h>
 
@@ -55,6 +58,13 @@ extern "C" {
 #define WISE_ERR_CUDA -4        /* a CUDA runtime call or kernel launch failed */
 #define WISE_ERR_TIMEOUT -5     /* a kernel's internal wait ran out (reported by wise_get_status) */
 #define WISE_ERR_BAD_SUPPORT -6 /* idx/counts held entries outside the rules (reported by wise_get_status) */
+#define WISE_ERR_BAD_CACHE -7   /* a cache's slots, lengths, pages or groups broke the rules (wise_get_status) */
+#define WISE_ERR_NO_PAGES -8    /* a cache ran out of free pages (reported by wise_get_status) */
+
+/* Element types of the serving calls. */
+#define WISE_BF16 0
+#define WISE_FP16 1
+#define WISE_FP32 2
 
 #define WISE_SEL_TOPK 0
 #define WISE_SEL_COVERAGE 1
@@ -276,9 +286,148 @@ int wise_support_overlap(const wise_shape_t* shape, const int32_t* idx_a, const 
                          const int32_t* idx_b, const int32_t* counts_b, int cap_b, unsigned long long* inter_union,
                          cudaStream_t stream);
 
+/* ------------------------------------------------------------- serving --
+ * What follows the recurrent steps when the model answers: a paged cache of
+ * keys and values, attention of new tokens over it with prefixes that
+ * requests share read once for all, and the verification of drafted tokens.
+ * The paper stops before this point; none of it changes the calls above.
+ *
+ * A cache is a pool of pages and, per sequence slot, a table row of page ids
+ * and a length in tokens.  Position p of the sequence in slot s is row
+ * p % page of page table[s][p / page]; only the first ceil(lens[s] / page)
+ * entries of a row mean anything.  refs[g] counts the table entries that hold
+ * page g; a page with refs 0 is free.  A page that several sequences hold is
+ * never written: wise_kv_extend gives a growing sequence a copy of its own.
+ * All of it is device memory that the caller owns and zeroes (table, lens,
+ * refs) before the first use; the pool needs no initial value.
+ *
+ * Calls that change the same cache must be ordered on a stream.  Faults in
+ * device data (a slot out of range or listed twice, a page id out of range,
+ * a length outside [0, max_pages * page]) make the entry concerned do nothing
+ * and are recorded for wise_get_status as WISE_ERR_BAD_CACHE; no call reads or
+ * writes outside the buffers for any table, lens, refs, slots or counts.  A
+ * negative slot in a list is an unused entry, which is passed over. */
+typedef struct {
+  int n_pages;    /* pages of the pool, below 2^30 - 1; n_pages * n_kv_heads < 2^31 */
+  int page;       /* tokens a page: 16, 32, 64 or 128 */
+  int n_slots;    /* sequences, at most 2^18 */
+  int max_pages;  /* width of a table row; max_pages * page <= 2^30 */
+  int n_layers;
+  int n_kv_heads;
+  int head_dim;   /* 64, 96 or 128 */
+  int dtype;      /* WISE_BF16 or WISE_FP16 */
+  void* pool;     /* [n_layers][2: keys, values][n_pages][n_kv_heads][page][head_dim], 16-byte aligned */
+  int32_t* table; /* [n_slots][max_pages] */
+  int32_t* lens;  /* [n_slots] */
+  int32_t* refs;  /* [n_pages] */
+} wise_cache_t;
+
+/* Forks sequences: slot dst[i] becomes a second holder of every page of slot
+ * src[i] (copy on write), for i < n.  What dst[i] held before is released
+ * first.  An entry whose dst is listed twice or is also a src, or whose src or
+ * dst is out of range, is skipped.  src, dst: device int32 [n]. */
+int wise_kv_fork(const wise_cache_t* cache, const int32_t* src, const int32_t* dst, int n, cudaStream_t stream);
+
+/* Bytes of workspace of wise_kv_extend (for lists of n) and wise_kv_compact
+ * (n ignored); one buffer of the larger size serves both. */
+size_t wise_kv_workspace(const wise_cache_t* cache, int n);
+
+/* Grows the sequence in slot slots[i] by n_new[i] >= 0 tokens, i < n: takes
+ * the pages it needs, lowest free ids first, in list order; where the last
+ * page is not full and held by others too, the sequence gets a copy of its
+ * rows in a page of its own (in every layer).  granted[i] = n_new[i], or 0
+ * where the entry was faulty, the row would exceed max_pages, or the entry
+ * needs pages and the needs up to and including it exceed the free pages
+ * (recorded as WISE_ERR_NO_PAGES); such a sequence stays as it was.  Pages
+ * that this call frees are not reused by it.  The new rows hold no value until
+ * they are written.  slots, n_new, granted: device int32 [n]; granted may be
+ * n_new.  workspace: wise_kv_workspace bytes, 16-byte aligned. */
+int wise_kv_extend(const wise_cache_t* cache, const int32_t* slots, const int32_t* n_new, int n, int32_t* granted,
+                   void* workspace, cudaStream_t stream);
+
+/* Stores new keys and values of one layer: row i < n_new[b] of K and V
+ * [batch, n_kv_heads, q_len, head_dim] becomes position
+ * lens[slots[b]] - n_new[b] + i of the sequence in slot slots[b] (lens as
+ * wise_kv_extend left it, n_new its `granted`; NULL = q_len for all).  Rows
+ * that fall on a page with several holders are left out and recorded as
+ * WISE_ERR_BAD_CACHE.  K, V: 16-byte aligned. */
+int wise_kv_write(const wise_cache_t* cache, int layer, const int32_t* slots, const int32_t* n_new, int batch,
+                  int q_len, const void* K, const void* V, cudaStream_t stream);
+
+/* Takes the last n_drop[i] tokens (at most all) off the sequence in slot
+ * slots[i], i < n, and releases the pages past its new end: rejected drafts,
+ * or a whole sequence that ends.  n_drop[i] < 0 is a fault. */
+int wise_kv_drop(const wise_cache_t* cache, const int32_t* slots, const int32_t* n_drop, int n, cudaStream_t stream);
+
+/* Moves the pages in use to ids 0 .. n_live[0] - 1: the k-th page in use at or
+ * past n_live goes to the k-th free id below it, the others stay; the tables
+ * and refs follow.  remap[g] = new id of page g, -1 if free.  remap: device
+ * int32 [n_pages]; n_live: device int32 [1]. */
+int wise_kv_compact(const wise_cache_t* cache, int32_t* remap, int32_t* n_live, void* workspace,
+                    cudaStream_t stream);
+
+/* Attention of new tokens over the cache.  Row i < n_new[b] of request b (slot
+ * s = slots[b]) sees the e = lens[s] - n_new[b] + i + 1 first positions of its
+ * sequence:
+ *   O[b,h,i] = sum_{j<e} softmax_j(scale * Q[b,h,i] . K[j]) V[j],
+ * with the keys and values of kv-head h / (n_heads / n_kv_heads) of `layer`.
+ * Rows with i >= n_new[b], e <= 0 or s < 0 give 0.
+ * Q, O: [batch, n_heads, q_len, head_dim] of the cache's type, 16-byte
+ * aligned.  n_new: device int32 [batch], or NULL (q_len for all).
+ * Sharing: the requests group_start[g] .. group_start[g+1] - 1 (g < n_groups,
+ * device int32 [n_groups + 1], ascending) declare that their first
+ * prefix_lens[g] tokens (device int32 [n_groups]) are the same pages, as
+ * wise_kv_fork leaves them; the whole pages among those tokens, up to the
+ * shortest active member, are read once for the group, through the first
+ * active member's table row.  Requests outside every group, and all of them
+ * when n_groups is 0, are read by themselves.
+ * Rows at or past lens in the pool may hold anything (infinities and NaN
+ * included); the K and V of positions below lens must be finite.
+ * Limits: batch <= 1024, q_len * n_heads / n_kv_heads <= 128.
+ * workspace: wise_prefix_attn_workspace bytes, 16-byte aligned, not shared
+ * with a call that may run at the same time; needs no initial value. */
+typedef struct {
+  int batch;
+  int q_len;
+  int n_heads;
+  int n_groups;
+  float scale; /* 0 selects 1/sqrt(head_dim) */
+} wise_prefix_t;
+
+size_t wise_prefix_attn_workspace(const wise_cache_t* cache, const wise_prefix_t* shape);
+
+int wise_prefix_attn(const wise_cache_t* cache, int layer, const wise_prefix_t* shape, const void* Q,
+                     const int32_t* slots, const int32_t* n_new, const int32_t* group_start,
+                     const int32_t* prefix_lens, void* O, void* workspace, size_t workspace_bytes,
+                     cudaStream_t stream);
+
+/* Verification of drafted tokens (speculative sampling).  Request b has
+ * n_draft[b] <= k_max drafted tokens x_i = draft[b][i] with draft
+ * probabilities q[b][i][:] and target probabilities p[b][i][:]; p has one row
+ * more.  With given random numbers in [0, 1):
+ *   accepted n = number of leading i with u_accept[b][i] * q_i(x_i) < p_i(x_i)
+ *                (the product rounded to fp32);
+ *   r_v = max(p_n(v) - q_n(v), 0) in fp32, or p_n(v) when n == n_draft[b];
+ *   w_v = floor(min(r_v, 1) * 2^40), of p_n(v) instead when every w_v is 0;
+ *   t = floor(W * floor(u_sample[b] * 2^24) / 2^24), W the sum of w;
+ *   next token = the lowest v with w_0 + .. + w_v > t   (-1 when W == 0).
+ * The sums are exact integers, so the tokens are a function of the inputs
+ * alone.  NaN counts as 0; a drafted token outside [0, vocab) is refused, with
+ * r = p_n, and recorded as WISE_ERR_BAD_CACHE.
+ * p: [batch, k_max + 1, vocab], q: [batch, k_max, vocab] of type dtype
+ * (WISE_BF16, WISE_FP16, WISE_FP32); draft int32 [batch, k_max]; n_draft int32
+ * [batch] or NULL (k_max for all); u_accept fp32 [batch, k_max]; u_sample fp32
+ * [batch]; accepted int32 [batch]; tokens int32 [batch, k_max + 1]: the
+ * accepted tokens, the next token, then -1.  k_max <= 1024, vocab <= 2^18;
+ * q, draft and u_accept may be NULL when k_max is 0. */
+int wise_verify_draft(int batch, int k_max, int vocab, int dtype, const void* p, const void* q,
+                      const int32_t* draft, const int32_t* n_draft, const float* u_accept, const float* u_sample,
+                      int32_t* accepted, int32_t* tokens, cudaStream_t stream);
+
 /* Synchronizes `stream`, then reads and clears the current device's status
- * word: WISE_OK, WISE_ERR_BAD_SUPPORT or WISE_ERR_TIMEOUT (the latter wins
- * when both were recorded), or WISE_ERR_CUDA if the synchronization failed. */
+ * word: WISE_OK, or what was recorded, in the order WISE_ERR_TIMEOUT,
+ * WISE_ERR_BAD_SUPPORT, WISE_ERR_BAD_CACHE, WISE_ERR_NO_PAGES when there was
+ * more than one; WISE_ERR_CUDA if the synchronization failed. */
 int wise_get_status(cudaStream_t stream);
 
 /* Sets the time limit of each internal wait of the attention kernels

@@ -1,0 +1,416 @@
+// The paged cache's own operations: forking sequences, growing them (page
+// allocation and copy-on-write), storing new keys and values, dropping tokens
+// and closing up the pages in use.  All state is integers in device memory;
+// every result is a function of the inputs alone, whatever order the threads
+// run in: pages are taken and moved by rank (prefix sums over refs), and the
+// atomics below are integer additions and ORs whose order does not show.
+#include <algorithm>
+
+#include "internal.cuh"
+
+namespace wise {
+namespace {
+
+constexpr int kPlanThreads = 1024;
+
+__device__ __forceinline__ void fault(const CacheView& c, int bits) { atomicOr(c.status, bits); }
+
+__device__ __forceinline__ bool valid_page(const CacheView& c, int page) { return page >= 0 && page < c.n_pages; }
+
+__device__ __forceinline__ int pages_of(const CacheView& c, int len) { return (len + c.page - 1) / c.page; }
+
+// One holder of a page less or more; ids out of range are skipped.
+__device__ __forceinline__ bool count_ref(const CacheView& c, int page, int by) {
+  if (!valid_page(c, page)) return false;
+  atomicAdd(c.refs + page, by);
+  return true;
+}
+
+// ---------------------------------------------------------------------- fork
+// One block per entry.  An entry whose dst occurs again in dst or in src is
+// left out, so no two blocks touch the same row.
+__global__ void __launch_bounds__(256) fork_kernel(const CacheView c, const int32_t* src, const int32_t* dst, int n) {
+  const int i = blockIdx.x;
+  const int s = src[i], d = dst[i];
+  if (s < 0 || d < 0) return;
+  int bad = s >= c.n_slots || d >= c.n_slots;
+  for (int j = threadIdx.x; j < n; j += blockDim.x)
+    if ((j != i && dst[j] == d) || src[j] == d) bad = 1;
+  int len = 0, old = 0;
+  if (s < c.n_slots && d < c.n_slots) {
+    len = c.lens[s];
+    old = c.lens[d];
+    if (len < 0 || len > c.max_len || old < 0 || old > c.max_len) bad = 1;
+  }
+  if (__syncthreads_or(bad)) {
+    if (threadIdx.x == 0) fault(c, kStatusBadCache);
+    return;
+  }
+  const int32_t* from = c.table + (size_t)s * c.max_pages;
+  int32_t* to = c.table + (size_t)d * c.max_pages;
+  for (int k = threadIdx.x; k < pages_of(c, old); k += blockDim.x) bad |= !count_ref(c, to[k], -1);
+  for (int k = threadIdx.x; k < pages_of(c, len); k += blockDim.x) {
+    const int page = from[k];
+    bad |= !count_ref(c, page, 1);
+    to[k] = page;
+  }
+  if (bad) fault(c, kStatusBadCache);
+  if (threadIdx.x == 0) c.lens[d] = len;  // every thread read it before the barrier
+}
+
+// ---------------------------------------------------------------------- drop
+__global__ void __launch_bounds__(256) drop_kernel(const CacheView c, const int32_t* slots, const int32_t* n_drop,
+                                                   int n) {
+  const int i = blockIdx.x;
+  const int s = slots[i];
+  if (s < 0) return;
+  const int drop = n_drop[i];
+  int bad = s >= c.n_slots || drop < 0;
+  for (int j = threadIdx.x; j < n; j += blockDim.x)
+    if (j != i && slots[j] == s) bad = 1;
+  int len = 0;
+  if (s < c.n_slots) {
+    len = c.lens[s];
+    if (len < 0 || len > c.max_len) bad = 1;
+  }
+  if (__syncthreads_or(bad)) {
+    if (threadIdx.x == 0) fault(c, kStatusBadCache);
+    return;
+  }
+  const int left = drop >= len ? 0 : len - drop;
+  const int32_t* row = c.table + (size_t)s * c.max_pages;
+  for (int k = pages_of(c, left) + threadIdx.x; k < pages_of(c, len); k += blockDim.x)
+    bad |= !count_ref(c, row[k], -1);
+  if (bad) fault(c, kStatusBadCache);
+  if (threadIdx.x == 0) c.lens[s] = left;
+}
+
+// -------------------------------------------------------------------- extend
+// Sums of page counts stop at kSumCap, above every n_pages, so that absurd
+// lists cannot wrap them around (the capped sum is still associative).
+constexpr int kSumCap = (1 << 30) - 1;
+__device__ __forceinline__ int capped_sum(int a, int b) { return min(a + b, kSumCap); }
+
+// Inclusive prefix sum over the block; `total` receives the block's sum.
+__device__ __forceinline__ int block_scan(int v, int* warp_sums, int& total) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int t = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v = capped_sum(v, t);
+  }
+  if (lane == 31) warp_sums[w] = v;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+  for (int k = 0; k < kPlanThreads / 32; ++k) {
+    const int t = warp_sums[k];
+    if (k < w) before = capped_sum(before, t);
+    total = capped_sum(total, t);
+  }
+  __syncthreads();
+  return capped_sum(v, before);
+}
+
+// Workspace words: [0] number of copies; then the free list, the entries'
+// needs, and the copies as (from, to, rows).
+struct ExtendWork {
+  int32_t* count;
+  int32_t* free_ids;
+  int32_t* need;
+  int32_t* copies;
+};
+__host__ __device__ inline ExtendWork extend_work(int32_t* w, int n_pages, int n) {
+  ExtendWork e;
+  e.count = w;
+  e.free_ids = w + 4;
+  e.need = e.free_ids + n_pages;
+  e.copies = e.need + n;
+  return e;
+}
+constexpr int kNeedCopy = 1 << 30;  // flag beside an entry's number of pages
+constexpr int kNeedNone = -1;       // unused or faulty entry
+
+// One block.  (1) the need of every entry from the state before the call,
+// (2) the lowest free pages, as many as are needed, (3) their assignment.
+__global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const CacheView c, const int32_t* slots,
+                                                                   const int32_t* n_new, int n, int32_t* granted,
+                                                                   int32_t* work) {
+  extern __shared__ uint32_t seen[];  // two bitmaps over the slots: listed, listed twice
+  __shared__ int warp_sums[kPlanThreads / 32];
+  __shared__ int n_copies;
+  const ExtendWork w = extend_work(work, c.n_pages, n);
+  const int words = (c.n_slots + 31) / 32;
+  uint32_t* twice = seen + words;
+  for (int k = threadIdx.x; k < 2 * words; k += kPlanThreads) seen[k] = 0;
+  if (threadIdx.x == 0) n_copies = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+    const int s = slots[i];
+    if (s >= 0 && s < c.n_slots) {
+      const uint32_t bit = 1u << (s & 31);
+      if (atomicOr(&seen[s >> 5], bit) & bit) atomicOr(&twice[s >> 5], bit);
+    }
+  }
+  __syncthreads();
+  int want = 0;
+  for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+    const int s = slots[i], add = n_new[i];
+    int need = kNeedNone;
+    if (s >= 0) {
+      const bool in = s < c.n_slots;
+      const int len = in ? c.lens[s] : -1;
+      if (!in || add < 0 || ((twice[s >> 5] >> (s & 31)) & 1u) || len < 0 || len > c.max_len) {
+        fault(c, kStatusBadCache);
+      } else if (add > c.max_len - len) {
+        fault(c, kStatusNoPages);
+      } else {
+        need = pages_of(c, len + add) - pages_of(c, len);
+        if (add > 0 && len % c.page != 0) {
+          const int tail = c.table[(size_t)s * c.max_pages + len / c.page];
+          if (!valid_page(c, tail)) {
+            fault(c, kStatusBadCache);
+            need = kNeedNone;
+          } else if (c.refs[tail] > 1) {
+            need = (need + 1) | kNeedCopy;
+          }
+        }
+      }
+    }
+    w.need[i] = need;
+    if (need != kNeedNone) want = capped_sum(want, need & ~kNeedCopy);
+  }
+  int total_want;
+  block_scan(want, warp_sums, total_want);
+  // Free pages in ascending order.
+  int found = 0;
+  for (int base = 0; base < c.n_pages && found < total_want; base += kPlanThreads) {
+    const int page = base + threadIdx.x;
+    const int is_free = page < c.n_pages && c.refs[page] == 0;
+    int t;
+    const int upto = block_scan(is_free, warp_sums, t);
+    if (is_free) w.free_ids[found + upto - 1] = page;
+    found += t;
+  }
+  __syncthreads();
+  // Assignment, in list order.
+  int carry = 0;
+  for (int base = 0; base < n; base += kPlanThreads) {
+    const int i = base + threadIdx.x;
+    const int info = i < n ? w.need[i] : kNeedNone;
+    const int need = info == kNeedNone ? 0 : info & ~kNeedCopy;
+    int t;
+    const int upto = block_scan(need, warp_sums, t);
+    if (i < n) {
+      const int s = slots[i], add = n_new[i];
+      const int end = capped_sum(carry, upto), first = end - need;
+      int give = 0;
+      if (info != kNeedNone) {
+        if (need == 0 || end <= found) {
+          give = add;
+          const int len = c.lens[s];
+          int32_t* row = c.table + (size_t)s * c.max_pages;
+          int k = pages_of(c, len);
+          if (info & kNeedCopy) {
+            --k;
+            const int tail = row[k];
+            atomicAdd(c.refs + tail, -1);
+            const int at = atomicAdd(&n_copies, 1);
+            w.copies[3 * at] = tail;
+            w.copies[3 * at + 1] = w.free_ids[first];
+            w.copies[3 * at + 2] = len % c.page;
+          }
+          for (int j = 0; j < need; ++j) {
+            const int page = w.free_ids[first + j];
+            row[k + j] = page;
+            c.refs[page] = 1;
+          }
+          c.lens[s] = len + add;
+        } else {
+          fault(c, kStatusNoPages);
+        }
+      }
+      granted[i] = give;
+    }
+    carry = capped_sum(carry, t);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) *w.count = n_copies;
+}
+
+// Copies the first `rows` rows of every head of a page, in every plane; one
+// block per (copy, plane, head) in turn.
+__global__ void __launch_bounds__(256) copy_tails_kernel(const CacheView c, int32_t* work, int n) {
+  const ExtendWork w = extend_work(work, c.n_pages, n);
+  const long long jobs = (long long)*w.count * c.n_planes * c.n_kv_heads;
+  for (long long job = blockIdx.x; job < jobs; job += gridDim.x) {
+    const int head = (int)(job % c.n_kv_heads);
+    const long long r = job / c.n_kv_heads;
+    const int plane = (int)(r % c.n_planes), at = (int)(r / c.n_planes);
+    uint8_t* base = c.pool + plane * c.plane_bytes + (size_t)head * c.head_bytes;
+    const uint4* from = reinterpret_cast<const uint4*>(base + (size_t)w.copies[3 * at] * c.page_bytes);
+    uint4* to = reinterpret_cast<uint4*>(base + (size_t)w.copies[3 * at + 1] * c.page_bytes);
+    const int units = w.copies[3 * at + 2] * (c.row_bytes / 16);
+    for (int k = threadIdx.x; k < units; k += blockDim.x) to[k] = from[k];
+  }
+}
+
+// --------------------------------------------------------------------- write
+// One thread per 16 bytes of K and of V (blockIdx.y = 0, 1).
+__global__ void __launch_bounds__(256) write_kernel(const CacheView c, int layer, const int32_t* slots,
+                                                    const int32_t* n_new, int q_len, long long units, const uint4* K,
+                                                    const uint4* V) {
+  const long long u = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  if (u >= units) return;
+  const int per_row = c.row_bytes / 16;
+  const long long r = u / per_row;
+  const int i = (int)(r % q_len);
+  const long long bh = r / q_len;
+  const int head = (int)(bh % c.n_kv_heads), b = (int)(bh / c.n_kv_heads);
+  const int s = slots[b];
+  if (s < 0) return;
+  if (s >= c.n_slots) {
+    fault(c, kStatusBadCache);
+    return;
+  }
+  const int len = c.lens[s];
+  int add = n_new ? n_new[b] : q_len;
+  if (len < 0 || len > c.max_len || add < 0 || add > q_len || add > len) {
+    fault(c, kStatusBadCache);
+    return;
+  }
+  if (i >= add) return;
+  const int pos = len - add + i;
+  const int page = c.table[(size_t)s * c.max_pages + pos / c.page];
+  if (!valid_page(c, page) || c.refs[page] > 1) {
+    fault(c, kStatusBadCache);
+    return;
+  }
+  uint8_t* to = c.pool + (2 * layer + blockIdx.y) * c.plane_bytes + (size_t)page * c.page_bytes +
+                (size_t)head * c.head_bytes + (size_t)(pos % c.page) * c.row_bytes;
+  reinterpret_cast<uint4*>(to)[u % per_row] = (blockIdx.y ? V : K)[u];
+}
+
+// ------------------------------------------------------------------- compact
+// Workspace words: [0] number of moves; then the holes and the pages that
+// move into them, both ascending.
+__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const CacheView c, int32_t* remap,
+                                                                    int32_t* n_live_out, int32_t* work) {
+  __shared__ int warp_sums[kPlanThreads / 32];
+  int32_t* holes = work + 4;
+  int32_t* movers = holes + c.n_pages;
+  int mine = 0, n_live;
+  for (int page = threadIdx.x; page < c.n_pages; page += kPlanThreads) mine += c.refs[page] != 0;
+  block_scan(mine, warp_sums, n_live);
+  int n_holes = 0, n_movers = 0;
+  for (int base = 0; base < c.n_pages; base += kPlanThreads) {
+    const int page = base + threadIdx.x;
+    const bool in = page < c.n_pages;
+    const bool live = in && c.refs[page] != 0;
+    const int hole = in && !live && page < n_live, mover = live && page >= n_live;
+    int t;
+    const int h = block_scan(hole, warp_sums, t);
+    if (hole) holes[n_holes + h - 1] = page;
+    n_holes += t;
+    const int m = block_scan(mover, warp_sums, t);
+    if (mover) movers[n_movers + m - 1] = page;
+    n_movers += t;
+    if (in && !mover) remap[page] = live ? page : -1;
+  }
+  __syncthreads();
+  for (int k = threadIdx.x; k < n_movers; k += kPlanThreads) {
+    const int from = movers[k], to = holes[k];
+    remap[from] = to;
+    c.refs[to] = c.refs[from];
+    c.refs[from] = 0;
+  }
+  if (threadIdx.x == 0) {
+    work[0] = n_movers;
+    *n_live_out = n_live;
+  }
+}
+
+// Moves pages (sources lie at or past n_live, destinations below it, so the
+// copies are independent) and renames the tables' entries.
+__global__ void __launch_bounds__(256) compact_move_kernel(const CacheView c, const int32_t* remap,
+                                                           const int32_t* work) {
+  const int32_t* holes = work + 4;
+  const int32_t* movers = holes + c.n_pages;
+  constexpr int kPiece = 16384;  // bytes of a page one block copies at a time
+  const int pieces = (c.page_bytes + kPiece - 1) / kPiece;
+  const long long jobs = (long long)work[0] * c.n_planes * pieces;
+  for (long long job = blockIdx.x; job < jobs; job += gridDim.x) {
+    const int piece = (int)(job % pieces);
+    const long long r = job / pieces;
+    const int plane = (int)(r % c.n_planes), at = (int)(r / c.n_planes);
+    uint8_t* base = c.pool + plane * c.plane_bytes + (size_t)piece * kPiece;
+    const uint4* from = reinterpret_cast<const uint4*>(base + (size_t)movers[at] * c.page_bytes);
+    uint4* to = reinterpret_cast<uint4*>(base + (size_t)holes[at] * c.page_bytes);
+    const int units = min(kPiece, c.page_bytes - piece * kPiece) / 16;
+    for (int k = threadIdx.x; k < units; k += blockDim.x) to[k] = from[k];
+  }
+  for (int s = blockIdx.x; s < c.n_slots; s += gridDim.x) {
+    const int len = c.lens[s];
+    if (len < 0 || len > c.max_len) {
+      if (threadIdx.x == 0) fault(c, kStatusBadCache);
+      continue;
+    }
+    int32_t* row = c.table + (size_t)s * c.max_pages;
+    for (int k = threadIdx.x; k < pages_of(c, len); k += blockDim.x) {
+      const int page = row[k];
+      if (!valid_page(c, page)) {
+        fault(c, kStatusBadCache);
+        continue;
+      }
+      const int to = remap[page];
+      if (to < 0)
+        fault(c, kStatusBadCache);  // a sequence holds a page that refs calls free
+      else if (to != page)
+        row[k] = to;
+    }
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_kv_fork(const CacheView& c, const int32_t* src, const int32_t* dst, int n, cudaStream_t stream) {
+  fork_kernel<<<n, 256, 0, stream>>>(c, src, dst, n);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv_drop(const CacheView& c, const int32_t* slots, const int32_t* n_drop, int n,
+                           cudaStream_t stream) {
+  drop_kernel<<<n, 256, 0, stream>>>(c, slots, n_drop, n);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv_extend(const CacheView& c, const int32_t* slots, const int32_t* n_new, int n, int32_t* granted,
+                             int32_t* work, int sm_count, cudaStream_t stream) {
+  const int smem = 2 * ((c.n_slots + 31) / 32) * 4;
+  cudaError_t e = cudaFuncSetAttribute(extend_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  extend_plan_kernel<<<1, kPlanThreads, smem, stream>>>(c, slots, n_new, n, granted, work);
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  copy_tails_kernel<<<sm_count * 8, 256, 0, stream>>>(c, work, n);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv_write(const CacheView& c, int layer, const int32_t* slots, const int32_t* n_new, int batch,
+                            int q_len, const void* K, const void* V, cudaStream_t stream) {
+  const long long units = (long long)batch * c.n_kv_heads * q_len * (c.row_bytes / 16);
+  const dim3 grid((unsigned)((units + 255) / 256), 2);
+  write_kernel<<<grid, 256, 0, stream>>>(c, layer, slots, n_new, q_len, units, reinterpret_cast<const uint4*>(K),
+                                         reinterpret_cast<const uint4*>(V));
+  return cudaGetLastError();
+}
+
+cudaError_t launch_kv_compact(const CacheView& c, int32_t* remap, int32_t* n_live, int32_t* work, int sm_count,
+                              cudaStream_t stream) {
+  compact_plan_kernel<<<1, kPlanThreads, 0, stream>>>(c, remap, n_live, work);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  compact_move_kernel<<<sm_count * 8, 256, 0, stream>>>(c, remap, work);
+  return cudaGetLastError();
+}
+
+}  // namespace wise

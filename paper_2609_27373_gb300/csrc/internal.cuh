@@ -26,6 +26,8 @@ __host__ __device__ constexpr size_t scratch_floats_per_cta(int n_tiles, int sub
 // Bits of the per-device status word.
 constexpr int kStatusTimeout = 1;
 constexpr int kStatusBadSupport = 2;
+constexpr int kStatusBadCache = 4;
+constexpr int kStatusNoPages = 8;
 
 struct AttnParams {
   int batch, seqlen, n_heads, n_kv_heads, group;
@@ -140,6 +142,77 @@ struct SupportOverlapParams {
   unsigned long long* inter_union;  // [batch][2]
   int* status;
 };
+
+// SM count and status word of the current device, which must be one that the
+// library runs on (defined in wise_api.cu).
+int current_device(int* sm_count, int** status);
+unsigned long long wait_limit_ns();
+
+// Tensor map of a 16-bit [outer, rows, cols] array with 64-column,
+// box_rows-row boxes in the 128-byte swizzle (defined in wise_api.cu).
+bool make_tile_map(CUtensorMap* map, const void* base, bool fp16, int cols, int rows, long long outer, int box_rows);
+
+// A paged cache as the kernels see it (wise_cache_t).
+struct CacheView {
+  int n_pages, page, n_slots, max_pages;
+  int n_planes;           // n_layers * 2
+  long long plane_bytes;  // n_pages * page_bytes
+  int page_bytes;         // n_kv_heads * page * head_dim * 2
+  int head_bytes;         // page * head_dim * 2
+  int row_bytes;          // head_dim * 2
+  int n_kv_heads;
+  uint8_t* pool;
+  int32_t* table;
+  int32_t* lens;
+  int32_t* refs;
+  int* status;
+  int max_len;            // max_pages * page
+};
+
+// Defined in cache.cu.
+cudaError_t launch_kv_fork(const CacheView& c, const int32_t* src, const int32_t* dst, int n, cudaStream_t stream);
+cudaError_t launch_kv_extend(const CacheView& c, const int32_t* slots, const int32_t* n_new, int n, int32_t* granted,
+                             int32_t* work, int sm_count, cudaStream_t stream);
+cudaError_t launch_kv_write(const CacheView& c, int layer, const int32_t* slots, const int32_t* n_new, int batch,
+                            int q_len, const void* K, const void* V, cudaStream_t stream);
+cudaError_t launch_kv_drop(const CacheView& c, const int32_t* slots, const int32_t* n_drop, int n,
+                           cudaStream_t stream);
+cudaError_t launch_kv_compact(const CacheView& c, int32_t* remap, int32_t* n_live, int32_t* work, int sm_count,
+                              cudaStream_t stream);
+
+struct PrefixParams {
+  CacheView cache;
+  int layer;
+  int batch, q_len, n_heads, group, n_groups, head_dim;
+  bool fp16;
+  float scale_log2;
+  const void* Q;
+  void* O;
+  const int32_t* slots;
+  const int32_t* n_new;
+  const int32_t* group_start;
+  const int32_t* prefix_lens;
+};
+
+// Defined in prefix_attn.cu.
+size_t prefix_attn_workspace(const PrefixParams& p, int sm_count);
+cudaError_t launch_prefix_attn(const PrefixParams& p, void* workspace, int sm_count, cudaStream_t stream);
+
+struct VerifyParams {
+  int batch, k_max, vocab;
+  const void* p;
+  const void* q;
+  const int32_t* draft;
+  const int32_t* n_draft;
+  const float* u_accept;
+  const float* u_sample;
+  int32_t* accepted;
+  int32_t* tokens;
+  int* status;
+};
+
+// Defined in verify.cu.
+cudaError_t launch_verify_draft(int dtype, const VerifyParams& p, cudaStream_t stream);
 
 // Defined in diag.cu.
 cudaError_t launch_support_mass(const SupportMassParams& p, cudaStream_t stream);

@@ -123,18 +123,34 @@ int check_shape(const wise_shape_t* sh, bool attention) {
 // box_rows-row boxes in the 128-byte swizzle.  Rows past seqlen read as zero
 // and are not written by stores.
 bool make_map(CUtensorMap* map, const void* base, int head_dim, int seqlen, long long outer, int box_rows) {
-  EncodeTiledFn enc = encode_tiled();
-  if (!enc) return false;
-  cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)seqlen, (cuuint64_t)outer};
-  cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)head_dim * 2 * (cuuint64_t)seqlen};
-  cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
-  cuuint32_t elem[3] = {1, 1, 1};
-  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, elem,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return make_tile_map(map, base, false, head_dim, seqlen, outer, box_rows);
 }
 
 }  // namespace
+
+int current_device(int* sm_count, int** status) {
+  int err = WISE_OK;
+  DeviceState* ds = device_state(&err);
+  if (!ds) return err;
+  *sm_count = ds->sm_count;
+  *status = ds->status;
+  return WISE_OK;
+}
+
+unsigned long long wait_limit_ns() { return g_wait_ns.load(std::memory_order_relaxed); }
+
+bool make_tile_map(CUtensorMap* map, const void* base, bool fp16, int cols, int rows, long long outer, int box_rows) {
+  EncodeTiledFn enc = encode_tiled();
+  if (!enc) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)outer};
+  cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)cols * 2 * (cuuint64_t)rows};
+  cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
+  cuuint32_t elem[3] = {1, 1, 1};
+  return enc(map, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+             const_cast<void*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 int launch_attention(const wise_shape_t* sh, const void* Q, const void* K, const void* V, void* O, int mode,
                      float* blockmass, int step, const int32_t* idx, const int32_t* counts, int cap,
@@ -478,6 +494,8 @@ extern "C" int wise_get_status(cudaStream_t stream) {
   }
   if (word & kStatusTimeout) return WISE_ERR_TIMEOUT;
   if (word & kStatusBadSupport) return WISE_ERR_BAD_SUPPORT;
+  if (word & kStatusBadCache) return WISE_ERR_BAD_CACHE;
+  if (word & kStatusNoPages) return WISE_ERR_NO_PAGES;
   return WISE_OK;
 }
 
@@ -490,6 +508,8 @@ extern "C" const char* wise_status_string(int status) {
     case WISE_ERR_CUDA: return "CUDA runtime error";
     case WISE_ERR_TIMEOUT: return "a kernel wait ran out of time";
     case WISE_ERR_BAD_SUPPORT: return "support list entries out of range, unordered or over cap";
+    case WISE_ERR_BAD_CACHE: return "cache slots, lengths, page ids, groups or draft tokens out of range or repeated";
+    case WISE_ERR_NO_PAGES: return "the cache has too few free pages";
     default: return "unknown status";
   }
 }

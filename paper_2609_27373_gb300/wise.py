@@ -23,6 +23,8 @@ WISE_ERR_SHAPE = -3
 WISE_ERR_CUDA = -4
 WISE_ERR_TIMEOUT = -5
 WISE_ERR_BAD_SUPPORT = -6
+WISE_ERR_BAD_CACHE = -7
+WISE_ERR_NO_PAGES = -8
 WISE_SEL_TOPK = 0
 WISE_SEL_COVERAGE = 1
 
@@ -30,7 +32,8 @@ EXPORTS = ("wise_full_attn_accumulate", "wise_full_attn_accumulate_noalloc", "wi
            "wise_sparse_attn", "wise_freeze_a_attn", "wise_freeze_a_probs", "wise_frozen_pv", "wise_support_mass",
            "wise_support_overlap",
            "wise_select_working_set", "wise_get_status", "wise_set_wait_limit_ns", "wise_status_string",
-           "wise_version")
+           "wise_version", "wise_kv_fork", "wise_kv_workspace", "wise_kv_extend", "wise_kv_write", "wise_kv_drop",
+           "wise_kv_compact", "wise_prefix_attn", "wise_prefix_attn_workspace", "wise_verify_draft")
 NOALLOC_SCRATCH_BYTES = 8 << 20
 
 
@@ -49,6 +52,18 @@ class wise_shape_t(ctypes.Structure):
 class wise_select_t(ctypes.Structure):
     _fields_ = [("n_sink", ctypes.c_int), ("n_local", ctypes.c_int), ("mode", ctypes.c_int),
                 ("topk", ctypes.c_int), ("eta", ctypes.c_float), ("cap", ctypes.c_int)]
+
+
+class wise_cache_t(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int), ("page", ctypes.c_int), ("n_slots", ctypes.c_int),
+                ("max_pages", ctypes.c_int), ("n_layers", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("dtype", ctypes.c_int), ("pool", ctypes.c_void_p),
+                ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+
+
+class wise_prefix_t(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int), ("q_len", ctypes.c_int), ("n_heads", ctypes.c_int),
+                ("n_groups", ctypes.c_int), ("scale", ctypes.c_float)]
 
 
 @dataclasses.dataclass(frozen=True)
@@ -113,6 +128,18 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         lib.wise_support_overlap.argtypes = [ctypes.POINTER(wise_shape_t), P, P, I, P, P, I, P, P]
         lib.wise_select_working_set.argtypes = [ctypes.POINTER(wise_shape_t), I, ctypes.c_float, I, I, P, I, P, P,
                                                 I, P, P, I, P]
+        C, Z = ctypes.POINTER(wise_cache_t), ctypes.c_size_t
+        lib.wise_kv_fork.argtypes = [C, P, P, I, P]
+        lib.wise_kv_workspace.argtypes = [C, I]
+        lib.wise_kv_workspace.restype = Z
+        lib.wise_kv_extend.argtypes = [C, P, P, I, P, P, P]
+        lib.wise_kv_write.argtypes = [C, I, P, P, I, I, P, P, P]
+        lib.wise_kv_drop.argtypes = [C, P, P, I, P]
+        lib.wise_kv_compact.argtypes = [C, P, P, P, P]
+        lib.wise_prefix_attn_workspace.argtypes = [C, ctypes.POINTER(wise_prefix_t)]
+        lib.wise_prefix_attn_workspace.restype = Z
+        lib.wise_prefix_attn.argtypes = [C, I, ctypes.POINTER(wise_prefix_t), P, P, P, P, P, P, P, Z, P]
+        lib.wise_verify_draft.argtypes = [I, I, I, I, P, P, P, P, P, P, P, P, P]
         lib.wise_get_status.argtypes = [P]
         lib.wise_set_wait_limit_ns.argtypes = [ctypes.c_ulonglong]
         lib.wise_status_string.argtypes = [ctypes.c_int]
@@ -358,6 +385,203 @@ def wise_select_working_set(shape: Shape, mode: int, step_masses, idx, counts, e
                                         _ptr(idx), _ptr(counts), cap, _stream(stream))
     if rc != WISE_OK:
         raise WiseError(rc, "wise_select_working_set")
+
+
+_CACHE_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+_PROB_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+class Cache:
+    """A paged cache's device memory, checked once: pool [2 * n_layers,
+    n_pages, n_kv_heads, page, head_dim] in bf16 or fp16 (plane 2 l holds the
+    keys of layer l, 2 l + 1 its values), and int32 table [n_slots, max_pages],
+    lens [n_slots] and refs [n_pages]."""
+
+    def __init__(self, pool, table, lens, refs):
+        if pool is None or pool.dim() != 5 or pool.dtype not in _CACHE_DTYPES:
+            raise ValueError("pool must be bf16 or fp16 [2 * n_layers, n_pages, n_kv_heads, page, head_dim]")
+        planes, n_pages, n_kv_heads, page, head_dim = pool.shape
+        if planes < 2 or planes % 2:
+            raise ValueError("pool must have a plane of keys and one of values for each layer")
+        if table is None or table.dim() != 2:
+            raise ValueError("table must be int32 [n_slots, max_pages]")
+        n_slots, max_pages = table.shape
+        _check(pool, "pool", pool.shape, pool.dtype)
+        _check(table, "table", (n_slots, max_pages), torch.int32)
+        _check(lens, "lens", (n_slots,), torch.int32)
+        _check(refs, "refs", (n_pages,), torch.int32)
+        if not (pool.device == table.device == lens.device == refs.device):
+            raise ValueError("pool, table, lens and refs must be on one device")
+        self.pool, self.table, self.lens, self.refs = pool, table, lens, refs
+        self.n_pages, self.page, self.n_slots, self.max_pages = n_pages, page, n_slots, max_pages
+        self.n_layers, self.n_kv_heads, self.head_dim = planes // 2, n_kv_heads, head_dim
+        self.device, self.dtype = pool.device, pool.dtype
+        self.c = wise_cache_t(n_pages, page, n_slots, max_pages, planes // 2, n_kv_heads, head_dim,
+                              _CACHE_DTYPES[pool.dtype], pool.data_ptr(), table.data_ptr(), lens.data_ptr(),
+                              refs.data_ptr())
+        self.ref = ctypes.byref(self.c)
+
+
+def _list32(t, name, n, device):
+    """An int32 list of n entries on the cache's device (the checks of _check, in one pass)."""
+    if t is None or t.dtype is not torch.int32 or t.shape != (n,) or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape ({n},) on {device}")
+
+
+def _rows16(t, name, shape, cache):
+    if t is None or t.dtype is not cache.dtype or t.shape != shape or t.device != cache.device or \
+            not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {cache.dtype} tensor of shape {tuple(shape)} on {cache.device}")
+
+
+def _raw_stream(stream, device) -> int:
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+
+def wise_kv_workspace(cache: Cache, n: int) -> int:
+    """Bytes of workspace of wise_kv_extend for lists of n, and of wise_kv_compact."""
+    return int(load().wise_kv_workspace(cache.ref, int(n)))
+
+
+def _workspace(t, need, cache):
+    if t is None or t.device != cache.device or not t.is_contiguous() or t.numel() * t.element_size() < need:
+        raise ValueError(f"workspace must be a contiguous tensor of {need} bytes on {cache.device}")
+
+
+def wise_kv_fork(cache: Cache, src, dst, stream=None) -> None:
+    """The sequences in slots dst become forks of those in slots src (int32 [n] each)."""
+    n = src.shape[0]
+    _list32(src, "src", n, cache.device)
+    _list32(dst, "dst", n, cache.device)
+    rc = load().wise_kv_fork(cache.ref, src.data_ptr(), dst.data_ptr(), n, _raw_stream(stream, cache.device))
+    if rc != WISE_OK:
+        raise WiseError(rc, "wise_kv_fork")
+
+
+def wise_kv_extend(cache: Cache, slots, n_new, granted, workspace, stream=None) -> None:
+    """Grows the sequences in slots by n_new tokens; granted receives n_new, or 0 where pages ran out."""
+    n = slots.shape[0]
+    _list32(slots, "slots", n, cache.device)
+    _list32(n_new, "n_new", n, cache.device)
+    _list32(granted, "granted", n, cache.device)
+    _workspace(workspace, wise_kv_workspace(cache, n), cache)
+    rc = load().wise_kv_extend(cache.ref, slots.data_ptr(), n_new.data_ptr(), n, granted.data_ptr(),
+                               workspace.data_ptr(), _raw_stream(stream, cache.device))
+    if rc != WISE_OK:
+        raise WiseError(rc, "wise_kv_extend")
+
+
+def wise_kv_write(cache: Cache, layer: int, slots, n_new, K, V, stream=None) -> None:
+    """Stores one layer's new keys and values, [batch, n_kv_heads, q_len, head_dim] each, at the ends of the
+    sequences (n_new: what wise_kv_extend granted, or None for q_len tokens each)."""
+    if K is None or K.dim() != 4:
+        raise ValueError("K must be [batch, n_kv_heads, q_len, head_dim]")
+    batch, _, q_len, _ = K.shape
+    shape = (batch, cache.n_kv_heads, q_len, cache.head_dim)
+    _rows16(K, "K", shape, cache)
+    _rows16(V, "V", shape, cache)
+    _list32(slots, "slots", batch, cache.device)
+    if n_new is not None:
+        _list32(n_new, "n_new", batch, cache.device)
+    rc = load().wise_kv_write(cache.ref, int(layer), slots.data_ptr(), 0 if n_new is None else n_new.data_ptr(),
+                              batch, q_len, K.data_ptr(), V.data_ptr(), _raw_stream(stream, cache.device))
+    if rc != WISE_OK:
+        raise WiseError(rc, "wise_kv_write")
+
+
+def wise_kv_drop(cache: Cache, slots, n_drop, stream=None) -> None:
+    """Takes the last n_drop tokens off the sequences in slots (int32 [n] each); all of them frees a sequence."""
+    n = slots.shape[0]
+    _list32(slots, "slots", n, cache.device)
+    _list32(n_drop, "n_drop", n, cache.device)
+    rc = load().wise_kv_drop(cache.ref, slots.data_ptr(), n_drop.data_ptr(), n, _raw_stream(stream, cache.device))
+    if rc != WISE_OK:
+        raise WiseError(rc, "wise_kv_drop")
+
+
+def wise_kv_compact(cache: Cache, remap, n_live, workspace, stream=None) -> None:
+    """Moves the pages in use to the front of the pool; remap int32 [n_pages] and n_live int32 [1] are written."""
+    _list32(remap, "remap", cache.n_pages, cache.device)
+    _list32(n_live, "n_live", 1, cache.device)
+    _workspace(workspace, wise_kv_workspace(cache, 0), cache)
+    rc = load().wise_kv_compact(cache.ref, remap.data_ptr(), n_live.data_ptr(), workspace.data_ptr(),
+                                _raw_stream(stream, cache.device))
+    if rc != WISE_OK:
+        raise WiseError(rc, "wise_kv_compact")
+
+
+def prefix_shape(cache: Cache, Q, n_groups: int, scale: float = 0.0) -> wise_prefix_t:
+    """The attention's shape for Q [batch, n_heads, q_len, head_dim]."""
+    if Q is None or Q.dim() != 4:
+        raise ValueError("Q must be [batch, n_heads, q_len, head_dim]")
+    return wise_prefix_t(Q.shape[0], Q.shape[2], Q.shape[1], int(n_groups), float(scale))
+
+
+def wise_prefix_attn_workspace(cache: Cache, shape: wise_prefix_t) -> int:
+    """Bytes of workspace of wise_prefix_attn."""
+    return int(load().wise_prefix_attn_workspace(cache.ref, ctypes.byref(shape)))
+
+
+def wise_prefix_attn(cache: Cache, layer: int, Q, O, slots, n_new=None, group_start=None, prefix_lens=None,
+                     workspace=None, scale: float = 0.0, stream=None) -> None:
+    """Attention of new tokens Q over the cached sequences in slots, into O (both [batch, n_heads, q_len,
+    head_dim]); the requests of group g, group_start[g] .. group_start[g + 1] - 1, share their first
+    prefix_lens[g] tokens (both None: nothing is shared)."""
+    n_groups = 0 if prefix_lens is None else prefix_lens.shape[0]
+    sh = prefix_shape(cache, Q, n_groups, scale)
+    shape = (sh.batch, sh.n_heads, sh.q_len, cache.head_dim)
+    _rows16(Q, "Q", shape, cache)
+    _rows16(O, "O", shape, cache)
+    _list32(slots, "slots", sh.batch, cache.device)
+    if n_new is not None:
+        _list32(n_new, "n_new", sh.batch, cache.device)
+    if prefix_lens is not None:
+        _list32(prefix_lens, "prefix_lens", n_groups, cache.device)
+        _list32(group_start, "group_start", n_groups + 1, cache.device)
+    elif group_start is not None:
+        raise ValueError("group_start needs prefix_lens")
+    ws_bytes = 0
+    if workspace is not None:
+        _workspace(workspace, 0, cache)
+        ws_bytes = workspace.numel() * workspace.element_size()
+    rc = load().wise_prefix_attn(cache.ref, int(layer), ctypes.byref(sh), Q.data_ptr(), slots.data_ptr(),
+                                 0 if n_new is None else n_new.data_ptr(),
+                                 0 if prefix_lens is None else group_start.data_ptr(),
+                                 0 if prefix_lens is None else prefix_lens.data_ptr(), O.data_ptr(),
+                                 0 if workspace is None else workspace.data_ptr(), ws_bytes,
+                                 _raw_stream(stream, cache.device))
+    if rc != WISE_OK:
+        raise WiseError(rc, "wise_prefix_attn")
+
+
+def wise_verify_draft(p, q, draft, n_draft, u_accept, u_sample, accepted, tokens, stream=None) -> None:
+    """Verifies drafted tokens: p [batch, k + 1, vocab] and q [batch, k, vocab] (bf16, fp16 or fp32), draft int32
+    [batch, k], n_draft int32 [batch] or None, u_accept fp32 [batch, k], u_sample fp32 [batch] -> accepted int32
+    [batch], tokens int32 [batch, k + 1].  q, draft and u_accept may be None when k is 0."""
+    if p is None or p.dim() != 3 or p.dtype not in _PROB_DTYPES:
+        raise ValueError("p must be bf16, fp16 or fp32 [batch, k + 1, vocab]")
+    batch, k, vocab = p.shape[0], p.shape[1] - 1, p.shape[2]
+    if k < 0:
+        raise ValueError("p needs at least one row a request")
+    _check(p, "p", p.shape, p.dtype)
+    optional = k == 0
+    for t, name, shape, dtype in ((q, "q", (batch, k, vocab), p.dtype), (draft, "draft", (batch, k), torch.int32),
+                                  (u_accept, "u_accept", (batch, k), torch.float32),
+                                  (u_sample, "u_sample", (batch,), torch.float32),
+                                  (accepted, "accepted", (batch,), torch.int32),
+                                  (tokens, "tokens", (batch, k + 1), torch.int32),
+                                  (n_draft, "n_draft", (batch,), torch.int32)):
+        if t is None and (name == "n_draft" or (optional and name in ("q", "draft", "u_accept"))):
+            continue
+        if t is None or t.dtype is not dtype or t.shape != shape or t.device != p.device or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {p.device}")
+    rc = load().wise_verify_draft(batch, k, vocab, _PROB_DTYPES[p.dtype], p.data_ptr(),
+                                  0 if q is None else q.data_ptr(), 0 if draft is None else draft.data_ptr(),
+                                  0 if n_draft is None else n_draft.data_ptr(),
+                                  0 if u_accept is None else u_accept.data_ptr(), u_sample.data_ptr(),
+                                  accepted.data_ptr(), tokens.data_ptr(), _raw_stream(stream, p.device))
+    if rc != WISE_OK:
+        raise WiseError(rc, "wise_verify_draft")
 
 
 def wise_get_status(stream=None) -> int:
