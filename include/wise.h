@@ -383,7 +383,8 @@ int wise_kv_compact(const wise_cache_t* cache, int32_t* remap, int32_t* n_live, 
  * when n_groups is 0, are read by themselves.
  * Rows at or past lens in the pool may hold anything (infinities and NaN
  * included); the K and V of positions below lens must be finite.
- * Limits: batch <= 1024, q_len * n_heads / n_kv_heads <= 128.
+ * Limits: batch <= 1024, n_groups <= 256, q_len * n_heads / n_kv_heads <= 128,
+ * batch * n_kv_heads * (max_pages * page / 128 + 1) <= 2^30.
  * workspace: wise_prefix_attn_workspace bytes, 16-byte aligned, not shared
  * with a call that may run at the same time; needs no initial value. */
 typedef struct {

@@ -151,6 +151,9 @@ unsigned long long wait_limit_ns();
 // Tensor map of a 16-bit [outer, rows, cols] array with 64-column,
 // box_rows-row boxes in the 128-byte swizzle (defined in wise_api.cu).
 bool make_tile_map(CUtensorMap* map, const void* base, bool fp16, int cols, int rows, long long outer, int box_rows);
+// The same for [batch, heads, rows, cols], with boxes of box_batch x 1 x rows x 64.
+bool make_query_map(CUtensorMap* map, const void* base, bool fp16, int cols, int rows, int heads, int batch,
+                    int box_batch);
 
 // A paged cache as the kernels see it (wise_cache_t).
 struct CacheView {
@@ -196,7 +199,7 @@ struct PrefixParams {
 
 // Defined in prefix_attn.cu.
 size_t prefix_attn_workspace(const PrefixParams& p, int sm_count);
-cudaError_t launch_prefix_attn(const PrefixParams& p, void* workspace, int sm_count, cudaStream_t stream);
+int launch_prefix_attn(const PrefixParams& p, void* workspace, int sm_count, cudaStream_t stream);
 
 struct VerifyParams {
   int batch, k_max, vocab;

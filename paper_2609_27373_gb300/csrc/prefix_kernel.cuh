@@ -1,0 +1,875 @@
+// The attention kernel of prefix_attn.cuh, one instance per head dimension and
+// 16-bit type.
+//
+// Warp roles (384 threads):
+//   warps 0-3, 4-7  softmax of stream 0 and 1: thread t of a warpgroup owns
+//                   query row t (TMEM lane t).  Reads S from tensor memory,
+//                   masks, keeps the row's running maximum and sum in fp32,
+//                   writes P over S as 16-bit pairs, rescales O when the
+//                   maximum moved by more than 2^8, and at the end of a
+//                   segment stores (m, l) and O to the workspace.  Warps
+//                   without a query row only keep the barriers going.
+//   warp 8          producer: walks the CTA's segments, looks the pages up (a
+//                   lane per page) and issues the TMA loads of Q, K and V.
+//   warps 9, 10     one thread each: the MMAs of stream 0 and 1.
+// TMEM: S and P of stream w at column 128 w, O at 256 + 128 w.  The two
+// streams alternate on the tensor cores: one computes while the other is in
+// its softmax.  K and V tiles go through one ring in shared memory.
+//
+// Every wait is bounded; one that runs out sets the status word and an abort
+// flag, and every role unwinds.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "attn_common.cuh"
+#include "prefix_attn.cuh"
+#include "ptx.cuh"
+
+namespace wise {
+
+template <int D>
+struct PfxCfg {
+  static constexpr int kBoxes = (D + 63) / 64;
+  static constexpr int kTileBytes = kBoxes * 128 * 128;  // a Q, K or V tile
+  static constexpr int kSlots = 128 * 1024 / kTileBytes; // K/V ring: 128 KB
+  static constexpr int kThreads = 384;
+  static constexpr int kRegsSoftmax = 216;  // 256 * 216 + 128 * 72 <= 384 * 168 registers
+  static constexpr int kRegsOther = 72;
+  static constexpr int kRingBytes = (2 + kSlots) * kTileBytes;  // two Q tiles, then the ring
+  static constexpr int kMaxPlanBytes = 29 * 1024;
+  static constexpr int kSmemFixed = kRingBytes + 1024;  // and the plan behind
+  static_assert(kSmemFixed + kMaxPlanBytes + 2560 <= 227 * 1024, "shared memory");
+  static_assert(256 * kRegsSoftmax + 128 * kRegsOther <= kThreads * 168, "register split");
+};
+
+constexpr int kPfxSched = 8;  // schedule entries per stream
+constexpr int kPfxFirst = 1, kPfxLast = 2, kPfxEnd = 4;
+
+// Schedule entry {ring position of the K tile (V follows), first key position,
+// request | (requests - 1) << 10 | kind << 17 | flags << 19, segment slot}.
+__device__ __forceinline__ int pfx_pack(int req, int nreq, int kind, int flags) {
+  return req | (nreq - 1) << 10 | kind << 17 | flags << 19;
+}
+
+template <int NS>
+struct PfxShared {
+  uint64_t kv_full[NS], kv_empty[NS];  // empty: one arrival per stream
+  uint64_t sched_full[2][kPfxSched], sched_empty[2][kPfxSched];  // empty: the issuer and 4 warps
+  uint64_t q_full[2], q_free[2];
+  uint64_t s_full[2];  // S written
+  uint64_t p_full[2];  // P written (and S read, and O read where a segment ended): 4 warps
+  uint64_t o_full[2];  // P V completed
+  uint64_t done[2];
+  int4 sched[2][kPfxSched];
+  uint32_t tmem_base;
+  int abort;
+};
+
+// ---------------------------------------------------------------------- plan
+// All threads of the CTA; `plan` in shared memory.
+__device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bool report) {
+  const CacheView& c = p.cache;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
+  int bad = 0;
+  for (int r = tid; r < p.batch; r += blockDim.x) {
+    const int s = p.slots[r];
+    const int add = p.n_new ? p.n_new[r] : p.q_len;
+    int len = 0;
+    if (s >= 0) {
+      len = s < c.n_slots ? c.lens[s] : -1;
+      if (len < 0 || len > c.max_len || add < 0 || add > p.q_len) {
+        bad = 1;
+        len = 0;
+      }
+    }
+    plan.len[r] = add > 0 ? len : 0;
+    plan.add[r] = add > 0 ? add : 0;
+    plan.lo[r] = 0;
+    plan.group[r] = -1;
+  }
+  int bad_groups = 0;
+  for (int g = tid; g <= p.n_groups; g += blockDim.x) {
+    if (p.n_groups == 0) break;
+    const int a = p.group_start[g];
+    if (a < 0 || a > p.batch || (g < p.n_groups && a > p.group_start[g + 1])) bad_groups = 1;
+    plan.start[g] = a;
+  }
+  if (report && (bad | bad_groups)) atomicOr(c.status, kStatusBadCache);
+  const bool grouped = !__syncthreads_or(bad_groups);
+  for (int g = warp; g < p.n_groups; g += n_warps) {
+    const int a = plan.start[g], e = plan.start[g + 1];
+    int shortest = INT_MAX, active = 0, lead = INT_MAX;
+    if (grouped) {
+      for (int r = a + lane; r < e; r += 32) {
+        const int len = plan.len[r];
+        if (len > 0) {
+          shortest = min(shortest, len);
+          lead = min(lead, r);
+          ++active;
+        }
+      }
+    }
+    shortest = __reduce_min_sync(0xffffffffu, shortest);
+    active = __reduce_add_sync(0xffffffffu, active);
+    lead = __reduce_min_sync(0xffffffffu, lead);
+    int shared = 0;
+    if (active > 1) shared = max(0, min(p.prefix_lens[g], shortest)) / c.page * c.page;
+    const int tiles = (shared + kPfxKeys - 1) / kPfxKeys;
+    if (lane == 0) {
+      plan.tiles[g] = tiles;
+      plan.lead[g] = lead;
+    }
+    if (shared > 0) {
+      for (int r = a + lane; r < e; r += 32) {
+        plan.lo[r] = shared;
+        plan.group[r] = g;
+      }
+    }
+  }
+  __syncthreads();
+  if (warp == 0) {
+    int before = 0;
+    for (int r0 = 0; r0 < p.batch; r0 += 32) {
+      const int r = r0 + lane;
+      const int t = r < p.batch ? max(0, plan.len[r] - plan.lo[r] + kPfxKeys - 1) / kPfxKeys : 0;
+      int v = t;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += u;
+      }
+      if (r < p.batch) plan.cum[r] = before + v - t;
+      before += __shfl_sync(0xffffffffu, v, 31);
+    }
+    if (lane == 0) plan.cum[p.batch] = before;
+  } else if (warp == 1) {
+    int b[4] = {0, 0, 0, 0};  // pair tiles, pair items, single tiles, single items
+    for (int g0 = 0; g0 < p.n_groups; g0 += 32) {
+      const int g = g0 + lane;
+      int own[4] = {0, 0, 0, 0}, v[4];
+      if (g < p.n_groups && plan.tiles[g] > 0) {
+        const int row_tiles = (plan.start[g + 1] - plan.start[g] + p.per_tile - 1) / p.per_tile;
+        own[1] = row_tiles / 2;
+        own[3] = row_tiles & 1;
+        own[0] = own[1] * plan.tiles[g] * c.n_kv_heads;
+        own[2] = own[3] * plan.tiles[g] * c.n_kv_heads;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[k] = own[k];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int u = __shfl_up_sync(0xffffffffu, v[k], o);
+          if (lane >= o) v[k] += u;
+        }
+      }
+      if (g < p.n_groups) {
+        plan.pair_base[g] = b[0] + v[0] - own[0];
+        plan.pair_item[g] = b[1] + v[1] - own[1];
+        plan.single_base[g] = b[2] + v[2] - own[2];
+        plan.single_item[g] = b[3] + v[3] - own[3];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) b[k] += __shfl_sync(0xffffffffu, v[k], 31);
+    }
+    if (lane == 0) {
+      plan.pair_base[p.n_groups] = b[0];
+      plan.single_base[p.n_groups] = b[2];
+    }
+  }
+  __syncthreads();
+  if (tid == 0) {
+    PfxTotals t = {};
+    t.pair_tiles = plan.pair_base[p.n_groups];
+    t.pair_runs = min((int)gridDim.x, t.pair_tiles);
+    t.single_tiles = plan.single_base[p.n_groups];
+    t.line_tiles = t.single_tiles + plan.cum[p.batch] * c.n_kv_heads;
+    t.line_runs = min(2 * (int)gridDim.x, t.line_tiles);
+    t.grouped = grouped;
+    *plan.t = t;
+  }
+  __syncthreads();
+}
+
+// Largest g with base[g] <= x (base ascending, base[0] <= x < base[n]).
+__device__ __forceinline__ int pfx_find(const int* base, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (base[mid] <= x)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+// A segment: key tiles t .. t_end - 1 of an item.
+struct PfxSeg {
+  int kind, req, nreq, nreq2;  // requests of the (first) tile, and of the pair's second
+  int kvh, table_row;          // kv head, cache slot whose pages are read
+  int pos, end;                // position of the first key of tile t; one past the item's keys
+  int left;                    // tiles left
+  int slot;                    // workspace slot
+};
+
+// The segment that starts at tile x of a line and ends at x_end or with its item.
+__device__ __forceinline__ PfxSeg pfx_segment(const PfxParams& p, const PfxPlan& plan, bool pairs, int x, int x_end,
+                                              int run) {
+  PfxSeg s;
+  const int kv = p.cache.n_kv_heads;
+  const int single_tiles = plan.t->single_tiles;
+  int tiles, t;
+  if (pairs || x < single_tiles) {
+    const int* base = pairs ? plan.pair_base : plan.single_base;
+    const int g = pfx_find(base, p.n_groups, x);
+    tiles = plan.tiles[g];
+    const int y = x - base[g];
+    const int it = y / tiles;
+    t = y - it * tiles;
+    const int a = plan.start[g], members = plan.start[g + 1] - a;
+    const int row_tiles = (members + p.per_tile - 1) / p.per_tile;
+    if (pairs) {
+      // kv head outermost: the pairs of one kv head read the same keys at about the same time.
+      const int n_pairs = row_tiles / 2;
+      s.kvh = it / n_pairs;
+      const int pair = it - s.kvh * n_pairs;
+      s.kind = kPfxPair;
+      s.req = a + 2 * pair * p.per_tile;
+      s.slot = 2 * (plan.pair_item[g] * kv + it + run);
+      s.nreq = p.per_tile;
+      s.nreq2 = min(p.per_tile, members - (2 * pair + 1) * p.per_tile);
+    } else {
+      s.kvh = it;
+      s.kind = kPfxSingle;
+      s.req = a + (row_tiles - 1) * p.per_tile;
+      s.slot = plan.single_item[g] * kv + it + run;
+      s.nreq = members - (row_tiles - 1) * p.per_tile;
+    }
+    const int lead = plan.lead[g];
+    s.table_row = p.slots[lead];
+    s.end = plan.lo[lead];
+    s.pos = t * kPfxKeys;
+  } else {
+    const int y = x - single_tiles;
+    // cum[r] * kv <= y < cum[r + 1] * kv
+    const int r = pfx_find(plan.cum, p.batch, y / kv);
+    tiles = plan.cum[r + 1] - plan.cum[r];
+    const int z = y - plan.cum[r] * kv;
+    s.kvh = z / tiles;
+    t = z - s.kvh * tiles;
+    s.kind = kPfxOwn;
+    s.req = r;
+    s.nreq = 1;
+    s.table_row = p.slots[r];
+    s.end = plan.len[r];
+    s.pos = plan.lo[r] + t * kPfxKeys;
+    s.slot = r * kv + s.kvh + run;
+  }
+  s.left = min(tiles - t, x_end - x);
+  return s;
+}
+
+// ------------------------------------------------------------------ producer
+// The whole warp 8.
+template <int D>
+__device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, const CUtensorMap* mapQ,
+                             const CUtensorMap* mapQ1, const PfxParams& p, const PfxPlan& plan, uint8_t* q_tiles,
+                             uint8_t* ring, PfxShared<PfxCfg<D>::kSlots>& sb) {
+  using C = PfxCfg<D>;
+  constexpr int NS = C::kSlots;
+  const CacheView& c = p.cache;
+  const int lane = threadIdx.x & 31;
+  volatile int* abort = &sb.abort;
+  int n_kv = 0;             // ring positions used
+  int n_ent[2] = {0, 0};    // schedule entries per stream
+  int n_q[2] = {0, 0};      // Q tiles loaded per stream
+  int bad = 0;
+  bool ok = true;
+  const int per_tile_pages = kPfxKeys / c.page;
+
+  auto emit = [&](int w, int4 ent) {
+    const int slot = n_ent[w] % kPfxSched;
+    if (n_ent[w] >= kPfxSched && !warp_wait(&sb.sched_empty[w][slot], ((n_ent[w] / kPfxSched) - 1) & 1, abort, p.wait_ns))
+      return false;
+    if (lane == 0) {
+      sb.sched[w][slot] = ent;
+      mbar_arrive(&sb.sched_full[w][slot]);
+    }
+    ++n_ent[w];
+    return true;
+  };
+  // The page of lane i of a tile (z coordinate of its kv head; out of range
+  // for a faulty id, which reads zeros), -1 past the item's end.
+  auto page_of = [&](const PfxSeg& s) -> int {
+    const int at = s.pos + lane * c.page;
+    if (lane >= per_tile_pages || at >= s.end) return -1;
+    const int page = __ldg(c.table + (size_t)s.table_row * c.max_pages + at / c.page);
+    if (page < 0 || page >= c.n_pages) {
+      bad = 1;
+      return c.n_pages * c.n_kv_heads;
+    }
+    return page * c.n_kv_heads + s.kvh;
+  };
+  auto load_tile = [&](const CUtensorMap* map, int z) -> bool {
+    const int slot = n_kv % NS;
+    if (n_kv >= NS && !warp_wait(&sb.kv_empty[slot], ((n_kv / NS) - 1) & 1, abort, p.wait_ns)) return false;
+    const int n = __popc(__ballot_sync(0xffffffffu, z >= 0));
+    if (lane == 0) mbar_arrive_expect_tx(&sb.kv_full[slot], n * c.page * 128 * C::kBoxes);
+    __syncwarp();
+    if (z >= 0) {
+      uint8_t* dst = ring + slot * C::kTileBytes + lane * c.page * 128;
+      for (int b = 0; b < C::kBoxes; ++b) tma_load_3d(dst + b * 128 * 128, map, &sb.kv_full[slot], 64 * b, 0, z);
+    }
+    ++n_kv;
+    return true;
+  };
+  auto load_q = [&](int w, int req, const PfxSeg& s) -> bool {
+    if (n_q[w] >= 1 && !warp_wait(&sb.q_free[w], (n_q[w] - 1) & 1, abort, p.wait_ns)) return false;
+    if (lane == 0) {
+      const int rows = s.kind == kPfxOwn ? p.rows : p.rows * p.per_tile;
+      mbar_arrive_expect_tx(&sb.q_full[w], rows * 128 * C::kBoxes);
+      for (int b = 0; b < C::kBoxes; ++b)
+        tma_load_4d(q_tiles + w * C::kTileBytes + b * 128 * 128, s.kind == kPfxOwn ? mapQ1 : mapQ, &sb.q_full[w],
+                    64 * b, 0, s.kvh, req);
+    }
+    ++n_q[w];
+    return true;
+  };
+  // One tile of a segment for the streams in `mask`.
+  auto tile = [&](const PfxSeg& s, bool first, int z, int w0, int w1) -> bool {
+    const int flags = (first ? kPfxFirst : 0) | (s.left == 1 ? kPfxLast : 0);
+    const int n = n_kv;
+    for (int w = w0; w <= w1; ++w) {
+      const bool second = s.kind == kPfxPair && w == 1;
+      const int req = second ? s.req + p.per_tile : s.req;
+      if (!emit(w, make_int4(n, s.pos, pfx_pack(req, second ? s.nreq2 : s.nreq, s.kind, flags), s.slot + second)))
+        return false;
+    }
+    if (!load_tile(mapK, z)) return false;
+    if (first) {
+      for (int w = w0; w <= w1; ++w)
+        if (!load_q(w, s.kind == kPfxPair && w == 1 ? s.req + p.per_tile : s.req, s)) return false;
+    }
+    return load_tile(mapV, z);
+  };
+
+  const PfxTotals t = *plan.t;
+  const int G = gridDim.x, cta = blockIdx.x;
+  // Pair items: this CTA's run, both streams.
+  if (cta < t.pair_runs) {
+    int x = pfx_cut(cta, t.pair_tiles, t.pair_runs);
+    const int x_end = pfx_cut(cta + 1, t.pair_tiles, t.pair_runs);
+    while (ok && x < x_end) {
+      PfxSeg s = pfx_segment(p, plan, true, x, x_end, cta);
+      x += s.left;
+      int z = page_of(s);
+      for (bool first = true; ok && s.left > 0; first = false) {
+        const int z_now = z;
+        PfxSeg next = s;
+        next.pos += kPfxKeys;
+        if (s.left > 1) z = page_of(next);  // looked up one tile ahead
+        ok = tile(s, first, z_now, 0, 1);
+        next.left -= 1;
+        s = next;
+      }
+    }
+  }
+  // The other items: one run per stream, tile by tile in turn.  Runs start
+  // at the CTA after the last one with pair items, so that small problems
+  // spread out.
+  int xs[2], xe[2];
+  PfxSeg seg[2];
+  int zs[2];
+  bool first[2] = {true, true};
+  const int shift = t.pair_runs % G;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const int run = (cta - shift + G) % G + w * G;
+    xs[w] = xe[w] = 0;
+    seg[w].left = 0;
+    if (run < t.line_runs) {
+      xs[w] = pfx_cut(run, t.line_tiles, t.line_runs);
+      xe[w] = pfx_cut(run + 1, t.line_tiles, t.line_runs);
+    }
+  }
+  while (ok && (seg[0].left > 0 || seg[1].left > 0 || xs[0] < xe[0] || xs[1] < xe[1])) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      if (!ok) break;
+      if (seg[w].left == 0) {
+        if (xs[w] >= xe[w]) continue;
+        const int run = (cta - shift + G) % G + w * G;
+        seg[w] = pfx_segment(p, plan, false, xs[w], xe[w], run);
+        xs[w] += seg[w].left;
+        zs[w] = page_of(seg[w]);
+        first[w] = true;
+      }
+      const int z_now = zs[w];
+      PfxSeg next = seg[w];
+      next.pos += kPfxKeys;
+      if (seg[w].left > 1) zs[w] = page_of(next);
+      ok = tile(seg[w], first[w], z_now, w, w);
+      first[w] = false;
+      next.left -= 1;
+      seg[w] = next;
+    }
+  }
+  for (int w = 0; w < 2 && ok; ++w) ok = emit(w, make_int4(0, 0, pfx_pack(0, 1, 0, kPfxEnd), 0));
+  if (bad) atomicOr(c.status, kStatusBadCache);
+  if (!ok) {
+    if (lane == 0) {
+      *reinterpret_cast<volatile int*>(&sb.abort) = 1;
+      atomicOr(c.status, kStatusTimeout);
+      // Copies already issued land before the CTA's shared memory is released.
+      int never = 0;
+      for (int n = max(0, n_kv - NS); n < n_kv; ++n) mbar_wait(&sb.kv_full[n % NS], (n / NS) & 1, &never);
+      for (int w = 0; w < 2; ++w)
+        if (n_q[w] > 0) mbar_wait(&sb.q_full[w], (n_q[w] - 1) & 1, &never);
+    }
+    __syncwarp();
+  }
+}
+
+// --------------------------------------------------------------- MMA issuers
+// One thread per stream.
+template <int D, bool FP16>
+__device__ void pfx_mma(const PfxParams& p, int w, uint32_t tmem, uint8_t* q_tiles, uint8_t* ring,
+                        PfxShared<PfxCfg<D>::kSlots>& sb) {
+  using C = PfxCfg<D>;
+  constexpr int NS = C::kSlots;
+  volatile int* abort = &sb.abort;
+  constexpr uint32_t fmt = FP16 ? ~((1u << 7) | (1u << 10)) : ~0u;  // operand type 0: fp16, 1: bf16
+  constexpr uint32_t idesc_s = idesc_bf16_f32(128, kPfxKeys, false, false) & fmt;
+  constexpr uint32_t idesc_o = idesc_bf16_f32(128, D, false, true) & fmt;
+  const uint32_t s_col = tmem + w * 128, o_col = tmem + 256 + w * 128;
+  int j = 0, nq = 0;
+  bool ok = true;
+  for (;; ++j) {
+    const int e = j % kPfxSched;
+    if (!mbar_wait(&sb.sched_full[w][e], (j / kPfxSched) & 1, abort, p.wait_ns)) {
+      ok = false;
+      break;
+    }
+    const int4 ent = sb.sched[w][e];
+    mbar_arrive(&sb.sched_empty[w][e]);
+    const int flags = ent.z >> 19;
+    if (flags & kPfxEnd) break;
+    const bool pair = ((ent.z >> 17) & 3) == kPfxPair;
+    if ((flags & kPfxFirst) && !mbar_wait(&sb.q_full[w], nq++ & 1, abort, p.wait_ns)) {
+      ok = false;
+      break;
+    }
+    const int k_slot = ent.x % NS, v_slot = (ent.x + 1) % NS;
+    if (!mbar_wait(&sb.kv_full[k_slot], (ent.x / NS) & 1, abort, p.wait_ns)) {
+      ok = false;
+      break;
+    }
+    tc_fence_after_sync();
+    const uint64_t q0 = smem_desc_sw128(smem_u32(q_tiles + w * C::kTileBytes), 16, 1024);
+    const uint64_t k0 = smem_desc_sw128(smem_u32(ring + k_slot * C::kTileBytes), 16, 1024);
+#pragma unroll 1
+    for (int kk = 0; kk < D / 16; ++kk) {
+      const uint32_t off = ((kk >> 2) * (128 * 128) + (kk & 3) * 32) >> 4;
+      umma_bf16_ss(s_col, q0 + off, k0 + off, idesc_s, kk > 0 ? 1u : 0u);
+    }
+    umma_commit(&sb.s_full[w]);
+    // A slot is empty after two arrivals: one of each stream for a pair's
+    // tile, both from this one otherwise.
+    umma_commit(&sb.kv_empty[k_slot]);
+    if (!pair) umma_commit(&sb.kv_empty[k_slot]);
+    if (flags & kPfxLast) umma_commit(&sb.q_free[w]);
+    if (!mbar_wait(&sb.kv_full[v_slot], ((ent.x + 1) / NS) & 1, abort, p.wait_ns) ||
+        !mbar_wait(&sb.p_full[w], j & 1, abort, p.wait_ns)) {
+      ok = false;
+      break;
+    }
+    tc_fence_after_sync();
+    const uint64_t v0 = smem_desc_sw128(smem_u32(ring + v_slot * C::kTileBytes), kPfxKeys * 128, 1024);
+#pragma unroll 1
+    for (int kk = 0; kk < kPfxKeys / 16; ++kk)
+      umma_bf16_ts(o_col, s_col + kk * 8, v0 + ((kk * 2048) >> 4), idesc_o,
+                   ((flags & kPfxFirst) && kk == 0) ? 0u : 1u);
+    umma_commit(&sb.o_full[w]);
+    umma_commit(&sb.kv_empty[v_slot]);
+    if (!pair) umma_commit(&sb.kv_empty[v_slot]);
+    // The next S overwrites P, which this product reads.
+    if (!mbar_wait(&sb.o_full[w], j & 1, abort, p.wait_ns)) {
+      ok = false;
+      break;
+    }
+  }
+  if (!ok) {
+    *reinterpret_cast<volatile int*>(&sb.abort) = 1;
+    atomicOr(p.cache.status, kStatusTimeout);
+  }
+  // Every MMA and commit of this thread completes before TMEM is released.
+  umma_commit(&sb.done[w]);
+  int never = 0;
+  mbar_wait(&sb.done[w], 0, &never);
+}
+
+// ------------------------------------------------------------------- softmax
+template <bool FP16>
+__device__ __forceinline__ uint32_t pack_16x2(float lo, float hi) {
+  if constexpr (FP16) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+  } else {
+    return pack_bf16x2(lo, hi);
+  }
+}
+
+template <int D, bool FP16>
+__device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint32_t tmem, uint8_t* ring,
+                            PfxShared<PfxCfg<D>::kSlots>& sb) {
+  using C = PfxCfg<D>;
+  constexpr int NS = C::kSlots;
+  constexpr float kRescaleThreshold = 8.0f;  // log2 units: P stays <= 256
+  volatile int* abort = &sb.abort;
+  const int r = threadIdx.x & 127, wq = r >> 5, lane = r & 31;
+  const uint32_t lane_tmem = tmem + ((uint32_t)(wq * 32) << 16);
+  const uint32_t s_col = w * 128, o_col = 256 + w * 128;
+  bool ok = true;
+  int limit = 0, end = 0;       // keys the row may see; one past the item's keys
+  bool row_on = false, warp_on = false;
+  float m = -INFINITY, l = 0.0f;
+  for (int j = 0;; ++j) {
+    const int e = j % kPfxSched;
+    if (!warp_wait(&sb.sched_full[w][e], (j / kPfxSched) & 1, abort, p.wait_ns)) {
+      ok = false;
+      break;
+    }
+    const int4 ent = sb.sched[w][e];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.sched_empty[w][e]);
+    const int flags = ent.z >> 19, kind = (ent.z >> 17) & 3;
+    if (flags & kPfxEnd) break;
+    if (flags & kPfxFirst) {
+      const int req0 = ent.z & 1023, nreq = ((ent.z >> 10) & 127) + 1;
+      const int of = r / p.rows, i = r % p.rows % p.q_len;
+      row_on = of < nreq;
+      limit = 0;
+      if (row_on) {
+        const int req = req0 + of, add = plan.add[req];
+        limit = i < add ? max(0, plan.len[req] - add + i + 1) : 0;
+      }
+      end = kind == kPfxOwn ? plan.len[req0] : plan.lo[req0];
+      warp_on = __any_sync(0xffffffffu, row_on);
+      m = -INFINITY;
+      l = 0.0f;
+    }
+    if (!warp_wait(&sb.s_full[w], j & 1, abort, p.wait_ns)) {
+      ok = false;
+      break;
+    }
+    tc_fence_after_sync();
+    if (warp_on) {
+      float s[kPfxKeys];
+      load_s_row<128>(lane_tmem + s_col, s, 1u, min(limit, end) - ent.y - 1);
+      const float m_tile = row_max(s) * p.scale_log2;
+      const float m_new = (m_tile > m + kRescaleThreshold) ? m_tile : m;
+      const bool rescale = m_new != m && m != -INFINITY;
+      const float f = rescale ? ex2_approx(m - m_new) : 1.0f;
+      const float sum = exp2_scaled(s, p.scale_log2, m_new == -INFINITY ? 0.0f : m_new);
+      l = l * f + sum;
+      m = m_new;
+#pragma unroll
+      for (int c = 0; c < kPfxKeys / 32; ++c) {
+        uint32_t q[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) q[k] = pack_16x2<FP16>(s[32 * c + 2 * k], s[32 * c + 2 * k + 1]);
+        tmem_st_32x32b_x16(lane_tmem + s_col + 16 * c, q);
+      }
+      // S of this tile was issued after the previous P V had completed, so O
+      // is at rest here.
+      if (__any_sync(0xffffffffu, rescale)) {
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          uint32_t v[16];
+          tmem_ld_32x32b_x16(lane_tmem + o_col + 16 * c, v);
+          tmem_ld_wait(v);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
+          tmem_st_32x32b_x16(lane_tmem + o_col + 16 * c, v);
+        }
+      }
+      tmem_st_wait();
+    }
+    const int valid = end - ent.y;
+    if (valid < kPfxKeys) {
+      // The item ends in this tile: rows of V past its end are whatever the
+      // pool or an earlier tile left there, and 0 * NaN would spread.
+      if (!warp_wait(&sb.kv_full[(ent.x + 1) % NS], ((ent.x + 1) / NS) & 1, abort, p.wait_ns)) {
+        ok = false;
+        break;
+      }
+      if (r >= valid) {
+        const uint32_t row = smem_u32(ring + ((ent.x + 1) % NS) * C::kTileBytes + r * 128);
+        for (int b = 0; b < C::kBoxes; ++b)
+          for (int k = 0; k < 8; ++k) st_shared_v4(row + b * 128 * 128 + k * 16, 0u, 0u, 0u, 0u);
+        fence_proxy_async_smem();
+      }
+    }
+    tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.p_full[w]);
+    if (flags & kPfxLast) {
+      if (!warp_wait(&sb.o_full[w], j & 1, abort, p.wait_ns)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after_sync();
+      if (warp_on) {
+        float o[D];
+        tmem_load_row<D>(lane_tmem + o_col, o);
+        tc_fence_before_sync();
+        if (row_on) {
+          const int rows = kind == kPfxOwn ? p.rows : kPfxRows;
+          const float2 v = make_float2(m, l);
+          float2* ml = kind == kPfxOwn ? p.work.ml[0] : kind == kPfxSingle ? p.work.ml[1] : p.work.ml[2];
+          float4* O = kind == kPfxOwn ? p.work.O[0] : kind == kPfxSingle ? p.work.O[1] : p.work.O[2];
+          ml[(size_t)ent.w * rows + r] = v;
+          float4* out = O + (size_t)ent.w * rows * (D / 4) + r;
+#pragma unroll
+          for (int c = 0; c < D / 4; ++c)
+            out[c * rows] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+        }
+      }
+    }
+  }
+  tmem_st_wait();
+  if (!ok && lane == 0) {
+    *reinterpret_cast<volatile int*>(&sb.abort) = 1;
+    atomicOr(p.cache.status, kStatusTimeout);
+  }
+}
+
+// -------------------------------------------------------------------- kernel
+template <int D, bool FP16>
+__global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
+    prefix_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
+                  const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapQ1,
+                  const __grid_constant__ PfxParams p) {
+  using C = PfxCfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* q_tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* ring = q_tiles + 2 * C::kTileBytes;
+  const PfxPlan plan = pfx_plan(reinterpret_cast<int*>(q_tiles + C::kRingBytes), p.batch, p.n_groups);
+  __shared__ PfxShared<C::kSlots> sb;
+  static_assert(sizeof(sb) <= 2048, "static shared memory");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    sb.abort = 0;
+    for (int i = 0; i < C::kSlots; ++i) {
+      mbar_init(&sb.kv_full[i], 1);
+      mbar_init(&sb.kv_empty[i], 2);
+    }
+    for (int w = 0; w < 2; ++w) {
+      for (int i = 0; i < kPfxSched; ++i) {
+        mbar_init(&sb.sched_full[w][i], 1);
+        mbar_init(&sb.sched_empty[w][i], 5);
+      }
+      mbar_init(&sb.q_full[w], 1);
+      mbar_init(&sb.q_free[w], 1);
+      mbar_init(&sb.s_full[w], 1);
+      mbar_init(&sb.p_full[w], 4);
+      mbar_init(&sb.o_full[w], 1);
+      mbar_init(&sb.done[w], 1);
+    }
+    fence_mbar_init();
+    tma_prefetch_map(&mapK);
+    tma_prefetch_map(&mapV);
+    tma_prefetch_map(&mapQ);
+    tma_prefetch_map(&mapQ1);
+  }
+  if (warp == 9) {
+    tmem_alloc(&sb.tmem_base, 512);
+    tmem_relinquish();
+  }
+  // Everything above may overlap the previous kernel of the stream.
+  griddep_wait();
+  tc_fence_before_sync();
+  pfx_make_plan(p, plan, blockIdx.x == 0);  // ends with a barrier
+  tc_fence_after_sync();
+  const uint32_t tmem = sb.tmem_base;
+  if (blockIdx.x == 0) {
+    const int* from = reinterpret_cast<const int*>(plan.t);
+    for (int i = threadIdx.x; i < pfx_plan_ints(p.batch, p.n_groups); i += C::kThreads) p.work.plan[i] = from[i];
+  }
+  if (threadIdx.x == 0) griddep_launch_dependents();  // the merge waits for this grid's end
+
+  if (warp < 8) {
+    warpgroup_reg_inc<C::kRegsSoftmax>();
+    pfx_softmax<D, FP16>(p, plan, warp >> 2, tmem, ring, sb);
+  } else {
+    warpgroup_reg_dec<C::kRegsOther>();
+    if (warp == 8) {
+      pfx_producer<D>(&mapK, &mapV, &mapQ, &mapQ1, p, plan, q_tiles, ring, sb);
+    } else if (warp <= 10) {
+      if (lane == 0) pfx_mma<D, FP16>(p, warp - 9, tmem, q_tiles, ring, sb);
+    }
+  }
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 9) {
+    __syncwarp();
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// --------------------------------------------------------------------- merge
+// One block per (request, kv head): joins the partial results of its rows.
+constexpr int kMergeThreads = 256;
+constexpr int kMergeChunk = 16;  // segments whose weights sit in shared memory at a time
+
+template <int D, bool FP16>
+__global__ void __launch_bounds__(kMergeThreads) prefix_merge_kernel(const PfxParams p, uint16_t* O) {
+  __shared__ float2 stat[kPfxRows];                 // per row M and 1 / L
+  __shared__ float weight[kMergeChunk][kPfxRows];
+  __shared__ float4 sums[kMergeThreads];
+  griddep_wait();
+  const PfxPlan plan = pfx_plan(p.work.plan, p.batch, p.n_groups);
+  const int kv = p.cache.n_kv_heads;
+  const int req = blockIdx.x / kv, kvh = blockIdx.x % kv;
+  const int R = p.rows, tid = threadIdx.x;
+  const PfxTotals t = *plan.t;
+  // Segments of the shared prefix (first), then of the request's own keys.
+  int n_pre = 0, n_own = 0, pre_slot = 0, pre_step = 0, own_slot = 0, row0 = 0, kind = kPfxSingle;
+  const int g = plan.group[req];
+  if (plan.add[req] > 0 && plan.len[req] > 0) {
+    if (g >= 0) {
+      const int at = req - plan.start[g], tile = at / p.per_tile;
+      const int row_tiles = (plan.start[g + 1] - plan.start[g] + p.per_tile - 1) / p.per_tile;
+      const int tiles = plan.tiles[g], n_pairs = row_tiles / 2;
+      row0 = (at - tile * p.per_tile) * R;
+      if (tile < 2 * n_pairs) {
+        kind = kPfxPair;
+        const int it = kvh * n_pairs + tile / 2;
+        const int x = plan.pair_base[g] + it * tiles;
+        const int k0 = pfx_run_of(x, t.pair_tiles, t.pair_runs), k1 = pfx_run_of(x + tiles - 1, t.pair_tiles, t.pair_runs);
+        pre_slot = 2 * (plan.pair_item[g] * kv + it + k0) + (tile & 1);
+        pre_step = 2;
+        n_pre = k1 - k0 + 1;
+      } else {
+        const int x = plan.single_base[g] + kvh * tiles;
+        const int k0 = pfx_run_of(x, t.line_tiles, t.line_runs), k1 = pfx_run_of(x + tiles - 1, t.line_tiles, t.line_runs);
+        pre_slot = plan.single_item[g] * kv + kvh + k0;
+        pre_step = 1;
+        n_pre = k1 - k0 + 1;
+      }
+    }
+    const int tiles = plan.cum[req + 1] - plan.cum[req];
+    if (tiles > 0) {
+      const int x = t.single_tiles + plan.cum[req] * kv + kvh * tiles;
+      const int k0 = pfx_run_of(x, t.line_tiles, t.line_runs), k1 = pfx_run_of(x + tiles - 1, t.line_tiles, t.line_runs);
+      own_slot = req * kv + kvh + k0;
+      n_own = k1 - k0 + 1;
+    }
+  }
+  const int n = n_pre + n_own;
+  auto ml_at = [&](int s, int row) -> float2 {
+    return s < n_pre ? p.work.ml[kind][(size_t)(pre_slot + s * pre_step) * kPfxRows + row0 + row]
+                     : p.work.ml[kPfxOwn][(size_t)(own_slot + s - n_pre) * R + row];
+  };
+  for (int row = tid; row < R; row += kMergeThreads) {
+    float m = -INFINITY, l = 0.0f;
+    for (int s = 0; s < n; ++s) m = fmaxf(m, ml_at(s, row).x);
+    for (int s = 0; s < n; ++s) {
+      const float2 v = ml_at(s, row);
+      if (v.y > 0.0f) l += v.y * ex2_approx(v.x - m);
+    }
+    stat[row] = make_float2(m, l > 0.0f ? 1.0f / l : 0.0f);
+  }
+  __syncthreads();
+  // Elements are 4 columns of a row.  With fewer elements than threads,
+  // threads share an element, each taking every `parts`-th segment.
+  const int n_el = R * (D / 4);
+  const int parts = n_el >= kMergeThreads ? 1 : kMergeThreads / n_el;
+  uint16_t* out = O + ((size_t)req * p.n_heads + (size_t)kvh * p.group) * p.q_len * D;
+  for (int e0 = 0; e0 < n_el; e0 += kMergeThreads) {
+    const int e = parts > 1 ? tid % n_el : e0 + tid;
+    const int part = parts > 1 ? tid / n_el : 0;
+    const bool on = e < n_el && part < parts;
+    const int row = e % R, c = e / R;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int s0 = 0; s0 < n; s0 += kMergeChunk) {
+      const int ns = min(kMergeChunk, n - s0);
+      __syncthreads();
+      for (int k = tid; k < ns * R; k += kMergeThreads) {
+        const float2 v = ml_at(s0 + k / R, k % R);
+        const float2 st = stat[k % R];
+        weight[k / R][k % R] = v.y > 0.0f ? ex2_approx(v.x - st.x) * st.y : 0.0f;
+      }
+      __syncthreads();
+      if (on) {
+        for (int k = part; k < ns; k += parts) {
+          const int s = s0 + k;
+          const float wgt = weight[k][row];
+          if (wgt == 0.0f) continue;  // nothing was seen, or O was not written for it
+          const float4 v =
+              s < n_pre ? p.work.O[kind][((size_t)(pre_slot + s * pre_step) * (D / 4) + c) * kPfxRows + row0 + row]
+                        : p.work.O[kPfxOwn][((size_t)(own_slot + s - n_pre) * (D / 4) + c) * R + row];
+          acc.x += wgt * v.x;
+          acc.y += wgt * v.y;
+          acc.z += wgt * v.z;
+          acc.w += wgt * v.w;
+        }
+      }
+    }
+    if (parts > 1) {
+      sums[tid] = acc;
+      __syncthreads();
+      if (part == 0 && on) {
+        for (int k = 1; k < parts; ++k) {
+          const float4 v = sums[tid + k * n_el];
+          acc.x += v.x;
+          acc.y += v.y;
+          acc.z += v.z;
+          acc.w += v.w;
+        }
+      }
+    }
+    if (on && part == 0)
+      *reinterpret_cast<uint2*>(out + (size_t)row * D + 4 * c) =
+          make_uint2(pack_16x2<FP16>(acc.x, acc.y), pack_16x2<FP16>(acc.z, acc.w));
+  }
+}
+
+template <int D, bool FP16>
+cudaError_t launch_prefix_instance(const PfxLaunch& L) {
+  using C = PfxCfg<D>;
+  auto kern = prefix_kernel<D, FP16>;
+  const int smem = C::kSmemFixed + pfx_plan_ints(L.p.batch, L.p.n_groups) * 4;
+  // At least 116 KB, so that one CTA holds an SM's tensor memory at a time.
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       C::kSmemFixed + C::kMaxPlanBytes);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(L.grid);
+  cfg.blockDim = dim3(C::kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = L.stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if ((e = cudaLaunchKernelEx(&cfg, kern, L.mapK, L.mapV, L.mapQ, L.mapQ1, L.p)) != cudaSuccess) return e;
+  cfg.gridDim = dim3(L.p.batch * L.p.cache.n_kv_heads);
+  cfg.blockDim = dim3(kMergeThreads);
+  cfg.dynamicSmemBytes = 0;
+  return cudaLaunchKernelEx(&cfg, prefix_merge_kernel<D, FP16>, L.p, reinterpret_cast<uint16_t*>(L.O));
+}
+
+template <int D>
+cudaError_t launch_prefix_for_dim(bool fp16, const PfxLaunch& L) {
+  return fp16 ? launch_prefix_instance<D, true>(L) : launch_prefix_instance<D, false>(L);
+}
+
+}  // namespace wise

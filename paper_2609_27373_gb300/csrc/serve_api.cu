@@ -5,14 +5,13 @@
 #include <string.h>
 
 #include "internal.cuh"
+#include "prefix_attn.cuh"
 #include "wise.h"
 
 namespace wise {
 namespace {
 
 constexpr int kMaxSlots = 1 << 18;
-constexpr int kMaxBatch = 1024;    // requests of one attention call (their plan sits in shared memory)
-constexpr int kMaxRows = 128;      // query rows of one request and kv head (rows of one tile)
 constexpr int kMaxVocab = 1 << 18; // weights of 2^40 at most add up within 2^58
 constexpr int kMaxDraft = 1024;
 
@@ -62,8 +61,12 @@ int check_prefix(const wise_cache_t* cache, const wise_prefix_t* sh, PrefixParam
     return WISE_ERR_INVALID_ARG;
   if (sh->n_heads % cache->n_kv_heads != 0) return WISE_ERR_UNSUPPORTED;
   const int group = sh->n_heads / cache->n_kv_heads;
-  if (sh->batch > kMaxBatch || (long long)sh->q_len * group > kMaxRows || sh->n_groups > sh->batch)
+  if (sh->batch > kPfxMaxBatch || (long long)sh->q_len * group > kPfxRows || sh->n_groups > sh->batch ||
+      sh->n_groups > kPfxMaxGroups)
     return WISE_ERR_UNSUPPORTED;
+  // Key tiles of all requests and kv heads are counted in 32 bits.
+  const long long max_tiles = ((long long)cache->max_pages * cache->page + kPfxKeys - 1) / kPfxKeys;
+  if ((long long)sh->batch * cache->n_kv_heads * (max_tiles + 1) > (1LL << 30)) return WISE_ERR_UNSUPPORTED;
   p->batch = sh->batch;
   p->q_len = sh->q_len;
   p->n_heads = sh->n_heads;
@@ -191,7 +194,7 @@ extern "C" int wise_prefix_attn(const wise_cache_t* cache, int layer, const wise
   p.n_new = n_new;
   p.group_start = group_start;
   p.prefix_lens = prefix_lens;
-  return result(launch_prefix_attn(p, workspace, sms, stream));
+  return launch_prefix_attn(p, workspace, sms, stream);
 }
 
 extern "C" int wise_verify_draft(int batch, int k_max, int vocab, int dtype, const void* p, const void* q,

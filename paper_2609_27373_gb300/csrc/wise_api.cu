@@ -139,17 +139,33 @@ int current_device(int* sm_count, int** status) {
 
 unsigned long long wait_limit_ns() { return g_wait_ns.load(std::memory_order_relaxed); }
 
-bool make_tile_map(CUtensorMap* map, const void* base, bool fp16, int cols, int rows, long long outer, int box_rows) {
+namespace {
+bool encode_16bit(CUtensorMap* map, const void* base, bool fp16, int rank, const cuuint64_t* dims,
+                  const cuuint32_t* box) {
   EncodeTiledFn enc = encode_tiled();
   if (!enc) return false;
-  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)outer};
-  cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)cols * 2 * (cuuint64_t)rows};
-  cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
-  cuuint32_t elem[3] = {1, 1, 1};
-  return enc(map, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+  cuuint64_t strides[3];  // bytes, of a contiguous array
+  cuuint64_t n = 2;
+  for (int k = 0; k + 1 < rank; ++k) strides[k] = n *= dims[k];
+  const cuuint32_t elem[4] = {1, 1, 1, 1};
+  return enc(map, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank,
              const_cast<void*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+}  // namespace
+
+bool make_tile_map(CUtensorMap* map, const void* base, bool fp16, int cols, int rows, long long outer, int box_rows) {
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)outer};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
+  return encode_16bit(map, base, fp16, 3, dims, box);
+}
+
+bool make_query_map(CUtensorMap* map, const void* base, bool fp16, int cols, int rows, int heads, int batch,
+                    int box_batch) {
+  const cuuint64_t dims[4] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)heads, (cuuint64_t)batch};
+  const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, (cuuint32_t)box_batch};
+  return encode_16bit(map, base, fp16, 4, dims, box);
 }
 
 int launch_attention(const wise_shape_t* sh, const void* Q, const void* K, const void* V, void* O, int mode,
