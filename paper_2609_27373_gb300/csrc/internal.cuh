@@ -202,7 +202,7 @@ size_t prefix_attn_workspace(const PrefixParams& p, int sm_count);
 int launch_prefix_attn(const PrefixParams& p, void* workspace, int sm_count, cudaStream_t stream);
 
 struct VerifyParams {
-  int batch, k_max, vocab;
+  int batch, k_max, vocab, sm_count;
   const void* p;
   const void* q;
   const int32_t* draft;

@@ -209,8 +209,8 @@ extern "C" int wise_verify_draft(int batch, int k_max, int vocab, int dtype, con
     return WISE_ERR_INVALID_ARG;
   if (k_max > 0 && (!q || !aligned(q, size) || !ok32(draft) || !ok32(u_accept))) return WISE_ERR_INVALID_ARG;
   VerifyParams vp;
-  int sms, rc;
-  if ((rc = current_device(&sms, &vp.status)) != WISE_OK) return rc;
+  int rc;
+  if ((rc = current_device(&vp.sm_count, &vp.status)) != WISE_OK) return rc;
   vp.batch = batch;
   vp.k_max = k_max;
   vp.vocab = vocab;
