@@ -39,19 +39,37 @@ constexpr int kPfxKeys = 128;  // keys of a tile
 
 enum PfxKind : int { kPfxOwn = 0, kPfxSingle = 1, kPfxPair = 2 };
 
+// A line of tiles cut into runs of q or q + 1 tiles, the longer ones (`longer`
+// of them) first: where run k starts, and the run that holds tile x.
+struct PfxCuts {
+  int runs, q, longer;
+};
+__host__ __device__ inline PfxCuts pfx_cuts(int tiles, int max_runs) {
+  PfxCuts c;
+  c.runs = tiles < max_runs ? tiles : max_runs;
+  c.q = c.runs > 0 ? tiles / c.runs : 0;
+  c.longer = tiles - c.q * c.runs;
+  return c;
+}
+__host__ __device__ inline int pfx_cut(const PfxCuts& c, int k) { return k * c.q + (k < c.longer ? k : c.longer); }
+__host__ __device__ inline int pfx_run_of(const PfxCuts& c, int x) {
+  const int y = x - c.longer * (c.q + 1);
+  return y < 0 ? x / (c.q + 1) : c.longer + y / c.q;
+}
+
 // The plan of a launch: every CTA derives it in shared memory, the first one
 // also stores it for the merge.  Lists are ints.
 struct PfxTotals {
-  int pair_tiles, pair_runs;    // the line of pair items
-  int single_tiles;             // the other line: single items first,
-  int line_tiles, line_runs;    // then own items
-  int grouped;                  // 0 when the groups were faulty (nothing is shared)
-  int pad[2];
+  PfxCuts pair;      // the line of pair items
+  PfxCuts line;      // the other line: single items first, then own items
+  int single_tiles;  // tiles of the single items
+  int grouped;       // 0 when the groups were faulty (nothing is shared)
 };
 
 struct PfxPlan {
   PfxTotals* t;
   // Per request.
+  int* slot;   // of the cache
   int* len;    // positions of its sequence, 0 for an unused or faulty request
   int* lo;     // positions read through its group
   int* add;    // new tokens
@@ -68,13 +86,14 @@ struct PfxPlan {
 };
 
 __host__ __device__ inline int pfx_plan_ints(int batch, int n_groups) {
-  return 8 + 5 * batch + 1 + 7 * n_groups + 3;
+  return 8 + 6 * batch + 1 + 7 * n_groups + 3;
 }
 
 __host__ __device__ inline PfxPlan pfx_plan(int* base, int batch, int n_groups) {
   PfxPlan p;
   p.t = reinterpret_cast<PfxTotals*>(base);
-  p.len = base + 8;
+  p.slot = base + 8;
+  p.len = p.slot + batch;
   p.lo = p.len + batch;
   p.add = p.lo + batch;
   p.group = p.add + batch;
@@ -87,12 +106,6 @@ __host__ __device__ inline PfxPlan pfx_plan(int* base, int batch, int n_groups) 
   p.single_base = p.pair_item + n_groups;
   p.single_item = p.single_base + n_groups + 1;
   return p;
-}
-
-// Run k of `runs` equal cuts of a line of `tiles`, and the run that holds tile x.
-__host__ __device__ inline int pfx_cut(int k, int tiles, int runs) { return (int)((long long)k * tiles / runs); }
-__host__ __device__ inline int pfx_run_of(int x, int tiles, int runs) {
-  return (int)((((long long)x + 1) * runs - 1) / tiles);
 }
 
 // Workspace: the plan, then for each kind its segments' (m, l) pairs and their

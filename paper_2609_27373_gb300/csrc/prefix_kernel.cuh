@@ -9,12 +9,13 @@
 //                   maximum moved by more than 2^8, and at the end of a
 //                   segment stores (m, l) and O to the workspace.  Warps
 //                   without a query row only keep the barriers going.
-//   warp 8          producer: walks the CTA's segments, looks the pages up (a
-//                   lane per page) and issues the TMA loads of Q, K and V.
+//   warps 8, 11     producers: walk the tiles of stream 0 and 1, look their
+//                   pages up (a lane per page, one tile ahead), publish the
+//                   schedule and issue the TMA loads of Q, K and V.
 //   warps 9, 10     one thread each: the MMAs of stream 0 and 1.
 // TMEM: S and P of stream w at column 128 w, O at 256 + 128 w.  The two
 // streams alternate on the tensor cores: one computes while the other is in
-// its softmax.  K and V tiles go through one ring in shared memory.
+// its softmax.  K and V tiles go through a ring each in shared memory.
 //
 // Every wait is bounded; one that runs out sets the status word and an abort
 // flag, and every role unwinds.
@@ -33,21 +34,21 @@ template <int D>
 struct PfxCfg {
   static constexpr int kBoxes = (D + 63) / 64;
   static constexpr int kTileBytes = kBoxes * 128 * 128;  // a Q, K or V tile
-  static constexpr int kSlots = 128 * 1024 / kTileBytes; // K/V ring: 128 KB
+  static constexpr int kSlots = 64 * 1024 / kTileBytes;  // of the K ring and of the V ring: 64 KB each
   static constexpr int kThreads = 384;
-  static constexpr int kRegsSoftmax = 216;  // 256 * 216 + 128 * 72 <= 384 * 168 registers
-  static constexpr int kRegsOther = 72;
-  static constexpr int kRingBytes = (2 + kSlots) * kTileBytes;  // two Q tiles, then the ring
-  static constexpr int kMaxPlanBytes = 29 * 1024;
+  static constexpr int kRegsSoftmax = 208;  // 256 * 208 + 128 * 88 <= 384 * 168 registers
+  static constexpr int kRegsOther = 88;
+  static constexpr int kRingBytes = (2 + 2 * kSlots) * kTileBytes;  // two Q tiles, then the rings
+  static constexpr int kMaxPlanBytes = 32 * 1024;
   static constexpr int kSmemFixed = kRingBytes + 1024;  // and the plan behind
-  static_assert(kSmemFixed + kMaxPlanBytes + 2560 <= 227 * 1024, "shared memory");
+  static_assert(kSmemFixed + kMaxPlanBytes + 1024 <= 227 * 1024, "shared memory");
   static_assert(256 * kRegsSoftmax + 128 * kRegsOther <= kThreads * 168, "register split");
 };
 
 constexpr int kPfxSched = 8;  // schedule entries per stream
 constexpr int kPfxFirst = 1, kPfxLast = 2, kPfxEnd = 4;
 
-// Schedule entry {ring position of the K tile (V follows), first key position,
+// Schedule entry {ring slot | parity of its use << 8, first key position,
 // request | (requests - 1) << 10 | kind << 17 | flags << 19, segment slot}.
 __device__ __forceinline__ int pfx_pack(int req, int nreq, int kind, int flags) {
   return req | (nreq - 1) << 10 | kind << 17 | flags << 19;
@@ -55,7 +56,7 @@ __device__ __forceinline__ int pfx_pack(int req, int nreq, int kind, int flags) 
 
 template <int NS>
 struct PfxShared {
-  uint64_t kv_full[NS], kv_empty[NS];  // empty: one arrival per stream
+  uint64_t k_full[NS], k_empty[NS], v_full[NS], v_empty[NS];  // empty: one arrival per stream
   uint64_t sched_full[2][kPfxSched], sched_empty[2][kPfxSched];  // empty: the issuer and 4 warps
   uint64_t q_full[2], q_free[2];
   uint64_t s_full[2];  // S written
@@ -72,7 +73,14 @@ struct PfxShared {
 __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bool report) {
   const CacheView& c = p.cache;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
-  int bad = 0;
+  int bad = 0, bad_groups = 0;
+  for (int g = tid; g <= p.n_groups; g += blockDim.x) {
+    if (p.n_groups == 0) break;
+    const int a = p.group_start[g], e = g < p.n_groups ? p.group_start[g + 1] : a;
+    if (g < p.n_groups) plan.tiles[g] = p.prefix_lens[g];  // the declared length, until the tiles are known
+    if (a < 0 || a > p.batch || a > e) bad_groups = 1;
+    plan.start[g] = a;
+  }
   for (int r = tid; r < p.batch; r += blockDim.x) {
     const int s = p.slots[r];
     const int add = p.n_new ? p.n_new[r] : p.q_len;
@@ -84,17 +92,11 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
         len = 0;
       }
     }
+    plan.slot[r] = s;
     plan.len[r] = add > 0 ? len : 0;
     plan.add[r] = add > 0 ? add : 0;
     plan.lo[r] = 0;
     plan.group[r] = -1;
-  }
-  int bad_groups = 0;
-  for (int g = tid; g <= p.n_groups; g += blockDim.x) {
-    if (p.n_groups == 0) break;
-    const int a = p.group_start[g];
-    if (a < 0 || a > p.batch || (g < p.n_groups && a > p.group_start[g + 1])) bad_groups = 1;
-    plan.start[g] = a;
   }
   if (report && (bad | bad_groups)) atomicOr(c.status, kStatusBadCache);
   const bool grouped = !__syncthreads_or(bad_groups);
@@ -115,7 +117,8 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
     active = __reduce_add_sync(0xffffffffu, active);
     lead = __reduce_min_sync(0xffffffffu, lead);
     int shared = 0;
-    if (active > 1) shared = max(0, min(p.prefix_lens[g], shortest)) / c.page * c.page;
+    if (active > 1) shared = max(0, min(plan.tiles[g], shortest)) / c.page * c.page;
+    __syncwarp();
     const int tiles = (shared + kPfxKeys - 1) / kPfxKeys;
     if (lane == 0) {
       plan.tiles[g] = tiles;
@@ -181,12 +184,10 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
   }
   __syncthreads();
   if (tid == 0) {
-    PfxTotals t = {};
-    t.pair_tiles = plan.pair_base[p.n_groups];
-    t.pair_runs = min((int)gridDim.x, t.pair_tiles);
+    PfxTotals t;
+    t.pair = pfx_cuts(plan.pair_base[p.n_groups], gridDim.x);
     t.single_tiles = plan.single_base[p.n_groups];
-    t.line_tiles = t.single_tiles + plan.cum[p.batch] * c.n_kv_heads;
-    t.line_runs = min(2 * (int)gridDim.x, t.line_tiles);
+    t.line = pfx_cuts(t.single_tiles + plan.cum[p.batch] * c.n_kv_heads, 2 * gridDim.x);
     t.grouped = grouped;
     *plan.t = t;
   }
@@ -206,13 +207,13 @@ __device__ __forceinline__ int pfx_find(const int* base, int n, int x) {
   return lo;
 }
 
-// A segment: key tiles t .. t_end - 1 of an item.
+// A segment: a run of key tiles of an item.
 struct PfxSeg {
-  int kind, req, nreq, nreq2;  // requests of the (first) tile, and of the pair's second
-  int kvh, table_row;          // kv head, cache slot whose pages are read
-  int pos, end;                // position of the first key of tile t; one past the item's keys
-  int left;                    // tiles left
-  int slot;                    // workspace slot
+  int word, word2;  // requests and kind as in a schedule entry; of a pair's second tile
+  int kvh, row;     // kv head, cache slot whose pages are read
+  int pos, end;     // position of the next tile's first key; one past the item's keys
+  int left;         // tiles left
+  int slot;         // workspace slot
 };
 
 // The segment that starts at tile x of a line and ends at x_end or with its item.
@@ -221,7 +222,7 @@ __device__ __forceinline__ PfxSeg pfx_segment(const PfxParams& p, const PfxPlan&
   PfxSeg s;
   const int kv = p.cache.n_kv_heads;
   const int single_tiles = plan.t->single_tiles;
-  int tiles, t;
+  int tiles, t, kind, nreq, nreq2 = 1, req;
   if (pairs || x < single_tiles) {
     const int* base = pairs ? plan.pair_base : plan.single_base;
     const int g = pfx_find(base, p.n_groups, x);
@@ -236,201 +237,192 @@ __device__ __forceinline__ PfxSeg pfx_segment(const PfxParams& p, const PfxPlan&
       const int n_pairs = row_tiles / 2;
       s.kvh = it / n_pairs;
       const int pair = it - s.kvh * n_pairs;
-      s.kind = kPfxPair;
-      s.req = a + 2 * pair * p.per_tile;
+      kind = kPfxPair;
+      req = a + 2 * pair * p.per_tile;
       s.slot = 2 * (plan.pair_item[g] * kv + it + run);
-      s.nreq = p.per_tile;
-      s.nreq2 = min(p.per_tile, members - (2 * pair + 1) * p.per_tile);
+      nreq = p.per_tile;
+      nreq2 = min(p.per_tile, members - (2 * pair + 1) * p.per_tile);
     } else {
       s.kvh = it;
-      s.kind = kPfxSingle;
-      s.req = a + (row_tiles - 1) * p.per_tile;
+      kind = kPfxSingle;
+      req = a + (row_tiles - 1) * p.per_tile;
       s.slot = plan.single_item[g] * kv + it + run;
-      s.nreq = members - (row_tiles - 1) * p.per_tile;
+      nreq = members - (row_tiles - 1) * p.per_tile;
     }
     const int lead = plan.lead[g];
-    s.table_row = p.slots[lead];
+    s.row = plan.slot[lead];
     s.end = plan.lo[lead];
     s.pos = t * kPfxKeys;
   } else {
     const int y = x - single_tiles;
     // cum[r] * kv <= y < cum[r + 1] * kv
-    const int r = pfx_find(plan.cum, p.batch, y / kv);
-    tiles = plan.cum[r + 1] - plan.cum[r];
-    const int z = y - plan.cum[r] * kv;
+    req = pfx_find(plan.cum, p.batch, y / kv);
+    tiles = plan.cum[req + 1] - plan.cum[req];
+    const int z = y - plan.cum[req] * kv;
     s.kvh = z / tiles;
     t = z - s.kvh * tiles;
-    s.kind = kPfxOwn;
-    s.req = r;
-    s.nreq = 1;
-    s.table_row = p.slots[r];
-    s.end = plan.len[r];
-    s.pos = plan.lo[r] + t * kPfxKeys;
-    s.slot = r * kv + s.kvh + run;
+    kind = kPfxOwn;
+    nreq = 1;
+    s.row = plan.slot[req];
+    s.end = plan.len[req];
+    s.pos = plan.lo[req] + t * kPfxKeys;
+    s.slot = req * kv + s.kvh + run;
   }
   s.left = min(tiles - t, x_end - x);
+  s.word = pfx_pack(req, nreq, kind, 0);
+  s.word2 = pairs ? pfx_pack(req + p.per_tile, nreq2, kind, 0) : 0;
   return s;
 }
 
-// ------------------------------------------------------------------ producer
-// The whole warp 8.
+// ----------------------------------------------------------------- producers
+// Ring slots.  While pair items run, tile n of the CTA sits in slot n % NS of
+// both rings and both streams use it.  Afterwards stream w has the slots
+// w * NS / 2 .. of each ring to itself.  A slot's uses are counted across both
+// phases: use u waits for the end of use u - 1.
+
+// One warp each: warp 8 (w = 0) and warp 11 (w = 1).  Each publishes the
+// schedule and loads Q of its stream.  While pair items run, warp 8 loads the
+// K tiles and warp 11 the V tiles of both; after that each loads its stream's.
 template <int D>
 __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, const CUtensorMap* mapQ,
-                             const CUtensorMap* mapQ1, const PfxParams& p, const PfxPlan& plan, uint8_t* q_tiles,
-                             uint8_t* ring, PfxShared<PfxCfg<D>::kSlots>& sb) {
+                             const CUtensorMap* mapQ1, const PfxParams& p, const PfxPlan& plan, int w,
+                             uint8_t* q_tiles, uint8_t* ring, PfxShared<PfxCfg<D>::kSlots>& sb) {
   using C = PfxCfg<D>;
-  constexpr int NS = C::kSlots;
+  constexpr int NS = C::kSlots, H = NS / 2;
   const CacheView& c = p.cache;
   const int lane = threadIdx.x & 31;
   volatile int* abort = &sb.abort;
-  int n_kv = 0;             // ring positions used
-  int n_ent[2] = {0, 0};    // schedule entries per stream
-  int n_q[2] = {0, 0};      // Q tiles loaded per stream
-  int bad = 0;
-  bool ok = true;
-  const int per_tile_pages = kPfxKeys / c.page;
-
-  auto emit = [&](int w, int4 ent) {
-    const int slot = n_ent[w] % kPfxSched;
-    if (n_ent[w] >= kPfxSched && !warp_wait(&sb.sched_empty[w][slot], ((n_ent[w] / kPfxSched) - 1) & 1, abort, p.wait_ns))
-      return false;
-    if (lane == 0) {
-      sb.sched[w][slot] = ent;
-      mbar_arrive(&sb.sched_full[w][slot]);
-    }
-    ++n_ent[w];
-    return true;
-  };
-  // The page of lane i of a tile (z coordinate of its kv head; out of range
-  // for a faulty id, which reads zeros), -1 past the item's end.
-  auto page_of = [&](const PfxSeg& s) -> int {
-    const int at = s.pos + lane * c.page;
-    if (lane >= per_tile_pages || at >= s.end) return -1;
-    const int page = __ldg(c.table + (size_t)s.table_row * c.max_pages + at / c.page);
-    if (page < 0 || page >= c.n_pages) {
-      bad = 1;
-      return c.n_pages * c.n_kv_heads;
-    }
-    return page * c.n_kv_heads + s.kvh;
-  };
-  auto load_tile = [&](const CUtensorMap* map, int z) -> bool {
-    const int slot = n_kv % NS;
-    if (n_kv >= NS && !warp_wait(&sb.kv_empty[slot], ((n_kv / NS) - 1) & 1, abort, p.wait_ns)) return false;
-    const int n = __popc(__ballot_sync(0xffffffffu, z >= 0));
-    if (lane == 0) mbar_arrive_expect_tx(&sb.kv_full[slot], n * c.page * 128 * C::kBoxes);
-    __syncwarp();
-    if (z >= 0) {
-      uint8_t* dst = ring + slot * C::kTileBytes + lane * c.page * 128;
-      for (int b = 0; b < C::kBoxes; ++b) tma_load_3d(dst + b * 128 * 128, map, &sb.kv_full[slot], 64 * b, 0, z);
-    }
-    ++n_kv;
-    return true;
-  };
-  auto load_q = [&](int w, int req, const PfxSeg& s) -> bool {
-    if (n_q[w] >= 1 && !warp_wait(&sb.q_free[w], (n_q[w] - 1) & 1, abort, p.wait_ns)) return false;
-    if (lane == 0) {
-      const int rows = s.kind == kPfxOwn ? p.rows : p.rows * p.per_tile;
-      mbar_arrive_expect_tx(&sb.q_full[w], rows * 128 * C::kBoxes);
-      for (int b = 0; b < C::kBoxes; ++b)
-        tma_load_4d(q_tiles + w * C::kTileBytes + b * 128 * 128, s.kind == kPfxOwn ? mapQ1 : mapQ, &sb.q_full[w],
-                    64 * b, 0, s.kvh, req);
-    }
-    ++n_q[w];
-    return true;
-  };
-  // One tile of a segment for the streams in `mask`.
-  auto tile = [&](const PfxSeg& s, bool first, int z, int w0, int w1) -> bool {
-    const int flags = (first ? kPfxFirst : 0) | (s.left == 1 ? kPfxLast : 0);
-    const int n = n_kv;
-    for (int w = w0; w <= w1; ++w) {
-      const bool second = s.kind == kPfxPair && w == 1;
-      const int req = second ? s.req + p.per_tile : s.req;
-      if (!emit(w, make_int4(n, s.pos, pfx_pack(req, second ? s.nreq2 : s.nreq, s.kind, flags), s.slot + second)))
-        return false;
-    }
-    if (!load_tile(mapK, z)) return false;
-    if (first) {
-      for (int w = w0; w <= w1; ++w)
-        if (!load_q(w, s.kind == kPfxPair && w == 1 ? s.req + p.per_tile : s.req, s)) return false;
-    }
-    return load_tile(mapV, z);
-  };
-
   const PfxTotals t = *plan.t;
   const int G = gridDim.x, cta = blockIdx.x;
-  // Pair items: this CTA's run, both streams.
-  if (cta < t.pair_runs) {
-    int x = pfx_cut(cta, t.pair_tiles, t.pair_runs);
-    const int x_end = pfx_cut(cta + 1, t.pair_tiles, t.pair_runs);
-    while (ok && x < x_end) {
-      PfxSeg s = pfx_segment(p, plan, true, x, x_end, cta);
-      x += s.left;
-      int z = page_of(s);
-      for (bool first = true; ok && s.left > 0; first = false) {
-        const int z_now = z;
-        PfxSeg next = s;
-        next.pos += kPfxKeys;
-        if (s.left > 1) z = page_of(next);  // looked up one tile ahead
-        ok = tile(s, first, z_now, 0, 1);
-        next.left -= 1;
-        s = next;
-      }
-    }
+  // Runs of the second phase start at the CTA after the last one with pair
+  // items, so that small problems spread out.
+  int line_run = cta - t.pair.runs;
+  if (line_run < 0) line_run += G;
+  line_run += w * G;
+  int n_ent = 0, n_q = 0;            // schedule entries published, Q tiles loaded
+  uint32_t issued = 0, parity = 0;   // by ring (8 bits each) and slot: loads of this warp, and their last use's parity
+  int bad = 0;
+  bool ok = true;
+
+  bool pair = cta < t.pair.runs;
+  const bool had_pairs = pair;
+  int run = pair ? cta : line_run;
+  int x = 0, x_end = 0;
+  if (pair) {
+    x = pfx_cut(t.pair, run);
+    x_end = pfx_cut(t.pair, run + 1);
+  } else if (run < t.line.runs) {
+    x = pfx_cut(t.line, run);
+    x_end = pfx_cut(t.line, run + 1);
   }
-  // The other items: one run per stream, tile by tile in turn.  Runs start
-  // at the CTA after the last one with pair items, so that small problems
-  // spread out.
-  int xs[2], xe[2];
-  PfxSeg seg[2];
-  int zs[2];
-  bool first[2] = {true, true};
-  const int shift = t.pair_runs % G;
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    const int run = (cta - shift + G) % G + w * G;
-    xs[w] = xe[w] = 0;
-    seg[w].left = 0;
-    if (run < t.line_runs) {
-      xs[w] = pfx_cut(run, t.line_tiles, t.line_runs);
-      xe[w] = pfx_cut(run + 1, t.line_tiles, t.line_runs);
-    }
-  }
-  while (ok && (seg[0].left > 0 || seg[1].left > 0 || xs[0] < xe[0] || xs[1] < xe[1])) {
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      if (!ok) break;
-      if (seg[w].left == 0) {
-        if (xs[w] >= xe[w]) continue;
-        const int run = (cta - shift + G) % G + w * G;
-        seg[w] = pfx_segment(p, plan, false, xs[w], xe[w], run);
-        xs[w] += seg[w].left;
-        zs[w] = page_of(seg[w]);
-        first[w] = true;
-      }
-      const int z_now = zs[w];
-      PfxSeg next = seg[w];
-      next.pos += kPfxKeys;
-      if (seg[w].left > 1) zs[w] = page_of(next);
-      ok = tile(seg[w], first[w], z_now, w, w);
-      first[w] = false;
-      next.left -= 1;
-      seg[w] = next;
-    }
-  }
-  for (int w = 0; w < 2 && ok; ++w) ok = emit(w, make_int4(0, 0, pfx_pack(0, 1, 0, kPfxEnd), 0));
-  if (bad) atomicOr(c.status, kStatusBadCache);
-  if (!ok) {
-    if (lane == 0) {
-      *reinterpret_cast<volatile int*>(&sb.abort) = 1;
-      atomicOr(c.status, kStatusTimeout);
-      // Copies already issued land before the CTA's shared memory is released.
-      int never = 0;
-      for (int n = max(0, n_kv - NS); n < n_kv; ++n) mbar_wait(&sb.kv_full[n % NS], (n / NS) & 1, &never);
-      for (int w = 0; w < 2; ++w)
-        if (n_q[w] > 0) mbar_wait(&sb.q_full[w], (n_q[w] - 1) & 1, &never);
-    }
+  const int n_pair = pair ? x_end - x : 0;
+  int n = 0;  // tiles of the phase so far
+  PfxSeg seg;
+  seg.left = 0;
+  int page = -1;       // this lane's page of the next tile, not looked at before its turn
+  bool first = false;  // the next tile starts its segment
+
+  auto fetch = [&]() {
+    const int at = seg.pos + lane * c.page;
+    page = -1;
+    if (lane * c.page < kPfxKeys && at < seg.end)
+      page = __ldg(c.table + (size_t)seg.row * c.max_pages + at / c.page);
+  };
+  auto load = [&](int r, const CUtensorMap* map, uint64_t* full, uint64_t* empty, int slot, int use) -> bool {
+    if (use >= 1 && !warp_wait(&empty[slot], (use - 1) & 1, abort, p.wait_ns)) return false;
+    // One lane per page of the tile that the item reaches.
+    const bool on = lane * c.page < kPfxKeys && seg.pos + lane * c.page < seg.end;
+    const int n_on = min(kPfxKeys / c.page, (seg.end - seg.pos + c.page - 1) / c.page);
+    if (lane == 0) mbar_arrive_expect_tx(&full[slot], n_on * c.page * 128 * C::kBoxes);
     __syncwarp();
+    if (on) {
+      // A faulty page id becomes a coordinate out of range, which reads zeros.
+      const bool valid = page >= 0 && page < c.n_pages;
+      if (!valid) bad = 1;
+      const int z = valid ? page * c.n_kv_heads + seg.kvh : c.n_pages * c.n_kv_heads;
+      uint8_t* dst = ring + (r * NS + slot) * C::kTileBytes + lane * c.page * 128;
+      for (int b = 0; b < C::kBoxes; ++b) tma_load_3d(dst + b * 128 * 128, map, &full[slot], 64 * b, 0, z);
+    }
+    const uint32_t bit = 1u << (r * 8 + slot);
+    issued |= bit;
+    parity = (use & 1) ? parity | bit : parity & ~bit;
+    return true;
+  };
+
+  for (;;) {
+    if (seg.left == 0) {
+      if (x == x_end) {
+        if (!pair) break;
+        // Both warps have issued all loads of the pair phase when they go on:
+        // the other's slots are then at most one use behind, which is as far
+        // as a wait can tell.
+        named_barrier_sync(1, 64);
+        pair = false;
+        n = 0;
+        run = line_run;
+        if (run >= t.line.runs) break;
+        x = pfx_cut(t.line, run);
+        x_end = pfx_cut(t.line, run + 1);
+      }
+      seg = pfx_segment(p, plan, pair, x, x_end, run);
+      x += seg.left;
+      first = true;
+      fetch();
+    }
+    const bool second = pair && w == 1;
+    const int slot = pair ? n % NS : w * H + n % H;
+    const int use = pair ? n / NS : n / H + (n_pair - slot + NS - 1) / NS;
+    const int word = second ? seg.word2 : seg.word;
+    const int e = n_ent % kPfxSched;
+    if (n_ent >= kPfxSched) ok = warp_wait(&sb.sched_empty[w][e], ((n_ent / kPfxSched) - 1) & 1, abort, p.wait_ns);
+    if (ok && lane == 0) {
+      const int flags = (first ? kPfxFirst : 0) | (seg.left == 1 ? kPfxLast : 0);
+      sb.sched[w][e] = make_int4(slot | (use & 1) << 8, seg.pos, word | flags << 19, seg.slot + second);
+      mbar_arrive(&sb.sched_full[w][e]);
+    }
+    ++n_ent;
+    if (ok && (!pair || w == 0)) ok = load(0, mapK, sb.k_full, sb.k_empty, slot, use);
+    if (ok && first) {
+      if (n_q >= 1) ok = warp_wait(&sb.q_free[w], (n_q - 1) & 1, abort, p.wait_ns);
+      if (ok && lane == 0) {
+        const bool own = ((word >> 17) & 3) == kPfxOwn;
+        mbar_arrive_expect_tx(&sb.q_full[w], (own ? p.rows : p.rows * p.per_tile) * 128 * C::kBoxes);
+        for (int b = 0; b < C::kBoxes; ++b)
+          tma_load_4d(q_tiles + w * C::kTileBytes + b * 128 * 128, own ? mapQ1 : mapQ, &sb.q_full[w], 64 * b, 0,
+                      seg.kvh, word & 1023);
+      }
+      if (ok) ++n_q;
+    }
+    if (ok && (!pair || w == 1)) ok = load(1, mapV, sb.v_full, sb.v_empty, slot, use);
+    if (!ok) break;
+    ++n;
+    --seg.left;
+    seg.pos += kPfxKeys;
+    first = false;
+    if (seg.left > 0) fetch();
   }
+  if (had_pairs && pair) named_barrier_sync(1, 64);  // gave up before the end of the pair phase
+  if (ok) {
+    const int e = n_ent % kPfxSched;
+    if (n_ent >= kPfxSched) ok = warp_wait(&sb.sched_empty[w][e], ((n_ent / kPfxSched) - 1) & 1, abort, p.wait_ns);
+    if (ok && lane == 0) {
+      sb.sched[w][e] = make_int4(0, 0, kPfxEnd << 19, 0);
+      mbar_arrive(&sb.sched_full[w][e]);
+    }
+  }
+  if (bad) atomicOr(c.status, kStatusBadCache);
+  if (!ok && lane == 0) {
+    *reinterpret_cast<volatile int*>(&sb.abort) = 1;
+    atomicOr(c.status, kStatusTimeout);
+    // Copies already issued land before the CTA's shared memory is released.
+    int never = 0;
+    for (int k = 0; k < NS; ++k) {
+      if ((issued >> k) & 1) mbar_wait(&sb.k_full[k], (parity >> k) & 1, &never);
+      if ((issued >> (8 + k)) & 1) mbar_wait(&sb.v_full[k], (parity >> (8 + k)) & 1, &never);
+    }
+    if (n_q > 0) mbar_wait(&sb.q_full[w], (n_q - 1) & 1, &never);
+  }
+  __syncwarp();
 }
 
 // --------------------------------------------------------------- MMA issuers
@@ -462,14 +454,15 @@ __device__ void pfx_mma(const PfxParams& p, int w, uint32_t tmem, uint8_t* q_til
       ok = false;
       break;
     }
-    const int k_slot = ent.x % NS, v_slot = (ent.x + 1) % NS;
-    if (!mbar_wait(&sb.kv_full[k_slot], (ent.x / NS) & 1, abort, p.wait_ns)) {
+    const int slot = ent.x & 255;
+    const uint32_t phase = ent.x >> 8;
+    if (!mbar_wait(&sb.k_full[slot], phase, abort, p.wait_ns)) {
       ok = false;
       break;
     }
     tc_fence_after_sync();
     const uint64_t q0 = smem_desc_sw128(smem_u32(q_tiles + w * C::kTileBytes), 16, 1024);
-    const uint64_t k0 = smem_desc_sw128(smem_u32(ring + k_slot * C::kTileBytes), 16, 1024);
+    const uint64_t k0 = smem_desc_sw128(smem_u32(ring + slot * C::kTileBytes), 16, 1024);
 #pragma unroll 1
     for (int kk = 0; kk < D / 16; ++kk) {
       const uint32_t off = ((kk >> 2) * (128 * 128) + (kk & 3) * 32) >> 4;
@@ -478,23 +471,23 @@ __device__ void pfx_mma(const PfxParams& p, int w, uint32_t tmem, uint8_t* q_til
     umma_commit(&sb.s_full[w]);
     // A slot is empty after two arrivals: one of each stream for a pair's
     // tile, both from this one otherwise.
-    umma_commit(&sb.kv_empty[k_slot]);
-    if (!pair) umma_commit(&sb.kv_empty[k_slot]);
+    umma_commit(&sb.k_empty[slot]);
+    if (!pair) umma_commit(&sb.k_empty[slot]);
     if (flags & kPfxLast) umma_commit(&sb.q_free[w]);
-    if (!mbar_wait(&sb.kv_full[v_slot], ((ent.x + 1) / NS) & 1, abort, p.wait_ns) ||
+    if (!mbar_wait(&sb.v_full[slot], phase, abort, p.wait_ns) ||
         !mbar_wait(&sb.p_full[w], j & 1, abort, p.wait_ns)) {
       ok = false;
       break;
     }
     tc_fence_after_sync();
-    const uint64_t v0 = smem_desc_sw128(smem_u32(ring + v_slot * C::kTileBytes), kPfxKeys * 128, 1024);
+    const uint64_t v0 = smem_desc_sw128(smem_u32(ring + (NS + slot) * C::kTileBytes), kPfxKeys * 128, 1024);
 #pragma unroll 1
     for (int kk = 0; kk < kPfxKeys / 16; ++kk)
       umma_bf16_ts(o_col, s_col + kk * 8, v0 + ((kk * 2048) >> 4), idesc_o,
                    ((flags & kPfxFirst) && kk == 0) ? 0u : 1u);
     umma_commit(&sb.o_full[w]);
-    umma_commit(&sb.kv_empty[v_slot]);
-    if (!pair) umma_commit(&sb.kv_empty[v_slot]);
+    umma_commit(&sb.v_empty[slot]);
+    if (!pair) umma_commit(&sb.v_empty[slot]);
     // The next S overwrites P, which this product reads.
     if (!mbar_wait(&sb.o_full[w], j & 1, abort, p.wait_ns)) {
       ok = false;
@@ -552,7 +545,9 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
       const int req0 = ent.z & 1023, nreq = ((ent.z >> 10) & 127) + 1;
       const int of = r / p.rows, i = r % p.rows % p.q_len;
       row_on = of < nreq;
-      limit = 0;
+      // Threads without a row compute on whatever Q holds there and store
+      // nothing; unmasked, they do not hold up their warp.
+      limit = INT_MAX;
       if (row_on) {
         const int req = req0 + of, add = plan.add[req];
         limit = i < add ? max(0, plan.len[req] - add + i + 1) : 0;
@@ -572,7 +567,7 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
       load_s_row<128>(lane_tmem + s_col, s, 1u, min(limit, end) - ent.y - 1);
       const float m_tile = row_max(s) * p.scale_log2;
       const float m_new = (m_tile > m + kRescaleThreshold) ? m_tile : m;
-      const bool rescale = m_new != m && m != -INFINITY;
+      const bool rescale = row_on && m_new != m && m != -INFINITY;
       const float f = rescale ? ex2_approx(m - m_new) : 1.0f;
       const float sum = exp2_scaled(s, p.scale_log2, m_new == -INFINITY ? 0.0f : m_new);
       l = l * f + sum;
@@ -603,12 +598,12 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
     if (valid < kPfxKeys) {
       // The item ends in this tile: rows of V past its end are whatever the
       // pool or an earlier tile left there, and 0 * NaN would spread.
-      if (!warp_wait(&sb.kv_full[(ent.x + 1) % NS], ((ent.x + 1) / NS) & 1, abort, p.wait_ns)) {
+      if (!warp_wait(&sb.v_full[ent.x & 255], ent.x >> 8, abort, p.wait_ns)) {
         ok = false;
         break;
       }
       if (r >= valid) {
-        const uint32_t row = smem_u32(ring + ((ent.x + 1) % NS) * C::kTileBytes + r * 128);
+        const uint32_t row = smem_u32(ring + (NS + (ent.x & 255)) * C::kTileBytes + r * 128);
         for (int b = 0; b < C::kBoxes; ++b)
           for (int k = 0; k < 8; ++k) st_shared_v4(row + b * 128 * 128 + k * 16, 0u, 0u, 0u, 0u);
         fence_proxy_async_smem();
@@ -660,13 +655,15 @@ __global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
   uint8_t* ring = q_tiles + 2 * C::kTileBytes;
   const PfxPlan plan = pfx_plan(reinterpret_cast<int*>(q_tiles + C::kRingBytes), p.batch, p.n_groups);
   __shared__ PfxShared<C::kSlots> sb;
-  static_assert(sizeof(sb) <= 2048, "static shared memory");
+  static_assert(sizeof(sb) <= 1024, "static shared memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     sb.abort = 0;
     for (int i = 0; i < C::kSlots; ++i) {
-      mbar_init(&sb.kv_full[i], 1);
-      mbar_init(&sb.kv_empty[i], 2);
+      mbar_init(&sb.k_full[i], 1);
+      mbar_init(&sb.v_full[i], 1);
+      mbar_init(&sb.k_empty[i], 2);
+      mbar_init(&sb.v_empty[i], 2);
     }
     for (int w = 0; w < 2; ++w) {
       for (int i = 0; i < kPfxSched; ++i) {
@@ -708,8 +705,10 @@ __global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
   } else {
     warpgroup_reg_dec<C::kRegsOther>();
     if (warp == 8) {
-      pfx_producer<D>(&mapK, &mapV, &mapQ, &mapQ1, p, plan, q_tiles, ring, sb);
-    } else if (warp <= 10) {
+      pfx_producer<D>(&mapK, &mapV, &mapQ, &mapQ1, p, plan, 0, q_tiles, ring, sb);
+    } else if (warp == 11) {
+      pfx_producer<D>(&mapK, &mapV, &mapQ, &mapQ1, p, plan, 1, q_tiles, ring, sb);
+    } else {
       if (lane == 0) pfx_mma<D, FP16>(p, warp - 9, tmem, q_tiles, ring, sb);
     }
   }
@@ -726,12 +725,14 @@ __global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
 // --------------------------------------------------------------------- merge
 // One block per (request, kv head): joins the partial results of its rows.
 constexpr int kMergeThreads = 256;
-constexpr int kMergeChunk = 16;  // segments whose weights sit in shared memory at a time
+constexpr int kMergeStats = 2048;  // (m, l) pairs in shared memory at a time
+constexpr int kMergeEach = 4;
 
 template <int D, bool FP16>
 __global__ void __launch_bounds__(kMergeThreads) prefix_merge_kernel(const PfxParams p, uint16_t* O) {
-  __shared__ float2 stat[kPfxRows];                 // per row M and 1 / L
-  __shared__ float weight[kMergeChunk][kPfxRows];
+  __shared__ float2 stats[kMergeStats];
+  __shared__ float2 row_max_sum[kPfxRows];
+  __shared__ float row_factor[kPfxRows];
   __shared__ float4 sums[kMergeThreads];
   griddep_wait();
   const PfxPlan plan = pfx_plan(p.work.plan, p.batch, p.n_groups);
@@ -752,13 +753,13 @@ __global__ void __launch_bounds__(kMergeThreads) prefix_merge_kernel(const PfxPa
         kind = kPfxPair;
         const int it = kvh * n_pairs + tile / 2;
         const int x = plan.pair_base[g] + it * tiles;
-        const int k0 = pfx_run_of(x, t.pair_tiles, t.pair_runs), k1 = pfx_run_of(x + tiles - 1, t.pair_tiles, t.pair_runs);
+        const int k0 = pfx_run_of(t.pair, x), k1 = pfx_run_of(t.pair, x + tiles - 1);
         pre_slot = 2 * (plan.pair_item[g] * kv + it + k0) + (tile & 1);
         pre_step = 2;
         n_pre = k1 - k0 + 1;
       } else {
         const int x = plan.single_base[g] + kvh * tiles;
-        const int k0 = pfx_run_of(x, t.line_tiles, t.line_runs), k1 = pfx_run_of(x + tiles - 1, t.line_tiles, t.line_runs);
+        const int k0 = pfx_run_of(t.line, x), k1 = pfx_run_of(t.line, x + tiles - 1);
         pre_slot = plan.single_item[g] * kv + kvh + k0;
         pre_step = 1;
         n_pre = k1 - k0 + 1;
@@ -767,77 +768,101 @@ __global__ void __launch_bounds__(kMergeThreads) prefix_merge_kernel(const PfxPa
     const int tiles = plan.cum[req + 1] - plan.cum[req];
     if (tiles > 0) {
       const int x = t.single_tiles + plan.cum[req] * kv + kvh * tiles;
-      const int k0 = pfx_run_of(x, t.line_tiles, t.line_runs), k1 = pfx_run_of(x + tiles - 1, t.line_tiles, t.line_runs);
+      const int k0 = pfx_run_of(t.line, x), k1 = pfx_run_of(t.line, x + tiles - 1);
       own_slot = req * kv + kvh + k0;
       n_own = k1 - k0 + 1;
     }
   }
   const int n = n_pre + n_own;
-  auto ml_at = [&](int s, int row) -> float2 {
-    return s < n_pre ? p.work.ml[kind][(size_t)(pre_slot + s * pre_step) * kPfxRows + row0 + row]
-                     : p.work.ml[kPfxOwn][(size_t)(own_slot + s - n_pre) * R + row];
-  };
-  for (int row = tid; row < R; row += kMergeThreads) {
-    float m = -INFINITY, l = 0.0f;
-    for (int s = 0; s < n; ++s) m = fmaxf(m, ml_at(s, row).x);
-    for (int s = 0; s < n; ++s) {
-      const float2 v = ml_at(s, row);
-      if (v.y > 0.0f) l += v.y * ex2_approx(v.x - m);
-    }
-    stat[row] = make_float2(m, l > 0.0f ? 1.0f / l : 0.0f);
-  }
-  __syncthreads();
-  // Elements are 4 columns of a row.  With fewer elements than threads,
-  // threads share an element, each taking every `parts`-th segment.
+  // Elements are 4 columns of a row, kEach per thread and pass.  With at most
+  // half as many elements as threads, `parts` threads share an element, each
+  // taking every parts-th segment.
   const int n_el = R * (D / 4);
-  const int parts = n_el >= kMergeThreads ? 1 : kMergeThreads / n_el;
+  const int parts = n_el > kMergeThreads / 2 ? 1 : min(kMergeThreads / n_el, 16);
+  const int chunk = min(kMergeStats / R, kMergeStats);  // segments whose (m, l) fit in shared memory
   uint16_t* out = O + ((size_t)req * p.n_heads + (size_t)kvh * p.group) * p.q_len * D;
-  for (int e0 = 0; e0 < n_el; e0 += kMergeThreads) {
-    const int e = parts > 1 ? tid % n_el : e0 + tid;
+  for (int e0 = 0; e0 < n_el; e0 += kMergeThreads * kMergeEach) {
     const int part = parts > 1 ? tid / n_el : 0;
-    const bool on = e < n_el && part < parts;
-    const int row = e % R, c = e / R;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int s0 = 0; s0 < n; s0 += kMergeChunk) {
-      const int ns = min(kMergeChunk, n - s0);
+    const int e_first = parts > 1 ? tid % n_el : e0 + tid;
+    float4 acc[kMergeEach];
+#pragma unroll
+    for (int k = 0; k < kMergeEach; ++k) acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int s0 = 0; s0 < n; s0 += chunk) {
+      const int ns = min(chunk, n - s0);
       __syncthreads();
       for (int k = tid; k < ns * R; k += kMergeThreads) {
-        const float2 v = ml_at(s0 + k / R, k % R);
-        const float2 st = stat[k % R];
-        weight[k / R][k % R] = v.y > 0.0f ? ex2_approx(v.x - st.x) * st.y : 0.0f;
+        const int s = s0 + k / R, row = k % R;
+        stats[k] = s < n_pre ? p.work.ml[kind][(size_t)(pre_slot + s * pre_step) * kPfxRows + row0 + row]
+                             : p.work.ml[kPfxOwn][(size_t)(own_slot + s - n_pre) * R + row];
       }
       __syncthreads();
-      if (on) {
-        for (int k = part; k < ns; k += parts) {
-          const int s = s0 + k;
-          const float wgt = weight[k][row];
-          if (wgt == 0.0f) continue;  // nothing was seen, or O was not written for it
-          const float4 v =
-              s < n_pre ? p.work.O[kind][((size_t)(pre_slot + s * pre_step) * (D / 4) + c) * kPfxRows + row0 + row]
-                        : p.work.O[kPfxOwn][((size_t)(own_slot + s - n_pre) * (D / 4) + c) * R + row];
-          acc.x += wgt * v.x;
-          acc.y += wgt * v.y;
-          acc.z += wgt * v.z;
-          acc.w += wgt * v.w;
+      // Per row: the maximum so far, the sum relative to it, and the factor
+      // of what has been accumulated; (m, l) become weights.
+      for (int row = tid; row < R; row += kMergeThreads) {
+        const float m_old = s0 > 0 ? row_max_sum[row].x : -INFINITY;
+        float m = m_old;
+        for (int s = 0; s < ns; ++s) m = fmaxf(m, stats[s * R + row].x);
+        const float f = m_old == -INFINITY ? 0.0f : ex2_approx(m_old - m);
+        float l = s0 > 0 ? row_max_sum[row].y * f : 0.0f;
+        for (int s = 0; s < ns; ++s) {
+          const float2 v = stats[s * R + row];
+          const float wgt = v.y > 0.0f ? ex2_approx(v.x - m) : 0.0f;
+          l += v.y * wgt;
+          stats[s * R + row].x = wgt;
+        }
+        row_max_sum[row] = make_float2(m, l);
+        row_factor[row] = f;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kMergeEach; ++k) {
+        const int e = e_first + k * kMergeThreads;
+        if (e >= n_el || part >= parts || (parts > 1 && k > 0)) continue;
+        const int row = e % R, c = e / R;
+        const float f = row_factor[row];
+        acc[k].x *= f;
+        acc[k].y *= f;
+        acc[k].z *= f;
+        acc[k].w *= f;
+#pragma unroll 4
+        for (int i = part; i < ns; i += parts) {
+          const int s = s0 + i;
+          const float4* from =
+              s < n_pre ? p.work.O[kind] + ((size_t)(pre_slot + s * pre_step) * (D / 4) + c) * kPfxRows + row0 + row
+                        : p.work.O[kPfxOwn] + ((size_t)(own_slot + s - n_pre) * (D / 4) + c) * R + row;
+          const float4 v = *from;
+          const float wgt = stats[i * R + row].x;
+          // A weight of 0: the row saw nothing there, and its sums may be anything.
+          acc[k].x += wgt > 0.0f ? wgt * v.x : 0.0f;
+          acc[k].y += wgt > 0.0f ? wgt * v.y : 0.0f;
+          acc[k].z += wgt > 0.0f ? wgt * v.z : 0.0f;
+          acc[k].w += wgt > 0.0f ? wgt * v.w : 0.0f;
         }
       }
     }
     if (parts > 1) {
-      sums[tid] = acc;
+      sums[tid] = acc[0];
       __syncthreads();
-      if (part == 0 && on) {
+      if (part == 0) {
         for (int k = 1; k < parts; ++k) {
           const float4 v = sums[tid + k * n_el];
-          acc.x += v.x;
-          acc.y += v.y;
-          acc.z += v.z;
-          acc.w += v.w;
+          acc[0].x += v.x;
+          acc[0].y += v.y;
+          acc[0].z += v.z;
+          acc[0].w += v.w;
         }
       }
     }
-    if (on && part == 0)
+#pragma unroll
+    for (int k = 0; k < kMergeEach; ++k) {
+      const int e = e_first + k * kMergeThreads;
+      if (e >= n_el || part > 0 || (parts > 1 && k > 0)) continue;
+      const int row = e % R, c = e / R;
+      const float l = n > 0 ? row_max_sum[row].y : 0.0f;
+      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
       *reinterpret_cast<uint2*>(out + (size_t)row * D + 4 * c) =
-          make_uint2(pack_16x2<FP16>(acc.x, acc.y), pack_16x2<FP16>(acc.z, acc.w));
+          make_uint2(pack_16x2<FP16>(acc[k].x * inv, acc[k].y * inv), pack_16x2<FP16>(acc[k].z * inv, acc[k].w * inv));
+    }
   }
 }
 
@@ -846,7 +871,6 @@ cudaError_t launch_prefix_instance(const PfxLaunch& L) {
   using C = PfxCfg<D>;
   auto kern = prefix_kernel<D, FP16>;
   const int smem = C::kSmemFixed + pfx_plan_ints(L.p.batch, L.p.n_groups) * 4;
-  // At least 116 KB, so that one CTA holds an SM's tensor memory at a time.
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        C::kSmemFixed + C::kMaxPlanBytes);
   if (e != cudaSuccess) return e;
