@@ -5,17 +5,22 @@
 //   warps 0-3, 4-7  softmax of stream 0 and 1: thread t of a warpgroup owns
 //                   query row t (TMEM lane t).  Reads S from tensor memory,
 //                   masks, keeps the row's running maximum and sum in fp32,
-//                   writes P over S as 16-bit pairs, rescales O when the
-//                   maximum moved by more than 2^8, and at the end of a
-//                   segment stores (m, l) and O to the workspace.  Warps
-//                   without a query row only keep the barriers going.
+//                   writes P as 16-bit pairs, rescales O when the maximum
+//                   moved by more than 2^8, and at the end of a segment stores
+//                   (m, l) and O to the workspace.  Warps without a query row
+//                   only keep the barriers going.
 //   warps 8, 11     producers: walk the tiles of stream 0 and 1, look their
 //                   pages up (a lane per page, one tile ahead), publish the
 //                   schedule and issue the TMA loads of Q, K and V.
-//   warps 9, 10     one thread each: the MMAs of stream 0 and 1.
-// TMEM: S and P of stream w at column 128 w, O at 256 + 128 w.  The two
-// streams alternate on the tensor cores: one computes while the other is in
-// its softmax.  K and V tiles go through a ring each in shared memory.
+//   warp 9          one thread: S = Q K^T of both streams, whichever is ready.
+//   warp 10         one thread: O += P V of both streams.
+// TMEM: S at column 0, P of stream w at 128 + 64 w, O at 256 + 128 w; with a
+// head dimension of 64 there is room for an S of each stream (stream 1's at
+// 384, O at 256 + 64 w).  S is handed to the next product as soon as it has
+// been read, so a stream's softmax runs beside the products of the other one
+// and beside its own next S.  (With P written over S, and one issuing thread a
+// stream, the next S had to wait for P V: 5250 clk a pair's tile of 128 + 128
+// rows at head dimension 128.)
 //
 // Every wait is bounded; one that runs out sets the status word and an abort
 // flag, and every role unwinds.
@@ -40,6 +45,10 @@ struct PfxCfg {
   static constexpr int kRegsOther = 88;
   static constexpr int kRingBytes = (2 + 2 * kSlots) * kTileBytes;  // two Q tiles, then the rings
   static constexpr int kMaxPlanBytes = 32 * 1024;
+  static constexpr int kSBufs = D == 64 ? 2 : 1;
+  static constexpr uint32_t kTmemP = 128, kTmemO = 256;
+  static constexpr uint32_t kTmemOStep = D == 64 ? 64 : 128;
+  static constexpr uint32_t kTmemS1 = 384;
   static constexpr int kSmemFixed = kRingBytes + 1024;  // and the plan behind
   static_assert(kSmemFixed + kMaxPlanBytes + 1024 <= 227 * 1024, "shared memory");
   static_assert(256 * kRegsSoftmax + 128 * kRegsOther <= kThreads * 168, "register split");
@@ -57,10 +66,11 @@ __device__ __forceinline__ int pfx_pack(int req, int nreq, int kind, int flags) 
 template <int NS>
 struct PfxShared {
   uint64_t k_full[NS], k_empty[NS], v_full[NS], v_empty[NS];  // empty: one arrival per stream
-  uint64_t sched_full[2][kPfxSched], sched_empty[2][kPfxSched];  // empty: the issuer and 4 warps
+  uint64_t sched_full[2][kPfxSched], sched_empty[2][kPfxSched];  // empty: the two issuers and 4 warps
   uint64_t q_full[2], q_free[2];
-  uint64_t s_full[2];  // S written
-  uint64_t p_full[2];  // P written (and S read, and O read where a segment ended): 4 warps
+  uint64_t s_full[2];  // S of a stream written
+  uint64_t s_free[2];  // S buffer read: 4 warps
+  uint64_t p_full[2];  // P written (and O read where a segment ended): 4 warps
   uint64_t o_full[2];  // P V completed
   uint64_t done[2];
   int4 sched[2][kPfxSched];
@@ -74,6 +84,7 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
   const CacheView& c = p.cache;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
   int bad = 0, bad_groups = 0;
+#pragma unroll 1
   for (int g = tid; g <= p.n_groups; g += blockDim.x) {
     if (p.n_groups == 0) break;
     const int a = p.group_start[g], e = g < p.n_groups ? p.group_start[g + 1] : a;
@@ -81,6 +92,7 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
     if (a < 0 || a > p.batch || a > e) bad_groups = 1;
     plan.start[g] = a;
   }
+#pragma unroll 1
   for (int r = tid; r < p.batch; r += blockDim.x) {
     const int s = p.slots[r];
     const int add = p.n_new ? p.n_new[r] : p.q_len;
@@ -100,10 +112,12 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
   }
   if (report && (bad | bad_groups)) atomicOr(c.status, kStatusBadCache);
   const bool grouped = !__syncthreads_or(bad_groups);
+#pragma unroll 1
   for (int g = warp; g < p.n_groups; g += n_warps) {
     const int a = plan.start[g], e = plan.start[g + 1];
     int shortest = INT_MAX, active = 0, lead = INT_MAX;
     if (grouped) {
+#pragma unroll 1
       for (int r = a + lane; r < e; r += 32) {
         const int len = plan.len[r];
         if (len > 0) {
@@ -125,6 +139,7 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
       plan.lead[g] = lead;
     }
     if (shared > 0) {
+#pragma unroll 1
       for (int r = a + lane; r < e; r += 32) {
         plan.lo[r] = shared;
         plan.group[r] = g;
@@ -134,11 +149,12 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
   __syncthreads();
   if (warp == 0) {
     int before = 0;
+#pragma unroll 1
     for (int r0 = 0; r0 < p.batch; r0 += 32) {
       const int r = r0 + lane;
       const int t = r < p.batch ? max(0, plan.len[r] - plan.lo[r] + kPfxKeys - 1) / kPfxKeys : 0;
       int v = t;
-#pragma unroll
+#pragma unroll 1
       for (int o = 1; o < 32; o <<= 1) {
         const int u = __shfl_up_sync(0xffffffffu, v, o);
         if (lane >= o) v += u;
@@ -149,6 +165,7 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
     if (lane == 0) plan.cum[p.batch] = before;
   } else if (warp == 1) {
     int b[4] = {0, 0, 0, 0};  // pair tiles, pair items, single tiles, single items
+#pragma unroll 1
     for (int g0 = 0; g0 < p.n_groups; g0 += 32) {
       const int g = g0 + lane;
       int own[4] = {0, 0, 0, 0}, v[4];
@@ -162,7 +179,7 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         v[k] = own[k];
-#pragma unroll
+#pragma unroll 1
         for (int o = 1; o < 32; o <<= 1) {
           const int u = __shfl_up_sync(0xffffffffu, v[k], o);
           if (lane >= o) v[k] += u;
@@ -426,72 +443,86 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
 }
 
 // --------------------------------------------------------------- MMA issuers
-// One thread per stream.
+// Both issuing threads take the streams in turn, tile by tile, until a stream
+// ends.  The streams' runs have equally many tiles up to one, so the fixed
+// order costs little; threads that poll both streams and take whichever is
+// ready load the shared-memory pipe so much that every other wait of the SM
+// slows down (94 us instead of 74 for 64 requests on a 32K prefix).
+struct PfxTurn {
+  int j;     // tile
+  int nq;    // segments started
+  bool end;
+};
+
+template <bool FP16>
+__device__ __forceinline__ constexpr uint32_t pfx_idesc(uint32_t bf16) {
+  return FP16 ? bf16 & ~((1u << 7) | (1u << 10)) : bf16;  // operand type 0: fp16, 1: bf16
+}
+
+// One thread: the S products.  (The two streams share one copy of the code, as
+// everywhere in this kernel: its loops together stay small enough for the
+// instruction cache, whose misses bounded larger variants.)
 template <int D, bool FP16>
-__device__ void pfx_mma(const PfxParams& p, int w, uint32_t tmem, uint8_t* q_tiles, uint8_t* ring,
-                        PfxShared<PfxCfg<D>::kSlots>& sb) {
+__device__ void pfx_mma_s(const PfxParams& p, uint32_t tmem, uint8_t* q_tiles, uint8_t* ring,
+                          PfxShared<PfxCfg<D>::kSlots>& sb) {
   using C = PfxCfg<D>;
-  constexpr int NS = C::kSlots;
   volatile int* abort = &sb.abort;
-  constexpr uint32_t fmt = FP16 ? ~((1u << 7) | (1u << 10)) : ~0u;  // operand type 0: fp16, 1: bf16
-  constexpr uint32_t idesc_s = idesc_bf16_f32(128, kPfxKeys, false, false) & fmt;
-  constexpr uint32_t idesc_o = idesc_bf16_f32(128, D, false, true) & fmt;
-  const uint32_t s_col = tmem + w * 128, o_col = tmem + 256 + w * 128;
-  int j = 0, nq = 0;
+  constexpr uint32_t idesc = pfx_idesc<FP16>(idesc_bf16_f32(128, kPfxKeys, false, false));
+  constexpr bool own_buf = C::kSBufs == 2;
+  PfxTurn t = {}, other = {};  // this turn's stream and the other one
+  int used = 0, used_other = 0;  // uses of the stream's S buffer
   bool ok = true;
-  for (;; ++j) {
-    const int e = j % kPfxSched;
-    if (!mbar_wait(&sb.sched_full[w][e], (j / kPfxSched) & 1, abort, p.wait_ns)) {
-      ok = false;
-      break;
-    }
-    const int4 ent = sb.sched[w][e];
-    mbar_arrive(&sb.sched_empty[w][e]);
-    const int flags = ent.z >> 19;
-    if (flags & kPfxEnd) break;
-    const bool pair = ((ent.z >> 17) & 3) == kPfxPair;
-    if ((flags & kPfxFirst) && !mbar_wait(&sb.q_full[w], nq++ & 1, abort, p.wait_ns)) {
-      ok = false;
-      break;
-    }
-    const int slot = ent.x & 255;
-    const uint32_t phase = ent.x >> 8;
-    if (!mbar_wait(&sb.k_full[slot], phase, abort, p.wait_ns)) {
-      ok = false;
-      break;
-    }
-    tc_fence_after_sync();
-    const uint64_t q0 = smem_desc_sw128(smem_u32(q_tiles + w * C::kTileBytes), 16, 1024);
-    const uint64_t k0 = smem_desc_sw128(smem_u32(ring + slot * C::kTileBytes), 16, 1024);
 #pragma unroll 1
-    for (int kk = 0; kk < D / 16; ++kk) {
-      const uint32_t off = ((kk >> 2) * (128 * 128) + (kk & 3) * 32) >> 4;
-      umma_bf16_ss(s_col, q0 + off, k0 + off, idesc_s, kk > 0 ? 1u : 0u);
-    }
-    umma_commit(&sb.s_full[w]);
-    // A slot is empty after two arrivals: one of each stream for a pair's
-    // tile, both from this one otherwise.
-    umma_commit(&sb.k_empty[slot]);
-    if (!pair) umma_commit(&sb.k_empty[slot]);
-    if (flags & kPfxLast) umma_commit(&sb.q_free[w]);
-    if (!mbar_wait(&sb.v_full[slot], phase, abort, p.wait_ns) ||
-        !mbar_wait(&sb.p_full[w], j & 1, abort, p.wait_ns)) {
-      ok = false;
-      break;
-    }
-    tc_fence_after_sync();
-    const uint64_t v0 = smem_desc_sw128(smem_u32(ring + (NS + slot) * C::kTileBytes), kPfxKeys * 128, 1024);
+  for (int w = 0; !(t.end && other.end); w ^= 1) {
+    if (!t.end) {
+      const int e = t.j % kPfxSched;
+      if (!mbar_wait(&sb.sched_full[w][e], (t.j / kPfxSched) & 1, abort, p.wait_ns)) {
+        ok = false;
+        break;
+      }
+      const int4 ent = sb.sched[w][e];
+      mbar_arrive(&sb.sched_empty[w][e]);
+      const int flags = ent.z >> 19, slot = ent.x & 255;
+      if (flags & kPfxEnd) {
+        t.end = true;
+      } else {
+        if (((flags & kPfxFirst) && !mbar_wait(&sb.q_full[w], t.nq++ & 1, abort, p.wait_ns)) ||
+            !mbar_wait(&sb.k_full[slot], ent.x >> 8, abort, p.wait_ns) ||
+            (used > 0 && !mbar_wait(&sb.s_free[own_buf ? w : 0], (used - 1) & 1, abort, p.wait_ns))) {
+          ok = false;
+          break;
+        }
+        tc_fence_after_sync();
+        const uint64_t q0 = smem_desc_sw128(smem_u32(q_tiles + w * C::kTileBytes), 16, 1024);
+        const uint64_t k0 = smem_desc_sw128(smem_u32(ring + slot * C::kTileBytes), 16, 1024);
+        const uint32_t s_col = tmem + (own_buf && w == 1 ? C::kTmemS1 : 0);
+        uint32_t acc = 0;
 #pragma unroll 1
-    for (int kk = 0; kk < kPfxKeys / 16; ++kk)
-      umma_bf16_ts(o_col, s_col + kk * 8, v0 + ((kk * 2048) >> 4), idesc_o,
-                   ((flags & kPfxFirst) && kk == 0) ? 0u : 1u);
-    umma_commit(&sb.o_full[w]);
-    umma_commit(&sb.v_empty[slot]);
-    if (!pair) umma_commit(&sb.v_empty[slot]);
-    // The next S overwrites P, which this product reads.
-    if (!mbar_wait(&sb.o_full[w], j & 1, abort, p.wait_ns)) {
-      ok = false;
-      break;
+        for (int kk = 0; kk < D / 16; kk += 2) {  // 32 columns at a time
+          const uint32_t off = ((kk >> 2) * (128 * 128) + (kk & 2) * 32) >> 4;
+          umma_ss_split(s_col, (uint32_t)q0 + off, (uint32_t)(q0 >> 32), (uint32_t)k0 + off, (uint32_t)(k0 >> 32), idesc,
+                        acc);
+          acc = 1;
+          umma_ss_split(s_col, (uint32_t)q0 + off + 2, (uint32_t)(q0 >> 32), (uint32_t)k0 + off + 2,
+                        (uint32_t)(k0 >> 32), idesc, acc);
+        }
+        umma_commit(&sb.s_full[w]);
+        // A slot is empty after two arrivals: one for each stream of a pair's
+        // tile, both for this one otherwise.
+        umma_commit(&sb.k_empty[slot]);
+        if (((ent.z >> 17) & 3) != kPfxPair) umma_commit(&sb.k_empty[slot]);
+        if (flags & kPfxLast) umma_commit(&sb.q_free[w]);
+        ++used;
+        ++t.j;
+      }
+    }
+    const PfxTurn swap = t;
+    t = other;
+    other = swap;
+    if (own_buf) {
+      const int u = used;
+      used = used_other;
+      used_other = u;
     }
   }
   if (!ok) {
@@ -499,9 +530,67 @@ __device__ void pfx_mma(const PfxParams& p, int w, uint32_t tmem, uint8_t* q_til
     atomicOr(p.cache.status, kStatusTimeout);
   }
   // Every MMA and commit of this thread completes before TMEM is released.
-  umma_commit(&sb.done[w]);
+  umma_commit(&sb.done[0]);
   int never = 0;
-  mbar_wait(&sb.done[w], 0, &never);
+  mbar_wait(&sb.done[0], 0, &never);
+}
+
+// One thread: the P V products.
+template <int D, bool FP16>
+__device__ void pfx_mma_pv(const PfxParams& p, uint32_t tmem, uint8_t* ring, PfxShared<PfxCfg<D>::kSlots>& sb) {
+  using C = PfxCfg<D>;
+  constexpr int NS = C::kSlots;
+  volatile int* abort = &sb.abort;
+  constexpr uint32_t idesc = pfx_idesc<FP16>(idesc_bf16_f32(128, D, false, true));
+  PfxTurn t = {}, other = {};
+  bool ok = true;
+#pragma unroll 1
+  for (int w = 0; !(t.end && other.end); w ^= 1) {
+    if (!t.end) {
+      const int e = t.j % kPfxSched;
+      if (!mbar_wait(&sb.sched_full[w][e], (t.j / kPfxSched) & 1, abort, p.wait_ns)) {
+        ok = false;
+        break;
+      }
+      const int4 ent = sb.sched[w][e];
+      mbar_arrive(&sb.sched_empty[w][e]);
+      const int flags = ent.z >> 19, slot = ent.x & 255;
+      if (flags & kPfxEnd) {
+        t.end = true;
+      } else {
+        if (!mbar_wait(&sb.v_full[slot], ent.x >> 8, abort, p.wait_ns) ||
+            !mbar_wait(&sb.p_full[w], t.j & 1, abort, p.wait_ns)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after_sync();
+        const uint64_t v0 = smem_desc_sw128(smem_u32(ring + (NS + slot) * C::kTileBytes), kPfxKeys * 128, 1024);
+        const uint32_t o_col = tmem + C::kTmemO + w * C::kTmemOStep, p_col = tmem + C::kTmemP + w * 64;
+        uint32_t acc = (flags & kPfxFirst) ? 0u : 1u;
+#pragma unroll 1
+        for (int kk = 0; kk < kPfxKeys / 16; kk += 2) {
+          const uint32_t v = (uint32_t)v0 + kk * (2048 / 16);
+          umma_ts_split(o_col, p_col + kk * 8, v, (uint32_t)(v0 >> 32), idesc, acc);
+          acc = 1;
+          umma_ts_split(o_col, p_col + kk * 8 + 8, v + 2048 / 16, (uint32_t)(v0 >> 32), idesc, acc);
+        }
+        umma_commit(&sb.o_full[w]);
+        umma_commit(&sb.v_empty[slot]);
+        if (((ent.z >> 17) & 3) != kPfxPair) umma_commit(&sb.v_empty[slot]);
+        ++t.j;
+      }
+    }
+    const PfxTurn swap = t;
+    t = other;
+    other = swap;
+  }
+  if (!ok) {
+    *reinterpret_cast<volatile int*>(&sb.abort) = 1;
+    atomicOr(p.cache.status, kStatusTimeout);
+  }
+  umma_commit(&sb.done[1]);
+  int never = 0;
+  mbar_wait(&sb.done[1], 0, &never);
 }
 
 // ------------------------------------------------------------------- softmax
@@ -525,7 +614,10 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
   volatile int* abort = &sb.abort;
   const int r = threadIdx.x & 127, wq = r >> 5, lane = r & 31;
   const uint32_t lane_tmem = tmem + ((uint32_t)(wq * 32) << 16);
-  const uint32_t s_col = w * 128, o_col = 256 + w * 128;
+  constexpr bool own_buf = C::kSBufs == 2;
+  const uint32_t s_col = own_buf && w == 1 ? C::kTmemS1 : 0, p_col = C::kTmemP + w * 64;
+  const uint32_t o_col = C::kTmemO + w * C::kTmemOStep;
+  uint64_t* s_free = &sb.s_free[own_buf ? w : 0];
   bool ok = true;
   int limit = 0, end = 0;       // keys the row may see; one past the item's keys
   bool row_on = false, warp_on = false;
@@ -562,27 +654,45 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
       break;
     }
     tc_fence_after_sync();
+    float f = 1.0f;
+    bool rescale = false;
+    uint32_t pw[kPfxKeys / 2];
     if (warp_on) {
       float s[kPfxKeys];
-      load_s_row<128>(lane_tmem + s_col, s, 1u, min(limit, end) - ent.y - 1);
+      tmem_load_row<kPfxKeys>(lane_tmem + s_col, s);
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(s_free);
+      mask_s_row<128>(s, 1u, min(limit, end) - ent.y - 1);
       const float m_tile = row_max(s) * p.scale_log2;
       const float m_new = (m_tile > m + kRescaleThreshold) ? m_tile : m;
-      const bool rescale = row_on && m_new != m && m != -INFINITY;
-      const float f = rescale ? ex2_approx(m - m_new) : 1.0f;
+      rescale = row_on && m_new != m && m != -INFINITY;
+      if (rescale) f = ex2_approx(m - m_new);
       const float sum = exp2_scaled(s, p.scale_log2, m_new == -INFINITY ? 0.0f : m_new);
       l = l * f + sum;
       m = m_new;
 #pragma unroll
+      for (int k = 0; k < kPfxKeys / 2; ++k) pw[k] = pack_16x2<FP16>(s[2 * k], s[2 * k + 1]);
+    } else if (lane == 0) {
+      mbar_arrive(s_free);
+    }
+    // P and O are at rest once the previous P V has completed.  (Warps without
+    // a row wait as well: their arrivals below must not run ahead.)
+    if (j > 0 && !warp_wait(&sb.o_full[w], (j - 1) & 1, abort, p.wait_ns)) {
+      ok = false;
+      break;
+    }
+    tc_fence_after_sync();
+    if (warp_on) {
+#pragma unroll
       for (int c = 0; c < kPfxKeys / 32; ++c) {
         uint32_t q[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) q[k] = pack_16x2<FP16>(s[32 * c + 2 * k], s[32 * c + 2 * k + 1]);
-        tmem_st_32x32b_x16(lane_tmem + s_col + 16 * c, q);
+        for (int k = 0; k < 16; ++k) q[k] = pw[16 * c + k];
+        tmem_st_32x32b_x16(lane_tmem + p_col + 16 * c, q);
       }
-      // S of this tile was issued after the previous P V had completed, so O
-      // is at rest here.
       if (__any_sync(0xffffffffu, rescale)) {
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < D / 16; ++c) {
           uint32_t v[16];
           tmem_ld_32x32b_x16(lane_tmem + o_col + 16 * c, v);
@@ -604,7 +714,9 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
       }
       if (r >= valid) {
         const uint32_t row = smem_u32(ring + (NS + (ent.x & 255)) * C::kTileBytes + r * 128);
+#pragma unroll 1
         for (int b = 0; b < C::kBoxes; ++b)
+#pragma unroll 1
           for (int k = 0; k < 8; ++k) st_shared_v4(row + b * 128 * 128 + k * 16, 0u, 0u, 0u, 0u);
         fence_proxy_async_smem();
       }
@@ -668,11 +780,12 @@ __global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
     for (int w = 0; w < 2; ++w) {
       for (int i = 0; i < kPfxSched; ++i) {
         mbar_init(&sb.sched_full[w][i], 1);
-        mbar_init(&sb.sched_empty[w][i], 5);
+        mbar_init(&sb.sched_empty[w][i], 6);
       }
       mbar_init(&sb.q_full[w], 1);
       mbar_init(&sb.q_free[w], 1);
       mbar_init(&sb.s_full[w], 1);
+      mbar_init(&sb.s_free[w], 4);
       mbar_init(&sb.p_full[w], 4);
       mbar_init(&sb.o_full[w], 1);
       mbar_init(&sb.done[w], 1);
@@ -704,12 +817,13 @@ __global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
     pfx_softmax<D, FP16>(p, plan, warp >> 2, tmem, ring, sb);
   } else {
     warpgroup_reg_dec<C::kRegsOther>();
-    if (warp == 8) {
-      pfx_producer<D>(&mapK, &mapV, &mapQ, &mapQ1, p, plan, 0, q_tiles, ring, sb);
-    } else if (warp == 11) {
-      pfx_producer<D>(&mapK, &mapV, &mapQ, &mapQ1, p, plan, 1, q_tiles, ring, sb);
-    } else {
-      if (lane == 0) pfx_mma<D, FP16>(p, warp - 9, tmem, q_tiles, ring, sb);
+    if (warp == 8 || warp == 11) {
+      pfx_producer<D>(&mapK, &mapV, &mapQ, &mapQ1, p, plan, warp == 11, q_tiles, ring, sb);
+    } else if (lane == 0) {
+      if (warp == 9)
+        pfx_mma_s<D, FP16>(p, tmem, q_tiles, ring, sb);
+      else
+        pfx_mma_pv<D, FP16>(p, tmem, ring, sb);
     }
   }
   __syncwarp();
@@ -723,144 +837,170 @@ __global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
 }
 
 // --------------------------------------------------------------------- merge
-// One block per (request, kv head): joins the partial results of its rows.
-constexpr int kMergeThreads = 256;
-constexpr int kMergeStats = 2048;  // (m, l) pairs in shared memory at a time
-constexpr int kMergeEach = 4;
+// Joins the partial results of one request and kv head; blockIdx.y takes a
+// share of the columns.  A thread owns 4 columns of one row (kMergeEach such
+// elements of the same row at a time); where a block has fewer elements than
+// threads, `parts` threads share an element, each taking every parts-th
+// segment.  What bounds it: a chain of four dependent loads (plan, group,
+// (m, l), O), so blocks are small and many share an SM.
+constexpr int kMergeThreads = 128;
+constexpr int kMergeStats = 1024;  // (m, l) pairs in shared memory at a time
+constexpr int kMergeEach = 2;
 
-template <int D, bool FP16>
-__global__ void __launch_bounds__(kMergeThreads) prefix_merge_kernel(const PfxParams p, uint16_t* O) {
-  __shared__ float2 stats[kMergeStats];
-  __shared__ float2 row_max_sum[kPfxRows];
-  __shared__ float row_factor[kPfxRows];
-  __shared__ float4 sums[kMergeThreads];
-  griddep_wait();
-  const PfxPlan plan = pfx_plan(p.work.plan, p.batch, p.n_groups);
+struct PfxMergeShape {
+  int log_rows;  // rows of a request rounded up to a power of two
+  int cols;      // groups of 4 columns of a block
+  int parts;
+};
+
+// Where the segments of a request and kv head lie: n_pre of the shared prefix
+// first, then n_own.
+struct PfxSources {
+  const float2* pre_ml;
+  const float2* own_ml;
+  const float4* pre_O;
+  const float4* own_O;
+  int n_pre, n, pre_step;
+};
+
+template <int D>
+__device__ __forceinline__ PfxSources pfx_sources(const PfxParams& p, const PfxPlan& plan, int req, int kvh) {
   const int kv = p.cache.n_kv_heads;
-  const int req = blockIdx.x / kv, kvh = blockIdx.x % kv;
-  const int R = p.rows, tid = threadIdx.x;
   const PfxTotals t = *plan.t;
-  // Segments of the shared prefix (first), then of the request's own keys.
-  int n_pre = 0, n_own = 0, pre_slot = 0, pre_step = 0, own_slot = 0, row0 = 0, kind = kPfxSingle;
-  const int g = plan.group[req];
-  if (plan.add[req] > 0 && plan.len[req] > 0) {
-    if (g >= 0) {
-      const int at = req - plan.start[g], tile = at / p.per_tile;
-      const int row_tiles = (plan.start[g + 1] - plan.start[g] + p.per_tile - 1) / p.per_tile;
-      const int tiles = plan.tiles[g], n_pairs = row_tiles / 2;
-      row0 = (at - tile * p.per_tile) * R;
-      if (tile < 2 * n_pairs) {
-        kind = kPfxPair;
-        const int it = kvh * n_pairs + tile / 2;
-        const int x = plan.pair_base[g] + it * tiles;
-        const int k0 = pfx_run_of(t.pair, x), k1 = pfx_run_of(t.pair, x + tiles - 1);
-        pre_slot = 2 * (plan.pair_item[g] * kv + it + k0) + (tile & 1);
-        pre_step = 2;
-        n_pre = k1 - k0 + 1;
-      } else {
-        const int x = plan.single_base[g] + kvh * tiles;
-        const int k0 = pfx_run_of(t.line, x), k1 = pfx_run_of(t.line, x + tiles - 1);
-        pre_slot = plan.single_item[g] * kv + kvh + k0;
-        pre_step = 1;
-        n_pre = k1 - k0 + 1;
-      }
-    }
-    const int tiles = plan.cum[req + 1] - plan.cum[req];
-    if (tiles > 0) {
-      const int x = t.single_tiles + plan.cum[req] * kv + kvh * tiles;
-      const int k0 = pfx_run_of(t.line, x), k1 = pfx_run_of(t.line, x + tiles - 1);
-      own_slot = req * kv + kvh + k0;
-      n_own = k1 - k0 + 1;
+  const int g = plan.group[req], own_tiles = plan.cum[req + 1] - plan.cum[req], own_first = plan.cum[req];
+  PfxSources s = {};
+  s.pre_step = 1;
+  if (plan.len[req] == 0) return s;
+  int pre_slot = 0, row0 = 0, kind = kPfxSingle;
+  if (g >= 0) {
+    const int start = plan.start[g], tiles = plan.tiles[g];
+    const int at = req - start, tile = at / p.per_tile;
+    const int row_tiles = (plan.start[g + 1] - start + p.per_tile - 1) / p.per_tile;
+    const int n_pairs = row_tiles / 2;
+    const bool pair = tile < 2 * n_pairs;
+    row0 = (at - tile * p.per_tile) * p.rows;
+    const int it = pair ? kvh * n_pairs + tile / 2 : kvh;
+    const int x = (pair ? plan.pair_base[g] : plan.single_base[g]) + it * tiles;
+    const PfxCuts cuts = pair ? t.pair : t.line;
+    const int k0 = pfx_run_of(cuts, x);
+    s.n_pre = pfx_run_of(cuts, x + tiles - 1) - k0 + 1;
+    if (pair) {
+      kind = kPfxPair;
+      pre_slot = 2 * (plan.pair_item[g] * kv + it + k0) + (tile & 1);
+      s.pre_step = 2;
+    } else {
+      pre_slot = plan.single_item[g] * kv + it + k0;
     }
   }
-  const int n = n_pre + n_own;
-  // Elements are 4 columns of a row, kEach per thread and pass.  With at most
-  // half as many elements as threads, `parts` threads share an element, each
-  // taking every parts-th segment.
-  const int n_el = R * (D / 4);
-  const int parts = n_el > kMergeThreads / 2 ? 1 : min(kMergeThreads / n_el, 16);
-  const int chunk = min(kMergeStats / R, kMergeStats);  // segments whose (m, l) fit in shared memory
-  uint16_t* out = O + ((size_t)req * p.n_heads + (size_t)kvh * p.group) * p.q_len * D;
-  for (int e0 = 0; e0 < n_el; e0 += kMergeThreads * kMergeEach) {
-    const int part = parts > 1 ? tid / n_el : 0;
-    const int e_first = parts > 1 ? tid % n_el : e0 + tid;
+  s.pre_ml = p.work.ml[kind] + (size_t)pre_slot * kPfxRows + row0;
+  s.pre_O = p.work.O[kind] + (size_t)pre_slot * kPfxRows * (D / 4) + row0;
+  s.n = s.n_pre;
+  if (own_tiles > 0) {
+    const int x = t.single_tiles + own_first * kv + kvh * own_tiles;
+    const int k0 = pfx_run_of(t.line, x);
+    s.n += pfx_run_of(t.line, x + own_tiles - 1) - k0 + 1;
+    const size_t own_slot = (size_t)req * kv + kvh + k0;
+    s.own_ml = p.work.ml[kPfxOwn] + own_slot * p.rows;
+    s.own_O = p.work.O[kPfxOwn] + own_slot * p.rows * (D / 4);
+  }
+  return s;
+}
+
+template <int D, bool FP16>
+__global__ void __launch_bounds__(kMergeThreads) prefix_merge_kernel(const PfxParams p, const PfxMergeShape sh,
+                                                                     uint16_t* O) {
+  __shared__ PfxSources src;
+  __shared__ float2 stats[kMergeStats];
+  __shared__ float4 sums[kMergeThreads];
+  __shared__ float part_l[kMergeThreads];
+  griddep_wait();
+  const int kv = p.cache.n_kv_heads;
+  const int req = blockIdx.x / kv, kvh = blockIdx.x - req * kv;
+  const int R = p.rows, tid = threadIdx.x;
+  if (tid == 0) src = pfx_sources<D>(p, pfx_plan(p.work.plan, p.batch, p.n_groups), req, kvh);
+  __syncthreads();
+  const PfxSources s = src;
+  const int row_mask = (1 << sh.log_rows) - 1;
+  const int row = tid & row_mask;
+  const int el = sh.cols << sh.log_rows;           // elements of this block
+  const int part = sh.parts > 1 ? tid / el : 0;    // more parts only where el <= half the threads
+  const int tid_e = tid - part * el;
+  const bool on = row < R && part < sh.parts;
+  const int c0 = blockIdx.y * sh.cols;
+  const int chunk = kMergeStats >> sh.log_rows;
+  uint16_t* out = O + (((size_t)req * p.n_heads + (size_t)kvh * p.group) * p.q_len + row) * D;
+  for (int e0 = 0; e0 < el; e0 += kMergeThreads * kMergeEach) {
     float4 acc[kMergeEach];
 #pragma unroll
     for (int k = 0; k < kMergeEach; ++k) acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int s0 = 0; s0 < n; s0 += chunk) {
-      const int ns = min(chunk, n - s0);
+    float m = -INFINITY, l = 0.0f;
+    for (int s0 = 0; s0 < s.n; s0 += chunk) {
+      const int ns = min(chunk, s.n - s0);
       __syncthreads();
-      for (int k = tid; k < ns * R; k += kMergeThreads) {
-        const int s = s0 + k / R, row = k % R;
-        stats[k] = s < n_pre ? p.work.ml[kind][(size_t)(pre_slot + s * pre_step) * kPfxRows + row0 + row]
-                             : p.work.ml[kPfxOwn][(size_t)(own_slot + s - n_pre) * R + row];
+      for (int k = tid; k < ns << sh.log_rows; k += kMergeThreads) {
+        const int i = s0 + (k >> sh.log_rows), rr = k & row_mask;
+        if (rr < R)
+          stats[k] = i < s.n_pre ? s.pre_ml[(size_t)i * s.pre_step * kPfxRows + rr] : s.own_ml[(size_t)(i - s.n_pre) * R + rr];
       }
       __syncthreads();
-      // Per row: the maximum so far, the sum relative to it, and the factor
-      // of what has been accumulated; (m, l) become weights.
-      for (int row = tid; row < R; row += kMergeThreads) {
-        const float m_old = s0 > 0 ? row_max_sum[row].x : -INFINITY;
-        float m = m_old;
-        for (int s = 0; s < ns; ++s) m = fmaxf(m, stats[s * R + row].x);
-        const float f = m_old == -INFINITY ? 0.0f : ex2_approx(m_old - m);
-        float l = s0 > 0 ? row_max_sum[row].y * f : 0.0f;
-        for (int s = 0; s < ns; ++s) {
-          const float2 v = stats[s * R + row];
-          const float wgt = v.y > 0.0f ? ex2_approx(v.x - m) : 0.0f;
-          l += v.y * wgt;
-          stats[s * R + row].x = wgt;
-        }
-        row_max_sum[row] = make_float2(m, l);
-        row_factor[row] = f;
-      }
-      __syncthreads();
+      if (!on) continue;
+      const float m_old = m;
+      for (int i = 0; i < ns; ++i) m = fmaxf(m, stats[(i << sh.log_rows) + row].x);
+      if (m == -INFINITY) continue;  // the row saw nothing yet
+      const float f = ex2_approx(m_old - m);
+      l *= f;
 #pragma unroll
       for (int k = 0; k < kMergeEach; ++k) {
-        const int e = e_first + k * kMergeThreads;
-        if (e >= n_el || part >= parts || (parts > 1 && k > 0)) continue;
-        const int row = e % R, c = e / R;
-        const float f = row_factor[row];
         acc[k].x *= f;
         acc[k].y *= f;
         acc[k].z *= f;
         acc[k].w *= f;
+      }
 #pragma unroll 4
-        for (int i = part; i < ns; i += parts) {
-          const int s = s0 + i;
-          const float4* from =
-              s < n_pre ? p.work.O[kind] + ((size_t)(pre_slot + s * pre_step) * (D / 4) + c) * kPfxRows + row0 + row
-                        : p.work.O[kPfxOwn] + ((size_t)(own_slot + s - n_pre) * (D / 4) + c) * R + row;
-          const float4 v = *from;
-          const float wgt = stats[i * R + row].x;
-          // A weight of 0: the row saw nothing there, and its sums may be anything.
-          acc[k].x += wgt > 0.0f ? wgt * v.x : 0.0f;
-          acc[k].y += wgt > 0.0f ? wgt * v.y : 0.0f;
-          acc[k].z += wgt > 0.0f ? wgt * v.z : 0.0f;
-          acc[k].w += wgt > 0.0f ? wgt * v.w : 0.0f;
+      for (int i = part; i < ns; i += sh.parts) {
+        const float2 st = stats[(i << sh.log_rows) + row];
+        const float w = ex2_approx(st.x - m);
+        const int g = s0 + i;
+        const bool pre = g < s.n_pre;
+        const float4* from =
+            pre ? s.pre_O + (size_t)g * s.pre_step * kPfxRows * (D / 4) : s.own_O + (size_t)(g - s.n_pre) * R * (D / 4);
+        const int stride = pre ? kPfxRows : R;
+        l += st.y * w;
+#pragma unroll
+        for (int k = 0; k < kMergeEach; ++k) {
+          const int e = tid_e + e0 + k * kMergeThreads;
+          if (e >= el) continue;
+          const float4 v = from[(c0 + (e >> sh.log_rows)) * stride + row];
+          // l of 0: the row saw nothing there, and its O is not defined.
+          const float u = st.y > 0.0f ? w : 0.0f;
+          acc[k].x += u > 0.0f ? u * v.x : 0.0f;
+          acc[k].y += u > 0.0f ? u * v.y : 0.0f;
+          acc[k].z += u > 0.0f ? u * v.z : 0.0f;
+          acc[k].w += u > 0.0f ? u * v.w : 0.0f;
         }
       }
     }
-    if (parts > 1) {
+    if (sh.parts > 1) {  // a single pass, one element a thread
       sums[tid] = acc[0];
+      part_l[tid] = l;
       __syncthreads();
       if (part == 0) {
-        for (int k = 1; k < parts; ++k) {
-          const float4 v = sums[tid + k * n_el];
+        for (int k = 1; k < sh.parts; ++k) {
+          const float4 v = sums[tid + k * el];
           acc[0].x += v.x;
           acc[0].y += v.y;
           acc[0].z += v.z;
           acc[0].w += v.w;
+          l += part_l[tid + k * el];
         }
       }
     }
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll
     for (int k = 0; k < kMergeEach; ++k) {
-      const int e = e_first + k * kMergeThreads;
-      if (e >= n_el || part > 0 || (parts > 1 && k > 0)) continue;
-      const int row = e % R, c = e / R;
-      const float l = n > 0 ? row_max_sum[row].y : 0.0f;
-      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-      *reinterpret_cast<uint2*>(out + (size_t)row * D + 4 * c) =
+      const int e = tid_e + e0 + k * kMergeThreads;
+      if (!on || part > 0 || e >= el) continue;
+      *reinterpret_cast<uint2*>(out + 4 * (c0 + (e >> sh.log_rows))) =
           make_uint2(pack_16x2<FP16>(acc[k].x * inv, acc[k].y * inv), pack_16x2<FP16>(acc[k].z * inv, acc[k].w * inv));
     }
   }
@@ -885,10 +1025,16 @@ cudaError_t launch_prefix_instance(const PfxLaunch& L) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   if ((e = cudaLaunchKernelEx(&cfg, kern, L.mapK, L.mapV, L.mapQ, L.mapQ1, L.p)) != cudaSuccess) return e;
-  cfg.gridDim = dim3(L.p.batch * L.p.cache.n_kv_heads);
+  // Shares of the columns: about two elements a thread.
+  PfxMergeShape sh = {0, D / 4, 1};
+  while ((1 << sh.log_rows) < L.p.rows) ++sh.log_rows;
+  while (sh.cols % 2 == 0 && (sh.cols << sh.log_rows) > kMergeThreads * kMergeEach) sh.cols /= 2;
+  sh.parts = kMergeThreads / (sh.cols << sh.log_rows);
+  if (sh.parts < 1) sh.parts = 1;
+  cfg.gridDim = dim3(L.p.batch * L.p.cache.n_kv_heads, D / 4 / sh.cols);
   cfg.blockDim = dim3(kMergeThreads);
   cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, prefix_merge_kernel<D, FP16>, L.p, reinterpret_cast<uint16_t*>(L.O));
+  return cudaLaunchKernelEx(&cfg, prefix_merge_kernel<D, FP16>, L.p, sh, reinterpret_cast<uint16_t*>(L.O));
 }
 
 template <int D>
