@@ -224,6 +224,18 @@ __device__ __forceinline__ int pfx_find(const int* base, int n, int x) {
   return lo;
 }
 
+// Waits of the producers and issuers: the polling loop is one function, to keep
+// their own loops short.
+static __device__ __noinline__ bool pfx_wait_long(uint64_t* bar, uint32_t parity, volatile int* abort, uint64_t limit_ns) {
+  return mbar_wait(bar, parity, abort, limit_ns);
+}
+__device__ __forceinline__ bool pfx_wait(uint64_t* bar, uint32_t parity, volatile int* abort, uint64_t limit_ns) {
+  return mbar_try_wait(bar, parity) || pfx_wait_long(bar, parity, abort, limit_ns);
+}
+__device__ __forceinline__ bool pfx_warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort, uint64_t limit_ns) {
+  return __all_sync(0xffffffffu, pfx_wait(bar, parity, abort, limit_ns));
+}
+
 // A segment: a run of key tiles of an item.
 struct PfxSeg {
   int word, word2;  // requests and kind as in a schedule entry; of a pair's second tile
@@ -345,27 +357,6 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
     if (lane * c.page < kPfxKeys && at < seg.end)
       page = __ldg(c.table + (size_t)seg.row * c.max_pages + at / c.page);
   };
-  auto load = [&](int r, const CUtensorMap* map, uint64_t* full, uint64_t* empty, int slot, int use) -> bool {
-    if (use >= 1 && !warp_wait(&empty[slot], (use - 1) & 1, abort, p.wait_ns)) return false;
-    // One lane per page of the tile that the item reaches.
-    const bool on = lane * c.page < kPfxKeys && seg.pos + lane * c.page < seg.end;
-    const int n_on = min(kPfxKeys / c.page, (seg.end - seg.pos + c.page - 1) / c.page);
-    if (lane == 0) mbar_arrive_expect_tx(&full[slot], n_on * c.page * 128 * C::kBoxes);
-    __syncwarp();
-    if (on) {
-      // A faulty page id becomes a coordinate out of range, which reads zeros.
-      const bool valid = page >= 0 && page < c.n_pages;
-      if (!valid) bad = 1;
-      const int z = valid ? page * c.n_kv_heads + seg.kvh : c.n_pages * c.n_kv_heads;
-      uint8_t* dst = ring + (r * NS + slot) * C::kTileBytes + lane * c.page * 128;
-      for (int b = 0; b < C::kBoxes; ++b) tma_load_3d(dst + b * 128 * 128, map, &full[slot], 64 * b, 0, z);
-    }
-    const uint32_t bit = 1u << (r * 8 + slot);
-    issued |= bit;
-    parity = (use & 1) ? parity | bit : parity & ~bit;
-    return true;
-  };
-
   for (;;) {
     if (seg.left == 0) {
       if (x == x_end) {
@@ -391,37 +382,63 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
     const int use = pair ? n / NS : n / H + (n_pair - slot + NS - 1) / NS;
     const int word = second ? seg.word2 : seg.word;
     const int e = n_ent % kPfxSched;
-    if (n_ent >= kPfxSched) ok = warp_wait(&sb.sched_empty[w][e], ((n_ent / kPfxSched) - 1) & 1, abort, p.wait_ns);
+    if (n_ent >= kPfxSched) ok = pfx_warp_wait(&sb.sched_empty[w][e], ((n_ent / kPfxSched) - 1) & 1, abort, p.wait_ns);
     if (ok && lane == 0) {
       const int flags = (first ? kPfxFirst : 0) | (seg.left == 1 ? kPfxLast : 0);
       sb.sched[w][e] = make_int4(slot | (use & 1) << 8, seg.pos, word | flags << 19, seg.slot + second);
       mbar_arrive(&sb.sched_full[w][e]);
     }
     ++n_ent;
-    if (ok && (!pair || w == 0)) ok = load(0, mapK, sb.k_full, sb.k_empty, slot, use);
-    if (ok && first) {
-      if (n_q >= 1) ok = warp_wait(&sb.q_free[w], (n_q - 1) & 1, abort, p.wait_ns);
-      if (ok && lane == 0) {
-        const bool own = ((word >> 17) & 3) == kPfxOwn;
-        mbar_arrive_expect_tx(&sb.q_full[w], (own ? p.rows : p.rows * p.per_tile) * 128 * C::kBoxes);
+    // The tile of the K ring (r = 0) and of the V ring; Q in between.  One lane
+    // per page that the item reaches.
+    const bool on = lane * c.page < kPfxKeys && seg.pos + lane * c.page < seg.end;
+    const bool valid = page >= 0 && page < c.n_pages;
+    if (on && !valid) bad = 1;
+    // A faulty page id becomes a coordinate out of range, which reads zeros.
+    const int z = valid ? page * c.n_kv_heads + seg.kvh : c.n_pages * c.n_kv_heads;
+    const int bytes = min(kPfxKeys, (seg.end - seg.pos + c.page - 1) / c.page * c.page) * 128 * C::kBoxes;
+#pragma unroll 1
+    for (int r = pair ? w : 0; ok && r <= (pair ? w : 1); ++r) {
+      uint64_t* full = r ? &sb.v_full[slot] : &sb.k_full[slot];
+      uint64_t* empty = r ? &sb.v_empty[slot] : &sb.k_empty[slot];
+      if (use >= 1) ok = pfx_warp_wait(empty, (use - 1) & 1, abort, p.wait_ns);
+      if (!ok) break;
+      if (lane == 0) mbar_arrive_expect_tx(full, bytes);
+      __syncwarp();
+      if (on) {
+        uint8_t* dst = ring + (r * NS + slot) * C::kTileBytes + lane * c.page * 128;
+#pragma unroll
         for (int b = 0; b < C::kBoxes; ++b)
-          tma_load_4d(q_tiles + w * C::kTileBytes + b * 128 * 128, own ? mapQ1 : mapQ, &sb.q_full[w], 64 * b, 0,
-                      seg.kvh, word & 1023);
+          tma_load_3d(dst + b * 128 * 128, r ? mapV : mapK, full, 64 * b, 0, z);
       }
-      if (ok) ++n_q;
+      const uint32_t bit = 1u << (r * 8 + slot);
+      issued |= bit;
+      parity = (use & 1) ? parity | bit : parity & ~bit;
+      if (first) {
+        first = false;
+        if (n_q >= 1) ok = pfx_warp_wait(&sb.q_free[w], (n_q - 1) & 1, abort, p.wait_ns);
+        if (!ok) break;
+        if (lane == 0) {
+          const bool own = ((word >> 17) & 3) == kPfxOwn;
+          mbar_arrive_expect_tx(&sb.q_full[w], (own ? p.rows : p.rows * p.per_tile) * 128 * C::kBoxes);
+#pragma unroll
+          for (int b = 0; b < C::kBoxes; ++b)
+            tma_load_4d(q_tiles + w * C::kTileBytes + b * 128 * 128, own ? mapQ1 : mapQ, &sb.q_full[w], 64 * b, 0,
+                        seg.kvh, word & 1023);
+        }
+        ++n_q;
+      }
     }
-    if (ok && (!pair || w == 1)) ok = load(1, mapV, sb.v_full, sb.v_empty, slot, use);
     if (!ok) break;
     ++n;
     --seg.left;
     seg.pos += kPfxKeys;
-    first = false;
     if (seg.left > 0) fetch();
   }
   if (had_pairs && pair) named_barrier_sync(1, 64);  // gave up before the end of the pair phase
   if (ok) {
     const int e = n_ent % kPfxSched;
-    if (n_ent >= kPfxSched) ok = warp_wait(&sb.sched_empty[w][e], ((n_ent / kPfxSched) - 1) & 1, abort, p.wait_ns);
+    if (n_ent >= kPfxSched) ok = pfx_warp_wait(&sb.sched_empty[w][e], ((n_ent / kPfxSched) - 1) & 1, abort, p.wait_ns);
     if (ok && lane == 0) {
       sb.sched[w][e] = make_int4(0, 0, kPfxEnd << 19, 0);
       mbar_arrive(&sb.sched_full[w][e]);
@@ -476,7 +493,7 @@ __device__ void pfx_mma_s(const PfxParams& p, uint32_t tmem, uint8_t* q_tiles, u
   for (int w = 0; !(t.end && other.end); w ^= 1) {
     if (!t.end) {
       const int e = t.j % kPfxSched;
-      if (!mbar_wait(&sb.sched_full[w][e], (t.j / kPfxSched) & 1, abort, p.wait_ns)) {
+      if (!pfx_wait(&sb.sched_full[w][e], (t.j / kPfxSched) & 1, abort, p.wait_ns)) {
         ok = false;
         break;
       }
@@ -486,9 +503,9 @@ __device__ void pfx_mma_s(const PfxParams& p, uint32_t tmem, uint8_t* q_tiles, u
       if (flags & kPfxEnd) {
         t.end = true;
       } else {
-        if (((flags & kPfxFirst) && !mbar_wait(&sb.q_full[w], t.nq++ & 1, abort, p.wait_ns)) ||
-            !mbar_wait(&sb.k_full[slot], ent.x >> 8, abort, p.wait_ns) ||
-            (used > 0 && !mbar_wait(&sb.s_free[own_buf ? w : 0], (used - 1) & 1, abort, p.wait_ns))) {
+        if (((flags & kPfxFirst) && !pfx_wait(&sb.q_full[w], t.nq++ & 1, abort, p.wait_ns)) ||
+            !pfx_wait(&sb.k_full[slot], ent.x >> 8, abort, p.wait_ns) ||
+            (used > 0 && !pfx_wait(&sb.s_free[own_buf ? w : 0], (used - 1) & 1, abort, p.wait_ns))) {
           ok = false;
           break;
         }
@@ -548,7 +565,7 @@ __device__ void pfx_mma_pv(const PfxParams& p, uint32_t tmem, uint8_t* ring, Pfx
   for (int w = 0; !(t.end && other.end); w ^= 1) {
     if (!t.end) {
       const int e = t.j % kPfxSched;
-      if (!mbar_wait(&sb.sched_full[w][e], (t.j / kPfxSched) & 1, abort, p.wait_ns)) {
+      if (!pfx_wait(&sb.sched_full[w][e], (t.j / kPfxSched) & 1, abort, p.wait_ns)) {
         ok = false;
         break;
       }
@@ -558,8 +575,8 @@ __device__ void pfx_mma_pv(const PfxParams& p, uint32_t tmem, uint8_t* ring, Pfx
       if (flags & kPfxEnd) {
         t.end = true;
       } else {
-        if (!mbar_wait(&sb.v_full[slot], ent.x >> 8, abort, p.wait_ns) ||
-            !mbar_wait(&sb.p_full[w], t.j & 1, abort, p.wait_ns)) {
+        if (!pfx_wait(&sb.v_full[slot], ent.x >> 8, abort, p.wait_ns) ||
+            !pfx_wait(&sb.p_full[w], t.j & 1, abort, p.wait_ns)) {
           ok = false;
           break;
         }
