@@ -4,14 +4,20 @@
 // every result is a function of the inputs alone, whatever order the threads
 // run in: pages are taken and moved by rank (prefix sums over refs), and the
 // atomics below are integer additions and ORs whose order does not show.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "internal.cuh"
+#include "ptx.cuh"
 
 namespace wise {
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr int kPlanThreads = 1024;
+constexpr int kPlanWarps = kPlanThreads / 32;
 
 __device__ __forceinline__ void fault(const CacheView& c, int bits) { atomicOr(c.status, bits); }
 
@@ -112,6 +118,85 @@ __device__ __forceinline__ int block_scan(int v, int* warp_sums, int& total) {
   return capped_sum(v, before);
 }
 
+// Ranks of the pages in use, over one cluster of 1 or 8 blocks.  A warp owns a
+// contiguous part of refs and passes over it twice, coalesced: once to count,
+// once (after the sums have been exchanged through distributed shared memory)
+// to hand each page its rank.
+struct PageScan {
+  int v0, v1;   // this warp's pages
+  int before;   // pages in use below v0
+  int total;    // pages in use
+};
+constexpr int kScanUnroll = 8;
+
+__device__ __forceinline__ int count_used(const CacheView& c, int v0, int v1, int lane) {
+  int n = 0;
+  for (int base = v0 + lane; base < v1; base += 32 * kScanUnroll) {
+    int r[kScanUnroll];
+#pragma unroll
+    for (int k = 0; k < kScanUnroll; ++k) r[k] = base + 32 * k < v1 ? c.refs[base + 32 * k] : 0;
+#pragma unroll
+    for (int k = 0; k < kScanUnroll; ++k) n += r[k] != 0;
+  }
+  return __reduce_add_sync(0xffffffffu, n);
+}
+
+// All threads of the cluster; `sums` (kPlanWarps ints) and `block_sum` are
+// shared memory.  The first pass; ends with a cluster barrier.
+__device__ __forceinline__ PageScan scan_pages(const CacheView& c, const cg::cluster_group& cluster, int* sums,
+                                               int* block_sum) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int n_warps = cluster.num_blocks() * kPlanWarps;
+  const int part = (c.n_pages + n_warps - 1) / n_warps;
+  PageScan s;
+  s.v0 = (int)min((long long)(cluster.block_rank() * kPlanWarps + w) * part, (long long)c.n_pages);
+  s.v1 = min(s.v0 + part, c.n_pages);
+  const int n = count_used(c, s.v0, s.v1, lane);
+  if (lane == 0) sums[w] = n;
+  __syncthreads();
+  if (w == 0) {
+    const int all = __reduce_add_sync(0xffffffffu, sums[lane]);
+    if (lane == 0) *block_sum = all;
+  }
+  cluster.sync();
+  s.before = 0;
+  s.total = 0;
+  for (int k = 0; k < (int)cluster.num_blocks(); ++k) {
+    const int t = *cluster.map_shared_rank(block_sum, k);
+    if (k < (int)cluster.block_rank()) s.before += t;
+    s.total += t;
+  }
+  const int mine = lane < w ? sums[lane] : 0;
+  s.before += __reduce_add_sync(0xffffffffu, mine);
+  return s;
+}
+
+// The second pass: visit(page, in use, pages in use below it) for the warp's pages.
+template <class Visit>
+__device__ __forceinline__ void visit_pages(const CacheView& c, const PageScan& s, Visit visit) {
+  const int lane = threadIdx.x & 31;
+  int before = s.before;
+  for (int base = s.v0; base < s.v1; base += 32 * kScanUnroll) {
+    int r[kScanUnroll];
+#pragma unroll
+    for (int k = 0; k < kScanUnroll; ++k) {
+      const int page = base + 32 * k + lane;
+      r[k] = page < s.v1 ? c.refs[page] : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < kScanUnroll; ++k) {
+      const int page = base + 32 * k + lane;
+      const uint32_t used = __ballot_sync(0xffffffffu, r[k] != 0);
+      if (page < s.v1) visit(page, r[k] != 0, before + __popc(used & ((1u << lane) - 1u)));
+      before += __popc(used);
+    }
+  }
+}
+
+// Blocks of a plan: one up to 8192 pages, where a block's two passes take less
+// than the cluster's barriers.
+inline int plan_blocks(const CacheView& c) { return c.n_pages <= 8192 ? 1 : 8; }
+
 // Workspace words: [0] number of copies; then the free list, the entries'
 // needs, and the copies as (from, to, rows).
 struct ExtendWork {
@@ -131,68 +216,73 @@ __host__ __device__ inline ExtendWork extend_work(int32_t* w, int n_pages, int n
 constexpr int kNeedCopy = 1 << 30;  // flag beside an entry's number of pages
 constexpr int kNeedNone = -1;       // unused or faulty entry
 
-// One block.  (1) the need of every entry from the state before the call,
-// (2) the lowest free pages, as many as are needed, (3) their assignment.
+// One cluster.  Block 0 finds the need of every entry from the state before
+// the call while all of them count the pages in use; then the lowest free
+// pages are listed, as many as are needed, and block 0 assigns them.
 __global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const CacheView c, const int32_t* slots,
                                                                    const int32_t* n_new, int n, int32_t* granted,
                                                                    int32_t* work) {
   extern __shared__ uint32_t seen[];  // two bitmaps over the slots: listed, listed twice
-  __shared__ int warp_sums[kPlanThreads / 32];
-  __shared__ int n_copies;
+  __shared__ int warp_sums[kPlanWarps], scan_sums[kPlanWarps];
+  __shared__ int block_used, total_want, n_copies;
+  const cg::cluster_group cluster = cg::this_cluster();
+  const bool lead = cluster.block_rank() == 0;
   const ExtendWork w = extend_work(work, c.n_pages, n);
-  const int words = (c.n_slots + 31) / 32;
-  uint32_t* twice = seen + words;
-  for (int k = threadIdx.x; k < 2 * words; k += kPlanThreads) seen[k] = 0;
-  if (threadIdx.x == 0) n_copies = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kPlanThreads) {
-    const int s = slots[i];
-    if (s >= 0 && s < c.n_slots) {
-      const uint32_t bit = 1u << (s & 31);
-      if (atomicOr(&seen[s >> 5], bit) & bit) atomicOr(&twice[s >> 5], bit);
+  griddep_launch_dependents();  // the copies wait for this grid's end
+  if (lead) {
+    const int words = (c.n_slots + 31) / 32;
+    uint32_t* twice = seen + words;
+    for (int k = threadIdx.x; k < 2 * words; k += kPlanThreads) seen[k] = 0;
+    if (threadIdx.x == 0) n_copies = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+      const int s = slots[i];
+      if (s >= 0 && s < c.n_slots) {
+        const uint32_t bit = 1u << (s & 31);
+        if (atomicOr(&seen[s >> 5], bit) & bit) atomicOr(&twice[s >> 5], bit);
+      }
     }
-  }
-  __syncthreads();
-  int want = 0;
-  for (int i = threadIdx.x; i < n; i += kPlanThreads) {
-    const int s = slots[i], add = n_new[i];
-    int need = kNeedNone;
-    if (s >= 0) {
-      const bool in = s < c.n_slots;
-      const int len = in ? c.lens[s] : -1;
-      if (!in || add < 0 || ((twice[s >> 5] >> (s & 31)) & 1u) || len < 0 || len > c.max_len) {
-        fault(c, kStatusBadCache);
-      } else if (add > c.max_len - len) {
-        fault(c, kStatusNoPages);
-      } else {
-        need = pages_of(c, len + add) - pages_of(c, len);
-        if (add > 0 && len % c.page != 0) {
-          const int tail = c.table[(size_t)s * c.max_pages + len / c.page];
-          if (!valid_page(c, tail)) {
-            fault(c, kStatusBadCache);
-            need = kNeedNone;
-          } else if (c.refs[tail] > 1) {
-            need = (need + 1) | kNeedCopy;
+    __syncthreads();
+    int want = 0;
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+      const int s = slots[i], add = n_new[i];
+      int need = kNeedNone;
+      if (s >= 0) {
+        const bool in = s < c.n_slots;
+        const int len = in ? c.lens[s] : -1;
+        if (!in || add < 0 || ((twice[s >> 5] >> (s & 31)) & 1u) || len < 0 || len > c.max_len) {
+          fault(c, kStatusBadCache);
+        } else if (add > c.max_len - len) {
+          fault(c, kStatusNoPages);
+        } else {
+          need = pages_of(c, len + add) - pages_of(c, len);
+          if (add > 0 && len % c.page != 0) {
+            const int tail = c.table[(size_t)s * c.max_pages + len / c.page];
+            if (!valid_page(c, tail)) {
+              fault(c, kStatusBadCache);
+              need = kNeedNone;
+            } else if (c.refs[tail] > 1) {
+              need = (need + 1) | kNeedCopy;
+            }
           }
         }
       }
+      w.need[i] = need;
+      if (need != kNeedNone) want = capped_sum(want, need & ~kNeedCopy);
     }
-    w.need[i] = need;
-    if (need != kNeedNone) want = capped_sum(want, need & ~kNeedCopy);
-  }
-  int total_want;
-  block_scan(want, warp_sums, total_want);
-  // Free pages in ascending order.
-  int found = 0;
-  for (int base = 0; base < c.n_pages && found < total_want; base += kPlanThreads) {
-    const int page = base + threadIdx.x;
-    const int is_free = page < c.n_pages && c.refs[page] == 0;
     int t;
-    const int upto = block_scan(is_free, warp_sums, t);
-    if (is_free) w.free_ids[found + upto - 1] = page;
-    found += t;
+    block_scan(want, warp_sums, t);
+    if (threadIdx.x == 0) total_want = t;
   }
-  __syncthreads();
+  const PageScan scan = scan_pages(c, cluster, scan_sums, &block_used);
+  const int wanted = *cluster.map_shared_rank(&total_want, 0);
+  const int found = min(wanted, c.n_pages - scan.total);
+  if (scan.v0 - scan.before < found)  // a free page of this warp's is among the first
+    visit_pages(c, scan, [&](int page, bool used, int below) {
+      if (!used && page - below < found) w.free_ids[page - below] = page;
+    });
+  cluster.sync();  // the list is complete, and the blocks' sums have been read
+  if (!lead) return;
   // Assignment, in list order.
   int carry = 0;
   for (int base = 0; base < n; base += kPlanThreads) {
@@ -241,6 +331,7 @@ __global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const CacheVi
 // Copies the first `rows` rows of every head of a page, in every plane; one
 // block per (copy, plane, head) in turn.
 __global__ void __launch_bounds__(256) copy_tails_kernel(const CacheView c, int32_t* work, int n) {
+  griddep_wait();
   const ExtendWork w = extend_work(work, c.n_pages, n);
   const long long jobs = (long long)*w.count * c.n_planes * c.n_kv_heads;
   for (long long job = blockIdx.x; job < jobs; job += gridDim.x) {
@@ -292,41 +383,45 @@ __global__ void __launch_bounds__(256) write_kernel(const CacheView c, int layer
 }
 
 // ------------------------------------------------------------------- compact
-// Workspace words: [0] number of moves; then the holes and the pages that
-// move into them, both ascending.
+// Workspace words: [0] number of moves; then the holes below n_live ascending,
+// and the pages that move into them descending.
+//
+// With u(g) = the pages in use below page g: a hole g has rank g - u(g) among
+// the free pages, hence among the holes; a page in use g >= n_live comes
+// n_live - 1 - u(g) places before the last one; and the number of moves is
+// n_live - u(n_live).
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const CacheView c, int32_t* remap,
                                                                     int32_t* n_live_out, int32_t* work) {
-  __shared__ int warp_sums[kPlanThreads / 32];
+  __shared__ int scan_sums[kPlanWarps];
+  __shared__ int block_used;
+  const cg::cluster_group cluster = cg::this_cluster();
+  griddep_launch_dependents();  // the moves wait for this grid's end
   int32_t* holes = work + 4;
   int32_t* movers = holes + c.n_pages;
-  int mine = 0, n_live;
-  for (int page = threadIdx.x; page < c.n_pages; page += kPlanThreads) mine += c.refs[page] != 0;
-  block_scan(mine, warp_sums, n_live);
-  int n_holes = 0, n_movers = 0;
-  for (int base = 0; base < c.n_pages; base += kPlanThreads) {
-    const int page = base + threadIdx.x;
-    const bool in = page < c.n_pages;
-    const bool live = in && c.refs[page] != 0;
-    const int hole = in && !live && page < n_live, mover = live && page >= n_live;
-    int t;
-    const int h = block_scan(hole, warp_sums, t);
-    if (hole) holes[n_holes + h - 1] = page;
-    n_holes += t;
-    const int m = block_scan(mover, warp_sums, t);
-    if (mover) movers[n_movers + m - 1] = page;
-    n_movers += t;
-    if (in && !mover) remap[page] = live ? page : -1;
+  const PageScan scan = scan_pages(c, cluster, scan_sums, &block_used);
+  const int n_live = scan.total;
+  visit_pages(c, scan, [&](int page, bool used, int below) {
+    if (page < n_live) {
+      remap[page] = used ? page : -1;
+      if (!used) holes[page - below] = page;
+    } else if (used) {
+      movers[n_live - 1 - below] = page;
+    } else {
+      remap[page] = -1;
+    }
+    if (page == n_live) work[0] = n_live - below;
+  });
+  if (cluster.block_rank() == 0 && threadIdx.x == 0) {
+    *n_live_out = n_live;
+    if (n_live == c.n_pages) work[0] = 0;  // no page lies past them
   }
-  __syncthreads();
-  for (int k = threadIdx.x; k < n_movers; k += kPlanThreads) {
-    const int from = movers[k], to = holes[k];
+  cluster.sync();
+  const int n_moves = *reinterpret_cast<volatile int32_t*>(work);
+  for (int k = cluster.block_rank() * kPlanThreads + threadIdx.x; k < n_moves; k += cluster.num_blocks() * kPlanThreads) {
+    const int from = movers[n_moves - 1 - k], to = holes[k];
     remap[from] = to;
     c.refs[to] = c.refs[from];
     c.refs[from] = 0;
-  }
-  if (threadIdx.x == 0) {
-    work[0] = n_movers;
-    *n_live_out = n_live;
   }
 }
 
@@ -334,17 +429,19 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const CacheV
 // copies are independent) and renames the tables' entries.
 __global__ void __launch_bounds__(256) compact_move_kernel(const CacheView c, const int32_t* remap,
                                                            const int32_t* work) {
+  griddep_wait();
   const int32_t* holes = work + 4;
   const int32_t* movers = holes + c.n_pages;
+  const int n_moves = work[0];
   constexpr int kPiece = 16384;  // bytes of a page one block copies at a time
   const int pieces = (c.page_bytes + kPiece - 1) / kPiece;
-  const long long jobs = (long long)work[0] * c.n_planes * pieces;
+  const long long jobs = (long long)n_moves * c.n_planes * pieces;
   for (long long job = blockIdx.x; job < jobs; job += gridDim.x) {
     const int piece = (int)(job % pieces);
     const long long r = job / pieces;
     const int plane = (int)(r % c.n_planes), at = (int)(r / c.n_planes);
     uint8_t* base = c.pool + plane * c.plane_bytes + (size_t)piece * kPiece;
-    const uint4* from = reinterpret_cast<const uint4*>(base + (size_t)movers[at] * c.page_bytes);
+    const uint4* from = reinterpret_cast<const uint4*>(base + (size_t)movers[n_moves - 1 - at] * c.page_bytes);
     uint4* to = reinterpret_cast<uint4*>(base + (size_t)holes[at] * c.page_bytes);
     const int units = min(kPiece, c.page_bytes - piece * kPiece) / 16;
     for (int k = threadIdx.x; k < units; k += blockDim.x) to[k] = from[k];
@@ -384,15 +481,47 @@ cudaError_t launch_kv_drop(const CacheView& c, const int32_t* slots, const int32
   return cudaGetLastError();
 }
 
+// A kernel that waits for the previous one itself (griddep_wait).
+template <class... Args>
+static cudaError_t launch_dependent(void (*kernel)(Args...), int grid, int threads, cudaStream_t stream, Args... args) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <class... Args>
+static cudaError_t launch_plan(void (*kernel)(Args...), int blocks, int smem, cudaStream_t stream, Args... args) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = blocks;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(kPlanThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 cudaError_t launch_kv_extend(const CacheView& c, const int32_t* slots, const int32_t* n_new, int n, int32_t* granted,
                              int32_t* work, int sm_count, cudaStream_t stream) {
   const int smem = 2 * ((c.n_slots + 31) / 32) * 4;
-  cudaError_t e = cudaFuncSetAttribute(extend_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = cudaSuccess;
+  if (smem > 40 * 1024)
+    e = cudaFuncSetAttribute(extend_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess)
+    e = launch_plan(extend_plan_kernel, plan_blocks(c), smem, stream, c, slots, n_new, n, granted, work);
   if (e != cudaSuccess) return e;
-  extend_plan_kernel<<<1, kPlanThreads, smem, stream>>>(c, slots, n_new, n, granted, work);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  copy_tails_kernel<<<sm_count * 8, 256, 0, stream>>>(c, work, n);
-  return cudaGetLastError();
+  return launch_dependent(copy_tails_kernel, sm_count * 8, 256, stream, c, work, n);
 }
 
 cudaError_t launch_kv_write(const CacheView& c, int layer, const int32_t* slots, const int32_t* n_new, int batch,
@@ -406,11 +535,10 @@ cudaError_t launch_kv_write(const CacheView& c, int layer, const int32_t* slots,
 
 cudaError_t launch_kv_compact(const CacheView& c, int32_t* remap, int32_t* n_live, int32_t* work, int sm_count,
                               cudaStream_t stream) {
-  compact_plan_kernel<<<1, kPlanThreads, 0, stream>>>(c, remap, n_live, work);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = launch_plan(compact_plan_kernel, plan_blocks(c), 0, stream, c, remap, n_live, work);
   if (e != cudaSuccess) return e;
-  compact_move_kernel<<<sm_count * 8, 256, 0, stream>>>(c, remap, work);
-  return cudaGetLastError();
+  return launch_dependent(compact_move_kernel, sm_count * 8, 256, stream, c, (const int32_t*)remap,
+                          (const int32_t*)work);
 }
 
 }  // namespace wise

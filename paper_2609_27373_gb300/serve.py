@@ -59,7 +59,7 @@ class PagedCache(wise.Cache):
         self._kv_ws = None
         self._kv_n = -1
         self._attn_ws = None
-        self._attn_shape = None
+        self._attn_key = self._attn_shape = None
 
     def _kv_workspace(self, n: int, stream):
         if n > self._kv_n:
@@ -99,13 +99,15 @@ class PagedCache(wise.Cache):
                stream=None) -> None:
         """Attention of Q [batch, n_heads, q_len, head_dim] over the sequences in slots, into O; the requests of
         each group share their first prefix_lens[g] tokens."""
-        key = (Q.shape, 0 if prefix_lens is None else prefix_lens.shape[0])
-        if key != self._attn_shape:
-            need = wise.wise_prefix_attn_workspace(self, wise.prefix_shape(self, Q, key[1], scale))
+        key = (Q.shape, 0 if prefix_lens is None else prefix_lens.shape[0], scale)
+        if key != self._attn_key:
+            shape = wise.prefix_shape(self, Q, key[1], scale)
+            need = wise.wise_prefix_attn_workspace(self, shape)
             if self._attn_ws is None or self._attn_ws.numel() < need:
                 self._attn_ws = _empty(max(need, 16), torch.uint8, self.device, stream, self._attn_ws)
-            self._attn_shape = key
-        wise.wise_prefix_attn(self, layer, Q, O, slots, n_new, group_start, prefix_lens, self._attn_ws, scale, stream)
+            self._attn_key, self._attn_shape = key, shape
+        wise.wise_prefix_attn(self, layer, Q, O, slots, n_new, group_start, prefix_lens, self._attn_ws, scale, stream,
+                              self._attn_shape)
 
 
 def verify_draft(p, q, draft, n_draft, u_accept, u_sample, stream=None):

@@ -415,45 +415,58 @@ class Cache:
         self.pool, self.table, self.lens, self.refs = pool, table, lens, refs
         self.n_pages, self.page, self.n_slots, self.max_pages = n_pages, page, n_slots, max_pages
         self.n_layers, self.n_kv_heads, self.head_dim = planes // 2, n_kv_heads, head_dim
-        self.device, self.dtype = pool.device, pool.dtype
+        self.device, self.dtype, self.index = pool.device, pool.dtype, pool.get_device()
         self.c = wise_cache_t(n_pages, page, n_slots, max_pages, planes // 2, n_kv_heads, head_dim,
                               _CACHE_DTYPES[pool.dtype], pool.data_ptr(), table.data_ptr(), lens.data_ptr(),
                               refs.data_ptr())
         self.ref = ctypes.byref(self.c)
+        self.ws_bytes = {}  # wise_kv_workspace by list length
 
 
-def _list32(t, name, n, device):
-    """An int32 list of n entries on the cache's device (the checks of _check, in one pass)."""
-    if t is None or t.dtype is not torch.int32 or t.shape != (n,) or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor of shape ({n},) on {device}")
+# The serving calls are short, so their checks read each tensor's properties once and nothing is formatted
+# before a check has failed.
+def _list32(t, name, n, cache):
+    """An int32 list of n entries on the cache's device."""
+    if t is None or t.dtype is not torch.int32 or t.shape != (n,) or t.get_device() != cache.index or \
+            not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape ({n},) on {cache.device}")
+    return t.data_ptr()
 
 
 def _rows16(t, name, shape, cache):
-    if t is None or t.dtype is not cache.dtype or t.shape != shape or t.device != cache.device or \
+    if t is None or t.dtype is not cache.dtype or t.shape != shape or t.get_device() != cache.index or \
             not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {cache.dtype} tensor of shape {tuple(shape)} on {cache.device}")
+    return t.data_ptr()
 
 
-def _raw_stream(stream, device) -> int:
-    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+# torch.cuda.current_stream builds an object at every call; the raw handle comes without.
+_current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _raw_stream(stream, index) -> int:
+    return _current_raw(index) if stream is None else stream.cuda_stream
 
 
 def wise_kv_workspace(cache: Cache, n: int) -> int:
     """Bytes of workspace of wise_kv_extend for lists of n, and of wise_kv_compact."""
-    return int(load().wise_kv_workspace(cache.ref, int(n)))
+    if n not in cache.ws_bytes:
+        cache.ws_bytes[n] = int(load().wise_kv_workspace(cache.ref, int(n)))
+    return cache.ws_bytes[n]
 
 
 def _workspace(t, need, cache):
-    if t is None or t.device != cache.device or not t.is_contiguous() or t.numel() * t.element_size() < need:
+    if t is None or t.get_device() != cache.index or not t.is_contiguous() or t.numel() * t.element_size() < need:
         raise ValueError(f"workspace must be a contiguous tensor of {need} bytes on {cache.device}")
+    return t.data_ptr()
 
 
 def wise_kv_fork(cache: Cache, src, dst, stream=None) -> None:
     """The sequences in slots dst become forks of those in slots src (int32 [n] each)."""
     n = src.shape[0]
-    _list32(src, "src", n, cache.device)
-    _list32(dst, "dst", n, cache.device)
-    rc = load().wise_kv_fork(cache.ref, src.data_ptr(), dst.data_ptr(), n, _raw_stream(stream, cache.device))
+    rc = load().wise_kv_fork(cache.ref, _list32(src, "src", n, cache), _list32(dst, "dst", n, cache), n,
+                             _raw_stream(stream, cache.index))
     if rc != WISE_OK:
         raise WiseError(rc, "wise_kv_fork")
 
@@ -461,12 +474,9 @@ def wise_kv_fork(cache: Cache, src, dst, stream=None) -> None:
 def wise_kv_extend(cache: Cache, slots, n_new, granted, workspace, stream=None) -> None:
     """Grows the sequences in slots by n_new tokens; granted receives n_new, or 0 where pages ran out."""
     n = slots.shape[0]
-    _list32(slots, "slots", n, cache.device)
-    _list32(n_new, "n_new", n, cache.device)
-    _list32(granted, "granted", n, cache.device)
-    _workspace(workspace, wise_kv_workspace(cache, n), cache)
-    rc = load().wise_kv_extend(cache.ref, slots.data_ptr(), n_new.data_ptr(), n, granted.data_ptr(),
-                               workspace.data_ptr(), _raw_stream(stream, cache.device))
+    ws = _workspace(workspace, wise_kv_workspace(cache, n), cache)
+    rc = load().wise_kv_extend(cache.ref, _list32(slots, "slots", n, cache), _list32(n_new, "n_new", n, cache), n,
+                               _list32(granted, "granted", n, cache), ws, _raw_stream(stream, cache.index))
     if rc != WISE_OK:
         raise WiseError(rc, "wise_kv_extend")
 
@@ -478,13 +488,10 @@ def wise_kv_write(cache: Cache, layer: int, slots, n_new, K, V, stream=None) -> 
         raise ValueError("K must be [batch, n_kv_heads, q_len, head_dim]")
     batch, _, q_len, _ = K.shape
     shape = (batch, cache.n_kv_heads, q_len, cache.head_dim)
-    _rows16(K, "K", shape, cache)
-    _rows16(V, "V", shape, cache)
-    _list32(slots, "slots", batch, cache.device)
-    if n_new is not None:
-        _list32(n_new, "n_new", batch, cache.device)
-    rc = load().wise_kv_write(cache.ref, int(layer), slots.data_ptr(), 0 if n_new is None else n_new.data_ptr(),
-                              batch, q_len, K.data_ptr(), V.data_ptr(), _raw_stream(stream, cache.device))
+    rc = load().wise_kv_write(cache.ref, layer, _list32(slots, "slots", batch, cache),
+                              0 if n_new is None else _list32(n_new, "n_new", batch, cache), batch, q_len,
+                              _rows16(K, "K", shape, cache), _rows16(V, "V", shape, cache),
+                              _raw_stream(stream, cache.index))
     if rc != WISE_OK:
         raise WiseError(rc, "wise_kv_write")
 
@@ -492,20 +499,17 @@ def wise_kv_write(cache: Cache, layer: int, slots, n_new, K, V, stream=None) -> 
 def wise_kv_drop(cache: Cache, slots, n_drop, stream=None) -> None:
     """Takes the last n_drop tokens off the sequences in slots (int32 [n] each); all of them frees a sequence."""
     n = slots.shape[0]
-    _list32(slots, "slots", n, cache.device)
-    _list32(n_drop, "n_drop", n, cache.device)
-    rc = load().wise_kv_drop(cache.ref, slots.data_ptr(), n_drop.data_ptr(), n, _raw_stream(stream, cache.device))
+    rc = load().wise_kv_drop(cache.ref, _list32(slots, "slots", n, cache), _list32(n_drop, "n_drop", n, cache), n,
+                             _raw_stream(stream, cache.index))
     if rc != WISE_OK:
         raise WiseError(rc, "wise_kv_drop")
 
 
 def wise_kv_compact(cache: Cache, remap, n_live, workspace, stream=None) -> None:
     """Moves the pages in use to the front of the pool; remap int32 [n_pages] and n_live int32 [1] are written."""
-    _list32(remap, "remap", cache.n_pages, cache.device)
-    _list32(n_live, "n_live", 1, cache.device)
-    _workspace(workspace, wise_kv_workspace(cache, 0), cache)
-    rc = load().wise_kv_compact(cache.ref, remap.data_ptr(), n_live.data_ptr(), workspace.data_ptr(),
-                                _raw_stream(stream, cache.device))
+    ws = _workspace(workspace, wise_kv_workspace(cache, 0), cache)
+    rc = load().wise_kv_compact(cache.ref, _list32(remap, "remap", cache.n_pages, cache),
+                                _list32(n_live, "n_live", 1, cache), ws, _raw_stream(stream, cache.index))
     if rc != WISE_OK:
         raise WiseError(rc, "wise_kv_compact")
 
@@ -523,63 +527,58 @@ def wise_prefix_attn_workspace(cache: Cache, shape: wise_prefix_t) -> int:
 
 
 def wise_prefix_attn(cache: Cache, layer: int, Q, O, slots, n_new=None, group_start=None, prefix_lens=None,
-                     workspace=None, scale: float = 0.0, stream=None) -> None:
+                     workspace=None, scale: float = 0.0, stream=None, shape: wise_prefix_t = None) -> None:
     """Attention of new tokens Q over the cached sequences in slots, into O (both [batch, n_heads, q_len,
     head_dim]); the requests of group g, group_start[g] .. group_start[g + 1] - 1, share their first
-    prefix_lens[g] tokens (both None: nothing is shared)."""
+    prefix_lens[g] tokens (both None: nothing is shared).  `shape`: what prefix_shape gives for Q, made anew
+    when absent."""
     n_groups = 0 if prefix_lens is None else prefix_lens.shape[0]
-    sh = prefix_shape(cache, Q, n_groups, scale)
-    shape = (sh.batch, sh.n_heads, sh.q_len, cache.head_dim)
-    _rows16(Q, "Q", shape, cache)
-    _rows16(O, "O", shape, cache)
-    _list32(slots, "slots", sh.batch, cache.device)
-    if n_new is not None:
-        _list32(n_new, "n_new", sh.batch, cache.device)
+    if shape is None:
+        shape = prefix_shape(cache, Q, n_groups, scale)
+    batch = shape.batch
+    full = (batch, shape.n_heads, shape.q_len, cache.head_dim)
+    starts = lens = 0
     if prefix_lens is not None:
-        _list32(prefix_lens, "prefix_lens", n_groups, cache.device)
-        _list32(group_start, "group_start", n_groups + 1, cache.device)
+        lens = _list32(prefix_lens, "prefix_lens", shape.n_groups, cache)
+        starts = _list32(group_start, "group_start", shape.n_groups + 1, cache)
     elif group_start is not None:
         raise ValueError("group_start needs prefix_lens")
-    ws_bytes = 0
+    ws = ws_bytes = 0
     if workspace is not None:
-        _workspace(workspace, 0, cache)
+        ws = _workspace(workspace, 0, cache)
         ws_bytes = workspace.numel() * workspace.element_size()
-    rc = load().wise_prefix_attn(cache.ref, int(layer), ctypes.byref(sh), Q.data_ptr(), slots.data_ptr(),
-                                 0 if n_new is None else n_new.data_ptr(),
-                                 0 if prefix_lens is None else group_start.data_ptr(),
-                                 0 if prefix_lens is None else prefix_lens.data_ptr(), O.data_ptr(),
-                                 0 if workspace is None else workspace.data_ptr(), ws_bytes,
-                                 _raw_stream(stream, cache.device))
+    rc = load().wise_prefix_attn(cache.ref, layer, ctypes.byref(shape), _rows16(Q, "Q", full, cache),
+                                 _list32(slots, "slots", batch, cache),
+                                 0 if n_new is None else _list32(n_new, "n_new", batch, cache), starts, lens,
+                                 _rows16(O, "O", full, cache), ws, ws_bytes, _raw_stream(stream, cache.index))
     if rc != WISE_OK:
         raise WiseError(rc, "wise_prefix_attn")
+
+
+def _on(t, name, shape, dtype, index):
+    if t is None or t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on device {index}")
+    return t.data_ptr()
 
 
 def wise_verify_draft(p, q, draft, n_draft, u_accept, u_sample, accepted, tokens, stream=None) -> None:
     """Verifies drafted tokens: p [batch, k + 1, vocab] and q [batch, k, vocab] (bf16, fp16 or fp32), draft int32
     [batch, k], n_draft int32 [batch] or None, u_accept fp32 [batch, k], u_sample fp32 [batch] -> accepted int32
     [batch], tokens int32 [batch, k + 1].  q, draft and u_accept may be None when k is 0."""
-    if p is None or p.dim() != 3 or p.dtype not in _PROB_DTYPES:
-        raise ValueError("p must be bf16, fp16 or fp32 [batch, k + 1, vocab]")
-    batch, k, vocab = p.shape[0], p.shape[1] - 1, p.shape[2]
-    if k < 0:
-        raise ValueError("p needs at least one row a request")
-    _check(p, "p", p.shape, p.dtype)
-    optional = k == 0
-    for t, name, shape, dtype in ((q, "q", (batch, k, vocab), p.dtype), (draft, "draft", (batch, k), torch.int32),
-                                  (u_accept, "u_accept", (batch, k), torch.float32),
-                                  (u_sample, "u_sample", (batch,), torch.float32),
-                                  (accepted, "accepted", (batch,), torch.int32),
-                                  (tokens, "tokens", (batch, k + 1), torch.int32),
-                                  (n_draft, "n_draft", (batch,), torch.int32)):
-        if t is None and (name == "n_draft" or (optional and name in ("q", "draft", "u_accept"))):
-            continue
-        if t is None or t.dtype is not dtype or t.shape != shape or t.device != p.device or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {p.device}")
-    rc = load().wise_verify_draft(batch, k, vocab, _PROB_DTYPES[p.dtype], p.data_ptr(),
-                                  0 if q is None else q.data_ptr(), 0 if draft is None else draft.data_ptr(),
-                                  0 if n_draft is None else n_draft.data_ptr(),
-                                  0 if u_accept is None else u_accept.data_ptr(), u_sample.data_ptr(),
-                                  accepted.data_ptr(), tokens.data_ptr(), _raw_stream(stream, p.device))
+    if p is None or p.dim() != 3 or p.dtype not in _PROB_DTYPES or not p.is_cuda or p.shape[1] == 0:
+        raise ValueError("p must be a CUDA tensor in bf16, fp16 or fp32 [batch, k + 1, vocab]")
+    batch, rows, vocab = p.shape
+    k, dt, index = rows - 1, p.dtype, p.get_device()
+    none = k == 0  # without drafts their arrays may be absent
+    rc = load().wise_verify_draft(
+        batch, k, vocab, _PROB_DTYPES[dt], _on(p, "p", (batch, rows, vocab), dt, index),
+        0 if none and q is None else _on(q, "q", (batch, k, vocab), dt, index),
+        0 if none and draft is None else _on(draft, "draft", (batch, k), torch.int32, index),
+        0 if n_draft is None else _on(n_draft, "n_draft", (batch,), torch.int32, index),
+        0 if none and u_accept is None else _on(u_accept, "u_accept", (batch, k), torch.float32, index),
+        _on(u_sample, "u_sample", (batch,), torch.float32, index),
+        _on(accepted, "accepted", (batch,), torch.int32, index),
+        _on(tokens, "tokens", (batch, rows), torch.int32, index), _raw_stream(stream, index))
     if rc != WISE_OK:
         raise WiseError(rc, "wise_verify_draft")
 
