@@ -157,7 +157,7 @@ bool make_query_map(CUtensorMap* map, const void* base, bool fp16, int cols, int
 
 // A paged cache as the kernels see it (wise_cache_t).
 struct CacheView {
-  int n_pages, page, n_slots, max_pages;
+  int n_pages, page, page_shift, n_slots, max_pages;  // page = 1 << page_shift
   int n_planes;           // n_layers * 2
   long long plane_bytes;  // n_pages * page_bytes
   int page_bytes;         // n_kv_heads * page * head_dim * 2

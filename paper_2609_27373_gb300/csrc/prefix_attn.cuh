@@ -79,6 +79,7 @@ struct PfxPlan {
   int* start;        // [n_groups + 1]
   int* lead;         // first active member
   int* tiles;        // key tiles of the shared prefix, 0 if nothing is shared
+  int* pairs;        // pairs of row tiles
   int* pair_base;    // [n_groups + 1] pair tiles before it
   int* pair_item;    // pair items (of one kv head) before it
   int* single_base;  // [n_groups + 1]
@@ -86,7 +87,7 @@ struct PfxPlan {
 };
 
 __host__ __device__ inline int pfx_plan_ints(int batch, int n_groups) {
-  return 8 + 6 * batch + 1 + 7 * n_groups + 3;
+  return 8 + 6 * batch + 1 + 8 * n_groups + 3;
 }
 
 __host__ __device__ inline PfxPlan pfx_plan(int* base, int batch, int n_groups) {
@@ -101,7 +102,8 @@ __host__ __device__ inline PfxPlan pfx_plan(int* base, int batch, int n_groups) 
   p.start = p.cum + batch + 1;
   p.lead = p.start + n_groups + 1;
   p.tiles = p.lead + n_groups;
-  p.pair_base = p.tiles + n_groups;
+  p.pairs = p.tiles + n_groups;
+  p.pair_base = p.pairs + n_groups;
   p.pair_item = p.pair_base + n_groups + 1;
   p.single_base = p.pair_item + n_groups;
   p.single_item = p.single_base + n_groups + 1;

@@ -44,7 +44,7 @@ struct PfxCfg {
   static constexpr int kRegsSoftmax = 208;  // 256 * 208 + 128 * 88 <= 384 * 168 registers
   static constexpr int kRegsOther = 88;
   static constexpr int kRingBytes = (2 + 2 * kSlots) * kTileBytes;  // two Q tiles, then the rings
-  static constexpr int kMaxPlanBytes = 32 * 1024;
+  static constexpr int kMaxPlanBytes = 33 * 1024;
   static constexpr int kSBufs = D == 64 ? 2 : 1;
   static constexpr uint32_t kTmemP = 128, kTmemO = 256;
   static constexpr uint32_t kTmemOStep = D == 64 ? 64 : 128;
@@ -57,7 +57,7 @@ struct PfxCfg {
 constexpr int kPfxSched = 8;  // schedule entries per stream
 constexpr int kPfxFirst = 1, kPfxLast = 2, kPfxEnd = 4;
 
-// Schedule entry {ring slot | parity of its use << 8, first key position,
+// Schedule entry {ring slot | parity of its use << 8 | keys << 16, first key position,
 // request | (requests - 1) << 10 | kind << 17 | flags << 19, segment slot}.
 __device__ __forceinline__ int pfx_pack(int req, int nreq, int kind, int flags) {
   return req | (nreq - 1) << 10 | kind << 17 | flags << 19;
@@ -131,7 +131,7 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
     active = __reduce_add_sync(0xffffffffu, active);
     lead = __reduce_min_sync(0xffffffffu, lead);
     int shared = 0;
-    if (active > 1) shared = max(0, min(plan.tiles[g], shortest)) / c.page * c.page;
+    if (active > 1) shared = max(0, min(plan.tiles[g], shortest)) & -c.page;
     __syncwarp();
     const int tiles = (shared + kPfxKeys - 1) / kPfxKeys;
     if (lane == 0) {
@@ -172,6 +172,7 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
       if (g < p.n_groups && plan.tiles[g] > 0) {
         const int row_tiles = (plan.start[g + 1] - plan.start[g] + p.per_tile - 1) / p.per_tile;
         own[1] = row_tiles / 2;
+        plan.pairs[g] = own[1];
         own[3] = row_tiles & 1;
         own[0] = own[1] * plan.tiles[g] * c.n_kv_heads;
         own[2] = own[3] * plan.tiles[g] * c.n_kv_heads;
@@ -224,9 +225,10 @@ __device__ __forceinline__ int pfx_find(const int* base, int n, int x) {
   return lo;
 }
 
-// Waits of the producers and issuers: the polling loop is one function, to keep
-// their own loops short.
-static __device__ __noinline__ bool pfx_wait_long(uint64_t* bar, uint32_t parity, volatile int* abort, uint64_t limit_ns) {
+// Waits of the producers and issuers: the polling loop is one function, which
+// keeps their own loops short.  (The softmax has no registers for a call.)
+static __device__ __noinline__ bool pfx_wait_long(uint64_t* bar, uint32_t parity, volatile int* abort,
+                                                  uint64_t limit_ns) {
   return mbar_wait(bar, parity, abort, limit_ns);
 }
 __device__ __forceinline__ bool pfx_wait(uint64_t* bar, uint32_t parity, volatile int* abort, uint64_t limit_ns) {
@@ -234,6 +236,11 @@ __device__ __forceinline__ bool pfx_wait(uint64_t* bar, uint32_t parity, volatil
 }
 __device__ __forceinline__ bool pfx_warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort, uint64_t limit_ns) {
   return __all_sync(0xffffffffu, pfx_wait(bar, parity, abort, limit_ns));
+}
+// A wait ran out: every role unwinds.
+static __device__ __noinline__ void pfx_give_up(int* abort, int* status) {
+  *reinterpret_cast<volatile int*>(abort) = 1;
+  atomicOr(status, kStatusTimeout);
 }
 
 // A segment: a run of key tiles of an item.
@@ -260,10 +267,9 @@ __device__ __forceinline__ PfxSeg pfx_segment(const PfxParams& p, const PfxPlan&
     const int it = y / tiles;
     t = y - it * tiles;
     const int a = plan.start[g], members = plan.start[g + 1] - a;
-    const int row_tiles = (members + p.per_tile - 1) / p.per_tile;
+    const int n_pairs = plan.pairs[g];
     if (pairs) {
       // kv head outermost: the pairs of one kv head read the same keys at about the same time.
-      const int n_pairs = row_tiles / 2;
       s.kvh = it / n_pairs;
       const int pair = it - s.kvh * n_pairs;
       kind = kPfxPair;
@@ -274,9 +280,9 @@ __device__ __forceinline__ PfxSeg pfx_segment(const PfxParams& p, const PfxPlan&
     } else {
       s.kvh = it;
       kind = kPfxSingle;
-      req = a + (row_tiles - 1) * p.per_tile;
+      req = a + 2 * n_pairs * p.per_tile;  // the odd tile is the last one
       s.slot = plan.single_item[g] * kv + it + run;
-      nreq = members - (row_tiles - 1) * p.per_tile;
+      nreq = members - 2 * n_pairs * p.per_tile;
     }
     const int lead = plan.lead[g];
     s.row = plan.slot[lead];
@@ -352,10 +358,10 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
   bool first = false;  // the next tile starts its segment
 
   auto fetch = [&]() {
-    const int at = seg.pos + lane * c.page;
+    const int at = seg.pos + (lane << c.page_shift);
     page = -1;
-    if (lane * c.page < kPfxKeys && at < seg.end)
-      page = __ldg(c.table + (size_t)seg.row * c.max_pages + at / c.page);
+    if (at - seg.pos < kPfxKeys && at < seg.end)
+      page = __ldg(c.table + (size_t)seg.row * c.max_pages + (at >> c.page_shift));
   };
   for (;;) {
     if (seg.left == 0) {
@@ -385,18 +391,20 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
     if (n_ent >= kPfxSched) ok = pfx_warp_wait(&sb.sched_empty[w][e], ((n_ent / kPfxSched) - 1) & 1, abort, p.wait_ns);
     if (ok && lane == 0) {
       const int flags = (first ? kPfxFirst : 0) | (seg.left == 1 ? kPfxLast : 0);
-      sb.sched[w][e] = make_int4(slot | (use & 1) << 8, seg.pos, word | flags << 19, seg.slot + second);
+      sb.sched[w][e] = make_int4(slot | (use & 1) << 8 | min(kPfxKeys, seg.end - seg.pos) << 16, seg.pos,
+                                 word | flags << 19, seg.slot + second);
       mbar_arrive(&sb.sched_full[w][e]);
     }
     ++n_ent;
     // The tile of the K ring (r = 0) and of the V ring; Q in between.  One lane
     // per page that the item reaches.
-    const bool on = lane * c.page < kPfxKeys && seg.pos + lane * c.page < seg.end;
+    const int at = lane << c.page_shift;
+    const bool on = at < kPfxKeys && seg.pos + at < seg.end;
     const bool valid = page >= 0 && page < c.n_pages;
     if (on && !valid) bad = 1;
     // A faulty page id becomes a coordinate out of range, which reads zeros.
     const int z = valid ? page * c.n_kv_heads + seg.kvh : c.n_pages * c.n_kv_heads;
-    const int bytes = min(kPfxKeys, (seg.end - seg.pos + c.page - 1) / c.page * c.page) * 128 * C::kBoxes;
+    const int bytes = min(kPfxKeys, (seg.end - seg.pos + c.page - 1) & -c.page) * 128 * C::kBoxes;
 #pragma unroll 1
     for (int r = pair ? w : 0; ok && r <= (pair ? w : 1); ++r) {
       uint64_t* full = r ? &sb.v_full[slot] : &sb.k_full[slot];
@@ -406,7 +414,7 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
       if (lane == 0) mbar_arrive_expect_tx(full, bytes);
       __syncwarp();
       if (on) {
-        uint8_t* dst = ring + (r * NS + slot) * C::kTileBytes + lane * c.page * 128;
+        uint8_t* dst = ring + (r * NS + slot) * C::kTileBytes + at * 128;
 #pragma unroll
         for (int b = 0; b < C::kBoxes; ++b)
           tma_load_3d(dst + b * 128 * 128, r ? mapV : mapK, full, 64 * b, 0, z);
@@ -446,8 +454,7 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
   }
   if (bad) atomicOr(c.status, kStatusBadCache);
   if (!ok && lane == 0) {
-    *reinterpret_cast<volatile int*>(&sb.abort) = 1;
-    atomicOr(c.status, kStatusTimeout);
+    pfx_give_up(&sb.abort, c.status);
     // Copies already issued land before the CTA's shared memory is released.
     int never = 0;
     for (int k = 0; k < NS; ++k) {
@@ -504,7 +511,7 @@ __device__ void pfx_mma_s(const PfxParams& p, uint32_t tmem, uint8_t* q_tiles, u
         t.end = true;
       } else {
         if (((flags & kPfxFirst) && !pfx_wait(&sb.q_full[w], t.nq++ & 1, abort, p.wait_ns)) ||
-            !pfx_wait(&sb.k_full[slot], ent.x >> 8, abort, p.wait_ns) ||
+            !pfx_wait(&sb.k_full[slot], (ent.x >> 8) & 1, abort, p.wait_ns) ||
             (used > 0 && !pfx_wait(&sb.s_free[own_buf ? w : 0], (used - 1) & 1, abort, p.wait_ns))) {
           ok = false;
           break;
@@ -543,8 +550,7 @@ __device__ void pfx_mma_s(const PfxParams& p, uint32_t tmem, uint8_t* q_tiles, u
     }
   }
   if (!ok) {
-    *reinterpret_cast<volatile int*>(&sb.abort) = 1;
-    atomicOr(p.cache.status, kStatusTimeout);
+    pfx_give_up(&sb.abort, p.cache.status);
   }
   // Every MMA and commit of this thread completes before TMEM is released.
   umma_commit(&sb.done[0]);
@@ -575,7 +581,7 @@ __device__ void pfx_mma_pv(const PfxParams& p, uint32_t tmem, uint8_t* ring, Pfx
       if (flags & kPfxEnd) {
         t.end = true;
       } else {
-        if (!pfx_wait(&sb.v_full[slot], ent.x >> 8, abort, p.wait_ns) ||
+        if (!pfx_wait(&sb.v_full[slot], (ent.x >> 8) & 1, abort, p.wait_ns) ||
             !pfx_wait(&sb.p_full[w], t.j & 1, abort, p.wait_ns)) {
           ok = false;
           break;
@@ -584,12 +590,11 @@ __device__ void pfx_mma_pv(const PfxParams& p, uint32_t tmem, uint8_t* ring, Pfx
         const uint64_t v0 = smem_desc_sw128(smem_u32(ring + (NS + slot) * C::kTileBytes), kPfxKeys * 128, 1024);
         const uint32_t o_col = tmem + C::kTmemO + w * C::kTmemOStep, p_col = tmem + C::kTmemP + w * 64;
         uint32_t acc = (flags & kPfxFirst) ? 0u : 1u;
+        const int steps = ((ent.x >> 16) + 15) / 16;  // of 16 keys; those past the item's end are left out
 #pragma unroll 1
-        for (int kk = 0; kk < kPfxKeys / 16; kk += 2) {
-          const uint32_t v = (uint32_t)v0 + kk * (2048 / 16);
-          umma_ts_split(o_col, p_col + kk * 8, v, (uint32_t)(v0 >> 32), idesc, acc);
+        for (int kk = 0; kk < steps; ++kk) {
+          umma_ts_split(o_col, p_col + kk * 8, (uint32_t)v0 + kk * (2048 / 16), (uint32_t)(v0 >> 32), idesc, acc);
           acc = 1;
-          umma_ts_split(o_col, p_col + kk * 8 + 8, v + 2048 / 16, (uint32_t)(v0 >> 32), idesc, acc);
         }
         umma_commit(&sb.o_full[w]);
         umma_commit(&sb.v_empty[slot]);
@@ -602,8 +607,7 @@ __device__ void pfx_mma_pv(const PfxParams& p, uint32_t tmem, uint8_t* ring, Pfx
     other = swap;
   }
   if (!ok) {
-    *reinterpret_cast<volatile int*>(&sb.abort) = 1;
-    atomicOr(p.cache.status, kStatusTimeout);
+    pfx_give_up(&sb.abort, p.cache.status);
   }
   umma_commit(&sb.done[1]);
   int never = 0;
@@ -636,8 +640,8 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
   const uint32_t o_col = C::kTmemO + w * C::kTmemOStep;
   uint64_t* s_free = &sb.s_free[own_buf ? w : 0];
   bool ok = true;
-  int limit = 0, end = 0;       // keys the row may see; one past the item's keys
-  bool row_on = false, warp_on = false;
+  int limit = 0;                                        // keys the row may see
+  bool row_on = false, live = false, warp_on = false;  // a row of the item; one that sees keys; a warp with such
   float m = -INFINITY, l = 0.0f;
   for (int j = 0;; ++j) {
     const int e = j % kPfxSched;
@@ -654,15 +658,16 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
       const int req0 = ent.z & 1023, nreq = ((ent.z >> 10) & 127) + 1;
       const int of = r / p.rows, i = r % p.rows % p.q_len;
       row_on = of < nreq;
-      // Threads without a row compute on whatever Q holds there and store
-      // nothing; unmasked, they do not hold up their warp.
-      limit = INT_MAX;
+      int seen = 0;
       if (row_on) {
         const int req = req0 + of, add = plan.add[req];
-        limit = i < add ? max(0, plan.len[req] - add + i + 1) : 0;
+        seen = i < add ? plan.len[req] - add + i + 1 : 0;
       }
-      end = kind == kPfxOwn ? plan.len[req0] : plan.lo[req0];
-      warp_on = __any_sync(0xffffffffu, row_on);
+      // Threads whose row sees nothing (or is none) compute on whatever Q
+      // holds there and store no O; unmasked, they do not hold up their warp.
+      live = seen > 0;
+      limit = live ? seen : INT_MAX;
+      warp_on = __any_sync(0xffffffffu, live);
       m = -INFINITY;
       l = 0.0f;
     }
@@ -671,28 +676,44 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
       break;
     }
     tc_fence_after_sync();
-    float f = 1.0f;
-    bool rescale = false;
+    const int keys = ent.x >> 16;                        // of the tile
+    const int lim = min(limit - ent.y, keys) - 1;        // last column the row sees
+    const bool masked = __any_sync(0xffffffffu, lim < kPfxKeys - 1);
+    const int chunks = (keys + 31) / 32;
+    float m_new = m, sum = 0.0f;
     uint32_t pw[kPfxKeys / 2];
-    if (warp_on) {
+    if (warp_on && !masked) {
       float s[kPfxKeys];
       tmem_load_row<kPfxKeys>(lane_tmem + s_col, s);
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(s_free);
-      mask_s_row<128>(s, 1u, min(limit, end) - ent.y - 1);
       const float m_tile = row_max(s) * p.scale_log2;
-      const float m_new = (m_tile > m + kRescaleThreshold) ? m_tile : m;
-      rescale = row_on && m_new != m && m != -INFINITY;
-      if (rescale) f = ex2_approx(m - m_new);
-      const float sum = exp2_scaled(s, p.scale_log2, m_new == -INFINITY ? 0.0f : m_new);
-      l = l * f + sum;
-      m = m_new;
+      m_new = (m_tile > m + kRescaleThreshold) ? m_tile : m;
+      sum = exp2_scaled(s, p.scale_log2, m_new == -INFINITY ? 0.0f : m_new);
 #pragma unroll
       for (int k = 0; k < kPfxKeys / 2; ++k) pw[k] = pack_16x2<FP16>(s[2 * k], s[2 * k + 1]);
+    } else if (warp_on) {
+      // 32 columns at a time, read twice: short items and the ends of long
+      // ones cost what they hold, and the loop's code is small.
+      float m_tile = -INFINITY;
+#pragma unroll 1
+      for (int c = 0; c < chunks; ++c) {
+        uint32_t v[32];
+        tmem_ld_32x32b_x32(lane_tmem + s_col + 32 * c, v);
+        tmem_ld_wait(v);
+        const int last = lim - 32 * c;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) m_tile = fmaxf(m_tile, k <= last ? __uint_as_float(v[k]) : -INFINITY);
+      }
+      m_tile *= p.scale_log2;
+      m_new = (m_tile > m + kRescaleThreshold) ? m_tile : m;
     } else if (lane == 0) {
       mbar_arrive(s_free);
     }
+    const bool rescale = live && m_new != m && m != -INFINITY;
+    const float f = rescale ? ex2_approx(m - m_new) : 1.0f;
+    m = m_new;
     // P and O are at rest once the previous P V has completed.  (Warps without
     // a row wait as well: their arrivals below must not run ahead.)
     if (j > 0 && !warp_wait(&sb.o_full[w], (j - 1) & 1, abort, p.wait_ns)) {
@@ -700,7 +721,7 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
       break;
     }
     tc_fence_after_sync();
-    if (warp_on) {
+    if (warp_on && !masked) {
 #pragma unroll
       for (int c = 0; c < kPfxKeys / 32; ++c) {
         uint32_t q[16];
@@ -708,6 +729,28 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
         for (int k = 0; k < 16; ++k) q[k] = pw[16 * c + k];
         tmem_st_32x32b_x16(lane_tmem + p_col + 16 * c, q);
       }
+    } else if (warp_on) {
+      const float shift = m == -INFINITY ? 0.0f : m;
+#pragma unroll 1
+      for (int c = 0; c < chunks; ++c) {
+        uint32_t v[32], q[16];
+        tmem_ld_32x32b_x32(lane_tmem + s_col + 32 * c, v);
+        tmem_ld_wait(v);
+        const int last = lim - 32 * c;
+        float x[32];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) x[k] = k <= last ? __uint_as_float(v[k]) : -INFINITY;
+        sum += exp2_scaled(x, p.scale_log2, shift);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) q[k] = pack_16x2<FP16>(x[2 * k], x[2 * k + 1]);
+        tmem_st_32x32b_x16(lane_tmem + p_col + 16 * c, q);
+      }
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(s_free);
+    }
+    l = l * f + sum;
+    if (warp_on) {
       if (__any_sync(0xffffffffu, rescale)) {
 #pragma unroll 1
         for (int c = 0; c < D / 16; ++c) {
@@ -721,20 +764,19 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
       }
       tmem_st_wait();
     }
-    const int valid = end - ent.y;
-    if (valid < kPfxKeys) {
-      // The item ends in this tile: rows of V past its end are whatever the
-      // pool or an earlier tile left there, and 0 * NaN would spread.
-      if (!warp_wait(&sb.v_full[ent.x & 255], ent.x >> 8, abort, p.wait_ns)) {
+    if (keys % 16 != 0) {
+      // The item ends inside a step of 16 keys: its rows of V past the end are
+      // whatever the pool or an earlier tile left there, and 0 * NaN would
+      // spread.
+      if (!warp_wait(&sb.v_full[ent.x & 255], (ent.x >> 8) & 1, abort, p.wait_ns)) {
         ok = false;
         break;
       }
-      if (r >= valid) {
+      if (r >= keys && r < (keys + 15) / 16 * 16) {
         const uint32_t row = smem_u32(ring + (NS + (ent.x & 255)) * C::kTileBytes + r * 128);
 #pragma unroll 1
-        for (int b = 0; b < C::kBoxes; ++b)
-#pragma unroll 1
-          for (int k = 0; k < 8; ++k) st_shared_v4(row + b * 128 * 128 + k * 16, 0u, 0u, 0u, 0u);
+        for (int k = 0; k < 8; ++k)
+          for (int b = 0; b < C::kBoxes; ++b) st_shared_v4(row + b * 128 * 128 + k * 16, 0u, 0u, 0u, 0u);
         fence_proxy_async_smem();
       }
     }
@@ -747,21 +789,25 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
         break;
       }
       tc_fence_after_sync();
+      const int rows = kind == kPfxOwn ? p.rows : kPfxRows;
+      float2* ml = kind == kPfxOwn ? p.work.ml[0] : kind == kPfxSingle ? p.work.ml[1] : p.work.ml[2];
+      if (row_on) ml[(size_t)ent.w * rows + r] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
       if (warp_on) {
-        float o[D];
-        tmem_load_row<D>(lane_tmem + o_col, o);
-        tc_fence_before_sync();
-        if (row_on) {
-          const int rows = kind == kPfxOwn ? p.rows : kPfxRows;
-          const float2 v = make_float2(m, l);
-          float2* ml = kind == kPfxOwn ? p.work.ml[0] : kind == kPfxSingle ? p.work.ml[1] : p.work.ml[2];
-          float4* O = kind == kPfxOwn ? p.work.O[0] : kind == kPfxSingle ? p.work.O[1] : p.work.O[2];
-          ml[(size_t)ent.w * rows + r] = v;
-          float4* out = O + (size_t)ent.w * rows * (D / 4) + r;
+        float4* O = kind == kPfxOwn ? p.work.O[0] : kind == kPfxSingle ? p.work.O[1] : p.work.O[2];
+        float4* out = O + (size_t)ent.w * rows * (D / 4) + r;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t v[32];
+          tmem_ld_32x32b_x32(lane_tmem + o_col + 32 * c, v);
+          tmem_ld_wait(v);
+          if (live) {
 #pragma unroll
-          for (int c = 0; c < D / 4; ++c)
-            out[c * rows] = make_float4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+            for (int k = 0; k < 8; ++k)
+              out[(8 * c + k) * rows] = make_float4(__uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1]),
+                                                    __uint_as_float(v[4 * k + 2]), __uint_as_float(v[4 * k + 3]));
+          }
         }
+        tc_fence_before_sync();
       }
     }
   }
@@ -892,8 +938,7 @@ __device__ __forceinline__ PfxSources pfx_sources(const PfxParams& p, const PfxP
   if (g >= 0) {
     const int start = plan.start[g], tiles = plan.tiles[g];
     const int at = req - start, tile = at / p.per_tile;
-    const int row_tiles = (plan.start[g + 1] - start + p.per_tile - 1) / p.per_tile;
-    const int n_pairs = row_tiles / 2;
+    const int n_pairs = plan.pairs[g];
     const bool pair = tile < 2 * n_pairs;
     row0 = (at - tile * p.per_tile) * p.rows;
     const int it = pair ? kvh * n_pairs + tile / 2 : kvh;

@@ -34,6 +34,7 @@ int check_cache(const wise_cache_t* c, bool pool, CacheView* v) {
   if (pool && (!c->pool || !aligned(c->pool, 16))) return WISE_ERR_INVALID_ARG;
   v->n_pages = c->n_pages;
   v->page = c->page;
+  v->page_shift = c->page == 16 ? 4 : c->page == 32 ? 5 : c->page == 64 ? 6 : 7;
   v->n_slots = c->n_slots;
   v->max_pages = c->max_pages;
   v->n_planes = 2 * c->n_layers;
