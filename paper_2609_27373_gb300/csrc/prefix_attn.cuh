@@ -57,8 +57,8 @@ __host__ __device__ inline int pfx_run_of(const PfxCuts& c, int x) {
   return y < 0 ? x / (c.q + 1) : c.longer + y / c.q;
 }
 
-// The plan of a launch: every CTA derives it in shared memory, the first one
-// also stores it for the merge.  Lists are ints.
+// The plan of a launch, which every CTA derives in shared memory.  Lists are
+// ints.
 struct PfxTotals {
   PfxCuts pair;      // the line of pair items
   PfxCuts line;      // the other line: single items first, then own items
@@ -110,11 +110,11 @@ __host__ __device__ inline PfxPlan pfx_plan(int* base, int batch, int n_groups) 
   return p;
 }
 
-// Workspace: the plan, then for each kind its segments' (m, l) pairs and their
-// O, transposed as [segment][head_dim / 4][rows][4] so that neighbouring
+// Workspace: where the merge finds its parts (two int4 per request and kv
+// head), then for each kind its segments' (m, l) pairs and their O, transposed as [segment][head_dim / 4][rows][4] so that neighbouring
 // threads (rows) store neighbouring 16 bytes.  A pair segment is two slots.
 struct PfxWork {
-  int* plan;
+  int4* sources;
   float2* ml[3];
   float4* O[3];
   int rows[3];  // rows of a slot
@@ -140,7 +140,7 @@ inline PfxWork pfx_work(void* base, int batch, int n_groups, int n_kv_heads, int
     off += (n + 255) / 256 * 256;
     return p;
   };
-  w.plan = reinterpret_cast<int*>(take((size_t)pfx_plan_ints(batch, n_groups) * 4));
+  w.sources = reinterpret_cast<int4*>(take((size_t)batch * n_kv_heads * 2 * sizeof(int4)));
   for (int k = 0; k < 3; ++k) w.ml[k] = reinterpret_cast<float2*>(take(slots[k] * w.rows[k] * sizeof(float2)));
   for (int k = 0; k < 3; ++k) w.O[k] = reinterpret_cast<float4*>(take(slots[k] * w.rows[k] * head_dim * 4));
   w.bytes = off;

@@ -74,13 +74,14 @@ struct PfxShared {
   uint64_t o_full[2];  // P V completed
   uint64_t done[2];
   int4 sched[2][kPfxSched];
+  int warp_sums[32];
   uint32_t tmem_base;
   int abort;
 };
 
 // ---------------------------------------------------------------------- plan
 // All threads of the CTA; `plan` in shared memory.
-__device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bool report) {
+__device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, int* warp_sums, bool report) {
   const CacheView& c = p.cache;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
   int bad = 0, bad_groups = 0;
@@ -147,23 +148,28 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
     }
   }
   __syncthreads();
-  if (warp == 0) {
-    int before = 0;
+  // Prefix sums: over the requests by all warps together, and then over the
+  // groups (four counts each) by warp 0.
+  int before = 0;
 #pragma unroll 1
-    for (int r0 = 0; r0 < p.batch; r0 += 32) {
-      const int r = r0 + lane;
-      const int t = r < p.batch ? max(0, plan.len[r] - plan.lo[r] + kPfxKeys - 1) / kPfxKeys : 0;
-      int v = t;
-#pragma unroll 1
-      for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += u;
-      }
-      if (r < p.batch) plan.cum[r] = before + v - t;
-      before += __shfl_sync(0xffffffffu, v, 31);
+  for (int r0 = 0; r0 < p.batch; r0 += blockDim.x) {
+    const int r = r0 + tid;
+    const int t = r < p.batch ? max(0, plan.len[r] - plan.lo[r] + kPfxKeys - 1) / kPfxKeys : 0;
+    int v = t;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += u;
     }
-    if (lane == 0) plan.cum[p.batch] = before;
-  } else if (warp == 1) {
+    if (lane == 31) warp_sums[warp] = v;
+    __syncthreads();
+    const int other = lane < n_warps ? warp_sums[lane] : 0;
+    const int below = __reduce_add_sync(0xffffffffu, lane < warp ? other : 0);
+    if (r < p.batch) plan.cum[r] = before + below + v - t;
+    before += __reduce_add_sync(0xffffffffu, other);
+    if (r0 + (int)blockDim.x < p.batch) __syncthreads();  // warp_sums is used again
+  }
+  if (warp == 0) {
     int b[4] = {0, 0, 0, 0};  // pair tiles, pair items, single tiles, single items
 #pragma unroll 1
     for (int g0 = 0; g0 < p.n_groups; g0 += 32) {
@@ -180,7 +186,7 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         v[k] = own[k];
-#pragma unroll 1
+#pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
           const int u = __shfl_up_sync(0xffffffffu, v[k], o);
           if (lane >= o) v[k] += u;
@@ -195,19 +201,19 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bo
 #pragma unroll
       for (int k = 0; k < 4; ++k) b[k] += __shfl_sync(0xffffffffu, v[k], 31);
     }
+    // Lane 0 cuts the line of pair items, lane 1 the other one.
+    const int line = b[2] + before * c.n_kv_heads;
+    const PfxCuts cuts = pfx_cuts(lane == 0 ? b[0] : line, gridDim.x << (lane == 0 ? 0 : 1));
     if (lane == 0) {
+      plan.cum[p.batch] = before;
       plan.pair_base[p.n_groups] = b[0];
       plan.single_base[p.n_groups] = b[2];
+      plan.t->pair = cuts;
+      plan.t->single_tiles = b[2];
+      plan.t->grouped = grouped;
+    } else if (lane == 1) {
+      plan.t->line = cuts;
     }
-  }
-  __syncthreads();
-  if (tid == 0) {
-    PfxTotals t;
-    t.pair = pfx_cuts(plan.pair_base[p.n_groups], gridDim.x);
-    t.single_tiles = plan.single_base[p.n_groups];
-    t.line = pfx_cuts(t.single_tiles + plan.cum[p.batch] * c.n_kv_heads, 2 * gridDim.x);
-    t.grouped = grouped;
-    *plan.t = t;
   }
   __syncthreads();
 }
@@ -818,6 +824,42 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
   }
 }
 
+// Where the partial results of request and kv head i = req * n_kv_heads + kvh
+// lie, as two int4: {n, n_pre, step, kind}, {slot, first row, own slot, 0}.
+// The first n_pre are those of the shared prefix, in every step-th slot of its
+// kind; the others, of the request's own keys, in consecutive slots.
+__device__ __forceinline__ void pfx_sources(const PfxParams& p, const PfxPlan& plan, int i, int4* out) {
+  const int kv = p.cache.n_kv_heads;
+  const int req = i / kv, kvh = i - req * kv;
+  const PfxTotals t = *plan.t;
+  const int g = plan.group[req], own_first = plan.cum[req], own_tiles = plan.cum[req + 1] - own_first;
+  int n_pre = 0, n_own = 0, step = 1, kind = kPfxSingle, slot = 0, row0 = 0, own_slot = 0;
+  if (plan.len[req] > 0) {
+    if (g >= 0) {
+      const int at = req - plan.start[g], tiles = plan.tiles[g], n_pairs = plan.pairs[g];
+      const int tile = at / p.per_tile;
+      const bool pair = tile < 2 * n_pairs;
+      row0 = (at - tile * p.per_tile) * p.rows;
+      const int it = pair ? kvh * n_pairs + tile / 2 : kvh;
+      const int x = (pair ? plan.pair_base[g] : plan.single_base[g]) + it * tiles;
+      const PfxCuts cuts = pair ? t.pair : t.line;
+      const int k0 = pfx_run_of(cuts, x);
+      n_pre = pfx_run_of(cuts, x + tiles - 1) - k0 + 1;
+      kind = pair ? kPfxPair : kPfxSingle;
+      step = pair ? 2 : 1;
+      slot = pair ? 2 * (plan.pair_item[g] * kv + it + k0) + (tile & 1) : plan.single_item[g] * kv + it + k0;
+    }
+    if (own_tiles > 0) {
+      const int x = t.single_tiles + own_first * kv + kvh * own_tiles;
+      const int k0 = pfx_run_of(t.line, x);
+      n_own = pfx_run_of(t.line, x + own_tiles - 1) - k0 + 1;
+      own_slot = i + k0;
+    }
+  }
+  out[0] = make_int4(n_pre + n_own, n_pre, step, kind);
+  out[1] = make_int4(slot, row0, own_slot, 0);
+}
+
 // -------------------------------------------------------------------- kernel
 template <int D, bool FP16>
 __global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
@@ -866,16 +908,16 @@ __global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
   // Everything above may overlap the previous kernel of the stream.
   griddep_wait();
   tc_fence_before_sync();
-  pfx_make_plan(p, plan, blockIdx.x == 0);  // ends with a barrier
+  pfx_make_plan(p, plan, sb.warp_sums, blockIdx.x == 0);  // ends with a barrier
   tc_fence_after_sync();
   const uint32_t tmem = sb.tmem_base;
-  if (blockIdx.x == 0) {
-    const int* from = reinterpret_cast<const int*>(plan.t);
-    for (int i = threadIdx.x; i < pfx_plan_ints(p.batch, p.n_groups); i += C::kThreads) p.work.plan[i] = from[i];
-  }
   if (threadIdx.x == 0) griddep_launch_dependents();  // the merge waits for this grid's end
 
   if (warp < 8) {
+    // While the first tiles are on their way: where the merge finds its parts.
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < p.batch * p.cache.n_kv_heads; i += gridDim.x * 256)
+      pfx_sources(p, plan, i, p.work.sources + 2 * (size_t)i);
+    __syncwarp();
     warpgroup_reg_inc<C::kRegsSoftmax>();
     pfx_softmax<D, FP16>(p, plan, warp >> 2, tmem, ring, sb);
   } else {
@@ -901,14 +943,13 @@ __global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
 
 // --------------------------------------------------------------------- merge
 // Joins the partial results of one request and kv head; blockIdx.y takes a
-// share of the columns.  A thread owns 4 columns of one row (kMergeEach such
-// elements of the same row at a time); where a block has fewer elements than
-// threads, `parts` threads share an element, each taking every parts-th
-// segment.  What bounds it: a chain of four dependent loads (plan, group,
-// (m, l), O), so blocks are small and many share an SM.
+// share of the columns.  A thread owns 4 columns of one row; where a block has
+// fewer such elements than threads, `parts` threads share an element, each
+// taking every parts-th segment.  What bounds it: a chain of three dependent
+// loads (the sources, (m, l), O), so blocks are small, many share an SM, and a
+// thread has eight loads of O in flight.
 constexpr int kMergeThreads = 128;
 constexpr int kMergeStats = 1024;  // (m, l) pairs in shared memory at a time
-constexpr int kMergeEach = 2;
 
 struct PfxMergeShape {
   int log_rows;  // rows of a request rounded up to a power of two
@@ -916,156 +957,89 @@ struct PfxMergeShape {
   int parts;
 };
 
-// Where the segments of a request and kv head lie: n_pre of the shared prefix
-// first, then n_own.
-struct PfxSources {
-  const float2* pre_ml;
-  const float2* own_ml;
-  const float4* pre_O;
-  const float4* own_O;
-  int n_pre, n, pre_step;
-};
-
-template <int D>
-__device__ __forceinline__ PfxSources pfx_sources(const PfxParams& p, const PfxPlan& plan, int req, int kvh) {
-  const int kv = p.cache.n_kv_heads;
-  const PfxTotals t = *plan.t;
-  const int g = plan.group[req], own_tiles = plan.cum[req + 1] - plan.cum[req], own_first = plan.cum[req];
-  PfxSources s = {};
-  s.pre_step = 1;
-  if (plan.len[req] == 0) return s;
-  int pre_slot = 0, row0 = 0, kind = kPfxSingle;
-  if (g >= 0) {
-    const int start = plan.start[g], tiles = plan.tiles[g];
-    const int at = req - start, tile = at / p.per_tile;
-    const int n_pairs = plan.pairs[g];
-    const bool pair = tile < 2 * n_pairs;
-    row0 = (at - tile * p.per_tile) * p.rows;
-    const int it = pair ? kvh * n_pairs + tile / 2 : kvh;
-    const int x = (pair ? plan.pair_base[g] : plan.single_base[g]) + it * tiles;
-    const PfxCuts cuts = pair ? t.pair : t.line;
-    const int k0 = pfx_run_of(cuts, x);
-    s.n_pre = pfx_run_of(cuts, x + tiles - 1) - k0 + 1;
-    if (pair) {
-      kind = kPfxPair;
-      pre_slot = 2 * (plan.pair_item[g] * kv + it + k0) + (tile & 1);
-      s.pre_step = 2;
-    } else {
-      pre_slot = plan.single_item[g] * kv + it + k0;
-    }
-  }
-  s.pre_ml = p.work.ml[kind] + (size_t)pre_slot * kPfxRows + row0;
-  s.pre_O = p.work.O[kind] + (size_t)pre_slot * kPfxRows * (D / 4) + row0;
-  s.n = s.n_pre;
-  if (own_tiles > 0) {
-    const int x = t.single_tiles + own_first * kv + kvh * own_tiles;
-    const int k0 = pfx_run_of(t.line, x);
-    s.n += pfx_run_of(t.line, x + own_tiles - 1) - k0 + 1;
-    const size_t own_slot = (size_t)req * kv + kvh + k0;
-    s.own_ml = p.work.ml[kPfxOwn] + own_slot * p.rows;
-    s.own_O = p.work.O[kPfxOwn] + own_slot * p.rows * (D / 4);
-  }
-  return s;
-}
-
 template <int D, bool FP16>
 __global__ void __launch_bounds__(kMergeThreads) prefix_merge_kernel(const PfxParams p, const PfxMergeShape sh,
                                                                      uint16_t* O) {
-  __shared__ PfxSources src;
   __shared__ float2 stats[kMergeStats];
   __shared__ float4 sums[kMergeThreads];
   __shared__ float part_l[kMergeThreads];
+  griddep_launch_dependents();  // what follows waits for this grid's end
   griddep_wait();
-  const int kv = p.cache.n_kv_heads;
-  const int req = blockIdx.x / kv, kvh = blockIdx.x - req * kv;
+  const int4 s0 = p.work.sources[2 * (size_t)blockIdx.x], s1 = p.work.sources[2 * (size_t)blockIdx.x + 1];
+  const int n = s0.x, n_pre = s0.y, pre_step = s0.z, kind = s0.w;
   const int R = p.rows, tid = threadIdx.x;
-  if (tid == 0) src = pfx_sources<D>(p, pfx_plan(p.work.plan, p.batch, p.n_groups), req, kvh);
-  __syncthreads();
-  const PfxSources s = src;
+  const float2* pre_ml = p.work.ml[kind] + (size_t)s1.x * kPfxRows + s1.y;
+  const float4* pre_O = p.work.O[kind] + (size_t)s1.x * kPfxRows * (D / 4) + s1.y;
+  const float2* own_ml = p.work.ml[kPfxOwn] + (size_t)s1.z * R;
+  const float4* own_O = p.work.O[kPfxOwn] + (size_t)s1.z * R * (D / 4);
   const int row_mask = (1 << sh.log_rows) - 1;
   const int row = tid & row_mask;
-  const int el = sh.cols << sh.log_rows;           // elements of this block
-  const int part = sh.parts > 1 ? tid / el : 0;    // more parts only where el <= half the threads
-  const int tid_e = tid - part * el;
-  const bool on = row < R && part < sh.parts;
-  const int c0 = blockIdx.y * sh.cols;
+  const int el = sh.cols << sh.log_rows;         // elements of this block, at most one a thread
+  const int part = sh.parts > 1 ? tid / el : 0;
+  const int e = tid - part * el;
+  const bool on = row < R && part < sh.parts && e < el;
+  const int col = blockIdx.y * sh.cols + (e >> sh.log_rows);
   const int chunk = kMergeStats >> sh.log_rows;
-  uint16_t* out = O + (((size_t)req * p.n_heads + (size_t)kvh * p.group) * p.q_len + row) * D;
-  for (int e0 = 0; e0 < el; e0 += kMergeThreads * kMergeEach) {
-    float4 acc[kMergeEach];
-#pragma unroll
-    for (int k = 0; k < kMergeEach; ++k) acc[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    float m = -INFINITY, l = 0.0f;
-    for (int s0 = 0; s0 < s.n; s0 += chunk) {
-      const int ns = min(chunk, s.n - s0);
-      __syncthreads();
-      for (int k = tid; k < ns << sh.log_rows; k += kMergeThreads) {
-        const int i = s0 + (k >> sh.log_rows), rr = k & row_mask;
-        if (rr < R)
-          stats[k] = i < s.n_pre ? s.pre_ml[(size_t)i * s.pre_step * kPfxRows + rr] : s.own_ml[(size_t)(i - s.n_pre) * R + rr];
-      }
-      __syncthreads();
-      if (!on) continue;
-      const float m_old = m;
-      for (int i = 0; i < ns; ++i) m = fmaxf(m, stats[(i << sh.log_rows) + row].x);
-      if (m == -INFINITY) continue;  // the row saw nothing yet
-      const float f = ex2_approx(m_old - m);
-      l *= f;
-#pragma unroll
-      for (int k = 0; k < kMergeEach; ++k) {
-        acc[k].x *= f;
-        acc[k].y *= f;
-        acc[k].z *= f;
-        acc[k].w *= f;
-      }
+  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  float m = -INFINITY, l = 0.0f;
+  for (int first = 0; first < n; first += chunk) {
+    const int ns = min(chunk, n - first);
+    if (first > 0) __syncthreads();
+    for (int k = tid; k < ns << sh.log_rows; k += kMergeThreads) {
+      const int i = first + (k >> sh.log_rows), rr = k & row_mask;
+      if (rr < R)
+        stats[k] = i < n_pre ? pre_ml[(size_t)i * pre_step * kPfxRows + rr] : own_ml[(size_t)(i - n_pre) * R + rr];
+    }
+    __syncthreads();
+    if (!on) continue;
+    const float m_old = m;
 #pragma unroll 4
-      for (int i = part; i < ns; i += sh.parts) {
-        const float2 st = stats[(i << sh.log_rows) + row];
-        const float w = ex2_approx(st.x - m);
-        const int g = s0 + i;
-        const bool pre = g < s.n_pre;
-        const float4* from =
-            pre ? s.pre_O + (size_t)g * s.pre_step * kPfxRows * (D / 4) : s.own_O + (size_t)(g - s.n_pre) * R * (D / 4);
-        const int stride = pre ? kPfxRows : R;
-        l += st.y * w;
-#pragma unroll
-        for (int k = 0; k < kMergeEach; ++k) {
-          const int e = tid_e + e0 + k * kMergeThreads;
-          if (e >= el) continue;
-          const float4 v = from[(c0 + (e >> sh.log_rows)) * stride + row];
-          // l of 0: the row saw nothing there, and its O is not defined.
-          const float u = st.y > 0.0f ? w : 0.0f;
-          acc[k].x += u > 0.0f ? u * v.x : 0.0f;
-          acc[k].y += u > 0.0f ? u * v.y : 0.0f;
-          acc[k].z += u > 0.0f ? u * v.z : 0.0f;
-          acc[k].w += u > 0.0f ? u * v.w : 0.0f;
-        }
-      }
-    }
-    if (sh.parts > 1) {  // a single pass, one element a thread
-      sums[tid] = acc[0];
-      part_l[tid] = l;
-      __syncthreads();
-      if (part == 0) {
-        for (int k = 1; k < sh.parts; ++k) {
-          const float4 v = sums[tid + k * el];
-          acc[0].x += v.x;
-          acc[0].y += v.y;
-          acc[0].z += v.z;
-          acc[0].w += v.w;
-          l += part_l[tid + k * el];
-        }
-      }
-    }
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-#pragma unroll
-    for (int k = 0; k < kMergeEach; ++k) {
-      const int e = tid_e + e0 + k * kMergeThreads;
-      if (!on || part > 0 || e >= el) continue;
-      *reinterpret_cast<uint2*>(out + 4 * (c0 + (e >> sh.log_rows))) =
-          make_uint2(pack_16x2<FP16>(acc[k].x * inv, acc[k].y * inv), pack_16x2<FP16>(acc[k].z * inv, acc[k].w * inv));
+    for (int i = 0; i < ns; ++i) m = fmaxf(m, stats[(i << sh.log_rows) + row].x);
+    if (m == -INFINITY) continue;  // the row saw nothing yet
+    const float f = ex2_approx(m_old - m);
+    l *= f;
+    acc.x *= f;
+    acc.y *= f;
+    acc.z *= f;
+    acc.w *= f;
+#pragma unroll 8
+    for (int i = part; i < ns; i += sh.parts) {
+      const int g = first + i;
+      const float2 st = stats[(i << sh.log_rows) + row];
+      const float4 v = g < n_pre ? pre_O[((size_t)g * pre_step * (D / 4) + col) * kPfxRows + row]
+                                 : own_O[((size_t)(g - n_pre) * (D / 4) + col) * R + row];
+      // l of 0: the row saw nothing there, and its O is not defined.
+      const bool seen = st.y > 0.0f;
+      const float u = seen ? ex2_approx(st.x - m) : 0.0f;
+      l += st.y * u;
+      acc.x += seen ? u * v.x : 0.0f;
+      acc.y += seen ? u * v.y : 0.0f;
+      acc.z += seen ? u * v.z : 0.0f;
+      acc.w += seen ? u * v.w : 0.0f;
     }
   }
+  if (sh.parts > 1) {
+    sums[tid] = acc;
+    part_l[tid] = l;
+    __syncthreads();
+    if (part == 0) {
+      for (int k = 1; k < sh.parts; ++k) {
+        const float4 v = sums[tid + k * el];
+        acc.x += v.x;
+        acc.y += v.y;
+        acc.z += v.z;
+        acc.w += v.w;
+        l += part_l[tid + k * el];
+      }
+    }
+  }
+  if (!on || part > 0) return;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  // Row `row` of the request's block of rows of this kv head: Q and O are
+  // [batch][n_kv_heads][rows][head_dim].
+  uint16_t* out = O + ((size_t)blockIdx.x * R + row) * D + 4 * col;
+  *reinterpret_cast<uint2*>(out) =
+      make_uint2(pack_16x2<FP16>(acc.x * inv, acc.y * inv), pack_16x2<FP16>(acc.z * inv, acc.w * inv));
 }
 
 template <int D, bool FP16>
@@ -1087,12 +1061,11 @@ cudaError_t launch_prefix_instance(const PfxLaunch& L) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   if ((e = cudaLaunchKernelEx(&cfg, kern, L.mapK, L.mapV, L.mapQ, L.mapQ1, L.p)) != cudaSuccess) return e;
-  // Shares of the columns: about two elements a thread.
+  // Shares of the columns: at most one element a thread.
   PfxMergeShape sh = {0, D / 4, 1};
   while ((1 << sh.log_rows) < L.p.rows) ++sh.log_rows;
-  while (sh.cols % 2 == 0 && (sh.cols << sh.log_rows) > kMergeThreads * kMergeEach) sh.cols /= 2;
+  while (sh.cols > 1 && (sh.cols << sh.log_rows) > kMergeThreads) sh.cols = sh.cols % 2 ? 1 : sh.cols / 2;
   sh.parts = kMergeThreads / (sh.cols << sh.log_rows);
-  if (sh.parts < 1) sh.parts = 1;
   cfg.gridDim = dim3(L.p.batch * L.p.cache.n_kv_heads, D / 4 / sh.cols);
   cfg.blockDim = dim3(kMergeThreads);
   cfg.dynamicSmemBytes = 0;
