@@ -315,15 +315,23 @@ __device__ __forceinline__ PfxSeg pfx_segment(const PfxParams& p, const PfxPlan&
   return s;
 }
 
+// Tiles of run k of a line (0 past its last run).
+__device__ __forceinline__ int pfx_run_tiles(const PfxCuts& c, int k) {
+  return k < c.runs ? pfx_cut(c, k + 1) - pfx_cut(c, k) : 0;
+}
+
 // ----------------------------------------------------------------- producers
-// Ring slots.  While pair items run, tile n of the CTA sits in slot n % NS of
-// both rings and both streams use it.  Afterwards stream w has the slots
-// w * NS / 2 .. of each ring to itself.  A slot's uses are counted across both
+// The items of the second line come first, then the pair items: their partial
+// results, the larger ones, are then still in L2 when the merge reads them.
+//
+// Ring slots.  At first stream w has the slots w * NS / 2 .. of each ring to
+// itself.  While pair items run, tile n of them sits in slot n % NS of both
+// rings and both streams use it.  A slot's uses are counted across both
 // phases: use u waits for the end of use u - 1.
 
 // One warp each: warp 8 (w = 0) and warp 11 (w = 1).  Each publishes the
-// schedule and loads Q of its stream.  While pair items run, warp 8 loads the
-// K tiles and warp 11 the V tiles of both; after that each loads its stream's.
+// schedule and loads Q of its stream, and at first its K and V tiles; while
+// pair items run, warp 8 loads the K tiles and warp 11 the V tiles of both.
 template <int D>
 __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, const CUtensorMap* mapQ,
                              const CUtensorMap* mapQ1, const PfxParams& p, const PfxPlan& plan, int w,
@@ -334,29 +342,22 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
   const int lane = threadIdx.x & 31;
   volatile int* abort = &sb.abort;
   const PfxTotals t = *plan.t;
-  const int G = gridDim.x, cta = blockIdx.x;
-  // Runs of the second phase start at the CTA after the last one with pair
-  // items, so that small problems spread out.
+  const int cta = blockIdx.x;
+  // Runs of the line start at the CTA after the last one with pair items, so
+  // that small problems spread out.
   int line_run = cta - t.pair.runs;
-  if (line_run < 0) line_run += G;
-  line_run += w * G;
+  if (line_run < 0) line_run += gridDim.x;
+  const int n0 = pfx_run_tiles(t.line, line_run), n1 = pfx_run_tiles(t.line, line_run + gridDim.x);
+  line_run += w * gridDim.x;
   int n_ent = 0, n_q = 0;            // schedule entries published, Q tiles loaded
   uint32_t issued = 0, parity = 0;   // by ring (8 bits each) and slot: loads of this warp, and their last use's parity
   int bad = 0;
   bool ok = true;
 
-  bool pair = cta < t.pair.runs;
-  const bool had_pairs = pair;
-  int run = pair ? cta : line_run;
-  int x = 0, x_end = 0;
-  if (pair) {
-    x = pfx_cut(t.pair, run);
-    x_end = pfx_cut(t.pair, run + 1);
-  } else if (run < t.line.runs) {
-    x = pfx_cut(t.line, run);
-    x_end = pfx_cut(t.line, run + 1);
-  }
-  const int n_pair = pair ? x_end - x : 0;
+  const bool has_pairs = cta < t.pair.runs;
+  bool pair = false;
+  int run = line_run;
+  int x = pfx_cut(t.line, run), x_end = x + (w ? n1 : n0);
   int n = 0;  // tiles of the phase so far
   PfxSeg seg;
   seg.left = 0;
@@ -372,17 +373,16 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
   for (;;) {
     if (seg.left == 0) {
       if (x == x_end) {
-        if (!pair) break;
-        // Both warps have issued all loads of the pair phase when they go on:
+        if (pair || !has_pairs) break;
+        // Both warps have issued all loads of the first phase when they go on:
         // the other's slots are then at most one use behind, which is as far
         // as a wait can tell.
         named_barrier_sync(1, 64);
-        pair = false;
+        pair = true;
         n = 0;
-        run = line_run;
-        if (run >= t.line.runs) break;
-        x = pfx_cut(t.line, run);
-        x_end = pfx_cut(t.line, run + 1);
+        run = cta;
+        x = pfx_cut(t.pair, run);
+        x_end = pfx_cut(t.pair, run + 1);
       }
       seg = pfx_segment(p, plan, pair, x, x_end, run);
       x += seg.left;
@@ -391,7 +391,7 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
     }
     const bool second = pair && w == 1;
     const int slot = pair ? n % NS : w * H + n % H;
-    const int use = pair ? n / NS : n / H + (n_pair - slot + NS - 1) / NS;
+    const int use = pair ? n / NS + ((slot < H ? n0 : n1) - slot % H + H - 1) / H : n / H;
     const int word = second ? seg.word2 : seg.word;
     const int e = n_ent % kPfxSched;
     if (n_ent >= kPfxSched) ok = pfx_warp_wait(&sb.sched_empty[w][e], ((n_ent / kPfxSched) - 1) & 1, abort, p.wait_ns);
@@ -449,7 +449,7 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
     seg.pos += kPfxKeys;
     if (seg.left > 0) fetch();
   }
-  if (had_pairs && pair) named_barrier_sync(1, 64);  // gave up before the end of the pair phase
+  if (has_pairs && !pair) named_barrier_sync(1, 64);  // gave up in the first phase
   if (ok) {
     const int e = n_ent % kPfxSched;
     if (n_ent >= kPfxSched) ok = pfx_warp_wait(&sb.sched_empty[w][e], ((n_ent / kPfxSched) - 1) & 1, abort, p.wait_ns);
@@ -1061,11 +1061,15 @@ cudaError_t launch_prefix_instance(const PfxLaunch& L) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   if ((e = cudaLaunchKernelEx(&cfg, kern, L.mapK, L.mapV, L.mapQ, L.mapQ1, L.p)) != cudaSuccess) return e;
-  // Shares of the columns: at most one element a thread.
+  // Shares of the columns: at most one element a thread, and more of them (the
+  // threads then share elements) while the blocks are few.
   PfxMergeShape sh = {0, D / 4, 1};
   while ((1 << sh.log_rows) < L.p.rows) ++sh.log_rows;
-  while (sh.cols > 1 && (sh.cols << sh.log_rows) > kMergeThreads) sh.cols = sh.cols % 2 ? 1 : sh.cols / 2;
+  const long long units = (long long)L.p.batch * L.p.cache.n_kv_heads;
+  while (sh.cols > 1 && ((sh.cols << sh.log_rows) > kMergeThreads || (units * (D / 4 / sh.cols) < 8 * L.grid && (sh.cols << sh.log_rows) > 32)))
+    sh.cols = sh.cols % 2 ? 1 : sh.cols / 2;
   sh.parts = kMergeThreads / (sh.cols << sh.log_rows);
+  if (sh.parts > 8) sh.parts = 8;
   cfg.gridDim = dim3(L.p.batch * L.p.cache.n_kv_heads, D / 4 / sh.cols);
   cfg.blockDim = dim3(kMergeThreads);
   cfg.dynamicSmemBytes = 0;
