@@ -958,7 +958,7 @@ struct PfxMergeShape {
 };
 
 template <int D, bool FP16>
-__global__ void __launch_bounds__(kMergeThreads) prefix_merge_kernel(const PfxParams p, const PfxMergeShape sh,
+__global__ void __launch_bounds__(kMergeThreads, 12) prefix_merge_kernel(const PfxParams p, const PfxMergeShape sh,
                                                                      uint16_t* O) {
   __shared__ float2 stats[kMergeStats];
   __shared__ float4 sums[kMergeThreads];
@@ -1002,21 +1002,31 @@ __global__ void __launch_bounds__(kMergeThreads) prefix_merge_kernel(const PfxPa
     acc.y *= f;
     acc.z *= f;
     acc.w *= f;
-#pragma unroll 8
-    for (int i = part; i < ns; i += sh.parts) {
-      const int g = first + i;
-      const float2 st = stats[(i << sh.log_rows) + row];
-      const float4 v = g < n_pre ? pre_O[((size_t)g * pre_step * (D / 4) + col) * kPfxRows + row]
-                                 : own_O[((size_t)(g - n_pre) * (D / 4) + col) * R + row];
-      // l of 0: the row saw nothing there, and its O is not defined.
-      const bool seen = st.y > 0.0f;
-      const float u = seen ? ex2_approx(st.x - m) : 0.0f;
-      l += st.y * u;
-      acc.x += seen ? u * v.x : 0.0f;
-      acc.y += seen ? u * v.y : 0.0f;
-      acc.z += seen ? u * v.z : 0.0f;
-      acc.w += seen ? u * v.w : 0.0f;
-    }
+    // The segments of the prefix in this chunk, then the own ones.  (A segment
+    // in which the row saw nothing has m = -inf and O = 0; a row that sees
+    // nothing anywhere has no O at all, and l stays 0.)
+    auto join = [&](int i0, int i1, const float4* from, size_t step) {
+      const float2* st = stats + (i0 << sh.log_rows) + row;
+      const int stat_step = sh.parts << sh.log_rows;
+#pragma unroll 4
+      for (int i = i0; i < i1; i += sh.parts) {
+        const float4 v = *from;
+        const float u = ex2_approx(st->x - m);
+        l += st->y * u;
+        acc.x += u * v.x;
+        acc.y += u * v.y;
+        acc.z += u * v.z;
+        acc.w += u * v.w;
+        from += step;
+        st += stat_step;
+      }
+    };
+    const int pre = min(max(n_pre - first, 0), ns);  // of the chunk
+    const size_t pre_seg = (size_t)pre_step * (D / 4) * kPfxRows, own_seg = (size_t)(D / 4) * R;
+    join(part, pre, pre_O + (first + part) * pre_seg + col * kPfxRows + row, sh.parts * pre_seg);
+    // This thread's next segment after those, counted in steps of `parts`.
+    const int i0 = part >= pre ? part : part + (pre - part + sh.parts - 1) / sh.parts * sh.parts;
+    join(i0, ns, own_O + (first + i0 - n_pre) * own_seg + col * R + row, sh.parts * own_seg);
   }
   if (sh.parts > 1) {
     sums[tid] = acc;
