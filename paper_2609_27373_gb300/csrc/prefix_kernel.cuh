@@ -65,7 +65,7 @@ __device__ __forceinline__ int pfx_pack(int req, int nreq, int kind, int flags) 
 
 template <int NS>
 struct PfxShared {
-  uint64_t k_full[NS], k_empty[NS], v_full[NS], v_empty[NS];  // empty: one arrival per stream
+  uint64_t k_full[NS], k_empty[NS], v_full[NS], v_empty[NS];
   uint64_t sched_full[2][kPfxSched], sched_empty[2][kPfxSched];  // empty: the two issuers and 4 warps
   uint64_t q_full[2], q_free[2];
   uint64_t s_full[2];  // S of a stream written
@@ -493,7 +493,7 @@ __device__ __forceinline__ constexpr uint32_t pfx_idesc(uint32_t bf16) {
 // everywhere in this kernel: its loops together stay small enough for the
 // instruction cache, whose misses bounded larger variants.)
 template <int D, bool FP16>
-__device__ void pfx_mma_s(const PfxParams& p, uint32_t tmem, uint8_t* q_tiles, uint8_t* ring,
+__device__ void pfx_mma_s(const PfxParams& p, int second, uint32_t tmem, uint8_t* q_tiles, uint8_t* ring,
                           PfxShared<PfxCfg<D>::kSlots>& sb) {
   using C = PfxCfg<D>;
   volatile int* abort = &sb.abort;
@@ -537,10 +537,9 @@ __device__ void pfx_mma_s(const PfxParams& p, uint32_t tmem, uint8_t* q_tiles, u
                         (uint32_t)(k0 >> 32), idesc, acc);
         }
         umma_commit(&sb.s_full[w]);
-        // A slot is empty after two arrivals: one for each stream of a pair's
-        // tile, both for this one otherwise.
-        umma_commit(&sb.k_empty[slot]);
-        if (((ent.z >> 17) & 3) != kPfxPair) umma_commit(&sb.k_empty[slot]);
+        // A commit covers every product of this thread before it, so a pair's
+        // slot is given back with the second of its two products.
+        if (((ent.z >> 17) & 3) != kPfxPair || w == second) umma_commit(&sb.k_empty[slot]);
         if (flags & kPfxLast) umma_commit(&sb.q_free[w]);
         ++used;
         ++t.j;
@@ -566,7 +565,7 @@ __device__ void pfx_mma_s(const PfxParams& p, uint32_t tmem, uint8_t* q_tiles, u
 
 // One thread: the P V products.
 template <int D, bool FP16>
-__device__ void pfx_mma_pv(const PfxParams& p, uint32_t tmem, uint8_t* ring, PfxShared<PfxCfg<D>::kSlots>& sb) {
+__device__ void pfx_mma_pv(const PfxParams& p, int second, uint32_t tmem, uint8_t* ring, PfxShared<PfxCfg<D>::kSlots>& sb) {
   using C = PfxCfg<D>;
   constexpr int NS = C::kSlots;
   volatile int* abort = &sb.abort;
@@ -603,8 +602,7 @@ __device__ void pfx_mma_pv(const PfxParams& p, uint32_t tmem, uint8_t* ring, Pfx
           acc = 1;
         }
         umma_commit(&sb.o_full[w]);
-        umma_commit(&sb.v_empty[slot]);
-        if (((ent.z >> 17) & 3) != kPfxPair) umma_commit(&sb.v_empty[slot]);
+        if (((ent.z >> 17) & 3) != kPfxPair || w == second) umma_commit(&sb.v_empty[slot]);
         ++t.j;
       }
     }
@@ -879,8 +877,8 @@ __global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
     for (int i = 0; i < C::kSlots; ++i) {
       mbar_init(&sb.k_full[i], 1);
       mbar_init(&sb.v_full[i], 1);
-      mbar_init(&sb.k_empty[i], 2);
-      mbar_init(&sb.v_empty[i], 2);
+      mbar_init(&sb.k_empty[i], 1);
+      mbar_init(&sb.v_empty[i], 1);
     }
     for (int w = 0; w < 2; ++w) {
       for (int i = 0; i < kPfxSched; ++i) {
@@ -925,10 +923,16 @@ __global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
     if (warp == 8 || warp == 11) {
       pfx_producer<D>(&mapK, &mapV, &mapQ, &mapQ1, p, plan, warp == 11, q_tiles, ring, sb);
     } else if (lane == 0) {
+      // The stream that takes the second turn at a pair's tile: stream 1,
+      // unless stream 0 had one tile more before.
+      const PfxCuts line = plan.t->line;
+      int run = (int)blockIdx.x - plan.t->pair.runs;
+      if (run < 0) run += gridDim.x;
+      const int second = pfx_run_tiles(line, run) == pfx_run_tiles(line, run + gridDim.x);
       if (warp == 9)
-        pfx_mma_s<D, FP16>(p, tmem, q_tiles, ring, sb);
+        pfx_mma_s<D, FP16>(p, second, tmem, q_tiles, ring, sb);
       else
-        pfx_mma_pv<D, FP16>(p, tmem, ring, sb);
+        pfx_mma_pv<D, FP16>(p, second, tmem, ring, sb);
     }
   }
   __syncwarp();
