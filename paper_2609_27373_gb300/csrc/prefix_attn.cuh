@@ -63,7 +63,7 @@ struct PfxTotals {
   PfxCuts pair;      // the line of pair items
   PfxCuts line;      // the other line: single items first, then own items
   int single_tiles;  // tiles of the single items
-  int grouped;       // 0 when the groups were faulty (nothing is shared)
+  int pad;
 };
 
 struct PfxPlan {
@@ -80,14 +80,15 @@ struct PfxPlan {
   int* lead;         // first active member
   int* tiles;        // key tiles of the shared prefix, 0 if nothing is shared
   int* pairs;        // pairs of row tiles
-  int* pair_base;    // [n_groups + 1] pair tiles before it
-  int* pair_item;    // pair items (of one kv head) before it
-  int* single_base;  // [n_groups + 1]
-  int* single_item;
+  // One after the other, [n_groups + 1] each: sums over the groups before.
+  int* pair_base;    // pair tiles
+  int* pair_item;    // pair items of one kv head
+  int* single_base;  // single tiles
+  int* single_item;  // single items of one kv head
 };
 
 __host__ __device__ inline int pfx_plan_ints(int batch, int n_groups) {
-  return 8 + 6 * batch + 1 + 8 * n_groups + 3;
+  return 8 + 6 * batch + 1 + 8 * n_groups + 5;
 }
 
 __host__ __device__ inline PfxPlan pfx_plan(int* base, int batch, int n_groups) {
@@ -105,7 +106,7 @@ __host__ __device__ inline PfxPlan pfx_plan(int* base, int batch, int n_groups) 
   p.pairs = p.tiles + n_groups;
   p.pair_base = p.pairs + n_groups;
   p.pair_item = p.pair_base + n_groups + 1;
-  p.single_base = p.pair_item + n_groups;
+  p.single_base = p.pair_item + n_groups + 1;
   p.single_item = p.single_base + n_groups + 1;
   return p;
 }

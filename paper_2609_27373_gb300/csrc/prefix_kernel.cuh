@@ -74,14 +74,15 @@ struct PfxShared {
   uint64_t o_full[2];  // P V completed
   uint64_t done[2];
   int4 sched[2][kPfxSched];
-  int warp_sums[32];
   uint32_t tmem_base;
   int abort;
 };
 
 // ---------------------------------------------------------------------- plan
+// Written for few instructions: in a launch's first microseconds every line of
+// code is fetched from far away (some 500 clk for 8 instructions).
 // All threads of the CTA; `plan` in shared memory.
-__device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, int* warp_sums, bool report) {
+__device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, bool report) {
   const CacheView& c = p.cache;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
   int bad = 0, bad_groups = 0;
@@ -138,6 +139,13 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, in
     if (lane == 0) {
       plan.tiles[g] = tiles;
       plan.lead[g] = lead;
+      const int row_tiles = tiles > 0 ? (e - a + p.per_tile - 1) / p.per_tile : 0;
+      const int pairs = row_tiles >> 1, single = row_tiles & 1;
+      plan.pairs[g] = pairs;
+      plan.pair_base[g] = pairs * tiles * c.n_kv_heads;
+      plan.pair_item[g] = pairs;
+      plan.single_base[g] = single * tiles * c.n_kv_heads;
+      plan.single_item[g] = single;
     }
     if (shared > 0) {
 #pragma unroll 1
@@ -148,72 +156,47 @@ __device__ inline void pfx_make_plan(const PfxParams& p, const PfxPlan& plan, in
     }
   }
   __syncthreads();
-  // Prefix sums: over the requests by all warps together, and then over the
-  // groups (four counts each) by warp 0.
-  int before = 0;
+  // Prefix sums, a warp each, four entries a lane: the groups' four counts
+  // (warps 0-3) and the requests' own tiles (warp 4).
+  if (warp < 5) {
+    int* list = warp < 4 ? plan.pair_base + warp * (p.n_groups + 1) : plan.cum;
+    const int n = warp < 4 ? p.n_groups : p.batch;
+    int before = 0;
 #pragma unroll 1
-  for (int r0 = 0; r0 < p.batch; r0 += blockDim.x) {
-    const int r = r0 + tid;
-    const int t = r < p.batch ? max(0, plan.len[r] - plan.lo[r] + kPfxKeys - 1) / kPfxKeys : 0;
-    int v = t;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, v, o);
-      if (lane >= o) v += u;
-    }
-    if (lane == 31) warp_sums[warp] = v;
-    __syncthreads();
-    const int other = lane < n_warps ? warp_sums[lane] : 0;
-    const int below = __reduce_add_sync(0xffffffffu, lane < warp ? other : 0);
-    if (r < p.batch) plan.cum[r] = before + below + v - t;
-    before += __reduce_add_sync(0xffffffffu, other);
-    if (r0 + (int)blockDim.x < p.batch) __syncthreads();  // warp_sums is used again
-  }
-  if (warp == 0) {
-    int b[4] = {0, 0, 0, 0};  // pair tiles, pair items, single tiles, single items
-#pragma unroll 1
-    for (int g0 = 0; g0 < p.n_groups; g0 += 32) {
-      const int g = g0 + lane;
-      int own[4] = {0, 0, 0, 0}, v[4];
-      if (g < p.n_groups && plan.tiles[g] > 0) {
-        const int row_tiles = (plan.start[g + 1] - plan.start[g] + p.per_tile - 1) / p.per_tile;
-        own[1] = row_tiles / 2;
-        plan.pairs[g] = own[1];
-        own[3] = row_tiles & 1;
-        own[0] = own[1] * plan.tiles[g] * c.n_kv_heads;
-        own[2] = own[3] * plan.tiles[g] * c.n_kv_heads;
-      }
+    for (int i0 = 0; i0 < n; i0 += 128) {
+      const int first = i0 + 4 * lane;
+      int x[4], sum = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        v[k] = own[k];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int u = __shfl_up_sync(0xffffffffu, v[k], o);
-          if (lane >= o) v[k] += u;
-        }
+        x[k] = 0;
+        if (first + k < n)
+          x[k] = warp < 4 ? list[first + k]
+                          : max(0, plan.len[first + k] - plan.lo[first + k] + kPfxKeys - 1) / kPfxKeys;
+        sum += x[k];
       }
-      if (g < p.n_groups) {
-        plan.pair_base[g] = b[0] + v[0] - own[0];
-        plan.pair_item[g] = b[1] + v[1] - own[1];
-        plan.single_base[g] = b[2] + v[2] - own[2];
-        plan.single_item[g] = b[3] + v[3] - own[3];
+      int upto = sum;
+#pragma unroll 1
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += u;
       }
+      int at = before + upto - sum;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) b[k] += __shfl_sync(0xffffffffu, v[k], 31);
+      for (int k = 0; k < 4; ++k) {
+        if (first + k < n) list[first + k] = at;
+        at += x[k];
+      }
+      before += __shfl_sync(0xffffffffu, upto, 31);
     }
-    // Lane 0 cuts the line of pair items, lane 1 the other one.
-    const int line = b[2] + before * c.n_kv_heads;
-    const PfxCuts cuts = pfx_cuts(lane == 0 ? b[0] : line, gridDim.x << (lane == 0 ? 0 : 1));
-    if (lane == 0) {
-      plan.cum[p.batch] = before;
-      plan.pair_base[p.n_groups] = b[0];
-      plan.single_base[p.n_groups] = b[2];
-      plan.t->pair = cuts;
-      plan.t->single_tiles = b[2];
-      plan.t->grouped = grouped;
-    } else if (lane == 1) {
-      plan.t->line = cuts;
-    }
+    if (lane == 0) list[n] = before;
+  }
+  __syncthreads();
+  if (tid < 2) {  // thread 0 cuts the line of pair items, thread 1 the other one
+    const int single = plan.single_base[p.n_groups];
+    const PfxCuts cuts = pfx_cuts(tid == 0 ? plan.pair_base[p.n_groups] : single + plan.cum[p.batch] * c.n_kv_heads,
+                                  gridDim.x << tid);
+    (tid == 0 ? plan.t->pair : plan.t->line) = cuts;
+    if (tid == 0) plan.t->single_tiles = single;
   }
   __syncthreads();
 }
@@ -906,7 +889,7 @@ __global__ void __launch_bounds__(PfxCfg<D>::kThreads, 1)
   // Everything above may overlap the previous kernel of the stream.
   griddep_wait();
   tc_fence_before_sync();
-  pfx_make_plan(p, plan, sb.warp_sums, blockIdx.x == 0);  // ends with a barrier
+  pfx_make_plan(p, plan, blockIdx.x == 0);  // ends with a barrier
   tc_fence_after_sync();
   const uint32_t tmem = sb.tmem_base;
   if (threadIdx.x == 0) griddep_launch_dependents();  // the merge waits for this grid's end
