@@ -12,15 +12,24 @@
 //   warps 8, 11     producers: walk the tiles of stream 0 and 1, look their
 //                   pages up (a lane per page, one tile ahead), publish the
 //                   schedule and issue the TMA loads of Q, K and V.
-//   warp 9          one thread: S = Q K^T of both streams, whichever is ready.
-//   warp 10         one thread: O += P V of both streams.
+//   warp 9          one thread: S = Q K^T of both streams in turn.
+//   warp 10         one thread: O += P V of both streams in turn.
 // TMEM: S at column 0, P of stream w at 128 + 64 w, O at 256 + 128 w; with a
 // head dimension of 64 there is room for an S of each stream (stream 1's at
 // 384, O at 256 + 64 w).  S is handed to the next product as soon as it has
 // been read, so a stream's softmax runs beside the products of the other one
 // and beside its own next S.  (With P written over S, and one issuing thread a
 // stream, the next S had to wait for P V: 5250 clk a pair's tile of 128 + 128
-// rows at head dimension 128.)
+// rows at head dimension 128; now 3700, two turns of the one S buffer: 8
+// products at 89 clk, 400 until the softmax sees S, 300 to read it, 380 until
+// the next product.)
+//
+// What bounds it.  Long unshared sequences: HBM (38 x 8 x 8000 tokens of 128,
+// 1.25 GB, in 182 us, 6.8 TB/s).  Prefixes with 256 or more query rows a kv
+// head: the S buffer, at about half of the tensor rate.  Short items: what a
+// segment costs besides its tiles (some 4000 clk of softmax, epilogue and
+// look-ups for one request's last tile).  Small calls: the first microseconds
+// of a launch, in which every line of code comes from far away.
 //
 // Every wait is bounded; one that runs out sets the status word and an abort
 // flag, and every role unwinds.
