@@ -689,27 +689,9 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
       sum = exp2_scaled(s, p.scale_log2, m_new == -INFINITY ? 0.0f : m_new);
 #pragma unroll
       for (int k = 0; k < kPfxKeys / 2; ++k) pw[k] = pack_16x2<FP16>(s[2 * k], s[2 * k + 1]);
-    } else if (warp_on) {
-      // 32 columns at a time, read twice: short items and the ends of long
-      // ones cost what they hold, and the loop's code is small.
-      float m_tile = -INFINITY;
-#pragma unroll 1
-      for (int c = 0; c < chunks; ++c) {
-        uint32_t v[32];
-        tmem_ld_32x32b_x32(lane_tmem + s_col + 32 * c, v);
-        tmem_ld_wait(v);
-        const int last = lim - 32 * c;
-#pragma unroll
-        for (int k = 0; k < 32; ++k) m_tile = fmaxf(m_tile, k <= last ? __uint_as_float(v[k]) : -INFINITY);
-      }
-      m_tile *= p.scale_log2;
-      m_new = (m_tile > m + kRescaleThreshold) ? m_tile : m;
-    } else if (lane == 0) {
+    } else if (!warp_on && lane == 0) {
       mbar_arrive(s_free);
     }
-    const bool rescale = live && m_new != m && m != -INFINITY;
-    const float f = rescale ? ex2_approx(m - m_new) : 1.0f;
-    m = m_new;
     // P and O are at rest once the previous P V has completed.  (Warps without
     // a row wait as well: their arrivals below must not run ahead.)
     if (j > 0 && !warp_wait(&sb.o_full[w], (j - 1) & 1, abort, p.wait_ns)) {
@@ -726,7 +708,9 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
         tmem_st_32x32b_x16(lane_tmem + p_col + 16 * c, q);
       }
     } else if (warp_on) {
-      const float shift = m == -INFINITY ? 0.0f : m;
+      // 32 columns at a time: short items and the ends of long ones cost what
+      // they hold, and the loop's code is small.  A later chunk whose maximum
+      // is far above the earlier ones' starts the tile over.
 #pragma unroll 1
       for (int c = 0; c < chunks; ++c) {
         uint32_t v[32], q[16];
@@ -736,7 +720,15 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
         float x[32];
 #pragma unroll
         for (int k = 0; k < 32; ++k) x[k] = k <= last ? __uint_as_float(v[k]) : -INFINITY;
-        sum += exp2_scaled(x, p.scale_log2, shift);
+        const float m_chunk = row_max(x) * p.scale_log2;
+        const bool grows = live && m_chunk > m_new + kRescaleThreshold;
+        if (grows) m_new = m_chunk;
+        if (c > 0 && __any_sync(0xffffffffu, grows)) {
+          sum = 0.0f;
+          c = -1;
+          continue;
+        }
+        sum += exp2_scaled(x, p.scale_log2, m_new == -INFINITY ? 0.0f : m_new);
 #pragma unroll
         for (int k = 0; k < 16; ++k) q[k] = pack_16x2<FP16>(x[2 * k], x[2 * k + 1]);
         tmem_st_32x32b_x16(lane_tmem + p_col + 16 * c, q);
@@ -745,6 +737,9 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
       __syncwarp();
       if (lane == 0) mbar_arrive(s_free);
     }
+    const bool rescale = live && m_new != m && m != -INFINITY;
+    const float f = rescale ? ex2_approx(m - m_new) : 1.0f;
+    m = m_new;
     l = l * f + sum;
     if (warp_on) {
       if (__any_sync(0xffffffffu, rescale)) {
