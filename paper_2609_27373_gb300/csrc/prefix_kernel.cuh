@@ -636,6 +636,8 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
   const uint32_t o_col = C::kTmemO + w * C::kTmemOStep;
   uint64_t* s_free = &sb.s_free[own_buf ? w : 0];
   bool ok = true;
+  // The thread's row of any tile: its request among the tile's, its new token.
+  const int of = r / p.rows, i = (r - of * p.rows) % p.q_len;
   int limit = 0;                                        // keys the row may see
   bool row_on = false, live = false, warp_on = false;  // a row of the item; one that sees keys; a warp with such
   float m = -INFINITY, l = 0.0f;
@@ -652,7 +654,6 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
     if (flags & kPfxEnd) break;
     if (flags & kPfxFirst) {
       const int req0 = ent.z & 1023, nreq = ((ent.z >> 10) & 127) + 1;
-      const int of = r / p.rows, i = r % p.rows % p.q_len;
       row_on = of < nreq;
       int seen = 0;
       if (row_on) {
