@@ -130,7 +130,7 @@ extern "C" int wise_kv_write(const wise_cache_t* cache, int layer, const int32_t
   if (rc != WISE_OK) return rc;
   if (layer < 0 || layer >= cache->n_layers || batch < 0 || q_len < 0) return WISE_ERR_INVALID_ARG;
   if (batch == 0 || q_len == 0) return WISE_OK;
-  if (batch > kMaxSlots || (long long)batch * q_len > (1LL << 30)) return WISE_ERR_UNSUPPORTED;
+  if (batch > kMaxSlots || (long long)batch * q_len > (1LL << 30) / cache->n_kv_heads) return WISE_ERR_UNSUPPORTED;
   if (!ok32(slots) || !aligned(n_new, 4) || !K || !V || !aligned(K, 16) || !aligned(V, 16))
     return WISE_ERR_INVALID_ARG;
   int sms;
