@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const CacheV
 // Moves pages (sources lie at or past n_live, destinations below it, so the
 // copies are independent) and renames the tables' entries.  A job is 16 KB of a
 // page in one plane, so that a few large pages still fill the GPU.  What bounds
-// it: memory (1.36 GB read and written in 219 us, 6.2 TB/s).
+// it: memory (0.68 GB read and as much written in 219 us, 6.2 TB/s).
 __global__ void __launch_bounds__(256) compact_move_kernel(const CacheView c, const int32_t* remap,
                                                            const int32_t* work) {
   griddep_wait();
