@@ -241,6 +241,11 @@ static __device__ __noinline__ void pfx_give_up(int* abort, int* status) {
   atomicOr(status, kStatusTimeout);
 }
 
+// The row of the tile at which an own item's rows start.  Few rows keep one
+// warp of a stream busy; that of stream 1 is then on another scheduler of the
+// SM than that of stream 0.
+__device__ __forceinline__ int pfx_own_row(const PfxParams& p, int w) { return w == 1 && p.rows <= 32 ? 96 : 0; }
+
 // A segment: a run of key tiles of an item.
 struct PfxSeg {
   int word, word2;  // requests and kind as in a schedule entry; of a pair's second tile
@@ -429,7 +434,7 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
           mbar_arrive_expect_tx(&sb.q_full[w], (own ? p.rows : p.rows * p.per_tile) * 128 * C::kBoxes);
 #pragma unroll
           for (int b = 0; b < C::kBoxes; ++b)
-            tma_load_4d(q_tiles + w * C::kTileBytes + b * 128 * 128, own ? mapQ1 : mapQ, &sb.q_full[w], 64 * b, 0,
+            tma_load_4d(q_tiles + w * C::kTileBytes + (b * 128 + (own ? pfx_own_row(p, w) : 0)) * 128, own ? mapQ1 : mapQ, &sb.q_full[w], 64 * b, 0,
                         seg.kvh, word & 1023);
         }
         ++n_q;
@@ -638,6 +643,7 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
   bool ok = true;
   // The thread's row of any tile: its request among the tile's, its new token.
   const int of = r / p.rows, i = (r - of * p.rows) % p.q_len;
+  const int own_r = r - pfx_own_row(p, w), own_i = own_r < 0 ? 0 : own_r % p.q_len;
   int limit = 0;                                        // keys the row may see
   bool row_on = false, live = false, warp_on = false;  // a row of the item; one that sees keys; a warp with such
   float m = -INFINITY, l = 0.0f;
@@ -654,11 +660,12 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
     if (flags & kPfxEnd) break;
     if (flags & kPfxFirst) {
       const int req0 = ent.z & 1023, nreq = ((ent.z >> 10) & 127) + 1;
-      row_on = of < nreq;
+      const bool own = kind == kPfxOwn;
+      row_on = own ? own_r >= 0 && own_r < p.rows : of < nreq;
       int seen = 0;
       if (row_on) {
-        const int req = req0 + of, add = plan.add[req];
-        seen = i < add ? plan.len[req] - add + i + 1 : 0;
+        const int req = req0 + (own ? 0 : of), add = plan.add[req], k = own ? own_i : i;
+        seen = k < add ? plan.len[req] - add + k + 1 : 0;
       }
       // Threads whose row sees nothing (or is none) compute on whatever Q
       // holds there and store no O; unmasked, they do not hold up their warp.
@@ -781,12 +788,12 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
         break;
       }
       tc_fence_after_sync();
-      const int rows = kind == kPfxOwn ? p.rows : kPfxRows;
+      const int rows = kind == kPfxOwn ? p.rows : kPfxRows, row = kind == kPfxOwn ? own_r : r;
       float2* ml = kind == kPfxOwn ? p.work.ml[0] : kind == kPfxSingle ? p.work.ml[1] : p.work.ml[2];
-      if (row_on) ml[(size_t)ent.w * rows + r] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
+      if (row_on) ml[(size_t)ent.w * rows + row] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
       if (warp_on) {
         float4* O = kind == kPfxOwn ? p.work.O[0] : kind == kPfxSingle ? p.work.O[1] : p.work.O[2];
-        float4* out = O + (size_t)ent.w * rows * (D / 4) + r;
+        float4* out = O + (size_t)ent.w * rows * (D / 4) + row;
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
           uint32_t v[32];
