@@ -243,7 +243,9 @@ static __device__ __noinline__ void pfx_give_up(int* abort, int* status) {
 
 // The row of the tile at which an own item's rows start.  Few rows keep one
 // warp of a stream busy; that of stream 1 is then on another scheduler of the
-// SM than that of stream 0.
+// SM than that of stream 0 (2432 items of one row and four tiles: 44 us on the
+// same scheduler, 39 us on any other one; the few rows of prefix items gain
+// nothing from it).
 __device__ __forceinline__ int pfx_own_row(const PfxParams& p, int w) { return w == 1 && p.rows <= 32 ? 96 : 0; }
 
 // A segment: a run of key tiles of an item.
