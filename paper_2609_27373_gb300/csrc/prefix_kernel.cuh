@@ -685,21 +685,24 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
     const int keys = ent.x >> 16;                        // of the tile
     const int lim = min(limit - ent.y, keys) - 1;        // last column the row sees
     const bool masked = __any_sync(0xffffffffu, lim < kPfxKeys - 1);
-    const int chunks = (keys + 31) / 32;
     float m_new = m, sum = 0.0f;
     uint32_t pw[kPfxKeys / 2];
-    if (warp_on && !masked) {
+    if (warp_on) {
       float s[kPfxKeys];
       tmem_load_row<kPfxKeys>(lane_tmem + s_col, s);
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(s_free);
+      if (masked) {
+#pragma unroll
+        for (int k = 0; k < kPfxKeys; ++k) s[k] = k <= lim ? s[k] : -INFINITY;
+      }
       const float m_tile = row_max(s) * p.scale_log2;
       m_new = (m_tile > m + kRescaleThreshold) ? m_tile : m;
       sum = exp2_scaled(s, p.scale_log2, m_new == -INFINITY ? 0.0f : m_new);
 #pragma unroll
       for (int k = 0; k < kPfxKeys / 2; ++k) pw[k] = pack_16x2<FP16>(s[2 * k], s[2 * k + 1]);
-    } else if (!warp_on && lane == 0) {
+    } else if (lane == 0) {
       mbar_arrive(s_free);
     }
     // P and O are at rest once the previous P V has completed.  (Warps without
@@ -709,7 +712,7 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
       break;
     }
     tc_fence_after_sync();
-    if (warp_on && !masked) {
+    if (warp_on) {
 #pragma unroll
       for (int c = 0; c < kPfxKeys / 32; ++c) {
         uint32_t q[16];
@@ -717,35 +720,6 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
         for (int k = 0; k < 16; ++k) q[k] = pw[16 * c + k];
         tmem_st_32x32b_x16(lane_tmem + p_col + 16 * c, q);
       }
-    } else if (warp_on) {
-      // 32 columns at a time: short items and the ends of long ones cost what
-      // they hold, and the loop's code is small.  A later chunk whose maximum
-      // is far above the earlier ones' starts the tile over.
-#pragma unroll 1
-      for (int c = 0; c < chunks; ++c) {
-        uint32_t v[32], q[16];
-        tmem_ld_32x32b_x32(lane_tmem + s_col + 32 * c, v);
-        tmem_ld_wait(v);
-        const int last = lim - 32 * c;
-        float x[32];
-#pragma unroll
-        for (int k = 0; k < 32; ++k) x[k] = k <= last ? __uint_as_float(v[k]) : -INFINITY;
-        const float m_chunk = row_max(x) * p.scale_log2;
-        const bool grows = live && m_chunk > m_new + kRescaleThreshold;
-        if (grows) m_new = m_chunk;
-        if (c > 0 && __any_sync(0xffffffffu, grows)) {
-          sum = 0.0f;
-          c = -1;
-          continue;
-        }
-        sum += exp2_scaled(x, p.scale_log2, m_new == -INFINITY ? 0.0f : m_new);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) q[k] = pack_16x2<FP16>(x[2 * k], x[2 * k + 1]);
-        tmem_st_32x32b_x16(lane_tmem + p_col + 16 * c, q);
-      }
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(s_free);
     }
     const bool rescale = live && m_new != m && m != -INFINITY;
     const float f = rescale ? ex2_approx(m - m_new) : 1.0f;
