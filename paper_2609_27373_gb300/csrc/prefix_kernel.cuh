@@ -695,7 +695,13 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
       if (lane == 0) mbar_arrive(s_free);
       if (masked) {
 #pragma unroll
-        for (int k = 0; k < kPfxKeys; ++k) s[k] = k <= lim ? s[k] : -INFINITY;
+        for (int c = 0; c < kPfxKeys / 32; ++c) {
+          // Bit k: the row sees column 32 c + k.
+          const int n = lim + 1 - 32 * c;
+          const uint32_t seen = n >= 32 ? ~0u : n > 0 ? (1u << n) - 1 : 0u;
+#pragma unroll
+          for (int k = 0; k < 32; ++k) s[32 * c + k] = (seen >> k) & 1 ? s[32 * c + k] : -INFINITY;
+        }
       }
       const float m_tile = row_max(s) * p.scale_log2;
       m_new = (m_tile > m + kRescaleThreshold) ? m_tile : m;
