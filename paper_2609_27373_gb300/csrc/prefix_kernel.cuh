@@ -26,10 +26,13 @@
 //
 // What bounds it.  Long unshared sequences: HBM (38 x 8 x 8000 tokens of 128,
 // 1.25 GB, in 182 us, 6.8 TB/s).  Prefixes with 256 or more query rows a kv
-// head: the S buffer, at about half of the tensor rate.  Short items: what a
-// segment costs besides its tiles (some 4000 clk of softmax, epilogue and
-// look-ups for one request's last tile).  Small calls: the first microseconds
-// of a launch, in which every line of code comes from far away.
+// head: the S buffer, at about half of the tensor rate.  Short items: one
+// warp's softmax of a tile (3600 to 4200 clk, twice what its instructions would
+// take if they were at hand) in 7000 clk from tile to tile.  So S is read whole
+// and given back before it is masked: with masked tiles taken 32 columns at a
+// time the other stream waited for S (256 samples on a prefix of 8192 tokens:
+// 74 us, now 71).  Small calls: the first microseconds of a launch, in which
+// every line of code comes from far away.
 //
 // Every wait is bounded; one that runs out sets the status word and an abort
 // flag, and every role unwinds.
