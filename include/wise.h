@@ -350,7 +350,8 @@ int wise_kv_extend(const wise_cache_t* cache, const int32_t* slots, const int32_
  * lens[slots[b]] - n_new[b] + i of the sequence in slot slots[b] (lens as
  * wise_kv_extend left it, n_new its `granted`; NULL = q_len for all).  Rows
  * that fall on a page with several holders are left out and recorded as
- * WISE_ERR_BAD_CACHE.  K, V: 16-byte aligned. */
+ * WISE_ERR_BAD_CACHE.  K, V: 16-byte aligned;
+ * batch * n_kv_heads * q_len <= 2^30. */
 int wise_kv_write(const wise_cache_t* cache, int layer, const int32_t* slots, const int32_t* n_new, int batch,
                   int q_len, const void* K, const void* V, cudaStream_t stream);
 

@@ -70,6 +70,12 @@ def test_null_and_misaligned_arguments():
     assert lib.wise_kv_compact(r, NULL, PTR, PTR, NULL) == bad
 
 
+def test_write_counts_rows_in_32_bits():
+    lib, r = wise.load(), ctypes.byref(cache(n_kv_heads=2))
+    assert lib.wise_kv_write(r, 0, PTR, NULL, 1, (1 << 29) + 1, PTR, PTR, NULL) == wise.WISE_ERR_UNSUPPORTED
+    assert lib.wise_kv_write(r, 0, PTR, NULL, 1 << 10, (1 << 19) + 1, PTR, PTR, NULL) == wise.WISE_ERR_UNSUPPORTED
+
+
 def test_empty_lists_do_nothing():
     lib, r = wise.load(), ctypes.byref(cache())
     assert lib.wise_kv_fork(r, NULL, NULL, 0, NULL) == 0
