@@ -17,7 +17,10 @@ the library's entry points in their order of use:
 Every call is asynchronous on `stream` (default: torch's current stream);
 calls on one cache must be ordered on a stream, and two calls that may run at
 the same time need a PagedCache each over the same tensors (`over`), since
-each keeps one workspace.
+each keeps one workspace.  The cache's own memory is recorded on every stream
+that its calls run on, so that the cache can be let go while they run; what a
+call is given besides (lists, keys and values, queries, outputs) is the
+caller's to keep.
 """
 from __future__ import annotations
 
@@ -26,10 +29,8 @@ import torch
 from . import wise
 
 
-def _empty(shape, dtype, device, stream, replaces=None):
-    """Memory of the stream that the call runs on.  `replaces` was used by earlier calls, which that stream follows."""
-    if replaces is not None:
-        replaces.record_stream(torch.cuda.current_stream(device) if stream is None else stream)
+def _empty(shape, dtype, device, stream):
+    """Memory of the stream that the call runs on."""
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
@@ -56,25 +57,42 @@ class PagedCache(wise.Cache):
 
     def _own(self, pool, table, lens, refs) -> None:
         wise.Cache.__init__(self, pool, table, lens, refs)
+        self._streams = {}  # streams that have used the cache, by handle
         self._kv_ws = None
         self._kv_n = -1
         self._attn_ws = None
         self._attn_key = self._attn_shape = None
 
+    def _use(self, stream) -> None:
+        """Before a call on `stream`: torch does not hand the cache's memory out again before that stream is done."""
+        raw = wise._raw_stream(stream, self.index)
+        if raw not in self._streams:
+            self._streams[raw] = torch.cuda.current_stream(self.device) if stream is None else stream
+            for t in (self.pool, self.table, self.lens, self.refs, self._kv_ws, self._attn_ws):
+                if t is not None:
+                    t.record_stream(self._streams[raw])
+
+    def _new_workspace(self, need: int, stream):
+        # 0 bytes: the library refuses this cache, and the call itself says why.
+        ws = _empty(max(need, 16), torch.uint8, self.device, stream)
+        for s in self._streams.values():
+            ws.record_stream(s)
+        return ws
+
     def _kv_workspace(self, n: int, stream):
         if n > self._kv_n:
-            # 0 bytes: the library refuses this cache, and the call itself says why.
-            need = max(wise.wise_kv_workspace(self, n), 16)
-            self._kv_ws = _empty(need, torch.uint8, self.device, stream, self._kv_ws)
+            self._kv_ws = self._new_workspace(wise.wise_kv_workspace(self, n), stream)
             self._kv_n = n
         return self._kv_ws
 
     def fork(self, src, dst, stream=None) -> None:
         """Slots dst[i] become forks of slots src[i]; pages are shared until one of the holders grows."""
+        self._use(stream)
         wise.wise_kv_fork(self, src, dst, stream)
 
     def extend(self, slots, n_new, granted=None, stream=None):
         """Grows the sequences by n_new tokens each; returns what was granted (n_new, or 0 where pages ran out)."""
+        self._use(stream)
         if granted is None:
             granted = _empty(n_new.shape, torch.int32, self.device, stream)
         wise.wise_kv_extend(self, slots, n_new, granted, self._kv_workspace(slots.shape[0], stream), stream)
@@ -82,14 +100,17 @@ class PagedCache(wise.Cache):
 
     def write(self, layer: int, slots, granted, K, V, stream=None) -> None:
         """Stores one layer's new keys and values [batch, n_kv_heads, q_len, head_dim] at the sequences' ends."""
+        self._use(stream)
         wise.wise_kv_write(self, layer, slots, granted, K, V, stream)
 
     def drop(self, slots, n_drop, stream=None) -> None:
         """Takes the last n_drop tokens (at most all) off each sequence."""
+        self._use(stream)
         wise.wise_kv_drop(self, slots, n_drop, stream)
 
     def compact(self, stream=None):
         """Moves the pages in use to the front of the pool; returns remap int32 [n_pages] and n_live int32 [1]."""
+        self._use(stream)
         remap = _empty(self.n_pages, torch.int32, self.device, stream)
         n_live = _empty(1, torch.int32, self.device, stream)
         wise.wise_kv_compact(self, remap, n_live, self._kv_workspace(0, stream), stream)
@@ -99,12 +120,13 @@ class PagedCache(wise.Cache):
                stream=None) -> None:
         """Attention of Q [batch, n_heads, q_len, head_dim] over the sequences in slots, into O; the requests of
         each group share their first prefix_lens[g] tokens."""
+        self._use(stream)
         key = (Q.shape, 0 if prefix_lens is None else prefix_lens.shape[0], scale)
         if key != self._attn_key:
             shape = wise.prefix_shape(self, Q, key[1], scale)
             need = wise.wise_prefix_attn_workspace(self, shape)
             if self._attn_ws is None or self._attn_ws.numel() < need:
-                self._attn_ws = _empty(max(need, 16), torch.uint8, self.device, stream, self._attn_ws)
+                self._attn_ws = self._new_workspace(need, stream)
             self._attn_key, self._attn_shape = key, shape
         wise.wise_prefix_attn(self, layer, Q, O, slots, n_new, group_start, prefix_lens, self._attn_ws, scale, stream,
                               self._attn_shape)
