@@ -17,7 +17,8 @@ the library's entry points in their order of use:
 Every call is asynchronous on `stream` (default: torch's current stream);
 calls on one cache must be ordered on a stream, and two calls that may run at
 the same time need a PagedCache each over the same tensors (`over`), since
-each keeps one workspace.  The cache's own memory is recorded on every stream
+each keeps one workspace.  Calls can be captured in a CUDA graph, for one shape
+after another; the cache must outlive the graphs.  The cache's own memory is recorded on every stream
 that its calls run on, so that the cache can be let go while they run; what a
 call is given besides (lists, keys and values, queries, outputs) is the
 caller's to keep.
@@ -57,7 +58,8 @@ class PagedCache(wise.Cache):
 
     def _own(self, pool, table, lens, refs) -> None:
         wise.Cache.__init__(self, pool, table, lens, refs)
-        self._streams = {}  # streams that have used the cache, by handle
+        self._streams = {}     # streams that have used the cache, by handle
+        self._workspaces = []  # all of them, see _grown
         self._kv_ws = None
         self._kv_n = -1
         self._attn_ws = None
@@ -68,20 +70,25 @@ class PagedCache(wise.Cache):
         raw = wise._raw_stream(stream, self.index)
         if raw not in self._streams:
             self._streams[raw] = torch.cuda.current_stream(self.device) if stream is None else stream
-            for t in (self.pool, self.table, self.lens, self.refs, self._kv_ws, self._attn_ws):
-                if t is not None:
-                    t.record_stream(self._streams[raw])
+            for t in (self.pool, self.table, self.lens, self.refs, *self._workspaces):
+                t.record_stream(self._streams[raw])
 
-    def _new_workspace(self, need: int, stream):
-        # 0 bytes: the library refuses this cache, and the call itself says why.
-        ws = _empty(max(need, 16), torch.uint8, self.device, stream)
-        for s in self._streams.values():
-            ws.record_stream(s)
+    def _grown(self, ws, need: int, stream):
+        """The workspace `ws`, or a new one where `need` is more than it has.  A captured graph goes on writing to the
+        one it was captured with, so none is given back before the cache is; each new one is at least twice as
+        large, so that all the old ones together are no larger than the last."""
+        have = 0 if ws is None else ws.numel()
+        if ws is None or need > have:
+            # 0 bytes: the library refuses this cache, and the call itself says why.
+            ws = _empty(max(need, 2 * have, 16), torch.uint8, self.device, stream)
+            self._workspaces.append(ws)
+            for s in self._streams.values():
+                ws.record_stream(s)
         return ws
 
     def _kv_workspace(self, n: int, stream):
         if n > self._kv_n:
-            self._kv_ws = self._new_workspace(wise.wise_kv_workspace(self, n), stream)
+            self._kv_ws = self._grown(self._kv_ws, wise.wise_kv_workspace(self, n), stream)
             self._kv_n = n
         return self._kv_ws
 
@@ -124,9 +131,7 @@ class PagedCache(wise.Cache):
         key = (Q.shape, 0 if prefix_lens is None else prefix_lens.shape[0], scale)
         if key != self._attn_key:
             shape = wise.prefix_shape(self, Q, key[1], scale)
-            need = wise.wise_prefix_attn_workspace(self, shape)
-            if self._attn_ws is None or self._attn_ws.numel() < need:
-                self._attn_ws = self._new_workspace(need, stream)
+            self._attn_ws = self._grown(self._attn_ws, wise.wise_prefix_attn_workspace(self, shape), stream)
             self._attn_key, self._attn_shape = key, shape
         wise.wise_prefix_attn(self, layer, Q, O, slots, n_new, group_start, prefix_lens, self._attn_ws, scale, stream,
                               self._attn_shape)

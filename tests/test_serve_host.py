@@ -112,3 +112,27 @@ def test_workspaces_are_recorded_on_streams_that_came_before_and_after_them(host
     attend(cache, 1, a)
     attend(cache, 1, b)
     assert len(host.recorded) == n   # once a stream
+
+
+def extend(cache, n):
+    cache.extend(i32(n), i32(n))
+
+
+def test_a_workspace_that_a_graph_may_hold_is_kept(host):
+    """A graph that was captured with a small batch still writes to the workspace of that time when larger batches
+    and longer lists have come since."""
+    cache = make()
+    attend(cache, 2)
+    extend(cache, 2)
+    small = list(host.lib.workspaces)
+    for n in (3, 9, 40, 41, 500):
+        attend(cache, n)
+        extend(cache, n)
+    held = {ws.data_ptr(): ws.numel() for ws in cache._workspaces}
+    assert set(host.lib.workspaces) <= set(held) and set(small) <= set(held)
+    assert len(set(host.lib.workspaces)) == len(held) >= 6
+    # What is kept beside the two in use is no more than those.
+    assert sum(held.values()) <= 2 * (cache._attn_ws.numel() + cache._kv_ws.numel())
+    attend(cache, 2)
+    extend(cache, 2)
+    assert host.lib.workspaces[-2:] == [cache._attn_ws.data_ptr(), cache._kv_ws.data_ptr()]
