@@ -445,8 +445,23 @@ _current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _on_device(index) -> None:
+    """The library launches on the current device, so that has to be the one that the tensors are on."""
+    if _current_device() != index:
+        raise ValueError(f"the tensors are on device {index}, but device {_current_device()} is current: "
+                         f"call inside torch.cuda.device({index})")
+
+
 def _raw_stream(stream, index) -> int:
-    return _current_raw(index) if stream is None else stream.cuda_stream
+    _on_device(index)
+    if stream is None:
+        return _current_raw(index)
+    if stream.device_index != index:
+        raise ValueError(f"stream is of device {stream.device_index}, the tensors are on device {index}")
+    return stream.cuda_stream
 
 
 def wise_kv_workspace(cache: Cache, n: int) -> int:
@@ -522,7 +537,8 @@ def prefix_shape(cache: Cache, Q, n_groups: int, scale: float = 0.0) -> wise_pre
 
 
 def wise_prefix_attn_workspace(cache: Cache, shape: wise_prefix_t) -> int:
-    """Bytes of workspace of wise_prefix_attn."""
+    """Bytes of workspace of wise_prefix_attn on the current device."""
+    _on_device(cache.index)
     return int(load().wise_prefix_attn_workspace(cache.ref, ctypes.byref(shape)))
 
 

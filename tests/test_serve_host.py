@@ -56,6 +56,7 @@ def host(monkeypatch):
     monkeypatch.setattr(wise, "load", lambda: t.lib)
     monkeypatch.setattr(wise, "_check", lambda *a: None)
     monkeypatch.setattr(wise, "_current_raw", lambda index: t.current.cuda_stream)
+    monkeypatch.setattr(wise, "_current_device", lambda: -1)
     monkeypatch.setattr(serve, "_empty", lambda shape, dtype, device, stream: torch.empty(shape, dtype=dtype))
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: t.current)
     monkeypatch.setattr(torch.Tensor, "record_stream",
@@ -136,3 +137,48 @@ def test_a_workspace_that_a_graph_may_hold_is_kept(host):
     attend(cache, 2)
     extend(cache, 2)
     assert host.lib.workspaces[-2:] == [cache._attn_ws.data_ptr(), cache._kv_ws.data_ptr()]
+
+
+def verify(stream=None):
+    p = torch.zeros((2, 2, 10))
+    return wise.wise_verify_draft(p, p[:, :1].contiguous(), i32((2, 1)), None, torch.zeros((2, 1)), torch.zeros(2),
+                                  i32(2), i32((2, 2)), stream)
+
+
+def test_tensors_of_another_device_than_the_current_one_are_refused(host, monkeypatch):
+    """The library takes the current device's status word, its number of SMs and its streams: nothing is launched
+    for tensors that lie elsewhere."""
+    cache = make()
+    shape = wise.prefix_shape(cache, torch.zeros((2, 4, 1, 64), dtype=torch.bfloat16), 0)
+    calls = everything(cache) + [lambda: wise.wise_prefix_attn_workspace(cache, shape)]
+    for call in calls:
+        call()
+    monkeypatch.setattr(wise, "_current_device", lambda: 1)
+    monkeypatch.setattr(wise, "load", lambda: pytest.fail("the library was called"))
+    fresh = make()
+    for call in everything(cache) + everything(fresh) + [lambda: wise.wise_prefix_attn_workspace(cache, shape)]:
+        with pytest.raises(ValueError, match="device"):
+            call()
+
+
+def test_a_stream_of_another_device_is_refused(host, monkeypatch):
+    cache, far = make(), Stream(9)
+    far.device_index = 1
+    monkeypatch.setattr(wise, "load", lambda: pytest.fail("the library was called"))
+    for call in everything(cache, far):
+        with pytest.raises(ValueError, match="stream"):
+            call()
+
+
+def test_the_binding_of_the_verification_looks_at_the_device(host, monkeypatch):
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True, raising=False)
+    host.lib.wise_verify_draft = lambda *a: 0
+    verify()
+    far = Stream(9)
+    far.device_index = 1
+    with pytest.raises(ValueError, match="stream"):
+        verify(far)
+    monkeypatch.setattr(wise, "_current_device", lambda: 1)
+    host.lib.wise_verify_draft = lambda *a: pytest.fail("the library was called")
+    with pytest.raises(ValueError, match="device"):
+        verify()
