@@ -352,37 +352,52 @@ __global__ void __launch_bounds__(256) copy_tails_kernel(const CacheView c, int3
 
 // --------------------------------------------------------------------- write
 // One thread per 16 bytes of K and of V (blockIdx.y = 0, 1); a block has
-// `rows_per_block` rows.  What bounds it: the chain slot, length, page, count
-// before the store (a ragged draft of 640 tokens of 8 heads of 128, 5 MB: about
-// 4 us), so the value is loaded beside it and the indexes take two 32-bit
-// divisions.  (With 64-bit ones and the value last, forking and growing 128
-// sequences and eight writes took 67 us, now 61.)
+// `rows_per_block` rows, of at most `max_req` requests.  What bounds it: the
+// chain slot, length, page, count before the store (a ragged draft of 640 tokens
+// of 8 heads of 128, 5 MB: about 4 us), so the value is loaded beside it and the
+// indexes take 32-bit divisions (forking and growing 128 sequences and eight
+// writes: 61 us, 67 with 64-bit divisions and the value last).  While the length
+// is on its way the block looks for its requests' slots in the whole list, since
+// two entries of one slot would store to the same places in any order; that
+// takes half a microsecond a write, 65.5 us in all.
 __global__ void __launch_bounds__(256) write_kernel(const CacheView c, int layer, const int32_t* slots,
-                                                    const int32_t* n_new, int q_len, int rows, int rows_per_block,
-                                                    const uint4* K, const uint4* V) {
+                                                    const int32_t* n_new, int batch, int q_len, int rows,
+                                                    int rows_per_block, int max_req, const uint4* K, const uint4* V) {
+  __shared__ uint32_t twice[8];  // by warp: bit k, request b0 + k is listed again
   const int per_row = c.row_bytes / 16;
-  const int in_block = threadIdx.x / per_row, r = blockIdx.x * rows_per_block + in_block;
-  if (in_block >= rows_per_block || r >= rows) return;
-  const int unit = threadIdx.x - in_block * per_row;
+  const int r0 = blockIdx.x * rows_per_block, in_block = threadIdx.x / per_row;
+  const bool on = in_block < rows_per_block && r0 + in_block < rows;
+  const int r = on ? r0 + in_block : r0, unit = threadIdx.x - in_block * per_row;
   // On its way while the page is looked up.
-  const uint4 value = (blockIdx.y ? V : K)[(size_t)r * per_row + unit];
+  uint4 value = make_uint4(0, 0, 0, 0);
+  if (on) value = (blockIdx.y ? V : K)[(size_t)r * per_row + unit];
   const int bh = r / q_len, i = r - bh * q_len;
   const int b = bh / c.n_kv_heads, head = bh - b * c.n_kv_heads;
-  const int s = slots[b];
-  if (s < 0) return;
-  if (s >= c.n_slots) {
-    fault(c, kStatusBadCache);
-    return;
+  const int s = slots[b], add = n_new ? n_new[b] : q_len;
+  const bool in = s >= 0 && s < c.n_slots;
+  const int len = in ? c.lens[s] : 0;
+  const int b0 = r0 / (c.n_kv_heads * q_len), n_req = min(max_req, batch - b0);
+  uint32_t again = 0;
+  for (int j = threadIdx.x; j < batch; j += blockDim.x) {
+    const int other = slots[j];
+    for (int k = 0; k < n_req; ++k)
+      if (other >= 0 && j != b0 + k && slots[b0 + k] == other) again |= 1u << k;
   }
-  const int len = c.lens[s];
-  int add = n_new ? n_new[b] : q_len;
-  if (len < 0 || len > c.max_len || add < 0 || add > q_len || add > len) {
+  again = __reduce_or_sync(0xffffffffu, again);
+  if (threadIdx.x % 32 == 0) twice[threadIdx.x / 32] = again;
+  const bool sound = in && len >= 0 && len <= c.max_len && add >= 0 && add <= q_len && add <= len;
+  const int pos = len - add + i;
+  const int page = on && sound && i < add ? c.table[(size_t)s * c.max_pages + pos / c.page] : -1;
+  __syncthreads();
+  if (!on || s < 0) return;
+  again = 0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) again |= twice[w];
+  if (!sound || ((again >> (b - b0)) & 1)) {
     fault(c, kStatusBadCache);
     return;
   }
   if (i >= add) return;
-  const int pos = len - add + i;
-  const int page = c.table[(size_t)s * c.max_pages + pos / c.page];
   if (!valid_page(c, page) || c.refs[page] > 1) {
     fault(c, kStatusBadCache);
     return;
@@ -539,9 +554,11 @@ cudaError_t launch_kv_extend(const CacheView& c, const int32_t* slots, const int
 cudaError_t launch_kv_write(const CacheView& c, int layer, const int32_t* slots, const int32_t* n_new, int batch,
                             int q_len, const void* K, const void* V, cudaStream_t stream) {
   const int rows = batch * c.n_kv_heads * q_len, per_block = 256 / (c.row_bytes / 16);
-  write_kernel<<<dim3((rows - 1) / per_block + 1, 2), 256, 0, stream>>>(c, layer, slots, n_new, q_len, rows, per_block,
-                                                                       reinterpret_cast<const uint4*>(K),
-                                                                       reinterpret_cast<const uint4*>(V));
+  static_assert(256 / (64 * 2 / 16) <= 32, "a bit per request of a block");
+  const int max_req = std::min(per_block, (per_block - 1) / (c.n_kv_heads * q_len) + 2);
+  write_kernel<<<dim3((rows - 1) / per_block + 1, 2), 256, 0, stream>>>(
+      c, layer, slots, n_new, batch, q_len, rows, per_block, max_req, reinterpret_cast<const uint4*>(K),
+      reinterpret_cast<const uint4*>(V));
   return cudaGetLastError();
 }
 
