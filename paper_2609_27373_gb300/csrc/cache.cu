@@ -34,8 +34,9 @@ __device__ __forceinline__ bool count_ref(const CacheView& c, int page, int by) 
 
 // ---------------------------------------------------------------------- fork
 // One block per entry.  An entry whose dst occurs again in dst or in src is
-// left out, so no two blocks touch the same row.  Bound by its chain of
-// dependent accesses (list, length, table, count) and the launch.
+// left out, so no two blocks touch the same row.  Both rows are looked through
+// before anything changes.  Bound by its chain of dependent accesses (list,
+// length, table, count) and the launch.
 __global__ void __launch_bounds__(256) fork_kernel(const CacheView c, const int32_t* src, const int32_t* dst, int n) {
   const int i = blockIdx.x;
   const int s = src[i], d = dst[i];
@@ -49,19 +50,22 @@ __global__ void __launch_bounds__(256) fork_kernel(const CacheView c, const int3
     old = c.lens[d];
     if (len < 0 || len > c.max_len || old < 0 || old > c.max_len) bad = 1;
   }
+  const int32_t* from = c.table + (size_t)s * c.max_pages;
+  int32_t* to = c.table + (size_t)d * c.max_pages;
+  if (!bad) {
+    for (int k = threadIdx.x; k < pages_of(c, old); k += blockDim.x) bad |= !valid_page(c, to[k]);
+    for (int k = threadIdx.x; k < pages_of(c, len); k += blockDim.x) bad |= !valid_page(c, from[k]);
+  }
   if (__syncthreads_or(bad)) {
     if (threadIdx.x == 0) fault(c, kStatusBadCache);
     return;
   }
-  const int32_t* from = c.table + (size_t)s * c.max_pages;
-  int32_t* to = c.table + (size_t)d * c.max_pages;
-  for (int k = threadIdx.x; k < pages_of(c, old); k += blockDim.x) bad |= !count_ref(c, to[k], -1);
+  for (int k = threadIdx.x; k < pages_of(c, old); k += blockDim.x) count_ref(c, to[k], -1);
   for (int k = threadIdx.x; k < pages_of(c, len); k += blockDim.x) {
     const int page = from[k];
-    bad |= !count_ref(c, page, 1);
+    count_ref(c, page, 1);
     to[k] = page;
   }
-  if (bad) fault(c, kStatusBadCache);
   if (threadIdx.x == 0) c.lens[d] = len;  // every thread read it before the barrier
 }
 

@@ -45,3 +45,58 @@ def test_a_slot_that_a_write_lists_twice_is_not_written(head_dim, batch, q_len, 
         cache.write(0, u32(at), u32(n_new), K, V)
         assert wise.wise_get_status() == (wise.WISE_ERR_BAD_CACHE if faults else wise.WISE_OK)
         assert torch.equal(cache.pool.view(torch.int16), want.view(torch.int16))
+
+
+def cache_of(rows, lens, n_pages=24, page=16, max_pages=4, n_kv_heads=2, head_dim=64, dtype=torch.bfloat16):
+    """A cache whose slot s holds lens[s] tokens in pages rows[s]."""
+    cache = serve.PagedCache(1, n_pages, n_kv_heads, page, head_dim, len(rows), max_pages, dtype)
+    cache.pool.copy_(torch.randn(cache.pool.shape, device="cuda"))
+    refs = [0] * n_pages
+    for s, row in enumerate(rows):
+        cache.table[s, :len(row)] = u32(row)
+        for g in row:
+            if 0 <= g < n_pages:
+                refs[g] += 1
+    cache.lens.copy_(u32(lens))
+    cache.refs.copy_(u32(refs))
+    return cache
+
+
+def state(cache):
+    return cache.table.tolist(), cache.lens.tolist(), cache.refs.tolist()
+
+
+FAULTY_IDS = [-1, 24, 2 ** 31 - 1, -2 ** 31]
+
+
+@pytest.mark.parametrize("bad", FAULTY_IDS)
+@pytest.mark.parametrize("at", [0, 1, 2])
+def test_a_fork_from_or_over_a_faulty_page_id_changes_nothing(bad, at):
+    row = [3, 4, 5]
+    row[at] = bad
+    # Slot 0 is faulty, slots 1 and 2 are sound, 3 and 4 hold something, 5 is empty.
+    rows = [row, [6, 7], [8], [9, 10], [11], []]
+    lens = [40, 20, 3, 32, 16, 0]
+    cache = cache_of(rows, lens)
+    before = state(cache)
+    cache.fork(u32([0]), u32([3]))                       # from the faulty row
+    assert wise.wise_get_status() == wise.WISE_ERR_BAD_CACHE
+    assert state(cache) == before
+    cache.fork(u32([1]), u32([0]))                       # over the faulty row
+    assert wise.wise_get_status() == wise.WISE_ERR_BAD_CACHE
+    assert state(cache) == before
+    cache.fork(u32([0, 1]), u32([4, 5]))                 # beside a sound entry
+    assert wise.wise_get_status() == wise.WISE_ERR_BAD_CACHE
+    table, lens2, refs = state(cache)
+    assert lens2 == [40, 20, 3, 32, 16, 20] and table[5][:2] == [6, 7] and table[:5] == before[0][:5]
+    assert refs == [before[2][g] + (g in (6, 7)) for g in range(24)]
+
+
+def test_a_fork_does_not_look_past_the_lengths():
+    """Entries behind a sequence's pages mean nothing, whatever they hold."""
+    cache = cache_of([[3], [4], []], [16, 9, 0])
+    cache.table[0, 1:] = -7
+    cache.table[1, 1:] = 1 << 30
+    cache.fork(u32([0]), u32([1]))
+    assert wise.wise_get_status() == wise.WISE_OK
+    assert cache.lens.tolist() == [16, 16, 0] and cache.table[1, 0].item() == 3 and cache.refs[3].item() == 2
