@@ -25,13 +25,6 @@ __device__ __forceinline__ bool valid_page(const CacheView& c, int page) { retur
 
 __device__ __forceinline__ int pages_of(const CacheView& c, int len) { return (len + c.page - 1) / c.page; }
 
-// One holder of a page less or more; ids out of range are skipped.
-__device__ __forceinline__ bool count_ref(const CacheView& c, int page, int by) {
-  if (!valid_page(c, page)) return false;
-  atomicAdd(c.refs + page, by);
-  return true;
-}
-
 // ---------------------------------------------------------------------- fork
 // One block per entry.  An entry whose dst occurs again in dst or in src is
 // left out, so no two blocks touch the same row.  Both rows are looked through
@@ -60,17 +53,18 @@ __global__ void __launch_bounds__(256) fork_kernel(const CacheView c, const int3
     if (threadIdx.x == 0) fault(c, kStatusBadCache);
     return;
   }
-  for (int k = threadIdx.x; k < pages_of(c, old); k += blockDim.x) count_ref(c, to[k], -1);
+  for (int k = threadIdx.x; k < pages_of(c, old); k += blockDim.x) atomicAdd(c.refs + to[k], -1);
   for (int k = threadIdx.x; k < pages_of(c, len); k += blockDim.x) {
     const int page = from[k];
-    count_ref(c, page, 1);
+    atomicAdd(c.refs + page, 1);
     to[k] = page;
   }
   if (threadIdx.x == 0) c.lens[d] = len;  // every thread read it before the barrier
 }
 
 // ---------------------------------------------------------------------- drop
-// One block per entry, and bound like a fork.
+// One block per entry, and bound like a fork; the pages are looked through before
+// anything changes.
 __global__ void __launch_bounds__(256) drop_kernel(const CacheView c, const int32_t* slots, const int32_t* n_drop,
                                                    int n) {
   const int i = blockIdx.x;
@@ -85,15 +79,17 @@ __global__ void __launch_bounds__(256) drop_kernel(const CacheView c, const int3
     len = c.lens[s];
     if (len < 0 || len > c.max_len) bad = 1;
   }
+  const int left = max(len - max(drop, 0), 0);
+  const int32_t* row = c.table + (size_t)s * c.max_pages;
+  if (!bad)
+    for (int k = pages_of(c, left) + threadIdx.x; k < pages_of(c, len); k += blockDim.x)
+      bad |= !valid_page(c, row[k]);
   if (__syncthreads_or(bad)) {
     if (threadIdx.x == 0) fault(c, kStatusBadCache);
     return;
   }
-  const int left = drop >= len ? 0 : len - drop;
-  const int32_t* row = c.table + (size_t)s * c.max_pages;
   for (int k = pages_of(c, left) + threadIdx.x; k < pages_of(c, len); k += blockDim.x)
-    bad |= !count_ref(c, row[k], -1);
-  if (bad) fault(c, kStatusBadCache);
+    atomicAdd(c.refs + row[k], -1);
   if (threadIdx.x == 0) c.lens[s] = left;
 }
 

@@ -100,3 +100,26 @@ def test_a_fork_does_not_look_past_the_lengths():
     cache.fork(u32([0]), u32([1]))
     assert wise.wise_get_status() == wise.WISE_OK
     assert cache.lens.tolist() == [16, 16, 0] and cache.table[1, 0].item() == 3 and cache.refs[3].item() == 2
+
+
+@pytest.mark.parametrize("bad", FAULTY_IDS)
+@pytest.mark.parametrize("at,drop", [(0, 40), (1, 25), (2, 10), (0, 1 << 30), (2, 40)])
+def test_a_drop_over_a_faulty_page_id_changes_nothing(bad, at, drop):
+    row = [3, 4, 5]
+    row[at] = bad
+    cache = cache_of([row, [6, 7]], [40, 20])
+    before = state(cache)
+    cache.drop(u32([0, 1]), u32([drop, 10]))
+    assert wise.wise_get_status() == wise.WISE_ERR_BAD_CACHE
+    table, lens, refs = state(cache)
+    assert table == before[0] and lens == [40, 10]
+    assert refs == [before[2][g] - (g == 7) for g in range(24)]
+
+
+def test_a_drop_does_not_look_past_what_it_releases():
+    """Pages that stay are not the call's concern, nor are entries behind the length."""
+    cache = cache_of([[-1, 4, 5]], [40])
+    cache.table[0, 3] = 1 << 30
+    cache.drop(u32([0]), u32([10]))
+    assert wise.wise_get_status() == wise.WISE_OK
+    assert cache.lens.tolist() == [30] and cache.refs[5].item() == 0 and cache.refs[4].item() == 1
