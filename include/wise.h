@@ -325,7 +325,8 @@ typedef struct {
 /* Forks sequences: slot dst[i] becomes a second holder of every page of slot
  * src[i] (copy on write), for i < n.  What dst[i] held before is released
  * first.  An entry whose dst is listed twice or is also a src, or whose src or
- * dst is out of range, is skipped.  src, dst: device int32 [n]. */
+ * dst is out of range, is skipped; an entry with a negative src or dst is
+ * unused, and lists nothing.  src, dst: device int32 [n]. */
 int wise_kv_fork(const wise_cache_t* cache, const int32_t* src, const int32_t* dst, int n, cudaStream_t stream);
 
 /* Bytes of workspace of wise_kv_extend (for lists of n) and wise_kv_compact

@@ -26,7 +26,7 @@ __device__ __forceinline__ bool valid_page(const CacheView& c, int page) { retur
 __device__ __forceinline__ int pages_of(const CacheView& c, int len) { return (len + c.page - 1) / c.page; }
 
 // ---------------------------------------------------------------------- fork
-// One block per entry.  An entry whose dst occurs again in dst or in src is
+// One block per entry.  An entry whose dst occurs again in a used entry is
 // left out, so no two blocks touch the same row.  Both rows are looked through
 // before anything changes.  Bound by its chain of dependent accesses (list,
 // length, table, count) and the launch.
@@ -35,8 +35,10 @@ __global__ void __launch_bounds__(256) fork_kernel(const CacheView c, const int3
   const int s = src[i], d = dst[i];
   if (s < 0 || d < 0) return;
   int bad = s >= c.n_slots || d >= c.n_slots;
-  for (int j = threadIdx.x; j < n; j += blockDim.x)
-    if ((j != i && dst[j] == d) || src[j] == d) bad = 1;
+  for (int j = threadIdx.x; j < n; j += blockDim.x) {
+    const int sj = src[j], dj = dst[j];
+    if (sj >= 0 && dj >= 0 && ((j != i && dj == d) || sj == d)) bad = 1;
+  }
   int len = 0, old = 0;
   if (s < c.n_slots && d < c.n_slots) {
     len = c.lens[s];

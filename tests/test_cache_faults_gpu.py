@@ -123,3 +123,20 @@ def test_a_drop_does_not_look_past_what_it_releases():
     cache.drop(u32([0]), u32([10]))
     assert wise.wise_get_status() == wise.WISE_OK
     assert cache.lens.tolist() == [30] and cache.refs[5].item() == 0 and cache.refs[4].item() == 1
+
+
+@pytest.mark.parametrize("src,dst", [([0, -1], [2, 2]), ([-5, 0], [2, 2]), ([0, 2], [2, -1]), ([0, -1, 1], [2, 0, 3]),
+                                     ([-1, -1, 0], [2, 2, 2]), ([0, 2, 1], [2, -3, 3])])
+def test_unused_entries_of_a_fork_are_passed_over(src, dst):
+    """What stands beside a negative slot is not looked at: it neither lists a slot twice nor makes one a source."""
+    rows, lens = [[3, 4], [5], [6], []], [20, 7, 2, 0]
+    cache = cache_of(rows, lens)
+    for s, d in zip(src, dst):
+        if s >= 0 and d >= 0:
+            rows[d], lens[d] = rows[s], lens[s]
+    refs = [sum(row.count(g) for row in rows) for g in range(24)]
+    cache.fork(u32(src), u32(dst))
+    assert wise.wise_get_status() == wise.WISE_OK
+    table, got, got_refs = state(cache)
+    assert got == lens and got_refs == refs
+    assert [t[:len(r)] for t, r in zip(table, rows)] == rows
