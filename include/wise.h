@@ -373,7 +373,9 @@ int wise_kv_compact(const wise_cache_t* cache, int32_t* remap, int32_t* n_live, 
  * sequence:
  *   O[b,h,i] = sum_{j<e} softmax_j(scale * Q[b,h,i] . K[j]) V[j],
  * with the keys and values of kv-head h / (n_heads / n_kv_heads) of `layer`.
- * Rows with i >= n_new[b], e <= 0 or s < 0 give 0.
+ * Rows with i >= n_new[b], e <= 0 or s < 0 give 0, and so does a request that
+ * reads a page id out of range; one in a shared prefix is read by all requests
+ * of the group.
  * Q, O: [batch, n_heads, q_len, head_dim] of the cache's type, 16-byte
  * aligned.  n_new: device int32 [batch], or NULL (q_len for all).
  * Sharing: the requests group_start[g] .. group_start[g+1] - 1 (g < n_groups,

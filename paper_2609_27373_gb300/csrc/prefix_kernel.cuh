@@ -67,7 +67,7 @@ struct PfxCfg {
 };
 
 constexpr int kPfxSched = 8;  // schedule entries per stream
-constexpr int kPfxFirst = 1, kPfxLast = 2, kPfxEnd = 4;
+constexpr int kPfxFirst = 1, kPfxLast = 2, kPfxEnd = 4, kPfxFaulty = 8;
 
 // Schedule entry {ring slot | parity of its use << 8 | keys << 16, first key position,
 // request | (requests - 1) << 10 | kind << 17 | flags << 19, segment slot}.
@@ -395,10 +395,16 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
     const int slot = pair ? n % NS : w * H + n % H;
     const int use = pair ? n / NS + ((slot < H ? n0 : n1) - slot % H + H - 1) / H : n / H;
     const int word = second ? seg.word2 : seg.word;
+    // The lane's page of the tile, if the item reaches it.
+    const int at = lane << c.page_shift;
+    const bool on = at < kPfxKeys && seg.pos + at < seg.end;
+    const bool valid = page >= 0 && page < c.n_pages;
+    const bool faulty = __any_sync(0xffffffffu, on && !valid);
+    if (faulty) bad = 1;
     const int e = n_ent % kPfxSched;
     if (n_ent >= kPfxSched) ok = pfx_warp_wait(&sb.sched_empty[w][e], ((n_ent / kPfxSched) - 1) & 1, abort, p.wait_ns);
     if (ok && lane == 0) {
-      const int flags = (first ? kPfxFirst : 0) | (seg.left == 1 ? kPfxLast : 0);
+      const int flags = (first ? kPfxFirst : 0) | (seg.left == 1 ? kPfxLast : 0) | (faulty ? kPfxFaulty : 0);
       sb.sched[w][e] = make_int4(slot | (use & 1) << 8 | min(kPfxKeys, seg.end - seg.pos) << 16, seg.pos,
                                  word | flags << 19, seg.slot + second);
       mbar_arrive(&sb.sched_full[w][e]);
@@ -406,10 +412,6 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
     ++n_ent;
     // The tile of the K ring (r = 0) and of the V ring; Q in between.  One lane
     // per page that the item reaches.
-    const int at = lane << c.page_shift;
-    const bool on = at < kPfxKeys && seg.pos + at < seg.end;
-    const bool valid = page >= 0 && page < c.n_pages;
-    if (on && !valid) bad = 1;
     // A faulty page id becomes a coordinate out of range, which reads zeros.
     const int z = valid ? page * c.n_kv_heads + seg.kvh : c.n_pages * c.n_kv_heads;
     const int bytes = min(kPfxKeys, (seg.end - seg.pos + c.page - 1) & -c.page) * 128 * C::kBoxes;
@@ -460,7 +462,7 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
       mbar_arrive(&sb.sched_full[w][e]);
     }
   }
-  if (bad) atomicOr(c.status, kStatusBadCache);
+  if (bad && lane == 0) atomicOr(c.status, kStatusBadCache);
   if (!ok && lane == 0) {
     pfx_give_up(&sb.abort, c.status);
     // Copies already issued land before the CTA's shared memory is released.
@@ -734,6 +736,8 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
     const float f = rescale ? ex2_approx(m - m_new) : 1.0f;
     m = m_new;
     l = l * f + sum;
+    // A page id out of range: the merge gives 0 to rows whose sum is no number.
+    if (flags & kPfxFaulty) l = __int_as_float(0x7fffffff);
     if (warp_on) {
       if (__any_sync(0xffffffffu, rescale)) {
 #pragma unroll 1
@@ -1028,7 +1032,7 @@ __global__ void __launch_bounds__(kMergeThreads, 12) prefix_merge_kernel(const P
     }
   }
   if (!on || part > 0) return;
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;  // 0 as well where a faulty page made l NaN
   // Row `row` of the request's block of rows of this kv head: Q and O are
   // [batch][n_kv_heads][rows][head_dim].
   uint16_t* out = O + ((size_t)blockIdx.x * R + row) * D + 4 * col;
