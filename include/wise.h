@@ -376,6 +376,9 @@ int wise_kv_compact(const wise_cache_t* cache, int32_t* remap, int32_t* n_live, 
  * Rows with i >= n_new[b], e <= 0 or s < 0 give 0, and so does a request that
  * reads a page id out of range; one in a shared prefix is read by all requests
  * of the group.
+ * Sums, maxima and partial results are fp32; the softmax's numerators are
+ * rounded to the cache's type for the product with V (in fp16, those below
+ * 2^-32 of their row's largest one vanish there).
  * Q, O: [batch, n_heads, q_len, head_dim] of the cache's type, 16-byte
  * aligned.  n_new: device int32 [batch], or NULL (q_len for all).
  * Sharing: the requests group_start[g] .. group_start[g+1] - 1 (g < n_groups,

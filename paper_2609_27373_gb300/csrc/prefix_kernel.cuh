@@ -639,7 +639,12 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
                             PfxShared<PfxCfg<D>::kSlots>& sb) {
   using C = PfxCfg<D>;
   constexpr int NS = C::kSlots;
-  constexpr float kRescaleThreshold = 8.0f;  // log2 units: P stays <= 256
+  constexpr float kRescaleThreshold = 8.0f;  // log2 units: P stays <= 2^(8 + kLift)
+  // P is rounded to the cache's type for the tensor cores (l is summed before).
+  // fp16 ends at 2^-24, so its P are held 2^7 higher, at most 2^15: what is lost
+  // is below 2^-32 of the row's largest a key.  (Without that 2^20 keys of 2^-26
+  // each, 1.5 % of a row, vanished from the numerator.)
+  constexpr float kLift = FP16 ? 7.0f : 0.0f;
   volatile int* abort = &sb.abort;
   const int r = threadIdx.x & 127, wq = r >> 5, lane = r & 31;
   const uint32_t lane_tmem = tmem + ((uint32_t)(wq * 32) << 16);
@@ -708,7 +713,7 @@ __device__ void pfx_softmax(const PfxParams& p, const PfxPlan& plan, int w, uint
           for (int k = 0; k < 32; ++k) s[32 * c + k] = (seen >> k) & 1 ? s[32 * c + k] : -INFINITY;
         }
       }
-      const float m_tile = row_max(s) * p.scale_log2;
+      const float m_tile = row_max(s) * p.scale_log2 - kLift;
       m_new = (m_tile > m + kRescaleThreshold) ? m_tile : m;
       sum = exp2_scaled(s, p.scale_log2, m_new == -INFINITY ? 0.0f : m_new);
 #pragma unroll
