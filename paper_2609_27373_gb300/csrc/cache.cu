@@ -545,8 +545,10 @@ cudaError_t launch_kv_extend(const CacheView& c, const int32_t* slots, const int
                              int32_t* work, int sm_count, cudaStream_t stream) {
   const int smem = 2 * ((c.n_slots + 31) / 32) * 4;
   cudaError_t e = cudaSuccess;
+  // The limit is the kernel's, not the launch's: always the largest one, so that
+  // calls of other threads cannot lower it before this launch.
   if (smem > 40 * 1024)
-    e = cudaFuncSetAttribute(extend_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    e = cudaFuncSetAttribute(extend_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlots / 32 * 2 * 4);
   if (e == cudaSuccess)
     e = launch_plan(extend_plan_kernel, plan_blocks(c), smem, stream, c, slots, n_new, n, granted, work);
   if (e != cudaSuccess) return e;

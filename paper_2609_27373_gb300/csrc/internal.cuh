@@ -155,6 +155,8 @@ bool make_tile_map(CUtensorMap* map, const void* base, bool fp16, int cols, int 
 bool make_query_map(CUtensorMap* map, const void* base, bool fp16, int cols, int rows, int heads, int batch,
                     int box_batch);
 
+constexpr int kMaxSlots = 1 << 18;  // of a cache, and entries of a list
+
 // A paged cache as the kernels see it (wise_cache_t).
 struct CacheView {
   int n_pages, page, page_shift, n_slots, max_pages;  // page = 1 << page_shift

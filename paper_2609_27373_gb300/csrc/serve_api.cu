@@ -11,7 +11,6 @@
 namespace wise {
 namespace {
 
-constexpr int kMaxSlots = 1 << 18;
 constexpr int kMaxVocab = 1 << 18; // weights of 2^40 at most add up within 2^58
 constexpr int kMaxDraft = 1024;
 
