@@ -51,8 +51,9 @@ def prefill(model, prompt, steps=4, discovery=2):
     sel = wise.Select(1, 1, wise.WISE_SEL_TOPK, 2, 0.0, 4)
     layer, O = wise.WiseAttention(shape, sel, discovery), torch.empty_like(Q)
     for t in range(steps):
+        if t > 0:
+            Q, K = Q + 0.01 * torch.randn_like(Q), K + 0.01 * torch.randn_like(K)
         layer.step(t, Q, K, V, O)
-        Q, K = Q + 0.01 * torch.randn_like(Q), K + 0.01 * torch.randn_like(K)
     return K, V
 
 
