@@ -94,8 +94,8 @@ def run(samples=8, rounds=12, draft=4, prompt_len=512, vocab=997, share=True, se
         u = torch.rand((samples, draft), generator=g, device="cuda")
         us = torch.rand((samples,), generator=g, device="cuda")
         accepted, tokens = serve.verify_draft(p, q, drafted.int(), None, u, us)
-        # What stays: the fed token and the accepted ones.  The next token is fed in the next round.
-        cache.drop(slots, draft - accepted)
+        # What stays of the granted tokens: the fed one and the accepted ones.  The next token is fed in the next round.
+        cache.drop(slots, (granted - 1 - accepted).clamp(min=0))
         last = tokens.gather(1, accepted[:, None].long())[:, 0].long()
         for s, (n, row) in enumerate(zip(accepted.tolist(), tokens.tolist())):
             answers[s] += row[:n + 1]
