@@ -420,8 +420,9 @@ int wise_prefix_attn(const wise_cache_t* cache, int layer, const wise_prefix_t* 
  *   t = floor(W * floor(u_sample[b] * 2^24) / 2^24), W the sum of w;
  *   next token = the lowest v with w_0 + .. + w_v > t   (-1 when W == 0).
  * The sums are exact integers, so the tokens are a function of the inputs
- * alone.  NaN counts as 0; a drafted token outside [0, vocab) is refused, with
- * r = p_n, and recorded as WISE_ERR_BAD_CACHE.
+ * alone.  NaN counts as 0, in r and in u_sample; a u_accept that is NaN
+ * refuses.  A drafted token outside [0, vocab) is refused, with r = p_n, and
+ * recorded as WISE_ERR_BAD_CACHE.
  * p: [batch, k_max + 1, vocab], q: [batch, k_max, vocab] of type dtype
  * (WISE_BF16, WISE_FP16, WISE_FP32); draft int32 [batch, k_max]; n_draft int32
  * [batch] or NULL (k_max for all); u_accept fp32 [batch, k_max]; u_sample fp32
