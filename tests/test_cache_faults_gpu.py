@@ -140,3 +140,17 @@ def test_unused_entries_of_a_fork_are_passed_over(src, dst):
     table, got, got_refs = state(cache)
     assert got == lens and got_refs == refs
     assert [t[:len(r)] for t, r in zip(table, rows)] == rows
+
+
+def test_lengths_next_to_the_largest_integer():
+    """Nothing is read, written or changed for a sequence whose length cannot be."""
+    K = torch.randn((1, 2, 2, 64), device="cuda").bfloat16()
+    for length in ((1 << 31) - 1, -(1 << 31), (1 << 31) - 65, 65):
+        cache = cache_of([[3, 4, 5], []], [length, 0])
+        pool, before = cache.pool.clone(), state(cache)
+        for call in (lambda: cache.fork(u32([0]), u32([1])), lambda: cache.fork(u32([1]), u32([0])),
+                     lambda: cache.extend(u32([0]), u32([30])), lambda: cache.write(0, u32([0]), None, K, K),
+                     lambda: cache.drop(u32([0]), u32([1 << 30]))):
+            call()
+            assert wise.wise_get_status() == wise.WISE_ERR_BAD_CACHE
+            assert state(cache) == before and torch.equal(cache.pool.view(torch.int16), pool.view(torch.int16))
