@@ -302,11 +302,17 @@ int wise_support_overlap(const wise_shape_t* shape, const int32_t* idx_a, const 
  * refs) before the first use; the pool needs no initial value.
  *
  * Calls that change the same cache must be ordered on a stream.  Faults in
- * device data (a slot out of range or listed twice, a page id out of range,
- * a length outside [0, max_pages * page]) make the entry concerned do nothing
- * and are recorded for wise_get_status as WISE_ERR_BAD_CACHE; no call reads or
- * writes outside the buffers for any table, lens, refs, slots or counts.  A
- * negative slot in a list is an unused entry, which is passed over. */
+ * device data (a slot out of range or, where the call changes the cache, listed
+ * twice; a length outside [0, max_pages * page]; a page id out of range among
+ * those that the call looks at) make the entry concerned do nothing and are
+ * recorded for wise_get_status as WISE_ERR_BAD_CACHE.  wise_kv_extend looks at
+ * the id of a last page that is not full, wise_kv_drop at those that it
+ * releases, wise_kv_fork at all of both sequences.  wise_kv_write leaves out the
+ * rows on a page without a sound id, wise_kv_compact leaves such ids, and the
+ * rows of sequences whose length is faulty, as they are, and wise_prefix_attn
+ * gives 0.  No call reads or writes outside the buffers for any table, lens,
+ * refs, slots or counts.  A negative slot in a list is an unused entry, which is
+ * passed over. */
 typedef struct {
   int n_pages;    /* pages of the pool, below 2^30 - 1; n_pages * n_kv_heads < 2^31 */
   int page;       /* tokens a page: 16, 32, 64 or 128 */
@@ -385,12 +391,15 @@ int wise_kv_compact(const wise_cache_t* cache, int32_t* remap, int32_t* n_live, 
  * device int32 [n_groups + 1], ascending) declare that their first
  * prefix_lens[g] tokens (device int32 [n_groups]) are the same pages, as
  * wise_kv_fork leaves them; the whole pages among those tokens, up to the
- * shortest active member, are read once for the group, through the first
- * active member's table row.  Requests outside every group, and all of them
- * when n_groups is 0, are read by themselves.
+ * shortest active member, are read through the first active member's table
+ * row, once for every 2 * floor(128 / R) requests of the group, R = q_len *
+ * n_heads / n_kv_heads.  Requests outside every group, and all of them when
+ * n_groups is 0 or group_start breaks its rules (recorded as
+ * WISE_ERR_BAD_CACHE), are read by themselves.  A slot may be listed more than
+ * once.
  * Rows at or past lens in the pool may hold anything (infinities and NaN
  * included); the K and V of positions below lens must be finite.
- * Limits: batch <= 1024, n_groups <= 256, q_len * n_heads / n_kv_heads <= 128,
+ * Limits: batch <= 1024, n_groups <= min(256, batch), q_len * n_heads / n_kv_heads <= 128,
  * batch * n_kv_heads * (max_pages * page / 128 + 1) <= 2^30.
  * workspace: wise_prefix_attn_workspace bytes, 16-byte aligned, not shared
  * with a call that may run at the same time; needs no initial value. */
