@@ -197,9 +197,12 @@ __device__ __forceinline__ void visit_pages(const CacheView& c, const PageScan& 
   }
 }
 
-// Blocks of a plan: one up to 8192 pages, where a block's two passes take less
-// than the cluster's barriers.
-inline int plan_blocks(const CacheView& c) { return c.n_pages <= 8192 ? 1 : 8; }
+// Blocks of a plan: one up to 4096 pages, where a block's two passes take no
+// longer than the cluster's barriers.  (64 sequences grown by a page and cut
+// again, and an empty compaction, with one block and with eight: 1000 pages 11.4
+// and 6.2 us, 11.7 and 6.4; 4000 pages 11.9 and 6.7, 11.9 and 6.6; 8000 pages
+// 12.4 and 7.3, 12.3 and 6.7; 64000 pages 20.3 and 18.0, 12.7 and 7.4.)
+inline int plan_blocks(const CacheView& c) { return c.n_pages <= 4096 ? 1 : 8; }
 
 // Workspace words: [0] number of copies; then the free list, the entries'
 // needs, and the copies as (from, to, rows).
