@@ -65,13 +65,15 @@ class PagedCache(wise.Cache):
         self._attn_ws = None
         self._attn_key = self._attn_shape = None
 
-    def _use(self, stream) -> None:
-        """Before a call on `stream`: torch does not hand the cache's memory out again before that stream is done."""
+    def _use(self, stream) -> int:
+        """Before a call on `stream`: torch does not hand the cache's memory out again before that stream is done.
+        Returns the stream's handle."""
         raw = wise._raw_stream(stream, self.index)
         if raw not in self._streams:
             self._streams[raw] = torch.cuda.current_stream(self.device) if stream is None else stream
             for t in (self.pool, self.table, self.lens, self.refs, *self._workspaces):
                 t.record_stream(self._streams[raw])
+        return raw
 
     def _grown(self, ws, need: int, stream):
         """The workspace `ws`, or a new one where `need` is more than it has.  A captured graph goes on writing to the
@@ -94,46 +96,43 @@ class PagedCache(wise.Cache):
 
     def fork(self, src, dst, stream=None) -> None:
         """Slots dst[i] become forks of slots src[i]; pages are shared until one of the holders grows."""
-        self._use(stream)
-        wise.wise_kv_fork(self, src, dst, stream)
+        wise.wise_kv_fork(self, src, dst, self._use(stream))
 
     def extend(self, slots, n_new, granted=None, stream=None):
         """Grows the sequences by n_new tokens each; returns what was granted (n_new, or 0 where pages ran out)."""
-        self._use(stream)
+        raw = self._use(stream)
         if granted is None:
             granted = _empty(n_new.shape, torch.int32, self.device, stream)
-        wise.wise_kv_extend(self, slots, n_new, granted, self._kv_workspace(slots.shape[0], stream), stream)
+        wise.wise_kv_extend(self, slots, n_new, granted, self._kv_workspace(slots.shape[0], stream), raw)
         return granted
 
     def write(self, layer: int, slots, granted, K, V, stream=None) -> None:
         """Stores one layer's new keys and values [batch, n_kv_heads, q_len, head_dim] at the sequences' ends."""
-        self._use(stream)
-        wise.wise_kv_write(self, layer, slots, granted, K, V, stream)
+        wise.wise_kv_write(self, layer, slots, granted, K, V, self._use(stream))
 
     def drop(self, slots, n_drop, stream=None) -> None:
         """Takes the last n_drop tokens (at most all) off each sequence."""
-        self._use(stream)
-        wise.wise_kv_drop(self, slots, n_drop, stream)
+        wise.wise_kv_drop(self, slots, n_drop, self._use(stream))
 
     def compact(self, stream=None):
         """Moves the pages in use to the front of the pool; returns remap int32 [n_pages] and n_live int32 [1]."""
-        self._use(stream)
+        raw = self._use(stream)
         remap = _empty(self.n_pages, torch.int32, self.device, stream)
         n_live = _empty(1, torch.int32, self.device, stream)
-        wise.wise_kv_compact(self, remap, n_live, self._kv_workspace(0, stream), stream)
+        wise.wise_kv_compact(self, remap, n_live, self._kv_workspace(0, stream), raw)
         return remap, n_live
 
     def attend(self, layer: int, Q, O, slots, n_new=None, group_start=None, prefix_lens=None, scale: float = 0.0,
                stream=None) -> None:
         """Attention of Q [batch, n_heads, q_len, head_dim] over the sequences in slots, into O; the requests of
         each group share their first prefix_lens[g] tokens."""
-        self._use(stream)
+        raw = self._use(stream)
         key = (Q.shape, 0 if prefix_lens is None else prefix_lens.shape[0], scale)
         if key != self._attn_key:
             shape = wise.prefix_shape(self, Q, key[1], scale)
             self._attn_ws = self._grown(self._attn_ws, wise.wise_prefix_attn_workspace(self, shape), stream)
             self._attn_key, self._attn_shape = key, shape
-        wise.wise_prefix_attn(self, layer, Q, O, slots, n_new, group_start, prefix_lens, self._attn_ws, scale, stream,
+        wise.wise_prefix_attn(self, layer, Q, O, slots, n_new, group_start, prefix_lens, self._attn_ws, scale, raw,
                               self._attn_shape)
 
 

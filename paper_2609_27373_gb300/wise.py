@@ -456,6 +456,8 @@ def _on_device(index) -> None:
 
 
 def _raw_stream(stream, index) -> int:
+    if type(stream) is int:  # a handle that came from here
+        return stream
     _on_device(index)
     if stream is None:
         return _current_raw(index)
