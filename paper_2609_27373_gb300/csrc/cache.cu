@@ -25,6 +25,24 @@ __device__ __forceinline__ bool valid_page(const CacheView& c, int page) { retur
 
 __device__ __forceinline__ int pages_of(const CacheView& c, int len) { return (len + c.page - 1) / c.page; }
 
+// Marks slots listed twice in bitmaps over the slots in shared memory; the second
+// one, behind the first, is the result.  Ends with a barrier.
+__device__ __forceinline__ const uint32_t* mark_twice(const CacheView& c, const int32_t* slots, int n, uint32_t* seen) {
+  const int words = (c.n_slots + 31) / 32;
+  uint32_t* twice = seen + words;
+  for (int k = threadIdx.x; k < 2 * words; k += blockDim.x) seen[k] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const int s = slots[i];
+    if (s >= 0 && s < c.n_slots) {
+      const uint32_t bit = 1u << (s & 31);
+      if (atomicOr(&seen[s >> 5], bit) & bit) atomicOr(&twice[s >> 5], bit);
+    }
+  }
+  __syncthreads();
+  return twice;
+}
+
 // ---------------------------------------------------------------------- fork
 // One block per entry.  An entry whose dst occurs again in a used entry is
 // left out, so no two blocks touch the same row.  Both rows are looked through
@@ -237,19 +255,8 @@ __global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const CacheVi
   const ExtendWork w = extend_work(work, c.n_pages, n);
   griddep_launch_dependents();  // the copies wait for this grid's end
   if (lead) {
-    const int words = (c.n_slots + 31) / 32;
-    uint32_t* twice = seen + words;
-    for (int k = threadIdx.x; k < 2 * words; k += kPlanThreads) seen[k] = 0;
     if (threadIdx.x == 0) n_copies = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
-      const int s = slots[i];
-      if (s >= 0 && s < c.n_slots) {
-        const uint32_t bit = 1u << (s & 31);
-        if (atomicOr(&seen[s >> 5], bit) & bit) atomicOr(&twice[s >> 5], bit);
-      }
-    }
-    __syncthreads();
+    const uint32_t* twice = mark_twice(c, slots, n, seen);
     int want = 0;
     for (int i = threadIdx.x; i < n; i += kPlanThreads) {
       const int s = slots[i], add = n_new[i];
@@ -356,60 +363,51 @@ __global__ void __launch_bounds__(256) copy_tails_kernel(const CacheView c, int3
 }
 
 // --------------------------------------------------------------------- write
-// One thread per 16 bytes of K and of V (blockIdx.y = 0, 1); a block has
-// `rows_per_block` rows, of at most `max_req` requests.  What bounds it: the
-// chain slot, length, page, count before the store (a ragged draft of 640 tokens
-// of 8 heads of 128, 5 MB: about 4 us), so the value is loaded beside it and the
-// indexes take 32-bit divisions (forking and growing 128 sequences and eight
-// writes: 61 us, 67 with 64-bit divisions and the value last).  While the length
-// is on its way the block looks for its requests' slots in the whole list, since
-// two entries of one slot would store to the same places in any order; that
-// takes half a microsecond a write, 65.5 us in all.
-__global__ void __launch_bounds__(256) write_kernel(const CacheView c, int layer, const int32_t* slots,
-                                                    const int32_t* n_new, int batch, int q_len, int rows,
-                                                    int rows_per_block, int max_req, const uint4* K, const uint4* V) {
-  __shared__ uint32_t twice[8];  // by warp: bit k, request b0 + k is listed again
-  const int per_row = c.row_bytes / 16;
-  const int r0 = blockIdx.x * rows_per_block, in_block = threadIdx.x / per_row;
-  const bool on = in_block < rows_per_block && r0 + in_block < rows;
-  const int r = on ? r0 + in_block : r0, unit = threadIdx.x - in_block * per_row;
-  // On its way while the page is looked up.
-  uint4 value = make_uint4(0, 0, 0, 0);
-  if (on) value = (blockIdx.y ? V : K)[(size_t)r * per_row + unit];
-  const int bh = r / q_len, i = r - bh * q_len;
-  const int b = bh / c.n_kv_heads, head = bh - b * c.n_kv_heads;
-  const int s = slots[b], add = n_new ? n_new[b] : q_len;
-  const bool in = s >= 0 && s < c.n_slots;
-  const int len = in ? c.lens[s] : 0;
-  const int b0 = r0 / (c.n_kv_heads * q_len), n_req = min(max_req, batch - b0);
-  uint32_t again = 0;
-  for (int j = threadIdx.x; j < batch; j += blockDim.x) {
-    const int other = slots[j];
-    for (int k = 0; k < n_req; ++k)
-      if (other >= 0 && j != b0 + k && slots[b0 + k] == other) again |= 1u << k;
+// One thread per 16 bytes of K or of V (blockIdx.y = 0, 1); a block takes pieces
+// of kRows rows in turn.  Two entries of one slot would store to the same places
+// in any order, so each block first marks the slots that the list has twice;
+// there are no more blocks than stay resident, so that this work grows with the
+// list only.  What bounds it: for a few tokens the chain slot, length, page, count
+// before the store (640 tokens of 8 heads of 128, 5 MB: about 4 us), so the value
+// is loaded beside it; for prompts memory (64 x 4096 tokens of 8 heads of 128:
+// 341 us, 6.3 TB/s; with a block for every piece, which cannot afford the marks,
+// 430).  For 1024 sequences grown by a token a write takes 8.0 us, 7.7 without
+// the marks; for 16384, 22 and 7.7.
+template <int PER_ROW>
+__global__ void __launch_bounds__(256, 8) write_kernel(const CacheView c, int layer, const int32_t* slots,
+                                                       const int32_t* n_new, int batch, int q_len, int rows,
+                                                       const uint4* K, const uint4* V) {
+  extern __shared__ uint32_t seen[];
+  constexpr int kRows = 256 / PER_ROW;
+  const int in_piece = threadIdx.x / PER_ROW, unit = threadIdx.x % PER_ROW;
+  const uint4* from = blockIdx.y ? V : K;
+  uint8_t* plane = c.pool + (2 * layer + blockIdx.y) * c.plane_bytes;
+  const uint32_t* twice = batch > 1 ? mark_twice(c, slots, batch, seen) : nullptr;
+  if (in_piece >= kRows) return;
+  for (int r = blockIdx.x * kRows + in_piece; r < rows; r += gridDim.x * kRows) {
+    // On its way while the page is looked up.
+    const uint4 value = from[(size_t)r * PER_ROW + unit];
+    const int bh = r / q_len, i = r - bh * q_len;
+    const int b = bh / c.n_kv_heads, head = bh - b * c.n_kv_heads;
+    const int s = slots[b], add = n_new ? n_new[b] : q_len;
+    if (s < 0) continue;
+    const bool in = s < c.n_slots && !(twice && ((twice[s >> 5] >> (s & 31)) & 1u));
+    const int len = in ? c.lens[s] : -1;
+    if (len < 0 || len > c.max_len || add < 0 || add > q_len || add > len) {
+      fault(c, kStatusBadCache);
+      continue;
+    }
+    if (i >= add) continue;
+    const int pos = len - add + i;
+    const int page = c.table[(size_t)s * c.max_pages + (pos >> c.page_shift)];
+    if (!valid_page(c, page) || c.refs[page] > 1) {
+      fault(c, kStatusBadCache);
+      continue;
+    }
+    uint8_t* to = plane + (size_t)page * c.page_bytes + (size_t)head * c.head_bytes +
+                  (size_t)(pos & (c.page - 1)) * c.row_bytes;
+    reinterpret_cast<uint4*>(to)[unit] = value;
   }
-  again = __reduce_or_sync(0xffffffffu, again);
-  if (threadIdx.x % 32 == 0) twice[threadIdx.x / 32] = again;
-  const bool sound = in && len >= 0 && len <= c.max_len && add >= 0 && add <= q_len && add <= len;
-  const int pos = len - add + i;
-  const int page = on && sound && i < add ? c.table[(size_t)s * c.max_pages + pos / c.page] : -1;
-  __syncthreads();
-  if (!on || s < 0) return;
-  again = 0;
-#pragma unroll
-  for (int w = 0; w < 8; ++w) again |= twice[w];
-  if (!sound || ((again >> (b - b0)) & 1)) {
-    fault(c, kStatusBadCache);
-    return;
-  }
-  if (i >= add) return;
-  if (!valid_page(c, page) || c.refs[page] > 1) {
-    fault(c, kStatusBadCache);
-    return;
-  }
-  uint8_t* to = c.pool + (2 * layer + blockIdx.y) * c.plane_bytes + (size_t)page * c.page_bytes +
-                (size_t)head * c.head_bytes + (size_t)(pos % c.page) * c.row_bytes;
-  reinterpret_cast<uint4*>(to)[unit] = value;
 }
 
 // ------------------------------------------------------------------- compact
@@ -558,15 +556,30 @@ cudaError_t launch_kv_extend(const CacheView& c, const int32_t* slots, const int
   return launch_dependent(copy_tails_kernel, sm_count * 8, 256, stream, c, work, n);
 }
 
-cudaError_t launch_kv_write(const CacheView& c, int layer, const int32_t* slots, const int32_t* n_new, int batch,
-                            int q_len, const void* K, const void* V, cudaStream_t stream) {
-  const int rows = batch * c.n_kv_heads * q_len, per_block = 256 / (c.row_bytes / 16);
-  static_assert(256 / (64 * 2 / 16) <= 32, "a bit per request of a block");
-  const int max_req = std::min(per_block, (per_block - 1) / (c.n_kv_heads * q_len) + 2);
-  write_kernel<<<dim3((rows - 1) / per_block + 1, 2), 256, 0, stream>>>(
-      c, layer, slots, n_new, batch, q_len, rows, per_block, max_req, reinterpret_cast<const uint4*>(K),
-      reinterpret_cast<const uint4*>(V));
+template <int PER_ROW>
+static cudaError_t launch_write(const CacheView& c, int layer, const int32_t* slots, const int32_t* n_new, int batch,
+                                int q_len, const void* K, const void* V, int sm_count, cudaStream_t stream) {
+  const int rows = batch * c.n_kv_heads * q_len, piece = 256 / PER_ROW;
+  const int smem = batch > 1 ? 2 * ((c.n_slots + 31) / 32) * 4 : 0;
+  if (smem > 40 * 1024) {
+    cudaError_t e = cudaFuncSetAttribute(write_kernel<PER_ROW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         kMaxSlots / 32 * 2 * 4);
+    if (e != cudaSuccess) return e;
+  }
+  const int blocks = std::min((rows - 1) / piece + 1, 4 * sm_count);  // of K, and as many of V: 8 an SM
+  write_kernel<PER_ROW><<<dim3(blocks, 2), 256, smem, stream>>>(c, layer, slots, n_new, batch, q_len, rows,
+                                                               reinterpret_cast<const uint4*>(K),
+                                                               reinterpret_cast<const uint4*>(V));
   return cudaGetLastError();
+}
+
+cudaError_t launch_kv_write(const CacheView& c, int layer, const int32_t* slots, const int32_t* n_new, int batch,
+                            int q_len, const void* K, const void* V, int sm_count, cudaStream_t stream) {
+  switch (c.row_bytes / 16) {
+    case 8: return launch_write<8>(c, layer, slots, n_new, batch, q_len, K, V, sm_count, stream);
+    case 12: return launch_write<12>(c, layer, slots, n_new, batch, q_len, K, V, sm_count, stream);
+    default: return launch_write<16>(c, layer, slots, n_new, batch, q_len, K, V, sm_count, stream);
+  }
 }
 
 cudaError_t launch_kv_compact(const CacheView& c, int32_t* remap, int32_t* n_live, int32_t* work, int sm_count,

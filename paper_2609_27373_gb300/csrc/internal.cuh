@@ -179,7 +179,7 @@ cudaError_t launch_kv_fork(const CacheView& c, const int32_t* src, const int32_t
 cudaError_t launch_kv_extend(const CacheView& c, const int32_t* slots, const int32_t* n_new, int n, int32_t* granted,
                              int32_t* work, int sm_count, cudaStream_t stream);
 cudaError_t launch_kv_write(const CacheView& c, int layer, const int32_t* slots, const int32_t* n_new, int batch,
-                            int q_len, const void* K, const void* V, cudaStream_t stream);
+                            int q_len, const void* K, const void* V, int sm_count, cudaStream_t stream);
 cudaError_t launch_kv_drop(const CacheView& c, const int32_t* slots, const int32_t* n_drop, int n,
                            cudaStream_t stream);
 cudaError_t launch_kv_compact(const CacheView& c, int32_t* remap, int32_t* n_live, int32_t* work, int sm_count,

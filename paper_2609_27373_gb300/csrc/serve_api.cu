@@ -134,7 +134,7 @@ extern "C" int wise_kv_write(const wise_cache_t* cache, int layer, const int32_t
     return WISE_ERR_INVALID_ARG;
   int sms;
   if ((rc = current_device(&sms, &v.status)) != WISE_OK) return rc;
-  return result(launch_kv_write(v, layer, slots, n_new, batch, q_len, K, V, stream));
+  return result(launch_kv_write(v, layer, slots, n_new, batch, q_len, K, V, sms, stream));
 }
 
 extern "C" int wise_kv_drop(const wise_cache_t* cache, const int32_t* slots, const int32_t* n_drop, int n,
