@@ -112,8 +112,9 @@ __host__ __device__ inline PfxPlan pfx_plan(int* base, int batch, int n_groups) 
 }
 
 // Workspace: where the merge finds its parts (two int4 per request and kv
-// head), then for each kind its segments' (m, l) pairs and their O, transposed as [segment][head_dim / 4][rows][4] so that neighbouring
-// threads (rows) store neighbouring 16 bytes.  A pair segment is two slots.
+// head), then for each kind its segments' (m, l) pairs and their O, transposed
+// as [segment][head_dim / 4][rows][4] so that neighbouring threads (rows) store
+// neighbouring 16 bytes.  A pair segment is two slots.
 struct PfxWork {
   int4* sources;
   float2* ml[3];

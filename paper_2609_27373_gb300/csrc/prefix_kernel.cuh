@@ -24,8 +24,11 @@
 // products at 89 clk, 400 until the softmax sees S, 300 to read it, 380 until
 // the next product.)
 //
-// What bounds it.  Long unshared sequences: HBM (38 x 8 x 8000 tokens of 128,
-// 1.25 GB, in 182 us, 6.8 TB/s).  Prefixes with 256 or more query rows a kv
+// What bounds it.  Long unshared sequences: HBM (38 x 8 x 8001 tokens of 128,
+// 1.25 GB, in 181 us, 6.9 TB/s).  Middling ones (64 x 1001 tokens, 53 us, floor
+// 39; 16 requests on a prefix of 4096, 32.5 us, floor 16) have too few tiles to
+// make up for the start, the merge and, at head dimensions 96 and 128, the one K
+// and one V slot of a stream that works alone.  Prefixes with 256 or more query rows a kv
 // head: the S buffer, at about half of the tensor rate.  Short items: one
 // warp's softmax of a tile (3600 to 4200 clk, twice what its instructions would
 // take if they were at hand) in 7000 clk from tile to tile.  So S is read whole
@@ -246,9 +249,10 @@ static __device__ __noinline__ void pfx_give_up(int* abort, int* status) {
 
 // The row of the tile at which an own item's rows start.  Few rows keep one
 // warp of a stream busy; that of stream 1 is then on another scheduler of the
-// SM than that of stream 0 (2432 items of one row and four tiles: 44 us on the
-// same scheduler, 39 us on any other one; the few rows of prefix items gain
-// nothing from it).
+// SM than that of stream 0 (256 samples on a prefix of 8192 tokens: 72.8 us on
+// the same scheduler, 71.0 on any other one; 64 requests on one of 32768: 72.2 and
+// 71.1; 2432 items of one row and one tile: 42.7 and 42.4; the few rows of prefix
+// items gain nothing from it).
 __device__ __forceinline__ int pfx_own_row(const PfxParams& p, int w) { return w == 1 && p.rows <= 32 ? 96 : 0; }
 
 // A segment: a run of key tiles of an item.
@@ -410,9 +414,8 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
       mbar_arrive(&sb.sched_full[w][e]);
     }
     ++n_ent;
-    // The tile of the K ring (r = 0) and of the V ring; Q in between.  One lane
-    // per page that the item reaches.
-    // A faulty page id becomes a coordinate out of range, which reads zeros.
+    // The tile of the K ring (r = 0) and of the V ring; Q in between.  A faulty
+    // page id becomes a coordinate out of range, which reads zeros.
     const int z = valid ? page * c.n_kv_heads + seg.kvh : c.n_pages * c.n_kv_heads;
     const int bytes = min(kPfxKeys, (seg.end - seg.pos + c.page - 1) & -c.page) * 128 * C::kBoxes;
 #pragma unroll 1
@@ -441,8 +444,8 @@ __device__ void pfx_producer(const CUtensorMap* mapK, const CUtensorMap* mapV, c
           mbar_arrive_expect_tx(&sb.q_full[w], (own ? p.rows : p.rows * p.per_tile) * 128 * C::kBoxes);
 #pragma unroll
           for (int b = 0; b < C::kBoxes; ++b)
-            tma_load_4d(q_tiles + w * C::kTileBytes + (b * 128 + (own ? pfx_own_row(p, w) : 0)) * 128, own ? mapQ1 : mapQ, &sb.q_full[w], 64 * b, 0,
-                        seg.kvh, word & 1023);
+            tma_load_4d(q_tiles + w * C::kTileBytes + (b * 128 + (own ? pfx_own_row(p, w) : 0)) * 128,
+                        own ? mapQ1 : mapQ, &sb.q_full[w], 64 * b, 0, seg.kvh, word & 1023);
         }
         ++n_q;
       }
@@ -1069,7 +1072,8 @@ cudaError_t launch_prefix_instance(const PfxLaunch& L) {
   PfxMergeShape sh = {0, D / 4, 1};
   while ((1 << sh.log_rows) < L.p.rows) ++sh.log_rows;
   const long long units = (long long)L.p.batch * L.p.cache.n_kv_heads;
-  while (sh.cols > 1 && ((sh.cols << sh.log_rows) > kMergeThreads || (units * (D / 4 / sh.cols) < 8 * L.grid && (sh.cols << sh.log_rows) > 32)))
+  while (sh.cols > 1 && ((sh.cols << sh.log_rows) > kMergeThreads ||
+                         (units * (D / 4 / sh.cols) < 8 * L.grid && (sh.cols << sh.log_rows) > 32)))
     sh.cols = sh.cols % 2 ? 1 : sh.cols / 2;
   sh.parts = kMergeThreads / (sh.cols << sh.log_rows);
   if (sh.parts > 8) sh.parts = 8;

@@ -20,9 +20,10 @@ namespace cg = cooperative_groups;
 // weights, the blocks exchange their sums through distributed shared memory,
 // and the block that holds the crossing reads the crossing part (at most 8192
 // tokens, by now in L2) once more, a few tokens per thread.  What bounds it:
-// memory bandwidth for full batches (160 x 131075 tokens in fp32: 34 us, 4.1
-// TB/s; 320: 56 us, 5.0 TB/s), the chain of dependent loads and the cluster
-// barrier for a few requests (5.1 us).  Blocks of 256 threads, five an SM, keep
+// memory for full batches, at less than its bandwidth since blocks with one row
+// run beside blocks with two and their set-up beside nothing (160 x 131075 tokens
+// in fp32, one wave: 34 us, 4.1 TB/s; 320: 56 us, 5.0 TB/s), the chain of
+// dependent loads and the cluster barrier for a few requests (5.1 us).  Blocks of 256 threads, five an SM, keep
 // requests in different phases side by side (512 threads, two an SM: 45 us for
 // the 160).
 constexpr int kThreads = 256;
@@ -221,8 +222,8 @@ template <typename T, int VEC>
 cudaError_t launch_instance(const VerifyParams& p, cudaStream_t stream) {
   // Blocks of a request: fewer for small vocabularies, where 8 would have
   // little to read each, and 4 once 8 a request are more than one wave (320
-  // rows of 65536 in bf16: 22.7 us with 4, 29.6 with 8; 80 rows: 8.7 and 9.1;
-  // 40 rows of 131075 in fp32, one wave: 18.3 and 13.5).
+  // requests of 65536 in bf16: 21.8 us with 4, 28.8 with 8; 80, one wave: 8.4
+  // and 8.5; 40 of 131075 in fp32: 18.0 and 12.6).
   int cluster = (long long)p.batch * 8 > (long long)p.sm_count * kBlocksPerSM ? 4 : 8;
   while (cluster > 1 && p.vocab <= cluster * kThreads * 4) cluster /= 2;
   cudaLaunchAttribute attr[1];
