@@ -289,7 +289,7 @@ int wise_support_overlap(const wise_shape_t* shape, const int32_t* idx_a, const 
 /* ------------------------------------------------------------- serving --
  * What follows the recurrent steps when the model answers: a paged cache of
  * keys and values, attention of new tokens over it with prefixes that
- * requests share read once for all, and the verification of drafted tokens.
+ * requests share read for up to 256 query rows at a time, and the verification of drafted tokens.
  * The paper stops before this point; none of it changes the calls above.
  *
  * A cache is a pool of pages and, per sequence slot, a table row of page ids
