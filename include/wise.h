@@ -65,6 +65,8 @@ extern "C" {
 #define WISE_BF16 0
 #define WISE_FP16 1
 #define WISE_FP32 2
+#define WISE_E4M3 3 /* caches only: 8 bits and a scale for 16 values */
+#define WISE_E2M1 4 /* caches only: 4 bits and a scale for 16 values */
 
 #define WISE_SEL_TOPK 0
 #define WISE_SEL_COVERAGE 1
@@ -321,8 +323,9 @@ typedef struct {
   int n_layers;
   int n_kv_heads;
   int head_dim;   /* 64, 96 or 128 */
-  int dtype;      /* WISE_BF16 or WISE_FP16 */
-  void* pool;     /* [n_layers][2: keys, values][n_pages][n_kv_heads][page][head_dim], 16-byte aligned */
+  int dtype;      /* WISE_BF16 or WISE_FP16, or WISE_E4M3 or WISE_E2M1 (see "Caches in 8 or 4 bits") */
+  void* pool;     /* [n_layers][2: keys, values][n_pages][n_kv_heads][page][head_dim], 16-byte aligned; in 8 or 4
+                     bits [n_layers][n_pages][n_kv_heads][wise_kvq_block_bytes] */
   int32_t* table; /* [n_slots][max_pages] */
   int32_t* lens;  /* [n_slots] */
   int32_t* refs;  /* [n_pages] */
@@ -417,6 +420,59 @@ int wise_prefix_attn(const wise_cache_t* cache, int layer, const wise_prefix_t* 
                      const int32_t* slots, const int32_t* n_new, const int32_t* group_start,
                      const int32_t* prefix_lens, void* O, void* workspace, size_t workspace_bytes,
                      cudaStream_t stream);
+
+/* Caches in 8 or 4 bits.  16 neighbouring values of a token's row in one kv
+ * head share a scale s; with a = the largest size among them
+ *   WISE_E2M1  s = a / 6 rounded to the nearest number of 5 exponent and 3
+ *              mantissa bits (steps of 2^-17 below 2^-14), at most 10240; a
+ *              value x becomes s times the nearest of 0, 0.5, 1, 1.5, 2, 3, 4
+ *              and 6 with x's sign to x / s (0 where s is 0);
+ *   WISE_E4M3  s = 2^k, k the smallest in [-15, 7] with a <= 448 * 2^k; x
+ *              becomes s times the nearest number of 4 exponent and 3 mantissa
+ *              bits, at most 448 in size, to x / s.
+ * Ties go to the even code.  What is stored is a number of bf16 and of fp16, so
+ * reading it back is exact; sizes above 61440 (WISE_E2M1) or 57344 (WISE_E4M3)
+ * become these.  K and V must be finite: an infinity becomes the largest
+ * number of its group's scale, a NaN has no meaning (the others of its group keep theirs).
+ *
+ * wise_kv_fork, _extend, _drop, _compact and _workspace take such a cache as
+ * they take one of 16 bits; wise_kv_write and wise_prefix_attn do not
+ * (WISE_ERR_UNSUPPORTED), the calls below are in their place.  The bytes of a
+ * token in one kv head are head_dim * bits / 4 + head_dim / 8 (two more with a
+ * head_dim of 96): 144 and 272 with 128, where 16 bits take 512. */
+
+/* Bytes of the block of one page and kv head (keys and values, with their
+ * scales) in a pool of type dtype; 0 where page, head_dim or dtype is none that
+ * a cache in 8 or 4 bits has. */
+size_t wise_kvq_block_bytes(int page, int head_dim, int dtype);
+
+/* wise_kv_write into a cache in 8 or 4 bits: K and V are of type dtype
+ * (WISE_BF16 or WISE_FP16), everything else is as there. */
+int wise_kvq_write(const wise_cache_t* cache, int layer, const int32_t* slots, const int32_t* n_new, int batch,
+                   int q_len, int dtype, const void* K, const void* V, cudaStream_t stream);
+
+/* Reads keys and values of one layer back, from a cache of any type: row
+ * i < count[b] of K and V [batch, n_kv_heads, rows, head_dim] becomes position
+ * first[b] + i of the sequence in slot slots[b].  Rows with i >= count[b], past
+ * the sequence's end, on a page without a sound id, of an unused (negative) slot or of a
+ * faulty entry (a slot out of range, first or count negative, count above
+ * rows, first above max_pages * page) become 0; faults are recorded.  A slot
+ * may be listed more than once.  dtype: the type of K and V, WISE_BF16 or
+ * WISE_FP16 (of a cache of 16 bits, its own).  first: device int32 [batch], or
+ * NULL (0 for all); count: device int32 [batch], or NULL (rows for all).  K,
+ * V: 16-byte aligned; batch * n_kv_heads * rows <= 2^29. */
+int wise_kv_read(const wise_cache_t* cache, int layer, const int32_t* slots, const int32_t* first,
+                 const int32_t* count, int batch, int rows, int dtype, void* K, void* V, cudaStream_t stream);
+
+/* wise_prefix_attn over a cache in 8 or 4 bits.  Q and O are of type dtype
+ * (WISE_BF16 or WISE_FP16); rows, groups, workspace, limits and faults are as
+ * there.  Rows at or past lens may hold anything here too. */
+size_t wise_kvq_attn_workspace(const wise_cache_t* cache, const wise_prefix_t* shape);
+
+int wise_kvq_attn(const wise_cache_t* cache, int layer, const wise_prefix_t* shape, int dtype, const void* Q,
+                  const int32_t* slots, const int32_t* n_new, const int32_t* group_start,
+                  const int32_t* prefix_lens, void* O, void* workspace, size_t workspace_bytes,
+                  cudaStream_t stream);
 
 /* Verification of drafted tokens (speculative sampling).  Request b has
  * n_draft[b] <= k_max drafted tokens x_i = draft[b][i] with draft

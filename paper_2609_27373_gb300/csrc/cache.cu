@@ -8,7 +8,7 @@
 
 #include <algorithm>
 
-#include "internal.cuh"
+#include "cache_common.cuh"
 #include "ptx.cuh"
 
 namespace wise {
@@ -18,30 +18,6 @@ namespace cg = cooperative_groups;
 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
-
-__device__ __forceinline__ void fault(const CacheView& c, int bits) { atomicOr(c.status, bits); }
-
-__device__ __forceinline__ bool valid_page(const CacheView& c, int page) { return page >= 0 && page < c.n_pages; }
-
-__device__ __forceinline__ int pages_of(const CacheView& c, int len) { return (len + c.page - 1) / c.page; }
-
-// Marks slots listed twice in bitmaps over the slots in shared memory; the second
-// one, behind the first, is the result.  Ends with a barrier.
-__device__ __forceinline__ const uint32_t* mark_twice(const CacheView& c, const int32_t* slots, int n, uint32_t* seen) {
-  const int words = (c.n_slots + 31) / 32;
-  uint32_t* twice = seen + words;
-  for (int k = threadIdx.x; k < 2 * words; k += blockDim.x) seen[k] = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const int s = slots[i];
-    if (s >= 0 && s < c.n_slots) {
-      const uint32_t bit = 1u << (s & 31);
-      if (atomicOr(&seen[s >> 5], bit) & bit) atomicOr(&twice[s >> 5], bit);
-    }
-  }
-  __syncthreads();
-  return twice;
-}
 
 // ---------------------------------------------------------------------- fork
 // One block per entry.  An entry whose dst occurs again in a used entry is
@@ -343,7 +319,8 @@ __global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const CacheVi
 }
 
 // Copies the first `rows` rows of every head of a page, in every plane; one
-// block per (copy, plane, head) in turn, whose rows are contiguous.  What
+// block per (copy, plane, head) in turn, whose rows are contiguous (in 8 and 4
+// bits the tokens of a page lie beside one another: all of them).  What
 // bounds it: memory for many copies (124 part-filled pages of 8 layers, 146 MB
 // written and as much read, most of it from L2, in 21 us).
 __global__ void __launch_bounds__(256) copy_tails_kernel(const CacheView c, int32_t* work, int n) {
@@ -357,7 +334,7 @@ __global__ void __launch_bounds__(256) copy_tails_kernel(const CacheView c, int3
     uint8_t* base = c.pool + plane * c.plane_bytes + (size_t)head * c.head_bytes;
     const uint4* from = reinterpret_cast<const uint4*>(base + (size_t)w.copies[3 * at] * c.page_bytes);
     uint4* to = reinterpret_cast<uint4*>(base + (size_t)w.copies[3 * at + 1] * c.page_bytes);
-    const int units = w.copies[3 * at + 2] * (c.row_bytes / 16);
+    const int units = c.bits == 16 ? w.copies[3 * at + 2] * (c.row_bytes / 16) : c.head_bytes / 16;
     for (int k = threadIdx.x; k < units; k += blockDim.x) to[k] = from[k];
   }
 }

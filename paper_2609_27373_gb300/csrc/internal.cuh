@@ -160,10 +160,11 @@ constexpr int kMaxSlots = 1 << 18;  // of a cache, and entries of a list
 // A paged cache as the kernels see it (wise_cache_t).
 struct CacheView {
   int n_pages, page, page_shift, n_slots, max_pages;  // page = 1 << page_shift
-  int n_planes;           // n_layers * 2
+  int bits;               // of a value: 16, 8 or 4
+  int n_planes;           // n_layers * 2; with 8 or 4 bits n_layers
   long long plane_bytes;  // n_pages * page_bytes
-  int page_bytes;         // n_kv_heads * page * head_dim * 2
-  int head_bytes;         // page * head_dim * 2
+  int page_bytes;         // n_kv_heads * head_bytes
+  int head_bytes;         // page * head_dim * 2; with 8 or 4 bits a block of quant.cuh
   int row_bytes;          // head_dim * 2
   int n_kv_heads;
   uint8_t* pool;
@@ -185,6 +186,21 @@ cudaError_t launch_kv_drop(const CacheView& c, const int32_t* slots, const int32
 cudaError_t launch_kv_compact(const CacheView& c, int32_t* remap, int32_t* n_live, int32_t* work, int sm_count,
                               cudaStream_t stream);
 
+// Writing to a cache in 8 or 4 bits, and reading from any cache (quant.cu).
+struct QuantIo {
+  CacheView cache;
+  int layer, head_dim, batch, rows;  // rows of K and V: [batch][n_kv_heads][rows][head_dim]
+  bool fp16;
+  const int32_t* slots;
+  const int32_t* first;  // reading: of the rows' positions, NULL for 0
+  const int32_t* count;  // rows of each sequence, NULL for all
+  const void* K;
+  const void* V;
+  int sm_count;
+};
+cudaError_t launch_kvq_write(const QuantIo& io, cudaStream_t stream);
+cudaError_t launch_kv_read(const QuantIo& io, cudaStream_t stream);
+
 struct PrefixParams {
   CacheView cache;
   int layer;
@@ -202,6 +218,10 @@ struct PrefixParams {
 // Defined in prefix_attn.cu.
 size_t prefix_attn_workspace(const PrefixParams& p, int sm_count);
 int launch_prefix_attn(const PrefixParams& p, void* workspace, int sm_count, cudaStream_t stream);
+
+// Attention over a cache in 8 or 4 bits (quant_attn.cu); p.fp16 is the type of Q and O.
+size_t quant_attn_workspace(const PrefixParams& p, int sm_count);
+int launch_quant_attn(const PrefixParams& p, void* workspace, int sm_count, cudaStream_t stream);
 
 struct VerifyParams {
   int batch, k_max, vocab, sm_count;

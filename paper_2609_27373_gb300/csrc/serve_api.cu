@@ -6,6 +6,7 @@
 
 #include "internal.cuh"
 #include "prefix_attn.cuh"
+#include "quant.cuh"
 #include "wise.h"
 
 namespace wise {
@@ -25,7 +26,8 @@ int check_cache(const wise_cache_t* c, bool pool, CacheView* v) {
     return WISE_ERR_INVALID_ARG;
   if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return WISE_ERR_UNSUPPORTED;
   if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128) return WISE_ERR_UNSUPPORTED;
-  if (c->dtype != WISE_BF16 && c->dtype != WISE_FP16) return WISE_ERR_UNSUPPORTED;
+  if (c->dtype != WISE_BF16 && c->dtype != WISE_FP16 && c->dtype != WISE_E4M3 && c->dtype != WISE_E2M1)
+    return WISE_ERR_UNSUPPORTED;
   if (c->n_slots > kMaxSlots || (long long)c->max_pages * c->page > (1LL << 30) ||
       (long long)c->n_pages * c->n_kv_heads > INT32_MAX || c->n_pages >= (1 << 30) - 1 || c->n_kv_heads > (1 << 14) || c->n_layers > (1 << 20))
     return WISE_ERR_UNSUPPORTED;
@@ -36,9 +38,10 @@ int check_cache(const wise_cache_t* c, bool pool, CacheView* v) {
   v->page_shift = c->page == 16 ? 4 : c->page == 32 ? 5 : c->page == 64 ? 6 : 7;
   v->n_slots = c->n_slots;
   v->max_pages = c->max_pages;
-  v->n_planes = 2 * c->n_layers;
+  v->bits = c->dtype == WISE_E4M3 ? 8 : c->dtype == WISE_E2M1 ? 4 : 16;
+  v->n_planes = v->bits == 16 ? 2 * c->n_layers : c->n_layers;
   v->row_bytes = c->head_dim * 2;
-  v->head_bytes = v->row_bytes * c->page;
+  v->head_bytes = v->bits == 16 ? v->row_bytes * c->page : q_block_bytes(v->bits, c->head_dim, c->page);
   v->page_bytes = v->head_bytes * c->n_kv_heads;
   v->plane_bytes = (long long)v->page_bytes * c->n_pages;
   v->n_kv_heads = c->n_kv_heads;
@@ -50,12 +53,16 @@ int check_cache(const wise_cache_t* c, bool pool, CacheView* v) {
   return WISE_OK;
 }
 
+bool type16(int dtype) { return dtype == WISE_BF16 || dtype == WISE_FP16; }
+
 int result(cudaError_t e) { return e == cudaSuccess ? WISE_OK : WISE_ERR_CUDA; }
 
-// Shape checks of the attention (everything but the device pointers).
-int check_prefix(const wise_cache_t* cache, const wise_prefix_t* sh, PrefixParams* p) {
+// Shape checks of the attention (everything but the device pointers), over a
+// cache of 16 bits or of fewer.
+int check_prefix(const wise_cache_t* cache, const wise_prefix_t* sh, bool quantised, PrefixParams* p) {
   int rc = check_cache(cache, true, &p->cache);
   if (rc != WISE_OK) return rc;
+  if ((p->cache.bits == 16) == quantised) return WISE_ERR_UNSUPPORTED;
   if (!sh || sh->batch < 0 || sh->q_len < 0 || sh->n_heads <= 0 || sh->n_groups < 0 || !(sh->scale >= 0.0f) ||
       isinf(sh->scale))
     return WISE_ERR_INVALID_ARG;
@@ -127,6 +134,7 @@ extern "C" int wise_kv_write(const wise_cache_t* cache, int layer, const int32_t
   CacheView v;
   int rc = check_cache(cache, true, &v);
   if (rc != WISE_OK) return rc;
+  if (v.bits != 16) return WISE_ERR_UNSUPPORTED;
   if (layer < 0 || layer >= cache->n_layers || batch < 0 || q_len < 0) return WISE_ERR_INVALID_ARG;
   if (batch == 0 || q_len == 0) return WISE_OK;
   if (batch > kMaxSlots || (long long)batch * q_len > (1LL << 30) / cache->n_kv_heads) return WISE_ERR_UNSUPPORTED;
@@ -135,6 +143,64 @@ extern "C" int wise_kv_write(const wise_cache_t* cache, int layer, const int32_t
   int sms;
   if ((rc = current_device(&sms, &v.status)) != WISE_OK) return rc;
   return result(launch_kv_write(v, layer, slots, n_new, batch, q_len, K, V, sms, stream));
+}
+
+extern "C" size_t wise_kvq_block_bytes(int page, int head_dim, int dtype) {
+  if (page != 16 && page != 32 && page != 64 && page != 128) return 0;
+  if (head_dim != 64 && head_dim != 96 && head_dim != 128) return 0;
+  if (dtype != WISE_E4M3 && dtype != WISE_E2M1) return 0;
+  return q_block_bytes(dtype == WISE_E4M3 ? 8 : 4, head_dim, page);
+}
+
+extern "C" int wise_kvq_write(const wise_cache_t* cache, int layer, const int32_t* slots, const int32_t* n_new,
+                              int batch, int q_len, int dtype, const void* K, const void* V, cudaStream_t stream) {
+  QuantIo io;
+  int rc = check_cache(cache, true, &io.cache);
+  if (rc != WISE_OK) return rc;
+  if (io.cache.bits == 16 || !type16(dtype)) return WISE_ERR_UNSUPPORTED;
+  if (layer < 0 || layer >= cache->n_layers || batch < 0 || q_len < 0) return WISE_ERR_INVALID_ARG;
+  if (batch == 0 || q_len == 0) return WISE_OK;
+  if (batch > kMaxSlots || (long long)batch * q_len > (1LL << 30) / cache->n_kv_heads) return WISE_ERR_UNSUPPORTED;
+  if (!ok32(slots) || !aligned(n_new, 4) || !K || !V || !aligned(K, 16) || !aligned(V, 16))
+    return WISE_ERR_INVALID_ARG;
+  if ((rc = current_device(&io.sm_count, &io.cache.status)) != WISE_OK) return rc;
+  io.layer = layer;
+  io.head_dim = cache->head_dim;
+  io.batch = batch;
+  io.rows = q_len;
+  io.fp16 = dtype == WISE_FP16;
+  io.slots = slots;
+  io.first = nullptr;
+  io.count = n_new;
+  io.K = K;
+  io.V = V;
+  return result(launch_kvq_write(io, stream));
+}
+
+extern "C" int wise_kv_read(const wise_cache_t* cache, int layer, const int32_t* slots, const int32_t* first,
+                            const int32_t* count, int batch, int rows, int dtype, void* K, void* V,
+                            cudaStream_t stream) {
+  QuantIo io;
+  int rc = check_cache(cache, true, &io.cache);
+  if (rc != WISE_OK) return rc;
+  if (!type16(dtype) || (io.cache.bits == 16 && dtype != cache->dtype)) return WISE_ERR_UNSUPPORTED;
+  if (layer < 0 || layer >= cache->n_layers || batch < 0 || rows < 0) return WISE_ERR_INVALID_ARG;
+  if (batch == 0 || rows == 0) return WISE_OK;
+  if (batch > kMaxSlots || (long long)batch * rows > (1LL << 29) / cache->n_kv_heads) return WISE_ERR_UNSUPPORTED;
+  if (!ok32(slots) || !aligned(first, 4) || !aligned(count, 4) || !K || !V || !aligned(K, 16) || !aligned(V, 16))
+    return WISE_ERR_INVALID_ARG;
+  if ((rc = current_device(&io.sm_count, &io.cache.status)) != WISE_OK) return rc;
+  io.layer = layer;
+  io.head_dim = cache->head_dim;
+  io.batch = batch;
+  io.rows = rows;
+  io.fp16 = dtype == WISE_FP16;
+  io.slots = slots;
+  io.first = first;
+  io.count = count;
+  io.K = K;
+  io.V = V;
+  return result(launch_kv_read(io, stream));
 }
 
 extern "C" int wise_kv_drop(const wise_cache_t* cache, const int32_t* slots, const int32_t* n_drop, int n,
@@ -164,7 +230,7 @@ extern "C" int wise_kv_compact(const wise_cache_t* cache, int32_t* remap, int32_
 
 extern "C" size_t wise_prefix_attn_workspace(const wise_cache_t* cache, const wise_prefix_t* shape) {
   PrefixParams p;
-  if (check_prefix(cache, shape, &p) != WISE_OK || p.batch == 0 || p.q_len == 0) return 0;
+  if (check_prefix(cache, shape, false, &p) != WISE_OK || p.batch == 0 || p.q_len == 0) return 0;
   int sms;
   int* status;
   if (current_device(&sms, &status) != WISE_OK) return 0;
@@ -176,7 +242,7 @@ extern "C" int wise_prefix_attn(const wise_cache_t* cache, int layer, const wise
                                 const int32_t* prefix_lens, void* O, void* workspace, size_t workspace_bytes,
                                 cudaStream_t stream) {
   PrefixParams p;
-  int rc = check_prefix(cache, shape, &p);
+  int rc = check_prefix(cache, shape, false, &p);
   if (rc != WISE_OK) return rc;
   if (layer < 0 || layer >= cache->n_layers) return WISE_ERR_INVALID_ARG;
   if (p.batch == 0 || p.q_len == 0) return WISE_OK;
@@ -195,6 +261,43 @@ extern "C" int wise_prefix_attn(const wise_cache_t* cache, int layer, const wise
   p.group_start = group_start;
   p.prefix_lens = prefix_lens;
   return launch_prefix_attn(p, workspace, sms, stream);
+}
+
+extern "C" size_t wise_kvq_attn_workspace(const wise_cache_t* cache, const wise_prefix_t* shape) {
+  PrefixParams p;
+  if (check_prefix(cache, shape, true, &p) != WISE_OK || p.batch == 0 || p.q_len == 0) return 0;
+  int sms;
+  int* status;
+  if (current_device(&sms, &status) != WISE_OK) return 0;
+  return quant_attn_workspace(p, sms);
+}
+
+extern "C" int wise_kvq_attn(const wise_cache_t* cache, int layer, const wise_prefix_t* shape, int dtype,
+                             const void* Q, const int32_t* slots, const int32_t* n_new, const int32_t* group_start,
+                             const int32_t* prefix_lens, void* O, void* workspace, size_t workspace_bytes,
+                             cudaStream_t stream) {
+  PrefixParams p;
+  int rc = check_prefix(cache, shape, true, &p);
+  if (rc != WISE_OK) return rc;
+  if (!type16(dtype)) return WISE_ERR_UNSUPPORTED;
+  if (layer < 0 || layer >= cache->n_layers) return WISE_ERR_INVALID_ARG;
+  if (p.batch == 0 || p.q_len == 0) return WISE_OK;
+  if (!Q || !O || !aligned(Q, 16) || !aligned(O, 16) || !ok32(slots) || !aligned(n_new, 4))
+    return WISE_ERR_INVALID_ARG;
+  if (p.n_groups > 0 && (!ok32(group_start) || !ok32(prefix_lens))) return WISE_ERR_INVALID_ARG;
+  int sms;
+  if ((rc = current_device(&sms, &p.cache.status)) != WISE_OK) return rc;
+  const size_t need = quant_attn_workspace(p, sms);
+  if (workspace_bytes < need || (need > 0 && (!workspace || !aligned(workspace, 16)))) return WISE_ERR_INVALID_ARG;
+  p.layer = layer;
+  p.fp16 = dtype == WISE_FP16;
+  p.Q = Q;
+  p.O = O;
+  p.slots = slots;
+  p.n_new = n_new;
+  p.group_start = group_start;
+  p.prefix_lens = prefix_lens;
+  return launch_quant_attn(p, workspace, sms, stream);
 }
 
 extern "C" int wise_verify_draft(int batch, int k_max, int vocab, int dtype, const void* p, const void* q,

@@ -13,6 +13,10 @@ the library's entry points in their order of use:
     accepted, tokens = verify_draft(p, q, draft, n_draft, u_accept, u_sample)
     cache.drop(slots, n_rejected)                   # rejected drafts, or sequences that ended
     cache.compact()                                 # pages in use to the front of the pool
+    cache.read(layer, K, V, slots)                  # keys and values out of the cache again
+
+With bits=8 or bits=4 the cache holds its keys and values in 8 or 4 bits (see
+include/wise.h); its calls are the same, and take and return tensors of `dtype`.
 
 Every call is asynchronous on `stream` (default: torch's current stream);
 calls on one cache must be ordered on a stream, and two calls that may run at
@@ -39,25 +43,29 @@ def _empty(shape, dtype, device, stream):
 
 
 class PagedCache(wise.Cache):
-    """A paged cache with its workspaces (see wise.Cache for the tensors)."""
+    """A paged cache with its workspaces (see wise.Cache for the tensors), in 16, 8 or 4 bits."""
 
     def __init__(self, n_layers: int, n_pages: int, n_kv_heads: int, page: int, head_dim: int, n_slots: int,
-                 max_pages: int, dtype=torch.bfloat16, device=None):
+                 max_pages: int, dtype=torch.bfloat16, device=None, bits: int = 16):
         dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-        self._own(torch.empty((2 * n_layers, n_pages, n_kv_heads, page, head_dim), dtype=dtype, device=dev),
-                  torch.zeros((n_slots, max_pages), dtype=torch.int32, device=dev),
+        if bits == 16:
+            pool = torch.empty((2 * n_layers, n_pages, n_kv_heads, page, head_dim), dtype=dtype, device=dev)
+        else:
+            pool = torch.empty((n_layers, n_pages, n_kv_heads, wise.kvq_block_bytes(page, head_dim, bits)),
+                               dtype=torch.uint8, device=dev)
+        self._own(pool, torch.zeros((n_slots, max_pages), dtype=torch.int32, device=dev),
                   torch.zeros((n_slots,), dtype=torch.int32, device=dev),
-                  torch.zeros((n_pages,), dtype=torch.int32, device=dev))
+                  torch.zeros((n_pages,), dtype=torch.int32, device=dev), bits, page, head_dim, dtype)
 
     @classmethod
-    def over(cls, pool, table, lens, refs) -> "PagedCache":
-        """A cache over tensors that the caller holds."""
+    def over(cls, pool, table, lens, refs, bits: int = 16, page=None, head_dim=None, dtype=None) -> "PagedCache":
+        """A cache over tensors that the caller holds; in 8 or 4 bits, page, head_dim and dtype are given too."""
         cache = cls.__new__(cls)
-        cache._own(pool, table, lens, refs)
+        cache._own(pool, table, lens, refs, bits, page, head_dim, dtype)
         return cache
 
-    def _own(self, pool, table, lens, refs) -> None:
-        wise.Cache.__init__(self, pool, table, lens, refs)
+    def _own(self, pool, table, lens, refs, bits=16, page=None, head_dim=None, dtype=None) -> None:
+        wise.Cache.__init__(self, pool, table, lens, refs, bits, page, head_dim, dtype)
         self._streams = {}     # streams that have used the cache, by handle
         self._workspaces = []  # all of them, see _grown
         self._kv_ws = None
@@ -108,7 +116,13 @@ class PagedCache(wise.Cache):
 
     def write(self, layer: int, slots, granted, K, V, stream=None) -> None:
         """Stores one layer's new keys and values [batch, n_kv_heads, q_len, head_dim] at the sequences' ends."""
-        wise.wise_kv_write(self, layer, slots, granted, K, V, self._use(stream))
+        write = wise.wise_kv_write if self.bits == 16 else wise.wise_kvq_write
+        write(self, layer, slots, granted, K, V, self._use(stream))
+
+    def read(self, layer: int, K, V, slots, first=None, count=None, stream=None) -> None:
+        """Reads one layer's keys and values back into K and V [batch, n_kv_heads, rows, head_dim]: positions first[b]
+        .. of each sequence, count[b] of them (None: from 0, and `rows`); the other rows become 0."""
+        wise.wise_kv_read(self, layer, K, V, slots, first, count, self._use(stream))
 
     def drop(self, slots, n_drop, stream=None) -> None:
         """Takes the last n_drop tokens (at most all) off each sequence."""
@@ -127,13 +141,15 @@ class PagedCache(wise.Cache):
         """Attention of Q [batch, n_heads, q_len, head_dim] over the sequences in slots, into O; the requests of
         each group share their first prefix_lens[g] tokens."""
         raw = self._use(stream)
+        plain = self.bits == 16
         key = (Q.shape, 0 if prefix_lens is None else prefix_lens.shape[0], scale)
         if key != self._attn_key:
             shape = wise.prefix_shape(self, Q, key[1], scale)
-            self._attn_ws = self._grown(self._attn_ws, wise.wise_prefix_attn_workspace(self, shape), stream)
+            need = (wise.wise_prefix_attn_workspace if plain else wise.wise_kvq_attn_workspace)(self, shape)
+            self._attn_ws = self._grown(self._attn_ws, need, stream)
             self._attn_key, self._attn_shape = key, shape
-        wise.wise_prefix_attn(self, layer, Q, O, slots, n_new, group_start, prefix_lens, self._attn_ws, scale, raw,
-                              self._attn_shape)
+        attn = wise.wise_prefix_attn if plain else wise.wise_kvq_attn
+        attn(self, layer, Q, O, slots, n_new, group_start, prefix_lens, self._attn_ws, scale, raw, self._attn_shape)
 
 
 def verify_draft(p, q, draft, n_draft, u_accept, u_sample, stream=None):

@@ -33,7 +33,8 @@ EXPORTS = ("wise_full_attn_accumulate", "wise_full_attn_accumulate_noalloc", "wi
            "wise_support_overlap",
            "wise_select_working_set", "wise_get_status", "wise_set_wait_limit_ns", "wise_status_string",
            "wise_version", "wise_kv_fork", "wise_kv_workspace", "wise_kv_extend", "wise_kv_write", "wise_kv_drop",
-           "wise_kv_compact", "wise_prefix_attn", "wise_prefix_attn_workspace", "wise_verify_draft")
+           "wise_kv_compact", "wise_prefix_attn", "wise_prefix_attn_workspace", "wise_kvq_block_bytes",
+           "wise_kvq_write", "wise_kv_read", "wise_kvq_attn", "wise_kvq_attn_workspace", "wise_verify_draft")
 NOALLOC_SCRATCH_BYTES = 8 << 20
 
 
@@ -139,6 +140,13 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         lib.wise_prefix_attn_workspace.argtypes = [C, ctypes.POINTER(wise_prefix_t)]
         lib.wise_prefix_attn_workspace.restype = Z
         lib.wise_prefix_attn.argtypes = [C, I, ctypes.POINTER(wise_prefix_t), P, P, P, P, P, P, P, Z, P]
+        lib.wise_kvq_block_bytes.argtypes = [I, I, I]
+        lib.wise_kvq_block_bytes.restype = Z
+        lib.wise_kvq_write.argtypes = [C, I, P, P, I, I, I, P, P, P]
+        lib.wise_kv_read.argtypes = [C, I, P, P, P, I, I, I, P, P, P]
+        lib.wise_kvq_attn_workspace.argtypes = [C, ctypes.POINTER(wise_prefix_t)]
+        lib.wise_kvq_attn_workspace.restype = Z
+        lib.wise_kvq_attn.argtypes = [C, I, ctypes.POINTER(wise_prefix_t), I, P, P, P, P, P, P, P, Z, P]
         lib.wise_verify_draft.argtypes = [I, I, I, I, P, P, P, P, P, P, P, P, P]
         lib.wise_get_status.argtypes = [P]
         lib.wise_set_wait_limit_ns.argtypes = [ctypes.c_ulonglong]
@@ -391,18 +399,49 @@ _CACHE_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 _PROB_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
+_CACHE_BITS = {8: 3, 4: 4}  # dtype codes of caches in 8 and 4 bits
+
+
+def kvq_block_bytes(page: int, head_dim: int, bits: int) -> int:
+    """Bytes of the block of one page and kv head in the pool of a cache in 8 or 4 bits."""
+    n = int(load().wise_kvq_block_bytes(page, head_dim, _CACHE_BITS.get(bits, -1)))
+    if n == 0:
+        raise ValueError(f"no cache has pages of {page} tokens, a head_dim of {head_dim} and {bits} bits")
+    return n
+
+
 class Cache:
     """A paged cache's device memory, checked once: pool [2 * n_layers,
     n_pages, n_kv_heads, page, head_dim] in bf16 or fp16 (plane 2 l holds the
     keys of layer l, 2 l + 1 its values), and int32 table [n_slots, max_pages],
-    lens [n_slots] and refs [n_pages]."""
+    lens [n_slots] and refs [n_pages].
 
-    def __init__(self, pool, table, lens, refs):
-        if pool is None or pool.dim() != 5 or pool.dtype not in _CACHE_DTYPES:
-            raise ValueError("pool must be bf16 or fp16 [2 * n_layers, n_pages, n_kv_heads, page, head_dim]")
-        planes, n_pages, n_kv_heads, page, head_dim = pool.shape
-        if planes < 2 or planes % 2:
-            raise ValueError("pool must have a plane of keys and one of values for each layer")
+    With bits = 8 or 4, pool is uint8 [n_layers, n_pages, n_kv_heads,
+    kvq_block_bytes(page, head_dim, bits)], and page, head_dim and dtype (bf16
+    or fp16: the type of the keys, values, queries and outputs that the calls
+    take) are given beside it."""
+
+    def __init__(self, pool, table, lens, refs, bits: int = 16, page=None, head_dim=None, dtype=None):
+        if bits == 16:
+            if pool is None or pool.dim() != 5 or pool.dtype not in _CACHE_DTYPES:
+                raise ValueError("pool must be bf16 or fp16 [2 * n_layers, n_pages, n_kv_heads, page, head_dim]")
+            planes, n_pages, n_kv_heads, *rest = pool.shape
+            if planes < 2 or planes % 2:
+                raise ValueError("pool must have a plane of keys and one of values for each layer")
+            for given, own in ((page, rest[0]), (head_dim, rest[1]), (dtype, pool.dtype)):
+                if given is not None and given != own:
+                    raise ValueError(f"{given} was given for a pool with {own}")
+            (page, head_dim), dtype, n_layers, code = rest, pool.dtype, planes // 2, _CACHE_DTYPES[pool.dtype]
+        else:
+            if bits not in _CACHE_BITS:
+                raise ValueError(f"bits must be 16, 8 or 4, not {bits}")
+            if page is None or head_dim is None or dtype not in _CACHE_DTYPES:
+                raise ValueError("a cache in 8 or 4 bits needs page, head_dim and dtype (bf16 or fp16)")
+            size = kvq_block_bytes(page, head_dim, bits)
+            if pool is None or pool.dim() != 4 or pool.dtype is not torch.uint8 or pool.shape[3] != size:
+                raise ValueError(f"pool must be uint8 [n_layers, n_pages, n_kv_heads, {size}]")
+            n_layers, n_pages, n_kv_heads, _ = pool.shape
+            code = _CACHE_BITS[bits]
         if table is None or table.dim() != 2:
             raise ValueError("table must be int32 [n_slots, max_pages]")
         n_slots, max_pages = table.shape
@@ -414,11 +453,11 @@ class Cache:
             raise ValueError("pool, table, lens and refs must be on one device")
         self.pool, self.table, self.lens, self.refs = pool, table, lens, refs
         self.n_pages, self.page, self.n_slots, self.max_pages = n_pages, page, n_slots, max_pages
-        self.n_layers, self.n_kv_heads, self.head_dim = planes // 2, n_kv_heads, head_dim
-        self.device, self.dtype, self.index = pool.device, pool.dtype, pool.get_device()
-        self.c = wise_cache_t(n_pages, page, n_slots, max_pages, planes // 2, n_kv_heads, head_dim,
-                              _CACHE_DTYPES[pool.dtype], pool.data_ptr(), table.data_ptr(), lens.data_ptr(),
-                              refs.data_ptr())
+        self.n_layers, self.n_kv_heads, self.head_dim, self.bits = n_layers, n_kv_heads, head_dim, bits
+        self.device, self.dtype, self.index = pool.device, dtype, pool.get_device()
+        self.type_code = _CACHE_DTYPES[dtype]  # of keys, values, queries and outputs
+        self.c = wise_cache_t(n_pages, page, n_slots, max_pages, n_layers, n_kv_heads, head_dim, code,
+                              pool.data_ptr(), table.data_ptr(), lens.data_ptr(), refs.data_ptr())
         self.ref = ctypes.byref(self.c)
         self.ws_bytes = {}  # wise_kv_workspace by list length
 
@@ -513,6 +552,36 @@ def wise_kv_write(cache: Cache, layer: int, slots, n_new, K, V, stream=None) -> 
         raise WiseError(rc, "wise_kv_write")
 
 
+def wise_kvq_write(cache: Cache, layer: int, slots, n_new, K, V, stream=None) -> None:
+    """wise_kv_write into a cache in 8 or 4 bits; K and V are of the cache's dtype."""
+    if K is None or K.dim() != 4:
+        raise ValueError("K must be [batch, n_kv_heads, q_len, head_dim]")
+    batch, _, q_len, _ = K.shape
+    shape = (batch, cache.n_kv_heads, q_len, cache.head_dim)
+    rc = load().wise_kvq_write(cache.ref, layer, _list32(slots, "slots", batch, cache),
+                               0 if n_new is None else _list32(n_new, "n_new", batch, cache), batch, q_len,
+                               cache.type_code, _rows16(K, "K", shape, cache), _rows16(V, "V", shape, cache),
+                               _raw_stream(stream, cache.index))
+    if rc != WISE_OK:
+        raise WiseError(rc, "wise_kvq_write")
+
+
+def wise_kv_read(cache: Cache, layer: int, K, V, slots, first=None, count=None, stream=None) -> None:
+    """Reads one layer's keys and values back into K and V [batch, n_kv_heads, rows, head_dim]: positions first[b] ..
+    of the sequences, count[b] of them (None: from 0, and `rows`); the other rows become 0."""
+    if K is None or K.dim() != 4:
+        raise ValueError("K must be [batch, n_kv_heads, rows, head_dim]")
+    batch, _, rows, _ = K.shape
+    shape = (batch, cache.n_kv_heads, rows, cache.head_dim)
+    rc = load().wise_kv_read(cache.ref, layer, _list32(slots, "slots", batch, cache),
+                             0 if first is None else _list32(first, "first", batch, cache),
+                             0 if count is None else _list32(count, "count", batch, cache), batch, rows,
+                             cache.type_code, _rows16(K, "K", shape, cache), _rows16(V, "V", shape, cache),
+                             _raw_stream(stream, cache.index))
+    if rc != WISE_OK:
+        raise WiseError(rc, "wise_kv_read")
+
+
 def wise_kv_drop(cache: Cache, slots, n_drop, stream=None) -> None:
     """Takes the last n_drop tokens off the sequences in slots (int32 [n] each); all of them frees a sequence."""
     n = slots.shape[0]
@@ -571,6 +640,39 @@ def wise_prefix_attn(cache: Cache, layer: int, Q, O, slots, n_new=None, group_st
                                  _rows16(O, "O", full, cache), ws, ws_bytes, _raw_stream(stream, cache.index))
     if rc != WISE_OK:
         raise WiseError(rc, "wise_prefix_attn")
+
+
+def wise_kvq_attn_workspace(cache: Cache, shape: wise_prefix_t) -> int:
+    """Bytes of workspace of wise_kvq_attn."""
+    return int(load().wise_kvq_attn_workspace(cache.ref, ctypes.byref(shape)))
+
+
+def wise_kvq_attn(cache: Cache, layer: int, Q, O, slots, n_new=None, group_start=None, prefix_lens=None,
+                  workspace=None, scale: float = 0.0, stream=None, shape=None) -> None:
+    """wise_prefix_attn over a cache in 8 or 4 bits; Q and O are of the cache's dtype."""
+    if Q is None or Q.dim() != 4:
+        raise ValueError("Q must be [batch, n_heads, q_len, head_dim]")
+    if shape is None:
+        shape = prefix_shape(cache, Q, 0 if prefix_lens is None else prefix_lens.shape[0], scale)
+    batch, full = shape.batch, Q.shape
+    if full[3] != cache.head_dim:
+        raise ValueError(f"Q must have the cache's head_dim {cache.head_dim}")
+    starts = lens = 0
+    if prefix_lens is not None:
+        lens = _list32(prefix_lens, "prefix_lens", shape.n_groups, cache)
+        starts = _list32(group_start, "group_start", shape.n_groups + 1, cache)
+    elif group_start is not None:
+        raise ValueError("group_start needs prefix_lens")
+    ws = ws_bytes = 0
+    if workspace is not None:
+        ws = _workspace(workspace, 0, cache)
+        ws_bytes = workspace.numel() * workspace.element_size()
+    rc = load().wise_kvq_attn(cache.ref, layer, ctypes.byref(shape), cache.type_code, _rows16(Q, "Q", full, cache),
+                              _list32(slots, "slots", batch, cache),
+                              0 if n_new is None else _list32(n_new, "n_new", batch, cache), starts, lens,
+                              _rows16(O, "O", full, cache), ws, ws_bytes, _raw_stream(stream, cache.index))
+    if rc != WISE_OK:
+        raise WiseError(rc, "wise_kvq_attn")
 
 
 def _on(t, name, shape, dtype, index):
