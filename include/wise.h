@@ -466,7 +466,10 @@ int wise_kv_read(const wise_cache_t* cache, int layer, const int32_t* slots, con
 
 /* wise_prefix_attn over a cache in 8 or 4 bits.  Q and O are of type dtype
  * (WISE_BF16 or WISE_FP16); rows, groups, workspace, limits and faults are as
- * there.  Rows at or past lens may hold anything here too. */
+ * there, but for two things: a shared prefix is read once for every floor(64 /
+ * R) requests of the group (R as there; by each request where that is 1 or 0),
+ * and with R above 64 the last limit is 2^29.  Rows at or past lens may hold
+ * anything here too. */
 size_t wise_kvq_attn_workspace(const wise_cache_t* cache, const wise_prefix_t* shape);
 
 int wise_kvq_attn(const wise_cache_t* cache, int layer, const wise_prefix_t* shape, int dtype, const void* Q,

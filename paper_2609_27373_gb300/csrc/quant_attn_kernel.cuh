@@ -1,0 +1,1235 @@
+// The attention kernel of quant_attn.cuh, one instance per head dimension,
+// number of bits and number of rows.
+//
+// Both products have the cache's side as operand A in tensor memory and the
+// query rows (16 to 64 of them) as N:
+//   S^T [128 keys x N] = K [keys x D] Q^T,    O^T [D x N] += V^T [D x keys] P^T.
+// So a few query rows cost few tensor cycles, and the codes go from shared
+// memory through registers right to where the product wants them: a thread
+// owns a row of K (a token) or of V^T (a channel), turns 16-byte pieces of
+// codes into fp16 pairs and stores those to its lane of tensor memory.
+//
+// Warp roles (480 threads):
+//   warps 0-3    softmax: S^T from tensor memory in fragments of 8 keys x 8
+//                rows, running maximum (raised only when a numerator passes
+//                2^15, which the four warps vote on), numerators as fp16 to
+//                shared memory (P, the B operand of the second product), O's
+//                rescaling and the end of a segment;
+//   warps 4-7    K: codes to tensor memory;
+//   warps 8-11   V: the same, scales of 8 tokens at a time;
+//   warp 12      producer: page look-ups, one bulk copy a page (codes and scales
+//                of keys and values lie together), the schedule;
+//   warp 13      Q: rows of the next segment to shared memory as fp16, scaled by a
+//                power of two so that the largest is next to 2^15 (exact down
+//                to 2^-28 of it), and how many keys each row sees;
+//   warp 14      one thread: the products.
+// TMEM columns: K 0 and 64, V 128 and 192, S 256 and 320, O 384.
+//
+// Every wait is bounded; one that runs out sets the status word and an abort
+// flag, and every role unwinds.
+#pragma once
+
+#include <float.h>
+
+#include "attn_common.cuh"
+#include "cache_common.cuh"
+#include "ptx.cuh"
+#include "quant.cuh"
+#include "quant_attn.cuh"
+
+namespace wise {
+
+template <int D, int BITS, int NMAX>
+struct QaCfg {
+  static constexpr int kThreads = 480;
+  static constexpr int kBoxes = (D + 63) / 64;
+  static constexpr int kBoxBytes = NMAX * 128;
+  static constexpr int kQBytes = kBoxes * kBoxBytes;
+  static constexpr int kPBytes = 2 * kBoxBytes;
+  static constexpr int kTileBytes = 128 / 16 * q_block_bytes(BITS, D, 16);  // the same for every page size
+  static constexpr int kMaxPlanBytes = 32 * 1024;
+  static constexpr int kFixed = 2 * kQBytes + 2 * kPBytes;
+  static constexpr int kRoom = (218 * 1024 - 1024 - kMaxPlanBytes - kFixed) / kTileBytes;
+  static constexpr int kStages = kRoom < 8 ? kRoom : 8;
+  static constexpr int kPlanAt = kFixed + kStages * kTileBytes;
+  static constexpr int kSmem = kPlanAt + kMaxPlanBytes + 1024;
+  static_assert(kStages >= 3 && kTileBytes % 128 == 0, "ring");
+};
+
+constexpr uint32_t kQaTmemK = 0, kQaTmemV = 128, kQaTmemS = 256, kQaTmemO = 384;
+constexpr int kQaSched = 16;
+constexpr int kQaFirst = 1, kQaLast = 2, kQaEnd = 4, kQaFaulty = 8;
+constexpr int kQaOwn = 0, kQaPrefix = 1;
+
+// Schedule entry of a tile, two int4: {flags | keys << 8 | rows << 16 | kind <<
+// 24, position of the first key, workspace slot or -1 (O itself), request},
+// {kv head, first row of the request, 0, 0}.  Entry t % 16 is written again for
+// tile t + 16 when the stage of tile t + 16 - NS, t + 8 or later, has been given
+// back by the V warps; they had to wait for P V of a tile two before that, and
+// with it for the softmax and the products to be past tile t.
+template <int NS>
+struct QaShared {
+  uint64_t full[NS], empty[NS];  // empty: 8 warps
+  uint64_t sched_full[kQaSched];
+  uint64_t k_ready[2], v_ready[2], p_ready[2];  // 4 warps
+  uint64_t s_full[2], s_free[2];                // products; 4 warps
+  uint64_t pv_done[2];
+  uint64_t q_ready[2], q_free[2];  // q_free: the products and 4 warps
+  uint64_t done;
+  int4 sched[kQaSched][2];
+  int lim[2][kQaRows];       // keys that a row sees, 0 for none
+  int min_lim[2];            // the least of those that see any
+  float q_scale[2];          // logits in base-2 units = S * q_scale
+  float warp_max[4][kQaRows];
+  float factor[kQaRows];
+  float sums[2][4][kQaRows];
+  float top[2][kQaRows];
+  int4 value_scales[4][32];  // a warp's two groups x 128 tokens as fp16
+  uint32_t tmem_base;
+  int abort, warp_ok[4];
+};
+
+// ---------------------------------------------------------------------- plan
+// All threads; `plan` in shared memory.
+__device__ inline void qa_make_plan(const QaParams& p, const QaPlan& plan, bool report) {
+  const CacheView& c = p.cache;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
+  int bad = 0, bad_groups = 0;
+#pragma unroll 1
+  for (int g = tid; g <= p.n_groups; g += blockDim.x) {
+    if (p.n_groups == 0) break;
+    const int a = p.group_start[g], e = g < p.n_groups ? p.group_start[g + 1] : a;
+    if (g < p.n_groups) plan.tiles[g] = p.prefix_lens[g];  // the declared length, until the tiles are known
+    if (a < 0 || a > p.batch || a > e) bad_groups = 1;
+    plan.start[g] = a;
+  }
+#pragma unroll 1
+  for (int r = tid; r < p.batch; r += blockDim.x) {
+    const int s = p.slots[r];
+    const int add = p.n_new ? p.n_new[r] : p.q_len;
+    int len = 0;
+    if (s >= 0) {
+      len = s < c.n_slots ? c.lens[s] : -1;
+      if (len < 0 || len > c.max_len || add < 0 || add > p.q_len) {
+        bad = 1;
+        len = 0;
+      }
+    }
+    plan.slot[r] = s;
+    plan.len[r] = add > 0 ? len : 0;
+    plan.add[r] = add > 0 ? add : 0;
+    plan.lo[r] = 0;
+    plan.group[r] = -1;
+  }
+  if (report && (bad | bad_groups)) atomicOr(c.status, kStatusBadCache);
+  const bool grouped = !__syncthreads_or(bad_groups) && p.per_tile > 0;
+#pragma unroll 1
+  for (int g = warp; g < p.n_groups; g += n_warps) {
+    const int a = plan.start[g], e = plan.start[g + 1];
+    int shortest = INT_MAX, active = 0, lead = INT_MAX;
+    if (grouped) {
+#pragma unroll 1
+      for (int r = a + lane; r < e; r += 32) {
+        const int len = plan.len[r];
+        if (len > 0) {
+          shortest = min(shortest, len);
+          lead = min(lead, r);
+          ++active;
+        }
+      }
+    }
+    shortest = __reduce_min_sync(0xffffffffu, shortest);
+    active = __reduce_add_sync(0xffffffffu, active);
+    lead = __reduce_min_sync(0xffffffffu, lead);
+    int shared = 0;
+    if (active > 1) shared = max(0, min(plan.tiles[g], shortest)) & -c.page;
+    __syncwarp();
+    if (lane == 0) {
+      const int tiles = (shared + kQaKeys - 1) / kQaKeys;
+      const int row_tiles = tiles > 0 ? (e - a + p.per_tile - 1) / p.per_tile : 0;
+      plan.tiles[g] = tiles;
+      plan.lead[g] = lead;
+      plan.row_tiles[g] = row_tiles;
+      plan.base[g] = row_tiles * tiles * c.n_kv_heads;
+      plan.item[g] = row_tiles;
+    }
+    if (shared > 0) {
+#pragma unroll 1
+      for (int r = a + lane; r < e; r += 32) {
+        plan.lo[r] = shared;
+        plan.group[r] = g;
+      }
+    }
+  }
+  __syncthreads();
+  // Prefix sums, a warp each: the groups' tiles and items, the requests' own tiles.
+  if (warp < 3) {
+    int* list = warp == 0 ? plan.base : warp == 1 ? plan.item : plan.cum;
+    const int n = warp < 2 ? p.n_groups : p.batch;
+    int before = 0;
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += 128) {
+      const int first = i0 + 4 * lane;
+      int x[4], sum = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x[k] = 0;
+        if (first + k < n)
+          x[k] = warp < 2 ? list[first + k]
+                          : max(0, plan.len[first + k] - plan.lo[first + k] + kQaKeys - 1) / kQaKeys;
+        sum += x[k];
+      }
+      int upto = sum;
+#pragma unroll 1
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += u;
+      }
+      int at = before + upto - sum;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (first + k < n) list[first + k] = at;
+        at += x[k];
+      }
+      before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (lane == 0) list[n] = before;
+  }
+  __syncthreads();
+  if (tid < 2) {
+    const PfxCuts cuts =
+        pfx_cuts(tid == 0 ? plan.cum[p.batch] * c.n_kv_heads * p.chunks : plan.base[p.n_groups], gridDim.x);
+    (tid == 0 ? plan.t->own : plan.t->pre) = cuts;
+  }
+  __syncthreads();
+}
+
+__device__ __forceinline__ int qa_find(const int* base, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (base[mid] <= x)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+struct QaSeg {
+  int kind, req, nreq, kvh;
+  int row0, rows;  // first row of the request (own), rows
+  int slot;        // of the workspace, -1: O itself
+  int seq;         // cache slot whose pages are read
+  int pos, end;    // position of the next tile's first key; one past the item's keys
+  int left;        // tiles left
+};
+
+__device__ __forceinline__ QaSeg qa_segment(const QaParams& p, const QaPlan& plan, int kind, int x, int x_end, int run) {
+  QaSeg s;
+  const int kv = p.cache.n_kv_heads;
+  int tiles, t;
+  s.kind = kind;
+  s.row0 = 0;
+  if (kind == kQaPrefix) {
+    const int g = qa_find(plan.base, p.n_groups, x);
+    tiles = plan.tiles[g];
+    const int y = x - plan.base[g], it = y / tiles, n = plan.row_tiles[g];
+    t = y - it * tiles;
+    // kv head outermost: the items of one kv head read the same keys at about the same time.
+    s.kvh = it / n;
+    const int tile = it - s.kvh * n;
+    s.req = plan.start[g] + tile * p.per_tile;
+    s.nreq = min(p.per_tile, plan.start[g + 1] - s.req);
+    s.rows = s.nreq * p.rows;
+    s.slot = plan.item[g] * kv + it + run;
+    const int lead = plan.lead[g];
+    s.seq = plan.slot[lead];
+    s.end = plan.lo[lead];
+    s.pos = t * kQaKeys;
+  } else {
+    const int per = kv * p.chunks;
+    s.req = qa_find(plan.cum, p.batch, x / per);  // cum[r] * per <= x < cum[r + 1] * per
+    s.nreq = 1;
+    tiles = plan.cum[s.req + 1] - plan.cum[s.req];
+    const int z = x - plan.cum[s.req] * per, unit = z / tiles;
+    t = z - unit * tiles;
+    s.kvh = unit / p.chunks;
+    s.row0 = (unit - s.kvh * p.chunks) * kQaRows;
+    s.rows = min(p.rows - s.row0, kQaRows);
+    s.slot = s.req * per + unit + run;
+    s.seq = plan.slot[s.req];
+    s.end = plan.len[s.req];
+    s.pos = plan.lo[s.req] + t * kQaKeys;
+    if (t == 0 && tiles <= x_end - x && plan.group[s.req] < 0) s.slot = -1;
+  }
+  s.left = min(tiles - t, x_end - x);
+  return s;
+}
+
+// Walks a CTA's segments: its run of own items, then its run of prefix items.
+// Runs of own items start at the CTA after the last one with prefix items, so
+// that small problems spread out.
+struct QaWalk {
+  int kind, run, x, x_end;
+  __device__ __forceinline__ void begin(const QaPlan& plan, int k) {
+    kind = k;
+    const PfxCuts c = k == kQaOwn ? plan.t->own : plan.t->pre;
+    run = blockIdx.x;
+    if (k == kQaOwn) {
+      run -= plan.t->pre.runs;
+      if (run < 0) run += gridDim.x;
+    }
+    x = x_end = 0;
+    if (run < c.runs) {
+      x = pfx_cut(c, run);
+      x_end = pfx_cut(c, run + 1);
+    }
+  }
+  __device__ __forceinline__ bool next(const QaParams& p, const QaPlan& plan, QaSeg& s) {
+    if (x == x_end && kind == kQaOwn) begin(plan, kQaPrefix);
+    if (x == x_end) return false;
+    s = qa_segment(p, plan, kind, x, x_end, run);
+    x += s.left;
+    return true;
+  }
+};
+
+static __device__ __noinline__ bool qa_wait_long(uint64_t* bar, uint32_t parity, volatile int* abort, uint64_t limit) {
+  return mbar_wait(bar, parity, abort, limit);
+}
+__device__ __forceinline__ bool qa_wait(uint64_t* bar, uint32_t parity, volatile int* abort, uint64_t limit) {
+  return mbar_try_wait(bar, parity) || qa_wait_long(bar, parity, abort, limit);
+}
+__device__ __forceinline__ bool qa_warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort, uint64_t limit) {
+  return __all_sync(0xffffffffu, qa_wait(bar, parity, abort, limit));
+}
+static __device__ __noinline__ void qa_give_up(int* abort, int* status) {
+  *reinterpret_cast<volatile int*>(abort) = 1;
+  atomicOr(status, kStatusTimeout);
+}
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                   smem_u32(dst)),
+               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+
+// ------------------------------------------------------------------ producer
+template <int D, int BITS, int NMAX>
+__device__ void qa_producer(const QaParams& p, const QaPlan& plan, uint8_t* ring,
+                            QaShared<QaCfg<D, BITS, NMAX>::kStages>& sb) {
+  using C = QaCfg<D, BITS, NMAX>;
+  constexpr int NS = C::kStages;
+  const CacheView& c = p.cache;
+  const int lane = threadIdx.x & 31;
+  volatile int* abort = &sb.abort;
+  const int block = c.head_bytes;
+  QaWalk walk;
+  walk.begin(plan, kQaOwn);
+  QaSeg seg;
+  int n = 0, bad = 0;
+  bool ok = true;
+  while (ok && walk.next(p, plan, seg)) {
+    int flags = kQaFirst;
+    auto look = [&](int pos) {
+      const int at = pos + (lane << c.page_shift);
+      return at - pos < kQaKeys && at < seg.end ? __ldg(c.table + (size_t)seg.seq * c.max_pages + (at >> c.page_shift))
+                                                : -1;
+    };
+    int page = look(seg.pos);
+    for (; seg.left > 0; --seg.left, seg.pos += kQaKeys, flags = 0) {
+      const int st = n % NS, at = lane << c.page_shift;
+      const bool on = at < kQaKeys && seg.pos + at < seg.end;
+      const bool valid = on && valid_page(c, page);
+      const uint32_t loads = __ballot_sync(0xffffffffu, valid);
+      if (__any_sync(0xffffffffu, on && !valid)) {
+        flags |= kQaFaulty;
+        bad = 1;
+      }
+      if (seg.left == 1) flags |= kQaLast;
+      if (n >= NS) ok = qa_warp_wait(&sb.empty[st], (n / NS - 1) & 1, abort, p.wait_ns);
+      if (!ok) break;
+      if (lane == 0) {
+        sb.sched[n % kQaSched][0] = make_int4(flags | min(kQaKeys, seg.end - seg.pos) << 8 | seg.rows << 16 | seg.kind << 24,
+                                              seg.pos, seg.slot, seg.req);
+        sb.sched[n % kQaSched][1] = make_int4(seg.kvh, seg.row0, 0, 0);
+        mbar_arrive(&sb.sched_full[n % kQaSched]);
+        mbar_arrive_expect_tx(&sb.full[st], __popc(loads) * block);
+      }
+      __syncwarp();
+      if (valid)
+        bulk_load(ring + st * C::kTileBytes + lane * block,
+                  p.plane + (size_t)page * c.page_bytes + (size_t)seg.kvh * block, block, &sb.full[st]);
+      ++n;
+      if (seg.left > 1) page = look(seg.pos + kQaKeys);
+    }
+  }
+  if (ok) {
+    const int st = n % NS;
+    if (n >= NS) ok = qa_warp_wait(&sb.empty[st], (n / NS - 1) & 1, abort, p.wait_ns);
+    if (ok && lane == 0) {
+      sb.sched[n % kQaSched][0] = make_int4(kQaEnd, 0, 0, 0);
+      mbar_arrive(&sb.sched_full[n % kQaSched]);
+      mbar_arrive(&sb.full[st]);
+    }
+  }
+  if (bad && lane == 0) atomicOr(c.status, kStatusBadCache);
+  if (lane == 0) {
+    if (!ok) qa_give_up(&sb.abort, c.status);
+    // Copies already issued land before the CTA's shared memory is released,
+    // whoever may have given up.  (The end took the stage of tile n - NS.)
+    int never = 0;
+    for (int k = max(0, ok ? n - NS + 1 : n - NS); k < n; ++k) mbar_wait(&sb.full[k % NS], (k / NS) & 1, &never);
+  }
+  __syncwarp();
+}
+
+// ------------------------------------------------------------------------- Q
+__device__ __forceinline__ float2 qa_widen(uint32_t v, bool fp16) {
+  if (fp16) return __half22float2(*reinterpret_cast<const __half2*>(&v));
+  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
+}
+__device__ __forceinline__ uint32_t qa_pack_half(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+template <int D, int BITS, int NMAX>
+__device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_tiles,
+                           QaShared<QaCfg<D, BITS, NMAX>::kStages>& sb) {
+  using C = QaCfg<D, BITS, NMAX>;
+  constexpr int kPieces = D / 8;  // of 16 bytes, of a row
+  const int lane = threadIdx.x & 31;
+  volatile int* abort = &sb.abort;
+  QaWalk walk;
+  walk.begin(plan, kQaOwn);
+  QaSeg seg;
+  bool ok = true;
+  for (int k = 0; walk.next(p, plan, seg); ++k) {
+    const int buf = k & 1;
+    if (k >= 2) ok = qa_warp_wait(&sb.q_free[buf], ((k >> 1) - 1) & 1, abort, p.wait_ns);
+    if (!ok) break;
+    // Rows of one request are contiguous: Q is [batch][n_kv_heads][rows][D].
+    const uint4* Q = reinterpret_cast<const uint4*>(p.Q) +
+                     (((size_t)seg.req * p.cache.n_kv_heads + seg.kvh) * p.rows + seg.row0) * kPieces;
+    const size_t next_req = (size_t)p.cache.n_kv_heads * p.rows * kPieces;
+    const int pieces = seg.rows * kPieces;
+    auto load = [&](int i) {
+      const int n = i / kPieces;
+      if (seg.kind == kQaOwn) return __ldg(Q + i);
+      const int r = n / p.rows;
+      return __ldg(Q + r * next_req + (i - r * p.rows * kPieces));
+    };
+    int least = INT_MAX;
+    for (int n = lane; n < seg.rows; n += 32) {
+      const int r = n / p.rows, row = seg.row0 + n - r * p.rows;  // (own items: r = 0)
+      const int i = row % p.q_len, req = seg.req + r;
+      int lim = 0;
+      if (i < plan.add[req]) lim = max(min(plan.len[req] - plan.add[req] + i + 1, seg.end), 0);
+      sb.lim[buf][n] = lim;
+      if (lim > 0) least = min(least, lim);
+    }
+    least = __reduce_min_sync(0xffffffffu, least);
+    uint32_t top = 0;
+    if (!p.fp16) {
+#pragma unroll 4
+      for (int i = lane; i < pieces; i += 32) {
+        const uint4 v = load(i);
+        top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu),
+                                     __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
+      }
+      top = __reduce_max_sync(0xffffffffu, max(top & 0xFFFFu, top >> 16));
+    }
+    // bf16: the largest size has exponent field E, and times 2^(141 - E) lies in [2^14, 2^15).
+    const int shift = p.fp16 || top == 0 ? 0 : min(141 - (int)(top >> 7), 126);
+    const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
+    if (lane == 0) {
+      sb.min_lim[buf] = least;
+      sb.q_scale[buf] = fmaxf(p.scale_log2 * __uint_as_float((uint32_t)(127 - shift) << 23), FLT_MIN);
+    }
+    uint8_t* tile = q_tiles + buf * C::kQBytes;
+    const int all = ((seg.rows + 15) & ~15) * kPieces;  // rows up to the product's N are 0
+#pragma unroll 4
+    for (int i = lane; i < all; i += 32) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (i < pieces) v = load(i);
+      if (!p.fp16) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 f = qa_widen(w[j], false);
+          w[j] = qa_pack_half(f.x * up, f.y * up);
+        }
+      }
+      const int n = i / kPieces, piece = i - n * kPieces;
+      *reinterpret_cast<uint4*>(tile + (piece >> 3) * C::kBoxBytes + n * 128 + (((piece & 7) ^ (n & 7)) << 4)) = v;
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.q_ready[buf]);
+  }
+  if (!ok && lane == 0) qa_give_up(&sb.abort, p.cache.status);
+  __syncwarp();
+}
+
+// ------------------------------------------------------------------ products
+// One thread.  S of tile t is issued before P V of tile t - 1.
+template <int D, int BITS, int NMAX>
+__device__ void qa_products(const QaParams& p, uint32_t tmem, uint8_t* q_tiles, uint8_t* p_tiles,
+                            QaShared<QaCfg<D, BITS, NMAX>::kStages>& sb) {
+  using C = QaCfg<D, BITS, NMAX>;
+  // fp16 operands, fp32 sums.
+  constexpr uint32_t base = idesc_bf16_f32(128, 0, false, false) & ~((1u << 7) | (1u << 10));
+  volatile int* abort = &sb.abort;
+  const uint64_t desc_hi = smem_desc_sw128(0, 16, 1024);
+  const uint32_t hi = (uint32_t)(desc_hi >> 32), lo0 = (uint32_t)desc_hi;
+  int seg = -1, info = 0, before = 0;
+  bool ok = true;
+  for (int t = 0;; ++t) {
+    if (!(ok = qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, abort, p.wait_ns))) break;
+    info = sb.sched[t % kQaSched][0].x;
+    if (!(info & kQaEnd)) {
+      const int b = t & 1;
+      if (info & kQaFirst) {
+        ++seg;
+        if (!(ok = qa_wait(&sb.q_ready[seg & 1], (seg >> 1) & 1, abort, p.wait_ns))) break;
+      }
+      if (!(ok = qa_wait(&sb.k_ready[b], (t >> 1) & 1, abort, p.wait_ns) &&
+                 (t < 2 || qa_wait(&sb.s_free[b], ((t >> 1) - 1) & 1, abort, p.wait_ns))))
+        break;
+      tc_fence_after_sync();
+      const uint32_t n16 = (((info >> 16) & 255) + 15) >> 4;
+      const uint32_t idesc = base | n16 << 18;  // N / 8 at bit 17
+      const uint32_t q0 = lo0 | (smem_u32(q_tiles + (seg & 1) * C::kQBytes) >> 4);
+      uint32_t acc = 0;
+#pragma unroll 2
+      for (int kk = 0; kk < D / 16; ++kk) {
+        umma_ts_split(tmem + kQaTmemS + 64 * b, tmem + kQaTmemK + 64 * b + 8 * kk,
+                      q0 + (((kk >> 2) * C::kBoxBytes + (kk & 3) * 32) >> 4), hi, idesc, acc);
+        acc = 1;
+      }
+      umma_commit(&sb.s_full[b]);
+      if (info & kQaLast) umma_commit(&sb.q_free[seg & 1]);
+    }
+    if (t > 0) {
+      const int u = t - 1, b = u & 1;
+      if (!(ok = qa_wait(&sb.v_ready[b], (u >> 1) & 1, abort, p.wait_ns) &&
+                 qa_wait(&sb.p_ready[b], (u >> 1) & 1, abort, p.wait_ns)))
+        break;
+      tc_fence_after_sync();
+      const uint32_t n16 = (((before >> 16) & 255) + 15) >> 4;
+      const uint32_t idesc = base | n16 << 18;
+      const uint32_t p0 = lo0 | (smem_u32(p_tiles + b * C::kPBytes) >> 4);
+      uint32_t acc = before & kQaFirst ? 0 : 1;
+#pragma unroll 2
+      for (int kk = 0; kk < 8; ++kk) {
+        umma_ts_split(tmem + kQaTmemO, tmem + kQaTmemV + 64 * b + 8 * kk,
+                      p0 + (((kk >> 2) * C::kBoxBytes + (kk & 3) * 32) >> 4), hi, idesc, acc);
+        acc = 1;
+      }
+      umma_commit(&sb.pv_done[b]);
+    }
+    if (info & kQaEnd) break;
+    before = info;
+  }
+  if (!ok) qa_give_up(&sb.abort, p.cache.status);
+  // All products end before tensor memory is given back.
+  int never = 0;
+  umma_commit(&sb.done);
+  mbar_wait(&sb.done, 0, &never);
+}
+
+// ------------------------------------------------------------ K and V to TMEM
+// Word of codes -> fp16 pairs times a scale pair each.
+template <int BITS>
+struct QaDecode;
+template <>
+struct QaDecode<4> {
+  static constexpr int kPairs = 4;  // of a word
+  __device__ static __forceinline__ void pairs(uint32_t w, uint32_t (&h)[4]) { q_decode4(w, h); }
+};
+template <>
+struct QaDecode<8> {
+  static constexpr int kPairs = 2;
+  __device__ static __forceinline__ void pairs(uint32_t w, uint32_t (&h)[2]) { q_decode8(w, h); }
+};
+
+template <int N>
+__device__ __forceinline__ void qa_tmem_store(uint32_t at, const uint32_t (&r)[N]) {
+  if constexpr (N == 32)
+    tmem_st_32x32b_x32(at, r);
+  else
+    tmem_st_32x32b_x16(at, r);
+}
+
+// Keys: this thread's token.  Values d0 .. d0 + 2 * COLS - 1 to COLS columns.
+template <int D, int BITS, int COLS>
+__device__ __forceinline__ void qa_key_columns(const uint8_t* data, int page, const uint8_t* scales, int d0, uint32_t at) {
+  uint32_t r[COLS];
+  constexpr int kPer = 128 / BITS;  // values of 16 bytes
+#pragma unroll
+  for (int v = 0; v < 2 * COLS; v += kPer) {
+    const uint4 x = *reinterpret_cast<const uint4*>(data + (d0 + v) / kPer * page * 16);
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t byte = scales[(d0 + v + k * kPer / 4) / 16];
+      const uint32_t s = byte << 7 | byte << 23;
+      uint32_t h[QaDecode<BITS>::kPairs];
+      QaDecode<BITS>::pairs(w[k], h);
+#pragma unroll
+      for (int j = 0; j < QaDecode<BITS>::kPairs; ++j) r[v / 2 + k * (kPer / 8) + j] = q_mul2(h[j], s);
+    }
+  }
+  qa_tmem_store<COLS>(at, r);
+}
+
+template <int D, int BITS, int NMAX>
+__device__ void qa_keys(const QaParams& p, uint32_t tmem, uint8_t* ring, QaShared<QaCfg<D, BITS, NMAX>::kStages>& sb) {
+  using C = QaCfg<D, BITS, NMAX>;
+  constexpr int NS = C::kStages;
+  const CacheView& c = p.cache;
+  const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
+  volatile int* abort = &sb.abort;
+  const int token = 32 * quarter + lane, off = token & (c.page - 1);
+  const int block_at = (token >> c.page_shift) * c.head_bytes;
+  const int data_at = block_at + off * 16;
+  const int scales_at = block_at + q_key_scales_at(BITS, D, c.page) + off * q_key_scale_bytes(D);
+  const uint32_t to = tmem + ((uint32_t)(32 * quarter) << 16) + kQaTmemK;
+  bool ok = true;
+  for (int t = 0;; ++t) {
+    const int st = t % NS, b = t & 1;
+    if (!(ok = qa_warp_wait(&sb.full[st], (t / NS) & 1, abort, p.wait_ns))) break;
+    if (sb.sched[t % kQaSched][0].x & kQaEnd) break;
+    if (t >= 2 && !(ok = qa_warp_wait(&sb.s_full[b], ((t >> 1) - 1) & 1, abort, p.wait_ns))) break;
+    tc_fence_after_sync();
+    const uint8_t* stage = ring + st * C::kTileBytes;
+    uint8_t scales[8];
+    if constexpr (D == 64)
+      *reinterpret_cast<uint32_t*>(scales) = *reinterpret_cast<const uint32_t*>(stage + scales_at);
+    else
+      *reinterpret_cast<uint2*>(scales) = *reinterpret_cast<const uint2*>(stage + scales_at);
+    const uint8_t* data = stage + data_at;
+    qa_key_columns<D, BITS, 32>(data, c.page, scales, 0, to + 64 * b);
+    if constexpr (D == 128) qa_key_columns<D, BITS, 32>(data, c.page, scales, 64, to + 64 * b + 32);
+    if constexpr (D == 96) qa_key_columns<D, BITS, 16>(data, c.page, scales, 64, to + 64 * b + 32);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.empty[st]);
+    tmem_st_wait();
+    tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.k_ready[b]);
+  }
+  if (!ok && lane == 0) qa_give_up(&sb.abort, c.status);
+  __syncwarp();
+}
+
+template <int D, int BITS, int NMAX>
+__device__ void qa_values(const QaParams& p, uint32_t tmem, uint8_t* ring, QaShared<QaCfg<D, BITS, NMAX>::kStages>& sb) {
+  using C = QaCfg<D, BITS, NMAX>;
+  constexpr int NS = C::kStages;
+  const CacheView& c = p.cache;
+  const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
+  volatile int* abort = &sb.abort;
+  const bool on = 32 * quarter < D;
+  const int channel = 32 * quarter + lane;
+  const int T = q_value_tokens(BITS, c.page), piece = T * BITS / 8;  // tokens and bytes of a piece
+  const int values_at = q_values_at(BITS, D, c.page) + channel * piece;
+  // Scales: this lane turns those of 8 tokens of one of the warp's two groups into fp16.
+  const int stoken = 8 * (lane & 15);
+  const int scales_at = (stoken >> c.page_shift) * c.head_bytes + q_value_scales_at(BITS, D, c.page) +
+                        (2 * quarter + (lane >> 4)) * c.page + (stoken & (c.page - 1));
+  const int4* scales = &sb.value_scales[quarter][lane & 16];
+  const uint32_t to = tmem + ((uint32_t)(32 * quarter) << 16) + kQaTmemV;
+  bool ok = true;
+  for (int t = 0;; ++t) {
+    const int st = t % NS, b = t & 1;
+    if (!(ok = qa_warp_wait(&sb.full[st], (t / NS) & 1, abort, p.wait_ns))) break;
+    const int info = sb.sched[t % kQaSched][0].x;
+    if (info & kQaEnd) break;
+    if (t >= 2 && !(ok = qa_warp_wait(&sb.pv_done[b], ((t >> 1) - 1) & 1, abort, p.wait_ns))) break;
+    tc_fence_after_sync();
+    if (on) {
+      const int keys = (info >> 8) & 255;
+      const uint8_t* stage = ring + st * C::kTileBytes;
+      const uint2 bytes = *reinterpret_cast<const uint2*>(stage + scales_at);
+      uint32_t s[4];
+      s[0] = __byte_perm(bytes.x, 0, 0x1404) >> 1;  // bytes 0 and 1, each shifted by 7 in its half
+      s[1] = __byte_perm(bytes.x, 0, 0x3424) >> 1;
+      s[2] = __byte_perm(bytes.y, 0, 0x1404) >> 1;
+      s[3] = __byte_perm(bytes.y, 0, 0x3424) >> 1;
+      if (stoken + 8 > keys) {  // tokens past the end count 0 whatever is stored there
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (stoken + 2 * k >= keys) s[k] = 0;
+          if (stoken + 2 * k + 1 >= keys) s[k] &= 0xFFFFu;
+        }
+      }
+      sb.value_scales[quarter][lane] = *reinterpret_cast<const int4*>(s);
+      __syncwarp();
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {  // 64 tokens, 32 columns
+        uint32_t r[32];
+#pragma unroll
+        for (int u = 0; u < 64; u += 16) {  // 16 tokens: 8 or 16 bytes of codes
+          const int token = 64 * half + u;
+          const int off = token & (c.page - 1);
+          const uint8_t* from =
+              stage + (token >> c.page_shift) * c.head_bytes + values_at + off / T * (D * piece) + off % T * BITS / 8;
+          uint32_t w[BITS / 2];
+          if constexpr (BITS == 4)
+            *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(from);
+          else
+            *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(from);
+          if (BITS == 8 && token + 16 > keys) {  // a code may be NaN there
+#pragma unroll
+            for (int k = 0; k < BITS / 2; ++k) {
+              const int n = min(max(keys - token - 4 * k, 0), 4);
+              w[k] = n == 4 ? w[k] : w[k] & ((1u << 8 * n) - 1u);
+            }
+          }
+          const int4 sa = scales[token / 8], sc = scales[token / 8 + 1];
+          const int f[8] = {sa.x, sa.y, sa.z, sa.w, sc.x, sc.y, sc.z, sc.w};
+#pragma unroll
+          for (int k = 0; k < BITS / 2; ++k) {
+            constexpr int kPairs = QaDecode<BITS>::kPairs;
+            uint32_t h[kPairs];
+            QaDecode<BITS>::pairs(w[k], h);
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) r[u / 2 + k * kPairs + j] = q_mul2(h[j], (uint32_t)f[k * kPairs + j]);
+          }
+        }
+        tmem_st_32x32b_x32(to + 64 * b + 32 * half, r);
+      }
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.empty[st]);
+    tmem_st_wait();
+    tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.v_ready[b]);
+  }
+  if (!ok && lane == 0) qa_give_up(&sb.abort, c.status);
+  __syncwarp();
+}
+
+// ------------------------------------------------------------------- softmax
+// 16 lanes x 8 columns a time: thread i holds row i / 4 (and that + 8, in the
+// other two), columns 2 (i % 4) and the next.
+template <int G>
+__device__ __forceinline__ void qa_load_fragments(uint32_t at, float (&s)[G][4]) {
+  if constexpr (G == 8) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(at));
+    tmem_ld_wait(r);
+#pragma unroll
+    for (int k = 0; k < 32; ++k) s[k / 4][k % 4] = __uint_as_float(r[k]);
+  } else {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(at));
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
+                 :
+                 : "memory");
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s[k / 4][k % 4] = __uint_as_float(r[k]);
+  }
+}
+
+__device__ __forceinline__ bool qa_vote(bool x) {  // of the 128 softmax threads
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, 1, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"((uint32_t)x)
+      : "memory");
+  return any != 0;
+}
+
+template <int D, int BITS, int NMAX>
+__device__ void qa_softmax(const QaParams& p, uint32_t tmem, uint8_t* p_tiles,
+                           QaShared<QaCfg<D, BITS, NMAX>::kStages>& sb) {
+  using C = QaCfg<D, BITS, NMAX>;
+  constexpr int G = NMAX / 8;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int key0 = 32 * w + lane / 4, col0 = 2 * (lane & 3);
+  volatile int* abort = &sb.abort;
+  const uint32_t lane_tmem = tmem + ((uint32_t)(32 * w) << 16);
+  // P: row n of 128 bytes in box (key / 64), 16-byte chunk ((key % 64) / 8) ^
+  // (n & 7); this lane gives the address of row lane & 7 of matrix lane >> 3.
+  const uint32_t p_at = smem_u32(p_tiles) + (w >> 1) * C::kBoxBytes + (lane & 7) * 128 +
+                        ((((w & 1) * 4 + (lane >> 3)) ^ (lane & 7)) << 4);
+  float shift[G][2], sum[G][2];  // added to the logits: 7 minus the reference, infinite where there is none yet
+  float scale = 1.0f;
+  int seg = -1, min_lim = 0;
+  bool ok = true, faulty = false, pending = false;
+  int4 e0 = make_int4(0, 0, 0, 0), e1 = e0, o0 = e0, o1 = e0;
+#pragma unroll
+  for (int g = 0; g < G; ++g) shift[g][0] = shift[g][1] = sum[g][0] = sum[g][1] = 0.0f;
+  // A wait that ran out: everybody is told, and the next vote ends all four warps.
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    if (qa_warp_wait(bar, parity, abort, p.wait_ns)) return true;
+    if (lane == 0) qa_give_up(&sb.abort, p.cache.status);
+    return false;
+  };
+  for (int t = 0;; ++t) {
+    const int b = t & 1;
+    ok = ok && wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1);
+    if (ok) {
+      e0 = sb.sched[t % kQaSched][0];
+      e1 = sb.sched[t % kQaSched][1];
+    }
+    const int flags = e0.x & 255, rows = (e0.x >> 16) & 255;
+    const bool end = flags & kQaEnd, first = flags & kQaFirst;
+    float s[2][G][4];
+    bool raise = false;
+    uint32_t dead = 0;  // of the rows of this thread's columns, those that see nothing anywhere
+    if (ok && !end) {
+      if (first) {
+        ++seg;
+        faulty = false;
+        ok = wait(&sb.q_ready[seg & 1], (seg >> 1) & 1);
+        scale = sb.q_scale[seg & 1];
+        min_lim = sb.min_lim[seg & 1];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          shift[g][0] = shift[g][1] = INFINITY;
+          sum[g][0] = sum[g][1] = 0.0f;
+        }
+      }
+      if (flags & kQaFaulty) faulty = true;
+      ok = ok && wait(&sb.s_full[b], (t >> 1) & 1);
+    }
+    if (ok && !end) {
+      tc_fence_after_sync();
+      qa_load_fragments<G>(lane_tmem + kQaTmemS + 64 * b, s[0]);
+      qa_load_fragments<G>(lane_tmem + (16u << 16) + kQaTmemS + 64 * b, s[1]);
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sb.s_free[b]);
+      if (e0.y + kQaKeys > min_lim) {  // keys that a row does not see count nothing, whatever S is
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          if (8 * g >= rows) break;
+          const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][8 * g + col0]);
+          const int a = lim.x - e0.y - key0, c = lim.y - e0.y - key0;
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            float* x = s[h >> 1][g] + 2 * (h & 1);
+            if (8 * h >= a) x[0] = -INFINITY;
+            if (8 * h >= c) x[1] = -INFINITY;
+          }
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        if (8 * g >= rows) break;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const float m = fmaxf(fmaxf(s[0][g][c], s[0][g][2 + c]), fmaxf(s[1][g][c], s[1][g][2 + c]));
+          raise |= fmaf(m, scale, shift[g][c]) > 15.0f;
+        }
+      }
+      if (flags & kQaLast) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          if (8 * g >= rows) break;
+          const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][8 * g + col0]);
+          dead |= (uint32_t)(lim.x <= 0) << (2 * g) | (uint32_t)(lim.y <= 0) << (2 * g + 1);
+        }
+        __syncwarp();  // the limits have been read
+        if (lane == 0) mbar_arrive(&sb.q_free[seg & 1]);
+      }
+    }
+    const bool raised = qa_vote(raise || !ok);
+    if (raised) {
+      // New references: the largest logits of the 128 keys.
+      if (ok && !end) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          if (8 * g >= rows) break;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float m = fmaxf(fmaxf(s[0][g][c], s[0][g][2 + c]), fmaxf(s[1][g][c], s[1][g][2 + c]));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+            if (lane < 4) sb.warp_max[w][8 * g + col0 + c] = m;
+          }
+        }
+      }
+      if (lane == 0) sb.warp_ok[w] = ok;
+      named_barrier_sync(2, 128);
+      if (!(sb.warp_ok[0] && sb.warp_ok[1] && sb.warp_ok[2] && sb.warp_ok[3])) return;
+      // All four warps have a tile here: one that has seen the end votes for nothing.
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        if (8 * g >= rows) break;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int n = 8 * g + col0 + c;
+          const float m =
+              fmaxf(fmaxf(sb.warp_max[0][n], sb.warp_max[1][n]), fmaxf(sb.warp_max[2][n], sb.warp_max[3][n]));
+          const float moved = fminf(shift[g][c], 7.0f - m * scale);
+          // 0 where there was no reference yet, 1 where there still is none.
+          const float f = moved == INFINITY ? 1.0f : ex2_approx(moved - shift[g][c]);
+          shift[g][c] = moved;
+          sum[g][c] *= f;
+          if (w == 0 && lane < 4) sb.factor[n] = f;
+        }
+      }
+      named_barrier_sync(2, 128);
+    }
+    // The end of the segment before this tile.
+    if (pending) {
+      pending = false;
+      const int u = t - 1;
+      if (!(ok = wait(&sb.pv_done[u & 1], (u >> 1) & 1))) continue;
+      tc_fence_after_sync();
+      const int n_rows = (o0.x >> 16) & 255, kind = (o0.x >> 24) & 1, which = o1.z;
+      const bool direct = o0.z < 0, o_faulty = o1.w;
+      constexpr int kParts = (NMAX + 31) / 32;
+      float l[kParts];
+      const int slot_rows = kind == kQaPrefix ? kQaRows : min(p.rows, kQaRows);
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) {
+        const int n = min(32 * k + lane, NMAX - 1);
+        l[k] = sb.sums[which][0][n] + sb.sums[which][1][n] + sb.sums[which][2][n] + sb.sums[which][3][n];
+        const float top = sb.top[which][n];
+        if (!direct && w == 0 && 32 * k + lane < n_rows)
+          p.work.ml[kind][(size_t)o0.z * slot_rows + 32 * k + lane] =
+              o_faulty ? make_float2(0.0f, NAN) : make_float2(top, l[k]);
+        l[k] = l[k] > 0.0f && !o_faulty && top > -INFINITY ? 1.0f / l[k] : 0.0f;
+      }
+      if (32 * w < D) {
+        const int d = 32 * w + lane;
+        float* part = p.work.O[kind] + (size_t)(direct ? 0 : o0.z) * slot_rows * D + d;
+        uint16_t* out = reinterpret_cast<uint16_t*>(p.O) +
+                        (((size_t)o0.w * p.cache.n_kv_heads + o1.x) * p.rows + o1.y) * D + d;
+#pragma unroll 1
+        for (int c = 0; 16 * c < n_rows; ++c) {
+          uint32_t v[16];
+          tmem_ld_32x32b_x16(lane_tmem + kQaTmemO + 16 * c, v);
+          tmem_ld_wait(v);
+          const float lc = kParts == 1 ? l[0] : c < 2 ? l[0] : l[kParts - 1];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const int n = 16 * c + k;
+            const float inv = __shfl_sync(0xffffffffu, lc, n & 31);
+            if (n >= n_rows) break;
+            if (direct) {
+              const float x = inv == 0.0f ? 0.0f : __uint_as_float(v[k]) * inv;
+              out[n * D] = p.fp16 ? __half_as_ushort(__float2half_rn(x)) : __bfloat16_as_ushort(__float2bfloat16_rn(x));
+            } else {
+              part[n * D] = __uint_as_float(v[k]);
+            }
+          }
+        }
+      }
+      tc_fence_before_sync();
+    }
+    if (end) return;
+    if (raised && !first) {  // O in units of the new references
+      const int u = t - 1;
+      if (!(ok = wait(&sb.pv_done[u & 1], (u >> 1) & 1))) continue;
+      tc_fence_after_sync();
+      if (32 * w < D) {
+#pragma unroll 1
+        for (int c = 0; 16 * c < rows; ++c) {
+          uint32_t v[16];
+          tmem_ld_32x32b_x16(lane_tmem + kQaTmemO + 16 * c, v);
+          tmem_ld_wait(v);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * sb.factor[16 * c + k]);
+          tmem_st_32x32b_x16(lane_tmem + kQaTmemO + 16 * c, v);
+        }
+        tmem_st_wait();
+      }
+      tc_fence_before_sync();
+    }
+    if (t >= 2 && !(ok = wait(&sb.pv_done[b], ((t >> 1) - 1) & 1))) continue;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      if (8 * g >= rows) break;
+      const float sh0 = shift[g][0] == INFINITY ? 0.0f : shift[g][0], sh1 = shift[g][1] == INFINITY ? 0.0f : shift[g][1];
+      uint32_t pk[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const float* x = s[h >> 1][g] + 2 * (h & 1);
+        const float a = ex2_approx(fmaf(x[0], scale, sh0)), c = ex2_approx(fmaf(x[1], scale, sh1));
+        sum[g][0] += a;
+        sum[g][1] += c;
+        pk[h] = qa_pack_half(a, c);
+      }
+      asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(p_at + b * C::kPBytes +
+                                                                                               g * 1024),
+                   "r"(pk[0]), "r"(pk[1]), "r"(pk[2]), "r"(pk[3])
+                   : "memory");
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.p_ready[b]);
+    if (flags & kQaLast) {
+      pending = true;
+      o0 = e0;
+      o1 = make_int4(e1.x, e1.y, seg & 1, faulty);
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        if (8 * g >= rows) break;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float x = sum[g][c];
+          x += __shfl_xor_sync(0xffffffffu, x, 4);
+          x += __shfl_xor_sync(0xffffffffu, x, 8);
+          x += __shfl_xor_sync(0xffffffffu, x, 16);
+          const int n = 8 * g + col0 + c;
+          if (lane < 4) sb.sums[seg & 1][w][n] = x;
+          if (w == 0 && lane < 4) sb.top[seg & 1][n] = (dead >> (2 * g + c)) & 1 ? -INFINITY : -shift[g][c];
+        }
+      }
+    }
+  }
+}
+
+// Where the partial results of a unit (request, kv head and row chunk) lie, as
+// two int4: {n, n_pre, row of the prefix items, 0}, {first prefix slot, first
+// own slot, 0, 0}; n is -1 where O has been written, 0 where nothing is seen.
+__device__ __forceinline__ void qa_sources(const QaParams& p, const QaPlan& plan, int unit, int4* out) {
+  const int kv = p.cache.n_kv_heads, per = kv * p.chunks;
+  const int req = unit / per, rest = unit - req * per, kvh = rest / p.chunks;
+  const int g = plan.group[req], tiles = plan.cum[req + 1] - plan.cum[req];
+  int n_pre = 0, n_own = 0, row0 = 0, pre_slot = 0, own_slot = 0;
+  if (plan.len[req] > 0) {
+    if (g >= 0) {
+      const int at = req - plan.start[g], tile = at / p.per_tile;
+      row0 = (at - tile * p.per_tile) * p.rows;
+      const int it = kvh * plan.row_tiles[g] + tile, x = plan.base[g] + it * plan.tiles[g];
+      const int k0 = pfx_run_of(plan.t->pre, x);
+      n_pre = pfx_run_of(plan.t->pre, x + plan.tiles[g] - 1) - k0 + 1;
+      pre_slot = plan.item[g] * kv + it + k0;
+    }
+    if (tiles > 0) {
+      const int x = plan.cum[req] * per + rest * tiles;
+      const int k0 = pfx_run_of(plan.t->own, x);
+      n_own = pfx_run_of(plan.t->own, x + tiles - 1) - k0 + 1;
+      own_slot = unit + k0;
+    }
+  }
+  out[0] = make_int4(g < 0 && n_own == 1 ? -1 : n_pre + n_own, n_pre, row0, 0);
+  out[1] = make_int4(pre_slot, own_slot, 0, 0);
+}
+
+// -------------------------------------------------------------------- kernel
+template <int D, int BITS, int NMAX>
+__global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
+    quant_attn_kernel(const __grid_constant__ QaParams p) {
+  using C = QaCfg<D, BITS, NMAX>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* q_tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* p_tiles = q_tiles + 2 * C::kQBytes;
+  uint8_t* ring = q_tiles + C::kFixed;
+  const QaPlan plan = qa_plan(reinterpret_cast<int*>(q_tiles + C::kPlanAt), p.batch, p.n_groups);
+  __shared__ QaShared<C::kStages> sb;
+  static_assert(C::kSmem + sizeof(sb) <= 227 * 1024, "shared memory");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    sb.abort = 0;
+    for (int i = 0; i < C::kStages; ++i) {
+      mbar_init(&sb.full[i], 1);
+      mbar_init(&sb.empty[i], 8);
+    }
+    for (int i = 0; i < kQaSched; ++i) mbar_init(&sb.sched_full[i], 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sb.k_ready[i], 4);
+      mbar_init(&sb.v_ready[i], 4);
+      mbar_init(&sb.p_ready[i], 4);
+      mbar_init(&sb.s_full[i], 1);
+      mbar_init(&sb.s_free[i], 4);
+      mbar_init(&sb.pv_done[i], 1);
+      mbar_init(&sb.q_ready[i], 1);
+      mbar_init(&sb.q_free[i], 5);
+    }
+    mbar_init(&sb.done, 1);
+    fence_mbar_init();
+  }
+  if (warp == 14) {
+    tmem_alloc(&sb.tmem_base, 512);
+    tmem_relinquish();
+  }
+  // Everything above may overlap the previous kernel of the stream.
+  griddep_wait();
+  tc_fence_before_sync();
+  qa_make_plan(p, plan, blockIdx.x == 0);  // ends with a barrier
+  tc_fence_after_sync();
+  const uint32_t tmem = sb.tmem_base;
+  if (threadIdx.x == 0) griddep_launch_dependents();  // the merge waits for this grid's end
+
+  if (warp < 4) {
+    qa_softmax<D, BITS, NMAX>(p, tmem, p_tiles, sb);
+  } else if (warp < 8) {
+    qa_keys<D, BITS, NMAX>(p, tmem, ring, sb);
+  } else if (warp < 12) {
+    qa_values<D, BITS, NMAX>(p, tmem, ring, sb);
+  } else if (warp == 12) {
+    qa_producer<D, BITS, NMAX>(p, plan, ring, sb);
+  } else if (warp == 13) {
+    qa_queries<D, BITS, NMAX>(p, plan, q_tiles, sb);
+    // Where the merge finds its parts.
+    const int units = p.batch * p.cache.n_kv_heads * p.chunks;
+    for (int i = blockIdx.x * 32 + lane; i < units; i += gridDim.x * 32)
+      qa_sources(p, plan, i, p.work.sources + 2 * (size_t)i);
+  } else if (lane == 0) {
+    qa_products<D, BITS, NMAX>(p, tmem, q_tiles, p_tiles, sb);
+  }
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 14) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// --------------------------------------------------------------------- merge
+// Joins the partial results of one unit; blockIdx.y takes a share of its rows.
+// A thread owns 4 columns of a row and every parts-th of its parts.
+constexpr int kQaMergeThreads = 128;
+
+struct QaMergeShape {
+  int rows, parts;  // rows of a block, threads that share an element
+};
+
+template <int D>
+__global__ void __launch_bounds__(kQaMergeThreads) quant_merge_kernel(const QaParams p, const QaMergeShape sh) {
+  extern __shared__ float2 stats[];
+  __shared__ float4 sums[kQaMergeThreads];
+  __shared__ float part_l[kQaMergeThreads];
+  constexpr int kCols = D / 4;
+  griddep_launch_dependents();  // what follows waits for this grid's end
+  griddep_wait();
+  const int unit = blockIdx.x, tid = threadIdx.x;
+  const int4 s0 = p.work.sources[2 * (size_t)unit], s1 = p.work.sources[2 * (size_t)unit + 1];
+  const int n = s0.x, n_pre = s0.y;
+  if (n < 0) return;
+  const int chunk = unit % p.chunks, first = blockIdx.y * sh.rows;
+  const int left = min(p.rows - chunk * kQaRows, kQaRows) - first;  // rows from this block's first
+  const int rows = min(sh.rows, left);
+  if (rows <= 0) return;
+  const int own_rows = min(p.rows, kQaRows);
+  const float2* pre_ml = p.work.ml[kQaPrefix] + (size_t)s1.x * kQaRows + s0.z + first;
+  const float2* own_ml = p.work.ml[kQaOwn] + (size_t)s1.y * own_rows + first;
+  for (int k = tid; k < n * rows; k += kQaMergeThreads) {
+    const int i = k / rows, r = k - i * rows;
+    stats[k] = i < n_pre ? pre_ml[(size_t)i * kQaRows + r] : own_ml[(size_t)(i - n_pre) * own_rows + r];
+  }
+  __syncthreads();
+  const int el = kCols * rows;
+  const int part = tid / el, e = tid - part * el, row = e / kCols, col = e - row * kCols;
+  const bool on = part < sh.parts;
+  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  float l = 0.0f;
+  if (on) {
+    float m = -INFINITY;
+    for (int i = 0; i < n; ++i) m = fmaxf(m, stats[i * rows + row].x);
+    if (m > -INFINITY) {
+      const float4* pre = reinterpret_cast<const float4*>(p.work.O[kQaPrefix]) +
+                          ((size_t)s1.x * kQaRows + s0.z + first + row) * kCols + col;
+      const float4* own = reinterpret_cast<const float4*>(p.work.O[kQaOwn]) +
+                          ((size_t)s1.y * own_rows + first + row) * kCols + col;
+#pragma unroll 4
+      for (int i = part; i < n; i += sh.parts) {
+        const float4 v = i < n_pre ? pre[(size_t)i * kQaRows * kCols] : own[(size_t)(i - n_pre) * own_rows * kCols];
+        const float2 st = stats[i * rows + row];
+        if (st.x == -INFINITY) continue;  // the row saw nothing there
+        const float u = ex2_approx(st.x - m);
+        l += st.y * u;
+        acc.x += u * v.x;
+        acc.y += u * v.y;
+        acc.z += u * v.z;
+        acc.w += u * v.w;
+      }
+    }
+  }
+  if (sh.parts > 1) {
+    sums[tid] = acc;
+    part_l[tid] = l;
+    __syncthreads();
+    if (part == 0) {
+      for (int k = 1; k < sh.parts; ++k) {
+        const float4 v = sums[tid + k * el];
+        acc.x += v.x;
+        acc.y += v.y;
+        acc.z += v.z;
+        acc.w += v.w;
+        l += part_l[tid + k * el];
+      }
+    }
+  }
+  if (part > 0) return;
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;  // 0 as well where a faulty page made l NaN
+  if (inv == 0.0f) acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const size_t out_row = (size_t)(unit / p.chunks) * p.rows + chunk * kQaRows + first + row;
+  uint2 out;
+  if (p.fp16)
+    out = make_uint2(qa_pack_half(acc.x * inv, acc.y * inv), qa_pack_half(acc.z * inv, acc.w * inv));
+  else
+    out = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+  reinterpret_cast<uint2*>(p.O)[out_row * kCols + col] = out;
+}
+
+template <int D, int BITS, int NMAX>
+cudaError_t launch_quant_attn_instance(const QaLaunch& L) {
+  using C = QaCfg<D, BITS, NMAX>;
+  auto kern = quant_attn_kernel<D, BITS, NMAX>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(L.grid);
+  cfg.blockDim = dim3(C::kThreads);
+  cfg.dynamicSmemBytes = C::kSmem;
+  cfg.stream = L.stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if ((e = cudaLaunchKernelEx(&cfg, kern, L.p)) != cudaSuccess) return e;
+  // Rows of a block: as many as it has threads for, fewer (the threads then
+  // share elements) while the blocks are few.
+  const int rows = L.p.rows < kQaRows ? L.p.rows : kQaRows;
+  const long long units = (long long)L.p.batch * L.p.cache.n_kv_heads * L.p.chunks;
+  QaMergeShape sh;
+  sh.rows = kQaMergeThreads / (D / 4);
+  if (sh.rows > rows) sh.rows = rows;
+  while (sh.rows > 1 && units * ((rows + sh.rows - 1) / sh.rows) < 8 * L.grid) sh.rows = (sh.rows + 1) / 2;
+  sh.parts = kQaMergeThreads / (D / 4 * sh.rows);
+  cfg.gridDim = dim3((unsigned)units, (rows + sh.rows - 1) / sh.rows);
+  cfg.blockDim = dim3(kQaMergeThreads);
+  cfg.dynamicSmemBytes = (size_t)(2 * L.grid + 2) * sh.rows * sizeof(float2);
+  return cudaLaunchKernelEx(&cfg, quant_merge_kernel<D>, L.p, sh);
+}
+
+template <int D>
+cudaError_t launch_quant_attn_for_dim(const QaLaunch& L) {
+  if (L.p.cache.bits == 4)
+    return L.wide ? launch_quant_attn_instance<D, 4, 64>(L) : launch_quant_attn_instance<D, 4, 16>(L);
+  return L.wide ? launch_quant_attn_instance<D, 8, 64>(L) : launch_quant_attn_instance<D, 8, 16>(L);
+}
+
+}  // namespace wise

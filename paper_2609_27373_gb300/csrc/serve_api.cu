@@ -73,7 +73,8 @@ int check_prefix(const wise_cache_t* cache, const wise_prefix_t* sh, bool quanti
     return WISE_ERR_UNSUPPORTED;
   // Key tiles of all requests and kv heads are counted in 32 bits.
   const long long max_tiles = ((long long)cache->max_pages * cache->page + kPfxKeys - 1) / kPfxKeys;
-  if ((long long)sh->batch * cache->n_kv_heads * (max_tiles + 1) > (1LL << 30)) return WISE_ERR_UNSUPPORTED;
+  const int chunks = quantised && sh->q_len * group > 64 ? 2 : 1;  // those of 64 rows, see quant_attn.cuh
+  if ((long long)sh->batch * cache->n_kv_heads * chunks * (max_tiles + 1) > (1LL << 30)) return WISE_ERR_UNSUPPORTED;
   p->batch = sh->batch;
   p->q_len = sh->q_len;
   p->n_heads = sh->n_heads;
