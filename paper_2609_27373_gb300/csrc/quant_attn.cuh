@@ -6,7 +6,7 @@
 //
 // Work.  With R = q_len * n_heads / n_kv_heads query rows a request and kv head
 // there are two kinds of items, each for one kv head, at most 64 rows and a
-// range of keys that is taken 128 at a time (a tile):
+// range of keys that is taken 128 or 256 at a time (a tile):
 //   prefix  the shared prefix of a group against floor(64 / R) of its requests
 //           (no sharing where that is 1);
 //   own     one request's keys past the shared prefix, its rows 64 at a time.
@@ -22,7 +22,6 @@
 namespace wise {
 
 constexpr int kQaRows = 64;
-constexpr int kQaKeys = 128;
 
 struct QaTotals {
   PfxCuts own, pre;
@@ -99,6 +98,7 @@ struct QaParams {
   int batch, q_len, n_heads, group, n_groups;
   int rows;      // of a request and kv head
   int chunks;    // of up to 64 rows
+  int keys;      // of a step
   int per_tile;  // requests of a prefix item, 0 where nothing is shared
   int fp16;
   float scale_log2;

@@ -9,7 +9,11 @@
 // owns a row of K (a token) or of V^T (a channel), turns 16-byte pieces of
 // codes into fp16 pairs and stores those to its lane of tensor memory.
 //
-// Warp roles (480 threads):
+// A step is what the softmax takes at once: 256 keys in the narrow instance (up
+// to 16 query rows an item), 128 in the wide one (up to 64).  The cache's side
+// moves by halves of 128 keys, one row of the product's M each.
+//
+// Warp roles (512 threads):
 //   warps 0-3    softmax: S^T from tensor memory in fragments of 8 keys x 8
 //                rows, running maximum (raised only when a numerator passes
 //                2^15, which the four warps vote on), numerators as fp16 to
@@ -22,8 +26,9 @@
 //   warp 13      Q: rows of the next segment to shared memory as fp16, scaled by a
 //                power of two so that the largest is next to 2^15 (exact down
 //                to 2^-28 of it), and how many keys each row sees;
-//   warp 14      one thread: the products.
-// TMEM columns: K 0 and 64, V 128 and 192, S 256 and 320, O 384.
+//   warp 14      S products, by one lane;
+//   warp 15      P V products, by one lane.
+// All of tensor memory is allocated, so that its first column is 0.
 //
 // Every wait is bounded; one that runs out sets the status word and an abort
 // flag, and every role unwinds.
@@ -41,41 +46,52 @@ namespace wise {
 
 template <int D, int BITS, int NMAX>
 struct QaCfg {
-  static constexpr int kThreads = 480;
+  static constexpr int kThreads = 512;
+  static constexpr int kHalves = NMAX == 16 ? 2 : 1;  // of 128 keys, of a step
+  static constexpr int kBuffers = NMAX == 16 ? 3 : 2;  // of K and of V in tensor memory
+  // Columns: K, V, S (two steps), O.
+  static constexpr uint32_t kTmemK = 0, kTmemV = 64 * kBuffers, kTmemS = 128 * kBuffers,
+                            kTmemO = kTmemS + 2 * kHalves * NMAX;
+  static_assert(kTmemO + NMAX <= 512, "tensor memory");
   static constexpr int kBoxes = (D + 63) / 64;
   static constexpr int kBoxBytes = NMAX * 128;
   static constexpr int kQBytes = kBoxes * kBoxBytes;
-  static constexpr int kPBytes = 2 * kBoxBytes;
-  static constexpr int kTileBytes = 128 / 16 * q_block_bytes(BITS, D, 16);  // the same for every page size
+  static constexpr int kPBytes = 2 * kHalves * kBoxBytes;
+  static constexpr int kStageBytes = 128 / 16 * q_block_bytes(BITS, D, 16);  // 128 tokens, whatever the page size
   static constexpr int kMaxPlanBytes = 32 * 1024;
   static constexpr int kFixed = 2 * kQBytes + 2 * kPBytes;
-  static constexpr int kRoom = (218 * 1024 - 1024 - kMaxPlanBytes - kFixed) / kTileBytes;
+  static constexpr int kRoom = (218 * 1024 - 1024 - kMaxPlanBytes - kFixed) / kStageBytes;
   static constexpr int kStages = kRoom < 8 ? kRoom : 8;
-  static constexpr int kPlanAt = kFixed + kStages * kTileBytes;
+  static constexpr int kPlanAt = kFixed + kStages * kStageBytes;
   static constexpr int kSmem = kPlanAt + kMaxPlanBytes + 1024;
-  static_assert(kStages >= 3 && kTileBytes % 128 == 0, "ring");
+  static_assert(kStages >= 3 && kStageBytes % 128 == 0, "ring");
 };
 
-constexpr uint32_t kQaTmemK = 0, kQaTmemV = 128, kQaTmemS = 256, kQaTmemO = 384;
 constexpr int kQaSched = 16;
 constexpr int kQaFirst = 1, kQaLast = 2, kQaEnd = 4, kQaFaulty = 8;
 constexpr int kQaOwn = 0, kQaPrefix = 1;
 
-// Schedule entry of a tile, two int4: {flags | keys << 8 | rows << 16 | kind <<
-// 24, position of the first key, workspace slot or -1 (O itself), request},
-// {kv head, first row of the request, 0, 0}.  Entry t % 16 is written again for
-// tile t + 16 when the stage of tile t + 16 - NS, t + 8 or later, has been given
-// back by the V warps; they had to wait for P V of a tile two before that, and
-// with it for the softmax and the products to be past tile t.
-template <int NS>
+// Schedule entry of a step, two int4: {flags | rows << 8 | kind << 16 | keys <<
+// 20, position of the first key, workspace slot or -1 (O itself), request}, {kv
+// head, first row of the request, 0, 0}.  Entry t % 16 is written again for step
+// t + 16 when the V warps have given back a stage at most 8 halves before that
+// step; they had to wait for the P V product of a half 3 before that one at
+// most, and with it for the softmax and the products to be past step t + 4.
+__device__ __forceinline__ int qa_rows(int info) { return (info >> 8) & 255; }
+__device__ __forceinline__ int qa_kind(int info) { return (info >> 16) & 1; }
+__device__ __forceinline__ int qa_keys_of(int info) { return info >> 20; }
+
+template <int NS, int NB>
 struct QaShared {
   uint64_t full[NS], empty[NS];  // empty: 8 warps
   uint64_t sched_full[kQaSched];
-  uint64_t k_ready[2], v_ready[2], p_ready[2];  // 4 warps
-  uint64_t s_full[2], s_free[2];                // products; 4 warps
+  uint64_t k_ready[NB], v_ready[NB];  // 4 warps
+  uint64_t k_free[NB], v_free[NB];    // products
+  uint64_t p_ready[2];                // 4 warps
+  uint64_t s_full[2], s_free[2];      // products; 4 warps
   uint64_t pv_done[2];
   uint64_t q_ready[2], q_free[2];  // q_free: the products and 4 warps
-  uint64_t done;
+  uint64_t done[2];
   int4 sched[kQaSched][2];
   int lim[2][kQaRows];       // keys that a row sees, 0 for none
   int min_lim[2];            // the least of those that see any
@@ -145,7 +161,7 @@ __device__ inline void qa_make_plan(const QaParams& p, const QaPlan& plan, bool 
     if (active > 1) shared = max(0, min(plan.tiles[g], shortest)) & -c.page;
     __syncwarp();
     if (lane == 0) {
-      const int tiles = (shared + kQaKeys - 1) / kQaKeys;
+      const int tiles = (shared + p.keys - 1) / p.keys;
       const int row_tiles = tiles > 0 ? (e - a + p.per_tile - 1) / p.per_tile : 0;
       plan.tiles[g] = tiles;
       plan.lead[g] = lead;
@@ -176,7 +192,7 @@ __device__ inline void qa_make_plan(const QaParams& p, const QaPlan& plan, bool 
         x[k] = 0;
         if (first + k < n)
           x[k] = warp < 2 ? list[first + k]
-                          : max(0, plan.len[first + k] - plan.lo[first + k] + kQaKeys - 1) / kQaKeys;
+                          : max(0, plan.len[first + k] - plan.lo[first + k] + p.keys - 1) / p.keys;
         sum += x[k];
       }
       int upto = sum;
@@ -246,7 +262,7 @@ __device__ __forceinline__ QaSeg qa_segment(const QaParams& p, const QaPlan& pla
     const int lead = plan.lead[g];
     s.seq = plan.slot[lead];
     s.end = plan.lo[lead];
-    s.pos = t * kQaKeys;
+    s.pos = t * p.keys;
   } else {
     const int per = kv * p.chunks;
     s.req = qa_find(plan.cum, p.batch, x / per);  // cum[r] * per <= x < cum[r + 1] * per
@@ -260,7 +276,7 @@ __device__ __forceinline__ QaSeg qa_segment(const QaParams& p, const QaPlan& pla
     s.slot = s.req * per + unit + run;
     s.seq = plan.slot[s.req];
     s.end = plan.len[s.req];
-    s.pos = plan.lo[s.req] + t * kQaKeys;
+    s.pos = plan.lo[s.req] + t * p.keys;
     if (t == 0 && tiles <= x_end - x && plan.group[s.req] < 0) s.slot = -1;
   }
   s.left = min(tiles - t, x_end - x);
@@ -295,19 +311,40 @@ struct QaWalk {
   }
 };
 
-static __device__ __noinline__ bool qa_wait_long(uint64_t* bar, uint32_t parity, volatile int* abort, uint64_t limit) {
-  return mbar_wait(bar, parity, abort, limit);
-}
-__device__ __forceinline__ bool qa_wait(uint64_t* bar, uint32_t parity, volatile int* abort, uint64_t limit) {
-  return mbar_try_wait(bar, parity) || qa_wait_long(bar, parity, abort, limit);
-}
-__device__ __forceinline__ bool qa_warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort, uint64_t limit) {
-  return __all_sync(0xffffffffu, qa_wait(bar, parity, abort, limit));
-}
+// Waits.  One that runs out tells everybody: the abort flag ends the others.
+struct QaWait {
+  int* abort;
+  int* status;
+  unsigned long long limit;
+};
 static __device__ __noinline__ void qa_give_up(int* abort, int* status) {
   *reinterpret_cast<volatile int*>(abort) = 1;
   atomicOr(status, kStatusTimeout);
 }
+static __device__ __noinline__ bool qa_wait_long(uint64_t* bar, uint32_t parity, int* abort, int* status,
+                                                 unsigned long long limit) {
+  const bool ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort, limit));
+  if (!ok && (threadIdx.x & 31) == 0) qa_give_up(abort, status);
+  return ok;
+}
+// All lanes of a warp.
+__device__ __forceinline__ bool qa_wait(uint64_t* bar, uint32_t parity, const QaWait& w) {
+  if (__builtin_expect(__all_sync(0xffffffffu, mbar_try_wait(bar, parity)), 1)) return true;
+  return qa_wait_long(bar, parity, w.abort, w.status, w.limit);
+}
+
+// A place in a ring of N, and how often the ring has been passed.
+template <int N>
+struct QaRing {
+  int at = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next() {
+    if (++at == N) {
+      at = 0;
+      phase ^= 1;
+    }
+  }
+};
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
@@ -316,32 +353,32 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                : "memory");
 }
 
+#define QA_SHARED QaShared<QaCfg<D, BITS, NMAX>::kStages, QaCfg<D, BITS, NMAX>::kBuffers>
+
 // ------------------------------------------------------------------ producer
 template <int D, int BITS, int NMAX>
-__device__ void qa_producer(const QaParams& p, const QaPlan& plan, uint8_t* ring,
-                            QaShared<QaCfg<D, BITS, NMAX>::kStages>& sb) {
+__device__ void qa_producer(const QaParams& p, const QaPlan& plan, uint8_t* ring, QA_SHARED& sb, const QaWait& wt) {
   using C = QaCfg<D, BITS, NMAX>;
-  constexpr int NS = C::kStages;
+  constexpr int NS = C::kStages, kKeys = 128 * C::kHalves;
   const CacheView& c = p.cache;
   const int lane = threadIdx.x & 31;
-  volatile int* abort = &sb.abort;
-  const int block = c.head_bytes;
+  const int block = c.head_bytes, at = lane << c.page_shift;
   QaWalk walk;
   walk.begin(plan, kQaOwn);
   QaSeg seg;
-  int n = 0, bad = 0;
+  QaRing<NS> st;
+  int n = 0, t = 0, bad = 0;
   bool ok = true;
   while (ok && walk.next(p, plan, seg)) {
     int flags = kQaFirst;
-    auto look = [&](int pos) {
-      const int at = pos + (lane << c.page_shift);
-      return at - pos < kQaKeys && at < seg.end ? __ldg(c.table + (size_t)seg.seq * c.max_pages + (at >> c.page_shift))
-                                                : -1;
+    auto look = [&](int pos) {  // this lane's page of a step (up to 16 pages)
+      return at < kKeys && pos + at < seg.end
+                 ? __ldg(c.table + (size_t)seg.seq * c.max_pages + ((pos + at) >> c.page_shift))
+                 : -1;
     };
     int page = look(seg.pos);
-    for (; seg.left > 0; --seg.left, seg.pos += kQaKeys, flags = 0) {
-      const int st = n % NS, at = lane << c.page_shift;
-      const bool on = at < kQaKeys && seg.pos + at < seg.end;
+    for (; ok && seg.left > 0; --seg.left, seg.pos += kKeys, flags = 0) {
+      const bool on = at < kKeys && seg.pos + at < seg.end;
       const bool valid = on && valid_page(c, page);
       const uint32_t loads = __ballot_sync(0xffffffffu, valid);
       if (__any_sync(0xffffffffu, on && !valid)) {
@@ -349,39 +386,44 @@ __device__ void qa_producer(const QaParams& p, const QaPlan& plan, uint8_t* ring
         bad = 1;
       }
       if (seg.left == 1) flags |= kQaLast;
-      if (n >= NS) ok = qa_warp_wait(&sb.empty[st], (n / NS - 1) & 1, abort, p.wait_ns);
-      if (!ok) break;
-      if (lane == 0) {
-        sb.sched[n % kQaSched][0] = make_int4(flags | min(kQaKeys, seg.end - seg.pos) << 8 | seg.rows << 16 | seg.kind << 24,
-                                              seg.pos, seg.slot, seg.req);
-        sb.sched[n % kQaSched][1] = make_int4(seg.kvh, seg.row0, 0, 0);
-        mbar_arrive(&sb.sched_full[n % kQaSched]);
-        mbar_arrive_expect_tx(&sb.full[st], __popc(loads) * block);
+      const int keys = min(kKeys, seg.end - seg.pos);
+      const uint8_t* from = p.plane + (size_t)max(page, 0) * c.page_bytes + (size_t)seg.kvh * block;
+#pragma unroll 1
+      for (int h = 0; 128 * h < keys; ++h) {
+        if (n >= NS && !(ok = qa_wait(&sb.empty[st.at], st.phase ^ 1, wt))) break;
+        const int first = (128 * h) >> c.page_shift, pages = 128 >> c.page_shift;  // this half's lanes
+        if (lane == 0) {
+          if (h == 0) {
+            sb.sched[t % kQaSched][0] = make_int4(flags | seg.rows << 8 | seg.kind << 16 | keys << 20, seg.pos, seg.slot, seg.req);
+            sb.sched[t % kQaSched][1] = make_int4(seg.kvh, seg.row0, 0, 0);
+            mbar_arrive(&sb.sched_full[t % kQaSched]);
+          }
+          mbar_arrive_expect_tx(&sb.full[st.at], __popc(loads >> first & ((1u << pages) - 1u)) * block);
+        }
+        __syncwarp();
+        const int mine = lane - first;
+        if (valid && mine >= 0 && mine < pages)
+          bulk_load(ring + st.at * C::kStageBytes + mine * block, from, block, &sb.full[st.at]);
+        st.next();
+        ++n;
       }
-      __syncwarp();
-      if (valid)
-        bulk_load(ring + st * C::kTileBytes + lane * block,
-                  p.plane + (size_t)page * c.page_bytes + (size_t)seg.kvh * block, block, &sb.full[st]);
-      ++n;
-      if (seg.left > 1) page = look(seg.pos + kQaKeys);
+      ++t;
+      if (seg.left > 1) page = look(seg.pos + kKeys);
     }
   }
   if (ok) {
-    const int st = n % NS;
-    if (n >= NS) ok = qa_warp_wait(&sb.empty[st], (n / NS - 1) & 1, abort, p.wait_ns);
+    if (n >= NS) ok = qa_wait(&sb.empty[st.at], st.phase ^ 1, wt);
     if (ok && lane == 0) {
-      sb.sched[n % kQaSched][0] = make_int4(kQaEnd, 0, 0, 0);
-      mbar_arrive(&sb.sched_full[n % kQaSched]);
-      mbar_arrive(&sb.full[st]);
+      sb.sched[t % kQaSched][0] = make_int4(kQaEnd, 0, 0, 0);
+      mbar_arrive(&sb.sched_full[t % kQaSched]);
     }
   }
   if (bad && lane == 0) atomicOr(c.status, kStatusBadCache);
   if (lane == 0) {
-    if (!ok) qa_give_up(&sb.abort, c.status);
     // Copies already issued land before the CTA's shared memory is released,
-    // whoever may have given up.  (The end took the stage of tile n - NS.)
+    // whoever may have given up.
     int never = 0;
-    for (int k = max(0, ok ? n - NS + 1 : n - NS); k < n; ++k) mbar_wait(&sb.full[k % NS], (k / NS) & 1, &never);
+    for (int k = max(0, n - NS); k < n; ++k) mbar_wait(&sb.full[k % NS], (k / NS) & 1, &never);
   }
   __syncwarp();
 }
@@ -398,20 +440,16 @@ __device__ __forceinline__ uint32_t qa_pack_half(float lo, float hi) {
 }
 
 template <int D, int BITS, int NMAX>
-__device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_tiles,
-                           QaShared<QaCfg<D, BITS, NMAX>::kStages>& sb) {
+__device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_tiles, QA_SHARED& sb, const QaWait& wt) {
   using C = QaCfg<D, BITS, NMAX>;
   constexpr int kPieces = D / 8;  // of 16 bytes, of a row
   const int lane = threadIdx.x & 31;
-  volatile int* abort = &sb.abort;
   QaWalk walk;
   walk.begin(plan, kQaOwn);
   QaSeg seg;
-  bool ok = true;
   for (int k = 0; walk.next(p, plan, seg); ++k) {
     const int buf = k & 1;
-    if (k >= 2) ok = qa_warp_wait(&sb.q_free[buf], ((k >> 1) - 1) & 1, abort, p.wait_ns);
-    if (!ok) break;
+    if (k >= 2 && !qa_wait(&sb.q_free[buf], ((k >> 1) - 1) & 1, wt)) break;
     // Rows of one request are contiguous: Q is [batch][n_kv_heads][rows][D].
     const uint4* Q = reinterpret_cast<const uint4*>(p.Q) +
                      (((size_t)seg.req * p.cache.n_kv_heads + seg.kvh) * p.rows + seg.row0) * kPieces;
@@ -471,79 +509,120 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
     __syncwarp();
     if (lane == 0) mbar_arrive(&sb.q_ready[buf]);
   }
-  if (!ok && lane == 0) qa_give_up(&sb.abort, p.cache.status);
   __syncwarp();
 }
 
 // ------------------------------------------------------------------ products
-// One thread.  S of tile t is issued before P V of tile t - 1.
-template <int D, int BITS, int NMAX>
-__device__ void qa_products(const QaParams& p, uint32_t tmem, uint8_t* q_tiles, uint8_t* p_tiles,
-                            QaShared<QaCfg<D, BITS, NMAX>::kStages>& sb) {
-  using C = QaCfg<D, BITS, NMAX>;
-  // fp16 operands, fp32 sums.
+// A warp each walks the steps and one lane issues, so that addresses and
+// descriptors stay in uniform registers, where the instruction wants them.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t on;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(on));
+  return on != 0;
+}
+
+// fp16 operands, fp32 sums; N as in the entry, rounded up to 16 (N / 8 at bit 17).
+__device__ __forceinline__ uint32_t qa_idesc(int info) {
   constexpr uint32_t base = idesc_bf16_f32(128, 0, false, false) & ~((1u << 7) | (1u << 10));
-  volatile int* abort = &sb.abort;
-  const uint64_t desc_hi = smem_desc_sw128(0, 16, 1024);
-  const uint32_t hi = (uint32_t)(desc_hi >> 32), lo0 = (uint32_t)desc_hi;
-  int seg = -1, info = 0, before = 0;
-  bool ok = true;
-  for (int t = 0;; ++t) {
-    if (!(ok = qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, abort, p.wait_ns))) break;
-    info = sb.sched[t % kQaSched][0].x;
-    if (!(info & kQaEnd)) {
-      const int b = t & 1;
-      if (info & kQaFirst) {
-        ++seg;
-        if (!(ok = qa_wait(&sb.q_ready[seg & 1], (seg >> 1) & 1, abort, p.wait_ns))) break;
-      }
-      if (!(ok = qa_wait(&sb.k_ready[b], (t >> 1) & 1, abort, p.wait_ns) &&
-                 (t < 2 || qa_wait(&sb.s_free[b], ((t >> 1) - 1) & 1, abort, p.wait_ns))))
-        break;
-      tc_fence_after_sync();
-      const uint32_t n16 = (((info >> 16) & 255) + 15) >> 4;
-      const uint32_t idesc = base | n16 << 18;  // N / 8 at bit 17
-      const uint32_t q0 = lo0 | (smem_u32(q_tiles + (seg & 1) * C::kQBytes) >> 4);
-      uint32_t acc = 0;
-#pragma unroll 2
-      for (int kk = 0; kk < D / 16; ++kk) {
-        umma_ts_split(tmem + kQaTmemS + 64 * b, tmem + kQaTmemK + 64 * b + 8 * kk,
-                      q0 + (((kk >> 2) * C::kBoxBytes + (kk & 3) * 32) >> 4), hi, idesc, acc);
-        acc = 1;
-      }
-      umma_commit(&sb.s_full[b]);
-      if (info & kQaLast) umma_commit(&sb.q_free[seg & 1]);
-    }
-    if (t > 0) {
-      const int u = t - 1, b = u & 1;
-      if (!(ok = qa_wait(&sb.v_ready[b], (u >> 1) & 1, abort, p.wait_ns) &&
-                 qa_wait(&sb.p_ready[b], (u >> 1) & 1, abort, p.wait_ns)))
-        break;
-      tc_fence_after_sync();
-      const uint32_t n16 = (((before >> 16) & 255) + 15) >> 4;
-      const uint32_t idesc = base | n16 << 18;
-      const uint32_t p0 = lo0 | (smem_u32(p_tiles + b * C::kPBytes) >> 4);
-      uint32_t acc = before & kQaFirst ? 0 : 1;
-#pragma unroll 2
-      for (int kk = 0; kk < 8; ++kk) {
-        umma_ts_split(tmem + kQaTmemO, tmem + kQaTmemV + 64 * b + 8 * kk,
-                      p0 + (((kk >> 2) * C::kBoxBytes + (kk & 3) * 32) >> 4), hi, idesc, acc);
-        acc = 1;
-      }
-      umma_commit(&sb.pv_done[b]);
-    }
-    if (info & kQaEnd) break;
-    before = info;
+  return base | (uint32_t)((qa_rows(info) + 15) >> 4) << 18;
+}
+
+// All products of this warp end before tensor memory is given back.
+__device__ __forceinline__ void qa_products_done(uint64_t* done) {
+  if (elect_one()) {
+    int never = 0;
+    umma_commit(done);
+    mbar_wait(done, 0, &never);
   }
-  if (!ok) qa_give_up(&sb.abort, p.cache.status);
-  // All products end before tensor memory is given back.
-  int never = 0;
-  umma_commit(&sb.done);
-  mbar_wait(&sb.done, 0, &never);
+  __syncwarp();
+}
+
+template <int D, int BITS, int NMAX>
+__device__ void qa_products_s(const QaParams& p, uint8_t* q_tiles, QA_SHARED& sb, const QaWait& wt) {
+  using C = QaCfg<D, BITS, NMAX>;
+  const uint64_t desc = smem_desc_sw128(0, 16, 1024);
+  const uint32_t hi = (uint32_t)(desc >> 32), q_lo = (uint32_t)desc + (smem_u32(q_tiles) >> 4);
+  QaRing<C::kBuffers> kb;
+  int seg = -1;
+#pragma unroll 1
+  for (int t = 0;; ++t) {
+    if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) break;
+    const int info = __shfl_sync(0xffffffffu, sb.sched[t % kQaSched][0].x, 0);
+    if (info & kQaEnd) break;
+    const int b = t & 1;
+    if (info & kQaFirst) {
+      ++seg;
+      if (!qa_wait(&sb.q_ready[seg & 1], (seg >> 1) & 1, wt)) break;
+    }
+    if (t >= 2 && !qa_wait(&sb.s_free[b], ((t >> 1) - 1) & 1, wt)) break;
+    const uint32_t idesc = qa_idesc(info), q0 = q_lo + (seg & 1) * (C::kQBytes >> 4);
+    bool ok = true;
+#pragma unroll 1
+    for (int h = 0; 128 * h < qa_keys_of(info); ++h) {
+      if (!(ok = qa_wait(&sb.k_ready[kb.at], kb.phase, wt))) break;
+      tc_fence_after_sync();
+      const uint32_t s_at = C::kTmemS + (b * C::kHalves + h) * NMAX, k_at = C::kTmemK + 64 * kb.at;
+      if (elect_one()) {
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          umma_ts_split(s_at, k_at + 8 * kk, q0 + (((kk >> 2) * C::kBoxBytes + (kk & 3) * 32) >> 4), hi, idesc, kk > 0);
+        umma_commit(&sb.k_free[kb.at]);
+        if (128 * (h + 1) >= qa_keys_of(info)) {
+          umma_commit(&sb.s_full[b]);
+          if (info & kQaLast) umma_commit(&sb.q_free[seg & 1]);
+        }
+      }
+      __syncwarp();
+      kb.next();
+    }
+    if (!ok) break;
+  }
+  qa_products_done(&sb.done[0]);
+}
+
+template <int D, int BITS, int NMAX>
+__device__ void qa_products_pv(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, const QaWait& wt) {
+  using C = QaCfg<D, BITS, NMAX>;
+  const uint64_t desc = smem_desc_sw128(0, 16, 1024);
+  const uint32_t hi = (uint32_t)(desc >> 32), p_lo = (uint32_t)desc + (smem_u32(p_tiles) >> 4);
+  QaRing<C::kBuffers> vb;
+#pragma unroll 1
+  for (int t = 0;; ++t) {
+    if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) break;
+    const int info = __shfl_sync(0xffffffffu, sb.sched[t % kQaSched][0].x, 0);
+    if (info & kQaEnd) break;
+    const int b = t & 1;
+    if (!qa_wait(&sb.p_ready[b], (t >> 1) & 1, wt)) break;
+    const uint32_t idesc = qa_idesc(info);
+    bool ok = true;
+#pragma unroll 1
+    for (int h = 0; 128 * h < qa_keys_of(info); ++h) {
+      if (!(ok = qa_wait(&sb.v_ready[vb.at], vb.phase, wt))) break;
+      tc_fence_after_sync();
+      const uint32_t p0 = p_lo + ((b * C::kPBytes + 2 * h * C::kBoxBytes) >> 4), v_at = C::kTmemV + 64 * vb.at;
+      const uint32_t more = h > 0 || !(info & kQaFirst);
+      if (elect_one()) {
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk)
+          umma_ts_split(C::kTmemO, v_at + 8 * kk, p0 + (((kk >> 2) * C::kBoxBytes + (kk & 3) * 32) >> 4), hi, idesc,
+                        kk > 0 ? 1 : more);
+        umma_commit(&sb.v_free[vb.at]);
+        if (128 * (h + 1) >= qa_keys_of(info)) umma_commit(&sb.pv_done[b]);
+      }
+      __syncwarp();
+      vb.next();
+    }
+    if (!ok) break;
+  }
+  qa_products_done(&sb.done[1]);
 }
 
 // ------------------------------------------------------------ K and V to TMEM
-// Word of codes -> fp16 pairs times a scale pair each.
+// Word of codes -> fp16 pairs.
 template <int BITS>
 struct QaDecode;
 template <>
@@ -557,197 +636,202 @@ struct QaDecode<8> {
   __device__ static __forceinline__ void pairs(uint32_t w, uint32_t (&h)[2]) { q_decode8(w, h); }
 };
 
-template <int N>
-__device__ __forceinline__ void qa_tmem_store(uint32_t at, const uint32_t (&r)[N]) {
-  if constexpr (N == 32)
-    tmem_st_32x32b_x32(at, r);
-  else
-    tmem_st_32x32b_x16(at, r);
-}
-
-// Keys: this thread's token.  Values d0 .. d0 + 2 * COLS - 1 to COLS columns.
-template <int D, int BITS, int COLS>
-__device__ __forceinline__ void qa_key_columns(const uint8_t* data, int page, const uint8_t* scales, int d0, uint32_t at) {
-  uint32_t r[COLS];
-  constexpr int kPer = 128 / BITS;  // values of 16 bytes
-#pragma unroll
-  for (int v = 0; v < 2 * COLS; v += kPer) {
-    const uint4 x = *reinterpret_cast<const uint4*>(data + (d0 + v) / kPer * page * 16);
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t byte = scales[(d0 + v + k * kPer / 4) / 16];
-      const uint32_t s = byte << 7 | byte << 23;
-      uint32_t h[QaDecode<BITS>::kPairs];
-      QaDecode<BITS>::pairs(w[k], h);
-#pragma unroll
-      for (int j = 0; j < QaDecode<BITS>::kPairs; ++j) r[v / 2 + k * (kPer / 8) + j] = q_mul2(h[j], s);
-    }
-  }
-  qa_tmem_store<COLS>(at, r);
-}
-
+// A thread owns a token: 32 of its values (two groups) at a time.
 template <int D, int BITS, int NMAX>
-__device__ void qa_keys(const QaParams& p, uint32_t tmem, uint8_t* ring, QaShared<QaCfg<D, BITS, NMAX>::kStages>& sb) {
+__device__ void qa_keys(const QaParams& p, uint8_t* ring, QA_SHARED& sb, const QaWait& wt) {
   using C = QaCfg<D, BITS, NMAX>;
-  constexpr int NS = C::kStages;
   const CacheView& c = p.cache;
   const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
-  volatile int* abort = &sb.abort;
   const int token = 32 * quarter + lane, off = token & (c.page - 1);
   const int block_at = (token >> c.page_shift) * c.head_bytes;
-  const int data_at = block_at + off * 16;
-  const int scales_at = block_at + q_key_scales_at(BITS, D, c.page) + off * q_key_scale_bytes(D);
-  const uint32_t to = tmem + ((uint32_t)(32 * quarter) << 16) + kQaTmemK;
-  bool ok = true;
+  const uint8_t* data_at = ring + block_at + off * 16;
+  const uint8_t* scales_at = ring + block_at + q_key_scales_at(BITS, D, c.page) + off * q_key_scale_bytes(D);
+  const int step = c.page * 16;  // from 16 bytes of a token to the next 16
+  const uint32_t to = ((uint32_t)(32 * quarter) << 16) + C::kTmemK;
+  QaRing<C::kStages> st;
+  QaRing<C::kBuffers> kb;
+  int u = 0;  // halves
+#pragma unroll 1
   for (int t = 0;; ++t) {
-    const int st = t % NS, b = t & 1;
-    if (!(ok = qa_warp_wait(&sb.full[st], (t / NS) & 1, abort, p.wait_ns))) break;
-    if (sb.sched[t % kQaSched][0].x & kQaEnd) break;
-    if (t >= 2 && !(ok = qa_warp_wait(&sb.s_full[b], ((t >> 1) - 1) & 1, abort, p.wait_ns))) break;
-    tc_fence_after_sync();
-    const uint8_t* stage = ring + st * C::kTileBytes;
-    uint8_t scales[8];
-    if constexpr (D == 64)
-      *reinterpret_cast<uint32_t*>(scales) = *reinterpret_cast<const uint32_t*>(stage + scales_at);
-    else
-      *reinterpret_cast<uint2*>(scales) = *reinterpret_cast<const uint2*>(stage + scales_at);
-    const uint8_t* data = stage + data_at;
-    qa_key_columns<D, BITS, 32>(data, c.page, scales, 0, to + 64 * b);
-    if constexpr (D == 128) qa_key_columns<D, BITS, 32>(data, c.page, scales, 64, to + 64 * b + 32);
-    if constexpr (D == 96) qa_key_columns<D, BITS, 16>(data, c.page, scales, 64, to + 64 * b + 32);
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sb.empty[st]);
-    tmem_st_wait();
-    tc_fence_before_sync();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sb.k_ready[b]);
+    if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) return;
+    const int info = sb.sched[t % kQaSched][0].x;
+    if (info & kQaEnd) return;
+#pragma unroll 1
+    for (int h = 0; 128 * h < qa_keys_of(info); ++h, ++u) {
+      if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
+      if (u >= C::kBuffers && !qa_wait(&sb.k_free[kb.at], kb.phase ^ 1, wt)) return;
+      tc_fence_after_sync();
+      const uint8_t* data = data_at + st.at * C::kStageBytes;
+      const uint8_t* scales = scales_at + st.at * C::kStageBytes;
+#pragma unroll 2
+      for (int d = 0; d < D / 32; ++d) {
+        const uint32_t both = *reinterpret_cast<const uint16_t*>(scales + 2 * d);
+        const uint32_t s0 = (both & 255) * 0x00800080u, s1 = (both >> 8) * 0x00800080u;
+        uint32_t w[BITS], r[16];
+        *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(data);
+        data += step;
+        if constexpr (BITS == 8) {
+          *reinterpret_cast<uint4*>(w + 4) = *reinterpret_cast<const uint4*>(data);
+          data += step;
+        }
+#pragma unroll
+        for (int k = 0; k < BITS; ++k) {
+          constexpr int kPairs = QaDecode<BITS>::kPairs;
+          uint32_t x[kPairs];
+          QaDecode<BITS>::pairs(w[k], x);
+#pragma unroll
+          for (int j = 0; j < kPairs; ++j) r[k * kPairs + j] = q_mul2(x[j], k < BITS / 2 ? s0 : s1);
+        }
+        tmem_st_32x32b_x16(to + 64 * kb.at + 16 * d, r);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sb.empty[st.at]);
+      tmem_st_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sb.k_ready[kb.at]);
+      st.next();
+      kb.next();
+    }
   }
-  if (!ok && lane == 0) qa_give_up(&sb.abort, c.status);
-  __syncwarp();
 }
 
+// A thread owns a channel: 32 tokens at a time.
 template <int D, int BITS, int NMAX>
-__device__ void qa_values(const QaParams& p, uint32_t tmem, uint8_t* ring, QaShared<QaCfg<D, BITS, NMAX>::kStages>& sb) {
+__device__ void qa_values(const QaParams& p, uint8_t* ring, QA_SHARED& sb, const QaWait& wt) {
   using C = QaCfg<D, BITS, NMAX>;
-  constexpr int NS = C::kStages;
   const CacheView& c = p.cache;
   const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
-  volatile int* abort = &sb.abort;
   const bool on = 32 * quarter < D;
-  const int channel = 32 * quarter + lane;
   const int T = q_value_tokens(BITS, c.page), piece = T * BITS / 8;  // tokens and bytes of a piece
-  const int values_at = q_values_at(BITS, D, c.page) + channel * piece;
+  const int values_at = q_values_at(BITS, D, c.page) + (32 * quarter + lane) * piece;
   // Scales: this lane turns those of 8 tokens of one of the warp's two groups into fp16.
   const int stoken = 8 * (lane & 15);
   const int scales_at = (stoken >> c.page_shift) * c.head_bytes + q_value_scales_at(BITS, D, c.page) +
                         (2 * quarter + (lane >> 4)) * c.page + (stoken & (c.page - 1));
-  const int4* scales = &sb.value_scales[quarter][lane & 16];
-  const uint32_t to = tmem + ((uint32_t)(32 * quarter) << 16) + kQaTmemV;
-  bool ok = true;
-  for (int t = 0;; ++t) {
-    const int st = t % NS, b = t & 1;
-    if (!(ok = qa_warp_wait(&sb.full[st], (t / NS) & 1, abort, p.wait_ns))) break;
-    const int info = sb.sched[t % kQaSched][0].x;
-    if (info & kQaEnd) break;
-    if (t >= 2 && !(ok = qa_warp_wait(&sb.pv_done[b], ((t >> 1) - 1) & 1, abort, p.wait_ns))) break;
-    tc_fence_after_sync();
-    if (on) {
-      const int keys = (info >> 8) & 255;
-      const uint8_t* stage = ring + st * C::kTileBytes;
-      const uint2 bytes = *reinterpret_cast<const uint2*>(stage + scales_at);
-      uint32_t s[4];
-      s[0] = __byte_perm(bytes.x, 0, 0x1404) >> 1;  // bytes 0 and 1, each shifted by 7 in its half
-      s[1] = __byte_perm(bytes.x, 0, 0x3424) >> 1;
-      s[2] = __byte_perm(bytes.y, 0, 0x1404) >> 1;
-      s[3] = __byte_perm(bytes.y, 0, 0x3424) >> 1;
-      if (stoken + 8 > keys) {  // tokens past the end count 0 whatever is stored there
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (stoken + 2 * k >= keys) s[k] = 0;
-          if (stoken + 2 * k + 1 >= keys) s[k] &= 0xFFFFu;
-        }
-      }
-      sb.value_scales[quarter][lane] = *reinterpret_cast<const int4*>(s);
-      __syncwarp();
+  const uint32_t to = ((uint32_t)(32 * quarter) << 16) + C::kTmemV;
+  QaRing<C::kStages> st;
+  QaRing<C::kBuffers> vb;
+  int u = 0;  // halves
 #pragma unroll 1
-      for (int half = 0; half < 2; ++half) {  // 64 tokens, 32 columns
-        uint32_t r[32];
+  for (int t = 0;; ++t) {
+    if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) return;
+    const int info = sb.sched[t % kQaSched][0].x;
+    if (info & kQaEnd) return;
+#pragma unroll 1
+    for (int h = 0; 128 * h < qa_keys_of(info); ++h, ++u) {
+      if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
+      if (u >= C::kBuffers && !qa_wait(&sb.v_free[vb.at], vb.phase ^ 1, wt)) return;
+      tc_fence_after_sync();
+      if (on) {
+        const int keys = qa_keys_of(info) - 128 * h;
+        const uint8_t* stage = ring + st.at * C::kStageBytes;
+        const uint2 bytes = *reinterpret_cast<const uint2*>(stage + scales_at);
+        uint32_t s[4];
+        s[0] = __byte_perm(bytes.x, 0, 0x1404) >> 1;  // bytes 0 and 1, each shifted by 7 in its half
+        s[1] = __byte_perm(bytes.x, 0, 0x3424) >> 1;
+        s[2] = __byte_perm(bytes.y, 0, 0x1404) >> 1;
+        s[3] = __byte_perm(bytes.y, 0, 0x3424) >> 1;
+        if (__builtin_expect(keys < 128, 0)) {  // tokens past the end count 0 whatever is stored there
 #pragma unroll
-        for (int u = 0; u < 64; u += 16) {  // 16 tokens: 8 or 16 bytes of codes
-          const int token = 64 * half + u;
-          const int off = token & (c.page - 1);
-          const uint8_t* from =
-              stage + (token >> c.page_shift) * c.head_bytes + values_at + off / T * (D * piece) + off % T * BITS / 8;
-          uint32_t w[BITS / 2];
-          if constexpr (BITS == 4)
-            *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(from);
-          else
-            *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(from);
-          if (BITS == 8 && token + 16 > keys) {  // a code may be NaN there
+          for (int k = 0; k < 4; ++k) {
+            if (stoken + 2 * k >= keys) s[k] = 0;
+            if (stoken + 2 * k + 1 >= keys) s[k] &= 0xFFFFu;
+          }
+        }
+        __syncwarp();  // the scales of the half before have been read
+        sb.value_scales[quarter][lane] = *reinterpret_cast<const int4*>(s);
+        __syncwarp();
+        const int4* scales = &sb.value_scales[quarter][lane & 16];
+#pragma unroll 2
+        for (int token = 0; token < 128; token += 32) {
+          uint32_t w[BITS], r[16];
 #pragma unroll
-            for (int k = 0; k < BITS / 2; ++k) {
+          for (int j = 0; j < 2; ++j) {  // 16 tokens: 8 or 16 bytes
+            const int x = token + 16 * j, off = x & (c.page - 1);
+            const uint8_t* from =
+                stage + (x >> c.page_shift) * c.head_bytes + values_at + off / T * (D * piece) + off % T * BITS / 8;
+            if constexpr (BITS == 8) {
+              *reinterpret_cast<uint4*>(w + 4 * j) = *reinterpret_cast<const uint4*>(from);
+            } else if (T == 32) {
+              if (j == 0) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(from);
+            } else {
+              *reinterpret_cast<uint2*>(w + 2 * j) = *reinterpret_cast<const uint2*>(from);
+            }
+          }
+          if (BITS == 8 && __builtin_expect(token + 32 > keys, 0)) {  // a code may be NaN there
+#pragma unroll
+            for (int k = 0; k < BITS; ++k) {
               const int n = min(max(keys - token - 4 * k, 0), 4);
               w[k] = n == 4 ? w[k] : w[k] & ((1u << 8 * n) - 1u);
             }
           }
-          const int4 sa = scales[token / 8], sc = scales[token / 8 + 1];
-          const int f[8] = {sa.x, sa.y, sa.z, sa.w, sc.x, sc.y, sc.z, sc.w};
 #pragma unroll
-          for (int k = 0; k < BITS / 2; ++k) {
+          for (int q = 0; q < 4; ++q) {  // 8 tokens
+            const int4 f = scales[token / 8 + q];
+            const uint32_t fs[4] = {(uint32_t)f.x, (uint32_t)f.y, (uint32_t)f.z, (uint32_t)f.w};
             constexpr int kPairs = QaDecode<BITS>::kPairs;
-            uint32_t h[kPairs];
-            QaDecode<BITS>::pairs(w[k], h);
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j) r[u / 2 + k * kPairs + j] = q_mul2(h[j], (uint32_t)f[k * kPairs + j]);
+            for (int k = 0; k < BITS / 4; ++k) {
+              uint32_t x[kPairs];
+              QaDecode<BITS>::pairs(w[q * (BITS / 4) + k], x);
+#pragma unroll
+              for (int j = 0; j < kPairs; ++j) r[4 * q + k * kPairs + j] = q_mul2(x[j], fs[k * kPairs + j]);
+            }
           }
+          tmem_st_32x32b_x16(to + 64 * vb.at + token / 2, r);
         }
-        tmem_st_32x32b_x32(to + 64 * b + 32 * half, r);
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sb.empty[st.at]);
+      tmem_st_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sb.v_ready[vb.at]);
+      st.next();
+      vb.next();
     }
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sb.empty[st]);
-    tmem_st_wait();
-    tc_fence_before_sync();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sb.v_ready[b]);
   }
-  if (!ok && lane == 0) qa_give_up(&sb.abort, c.status);
-  __syncwarp();
 }
 
 // ------------------------------------------------------------------- softmax
 // 16 lanes x 8 columns a time: thread i holds row i / 4 (and that + 8, in the
 // other two), columns 2 (i % 4) and the next.
 template <int G>
-__device__ __forceinline__ void qa_load_fragments(uint32_t at, float (&s)[G][4]) {
-  if constexpr (G == 8) {
-    uint32_t r[32];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(at));
-    tmem_ld_wait(r);
-#pragma unroll
-    for (int k = 0; k < 32; ++k) s[k / 4][k % 4] = __uint_as_float(r[k]);
-  } else {
-    uint32_t r[8];
-    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(at));
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
-                 :
-                 : "memory");
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s[k / 4][k % 4] = __uint_as_float(r[k]);
+struct QaFragments {
+  uint32_t r[4 * G];
+  __device__ __forceinline__ void load(uint32_t at) {
+    if constexpr (G == 8) {
+      asm volatile(
+          "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+          "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+          "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+          : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+            "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+            "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+            "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+          : "r"(at));
+    } else {
+      asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                   : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                   : "r"(at));
+    }
   }
-}
+  __device__ __forceinline__ void wait() {  // nothing reads the registers before it
+    if constexpr (G == 8) {
+      tmem_ld_wait(r);
+    } else {
+      asm volatile("tcgen05.wait::ld.sync.aligned;"
+                   : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
+                   :
+                   : "memory");
+    }
+  }
+  __device__ __forceinline__ void give(float (&s)[G][4]) const {
+#pragma unroll
+    for (int k = 0; k < 4 * G; ++k) s[k / 4][k % 4] = __uint_as_float(r[k]);
+  }
+};
 
 __device__ __forceinline__ bool qa_vote(bool x) {  // of the 128 softmax threads
   uint32_t any;
@@ -763,14 +847,12 @@ __device__ __forceinline__ bool qa_vote(bool x) {  // of the 128 softmax threads
 }
 
 template <int D, int BITS, int NMAX>
-__device__ void qa_softmax(const QaParams& p, uint32_t tmem, uint8_t* p_tiles,
-                           QaShared<QaCfg<D, BITS, NMAX>::kStages>& sb) {
+__device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, const QaWait& wt) {
   using C = QaCfg<D, BITS, NMAX>;
-  constexpr int G = NMAX / 8;
+  constexpr int G = NMAX / 8, H = C::kHalves;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int key0 = 32 * w + lane / 4, col0 = 2 * (lane & 3);
-  volatile int* abort = &sb.abort;
-  const uint32_t lane_tmem = tmem + ((uint32_t)(32 * w) << 16);
+  const uint32_t lane_tmem = (uint32_t)(32 * w) << 16;
   // P: row n of 128 bytes in box (key / 64), 16-byte chunk ((key % 64) / 8) ^
   // (n & 7); this lane gives the address of row lane & 7 of matrix lane >> 3.
   const uint32_t p_at = smem_u32(p_tiles) + (w >> 1) * C::kBoxBytes + (lane & 7) * 128 +
@@ -782,29 +864,25 @@ __device__ void qa_softmax(const QaParams& p, uint32_t tmem, uint8_t* p_tiles,
   int4 e0 = make_int4(0, 0, 0, 0), e1 = e0, o0 = e0, o1 = e0;
 #pragma unroll
   for (int g = 0; g < G; ++g) shift[g][0] = shift[g][1] = sum[g][0] = sum[g][1] = 0.0f;
-  // A wait that ran out: everybody is told, and the next vote ends all four warps.
-  auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (qa_warp_wait(bar, parity, abort, p.wait_ns)) return true;
-    if (lane == 0) qa_give_up(&sb.abort, p.cache.status);
-    return false;
-  };
+  // Once a wait of a warp has run out, the next vote ends all four.
+#pragma unroll 1
   for (int t = 0;; ++t) {
     const int b = t & 1;
-    ok = ok && wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1);
+    ok = ok && qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt);
     if (ok) {
       e0 = sb.sched[t % kQaSched][0];
       e1 = sb.sched[t % kQaSched][1];
     }
-    const int flags = e0.x & 255, rows = (e0.x >> 16) & 255;
+    const int flags = e0.x & 255, rows = qa_rows(e0.x);
     const bool end = flags & kQaEnd, first = flags & kQaFirst;
-    float s[2][G][4];
+    float s[H][2][G][4];
     bool raise = false;
     uint32_t dead = 0;  // of the rows of this thread's columns, those that see nothing anywhere
     if (ok && !end) {
       if (first) {
         ++seg;
         faulty = false;
-        ok = wait(&sb.q_ready[seg & 1], (seg >> 1) & 1);
+        ok = qa_wait(&sb.q_ready[seg & 1], (seg >> 1) & 1, wt);
         scale = sb.q_scale[seg & 1];
         min_lim = sb.min_lim[seg & 1];
 #pragma unroll
@@ -814,26 +892,42 @@ __device__ void qa_softmax(const QaParams& p, uint32_t tmem, uint8_t* p_tiles,
         }
       }
       if (flags & kQaFaulty) faulty = true;
-      ok = ok && wait(&sb.s_full[b], (t >> 1) & 1);
+      ok = ok && qa_wait(&sb.s_full[b], (t >> 1) & 1, wt);
     }
     if (ok && !end) {
       tc_fence_after_sync();
-      qa_load_fragments<G>(lane_tmem + kQaTmemS + 64 * b, s[0]);
-      qa_load_fragments<G>(lane_tmem + (16u << 16) + kQaTmemS + 64 * b, s[1]);
+      {
+        QaFragments<G> f[H][2];
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          f[h][0].load(lane_tmem + C::kTmemS + (b * H + h) * NMAX);
+          f[h][1].load(lane_tmem + (16u << 16) + C::kTmemS + (b * H + h) * NMAX);
+        }
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          f[h][0].wait();
+          f[h][1].wait();
+          f[h][0].give(s[h][0]);
+          f[h][1].give(s[h][1]);
+        }
+      }
       tc_fence_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive(&sb.s_free[b]);
-      if (e0.y + kQaKeys > min_lim) {  // keys that a row does not see count nothing, whatever S is
+      // Keys that a row does not see count nothing, whatever S is (a step of 128
+      // keys of 256 has none in its second half).
+      if (__builtin_expect(e0.y + 128 * H > min_lim, 0)) {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
           if (8 * g >= rows) break;
           const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][8 * g + col0]);
           const int a = lim.x - e0.y - key0, c = lim.y - e0.y - key0;
 #pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            float* x = s[h >> 1][g] + 2 * (h & 1);
-            if (8 * h >= a) x[0] = -INFINITY;
-            if (8 * h >= c) x[1] = -INFINITY;
+          for (int h = 0; h < 4 * H; ++h) {
+            float* x = s[h >> 2][(h >> 1) & 1][g] + 2 * (h & 1);
+            const int key = 128 * (h >> 2) + 8 * (h & 3);
+            if (key >= a) x[0] = -INFINITY;
+            if (key >= c) x[1] = -INFINITY;
           }
         }
       }
@@ -842,7 +936,9 @@ __device__ void qa_softmax(const QaParams& p, uint32_t tmem, uint8_t* p_tiles,
         if (8 * g >= rows) break;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const float m = fmaxf(fmaxf(s[0][g][c], s[0][g][2 + c]), fmaxf(s[1][g][c], s[1][g][2 + c]));
+          float m = -INFINITY;
+#pragma unroll
+          for (int h = 0; h < 2 * H; ++h) m = fmaxf(m, fmaxf(s[h >> 1][h & 1][g][c], s[h >> 1][h & 1][g][2 + c]));
           raise |= fmaf(m, scale, shift[g][c]) > 15.0f;
         }
       }
@@ -858,15 +954,17 @@ __device__ void qa_softmax(const QaParams& p, uint32_t tmem, uint8_t* p_tiles,
       }
     }
     const bool raised = qa_vote(raise || !ok);
-    if (raised) {
-      // New references: the largest logits of the 128 keys.
+    if (__builtin_expect(raised, 0)) {
+      // New references: the largest logits of the step's keys.
       if (ok && !end) {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
           if (8 * g >= rows) break;
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float m = fmaxf(fmaxf(s[0][g][c], s[0][g][2 + c]), fmaxf(s[1][g][c], s[1][g][2 + c]));
+            float m = -INFINITY;
+#pragma unroll
+            for (int h = 0; h < 2 * H; ++h) m = fmaxf(m, fmaxf(s[h >> 1][h & 1][g][c], s[h >> 1][h & 1][g][2 + c]));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
@@ -877,7 +975,7 @@ __device__ void qa_softmax(const QaParams& p, uint32_t tmem, uint8_t* p_tiles,
       if (lane == 0) sb.warp_ok[w] = ok;
       named_barrier_sync(2, 128);
       if (!(sb.warp_ok[0] && sb.warp_ok[1] && sb.warp_ok[2] && sb.warp_ok[3])) return;
-      // All four warps have a tile here: one that has seen the end votes for nothing.
+      // All four warps have a step here: one that has seen the end votes for nothing.
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         if (8 * g >= rows) break;
@@ -896,13 +994,13 @@ __device__ void qa_softmax(const QaParams& p, uint32_t tmem, uint8_t* p_tiles,
       }
       named_barrier_sync(2, 128);
     }
-    // The end of the segment before this tile.
-    if (pending) {
+    // The end of the segment before this step.
+    if (__builtin_expect(pending, 0)) {
       pending = false;
       const int u = t - 1;
-      if (!(ok = wait(&sb.pv_done[u & 1], (u >> 1) & 1))) continue;
+      if (!(ok = qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt))) continue;
       tc_fence_after_sync();
-      const int n_rows = (o0.x >> 16) & 255, kind = (o0.x >> 24) & 1, which = o1.z;
+      const int n_rows = qa_rows(o0.x), kind = qa_kind(o0.x), which = o1.z;
       const bool direct = o0.z < 0, o_faulty = o1.w;
       constexpr int kParts = (NMAX + 31) / 32;
       float l[kParts];
@@ -925,7 +1023,7 @@ __device__ void qa_softmax(const QaParams& p, uint32_t tmem, uint8_t* p_tiles,
 #pragma unroll 1
         for (int c = 0; 16 * c < n_rows; ++c) {
           uint32_t v[16];
-          tmem_ld_32x32b_x16(lane_tmem + kQaTmemO + 16 * c, v);
+          tmem_ld_32x32b_x16(lane_tmem + C::kTmemO + 16 * c, v);
           tmem_ld_wait(v);
           const float lc = kParts == 1 ? l[0] : c < 2 ? l[0] : l[kParts - 1];
 #pragma unroll
@@ -945,42 +1043,45 @@ __device__ void qa_softmax(const QaParams& p, uint32_t tmem, uint8_t* p_tiles,
       tc_fence_before_sync();
     }
     if (end) return;
-    if (raised && !first) {  // O in units of the new references
+    if (__builtin_expect(raised && !first, 0)) {  // O in units of the new references
       const int u = t - 1;
-      if (!(ok = wait(&sb.pv_done[u & 1], (u >> 1) & 1))) continue;
+      if (!(ok = qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt))) continue;
       tc_fence_after_sync();
       if (32 * w < D) {
 #pragma unroll 1
         for (int c = 0; 16 * c < rows; ++c) {
           uint32_t v[16];
-          tmem_ld_32x32b_x16(lane_tmem + kQaTmemO + 16 * c, v);
+          tmem_ld_32x32b_x16(lane_tmem + C::kTmemO + 16 * c, v);
           tmem_ld_wait(v);
 #pragma unroll
           for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * sb.factor[16 * c + k]);
-          tmem_st_32x32b_x16(lane_tmem + kQaTmemO + 16 * c, v);
+          tmem_st_32x32b_x16(lane_tmem + C::kTmemO + 16 * c, v);
         }
         tmem_st_wait();
       }
       tc_fence_before_sync();
     }
-    if (t >= 2 && !(ok = wait(&sb.pv_done[b], ((t >> 1) - 1) & 1))) continue;
+    if (t >= 2 && !(ok = qa_wait(&sb.pv_done[b], ((t >> 1) - 1) & 1, wt))) continue;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       if (8 * g >= rows) break;
       const float sh0 = shift[g][0] == INFINITY ? 0.0f : shift[g][0], sh1 = shift[g][1] == INFINITY ? 0.0f : shift[g][1];
-      uint32_t pk[4];
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const float* x = s[h >> 1][g] + 2 * (h & 1);
-        const float a = ex2_approx(fmaf(x[0], scale, sh0)), c = ex2_approx(fmaf(x[1], scale, sh1));
-        sum[g][0] += a;
-        sum[g][1] += c;
-        pk[h] = qa_pack_half(a, c);
+      for (int h = 0; h < H; ++h) {
+        uint32_t pk[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float* x = s[h][k >> 1][g] + 2 * (k & 1);
+          const float a = ex2_approx(fmaf(x[0], scale, sh0)), c = ex2_approx(fmaf(x[1], scale, sh1));
+          sum[g][0] += a;
+          sum[g][1] += c;
+          pk[k] = qa_pack_half(a, c);
+        }
+        asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
+                         p_at + b * C::kPBytes + 2 * h * C::kBoxBytes + g * 1024),
+                     "r"(pk[0]), "r"(pk[1]), "r"(pk[2]), "r"(pk[3])
+                     : "memory");
       }
-      asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(p_at + b * C::kPBytes +
-                                                                                               g * 1024),
-                   "r"(pk[0]), "r"(pk[1]), "r"(pk[2]), "r"(pk[3])
-                   : "memory");
     }
     fence_proxy_async_smem();
     __syncwarp();
@@ -1045,7 +1146,7 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
   uint8_t* p_tiles = q_tiles + 2 * C::kQBytes;
   uint8_t* ring = q_tiles + C::kFixed;
   const QaPlan plan = qa_plan(reinterpret_cast<int*>(q_tiles + C::kPlanAt), p.batch, p.n_groups);
-  __shared__ QaShared<C::kStages> sb;
+  __shared__ QA_SHARED sb;
   static_assert(C::kSmem + sizeof(sb) <= 227 * 1024, "shared memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -1055,17 +1156,21 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
       mbar_init(&sb.empty[i], 8);
     }
     for (int i = 0; i < kQaSched; ++i) mbar_init(&sb.sched_full[i], 1);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < C::kBuffers; ++i) {
       mbar_init(&sb.k_ready[i], 4);
       mbar_init(&sb.v_ready[i], 4);
+      mbar_init(&sb.k_free[i], 1);
+      mbar_init(&sb.v_free[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
       mbar_init(&sb.p_ready[i], 4);
       mbar_init(&sb.s_full[i], 1);
       mbar_init(&sb.s_free[i], 4);
       mbar_init(&sb.pv_done[i], 1);
       mbar_init(&sb.q_ready[i], 1);
       mbar_init(&sb.q_free[i], 5);
+      mbar_init(&sb.done[i], 1);
     }
-    mbar_init(&sb.done, 1);
     fence_mbar_init();
   }
   if (warp == 14) {
@@ -1077,32 +1182,34 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
   tc_fence_before_sync();
   qa_make_plan(p, plan, blockIdx.x == 0);  // ends with a barrier
   tc_fence_after_sync();
-  const uint32_t tmem = sb.tmem_base;
   if (threadIdx.x == 0) griddep_launch_dependents();  // the merge waits for this grid's end
+  const QaWait wt = {&sb.abort, p.cache.status, p.wait_ns};
 
   if (warp < 4) {
-    qa_softmax<D, BITS, NMAX>(p, tmem, p_tiles, sb);
+    qa_softmax<D, BITS, NMAX>(p, p_tiles, sb, wt);
   } else if (warp < 8) {
-    qa_keys<D, BITS, NMAX>(p, tmem, ring, sb);
+    qa_keys<D, BITS, NMAX>(p, ring, sb, wt);
   } else if (warp < 12) {
-    qa_values<D, BITS, NMAX>(p, tmem, ring, sb);
+    qa_values<D, BITS, NMAX>(p, ring, sb, wt);
   } else if (warp == 12) {
-    qa_producer<D, BITS, NMAX>(p, plan, ring, sb);
+    qa_producer<D, BITS, NMAX>(p, plan, ring, sb, wt);
   } else if (warp == 13) {
-    qa_queries<D, BITS, NMAX>(p, plan, q_tiles, sb);
+    qa_queries<D, BITS, NMAX>(p, plan, q_tiles, sb, wt);
     // Where the merge finds its parts.
     const int units = p.batch * p.cache.n_kv_heads * p.chunks;
     for (int i = blockIdx.x * 32 + lane; i < units; i += gridDim.x * 32)
       qa_sources(p, plan, i, p.work.sources + 2 * (size_t)i);
-  } else if (lane == 0) {
-    qa_products<D, BITS, NMAX>(p, tmem, q_tiles, p_tiles, sb);
+  } else if (warp == 14) {
+    qa_products_s<D, BITS, NMAX>(p, q_tiles, sb, wt);
+  } else {
+    qa_products_pv<D, BITS, NMAX>(p, p_tiles, sb, wt);
   }
   __syncwarp();
   tc_fence_before_sync();
   __syncthreads();
   if (warp == 14) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(0, 512);
   }
 }
 
@@ -1194,9 +1301,10 @@ __global__ void __launch_bounds__(kQaMergeThreads) quant_merge_kernel(const QaPa
 }
 
 template <int D, int BITS, int NMAX>
-cudaError_t launch_quant_attn_instance(const QaLaunch& L) {
+cudaError_t launch_quant_attn_instance(QaLaunch L) {
   using C = QaCfg<D, BITS, NMAX>;
   auto kern = quant_attn_kernel<D, BITS, NMAX>;
+  L.p.keys = 128 * C::kHalves;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
