@@ -13,21 +13,22 @@
 // to 16 query rows an item), 128 in the wide one (up to 64).  The cache's side
 // moves by halves of 128 keys, one row of the product's M each.
 //
-// Warp roles (512 threads):
-//   warps 0-3    softmax: S^T from tensor memory in fragments of 8 keys x 8
+// Warp roles (768 threads, 512 in the wide instance):
+//   a warpgroup  softmax: S^T from tensor memory in fragments of 8 keys x 8
 //                rows, running maximum (raised only when a numerator passes
 //                2^15, which the four warps vote on), numerators as fp16 to
 //                shared memory (P, the B operand of the second product), O's
 //                rescaling and the end of a segment;
-//   warps 4-7    K: codes to tensor memory;
-//   warps 8-11   V: the same, scales of 8 tokens at a time;
-//   warp 12      producer: page look-ups, one bulk copy a page (codes and scales
+//   then in turn (two teams of each that take every other half, in the wide
+//                instance one)
+//                K: codes to tensor memory;
+//                V: the same, scales of 8 tokens at a time;
+//   a warp       producer: page look-ups, one bulk copy a page (codes and scales
 //                of keys and values lie together), the schedule;
-//   warp 13      Q: rows of the next segment to shared memory as fp16, scaled by a
+//   a warp       Q: rows of the next segment to shared memory as fp16, scaled by a
 //                power of two so that the largest is next to 2^15 (exact down
 //                to 2^-28 of it), and how many keys each row sees;
-//   warp 14      S products, by one lane;
-//   warp 15      P V products, by one lane.
+//   two warps    S products and P V products, each issued by one lane.
 // All of tensor memory is allocated, so that its first column is 0.
 //
 // Every wait is bounded; one that runs out sets the status word and an abort
@@ -46,8 +47,12 @@ namespace wise {
 
 template <int D, int BITS, int NMAX>
 struct QaCfg {
-  static constexpr int kThreads = 512;
   static constexpr int kHalves = NMAX == 16 ? 2 : 1;  // of 128 keys, of a step
+  static constexpr int kTeams = NMAX == 16 ? 2 : 1;    // of four warps that take the halves in turn, of K and of V
+  static constexpr int kThreads = 128 * (2 + 2 * kTeams);
+  // Registers: the block is launched with 80 or 128 a thread, which the roles split anew.
+  static constexpr int kRegsSoftmax = NMAX == 16 ? 120 : 200, kRegsOther = NMAX == 16 ? 72 : 104;
+  static_assert(128 * kRegsSoftmax + (kThreads - 128) * kRegsOther <= kThreads * (NMAX == 16 ? 80 : 128), "registers");
   static constexpr int kBuffers = NMAX == 16 ? 3 : 2;  // of K and of V in tensor memory
   // Columns: K, V, S (two steps), O.
   static constexpr uint32_t kTmemK = 0, kTmemV = 64 * kBuffers, kTmemS = 128 * kBuffers,
@@ -73,7 +78,8 @@ constexpr int kQaOwn = 0, kQaPrefix = 1;
 
 // Schedule entry of a step, two int4: {flags | rows << 8 | kind << 16 | keys <<
 // 20, position of the first key, workspace slot or -1 (O itself), request}, {kv
-// head, first row of the request, 0, 0}.  Entry t % 16 is written again for step
+// head, first row of the request, 0, 0}.  The K and V warps go by halves and
+// need no more than half_keys, which comes with the stage.  Entry t % 16 is written again for step
 // t + 16 when the V warps have given back a stage at most 8 halves before that
 // step; they had to wait for the P V product of a half 3 before that one at
 // most, and with it for the softmax and the products to be past step t + 4.
@@ -81,7 +87,7 @@ __device__ __forceinline__ int qa_rows(int info) { return (info >> 8) & 255; }
 __device__ __forceinline__ int qa_kind(int info) { return (info >> 16) & 1; }
 __device__ __forceinline__ int qa_keys_of(int info) { return info >> 20; }
 
-template <int NS, int NB>
+template <int NS, int NB, int NT>
 struct QaShared {
   uint64_t full[NS], empty[NS];  // empty: 8 warps
   uint64_t sched_full[kQaSched];
@@ -93,14 +99,15 @@ struct QaShared {
   uint64_t q_ready[2], q_free[2];  // q_free: the products and 4 warps
   uint64_t done[2];
   int4 sched[kQaSched][2];
-  int lim[2][kQaRows];       // keys that a row sees, 0 for none
+  alignas(16) int lim[2][kQaRows];  // keys that a row sees, 0 for none
   int min_lim[2];            // the least of those that see any
   float q_scale[2];          // logits in base-2 units = S * q_scale
-  float warp_max[4][kQaRows];
-  float factor[kQaRows];
-  float sums[2][4][kQaRows];
-  float top[2][kQaRows];
-  int4 value_scales[4][32];  // a warp's two groups x 128 tokens as fp16
+  alignas(16) float warp_max[4][kQaRows];
+  alignas(16) float shift[2][kQaRows];  // added to a row's logits: 7 minus the reference, infinite where nothing is seen
+  alignas(16) float factor[kQaRows];    // of O and the sums where the references have moved
+  alignas(16) float sums[2][4][kQaRows];
+  alignas(16) int4 value_scales[4 * NT][32];  // a warp's two groups x 128 tokens as fp16
+  int half_keys[NS];  // keys of the half in a stage, 0 at the end
   uint32_t tmem_base;
   int abort, warp_ok[4];
 };
@@ -321,6 +328,18 @@ static __device__ __noinline__ void qa_give_up(int* abort, int* status) {
   *reinterpret_cast<volatile int*>(abort) = 1;
   atomicOr(status, kStatusTimeout);
 }
+// Suspends for up to 10 us before it says that the phase is not complete.
+__device__ __forceinline__ bool qa_try_wait(uint64_t* bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(done)
+      : "r"(smem_u32(bar)), "r"(parity), "r"(10000u)
+      : "memory");
+  return done != 0;
+}
 static __device__ __noinline__ bool qa_wait_long(uint64_t* bar, uint32_t parity, int* abort, int* status,
                                                  unsigned long long limit) {
   const bool ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort, limit));
@@ -329,7 +348,7 @@ static __device__ __noinline__ bool qa_wait_long(uint64_t* bar, uint32_t parity,
 }
 // All lanes of a warp.
 __device__ __forceinline__ bool qa_wait(uint64_t* bar, uint32_t parity, const QaWait& w) {
-  if (__builtin_expect(__all_sync(0xffffffffu, mbar_try_wait(bar, parity)), 1)) return true;
+  if (__builtin_expect(__all_sync(0xffffffffu, qa_try_wait(bar, parity)), 1)) return true;
   return qa_wait_long(bar, parity, w.abort, w.status, w.limit);
 }
 
@@ -353,7 +372,7 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                : "memory");
 }
 
-#define QA_SHARED QaShared<QaCfg<D, BITS, NMAX>::kStages, QaCfg<D, BITS, NMAX>::kBuffers>
+#define QA_SHARED QaShared<QaCfg<D, BITS, NMAX>::kStages, QaCfg<D, BITS, NMAX>::kBuffers, QaCfg<D, BITS, NMAX>::kTeams>
 
 // ------------------------------------------------------------------ producer
 template <int D, int BITS, int NMAX>
@@ -398,6 +417,7 @@ __device__ void qa_producer(const QaParams& p, const QaPlan& plan, uint8_t* ring
             sb.sched[t % kQaSched][1] = make_int4(seg.kvh, seg.row0, 0, 0);
             mbar_arrive(&sb.sched_full[t % kQaSched]);
           }
+          sb.half_keys[st.at] = min(128, keys - 128 * h);
           mbar_arrive_expect_tx(&sb.full[st.at], __popc(loads >> first & ((1u << pages) - 1u)) * block);
         }
         __syncwarp();
@@ -411,19 +431,26 @@ __device__ void qa_producer(const QaParams& p, const QaPlan& plan, uint8_t* ring
       if (seg.left > 1) page = look(seg.pos + kKeys);
     }
   }
-  if (ok) {
-    if (n >= NS) ok = qa_wait(&sb.empty[st.at], st.phase ^ 1, wt);
-    if (ok && lane == 0) {
-      sb.sched[t % kQaSched][0] = make_int4(kQaEnd, 0, 0, 0);
-      mbar_arrive(&sb.sched_full[t % kQaSched]);
+  // The end, for each of the teams.
+#pragma unroll 1
+  for (int k = 0; ok && k < C::kTeams; ++k) {
+    if (n + k >= NS && !(ok = qa_wait(&sb.empty[st.at], st.phase ^ 1, wt))) break;
+    if (lane == 0) {
+      if (k == 0) {
+        sb.sched[t % kQaSched][0] = make_int4(kQaEnd, 0, 0, 0);
+        mbar_arrive(&sb.sched_full[t % kQaSched]);
+      }
+      sb.half_keys[st.at] = 0;
+      mbar_arrive(&sb.full[st.at]);
     }
+    st.next();
   }
   if (bad && lane == 0) atomicOr(c.status, kStatusBadCache);
   if (lane == 0) {
     // Copies already issued land before the CTA's shared memory is released,
-    // whoever may have given up.
+    // whoever may have given up.  (Where the end took a stage they have.)
     int never = 0;
-    for (int k = max(0, n - NS); k < n; ++k) mbar_wait(&sb.full[k % NS], (k / NS) & 1, &never);
+    for (int k = max(0, ok ? n - NS + C::kTeams : n - NS); k < n; ++k) mbar_wait(&sb.full[k % NS], (k / NS) & 1, &never);
   }
   __syncwarp();
 }
@@ -471,10 +498,12 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
       if (lim > 0) least = min(least, lim);
     }
     least = __reduce_min_sync(0xffffffffu, least);
+    __syncwarp();
     uint32_t top = 0;
     if (!p.fp16) {
 #pragma unroll 4
       for (int i = lane; i < pieces; i += 32) {
+        if (sb.lim[buf][i / kPieces] <= 0) continue;
         const uint4 v = load(i);
         top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu),
                                      __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
@@ -493,7 +522,7 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
 #pragma unroll 4
     for (int i = lane; i < all; i += 32) {
       uint4 v = make_uint4(0, 0, 0, 0);
-      if (i < pieces) v = load(i);
+      if (i < pieces && sb.lim[buf][i / kPieces] > 0) v = load(i);  // what sees nothing may hold anything
       if (!p.fp16) {
         uint32_t* w = reinterpret_cast<uint32_t*>(&v);
 #pragma unroll
@@ -552,13 +581,21 @@ __device__ void qa_products_s(const QaParams& p, uint8_t* q_tiles, QA_SHARED& sb
   for (int t = 0;; ++t) {
     if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) break;
     const int info = __shfl_sync(0xffffffffu, sb.sched[t % kQaSched][0].x, 0);
-    if (info & kQaEnd) break;
     const int b = t & 1;
+    // (The end too waits for the softmax to have seen the step two before.)
+    if (t >= 2 && !qa_wait(&sb.s_free[b], ((t >> 1) - 1) & 1, wt)) break;
+    if (info & kQaEnd) {
+      if (elect_one()) {
+        mbar_arrive(&sb.s_full[b]);
+        mbar_arrive(&sb.s_full[b]);
+      }
+      __syncwarp();
+      break;
+    }
     if (info & kQaFirst) {
       ++seg;
       if (!qa_wait(&sb.q_ready[seg & 1], (seg >> 1) & 1, wt)) break;
     }
-    if (t >= 2 && !qa_wait(&sb.s_free[b], ((t >> 1) - 1) & 1, wt)) break;
     const uint32_t idesc = qa_idesc(info), q0 = q_lo + (seg & 1) * (C::kQBytes >> 4);
     bool ok = true;
 #pragma unroll 1
@@ -573,6 +610,7 @@ __device__ void qa_products_s(const QaParams& p, uint8_t* q_tiles, QA_SHARED& sb
         umma_commit(&sb.k_free[kb.at]);
         if (128 * (h + 1) >= qa_keys_of(info)) {
           umma_commit(&sb.s_full[b]);
+          mbar_arrive(&sb.s_full[b]);  // and what this warp knows of the schedule and the queries
           if (info & kQaLast) umma_commit(&sb.q_free[seg & 1]);
         }
       }
@@ -638,7 +676,7 @@ struct QaDecode<8> {
 
 // A thread owns a token: 32 of its values (two groups) at a time.
 template <int D, int BITS, int NMAX>
-__device__ void qa_keys(const QaParams& p, uint8_t* ring, QA_SHARED& sb, const QaWait& wt) {
+__device__ void qa_keys(const QaParams& p, int team, uint8_t* ring, QA_SHARED& sb, const QaWait& wt) {
   using C = QaCfg<D, BITS, NMAX>;
   const CacheView& c = p.cache;
   const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
@@ -650,46 +688,48 @@ __device__ void qa_keys(const QaParams& p, uint8_t* ring, QA_SHARED& sb, const Q
   const uint32_t to = ((uint32_t)(32 * quarter) << 16) + C::kTmemK;
   QaRing<C::kStages> st;
   QaRing<C::kBuffers> kb;
-  int u = 0;  // halves
+  for (int k = 0; k < team; ++k) {
+    st.next();
+    kb.next();
+  }
 #pragma unroll 1
-  for (int t = 0;; ++t) {
-    if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) return;
-    const int info = sb.sched[t % kQaSched][0].x;
-    if (info & kQaEnd) return;
-#pragma unroll 1
-    for (int h = 0; 128 * h < qa_keys_of(info); ++h, ++u) {
-      if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
-      if (u >= C::kBuffers && !qa_wait(&sb.k_free[kb.at], kb.phase ^ 1, wt)) return;
-      tc_fence_after_sync();
-      const uint8_t* data = data_at + st.at * C::kStageBytes;
-      const uint8_t* scales = scales_at + st.at * C::kStageBytes;
+  for (int u = team;; u += C::kTeams) {  // halves
+    if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
+    const int keys = sb.half_keys[st.at];
+    if (keys == 0) return;
+    if (u >= C::kBuffers && !qa_wait(&sb.k_free[kb.at], kb.phase ^ 1, wt)) return;
+    tc_fence_after_sync();
+    const uint8_t* data = data_at + st.at * C::kStageBytes;
+    const uint8_t* scales = scales_at + st.at * C::kStageBytes;
 #pragma unroll 2
-      for (int d = 0; d < D / 32; ++d) {
-        const uint32_t both = *reinterpret_cast<const uint16_t*>(scales + 2 * d);
-        const uint32_t s0 = (both & 255) * 0x00800080u, s1 = (both >> 8) * 0x00800080u;
-        uint32_t w[BITS], r[16];
-        *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(data);
+    for (int d = 0; d < D / 32; ++d) {
+      const uint32_t both = *reinterpret_cast<const uint16_t*>(scales + 2 * d);
+      const uint32_t s0 = (both & 255) * 0x00800080u, s1 = (both >> 8) * 0x00800080u;
+      uint32_t w[BITS], r[16];
+      *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(data);
+      data += step;
+      if constexpr (BITS == 8) {
+        *reinterpret_cast<uint4*>(w + 4) = *reinterpret_cast<const uint4*>(data);
         data += step;
-        if constexpr (BITS == 8) {
-          *reinterpret_cast<uint4*>(w + 4) = *reinterpret_cast<const uint4*>(data);
-          data += step;
-        }
-#pragma unroll
-        for (int k = 0; k < BITS; ++k) {
-          constexpr int kPairs = QaDecode<BITS>::kPairs;
-          uint32_t x[kPairs];
-          QaDecode<BITS>::pairs(w[k], x);
-#pragma unroll
-          for (int j = 0; j < kPairs; ++j) r[k * kPairs + j] = q_mul2(x[j], k < BITS / 2 ? s0 : s1);
-        }
-        tmem_st_32x32b_x16(to + 64 * kb.at + 16 * d, r);
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sb.empty[st.at]);
-      tmem_st_wait();
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sb.k_ready[kb.at]);
+#pragma unroll
+      for (int k = 0; k < BITS; ++k) {
+        constexpr int kPairs = QaDecode<BITS>::kPairs;
+        uint32_t x[kPairs];
+        QaDecode<BITS>::pairs(w[k], x);
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) r[k * kPairs + j] = q_mul2(x[j], k < BITS / 2 ? s0 : s1);
+      }
+      tmem_st_32x32b_x16(to + 64 * kb.at + 16 * d, r);
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.empty[st.at]);
+    tmem_st_wait();
+    tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.k_ready[kb.at]);
+#pragma unroll
+    for (int k = 0; k < C::kTeams; ++k) {
       st.next();
       kb.next();
     }
@@ -698,7 +738,7 @@ __device__ void qa_keys(const QaParams& p, uint8_t* ring, QA_SHARED& sb, const Q
 
 // A thread owns a channel: 32 tokens at a time.
 template <int D, int BITS, int NMAX>
-__device__ void qa_values(const QaParams& p, uint8_t* ring, QA_SHARED& sb, const QaWait& wt) {
+__device__ void qa_values(const QaParams& p, int team, uint8_t* ring, QA_SHARED& sb, const QaWait& wt) {
   using C = QaCfg<D, BITS, NMAX>;
   const CacheView& c = p.cache;
   const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
@@ -712,82 +752,83 @@ __device__ void qa_values(const QaParams& p, uint8_t* ring, QA_SHARED& sb, const
   const uint32_t to = ((uint32_t)(32 * quarter) << 16) + C::kTmemV;
   QaRing<C::kStages> st;
   QaRing<C::kBuffers> vb;
-  int u = 0;  // halves
+  for (int k = 0; k < team; ++k) {
+    st.next();
+    vb.next();
+  }
 #pragma unroll 1
-  for (int t = 0;; ++t) {
-    if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) return;
-    const int info = sb.sched[t % kQaSched][0].x;
-    if (info & kQaEnd) return;
-#pragma unroll 1
-    for (int h = 0; 128 * h < qa_keys_of(info); ++h, ++u) {
-      if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
-      if (u >= C::kBuffers && !qa_wait(&sb.v_free[vb.at], vb.phase ^ 1, wt)) return;
-      tc_fence_after_sync();
-      if (on) {
-        const int keys = qa_keys_of(info) - 128 * h;
-        const uint8_t* stage = ring + st.at * C::kStageBytes;
-        const uint2 bytes = *reinterpret_cast<const uint2*>(stage + scales_at);
-        uint32_t s[4];
-        s[0] = __byte_perm(bytes.x, 0, 0x1404) >> 1;  // bytes 0 and 1, each shifted by 7 in its half
-        s[1] = __byte_perm(bytes.x, 0, 0x3424) >> 1;
-        s[2] = __byte_perm(bytes.y, 0, 0x1404) >> 1;
-        s[3] = __byte_perm(bytes.y, 0, 0x3424) >> 1;
-        if (__builtin_expect(keys < 128, 0)) {  // tokens past the end count 0 whatever is stored there
+  for (int u = team;; u += C::kTeams) {  // halves
+    if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
+    const int keys = sb.half_keys[st.at];
+    if (keys == 0) return;
+    if (u >= C::kBuffers && !qa_wait(&sb.v_free[vb.at], vb.phase ^ 1, wt)) return;
+    tc_fence_after_sync();
+    if (on) {
+      const uint8_t* stage = ring + st.at * C::kStageBytes;
+      const uint2 bytes = *reinterpret_cast<const uint2*>(stage + scales_at);
+      uint32_t s[4];
+      s[0] = __byte_perm(bytes.x, 0, 0x1404) >> 1;  // bytes 0 and 1, each shifted by 7 in its half
+      s[1] = __byte_perm(bytes.x, 0, 0x3424) >> 1;
+      s[2] = __byte_perm(bytes.y, 0, 0x1404) >> 1;
+      s[3] = __byte_perm(bytes.y, 0, 0x3424) >> 1;
+      if (__builtin_expect(keys < 128, 0)) {  // tokens past the end count 0 whatever is stored there
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            if (stoken + 2 * k >= keys) s[k] = 0;
-            if (stoken + 2 * k + 1 >= keys) s[k] &= 0xFFFFu;
-          }
-        }
-        __syncwarp();  // the scales of the half before have been read
-        sb.value_scales[quarter][lane] = *reinterpret_cast<const int4*>(s);
-        __syncwarp();
-        const int4* scales = &sb.value_scales[quarter][lane & 16];
-#pragma unroll 2
-        for (int token = 0; token < 128; token += 32) {
-          uint32_t w[BITS], r[16];
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {  // 16 tokens: 8 or 16 bytes
-            const int x = token + 16 * j, off = x & (c.page - 1);
-            const uint8_t* from =
-                stage + (x >> c.page_shift) * c.head_bytes + values_at + off / T * (D * piece) + off % T * BITS / 8;
-            if constexpr (BITS == 8) {
-              *reinterpret_cast<uint4*>(w + 4 * j) = *reinterpret_cast<const uint4*>(from);
-            } else if (T == 32) {
-              if (j == 0) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(from);
-            } else {
-              *reinterpret_cast<uint2*>(w + 2 * j) = *reinterpret_cast<const uint2*>(from);
-            }
-          }
-          if (BITS == 8 && __builtin_expect(token + 32 > keys, 0)) {  // a code may be NaN there
-#pragma unroll
-            for (int k = 0; k < BITS; ++k) {
-              const int n = min(max(keys - token - 4 * k, 0), 4);
-              w[k] = n == 4 ? w[k] : w[k] & ((1u << 8 * n) - 1u);
-            }
-          }
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {  // 8 tokens
-            const int4 f = scales[token / 8 + q];
-            const uint32_t fs[4] = {(uint32_t)f.x, (uint32_t)f.y, (uint32_t)f.z, (uint32_t)f.w};
-            constexpr int kPairs = QaDecode<BITS>::kPairs;
-#pragma unroll
-            for (int k = 0; k < BITS / 4; ++k) {
-              uint32_t x[kPairs];
-              QaDecode<BITS>::pairs(w[q * (BITS / 4) + k], x);
-#pragma unroll
-              for (int j = 0; j < kPairs; ++j) r[4 * q + k * kPairs + j] = q_mul2(x[j], fs[k * kPairs + j]);
-            }
-          }
-          tmem_st_32x32b_x16(to + 64 * vb.at + token / 2, r);
+        for (int k = 0; k < 4; ++k) {
+          if (stoken + 2 * k >= keys) s[k] = 0;
+          if (stoken + 2 * k + 1 >= keys) s[k] &= 0xFFFFu;
         }
       }
+      __syncwarp();  // the scales of the half before have been read
+      sb.value_scales[4 * team + quarter][lane] = *reinterpret_cast<const int4*>(s);
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sb.empty[st.at]);
-      tmem_st_wait();
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sb.v_ready[vb.at]);
+      const int4* scales = &sb.value_scales[4 * team + quarter][lane & 16];
+#pragma unroll 2
+      for (int token = 0; token < 128; token += 32) {
+        uint32_t w[BITS], r[16];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {  // 16 tokens: 8 or 16 bytes
+          const int x = token + 16 * j, off = x & (c.page - 1);
+          const uint8_t* from =
+              stage + (x >> c.page_shift) * c.head_bytes + values_at + off / T * (D * piece) + off % T * BITS / 8;
+          if constexpr (BITS == 8) {
+            *reinterpret_cast<uint4*>(w + 4 * j) = *reinterpret_cast<const uint4*>(from);
+          } else if (T == 32) {
+            if (j == 0) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(from);
+          } else {
+            *reinterpret_cast<uint2*>(w + 2 * j) = *reinterpret_cast<const uint2*>(from);
+          }
+        }
+        if (BITS == 8 && __builtin_expect(token + 32 > keys, 0)) {  // a code may be NaN there
+#pragma unroll
+          for (int k = 0; k < BITS; ++k) {
+            const int n = min(max(keys - token - 4 * k, 0), 4);
+            w[k] = n == 4 ? w[k] : w[k] & ((1u << 8 * n) - 1u);
+          }
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {  // 8 tokens
+          const int4 f = scales[token / 8 + q];
+          const uint32_t fs[4] = {(uint32_t)f.x, (uint32_t)f.y, (uint32_t)f.z, (uint32_t)f.w};
+          constexpr int kPairs = QaDecode<BITS>::kPairs;
+#pragma unroll
+          for (int k = 0; k < BITS / 4; ++k) {
+            uint32_t x[kPairs];
+            QaDecode<BITS>::pairs(w[q * (BITS / 4) + k], x);
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) r[4 * q + k * kPairs + j] = q_mul2(x[j], fs[k * kPairs + j]);
+          }
+        }
+        tmem_st_32x32b_x16(to + 64 * vb.at + token / 2, r);
+      }
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.empty[st.at]);
+    tmem_st_wait();
+    tc_fence_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.v_ready[vb.at]);
+#pragma unroll
+    for (int k = 0; k < C::kTeams; ++k) {
       st.next();
       vb.next();
     }
@@ -795,43 +836,21 @@ __device__ void qa_values(const QaParams& p, uint8_t* ring, QA_SHARED& sb, const
 }
 
 // ------------------------------------------------------------------- softmax
-// 16 lanes x 8 columns a time: thread i holds row i / 4 (and that + 8, in the
-// other two), columns 2 (i % 4) and the next.
-template <int G>
-struct QaFragments {
-  uint32_t r[4 * G];
-  __device__ __forceinline__ void load(uint32_t at) {
-    if constexpr (G == 8) {
-      asm volatile(
-          "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
-          "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-          "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-          : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-            "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-            "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-            "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-          : "r"(at));
-    } else {
-      asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                   : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                   : "r"(at));
-    }
-  }
-  __device__ __forceinline__ void wait() {  // nothing reads the registers before it
-    if constexpr (G == 8) {
-      tmem_ld_wait(r);
-    } else {
-      asm volatile("tcgen05.wait::ld.sync.aligned;"
-                   : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
-                   :
-                   : "memory");
-    }
-  }
-  __device__ __forceinline__ void give(float (&s)[G][4]) const {
-#pragma unroll
-    for (int k = 0; k < 4 * G; ++k) s[k / 4][k % 4] = __uint_as_float(r[k]);
-  }
-};
+// Fragments of 16 lanes x 8 columns: thread i holds row i / 4 in two registers
+// and that + 8 in the other two, columns 2 (i % 4) and the next.
+__device__ __forceinline__ void qa_load_8(uint32_t at, uint32_t (&r)[4]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at));
+}
+__device__ __forceinline__ void qa_load_16(uint32_t at, uint32_t (&a)[4], uint32_t (&b)[4]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3])
+               : "r"(at));
+}
+__device__ __forceinline__ void qa_load_wait(uint32_t (&r)[4]) {  // nothing reads the registers before it
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]) : : "memory");
+}
 
 __device__ __forceinline__ bool qa_vote(bool x) {  // of the 128 softmax threads
   uint32_t any;
@@ -846,6 +865,143 @@ __device__ __forceinline__ bool qa_vote(bool x) {  // of the 128 softmax threads
   return any != 0;
 }
 
+// What a step has to do now and then stands apart, so that the code of most
+// steps is short: with all of it in one loop the four warps spent more time on
+// fetching instructions than on anything else (2900 clk a step of 256 keys).
+
+// The end of a segment, the step before t: O, or a partial result.
+template <int D, int NMAX, uint32_t TMEM_O, class Shared>
+__device__ __noinline__ bool qa_segment_end(const QaParams& p, Shared& sb, const QaWait& wt, int t, int which,
+                                            bool faulty) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, u = t - 1;
+  if (!qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt)) return false;
+  tc_fence_after_sync();
+  const int4 e0 = sb.sched[u % kQaSched][0], e1 = sb.sched[u % kQaSched][1];
+  const int rows = qa_rows(e0.x), kind = qa_kind(e0.x);
+  const bool direct = e0.z < 0;
+  const int slot_rows = kind == kQaPrefix ? kQaRows : min(p.rows, kQaRows);
+#pragma unroll 1
+  for (int n0 = 0; n0 < rows; n0 += 16) {
+    const int mine = n0 + (lane & 15);
+    const float l = sb.sums[which][0][mine] + sb.sums[which][1][mine] + sb.sums[which][2][mine] + sb.sums[which][3][mine];
+    const float top = -sb.shift[which][mine];
+    if (!direct && w == 0 && lane < 16 && mine < rows)
+      p.work.ml[kind][(size_t)e0.z * slot_rows + mine] = faulty ? make_float2(0.0f, NAN) : make_float2(top, l);
+    const float inv = l > 0.0f && !faulty && top > -INFINITY ? 1.0f / l : 0.0f;
+    if (32 * w < D) {
+      const int d = 32 * w + lane;
+      uint32_t v[16];
+      tmem_ld_32x32b_x16(((uint32_t)(32 * w) << 16) + TMEM_O + n0, v);
+      tmem_ld_wait(v);
+      float* part = p.work.O[kind] + ((size_t)(direct ? 0 : e0.z) * slot_rows + n0) * D + d;
+      uint16_t* out = reinterpret_cast<uint16_t*>(p.O) +
+                      (((size_t)e0.w * p.cache.n_kv_heads + e1.x) * p.rows + e1.y + n0) * D + d;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const float f = __shfl_sync(0xffffffffu, inv, k);
+        if (n0 + k >= rows) break;
+        if (direct) {
+          const float x = f == 0.0f ? 0.0f : __uint_as_float(v[k]) * f;
+          out[k * D] = p.fp16 ? __half_as_ushort(__float2half_rn(x)) : __bfloat16_as_ushort(__float2bfloat16_rn(x));
+        } else {
+          part[k * D] = __uint_as_float(v[k]);
+        }
+      }
+    }
+  }
+  tc_fence_before_sync();
+  return true;
+}
+
+// New references of step t's rows (at the start of a segment, or where a
+// numerator passed 2^15), the end of the segment before, or of everything.
+// All four warps; `ok`: this warp's waits have not run out.  Returns 0: that is
+// all, 1: go on, 2: a wait has run out, which the next vote will tell.
+template <int D, int NMAX, int H, uint32_t TMEM_S, uint32_t TMEM_O, class Shared>
+__device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait& wt, int t, int seg, bool ok,
+                                    bool faulty) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, b = t & 1;
+  const uint32_t lane_tmem = (uint32_t)(32 * w) << 16;
+  const int2 e = ok ? *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]) : make_int2(kQaEnd, 0);
+  const int rows = qa_rows(e.x);
+  bool end = e.x & kQaEnd;
+  const bool first = e.x & kQaFirst;
+  float scale = 1.0f;
+  if (ok && !end) {
+    scale = sb.q_scale[seg & 1];
+    // The largest logit of each row among this warp's keys.
+#pragma unroll 1
+    for (int g = 0; 8 * g < rows; g += 2) {
+      uint32_t r[2 * H][2][4];
+#pragma unroll
+      for (int h = 0; h < 2 * H; ++h)
+        qa_load_16(lane_tmem + ((uint32_t)(16 * (h & 1)) << 16) + TMEM_S + (b * H + (h >> 1)) * NMAX + 8 * g, r[h][0], r[h][1]);
+#pragma unroll
+      for (int h = 0; h < 2 * H; ++h) {
+        qa_load_wait(r[h][0]);
+        qa_load_wait(r[h][1]);
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int n = 8 * (g + k) + 2 * (lane & 3);
+        const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][n]);
+        float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < 4 * H; ++h) {
+          const uint32_t* x = r[h >> 1][k] + 2 * (h & 1);
+          const int key = e.y + 128 * (h >> 2) + 32 * w + 8 * (h & 3) + lane / 4;
+          if (key < lim.x) m0 = fmaxf(m0, __uint_as_float(x[0]));
+          if (key < lim.y) m1 = fmaxf(m1, __uint_as_float(x[1]));
+        }
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) {
+          m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, x));
+          m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, x));
+        }
+        if (lane < 4) *reinterpret_cast<float2*>(&sb.warp_max[w][n]) = make_float2(m0, m1);
+      }
+    }
+    tc_fence_before_sync();
+  }
+  if (lane == 0) sb.warp_ok[w] = ok;
+  named_barrier_sync(2, 128);
+  if (!(sb.warp_ok[0] && sb.warp_ok[1] && sb.warp_ok[2] && sb.warp_ok[3])) return 0;
+  if (t > 0 && (first || end)) ok = qa_segment_end<D, NMAX, TMEM_O>(p, sb, wt, t, (seg ^ first) & 1, faulty);
+  if (end) return 0;
+  const int n = threadIdx.x;
+  if (n >= rows && n < NMAX) {  // rows that are not there (their queries are 0)
+    sb.shift[seg & 1][n] = INFINITY;
+    sb.factor[n] = 1.0f;
+  } else if (n < rows) {
+    const float m = fmaxf(fmaxf(sb.warp_max[0][n], sb.warp_max[1][n]), fmaxf(sb.warp_max[2][n], sb.warp_max[3][n]));
+    const float old = first ? INFINITY : sb.shift[seg & 1][n];
+    const float moved = fminf(old, 7.0f - m * scale);
+    sb.shift[seg & 1][n] = moved;
+    sb.factor[n] = moved == INFINITY ? 1.0f : ex2_approx(moved - old);
+  }
+  named_barrier_sync(2, 128);
+  if (!first && ok) {  // O in units of the new references
+    const int u = t - 1;
+    if ((ok = qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt))) {
+      tc_fence_after_sync();
+      if (32 * w < D) {
+#pragma unroll 1
+        for (int c = 0; 16 * c < rows; ++c) {
+          uint32_t v[16];
+          tmem_ld_32x32b_x16(lane_tmem + TMEM_O + 16 * c, v);
+          tmem_ld_wait(v);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * sb.factor[16 * c + k]);
+          tmem_st_32x32b_x16(lane_tmem + TMEM_O + 16 * c, v);
+        }
+        tmem_st_wait();
+      }
+      tc_fence_before_sync();
+    }
+  }
+  return ok ? 1 : 2;
+}
+
 template <int D, int BITS, int NMAX>
 __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, const QaWait& wt) {
   using C = QaCfg<D, BITS, NMAX>;
@@ -857,252 +1013,139 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, c
   // (n & 7); this lane gives the address of row lane & 7 of matrix lane >> 3.
   const uint32_t p_at = smem_u32(p_tiles) + (w >> 1) * C::kBoxBytes + (lane & 7) * 128 +
                         ((((w & 1) * 4 + (lane >> 3)) ^ (lane & 7)) << 4);
-  float shift[G][2], sum[G][2];  // added to the logits: 7 minus the reference, infinite where there is none yet
+  float shift[G][2], sum[G][2];
   float scale = 1.0f;
   int seg = -1, min_lim = 0;
-  bool ok = true, faulty = false, pending = false;
-  int4 e0 = make_int4(0, 0, 0, 0), e1 = e0, o0 = e0, o1 = e0;
+  bool ok = true, faulty = false;
 #pragma unroll
   for (int g = 0; g < G; ++g) shift[g][0] = shift[g][1] = sum[g][0] = sum[g][1] = 0.0f;
-  // Once a wait of a warp has run out, the next vote ends all four.
+  // Once a wait of a warp has run out, the next vote ends all four; every step
+  // has one.
 #pragma unroll 1
   for (int t = 0;; ++t) {
     const int b = t & 1;
-    ok = ok && qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt);
-    if (ok) {
-      e0 = sb.sched[t % kQaSched][0];
-      e1 = sb.sched[t % kQaSched][1];
+    ok = ok && qa_wait(&sb.s_full[b], (t >> 1) & 1, wt) &&
+         (t < 2 || qa_wait(&sb.pv_done[b], ((t >> 1) - 1) & 1, wt));
+    const int2 e = *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]);
+    const int info = ok ? e.x : kQaEnd, rows = qa_rows(info);
+    bool turn = info & (kQaFirst | kQaEnd), turned = false;
+    if (info & kQaFirst) {
+      ++seg;
+      scale = sb.q_scale[seg & 1];
+      min_lim = sb.min_lim[seg & 1];
     }
-    const int flags = e0.x & 255, rows = qa_rows(e0.x);
-    const bool end = flags & kQaEnd, first = flags & kQaFirst;
-    float s[H][2][G][4];
-    bool raise = false;
-    uint32_t dead = 0;  // of the rows of this thread's columns, those that see nothing anywhere
-    if (ok && !end) {
-      if (first) {
-        ++seg;
-        faulty = false;
-        ok = qa_wait(&sb.q_ready[seg & 1], (seg >> 1) & 1, wt);
-        scale = sb.q_scale[seg & 1];
-        min_lim = sb.min_lim[seg & 1];
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          shift[g][0] = shift[g][1] = INFINITY;
-          sum[g][0] = sum[g][1] = 0.0f;
-        }
-      }
-      if (flags & kQaFaulty) faulty = true;
-      ok = ok && qa_wait(&sb.s_full[b], (t >> 1) & 1, wt);
-    }
-    if (ok && !end) {
-      tc_fence_after_sync();
-      {
-        QaFragments<G> f[H][2];
-#pragma unroll
-        for (int h = 0; h < H; ++h) {
-          f[h][0].load(lane_tmem + C::kTmemS + (b * H + h) * NMAX);
-          f[h][1].load(lane_tmem + (16u << 16) + C::kTmemS + (b * H + h) * NMAX);
-        }
-#pragma unroll
-        for (int h = 0; h < H; ++h) {
-          f[h][0].wait();
-          f[h][1].wait();
-          f[h][0].give(s[h][0]);
-          f[h][1].give(s[h][1]);
-        }
-      }
-      tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sb.s_free[b]);
-      // Keys that a row does not see count nothing, whatever S is (a step of 128
-      // keys of 256 has none in its second half).
-      if (__builtin_expect(e0.y + 128 * H > min_lim, 0)) {
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          if (8 * g >= rows) break;
-          const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][8 * g + col0]);
-          const int a = lim.x - e0.y - key0, c = lim.y - e0.y - key0;
-#pragma unroll
-          for (int h = 0; h < 4 * H; ++h) {
-            float* x = s[h >> 2][(h >> 1) & 1][g] + 2 * (h & 1);
-            const int key = 128 * (h >> 2) + 8 * (h & 3);
-            if (key >= a) x[0] = -INFINITY;
-            if (key >= c) x[1] = -INFINITY;
-          }
-        }
-      }
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        if (8 * g >= rows) break;
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float m = -INFINITY;
-#pragma unroll
-          for (int h = 0; h < 2 * H; ++h) m = fmaxf(m, fmaxf(s[h >> 1][h & 1][g][c], s[h >> 1][h & 1][g][2 + c]));
-          raise |= fmaf(m, scale, shift[g][c]) > 15.0f;
-        }
-      }
-      if (flags & kQaLast) {
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          if (8 * g >= rows) break;
-          const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][8 * g + col0]);
-          dead |= (uint32_t)(lim.x <= 0) << (2 * g) | (uint32_t)(lim.y <= 0) << (2 * g + 1);
-        }
-        __syncwarp();  // the limits have been read
-        if (lane == 0) mbar_arrive(&sb.q_free[seg & 1]);
-      }
-    }
-    const bool raised = qa_vote(raise || !ok);
-    if (__builtin_expect(raised, 0)) {
-      // New references: the largest logits of the step's keys.
-      if (ok && !end) {
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          if (8 * g >= rows) break;
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            float m = -INFINITY;
-#pragma unroll
-            for (int h = 0; h < 2 * H; ++h) m = fmaxf(m, fmaxf(s[h >> 1][h & 1][g][c], s[h >> 1][h & 1][g][2 + c]));
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-            if (lane < 4) sb.warp_max[w][8 * g + col0 + c] = m;
-          }
-        }
-      }
-      if (lane == 0) sb.warp_ok[w] = ok;
-      named_barrier_sync(2, 128);
-      if (!(sb.warp_ok[0] && sb.warp_ok[1] && sb.warp_ok[2] && sb.warp_ok[3])) return;
-      // All four warps have a step here: one that has seen the end votes for nothing.
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        if (8 * g >= rows) break;
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int n = 8 * g + col0 + c;
-          const float m =
-              fmaxf(fmaxf(sb.warp_max[0][n], sb.warp_max[1][n]), fmaxf(sb.warp_max[2][n], sb.warp_max[3][n]));
-          const float moved = fminf(shift[g][c], 7.0f - m * scale);
-          // 0 where there was no reference yet, 1 where there still is none.
-          const float f = moved == INFINITY ? 1.0f : ex2_approx(moved - shift[g][c]);
-          shift[g][c] = moved;
-          sum[g][c] *= f;
-          if (w == 0 && lane < 4) sb.factor[n] = f;
-        }
-      }
-      named_barrier_sync(2, 128);
-    }
-    // The end of the segment before this step.
-    if (__builtin_expect(pending, 0)) {
-      pending = false;
-      const int u = t - 1;
-      if (!(ok = qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt))) continue;
-      tc_fence_after_sync();
-      const int n_rows = qa_rows(o0.x), kind = qa_kind(o0.x), which = o1.z;
-      const bool direct = o0.z < 0, o_faulty = o1.w;
-      constexpr int kParts = (NMAX + 31) / 32;
-      float l[kParts];
-      const int slot_rows = kind == kQaPrefix ? kQaRows : min(p.rows, kQaRows);
-#pragma unroll
-      for (int k = 0; k < kParts; ++k) {
-        const int n = min(32 * k + lane, NMAX - 1);
-        l[k] = sb.sums[which][0][n] + sb.sums[which][1][n] + sb.sums[which][2][n] + sb.sums[which][3][n];
-        const float top = sb.top[which][n];
-        if (!direct && w == 0 && 32 * k + lane < n_rows)
-          p.work.ml[kind][(size_t)o0.z * slot_rows + 32 * k + lane] =
-              o_faulty ? make_float2(0.0f, NAN) : make_float2(top, l[k]);
-        l[k] = l[k] > 0.0f && !o_faulty && top > -INFINITY ? 1.0f / l[k] : 0.0f;
-      }
-      if (32 * w < D) {
-        const int d = 32 * w + lane;
-        float* part = p.work.O[kind] + (size_t)(direct ? 0 : o0.z) * slot_rows * D + d;
-        uint16_t* out = reinterpret_cast<uint16_t*>(p.O) +
-                        (((size_t)o0.w * p.cache.n_kv_heads + o1.x) * p.rows + o1.y) * D + d;
+    const bool masked = e.y + 128 * H > min_lim;
+    tc_fence_after_sync();
+    float part[G][2];
 #pragma unroll 1
-        for (int c = 0; 16 * c < n_rows; ++c) {
-          uint32_t v[16];
-          tmem_ld_32x32b_x16(lane_tmem + C::kTmemO + 16 * c, v);
-          tmem_ld_wait(v);
-          const float lc = kParts == 1 ? l[0] : c < 2 ? l[0] : l[kParts - 1];
+    for (;;) {
+      if (!turn) {
+        // P with the references as they are, and whether a numerator passes 2^15.
+        float top = -INFINITY;
+        uint32_t s[2][2 * H][2][4];
+        auto load = [&](int g, uint32_t (&r)[2 * H][2][4]) {
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const int n = 16 * c + k;
-            const float inv = __shfl_sync(0xffffffffu, lc, n & 31);
-            if (n >= n_rows) break;
-            if (direct) {
-              const float x = inv == 0.0f ? 0.0f : __uint_as_float(v[k]) * inv;
-              out[n * D] = p.fp16 ? __half_as_ushort(__float2half_rn(x)) : __bfloat16_as_ushort(__float2bfloat16_rn(x));
-            } else {
-              part[n * D] = __uint_as_float(v[k]);
+          for (int h = 0; h < 2 * H; ++h)
+            qa_load_16(lane_tmem + ((uint32_t)(16 * (h & 1)) << 16) + C::kTmemS + (b * H + (h >> 1)) * NMAX + 8 * g, r[h][0],
+                       r[h][1]);
+        };
+        load(0, s[0]);
+#pragma unroll
+        for (int g2 = 0; g2 < G; g2 += 2) {
+          if (8 * g2 >= rows) break;
+          uint32_t(&r)[2 * H][2][4] = s[(g2 >> 1) & 1];
+#pragma unroll
+          for (int h = 0; h < 2 * H; ++h) {
+            qa_load_wait(r[h][0]);
+            qa_load_wait(r[h][1]);
+          }
+          if (g2 + 2 < G && 8 * (g2 + 2) < rows) load(g2 + 2, s[((g2 >> 1) + 1) & 1]);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int g = g2 + k;
+            if (8 * g >= rows) break;
+            if (masked) {  // keys that a row does not see count nothing, whatever S is
+              const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][8 * g + col0]);
+              const int a = lim.x - e.y - key0, c = lim.y - e.y - key0;
+#pragma unroll
+              for (int h = 0; h < 4 * H; ++h) {
+                uint32_t* x = r[h >> 1][k] + 2 * (h & 1);
+                const int key = 128 * (h >> 2) + 8 * (h & 3);
+                if (key >= a) x[0] = 0xFF800000u;
+                if (key >= c) x[1] = 0xFF800000u;
+              }
             }
+            float l0 = 0.0f, l1 = 0.0f;
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+              uint32_t pk[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const uint32_t* x = r[2 * h + (j >> 1)][k] + 2 * (j & 1);
+                const float x0 = fmaf(__uint_as_float(x[0]), scale, shift[g][0]);
+                const float x1 = fmaf(__uint_as_float(x[1]), scale, shift[g][1]);
+                top = fmax3(top, x0, x1);
+                const float a = ex2_approx(x0), c = ex2_approx(x1);
+                l0 += a;
+                l1 += c;
+                pk[j] = qa_pack_half(a, c);
+              }
+              asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
+                               p_at + b * C::kPBytes + 2 * h * C::kBoxBytes + g * 1024),
+                           "r"(pk[0]), "r"(pk[1]), "r"(pk[2]), "r"(pk[3])
+                           : "memory");
+            }
+            part[g][0] = l0;
+            part[g][1] = l1;
           }
         }
+        if (turned) break;
+        turn = top > 15.0f;
       }
-      tc_fence_before_sync();
-    }
-    if (end) return;
-    if (__builtin_expect(raised && !first, 0)) {  // O in units of the new references
-      const int u = t - 1;
-      if (!(ok = qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt))) continue;
-      tc_fence_after_sync();
-      if (32 * w < D) {
-#pragma unroll 1
-        for (int c = 0; 16 * c < rows; ++c) {
-          uint32_t v[16];
-          tmem_ld_32x32b_x16(lane_tmem + C::kTmemO + 16 * c, v);
-          tmem_ld_wait(v);
+      if (!qa_vote(turn)) break;
+      const int next = qa_turn<D, NMAX, H, C::kTmemS, C::kTmemO>(p, sb, wt, t, seg, ok, faulty);
+      if (next == 0) return;
+      ok = next == 1;
+      if (info & kQaFirst) faulty = false;
 #pragma unroll
-          for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * sb.factor[16 * c + k]);
-          tmem_st_32x32b_x16(lane_tmem + C::kTmemO + 16 * c, v);
-        }
-        tmem_st_wait();
+      for (int g = 0; g < G; ++g) {
+        if (8 * g >= rows) break;
+        const float2 to = *reinterpret_cast<const float2*>(&sb.shift[seg & 1][8 * g + col0]);
+        const float2 f = *reinterpret_cast<const float2*>(&sb.factor[8 * g + col0]);
+        // A row without a reference sees nothing in this segment.
+        shift[g][0] = to.x == INFINITY ? 0.0f : to.x;
+        shift[g][1] = to.y == INFINITY ? 0.0f : to.y;
+        sum[g][0] = info & kQaFirst ? 0.0f : sum[g][0] * f.x;
+        sum[g][1] = info & kQaFirst ? 0.0f : sum[g][1] * f.y;
       }
-      tc_fence_before_sync();
+      turn = false;
+      turned = true;
     }
-    if (t >= 2 && !(ok = qa_wait(&sb.pv_done[b], ((t >> 1) - 1) & 1, wt))) continue;
+    if (info & kQaFaulty) faulty = true;
+    tc_fence_before_sync();
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive(&sb.s_free[b]);
+      mbar_arrive(&sb.p_ready[b]);
+    }
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       if (8 * g >= rows) break;
-      const float sh0 = shift[g][0] == INFINITY ? 0.0f : shift[g][0], sh1 = shift[g][1] == INFINITY ? 0.0f : shift[g][1];
-#pragma unroll
-      for (int h = 0; h < H; ++h) {
-        uint32_t pk[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float* x = s[h][k >> 1][g] + 2 * (k & 1);
-          const float a = ex2_approx(fmaf(x[0], scale, sh0)), c = ex2_approx(fmaf(x[1], scale, sh1));
-          sum[g][0] += a;
-          sum[g][1] += c;
-          pk[k] = qa_pack_half(a, c);
-        }
-        asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
-                         p_at + b * C::kPBytes + 2 * h * C::kBoxBytes + g * 1024),
-                     "r"(pk[0]), "r"(pk[1]), "r"(pk[2]), "r"(pk[3])
-                     : "memory");
-      }
+      sum[g][0] += part[g][0];
+      sum[g][1] += part[g][1];
     }
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sb.p_ready[b]);
-    if (flags & kQaLast) {
-      pending = true;
-      o0 = e0;
-      o1 = make_int4(e1.x, e1.y, seg & 1, faulty);
+    if (info & kQaLast) {
+      if (lane == 0) mbar_arrive(&sb.q_free[seg & 1]);  // the limits have been read
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         if (8 * g >= rows) break;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float x = sum[g][c];
-          x += __shfl_xor_sync(0xffffffffu, x, 4);
-          x += __shfl_xor_sync(0xffffffffu, x, 8);
-          x += __shfl_xor_sync(0xffffffffu, x, 16);
-          const int n = 8 * g + col0 + c;
-          if (lane < 4) sb.sums[seg & 1][w][n] = x;
-          if (w == 0 && lane < 4) sb.top[seg & 1][n] = (dead >> (2 * g + c)) & 1 ? -INFINITY : -shift[g][c];
+        for (int x = 4; x < 32; x <<= 1) {
+          sum[g][0] += __shfl_xor_sync(0xffffffffu, sum[g][0], x);
+          sum[g][1] += __shfl_xor_sync(0xffffffffu, sum[g][1], x);
         }
+        if (lane < 4) *reinterpret_cast<float2*>(&sb.sums[seg & 1][w][8 * g + col0]) = make_float2(sum[g][0], sum[g][1]);
       }
     }
   }
@@ -1149,6 +1192,7 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
   __shared__ QA_SHARED sb;
   static_assert(C::kSmem + sizeof(sb) <= 227 * 1024, "shared memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int kOther = C::kThreads / 32 - 4;
   if (threadIdx.x == 0) {
     sb.abort = 0;
     for (int i = 0; i < C::kStages; ++i) {
@@ -1164,7 +1208,7 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sb.p_ready[i], 4);
-      mbar_init(&sb.s_full[i], 1);
+      mbar_init(&sb.s_full[i], 2);
       mbar_init(&sb.s_free[i], 4);
       mbar_init(&sb.pv_done[i], 1);
       mbar_init(&sb.q_ready[i], 1);
@@ -1173,7 +1217,7 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
     }
     fence_mbar_init();
   }
-  if (warp == 14) {
+  if (warp == kOther + 2) {
     tmem_alloc(&sb.tmem_base, 512);
     tmem_relinquish();
   }
@@ -1186,28 +1230,34 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
   const QaWait wt = {&sb.abort, p.cache.status, p.wait_ns};
 
   if (warp < 4) {
+    warpgroup_reg_inc<C::kRegsSoftmax>();
     qa_softmax<D, BITS, NMAX>(p, p_tiles, sb, wt);
-  } else if (warp < 8) {
-    qa_keys<D, BITS, NMAX>(p, ring, sb, wt);
-  } else if (warp < 12) {
-    qa_values<D, BITS, NMAX>(p, ring, sb, wt);
-  } else if (warp == 12) {
-    qa_producer<D, BITS, NMAX>(p, plan, ring, sb, wt);
-  } else if (warp == 13) {
-    qa_queries<D, BITS, NMAX>(p, plan, q_tiles, sb, wt);
-    // Where the merge finds its parts.
-    const int units = p.batch * p.cache.n_kv_heads * p.chunks;
-    for (int i = blockIdx.x * 32 + lane; i < units; i += gridDim.x * 32)
-      qa_sources(p, plan, i, p.work.sources + 2 * (size_t)i);
-  } else if (warp == 14) {
-    qa_products_s<D, BITS, NMAX>(p, q_tiles, sb, wt);
   } else {
-    qa_products_pv<D, BITS, NMAX>(p, p_tiles, sb, wt);
+    warpgroup_reg_dec<C::kRegsOther>();
+    if (warp < kOther) {
+      const int team = ((warp >> 2) - 1) >> 1;
+      if ((warp >> 2) & 1)
+        qa_keys<D, BITS, NMAX>(p, team, ring, sb, wt);
+      else
+        qa_values<D, BITS, NMAX>(p, team, ring, sb, wt);
+    } else if (warp == kOther) {
+      qa_producer<D, BITS, NMAX>(p, plan, ring, sb, wt);
+    } else if (warp == kOther + 1) {
+      qa_queries<D, BITS, NMAX>(p, plan, q_tiles, sb, wt);
+      // Where the merge finds its parts.
+      const int units = p.batch * p.cache.n_kv_heads * p.chunks;
+      for (int i = blockIdx.x * 32 + lane; i < units; i += gridDim.x * 32)
+        qa_sources(p, plan, i, p.work.sources + 2 * (size_t)i);
+    } else if (warp == kOther + 2) {
+      qa_products_s<D, BITS, NMAX>(p, q_tiles, sb, wt);
+    } else {
+      qa_products_pv<D, BITS, NMAX>(p, p_tiles, sb, wt);
+    }
   }
   __syncwarp();
   tc_fence_before_sync();
   __syncthreads();
-  if (warp == 14) {
+  if (warp == kOther + 2) {
     tc_fence_after_sync();
     tmem_dealloc(0, 512);
   }
