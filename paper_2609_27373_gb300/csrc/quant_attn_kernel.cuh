@@ -13,10 +13,10 @@
 // to 16 query rows an item), 128 in the wide one (up to 64).  The cache's side
 // moves by halves of 128 keys, one row of the product's M each.
 //
-// Warp roles (768 threads, 512 in the wide instance):
-//   a warpgroup  softmax: S^T from tensor memory in fragments of 8 keys x 8
+// Warp roles (768 threads, 640 in the wide instance):
+//   4 warps      softmax (8 in the wide instance, each 4 for 32 of the rows): S^T from tensor memory in fragments of 8 keys x 8
 //                rows, running maximum (raised only when a numerator passes
-//                2^15, which the four warps vote on), numerators as fp16 to
+//                2^15, which the warps vote on), numerators as fp16 to
 //                shared memory (P, the B operand of the second product), O's
 //                rescaling and the end of a segment;
 //   then in turn (two teams of each that take every other half, in the wide
@@ -49,10 +49,11 @@ template <int D, int BITS, int NMAX>
 struct QaCfg {
   static constexpr int kHalves = NMAX == 16 ? 2 : 1;  // of 128 keys, of a step
   static constexpr int kTeams = NMAX == 16 ? 2 : 1;    // of four warps that take the halves in turn, of K and of V
-  static constexpr int kThreads = 128 * (2 + 2 * kTeams);
-  // Registers: the block is launched with 80 or 128 a thread, which the roles split anew.
-  static constexpr int kRegsSoftmax = NMAX == 16 ? 120 : 200, kRegsOther = NMAX == 16 ? 72 : 104;
-  static_assert(128 * kRegsSoftmax + (kThreads - 128) * kRegsOther <= kThreads * (NMAX == 16 ? 80 : 128), "registers");
+  static constexpr int kGroups = NMAX == 16 ? 1 : 2;   // of four softmax warps
+  static constexpr int kThreads = 128 * (kGroups + 2 * kTeams + 1);
+  // Registers: a block is launched with 80 or 96 a thread; the narrow one's roles split them anew.
+  static constexpr int kRegsSoftmax = 120, kRegsOther = 72;
+  static_assert(NMAX > 16 || 128 * kRegsSoftmax + (kThreads - 128) * kRegsOther <= kThreads * 80, "registers");
   static constexpr int kBuffers = NMAX == 16 ? 3 : 2;  // of K and of V in tensor memory
   // Columns: K, V, S (two steps), O.
   static constexpr uint32_t kTmemK = 0, kTmemV = 64 * kBuffers, kTmemS = 128 * kBuffers,
@@ -65,7 +66,7 @@ struct QaCfg {
   static constexpr int kStageBytes = 128 / 16 * q_block_bytes(BITS, D, 16);  // 128 tokens, whatever the page size
   static constexpr int kMaxPlanBytes = 32 * 1024;
   static constexpr int kFixed = 2 * kQBytes + 2 * kPBytes;
-  static constexpr int kRoom = (218 * 1024 - 1024 - kMaxPlanBytes - kFixed) / kStageBytes;
+  static constexpr int kRoom = (214 * 1024 - 1024 - kMaxPlanBytes - kFixed) / kStageBytes;
   static constexpr int kStages = kRoom < 8 ? kRoom : 8;
   static constexpr int kPlanAt = kFixed + kStages * kStageBytes;
   static constexpr int kSmem = kPlanAt + kMaxPlanBytes + 1024;
@@ -87,29 +88,29 @@ __device__ __forceinline__ int qa_rows(int info) { return (info >> 8) & 255; }
 __device__ __forceinline__ int qa_kind(int info) { return (info >> 16) & 1; }
 __device__ __forceinline__ int qa_keys_of(int info) { return info >> 20; }
 
-template <int NS, int NB, int NT>
+template <int NS, int NB, int NT, int NG>
 struct QaShared {
   uint64_t full[NS], empty[NS];  // empty: 8 warps
   uint64_t sched_full[kQaSched];
   uint64_t k_ready[NB], v_ready[NB];  // 4 warps
   uint64_t k_free[NB], v_free[NB];    // products
-  uint64_t p_ready[2];                // 4 warps
-  uint64_t s_full[2], s_free[2];      // products; 4 warps
+  uint64_t p_ready[2];                // softmax warps
+  uint64_t s_full[2], s_free[2];      // products; softmax warps
   uint64_t pv_done[2];
-  uint64_t q_ready[2], q_free[2];  // q_free: the products and 4 warps
+  uint64_t q_ready[2], q_free[2];  // q_free: the products and the softmax warps
   uint64_t done[2];
   int4 sched[kQaSched][2];
   alignas(16) int lim[2][kQaRows];  // keys that a row sees, 0 for none
   int min_lim[2];            // the least of those that see any
   float q_scale[2];          // logits in base-2 units = S * q_scale
-  alignas(16) float warp_max[4][kQaRows];
+  alignas(16) float warp_max[4 * NG][kQaRows];
   alignas(16) float shift[2][kQaRows];  // added to a row's logits: 7 minus the reference, infinite where nothing is seen
   alignas(16) float factor[kQaRows];    // of O and the sums where the references have moved
-  alignas(16) float sums[2][4][kQaRows];
+  alignas(16) float sums[2][4 * NG][kQaRows];
   alignas(16) int4 value_scales[4 * NT][32];  // a warp's two groups x 128 tokens as fp16
   int half_keys[NS];  // keys of the half in a stage, 0 at the end
   uint32_t tmem_base;
-  int abort, warp_ok[4];
+  int abort, warp_ok[4 * NG];
 };
 
 // ---------------------------------------------------------------------- plan
@@ -372,7 +373,8 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                : "memory");
 }
 
-#define QA_SHARED QaShared<QaCfg<D, BITS, NMAX>::kStages, QaCfg<D, BITS, NMAX>::kBuffers, QaCfg<D, BITS, NMAX>::kTeams>
+#define QA_SHARED QaShared<QaCfg<D, BITS, NMAX>::kStages, QaCfg<D, BITS, NMAX>::kBuffers, QaCfg<D, BITS, NMAX>::kTeams, \
+                                QaCfg<D, BITS, NMAX>::kGroups>
 
 // ------------------------------------------------------------------ producer
 template <int D, int BITS, int NMAX>
@@ -852,18 +854,30 @@ __device__ __forceinline__ void qa_load_wait(uint32_t (&r)[4]) {  // nothing rea
   asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]) : : "memory");
 }
 
-__device__ __forceinline__ bool qa_vote(bool x) {  // of the 128 softmax threads
-  uint32_t any;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %1, 0;\n\t"
-      "barrier.cta.red.or.pred q, 1, 128, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(any)
-      : "r"((uint32_t)x)
-      : "memory");
-  return any != 0;
-}
+// A group of four softmax warps: the only one, or one with 32 of the rows to
+// itself.
+template <int NMAX>
+struct QaGroup {
+  static constexpr int kRows = NMAX == 16 ? 16 : 32;
+  int lane, w, i;  // of the warp; warp of the group (TMEM lanes 32 w ..), group
+  __device__ __forceinline__ QaGroup() : lane(threadIdx.x & 31), w((threadIdx.x >> 5) & 3), i(NMAX == 16 ? 0 : threadIdx.x >> 7) {}
+  __device__ __forceinline__ int row0() const { return kRows * i; }
+  __device__ __forceinline__ int rows(int all) const { return NMAX == 16 ? all : min(max(all - kRows * i, 0), kRows); }
+  __device__ __forceinline__ bool vote(bool x) const {
+    uint32_t any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.pred q, %2, 128, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(any)
+        : "r"((uint32_t)x), "r"(1 + 2 * i)
+        : "memory");
+    return any != 0;
+  }
+  __device__ __forceinline__ void sync() const { named_barrier_sync(2 + 2 * i, 128); }
+  __device__ __forceinline__ uint32_t lanes() const { return (uint32_t)(32 * w) << 16; }
+};
 
 // What a step has to do now and then stands apart, so that the code of most
 // steps is short: with all of it in one loop the four warps spent more time on
@@ -873,25 +887,28 @@ __device__ __forceinline__ bool qa_vote(bool x) {  // of the 128 softmax threads
 template <int D, int NMAX, uint32_t TMEM_O, class Shared>
 __device__ __noinline__ bool qa_segment_end(const QaParams& p, Shared& sb, const QaWait& wt, int t, int which,
                                             bool faulty) {
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, u = t - 1;
+  const QaGroup<NMAX> q;
+  const int u = t - 1;
   if (!qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt)) return false;
   tc_fence_after_sync();
   const int4 e0 = sb.sched[u % kQaSched][0], e1 = sb.sched[u % kQaSched][1];
-  const int rows = qa_rows(e0.x), kind = qa_kind(e0.x);
+  const int kind = qa_kind(e0.x), end = q.row0() + q.rows(qa_rows(e0.x));
   const bool direct = e0.z < 0;
   const int slot_rows = kind == kQaPrefix ? kQaRows : min(p.rows, kQaRows);
 #pragma unroll 1
-  for (int n0 = 0; n0 < rows; n0 += 16) {
-    const int mine = n0 + (lane & 15);
-    const float l = sb.sums[which][0][mine] + sb.sums[which][1][mine] + sb.sums[which][2][mine] + sb.sums[which][3][mine];
+  for (int n0 = q.row0(); n0 < end; n0 += 16) {
+    const int mine = n0 + (q.lane & 15);
+    float l = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) l += sb.sums[which][4 * q.i + k][mine];
     const float top = -sb.shift[which][mine];
-    if (!direct && w == 0 && lane < 16 && mine < rows)
+    if (!direct && q.w == 0 && q.lane < 16 && mine < end)
       p.work.ml[kind][(size_t)e0.z * slot_rows + mine] = faulty ? make_float2(0.0f, NAN) : make_float2(top, l);
     const float inv = l > 0.0f && !faulty && top > -INFINITY ? 1.0f / l : 0.0f;
-    if (32 * w < D) {
-      const int d = 32 * w + lane;
+    if (32 * q.w < D) {
+      const int d = 32 * q.w + q.lane;
       uint32_t v[16];
-      tmem_ld_32x32b_x16(((uint32_t)(32 * w) << 16) + TMEM_O + n0, v);
+      tmem_ld_32x32b_x16(q.lanes() + TMEM_O + n0, v);
       tmem_ld_wait(v);
       float* part = p.work.O[kind] + ((size_t)(direct ? 0 : e0.z) * slot_rows + n0) * D + d;
       uint16_t* out = reinterpret_cast<uint16_t*>(p.O) +
@@ -899,7 +916,7 @@ __device__ __noinline__ bool qa_segment_end(const QaParams& p, Shared& sb, const
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
         const float f = __shfl_sync(0xffffffffu, inv, k);
-        if (n0 + k >= rows) break;
+        if (n0 + k >= end) break;
         if (direct) {
           const float x = f == 0.0f ? 0.0f : __uint_as_float(v[k]) * f;
           out[k * D] = p.fp16 ? __half_as_ushort(__float2half_rn(x)) : __bfloat16_as_ushort(__float2bfloat16_rn(x));
@@ -915,41 +932,38 @@ __device__ __noinline__ bool qa_segment_end(const QaParams& p, Shared& sb, const
 
 // New references of step t's rows (at the start of a segment, or where a
 // numerator passed 2^15), the end of the segment before, or of everything.
-// All four warps; `ok`: this warp's waits have not run out.  Returns 0: that is
-// all, 1: go on, 2: a wait has run out, which the next vote will tell.
+// All four warps of a group; `ok`: this warp's waits have not run out.
+// Returns 0: that is all, 1: go on, 2: a wait has run out, which the next vote
+// will tell.
 template <int D, int NMAX, int H, uint32_t TMEM_S, uint32_t TMEM_O, class Shared>
 __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait& wt, int t, int seg, bool ok,
                                     bool faulty) {
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, b = t & 1;
-  const uint32_t lane_tmem = (uint32_t)(32 * w) << 16;
+  const QaGroup<NMAX> q;
+  const int lane = q.lane, b = t & 1;
   const int2 e = ok ? *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]) : make_int2(kQaEnd, 0);
-  const int rows = qa_rows(e.x);
-  bool end = e.x & kQaEnd;
-  const bool first = e.x & kQaFirst;
+  const int row0 = q.row0(), row_end = row0 + q.rows(qa_rows(e.x));
+  const bool end = e.x & kQaEnd, first = e.x & kQaFirst;
   float scale = 1.0f;
   if (ok && !end) {
     scale = sb.q_scale[seg & 1];
     // The largest logit of each row among this warp's keys.
 #pragma unroll 1
-    for (int g = 0; 8 * g < rows; g += 2) {
+    for (int n0 = row0; n0 < row_end; n0 += 16) {
       uint32_t r[2 * H][2][4];
 #pragma unroll
       for (int h = 0; h < 2 * H; ++h)
-        qa_load_16(lane_tmem + ((uint32_t)(16 * (h & 1)) << 16) + TMEM_S + (b * H + (h >> 1)) * NMAX + 8 * g, r[h][0], r[h][1]);
+        qa_load_16(q.lanes() + ((uint32_t)(16 * (h & 1)) << 16) + TMEM_S + (b * H + (h >> 1)) * NMAX + n0, r[h][0], r[h][1]);
 #pragma unroll
-      for (int h = 0; h < 2 * H; ++h) {
-        qa_load_wait(r[h][0]);
-        qa_load_wait(r[h][1]);
-      }
+      for (int h = 0; h < 4 * H; ++h) qa_load_wait(r[h >> 1][h & 1]);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const int n = 8 * (g + k) + 2 * (lane & 3);
+        const int n = n0 + 8 * k + 2 * (lane & 3);
         const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][n]);
         float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
         for (int h = 0; h < 4 * H; ++h) {
           const uint32_t* x = r[h >> 1][k] + 2 * (h & 1);
-          const int key = e.y + 128 * (h >> 2) + 32 * w + 8 * (h & 3) + lane / 4;
+          const int key = e.y + 128 * (h >> 2) + 32 * q.w + 8 * (h & 3) + lane / 4;
           if (key < lim.x) m0 = fmaxf(m0, __uint_as_float(x[0]));
           if (key < lim.y) m1 = fmaxf(m1, __uint_as_float(x[1]));
         }
@@ -958,46 +972,47 @@ __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait&
           m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, x));
           m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, x));
         }
-        if (lane < 4) *reinterpret_cast<float2*>(&sb.warp_max[w][n]) = make_float2(m0, m1);
+        if (lane < 4) *reinterpret_cast<float2*>(&sb.warp_max[4 * q.i + q.w][n]) = make_float2(m0, m1);
       }
     }
     tc_fence_before_sync();
   }
-  if (lane == 0) sb.warp_ok[w] = ok;
-  named_barrier_sync(2, 128);
-  if (!(sb.warp_ok[0] && sb.warp_ok[1] && sb.warp_ok[2] && sb.warp_ok[3])) return 0;
+  if (lane == 0) sb.warp_ok[4 * q.i + q.w] = ok;
+  q.sync();
+  const int from = 4 * q.i;
+  if (!(sb.warp_ok[from] && sb.warp_ok[from + 1] && sb.warp_ok[from + 2] && sb.warp_ok[from + 3])) return 0;
   if (t > 0 && (first || end)) ok = qa_segment_end<D, NMAX, TMEM_O>(p, sb, wt, t, (seg ^ first) & 1, faulty);
   if (end) return 0;
-  const int n = threadIdx.x;
-  if (n >= rows && n < NMAX) {  // rows that are not there (their queries are 0)
-    sb.shift[seg & 1][n] = INFINITY;
-    sb.factor[n] = 1.0f;
-  } else if (n < rows) {
-    const float m = fmaxf(fmaxf(sb.warp_max[0][n], sb.warp_max[1][n]), fmaxf(sb.warp_max[2][n], sb.warp_max[3][n]));
-    const float old = first ? INFINITY : sb.shift[seg & 1][n];
-    const float moved = fminf(old, 7.0f - m * scale);
-    sb.shift[seg & 1][n] = moved;
-    sb.factor[n] = moved == INFINITY ? 1.0f : ex2_approx(moved - old);
+  const int n = row0 + threadIdx.x % 128;
+  if (n < row0 + q.kRows) {
+    float moved = INFINITY, f = 1.0f;
+    if (n < row_end) {
+      const float m = fmaxf(fmaxf(sb.warp_max[from][n], sb.warp_max[from + 1][n]),
+                            fmaxf(sb.warp_max[from + 2][n], sb.warp_max[from + 3][n]));
+      const float old = first ? INFINITY : sb.shift[seg & 1][n];
+      moved = fminf(old, 7.0f - m * scale);
+      if (moved != INFINITY) f = ex2_approx(moved - old);
+    }
+    sb.shift[seg & 1][n] = moved;  // rows that are not there (their queries are 0) have none
+    sb.factor[n] = f;
   }
-  named_barrier_sync(2, 128);
+  q.sync();
   if (!first && ok) {  // O in units of the new references
     const int u = t - 1;
-    if ((ok = qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt))) {
+    if ((ok = qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt)) && 32 * q.w < D) {
       tc_fence_after_sync();
-      if (32 * w < D) {
 #pragma unroll 1
-        for (int c = 0; 16 * c < rows; ++c) {
-          uint32_t v[16];
-          tmem_ld_32x32b_x16(lane_tmem + TMEM_O + 16 * c, v);
-          tmem_ld_wait(v);
+      for (int n0 = row0; n0 < row_end; n0 += 16) {
+        uint32_t v[16];
+        tmem_ld_32x32b_x16(q.lanes() + TMEM_O + n0, v);
+        tmem_ld_wait(v);
 #pragma unroll
-          for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * sb.factor[16 * c + k]);
-          tmem_st_32x32b_x16(lane_tmem + TMEM_O + 16 * c, v);
-        }
-        tmem_st_wait();
+        for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * sb.factor[n0 + k]);
+        tmem_st_32x32b_x16(q.lanes() + TMEM_O + n0, v);
       }
-      tc_fence_before_sync();
+      tmem_st_wait();
     }
+    tc_fence_before_sync();
   }
   return ok ? 1 : 2;
 }
@@ -1005,29 +1020,29 @@ __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait&
 template <int D, int BITS, int NMAX>
 __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, const QaWait& wt) {
   using C = QaCfg<D, BITS, NMAX>;
-  constexpr int G = NMAX / 8, H = C::kHalves;
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int key0 = 32 * w + lane / 4, col0 = 2 * (lane & 3);
-  const uint32_t lane_tmem = (uint32_t)(32 * w) << 16;
+  const QaGroup<NMAX> q;
+  constexpr int G = q.kRows / 8, H = C::kHalves;
+  const int lane = q.lane;
+  const int key0 = 32 * q.w + lane / 4, col0 = q.row0() + 2 * (lane & 3);
+  const uint32_t s_at = q.lanes() + C::kTmemS + q.row0();
   // P: row n of 128 bytes in box (key / 64), 16-byte chunk ((key % 64) / 8) ^
   // (n & 7); this lane gives the address of row lane & 7 of matrix lane >> 3.
-  const uint32_t p_at = smem_u32(p_tiles) + (w >> 1) * C::kBoxBytes + (lane & 7) * 128 +
-                        ((((w & 1) * 4 + (lane >> 3)) ^ (lane & 7)) << 4);
+  const uint32_t p_at = smem_u32(p_tiles) + (q.w >> 1) * C::kBoxBytes + (q.row0() + (lane & 7)) * 128 +
+                        ((((q.w & 1) * 4 + (lane >> 3)) ^ (lane & 7)) << 4);
   float shift[G][2], sum[G][2];
   float scale = 1.0f;
   int seg = -1, min_lim = 0;
   bool ok = true, faulty = false;
 #pragma unroll
   for (int g = 0; g < G; ++g) shift[g][0] = shift[g][1] = sum[g][0] = sum[g][1] = 0.0f;
-  // Once a wait of a warp has run out, the next vote ends all four; every step
-  // has one.
+  // Once a wait of a warp has run out, the next vote ends all; every step has one.
 #pragma unroll 1
   for (int t = 0;; ++t) {
     const int b = t & 1;
     ok = ok && qa_wait(&sb.s_full[b], (t >> 1) & 1, wt) &&
          (t < 2 || qa_wait(&sb.pv_done[b], ((t >> 1) - 1) & 1, wt));
     const int2 e = *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]);
-    const int info = ok ? e.x : kQaEnd, rows = qa_rows(info);
+    const int info = ok ? e.x : kQaEnd, rows = q.rows(qa_rows(info));
     bool turn = info & (kQaFirst | kQaEnd), turned = false;
     if (info & kQaFirst) {
       ++seg;
@@ -1042,24 +1057,15 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, c
       if (!turn) {
         // P with the references as they are, and whether a numerator passes 2^15.
         float top = -INFINITY;
-        uint32_t s[2][2 * H][2][4];
-        auto load = [&](int g, uint32_t (&r)[2 * H][2][4]) {
-#pragma unroll
-          for (int h = 0; h < 2 * H; ++h)
-            qa_load_16(lane_tmem + ((uint32_t)(16 * (h & 1)) << 16) + C::kTmemS + (b * H + (h >> 1)) * NMAX + 8 * g, r[h][0],
-                       r[h][1]);
-        };
-        load(0, s[0]);
 #pragma unroll
         for (int g2 = 0; g2 < G; g2 += 2) {
           if (8 * g2 >= rows) break;
-          uint32_t(&r)[2 * H][2][4] = s[(g2 >> 1) & 1];
+          uint32_t r[2 * H][2][4];
 #pragma unroll
-          for (int h = 0; h < 2 * H; ++h) {
-            qa_load_wait(r[h][0]);
-            qa_load_wait(r[h][1]);
-          }
-          if (g2 + 2 < G && 8 * (g2 + 2) < rows) load(g2 + 2, s[((g2 >> 1) + 1) & 1]);
+          for (int h = 0; h < 2 * H; ++h)
+            qa_load_16(s_at + ((uint32_t)(16 * (h & 1)) << 16) + (b * H + (h >> 1)) * NMAX + 8 * g2, r[h][0], r[h][1]);
+#pragma unroll
+          for (int h = 0; h < 4 * H; ++h) qa_load_wait(r[h >> 1][h & 1]);
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const int g = g2 + k;
@@ -1102,7 +1108,7 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, c
         if (turned) break;
         turn = top > 15.0f;
       }
-      if (!qa_vote(turn)) break;
+      if (!q.vote(turn)) break;
       const int next = qa_turn<D, NMAX, H, C::kTmemS, C::kTmemO>(p, sb, wt, t, seg, ok, faulty);
       if (next == 0) return;
       ok = next == 1;
@@ -1145,7 +1151,8 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, c
           sum[g][0] += __shfl_xor_sync(0xffffffffu, sum[g][0], x);
           sum[g][1] += __shfl_xor_sync(0xffffffffu, sum[g][1], x);
         }
-        if (lane < 4) *reinterpret_cast<float2*>(&sb.sums[seg & 1][w][8 * g + col0]) = make_float2(sum[g][0], sum[g][1]);
+        if (lane < 4)
+          *reinterpret_cast<float2*>(&sb.sums[seg & 1][4 * q.i + q.w][8 * g + col0]) = make_float2(sum[g][0], sum[g][1]);
       }
     }
   }
@@ -1207,12 +1214,12 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
       mbar_init(&sb.v_free[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sb.p_ready[i], 4);
+      mbar_init(&sb.p_ready[i], 4 * C::kGroups);
       mbar_init(&sb.s_full[i], 2);
-      mbar_init(&sb.s_free[i], 4);
+      mbar_init(&sb.s_free[i], 4 * C::kGroups);
       mbar_init(&sb.pv_done[i], 1);
       mbar_init(&sb.q_ready[i], 1);
-      mbar_init(&sb.q_free[i], 5);
+      mbar_init(&sb.q_free[i], 4 * C::kGroups + 1);
       mbar_init(&sb.done[i], 1);
     }
     fence_mbar_init();
@@ -1229,17 +1236,17 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
   if (threadIdx.x == 0) griddep_launch_dependents();  // the merge waits for this grid's end
   const QaWait wt = {&sb.abort, p.cache.status, p.wait_ns};
 
-  if (warp < 4) {
-    warpgroup_reg_inc<C::kRegsSoftmax>();
+  if (warp < 4 * C::kGroups) {
+    if constexpr (NMAX == 16) warpgroup_reg_inc<C::kRegsSoftmax>();
     qa_softmax<D, BITS, NMAX>(p, p_tiles, sb, wt);
   } else {
-    warpgroup_reg_dec<C::kRegsOther>();
+    if constexpr (NMAX == 16) warpgroup_reg_dec<C::kRegsOther>();
     if (warp < kOther) {
-      const int team = ((warp >> 2) - 1) >> 1;
-      if ((warp >> 2) & 1)
-        qa_keys<D, BITS, NMAX>(p, team, ring, sb, wt);
-      else
+      const int k = warp / 4 - C::kGroups, team = k >> 1;
+      if (k & 1)
         qa_values<D, BITS, NMAX>(p, team, ring, sb, wt);
+      else
+        qa_keys<D, BITS, NMAX>(p, team, ring, sb, wt);
     } else if (warp == kOther) {
       qa_producer<D, BITS, NMAX>(p, plan, ring, sb, wt);
     } else if (warp == kOther + 1) {
