@@ -48,12 +48,9 @@ namespace wise {
 template <int D, int BITS, int NMAX>
 struct QaCfg {
   static constexpr int kHalves = NMAX == 16 ? 2 : 1;  // of 128 keys, of a step
-  static constexpr int kTeams = NMAX == 16 ? 2 : 1;    // of four warps that take the halves in turn, of K and of V
-  static constexpr int kGroups = NMAX == 16 ? 1 : 2;   // of four softmax warps
-  static constexpr int kThreads = 128 * (kGroups + 2 * kTeams + 1);
-  // Registers: a block is launched with 80 or 96 a thread; the narrow one's roles split them anew.
-  static constexpr int kRegsSoftmax = 120, kRegsOther = 72;
-  static_assert(NMAX > 16 || 128 * kRegsSoftmax + (kThreads - 128) * kRegsOther <= kThreads * 80, "registers");
+  // Warpgroups: softmax, K, V (teams that take the halves in turn), and one for the rest.
+  static constexpr int kGroups = NMAX == 16 ? 1 : 2, kKeyTeams = 1, kTeams = NMAX == 16 ? 2 : 1;
+  static constexpr int kThreads = 128 * (kGroups + kKeyTeams + kTeams + 1);
   static constexpr int kBuffers = NMAX == 16 ? 3 : 2;  // of K and of V in tensor memory
   // Columns: K, V, S (two steps), O.
   static constexpr uint32_t kTmemK = 0, kTmemV = 64 * kBuffers, kTmemS = 128 * kBuffers,
@@ -695,7 +692,7 @@ __device__ void qa_keys(const QaParams& p, int team, uint8_t* ring, QA_SHARED& s
     kb.next();
   }
 #pragma unroll 1
-  for (int u = team;; u += C::kTeams) {  // halves
+  for (int u = team;; u += C::kKeyTeams) {  // halves
     if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
     const int keys = sb.half_keys[st.at];
     if (keys == 0) return;
@@ -731,7 +728,7 @@ __device__ void qa_keys(const QaParams& p, int team, uint8_t* ring, QA_SHARED& s
     __syncwarp();
     if (lane == 0) mbar_arrive(&sb.k_ready[kb.at]);
 #pragma unroll
-    for (int k = 0; k < C::kTeams; ++k) {
+    for (int k = 0; k < C::kKeyTeams; ++k) {
       st.next();
       kb.next();
     }
@@ -1237,16 +1234,14 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
   const QaWait wt = {&sb.abort, p.cache.status, p.wait_ns};
 
   if (warp < 4 * C::kGroups) {
-    if constexpr (NMAX == 16) warpgroup_reg_inc<C::kRegsSoftmax>();
     qa_softmax<D, BITS, NMAX>(p, p_tiles, sb, wt);
   } else {
-    if constexpr (NMAX == 16) warpgroup_reg_dec<C::kRegsOther>();
     if (warp < kOther) {
-      const int k = warp / 4 - C::kGroups, team = k >> 1;
-      if (k & 1)
-        qa_values<D, BITS, NMAX>(p, team, ring, sb, wt);
+      const int k = warp / 4 - C::kGroups;
+      if (k < C::kKeyTeams)
+        qa_keys<D, BITS, NMAX>(p, k, ring, sb, wt);
       else
-        qa_keys<D, BITS, NMAX>(p, team, ring, sb, wt);
+        qa_values<D, BITS, NMAX>(p, k - C::kKeyTeams, ring, sb, wt);
     } else if (warp == kOther) {
       qa_producer<D, BITS, NMAX>(p, plan, ring, sb, wt);
     } else if (warp == kOther + 1) {
