@@ -700,26 +700,37 @@ __device__ void qa_keys(const QaParams& p, int team, uint8_t* ring, QA_SHARED& s
     tc_fence_after_sync();
     const uint8_t* data = data_at + st.at * C::kStageBytes;
     const uint8_t* scales = scales_at + st.at * C::kStageBytes;
+    // kTogether pieces of 32 values at a time: all of them in the narrow instance
+    // of 4 bits, whose K warps then wait for shared memory once (32 x 12K tokens:
+    // 117 -> 112 us; in 8 bits that costs more code than it saves, 107 -> 113).
+    constexpr int kTogether = BITS == 4 && NMAX == 16 ? D / 32 : 1;
 #pragma unroll 2
-    for (int d = 0; d < D / 32; ++d) {
-      const uint32_t both = *reinterpret_cast<const uint16_t*>(scales + 2 * d);
-      const uint32_t s0 = (both & 255) * 0x00800080u, s1 = (both >> 8) * 0x00800080u;
-      uint32_t w[BITS], r[16];
-      *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(data);
-      data += step;
-      if constexpr (BITS == 8) {
-        *reinterpret_cast<uint4*>(w + 4) = *reinterpret_cast<const uint4*>(data);
-        data += step;
+    for (int d0 = 0; d0 < D / 32; d0 += kTogether) {
+      uint32_t w[kTogether][BITS];
+      uint16_t both[kTogether];
+#pragma unroll
+      for (int d = 0; d < kTogether; ++d) {
+        both[d] = *reinterpret_cast<const uint16_t*>(scales + 2 * (d0 + d));
+#pragma unroll
+        for (int k = 0; k < BITS; k += 4) {
+          *reinterpret_cast<uint4*>(w[d] + k) = *reinterpret_cast<const uint4*>(data);
+          data += step;
+        }
       }
 #pragma unroll
-      for (int k = 0; k < BITS; ++k) {
-        constexpr int kPairs = QaDecode<BITS>::kPairs;
-        uint32_t x[kPairs];
-        QaDecode<BITS>::pairs(w[k], x);
+      for (int d = 0; d < kTogether; ++d) {
+        const uint32_t s0 = (both[d] & 255) * 0x00800080u, s1 = (uint32_t)(both[d] >> 8) * 0x00800080u;
+        uint32_t r[16];
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) r[k * kPairs + j] = q_mul2(x[j], k < BITS / 2 ? s0 : s1);
+        for (int k = 0; k < BITS; ++k) {
+          constexpr int kPairs = QaDecode<BITS>::kPairs;
+          uint32_t x[kPairs];
+          QaDecode<BITS>::pairs(w[d][k], x);
+#pragma unroll
+          for (int j = 0; j < kPairs; ++j) r[k * kPairs + j] = q_mul2(x[j], k < BITS / 2 ? s0 : s1);
+        }
+        tmem_st_32x32b_x16(to + 64 * kb.at + 16 * (d0 + d), r);
       }
-      tmem_st_32x32b_x16(to + 64 * kb.at + 16 * d, r);
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&sb.empty[st.at]);
@@ -837,18 +848,20 @@ __device__ void qa_values(const QaParams& p, int team, uint8_t* ring, QA_SHARED&
 // ------------------------------------------------------------------- softmax
 // Fragments of 16 lanes x 8 columns: thread i holds row i / 4 in two registers
 // and that + 8 in the other two, columns 2 (i % 4) and the next.
-__device__ __forceinline__ void qa_load_8(uint32_t at, uint32_t (&r)[4]) {
-  asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(at));
-}
 __device__ __forceinline__ void qa_load_16(uint32_t at, uint32_t (&a)[4], uint32_t (&b)[4]) {
   asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3])
                : "r"(at));
 }
-__device__ __forceinline__ void qa_load_wait(uint32_t (&r)[4]) {  // nothing reads the registers before it
-  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]) : : "memory");
+// Completes the loads of n fragments; nothing reads the registers before it.
+template <int N>
+__device__ __forceinline__ void qa_load_wait(uint32_t (&r)[N][2][4]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int k = 0; k < 2 * N; ++k) {
+    uint32_t* x = r[k >> 1][k & 1];
+    asm volatile("" : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]) : : "memory");
+  }
 }
 
 // A group of four softmax warps: the only one, or one with 32 of the rows to
@@ -950,8 +963,7 @@ __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait&
 #pragma unroll
       for (int h = 0; h < 2 * H; ++h)
         qa_load_16(q.lanes() + ((uint32_t)(16 * (h & 1)) << 16) + TMEM_S + (b * H + (h >> 1)) * NMAX + n0, r[h][0], r[h][1]);
-#pragma unroll
-      for (int h = 0; h < 4 * H; ++h) qa_load_wait(r[h >> 1][h & 1]);
+      qa_load_wait(r);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const int n = n0 + 8 * k + 2 * (lane & 3);
@@ -1061,8 +1073,7 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, c
 #pragma unroll
           for (int h = 0; h < 2 * H; ++h)
             qa_load_16(s_at + ((uint32_t)(16 * (h & 1)) << 16) + (b * H + (h >> 1)) * NMAX + 8 * g2, r[h][0], r[h][1]);
-#pragma unroll
-          for (int h = 0; h < 4 * H; ++h) qa_load_wait(r[h >> 1][h & 1]);
+          qa_load_wait(r);
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const int g = g2 + k;
