@@ -848,18 +848,23 @@ __device__ void qa_values(const QaParams& p, int team, uint8_t* ring, QA_SHARED&
 // ------------------------------------------------------------------- softmax
 // Fragments of 16 lanes x 8 columns: thread i holds row i / 4 in two registers
 // and that + 8 in the other two, columns 2 (i % 4) and the next.
+__device__ __forceinline__ void qa_load_8(uint32_t at, uint32_t (&r)[4]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at));
+}
 __device__ __forceinline__ void qa_load_16(uint32_t at, uint32_t (&a)[4], uint32_t (&b)[4]) {
   asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3])
                : "r"(at));
 }
 // Completes the loads of n fragments; nothing reads the registers before it.
-template <int N>
-__device__ __forceinline__ void qa_load_wait(uint32_t (&r)[N][2][4]) {
+template <int N, int K>
+__device__ __forceinline__ void qa_load_wait(uint32_t (&r)[N][K][4]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-  for (int k = 0; k < 2 * N; ++k) {
-    uint32_t* x = r[k >> 1][k & 1];
+  for (int k = 0; k < K * N; ++k) {
+    uint32_t* x = r[k / K][k % K];
     asm volatile("" : "+r"(x[0]), "+r"(x[1]), "+r"(x[2]), "+r"(x[3]) : : "memory");
   }
 }
@@ -1066,16 +1071,22 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, c
       if (!turn) {
         // P with the references as they are, and whether a numerator passes 2^15.
         float top = -INFINITY;
+        constexpr int kAt = NMAX == 16 ? 1 : 2;  // groups of 8 rows at a time
 #pragma unroll
-        for (int g2 = 0; g2 < G; g2 += 2) {
+        for (int g2 = 0; g2 < G; g2 += kAt) {
           if (8 * g2 >= rows) break;
-          uint32_t r[2 * H][2][4];
+          uint32_t r[2 * H][kAt][4];
 #pragma unroll
-          for (int h = 0; h < 2 * H; ++h)
-            qa_load_16(s_at + ((uint32_t)(16 * (h & 1)) << 16) + (b * H + (h >> 1)) * NMAX + 8 * g2, r[h][0], r[h][1]);
+          for (int h = 0; h < 2 * H; ++h) {
+            const uint32_t at = s_at + ((uint32_t)(16 * (h & 1)) << 16) + (b * H + (h >> 1)) * NMAX + 8 * g2;
+            if constexpr (kAt == 2)
+              qa_load_16(at, r[h][0], r[h][1]);
+            else
+              qa_load_8(at, r[h][0]);
+          }
           qa_load_wait(r);
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
+          for (int k = 0; k < kAt; ++k) {
             const int g = g2 + k;
             if (8 * g >= rows) break;
             if (masked) {  // keys that a row does not see count nothing, whatever S is
