@@ -62,8 +62,9 @@ struct QaCfg {
   static constexpr int kPBytes = 2 * kHalves * kBoxBytes;
   static constexpr int kStageBytes = 128 / 16 * q_block_bytes(BITS, D, 16);  // 128 tokens, whatever the page size
   static constexpr int kMaxPlanBytes = 32 * 1024;
-  static constexpr int kFixed = 2 * kQBytes + 2 * kPBytes;
-  static constexpr int kRoom = (214 * 1024 - 1024 - kMaxPlanBytes - kFixed) / kStageBytes;
+  static constexpr int kSumBytes = 2 * (NMAX / 8) * 128 * 8;  // of two steps, a pair of rows' sums for each thread
+  static constexpr int kFixed = 2 * kQBytes + 2 * kPBytes + kSumBytes;
+  static constexpr int kRoom = (217 * 1024 - 1024 - kMaxPlanBytes - kFixed) / kStageBytes;
   static constexpr int kStages = kRoom < 8 ? kRoom : 8;
   static constexpr int kPlanAt = kFixed + kStages * kStageBytes;
   static constexpr int kSmem = kPlanAt + kMaxPlanBytes + 1024;
@@ -101,9 +102,10 @@ struct QaShared {
   int min_lim[2];            // the least of those that see any
   float q_scale[2];          // logits in base-2 units = S * q_scale
   alignas(16) float warp_max[4 * NG][kQaRows];
-  alignas(16) float shift[2][kQaRows];  // added to a row's logits: 7 minus the reference, infinite where nothing is seen
+  alignas(16) float shift[2][kQaRows];  // added to a row's logits: 7 minus the reference, 0 where nothing is seen
+  alignas(16) float top[2][kQaRows];    // the reference less 7, -inf where nothing is seen
   alignas(16) float factor[kQaRows];    // of O and the sums where the references have moved
-  alignas(16) float sums[2][4 * NG][kQaRows];
+  alignas(16) float sums[4 * NG][kQaRows];
   alignas(16) int4 value_scales[4 * NT][32];  // a warp's two groups x 128 tokens as fp16
   int half_keys[NS];  // keys of the half in a stage, 0 at the end
   uint32_t tmem_base;
@@ -700,37 +702,25 @@ __device__ void qa_keys(const QaParams& p, int team, uint8_t* ring, QA_SHARED& s
     tc_fence_after_sync();
     const uint8_t* data = data_at + st.at * C::kStageBytes;
     const uint8_t* scales = scales_at + st.at * C::kStageBytes;
-    // kTogether pieces of 32 values at a time: all of them in the narrow instance
-    // of 4 bits, whose K warps then wait for shared memory once (32 x 12K tokens:
-    // 117 -> 112 us; in 8 bits that costs more code than it saves, 107 -> 113).
-    constexpr int kTogether = BITS == 4 && NMAX == 16 ? D / 32 : 1;
-#pragma unroll 2
-    for (int d0 = 0; d0 < D / 32; d0 += kTogether) {
-      uint32_t w[kTogether][BITS];
-      uint16_t both[kTogether];
+#pragma unroll 1
+    for (int d = 0; d < D / 32; ++d) {
+      const uint32_t both = *reinterpret_cast<const uint16_t*>(scales + 2 * d);
+      const uint32_t s0 = (both & 255) * 0x00800080u, s1 = (both >> 8) * 0x00800080u;
+      uint32_t w[BITS], r[16];
 #pragma unroll
-      for (int d = 0; d < kTogether; ++d) {
-        both[d] = *reinterpret_cast<const uint16_t*>(scales + 2 * (d0 + d));
-#pragma unroll
-        for (int k = 0; k < BITS; k += 4) {
-          *reinterpret_cast<uint4*>(w[d] + k) = *reinterpret_cast<const uint4*>(data);
-          data += step;
-        }
+      for (int k = 0; k < BITS; k += 4) {
+        *reinterpret_cast<uint4*>(w + k) = *reinterpret_cast<const uint4*>(data);
+        data += step;
       }
 #pragma unroll
-      for (int d = 0; d < kTogether; ++d) {
-        const uint32_t s0 = (both[d] & 255) * 0x00800080u, s1 = (uint32_t)(both[d] >> 8) * 0x00800080u;
-        uint32_t r[16];
+      for (int k = 0; k < BITS; ++k) {
+        constexpr int kPairs = QaDecode<BITS>::kPairs;
+        uint32_t x[kPairs];
+        QaDecode<BITS>::pairs(w[k], x);
 #pragma unroll
-        for (int k = 0; k < BITS; ++k) {
-          constexpr int kPairs = QaDecode<BITS>::kPairs;
-          uint32_t x[kPairs];
-          QaDecode<BITS>::pairs(w[d][k], x);
-#pragma unroll
-          for (int j = 0; j < kPairs; ++j) r[k * kPairs + j] = q_mul2(x[j], k < BITS / 2 ? s0 : s1);
-        }
-        tmem_st_32x32b_x16(to + 64 * kb.at + 16 * (d0 + d), r);
+        for (int j = 0; j < kPairs; ++j) r[k * kPairs + j] = q_mul2(x[j], k < BITS / 2 ? s0 : s1);
       }
+      tmem_st_32x32b_x16(to + 64 * kb.at + 16 * d, r);
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&sb.empty[st.at]);
@@ -792,7 +782,7 @@ __device__ void qa_values(const QaParams& p, int team, uint8_t* ring, QA_SHARED&
       sb.value_scales[4 * team + quarter][lane] = *reinterpret_cast<const int4*>(s);
       __syncwarp();
       const int4* scales = &sb.value_scales[4 * team + quarter][lane & 16];
-#pragma unroll 2
+#pragma unroll 1
       for (int token = 0; token < 128; token += 32) {
         uint32_t w[BITS], r[16];
 #pragma unroll
@@ -915,8 +905,8 @@ __device__ __noinline__ bool qa_segment_end(const QaParams& p, Shared& sb, const
     const int mine = n0 + (q.lane & 15);
     float l = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) l += sb.sums[which][4 * q.i + k][mine];
-    const float top = -sb.shift[which][mine];
+    for (int k = 0; k < 4; ++k) l += sb.sums[4 * q.i + k][mine];
+    const float top = sb.top[which][mine];
     if (!direct && q.w == 0 && q.lane < 16 && mine < end)
       p.work.ml[kind][(size_t)e0.z * slot_rows + mine] = faulty ? make_float2(0.0f, NAN) : make_float2(top, l);
     const float inv = l > 0.0f && !faulty && top > -INFINITY ? 1.0f / l : 0.0f;
@@ -945,20 +935,64 @@ __device__ __noinline__ bool qa_segment_end(const QaParams& p, Shared& sb, const
   return true;
 }
 
+// Keys of step t that a row does not see get the logit -inf in tensor memory,
+// whatever S is.
+template <int NMAX, int H, uint32_t TMEM_S, class Shared>
+__device__ __noinline__ void qa_mask(Shared& sb, int t, int seg, int rows) {
+  const QaGroup<NMAX> q;
+  const int row0 = q.row0(), row_end = row0 + q.rows(rows);
+  const int key0 = sb.sched[t % kQaSched][0].y + 32 * q.w + q.lane / 4;
+#pragma unroll 1
+  for (int n0 = row0; n0 < row_end; n0 += 8) {
+    const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][n0 + 2 * (q.lane & 3)]);
+#pragma unroll 1
+    for (int h = 0; h < 2 * H; ++h) {
+      const uint32_t at = q.lanes() + ((uint32_t)(16 * (h & 1)) << 16) + TMEM_S + ((t & 1) * H + (h >> 1)) * NMAX + n0;
+      const int key = key0 + 128 * (h >> 1) + 16 * (h & 1);
+      uint32_t r[1][1][4];
+      qa_load_8(at, r[0][0]);
+      qa_load_wait(r);
+      uint32_t* x = r[0][0];
+      if (key >= lim.x) x[0] = 0xFF800000u;
+      if (key >= lim.y) x[1] = 0xFF800000u;
+      if (key + 8 >= lim.x) x[2] = 0xFF800000u;
+      if (key + 8 >= lim.y) x[3] = 0xFF800000u;
+      asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]),
+                   "r"(x[3])
+                   : "memory");
+    }
+  }
+  tmem_st_wait();
+}
+
 // New references of step t's rows (at the start of a segment, or where a
 // numerator passed 2^15), the end of the segment before, or of everything.
 // All four warps of a group; `ok`: this warp's waits have not run out.
-// Returns 0: that is all, 1: go on, 2: a wait has run out, which the next vote
-// will tell.
+// `sums`: this thread's entries of its group's rows, as the step before left
+// them.  Returns 0: that is all, 1: go on, 2: a wait has run out, which the next
+// vote will tell.
 template <int D, int NMAX, int H, uint32_t TMEM_S, uint32_t TMEM_O, class Shared>
 __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait& wt, int t, int seg, bool ok,
-                                    bool faulty) {
+                                    bool faulty, float2* sums) {
   const QaGroup<NMAX> q;
   const int lane = q.lane, b = t & 1;
   const int2 e = ok ? *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]) : make_int2(kQaEnd, 0);
   const int row0 = q.row0(), row_end = row0 + q.rows(qa_rows(e.x));
   const bool end = e.x & kQaEnd, first = e.x & kQaFirst;
   float scale = 1.0f;
+  if (ok && t > 0 && (first || end)) {  // the sums of the segment that ended
+    const int before = row0 + q.rows(qa_rows(sb.sched[(t - 1) % kQaSched][0].x));
+#pragma unroll 1
+    for (int n0 = row0; n0 < before; n0 += 8) {
+      float2 l = sums[(n0 - row0) * 16];
+#pragma unroll
+      for (int x = 4; x < 32; x <<= 1) {
+        l.x += __shfl_xor_sync(0xffffffffu, l.x, x);
+        l.y += __shfl_xor_sync(0xffffffffu, l.y, x);
+      }
+      if (lane < 4) *reinterpret_cast<float2*>(&sb.sums[4 * q.i + q.w][n0 + 2 * lane]) = l;
+    }
+  }
   if (ok && !end) {
     scale = sb.q_scale[seg & 1];
     // The largest logit of each row among this warp's keys.
@@ -971,22 +1005,18 @@ __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait&
       qa_load_wait(r);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const int n = n0 + 8 * k + 2 * (lane & 3);
-        const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][n]);
         float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-        for (int h = 0; h < 4 * H; ++h) {
-          const uint32_t* x = r[h >> 1][k] + 2 * (h & 1);
-          const int key = e.y + 128 * (h >> 2) + 32 * q.w + 8 * (h & 3) + lane / 4;
-          if (key < lim.x) m0 = fmaxf(m0, __uint_as_float(x[0]));
-          if (key < lim.y) m1 = fmaxf(m1, __uint_as_float(x[1]));
+        for (int h = 0; h < 2 * H; ++h) {
+          m0 = fmax3(m0, __uint_as_float(r[h][k][0]), __uint_as_float(r[h][k][2]));
+          m1 = fmax3(m1, __uint_as_float(r[h][k][1]), __uint_as_float(r[h][k][3]));
         }
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) {
           m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, x));
           m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, x));
         }
-        if (lane < 4) *reinterpret_cast<float2*>(&sb.warp_max[4 * q.i + q.w][n]) = make_float2(m0, m1);
+        if (lane < 4) *reinterpret_cast<float2*>(&sb.warp_max[4 * q.i + q.w][n0 + 8 * k + 2 * lane]) = make_float2(m0, m1);
       }
     }
     tc_fence_before_sync();
@@ -1000,17 +1030,24 @@ __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait&
   const int n = row0 + threadIdx.x % 128;
   if (n < row0 + q.kRows) {
     float moved = INFINITY, f = 1.0f;
-    if (n < row_end) {
+    if (n < row_end && sb.lim[seg & 1][n] > 0) {  // rows that see nothing anywhere have queries of 0
       const float m = fmaxf(fmaxf(sb.warp_max[from][n], sb.warp_max[from + 1][n]),
                             fmaxf(sb.warp_max[from + 2][n], sb.warp_max[from + 3][n]));
-      const float old = first ? INFINITY : sb.shift[seg & 1][n];
+      const float old = first ? INFINITY : -sb.top[seg & 1][n];
       moved = fminf(old, 7.0f - m * scale);
       if (moved != INFINITY) f = ex2_approx(moved - old);
     }
-    sb.shift[seg & 1][n] = moved;  // rows that are not there (their queries are 0) have none
+    sb.top[seg & 1][n] = -moved;
+    sb.shift[seg & 1][n] = moved == INFINITY ? 0.0f : moved;
     sb.factor[n] = f;
   }
   q.sync();
+#pragma unroll 1
+  for (int n0 = row0; n0 < row_end; n0 += 8) {
+    float2* l = sums + (n0 - row0) * 16;
+    const float2 f = *reinterpret_cast<const float2*>(&sb.factor[n0 + 2 * (lane & 3)]);
+    *l = first ? make_float2(0.0f, 0.0f) : make_float2(l->x * f.x, l->y * f.y);
+  }
   if (!first && ok) {  // O in units of the new references
     const int u = t - 1;
     if ((ok = qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt)) && 32 * q.w < D) {
@@ -1032,23 +1069,23 @@ __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait&
 }
 
 template <int D, int BITS, int NMAX>
-__device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, const QaWait& wt) {
+__device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums, QA_SHARED& sb, const QaWait& wt) {
   using C = QaCfg<D, BITS, NMAX>;
   const QaGroup<NMAX> q;
-  constexpr int G = q.kRows / 8, H = C::kHalves;
+  constexpr int H = C::kHalves;
+  constexpr int kAt = NMAX == 16 ? 1 : 2;  // groups of 8 rows at a time
   const int lane = q.lane;
-  const int key0 = 32 * q.w + lane / 4, col0 = q.row0() + 2 * (lane & 3);
   const uint32_t s_at = q.lanes() + C::kTmemS + q.row0();
   // P: row n of 128 bytes in box (key / 64), 16-byte chunk ((key % 64) / 8) ^
   // (n & 7); this lane gives the address of row lane & 7 of matrix lane >> 3.
   const uint32_t p_at = smem_u32(p_tiles) + (q.w >> 1) * C::kBoxBytes + (q.row0() + (lane & 7)) * 128 +
                         ((((q.w & 1) * 4 + (lane >> 3)) ^ (lane & 7)) << 4);
-  float shift[G][2], sum[G][2];
+  // Sums: [step & 1][rows / 8][thread]; a step adds to those of the step before.
+  float2* const sums = all_sums + q.row0() * 16 + threadIdx.x % 128;
+  constexpr int kSumsStep = NMAX / 8 * 128;
   float scale = 1.0f;
-  int seg = -1, min_lim = 0;
+  int seg = -1;
   bool ok = true, faulty = false;
-#pragma unroll
-  for (int g = 0; g < G; ++g) shift[g][0] = shift[g][1] = sum[g][0] = sum[g][1] = 0.0f;
   // Once a wait of a warp has run out, the next vote ends all; every step has one.
 #pragma unroll 1
   for (int t = 0;; ++t) {
@@ -1058,23 +1095,17 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, c
     const int2 e = *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]);
     const int info = ok ? e.x : kQaEnd, rows = q.rows(qa_rows(info));
     bool turn = info & (kQaFirst | kQaEnd), turned = false;
-    if (info & kQaFirst) {
-      ++seg;
-      scale = sb.q_scale[seg & 1];
-      min_lim = sb.min_lim[seg & 1];
-    }
-    const bool masked = e.y + 128 * H > min_lim;
+    if (info & kQaFirst) ++seg;
     tc_fence_after_sync();
-    float part[G][2];
+    if (!(info & kQaEnd) && e.y + 128 * H > sb.min_lim[seg & 1])
+      qa_mask<NMAX, H, C::kTmemS>(sb, t, seg, qa_rows(info));
 #pragma unroll 1
     for (;;) {
       if (!turn) {
         // P with the references as they are, and whether a numerator passes 2^15.
         float top = -INFINITY;
-        constexpr int kAt = NMAX == 16 ? 1 : 2;  // groups of 8 rows at a time
-#pragma unroll
-        for (int g2 = 0; g2 < G; g2 += kAt) {
-          if (8 * g2 >= rows) break;
+#pragma unroll 1
+        for (int g2 = 0; 8 * g2 < rows; g2 += kAt) {
           uint32_t r[2 * H][kAt][4];
 #pragma unroll
           for (int h = 0; h < 2 * H; ++h) {
@@ -1084,65 +1115,50 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, c
             else
               qa_load_8(at, r[h][0]);
           }
+          const float* shifts = &sb.shift[seg & 1][q.row0() + 8 * g2 + 2 * (lane & 3)];
+          float2* const from = sums + (b ^ 1) * kSumsStep + g2 * 128;
+          float2* const to = sums + b * kSumsStep + g2 * 128;
+          float2 shift[kAt], l[kAt];
+#pragma unroll
+          for (int k = 0; k < kAt; ++k) {
+            shift[k] = *reinterpret_cast<const float2*>(shifts + 8 * k);
+            l[k] = from[128 * k];
+          }
           qa_load_wait(r);
 #pragma unroll
           for (int k = 0; k < kAt; ++k) {
-            const int g = g2 + k;
-            if (8 * g >= rows) break;
-            if (masked) {  // keys that a row does not see count nothing, whatever S is
-              const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][8 * g + col0]);
-              const int a = lim.x - e.y - key0, c = lim.y - e.y - key0;
-#pragma unroll
-              for (int h = 0; h < 4 * H; ++h) {
-                uint32_t* x = r[h >> 1][k] + 2 * (h & 1);
-                const int key = 128 * (h >> 2) + 8 * (h & 3);
-                if (key >= a) x[0] = 0xFF800000u;
-                if (key >= c) x[1] = 0xFF800000u;
-              }
-            }
-            float l0 = 0.0f, l1 = 0.0f;
+            float2 part = make_float2(0.0f, 0.0f);
 #pragma unroll
             for (int h = 0; h < H; ++h) {
               uint32_t pk[4];
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 const uint32_t* x = r[2 * h + (j >> 1)][k] + 2 * (j & 1);
-                const float x0 = fmaf(__uint_as_float(x[0]), scale, shift[g][0]);
-                const float x1 = fmaf(__uint_as_float(x[1]), scale, shift[g][1]);
+                const float x0 = fmaf(__uint_as_float(x[0]), scale, shift[k].x);
+                const float x1 = fmaf(__uint_as_float(x[1]), scale, shift[k].y);
                 top = fmax3(top, x0, x1);
                 const float a = ex2_approx(x0), c = ex2_approx(x1);
-                l0 += a;
-                l1 += c;
+                part.x += a;
+                part.y += c;
                 pk[j] = qa_pack_half(a, c);
               }
               asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(
-                               p_at + b * C::kPBytes + 2 * h * C::kBoxBytes + g * 1024),
+                               p_at + b * C::kPBytes + 2 * h * C::kBoxBytes + (g2 + k) * 1024),
                            "r"(pk[0]), "r"(pk[1]), "r"(pk[2]), "r"(pk[3])
                            : "memory");
             }
-            part[g][0] = l0;
-            part[g][1] = l1;
+            to[128 * k] = make_float2(l[k].x + part.x, l[k].y + part.y);
           }
         }
         if (turned) break;
         turn = top > 15.0f;
       }
       if (!q.vote(turn)) break;
-      const int next = qa_turn<D, NMAX, H, C::kTmemS, C::kTmemO>(p, sb, wt, t, seg, ok, faulty);
+      const int next = qa_turn<D, NMAX, H, C::kTmemS, C::kTmemO>(p, sb, wt, t, seg, ok, faulty, sums + (b ^ 1) * kSumsStep);
       if (next == 0) return;
       ok = next == 1;
       if (info & kQaFirst) faulty = false;
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        if (8 * g >= rows) break;
-        const float2 to = *reinterpret_cast<const float2*>(&sb.shift[seg & 1][8 * g + col0]);
-        const float2 f = *reinterpret_cast<const float2*>(&sb.factor[8 * g + col0]);
-        // A row without a reference sees nothing in this segment.
-        shift[g][0] = to.x == INFINITY ? 0.0f : to.x;
-        shift[g][1] = to.y == INFINITY ? 0.0f : to.y;
-        sum[g][0] = info & kQaFirst ? 0.0f : sum[g][0] * f.x;
-        sum[g][1] = info & kQaFirst ? 0.0f : sum[g][1] * f.y;
-      }
+      scale = sb.q_scale[seg & 1];
       turn = false;
       turned = true;
     }
@@ -1153,26 +1169,7 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, QA_SHARED& sb, c
     if (lane == 0) {
       mbar_arrive(&sb.s_free[b]);
       mbar_arrive(&sb.p_ready[b]);
-    }
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      if (8 * g >= rows) break;
-      sum[g][0] += part[g][0];
-      sum[g][1] += part[g][1];
-    }
-    if (info & kQaLast) {
-      if (lane == 0) mbar_arrive(&sb.q_free[seg & 1]);  // the limits have been read
-#pragma unroll
-      for (int g = 0; g < G; ++g) {
-        if (8 * g >= rows) break;
-#pragma unroll
-        for (int x = 4; x < 32; x <<= 1) {
-          sum[g][0] += __shfl_xor_sync(0xffffffffu, sum[g][0], x);
-          sum[g][1] += __shfl_xor_sync(0xffffffffu, sum[g][1], x);
-        }
-        if (lane < 4)
-          *reinterpret_cast<float2*>(&sb.sums[seg & 1][4 * q.i + q.w][8 * g + col0]) = make_float2(sum[g][0], sum[g][1]);
-      }
+      if (info & kQaLast) mbar_arrive(&sb.q_free[seg & 1]);  // the limits have been read
     }
   }
 }
@@ -1256,7 +1253,7 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
   const QaWait wt = {&sb.abort, p.cache.status, p.wait_ns};
 
   if (warp < 4 * C::kGroups) {
-    qa_softmax<D, BITS, NMAX>(p, p_tiles, sb, wt);
+    qa_softmax<D, BITS, NMAX>(p, p_tiles, reinterpret_cast<float2*>(p_tiles + 2 * C::kPBytes), sb, wt);
   } else {
     if (warp < kOther) {
       const int k = warp / 4 - C::kGroups;
