@@ -357,13 +357,24 @@ template <int N>
 struct QaRing {
   int at = 0;
   uint32_t phase = 0;
-  __device__ __forceinline__ void next() {
-    if (++at == N) {
-      at = 0;
+  __device__ __forceinline__ void next(int k = 1) {
+    at += k;
+    if (at >= N) {
+      at -= N;
       phase ^= 1;
     }
   }
 };
+
+// One lane of a warp arrives (without a branch around it).
+__device__ __forceinline__ void qa_arrive(uint64_t* bar, int lane) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.eq.s32 p, %1, 0;\n\t"
+      "@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(smem_u32(bar)),
+      "r"(lane)
+      : "memory");
+}
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
@@ -689,10 +700,8 @@ __device__ void qa_keys(const QaParams& p, int team, uint8_t* ring, QA_SHARED& s
   const uint32_t to = ((uint32_t)(32 * quarter) << 16) + C::kTmemK;
   QaRing<C::kStages> st;
   QaRing<C::kBuffers> kb;
-  for (int k = 0; k < team; ++k) {
-    st.next();
-    kb.next();
-  }
+  st.next(team);
+  kb.next(team);
 #pragma unroll 1
   for (int u = team;; u += C::kKeyTeams) {  // halves
     if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
@@ -702,37 +711,45 @@ __device__ void qa_keys(const QaParams& p, int team, uint8_t* ring, QA_SHARED& s
     tc_fence_after_sync();
     const uint8_t* data = data_at + st.at * C::kStageBytes;
     const uint8_t* scales = scales_at + st.at * C::kStageBytes;
+    // kTogether pieces of 32 values at a time: all of them in the narrow instance
+    // of 4 bits, whose K warps then wait for shared memory once.
+    constexpr int kTogether = BITS == 4 && NMAX == 16 ? D / 32 : 1;
 #pragma unroll 1
-    for (int d = 0; d < D / 32; ++d) {
-      const uint32_t both = *reinterpret_cast<const uint16_t*>(scales + 2 * d);
-      const uint32_t s0 = (both & 255) * 0x00800080u, s1 = (both >> 8) * 0x00800080u;
-      uint32_t w[BITS], r[16];
+    for (int d0 = 0; d0 < D / 32; d0 += kTogether) {
+      uint32_t w[kTogether][BITS];
+      uint16_t both[kTogether];
 #pragma unroll
-      for (int k = 0; k < BITS; k += 4) {
-        *reinterpret_cast<uint4*>(w + k) = *reinterpret_cast<const uint4*>(data);
-        data += step;
+      for (int d = 0; d < kTogether; ++d) {
+        both[d] = *reinterpret_cast<const uint16_t*>(scales + 2 * (d0 + d));
+#pragma unroll
+        for (int k = 0; k < BITS; k += 4) {
+          *reinterpret_cast<uint4*>(w[d] + k) = *reinterpret_cast<const uint4*>(data);
+          data += step;
+        }
       }
 #pragma unroll
-      for (int k = 0; k < BITS; ++k) {
-        constexpr int kPairs = QaDecode<BITS>::kPairs;
-        uint32_t x[kPairs];
-        QaDecode<BITS>::pairs(w[k], x);
+      for (int d = 0; d < kTogether; ++d) {
+        const uint32_t s0 = (both[d] & 255) * 0x00800080u, s1 = (uint32_t)(both[d] >> 8) * 0x00800080u;
+        uint32_t r[16];
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) r[k * kPairs + j] = q_mul2(x[j], k < BITS / 2 ? s0 : s1);
+        for (int k = 0; k < BITS; ++k) {
+          constexpr int kPairs = QaDecode<BITS>::kPairs;
+          uint32_t x[kPairs];
+          QaDecode<BITS>::pairs(w[d][k], x);
+#pragma unroll
+          for (int j = 0; j < kPairs; ++j) r[k * kPairs + j] = q_mul2(x[j], k < BITS / 2 ? s0 : s1);
+        }
+        tmem_st_32x32b_x16(to + 64 * kb.at + 16 * (d0 + d), r);
       }
-      tmem_st_32x32b_x16(to + 64 * kb.at + 16 * d, r);
     }
     __syncwarp();
-    if (lane == 0) mbar_arrive(&sb.empty[st.at]);
+    qa_arrive(&sb.empty[st.at], lane);
     tmem_st_wait();
     tc_fence_before_sync();
     __syncwarp();
-    if (lane == 0) mbar_arrive(&sb.k_ready[kb.at]);
-#pragma unroll
-    for (int k = 0; k < C::kKeyTeams; ++k) {
-      st.next();
-      kb.next();
-    }
+    qa_arrive(&sb.k_ready[kb.at], lane);
+    st.next(C::kKeyTeams);
+    kb.next(C::kKeyTeams);
   }
 }
 
@@ -745,6 +762,12 @@ __device__ void qa_values(const QaParams& p, int team, uint8_t* ring, QA_SHARED&
   const bool on = 32 * quarter < D;
   const int T = q_value_tokens(BITS, c.page), piece = T * BITS / 8;  // tokens and bytes of a piece
   const int values_at = q_values_at(BITS, D, c.page) + (32 * quarter + lane) * piece;
+  // From 32 tokens to the next 32 (in turn, as pages of 64 have two of them), and
+  // from their first 16 to the others where those lie apart.
+  const int inside = 32 / T * D * piece;
+  const int even = c.page == 16 ? 2 * c.head_bytes : c.page == 32 ? c.head_bytes : inside;
+  const int odd = c.page == 64 ? c.head_bytes - inside : even;
+  const int apart = c.page == 16 ? c.head_bytes : D * piece;
   // Scales: this lane turns those of 8 tokens of one of the warp's two groups into fp16.
   const int stoken = 8 * (lane & 15);
   const int scales_at = (stoken >> c.page_shift) * c.head_bytes + q_value_scales_at(BITS, D, c.page) +
@@ -752,10 +775,8 @@ __device__ void qa_values(const QaParams& p, int team, uint8_t* ring, QA_SHARED&
   const uint32_t to = ((uint32_t)(32 * quarter) << 16) + C::kTmemV;
   QaRing<C::kStages> st;
   QaRing<C::kBuffers> vb;
-  for (int k = 0; k < team; ++k) {
-    st.next();
-    vb.next();
-  }
+  st.next(team);
+  vb.next(team);
 #pragma unroll 1
   for (int u = team;; u += C::kTeams) {  // halves
     if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
@@ -782,22 +803,20 @@ __device__ void qa_values(const QaParams& p, int team, uint8_t* ring, QA_SHARED&
       sb.value_scales[4 * team + quarter][lane] = *reinterpret_cast<const int4*>(s);
       __syncwarp();
       const int4* scales = &sb.value_scales[4 * team + quarter][lane & 16];
+      const uint8_t* from = stage + values_at;
 #pragma unroll 1
       for (int token = 0; token < 128; token += 32) {
         uint32_t w[BITS], r[16];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {  // 16 tokens: 8 or 16 bytes
-          const int x = token + 16 * j, off = x & (c.page - 1);
-          const uint8_t* from =
-              stage + (x >> c.page_shift) * c.head_bytes + values_at + off / T * (D * piece) + off % T * BITS / 8;
-          if constexpr (BITS == 8) {
-            *reinterpret_cast<uint4*>(w + 4 * j) = *reinterpret_cast<const uint4*>(from);
-          } else if (T == 32) {
-            if (j == 0) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(from);
-          } else {
-            *reinterpret_cast<uint2*>(w + 2 * j) = *reinterpret_cast<const uint2*>(from);
-          }
+        if constexpr (BITS == 8) {
+          *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(from);
+          *reinterpret_cast<uint4*>(w + 4) = *reinterpret_cast<const uint4*>(from + apart);
+        } else if (T == 32) {
+          *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(from);
+        } else {
+          *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(from);
+          *reinterpret_cast<uint2*>(w + 2) = *reinterpret_cast<const uint2*>(from + apart);
         }
+        from += token & 32 ? odd : even;
         if (BITS == 8 && __builtin_expect(token + 32 > keys, 0)) {  // a code may be NaN there
 #pragma unroll
           for (int k = 0; k < BITS; ++k) {
@@ -822,16 +841,13 @@ __device__ void qa_values(const QaParams& p, int team, uint8_t* ring, QA_SHARED&
       }
     }
     __syncwarp();
-    if (lane == 0) mbar_arrive(&sb.empty[st.at]);
+    qa_arrive(&sb.empty[st.at], lane);
     tmem_st_wait();
     tc_fence_before_sync();
     __syncwarp();
-    if (lane == 0) mbar_arrive(&sb.v_ready[vb.at]);
-#pragma unroll
-    for (int k = 0; k < C::kTeams; ++k) {
-      st.next();
-      vb.next();
-    }
+    qa_arrive(&sb.v_ready[vb.at], lane);
+    st.next(C::kTeams);
+    vb.next(C::kTeams);
   }
 }
 
@@ -1166,11 +1182,9 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
     tc_fence_before_sync();
     fence_proxy_async_smem();
     __syncwarp();
-    if (lane == 0) {
-      mbar_arrive(&sb.s_free[b]);
-      mbar_arrive(&sb.p_ready[b]);
-      if (info & kQaLast) mbar_arrive(&sb.q_free[seg & 1]);  // the limits have been read
-    }
+    qa_arrive(&sb.s_free[b], lane);
+    qa_arrive(&sb.p_ready[b], lane);
+    if (info & kQaLast) qa_arrive(&sb.q_free[seg & 1], lane);  // the limits have been read
   }
 }
 
