@@ -25,8 +25,8 @@
 //                V: the same, scales of 8 tokens at a time;
 //   a warp       producer: page look-ups, one bulk copy a page (codes and scales
 //                of keys and values lie together), the schedule;
-//   a warp       Q: rows of the next segment to shared memory as fp16, scaled by a
-//                power of two so that the largest is next to 2^15 (exact down
+//   a warp       Q: rows of the next segment to shared memory as fp16, each scaled by
+//                a power of two so that its largest is next to 2^15 (exact down
 //                to 2^-28 of it), and how many keys each row sees;
 //   two warps    S products and P V products, each issued by one lane.
 // All of tensor memory is allocated, so that its first column is 0.
@@ -100,7 +100,7 @@ struct QaShared {
   int4 sched[kQaSched][2];
   alignas(16) int lim[2][kQaRows];  // keys that a row sees, 0 for none
   int min_lim[2];            // the least of those that see any
-  float q_scale[2];          // logits in base-2 units = S * q_scale
+  alignas(16) float q_scale[2][kQaRows];  // a row's logits in base-2 units = S * q_scale
   alignas(16) float warp_max[4 * NG][kQaRows];
   alignas(16) float shift[2][kQaRows];  // added to a row's logits: 7 minus the reference, 0 where nothing is seen
   alignas(16) float top[2][kQaRows];    // the reference less 7, -inf where nothing is seen
@@ -295,7 +295,7 @@ __device__ __forceinline__ QaSeg qa_segment(const QaParams& p, const QaPlan& pla
 // that small problems spread out.
 struct QaWalk {
   int kind, run, x, x_end;
-  __device__ __forceinline__ void begin(const QaPlan& plan, int k) {
+  __device__ void begin(const QaPlan& plan, int k) {
     kind = k;
     const PfxCuts c = k == kQaOwn ? plan.t->own : plan.t->pre;
     run = blockIdx.x;
@@ -468,10 +468,6 @@ __device__ void qa_producer(const QaParams& p, const QaPlan& plan, uint8_t* ring
 }
 
 // ------------------------------------------------------------------------- Q
-__device__ __forceinline__ float2 qa_widen(uint32_t v, bool fp16) {
-  if (fp16) return __half22float2(*reinterpret_cast<const __half2*>(&v));
-  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
-}
 __device__ __forceinline__ uint32_t qa_pack_half(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -489,18 +485,8 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
   for (int k = 0; walk.next(p, plan, seg); ++k) {
     const int buf = k & 1;
     if (k >= 2 && !qa_wait(&sb.q_free[buf], ((k >> 1) - 1) & 1, wt)) break;
-    // Rows of one request are contiguous: Q is [batch][n_kv_heads][rows][D].
-    const uint4* Q = reinterpret_cast<const uint4*>(p.Q) +
-                     (((size_t)seg.req * p.cache.n_kv_heads + seg.kvh) * p.rows + seg.row0) * kPieces;
-    const size_t next_req = (size_t)p.cache.n_kv_heads * p.rows * kPieces;
-    const int pieces = seg.rows * kPieces;
-    auto load = [&](int i) {
-      const int n = i / kPieces;
-      if (seg.kind == kQaOwn) return __ldg(Q + i);
-      const int r = n / p.rows;
-      return __ldg(Q + r * next_req + (i - r * p.rows * kPieces));
-    };
     int least = INT_MAX;
+#pragma unroll 1
     for (int n = lane; n < seg.rows; n += 32) {
       const int r = n / p.rows, row = seg.row0 + n - r * p.rows;  // (own items: r = 0)
       const int i = row % p.q_len, req = seg.req + r;
@@ -510,41 +496,61 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
       if (lim > 0) least = min(least, lim);
     }
     least = __reduce_min_sync(0xffffffffu, least);
+    if (lane == 0) sb.min_lim[buf] = least;
     __syncwarp();
-    uint32_t top = 0;
-    if (!p.fp16) {
-#pragma unroll 4
-      for (int i = lane; i < pieces; i += 32) {
-        if (sb.lim[buf][i / kPieces] <= 0) continue;
-        const uint4 v = load(i);
-        top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu),
-                                     __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
-      }
-      top = __reduce_max_sync(0xffffffffu, max(top & 0xFFFFu, top >> 16));
-    }
-    // bf16: the largest size has exponent field E, and times 2^(141 - E) lies in [2^14, 2^15).
-    const int shift = p.fp16 || top == 0 ? 0 : min(141 - (int)(top >> 7), 126);
-    const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
-    if (lane == 0) {
-      sb.min_lim[buf] = least;
-      sb.q_scale[buf] = fmaxf(p.scale_log2 * __uint_as_float((uint32_t)(127 - shift) << 23), FLT_MIN);
-    }
-    uint8_t* tile = q_tiles + buf * C::kQBytes;
-    const int all = ((seg.rows + 15) & ~15) * kPieces;  // rows up to the product's N are 0
-#pragma unroll 4
-    for (int i = lane; i < all; i += 32) {
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (i < pieces && sb.lim[buf][i / kPieces] > 0) v = load(i);  // what sees nothing may hold anything
-      if (!p.fp16) {
-        uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+    // Rows of one request are contiguous: Q is [batch][n_kv_heads][rows][D].  A
+    // row takes kPieces lanes; kMany rows of each are on their way at a time.
+    // Rows up to the product's N, and those that see nothing (which may hold
+    // anything), are 0.
+    constexpr int kAtOnce = 32 / kPieces, kMany = 4;
+    const int sub = lane / kPieces, piece = lane - sub * kPieces;
+    const size_t row_bytes = (size_t)D * 2;
+    const uint8_t* Q = reinterpret_cast<const uint8_t*>(p.Q) +
+                       (((size_t)seg.req * p.cache.n_kv_heads + seg.kvh) * p.rows + seg.row0) * row_bytes + 16 * piece;
+    const size_t next_req = (size_t)(p.cache.n_kv_heads - 1) * p.rows * row_bytes;  // beyond the rows between
+    uint8_t* tile = q_tiles + buf * C::kQBytes + (piece >> 3) * C::kBoxBytes;
+    const int all = (seg.rows + 15) & ~15;
+#pragma unroll 1
+    for (int n0 = sub; n0 < all + sub; n0 += kAtOnce * kMany) {
+      uint4 v[kMany];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 f = qa_widen(w[j], false);
-          w[j] = qa_pack_half(f.x * up, f.y * up);
-        }
+      for (int k = 0; k < kMany; ++k) {
+        const int n = n0 + kAtOnce * k;
+        v[k] = make_uint4(0, 0, 0, 0);
+        if (sub < kAtOnce && n < seg.rows && sb.lim[buf][n] > 0)
+          v[k] = __ldg(reinterpret_cast<const uint4*>(Q + n * row_bytes + (seg.kind == kQaOwn ? 0 : n / p.rows) * next_req));
       }
-      const int n = i / kPieces, piece = i - n * kPieces;
-      *reinterpret_cast<uint4*>(tile + (piece >> 3) * C::kBoxBytes + n * 128 + (((piece & 7) ^ (n & 7)) << 4)) = v;
+#pragma unroll
+      for (int k = 0; k < kMany; ++k) {
+        const int n = n0 + kAtOnce * k;
+        if (!p.fp16) {
+          // The row's largest size has exponent field E; times 2^(141 - E) it lies in [2^14, 2^15).
+          uint32_t top = __vmaxu2(__vmaxu2(v[k].x & 0x7FFF7FFFu, v[k].y & 0x7FFF7FFFu),
+                                  __vmaxu2(v[k].z & 0x7FFF7FFFu, v[k].w & 0x7FFF7FFFu));
+          top = max(top & 0xFFFFu, top >> 16);
+          if constexpr (kPieces == 12) {
+            // 12 lanes: those of the other row keep their own maximum.
+            const uint32_t mine = __reduce_max_sync(0xffffffffu, sub == 0 ? top : 0u);
+            const uint32_t other = __reduce_max_sync(0xffffffffu, sub == 1 ? top : 0u);
+            top = sub == 0 ? mine : other;
+          } else {
+#pragma unroll
+            for (int x = 1; x < kPieces; x <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, x));
+          }
+          const int shift = top == 0 ? 0 : min(141 - (int)(top >> 7), 126);
+          const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
+          uint32_t* w = reinterpret_cast<uint32_t*>(&v[k]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            w[j] = qa_pack_half(__uint_as_float(w[j] << 16) * up, __uint_as_float(w[j] & 0xFFFF0000u) * up);
+          if (piece == 0 && sub < kAtOnce && n < all)
+            sb.q_scale[buf][n] = fmaxf(p.scale_log2 * __uint_as_float((uint32_t)(127 - shift) << 23), FLT_MIN);
+        } else if (piece == 0 && sub < kAtOnce && n < all) {
+          sb.q_scale[buf][n] = fmaxf(p.scale_log2, FLT_MIN);
+        }
+        if (sub < kAtOnce && n < all)
+          *reinterpret_cast<uint4*>(tile + n * 128 + (((piece & 7) ^ (n & 7)) << 4)) = v[k];
+      }
     }
     fence_proxy_async_smem();
     __syncwarp();
@@ -916,33 +922,37 @@ __device__ __noinline__ bool qa_segment_end(const QaParams& p, Shared& sb, const
   const int kind = qa_kind(e0.x), end = q.row0() + q.rows(qa_rows(e0.x));
   const bool direct = e0.z < 0;
   const int slot_rows = kind == kQaPrefix ? kQaRows : min(p.rows, kQaRows);
+  // A lane has the sum and the reference of one row; then four rows at a time.
+  const int mine = min(q.row0() + q.lane, kQaRows - 1);
+  const float l = sb.sums[4 * q.i][mine] + sb.sums[4 * q.i + 1][mine] + sb.sums[4 * q.i + 2][mine] + sb.sums[4 * q.i + 3][mine];
+  const float top = sb.top[which][mine];
+  if (!direct && q.w == 0 && q.row0() + q.lane < end)
+    p.work.ml[kind][(size_t)e0.z * slot_rows + mine] = faulty ? make_float2(0.0f, NAN) : make_float2(top, l);
+  const float inv = l > 0.0f && !faulty && top > -INFINITY ? 1.0f / l : 0.0f;
+  if (32 * q.w < D) {
+    const int d = 32 * q.w + q.lane;
+    float* part = p.work.O[kind] + ((size_t)(direct ? 0 : e0.z) * slot_rows + q.row0()) * D + d;
+    uint16_t* out = reinterpret_cast<uint16_t*>(p.O) +
+                    (((size_t)e0.w * p.cache.n_kv_heads + e1.x) * p.rows + e1.y + q.row0()) * D + d;
 #pragma unroll 1
-  for (int n0 = q.row0(); n0 < end; n0 += 16) {
-    const int mine = n0 + (q.lane & 15);
-    float l = 0.0f;
+    for (int n0 = 0; n0 < end - q.row0(); n0 += 4, part += 4 * D, out += 4 * D) {
+      uint32_t v[4];
+      asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
+                   : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                   : "r"(q.lanes() + TMEM_O + q.row0() + n0));
+      asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]) : : "memory");
+      const int left = end - q.row0() - n0;
+      if (!direct) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) l += sb.sums[4 * q.i + k][mine];
-    const float top = sb.top[which][mine];
-    if (!direct && q.w == 0 && q.lane < 16 && mine < end)
-      p.work.ml[kind][(size_t)e0.z * slot_rows + mine] = faulty ? make_float2(0.0f, NAN) : make_float2(top, l);
-    const float inv = l > 0.0f && !faulty && top > -INFINITY ? 1.0f / l : 0.0f;
-    if (32 * q.w < D) {
-      const int d = 32 * q.w + q.lane;
-      uint32_t v[16];
-      tmem_ld_32x32b_x16(q.lanes() + TMEM_O + n0, v);
-      tmem_ld_wait(v);
-      float* part = p.work.O[kind] + ((size_t)(direct ? 0 : e0.z) * slot_rows + n0) * D + d;
-      uint16_t* out = reinterpret_cast<uint16_t*>(p.O) +
-                      (((size_t)e0.w * p.cache.n_kv_heads + e1.x) * p.rows + e1.y + n0) * D + d;
+        for (int k = 0; k < 4; ++k)
+          if (k < left) part[k * D] = __uint_as_float(v[k]);
+      } else {
 #pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        const float f = __shfl_sync(0xffffffffu, inv, k);
-        if (n0 + k >= end) break;
-        if (direct) {
+        for (int k = 0; k < 4; ++k) {
+          const float f = __shfl_sync(0xffffffffu, inv, n0 + k);
           const float x = f == 0.0f ? 0.0f : __uint_as_float(v[k]) * f;
-          out[k * D] = p.fp16 ? __half_as_ushort(__float2half_rn(x)) : __bfloat16_as_ushort(__float2bfloat16_rn(x));
-        } else {
-          part[k * D] = __uint_as_float(v[k]);
+          const uint32_t both = p.fp16 ? qa_pack_half(x, x) : pack_bf16x2(x, x);
+          if (k < left) out[k * D] = (uint16_t)both;
         }
       }
     }
@@ -995,7 +1005,6 @@ __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait&
   const int2 e = ok ? *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]) : make_int2(kQaEnd, 0);
   const int row0 = q.row0(), row_end = row0 + q.rows(qa_rows(e.x));
   const bool end = e.x & kQaEnd, first = e.x & kQaFirst;
-  float scale = 1.0f;
   if (ok && t > 0 && (first || end)) {  // the sums of the segment that ended
     const int before = row0 + q.rows(qa_rows(sb.sched[(t - 1) % kQaSched][0].x));
 #pragma unroll 1
@@ -1010,30 +1019,26 @@ __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait&
     }
   }
   if (ok && !end) {
-    scale = sb.q_scale[seg & 1];
-    // The largest logit of each row among this warp's keys.
+    // The largest entry of S of each row among this warp's keys.
 #pragma unroll 1
-    for (int n0 = row0; n0 < row_end; n0 += 16) {
-      uint32_t r[2 * H][2][4];
+    for (int n0 = row0; n0 < row_end; n0 += 8) {
+      uint32_t r[2 * H][1][4];
 #pragma unroll
       for (int h = 0; h < 2 * H; ++h)
-        qa_load_16(q.lanes() + ((uint32_t)(16 * (h & 1)) << 16) + TMEM_S + (b * H + (h >> 1)) * NMAX + n0, r[h][0], r[h][1]);
+        qa_load_8(q.lanes() + ((uint32_t)(16 * (h & 1)) << 16) + TMEM_S + (b * H + (h >> 1)) * NMAX + n0, r[h][0]);
       qa_load_wait(r);
+      float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        float m0 = -INFINITY, m1 = -INFINITY;
-#pragma unroll
-        for (int h = 0; h < 2 * H; ++h) {
-          m0 = fmax3(m0, __uint_as_float(r[h][k][0]), __uint_as_float(r[h][k][2]));
-          m1 = fmax3(m1, __uint_as_float(r[h][k][1]), __uint_as_float(r[h][k][3]));
-        }
-#pragma unroll
-        for (int x = 4; x < 32; x <<= 1) {
-          m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, x));
-          m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, x));
-        }
-        if (lane < 4) *reinterpret_cast<float2*>(&sb.warp_max[4 * q.i + q.w][n0 + 8 * k + 2 * lane]) = make_float2(m0, m1);
+      for (int h = 0; h < 2 * H; ++h) {
+        m0 = fmax3(m0, __uint_as_float(r[h][0][0]), __uint_as_float(r[h][0][2]));
+        m1 = fmax3(m1, __uint_as_float(r[h][0][1]), __uint_as_float(r[h][0][3]));
       }
+#pragma unroll
+      for (int x = 4; x < 32; x <<= 1) {
+        m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, x));
+        m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, x));
+      }
+      if (lane < 4) *reinterpret_cast<float2*>(&sb.warp_max[4 * q.i + q.w][n0 + 2 * lane]) = make_float2(m0, m1);
     }
     tc_fence_before_sync();
   }
@@ -1050,7 +1055,7 @@ __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait&
       const float m = fmaxf(fmaxf(sb.warp_max[from][n], sb.warp_max[from + 1][n]),
                             fmaxf(sb.warp_max[from + 2][n], sb.warp_max[from + 3][n]));
       const float old = first ? INFINITY : -sb.top[seg & 1][n];
-      moved = fminf(old, 7.0f - m * scale);
+      moved = fminf(old, 7.0f - m * sb.q_scale[seg & 1][n]);
       if (moved != INFINITY) f = ex2_approx(moved - old);
     }
     sb.top[seg & 1][n] = -moved;
@@ -1069,13 +1074,17 @@ __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait&
     if ((ok = qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt)) && 32 * q.w < D) {
       tc_fence_after_sync();
 #pragma unroll 1
-      for (int n0 = row0; n0 < row_end; n0 += 16) {
-        uint32_t v[16];
-        tmem_ld_32x32b_x16(q.lanes() + TMEM_O + n0, v);
-        tmem_ld_wait(v);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * sb.factor[n0 + k]);
-        tmem_st_32x32b_x16(q.lanes() + TMEM_O + n0, v);
+      for (int n0 = row0; n0 < row_end; n0 += 4) {
+        uint32_t v[4];
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                     : "r"(q.lanes() + TMEM_O + n0));
+        asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]) : : "memory");
+        const float4 f = *reinterpret_cast<const float4*>(&sb.factor[n0]);
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(q.lanes() + TMEM_O + n0),
+                     "r"(__float_as_uint(__uint_as_float(v[0]) * f.x)), "r"(__float_as_uint(__uint_as_float(v[1]) * f.y)),
+                     "r"(__float_as_uint(__uint_as_float(v[2]) * f.z)), "r"(__float_as_uint(__uint_as_float(v[3]) * f.w))
+                     : "memory");
       }
       tmem_st_wait();
     }
@@ -1099,7 +1108,6 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
   // Sums: [step & 1][rows / 8][thread]; a step adds to those of the step before.
   float2* const sums = all_sums + q.row0() * 16 + threadIdx.x % 128;
   constexpr int kSumsStep = NMAX / 8 * 128;
-  float scale = 1.0f;
   int seg = -1;
   bool ok = true, faulty = false;
   // Once a wait of a warp has run out, the next vote ends all; every step has one.
@@ -1131,12 +1139,14 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
             else
               qa_load_8(at, r[h][0]);
           }
-          const float* shifts = &sb.shift[seg & 1][q.row0() + 8 * g2 + 2 * (lane & 3)];
+          const int n = q.row0() + 8 * g2 + 2 * (lane & 3);
+          const float *shifts = &sb.shift[seg & 1][n], *scales = &sb.q_scale[seg & 1][n];
           float2* const from = sums + (b ^ 1) * kSumsStep + g2 * 128;
           float2* const to = sums + b * kSumsStep + g2 * 128;
-          float2 shift[kAt], l[kAt];
+          float2 scale[kAt], shift[kAt], l[kAt];
 #pragma unroll
           for (int k = 0; k < kAt; ++k) {
+            scale[k] = *reinterpret_cast<const float2*>(scales + 8 * k);
             shift[k] = *reinterpret_cast<const float2*>(shifts + 8 * k);
             l[k] = from[128 * k];
           }
@@ -1150,8 +1160,8 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 const uint32_t* x = r[2 * h + (j >> 1)][k] + 2 * (j & 1);
-                const float x0 = fmaf(__uint_as_float(x[0]), scale, shift[k].x);
-                const float x1 = fmaf(__uint_as_float(x[1]), scale, shift[k].y);
+                const float x0 = fmaf(__uint_as_float(x[0]), scale[k].x, shift[k].x);
+                const float x1 = fmaf(__uint_as_float(x[1]), scale[k].y, shift[k].y);
                 top = fmax3(top, x0, x1);
                 const float a = ex2_approx(x0), c = ex2_approx(x1);
                 part.x += a;
@@ -1174,7 +1184,6 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
       if (next == 0) return;
       ok = next == 1;
       if (info & kQaFirst) faulty = false;
-      scale = sb.q_scale[seg & 1];
       turn = false;
       turned = true;
     }
@@ -1191,7 +1200,7 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
 // Where the partial results of a unit (request, kv head and row chunk) lie, as
 // two int4: {n, n_pre, row of the prefix items, 0}, {first prefix slot, first
 // own slot, 0, 0}; n is -1 where O has been written, 0 where nothing is seen.
-__device__ __forceinline__ void qa_sources(const QaParams& p, const QaPlan& plan, int unit, int4* out) {
+static __device__ __noinline__ void qa_sources(const QaParams& p, const QaPlan& plan, int unit, int4* out) {
   const int kv = p.cache.n_kv_heads, per = kv * p.chunks;
   const int req = unit / per, rest = unit - req * per, kvh = rest / p.chunks;
   const int g = plan.group[req], tiles = plan.cum[req + 1] - plan.cum[req];
