@@ -51,9 +51,12 @@ struct QaCfg {
   // Warpgroups: softmax, K, V (teams that take the halves in turn), and one for the rest.
   static constexpr int kGroups = NMAX == 16 ? 1 : 2, kKeyTeams = 1, kTeams = NMAX == 16 ? 2 : 1;
   static constexpr int kThreads = 128 * (kGroups + kKeyTeams + kTeams + 1);
-  static constexpr int kBuffers = NMAX == 16 ? 3 : 2;  // of K and of V in tensor memory
+  // Halves of K and of V in tensor memory.  V stays until the softmax has been
+  // through its step: with 3 buffers one half of a step had to wait for the
+  // products of the step before (32 x 12K tokens: 111 us).
+  static constexpr int kKeyBuffers = 2, kValueBuffers = NMAX == 16 ? 4 : 3;
   // Columns: K, V, S (two steps), O.
-  static constexpr uint32_t kTmemK = 0, kTmemV = 64 * kBuffers, kTmemS = 128 * kBuffers,
+  static constexpr uint32_t kTmemK = 0, kTmemV = 64 * kKeyBuffers, kTmemS = kTmemV + 64 * kValueBuffers,
                             kTmemO = kTmemS + 2 * kHalves * NMAX;
   static_assert(kTmemO + NMAX <= 512, "tensor memory");
   static constexpr int kBoxes = (D + 63) / 64;
@@ -86,12 +89,12 @@ __device__ __forceinline__ int qa_rows(int info) { return (info >> 8) & 255; }
 __device__ __forceinline__ int qa_kind(int info) { return (info >> 16) & 1; }
 __device__ __forceinline__ int qa_keys_of(int info) { return info >> 20; }
 
-template <int NS, int NB, int NT, int NG>
+template <int NS, int NK, int NV, int NT, int NG>
 struct QaShared {
   uint64_t full[NS], empty[NS];  // empty: 8 warps
   uint64_t sched_full[kQaSched];
-  uint64_t k_ready[NB], v_ready[NB];  // 4 warps
-  uint64_t k_free[NB], v_free[NB];    // products
+  uint64_t k_ready[NK], k_free[NK];  // 4 warps; products
+  uint64_t v_ready[NV], v_free[NV];
   uint64_t p_ready[2];                // softmax warps
   uint64_t s_full[2], s_free[2];      // products; softmax warps
   uint64_t pv_done[2];
@@ -383,7 +386,8 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                : "memory");
 }
 
-#define QA_SHARED QaShared<QaCfg<D, BITS, NMAX>::kStages, QaCfg<D, BITS, NMAX>::kBuffers, QaCfg<D, BITS, NMAX>::kTeams, \
+#define QA_SHARED QaShared<QaCfg<D, BITS, NMAX>::kStages, QaCfg<D, BITS, NMAX>::kKeyBuffers, \
+                                QaCfg<D, BITS, NMAX>::kValueBuffers, QaCfg<D, BITS, NMAX>::kTeams, \
                                 QaCfg<D, BITS, NMAX>::kGroups>
 
 // ------------------------------------------------------------------ producer
@@ -593,7 +597,7 @@ __device__ void qa_products_s(const QaParams& p, uint8_t* q_tiles, QA_SHARED& sb
   using C = QaCfg<D, BITS, NMAX>;
   const uint64_t desc = smem_desc_sw128(0, 16, 1024);
   const uint32_t hi = (uint32_t)(desc >> 32), q_lo = (uint32_t)desc + (smem_u32(q_tiles) >> 4);
-  QaRing<C::kBuffers> kb;
+  QaRing<C::kKeyBuffers> kb;
   int seg = -1;
 #pragma unroll 1
   for (int t = 0;; ++t) {
@@ -645,7 +649,7 @@ __device__ void qa_products_pv(const QaParams& p, uint8_t* p_tiles, QA_SHARED& s
   using C = QaCfg<D, BITS, NMAX>;
   const uint64_t desc = smem_desc_sw128(0, 16, 1024);
   const uint32_t hi = (uint32_t)(desc >> 32), p_lo = (uint32_t)desc + (smem_u32(p_tiles) >> 4);
-  QaRing<C::kBuffers> vb;
+  QaRing<C::kValueBuffers> vb;
 #pragma unroll 1
   for (int t = 0;; ++t) {
     if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) break;
@@ -705,7 +709,7 @@ __device__ void qa_keys(const QaParams& p, int team, uint8_t* ring, QA_SHARED& s
   const int step = c.page * 16;  // from 16 bytes of a token to the next 16
   const uint32_t to = ((uint32_t)(32 * quarter) << 16) + C::kTmemK;
   QaRing<C::kStages> st;
-  QaRing<C::kBuffers> kb;
+  QaRing<C::kKeyBuffers> kb;
   st.next(team);
   kb.next(team);
 #pragma unroll 1
@@ -713,7 +717,7 @@ __device__ void qa_keys(const QaParams& p, int team, uint8_t* ring, QA_SHARED& s
     if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
     const int keys = sb.half_keys[st.at];
     if (keys == 0) return;
-    if (u >= C::kBuffers && !qa_wait(&sb.k_free[kb.at], kb.phase ^ 1, wt)) return;
+    if (u >= C::kKeyBuffers && !qa_wait(&sb.k_free[kb.at], kb.phase ^ 1, wt)) return;
     tc_fence_after_sync();
     const uint8_t* data = data_at + st.at * C::kStageBytes;
     const uint8_t* scales = scales_at + st.at * C::kStageBytes;
@@ -780,7 +784,7 @@ __device__ void qa_values(const QaParams& p, int team, uint8_t* ring, QA_SHARED&
                         (2 * quarter + (lane >> 4)) * c.page + (stoken & (c.page - 1));
   const uint32_t to = ((uint32_t)(32 * quarter) << 16) + C::kTmemV;
   QaRing<C::kStages> st;
-  QaRing<C::kBuffers> vb;
+  QaRing<C::kValueBuffers> vb;
   st.next(team);
   vb.next(team);
 #pragma unroll 1
@@ -788,7 +792,7 @@ __device__ void qa_values(const QaParams& p, int team, uint8_t* ring, QA_SHARED&
     if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
     const int keys = sb.half_keys[st.at];
     if (keys == 0) return;
-    if (u >= C::kBuffers && !qa_wait(&sb.v_free[vb.at], vb.phase ^ 1, wt)) return;
+    if (u >= C::kValueBuffers && !qa_wait(&sb.v_free[vb.at], vb.phase ^ 1, wt)) return;
     tc_fence_after_sync();
     if (on) {
       const uint8_t* stage = ring + st.at * C::kStageBytes;
@@ -1246,10 +1250,12 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
       mbar_init(&sb.empty[i], 8);
     }
     for (int i = 0; i < kQaSched; ++i) mbar_init(&sb.sched_full[i], 1);
-    for (int i = 0; i < C::kBuffers; ++i) {
+    for (int i = 0; i < C::kKeyBuffers; ++i) {
       mbar_init(&sb.k_ready[i], 4);
-      mbar_init(&sb.v_ready[i], 4);
       mbar_init(&sb.k_free[i], 1);
+    }
+    for (int i = 0; i < C::kValueBuffers; ++i) {
+      mbar_init(&sb.v_ready[i], 4);
       mbar_init(&sb.v_free[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
