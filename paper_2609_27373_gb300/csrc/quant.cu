@@ -2,11 +2,13 @@
 // any cache back.  Formulas and layout: quant.cuh.
 //
 // A warp takes 32 neighbouring positions of a sequence (a span, aligned to 32)
-// and 32 channels of one kv head, of the keys or of the values (blockIdx.y).
-// Outside the cache a lane is a token: it reads or writes 64 neighbouring
-// bytes of that token's row, two groups with a scale each.  In the cache that
-// holds for keys too; values lie by channels, so a warp transposes its 32 x 32
-// codes in registers, exchanging lane bit i with index bit i at a time.
+// of one kv head, of the keys or of the values (blockIdx.y), and goes through
+// their channels 32 at a time; where that gives too few warps, each takes 32
+// channels.  Outside the cache a lane is a token: it reads or writes 64
+// neighbouring bytes of that token's row, two groups with a scale each.  In the
+// cache that holds for keys too; values lie by channels, so a warp transposes
+// its 32 x 32 codes in registers, exchanging lane bit i with index bit i at a
+// time.
 #include <algorithm>
 
 #include "cache_common.cuh"
@@ -95,7 +97,7 @@ __device__ __forceinline__ uint32_t encode_group(const uint4& a, const uint4& b,
   float m = largest<FP16>(a, b);
   if (!(m >= 0.0f)) m = 0.0f;  // all NaN
   const uint32_t byte = BITS == 4 ? q_scale4(m) : q_scale8(m);
-  const float inv = byte ? __frcp_rn(q_scale_value(byte)) : 0.0f;
+  const float inv = byte ? __frcp_ru(q_scale_value(byte)) : 0.0f;
   const uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
   for (int k = 0; k < 8; k += 4) {
@@ -173,21 +175,56 @@ __device__ __forceinline__ void store_chunk(uint8_t* to, const uint32_t* w, int 
     *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(v);
 }
 
+// Work of one warp: spans of heads, and for each all channels or 32 of them.
+struct QuantJobs {
+  int parts;    // of 32 channels, of a row
+  int per_job;  // of them that a job has: all or 1
+  int spans;
+  int jobs;
+  bool wide;    // K and V are aligned to 32 bytes
+};
+
+// 64 bytes of a row.
+__device__ __forceinline__ void load_row(const uint8_t* at, bool wide, uint4 (&x)[4]) {
+  if (wide) {
+#pragma unroll
+    for (int k = 0; k < 4; k += 2)
+      asm volatile("ld.global.nc.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                   : "=r"(x[k].x), "=r"(x[k].y), "=r"(x[k].z), "=r"(x[k].w), "=r"(x[k + 1].x), "=r"(x[k + 1].y),
+                     "=r"(x[k + 1].z), "=r"(x[k + 1].w)
+                   : "l"(at + 16 * k));
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = __ldg(reinterpret_cast<const uint4*>(at) + k);
+  }
+}
+__device__ __forceinline__ void store_row(uint8_t* at, bool wide, const uint4 (&x)[4]) {
+  if (wide) {
+#pragma unroll
+    for (int k = 0; k < 4; k += 2)
+      asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(x[k].x), "r"(x[k].y), "r"(x[k].z),
+                   "r"(x[k].w), "r"(x[k + 1].x), "r"(x[k + 1].y), "r"(x[k + 1].z), "r"(x[k + 1].w), "l"(at + 16 * k)
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) reinterpret_cast<uint4*>(at)[k] = x[k];
+  }
+}
+
 template <int BITS, bool FP16>
-__global__ void __launch_bounds__(kIoThreads) quant_write_kernel(const QuantIo io, const QuantShape sh) {
+__global__ void __launch_bounds__(kIoThreads, 4) quant_write_kernel(const QuantIo io, const QuantShape sh,
+                                                                    const QuantJobs jb) {
   extern __shared__ uint32_t seen[];
   const CacheView& c = io.cache;
-  const int lane = threadIdx.x & 31, parts = io.head_dim / 32, spans = spans_of(io.rows);
+  const int lane = threadIdx.x & 31;
   const uint32_t* twice = io.batch > 1 ? mark_twice(c, io.slots, io.batch, seen) : nullptr;
   const bool values = blockIdx.y;
   const uint8_t* in = reinterpret_cast<const uint8_t*>(values ? io.V : io.K);
   uint8_t* plane = c.pool + io.layer * c.plane_bytes;
-  const long long jobs = (long long)io.batch * c.n_kv_heads * spans * parts;
-  for (long long job = (long long)blockIdx.x * kIoWarps + threadIdx.x / 32; job < jobs;
-       job += (long long)gridDim.x * kIoWarps) {
-    const int part = (int)(job % parts);
-    const long long r = job / parts;
-    const int span = (int)(r % spans), bh = (int)(r / spans);
+  for (int job = blockIdx.x * kIoWarps + threadIdx.x / 32; job < jb.jobs; job += gridDim.x * kIoWarps) {
+    const int unit = jb.per_job == 1 ? job / jb.parts : job;
+    const int part0 = jb.per_job == 1 ? job - unit * jb.parts : 0;
+    const int bh = unit / jb.spans, span = unit - bh * jb.spans;
     const int b = bh / c.n_kv_heads, head = bh - b * c.n_kv_heads;
     const int s = io.slots[b], add = io.count ? io.count[b] : io.rows;
     if (s < 0) continue;
@@ -202,6 +239,9 @@ __global__ void __launch_bounds__(kIoThreads) quant_write_kernel(const QuantIo i
     const int base = (start & ~31) + 32 * span;
     const int pos = base + lane;
     const bool on = pos >= start && pos < len;
+    const uint8_t* row = in + (((size_t)bh * io.rows + (on ? pos - start : 0)) * io.head_dim + 32 * part0) * 2;
+    uint4 x[4] = {};
+    if (on) load_row(row, jb.wide, x);
     int page = -1;
     if (on) {
       page = c.table[(size_t)s * c.max_pages + (pos >> c.page_shift)];
@@ -210,66 +250,68 @@ __global__ void __launch_bounds__(kIoThreads) quant_write_kernel(const QuantIo i
         page = -1;
       }
     }
-    uint4 x[4] = {};
-    if (on) {
-      const uint4* from =
-          reinterpret_cast<const uint4*>(in + (((size_t)bh * io.rows + (pos - start)) * io.head_dim + 32 * part) * 2);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = __ldg(from + k);
-    }
-    uint32_t w[BITS];
-    const uint32_t s0 = encode_group<BITS, FP16>(x[0], x[1], w);
-    const uint32_t s1 = encode_group<BITS, FP16>(x[2], x[3], w + BITS / 2);
     const int off = pos & (c.page - 1);
     uint8_t* block = plane + (size_t)max(page, 0) * c.page_bytes + (size_t)head * c.head_bytes;
-    if (!values) {
-      if (page < 0) continue;
-      uint8_t* to = block + ((size_t)part * (BITS / 4) * c.page + off) * 16;
-      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(w);
-      if (BITS == 8) *reinterpret_cast<uint4*>(to + c.page * 16) = *reinterpret_cast<const uint4*>(w + BITS / 2);
-      *reinterpret_cast<uint16_t*>(block + sh.key_scales + off * sh.key_scale_bytes + 2 * part) =
-          (uint16_t)(s0 | s1 << 8);
-      continue;
-    }
-    if (page >= 0) {
-      block[sh.value_scales + 2 * part * c.page + off] = (uint8_t)s0;
-      block[sh.value_scales + (2 * part + 1) * c.page + off] = (uint8_t)s1;
-    }
-    transpose_codes<BITS>(w, lane);
-    // Chunks of T tokens of the span, each in one page.
-    const int channel = 32 * part + lane;
+    // The span's pieces of values in the cache: T tokens each, in one page.
     const int T = BITS == 8 || c.page == 16 ? 16 : 32;
-    for (int t = 0; t < 32; t += T) {
-      const int from = max(start - (base + t), 0);
-      const int p = __shfl_sync(0xffffffffu, page, min(t + from, 31));  // of the chunk's first new token
-      if (from >= T || base + t >= len || p < 0) continue;
-      const int chunk = ((base + t) & (c.page - 1)) / T;
-      uint8_t* to = plane + (size_t)p * c.page_bytes + (size_t)head * c.head_bytes + sh.values +
-                    ((size_t)chunk * io.head_dim + channel) * (T * BITS / 8);
-      if (BITS == 8)
-        store_chunk<4, 8>(to, w + (t ? BITS / 2 : 0), from);
-      else if (T == 32)
-        store_chunk<4, 4>(to, w, from);
-      else
-        store_chunk<2, 4>(to, w + (t ? BITS / 2 : 0), from);
+    const int from0 = max(start - base, 0), from1 = max(start - (base + 16), 0);  // first new tokens
+    const int page0 = __shfl_sync(0xffffffffu, page, min(from0, 31)), page1 = __shfl_sync(0xffffffffu, page, min(16 + from1, 31));
+#pragma unroll 1
+    for (int part = part0; part < part0 + jb.per_job; ++part) {
+      uint32_t w[BITS];
+      const uint32_t s0 = encode_group<BITS, FP16>(x[0], x[1], w);
+      const uint32_t s1 = encode_group<BITS, FP16>(x[2], x[3], w + BITS / 2);
+      if (on && part + 1 < part0 + jb.per_job) {  // the next channels are on their way meanwhile
+        row += 64;
+        load_row(row, jb.wide, x);
+      }
+      if (!values) {
+        if (page >= 0) {
+          uint8_t* to = block + ((size_t)part * (BITS / 4) * c.page + off) * 16;
+          *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(w);
+          if (BITS == 8) *reinterpret_cast<uint4*>(to + c.page * 16) = *reinterpret_cast<const uint4*>(w + BITS / 2);
+          *reinterpret_cast<uint16_t*>(block + sh.key_scales + off * sh.key_scale_bytes + 2 * part) =
+              (uint16_t)(s0 | s1 << 8);
+        }
+        continue;
+      }
+      if (page >= 0) {
+        block[sh.value_scales + 2 * part * c.page + off] = (uint8_t)s0;
+        block[sh.value_scales + (2 * part + 1) * c.page + off] = (uint8_t)s1;
+      }
+      transpose_codes<BITS>(w, lane);
+      const int channel = 32 * part + lane;
+#pragma unroll
+      for (int t = 0; t < 32; t += 16) {
+        if (T == 32 && t) break;
+        const int from = t ? from1 : from0, p = t ? page1 : page0;
+        if (from >= T || base + t >= len || p < 0) continue;
+        uint8_t* to = plane + (size_t)p * c.page_bytes + (size_t)head * c.head_bytes + sh.values +
+                      ((size_t)(((base + t) & (c.page - 1)) / T) * io.head_dim + channel) * (T * BITS / 8);
+        if (BITS == 8)
+          store_chunk<4, 8>(to, w + (t ? BITS / 2 : 0), from);
+        else if (T == 32)
+          store_chunk<4, 4>(to, w, from);
+        else
+          store_chunk<2, 4>(to, w + (t ? BITS / 2 : 0), from);
+      }
     }
   }
 }
 
 // ---------------------------------------------------------------------- read
 template <int BITS, bool FP16>
-__global__ void __launch_bounds__(kIoThreads) read_kernel(const QuantIo io, const QuantShape sh) {
+__global__ void __launch_bounds__(kIoThreads, 4) read_kernel(const QuantIo io, const QuantShape sh, const QuantJobs jb) {
+  constexpr int W = BITS == 8 ? 8 : 4;  // words of a lane's 32 codes
   const CacheView& c = io.cache;
-  const int lane = threadIdx.x & 31, parts = io.head_dim / 32, spans = spans_of(io.rows);
+  const int lane = threadIdx.x & 31;
   const bool values = blockIdx.y;
   uint8_t* out = reinterpret_cast<uint8_t*>(const_cast<void*>(values ? io.V : io.K));
   const uint8_t* plane = c.pool + (BITS == 16 ? 2 * io.layer + values : io.layer) * c.plane_bytes;
-  const long long jobs = (long long)io.batch * c.n_kv_heads * spans * parts;
-  for (long long job = (long long)blockIdx.x * kIoWarps + threadIdx.x / 32; job < jobs;
-       job += (long long)gridDim.x * kIoWarps) {
-    const int part = (int)(job % parts);
-    const long long r = job / parts;
-    const int span = (int)(r % spans), bh = (int)(r / spans);
+  for (int job = blockIdx.x * kIoWarps + threadIdx.x / 32; job < jb.jobs; job += gridDim.x * kIoWarps) {
+    const int unit = jb.per_job == 1 ? job / jb.parts : job;
+    const int part0 = jb.per_job == 1 ? job - unit * jb.parts : 0, part_end = part0 + jb.per_job;
+    const int bh = unit / jb.spans, span = unit - bh * jb.spans;
     const int b = bh / c.n_kv_heads, head = bh - b * c.n_kv_heads;
     const int s = io.slots[b];
     int first = io.first ? io.first[b] : 0, n = io.count ? io.count[b] : io.rows;
@@ -293,67 +335,91 @@ __global__ void __launch_bounds__(kIoThreads) read_kernel(const QuantIo io, cons
         page = -1;
       }
     }
+    const bool row_on = i >= 0 && i < io.rows;
+    uint8_t* to = out + (((size_t)bh * io.rows + (row_on ? i : 0)) * io.head_dim + 32 * part0) * 2;
     const int off = pos & (c.page - 1);
     const uint8_t* block = plane + (size_t)max(page, 0) * c.page_bytes + (size_t)head * c.head_bytes;
-    uint4 y[4] = {};
+    // Where this lane's codes of the first channels lie, and how far it is to the
+    // next ones; for values (a lane is a channel) those of tokens 0 .. 15 and 16
+    // .. 31, or of all, through the page of a token that is read.
+    const int T = BITS == 8 || c.page == 16 ? 16 : 32;
+    const uint8_t *at = block, *at2 = block;
+    int step = 0;
+    bool there = page >= 0, there2 = page >= 0;
     if (BITS == 16) {
-      if (page >= 0) {
-        const uint4* from = reinterpret_cast<const uint4*>(block + (size_t)off * c.row_bytes + 64 * part);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) y[k] = from[k];
-      }
+      at += (size_t)off * c.row_bytes + 64 * part0;
+      step = 64;
+    } else if (!values) {
+      at += ((size_t)part0 * (BITS / 4) * c.page + off) * 16;
+      at2 = at + c.page * 16;
+      step = BITS / 4 * c.page * 16;
     } else {
-      uint32_t w[BITS == 4 ? 4 : 8] = {};
-      uint32_t s0 = 0, s1 = 0;
-      if (!values) {
-        if (page >= 0) {
-          const uint8_t* from = block + ((size_t)part * (BITS / 4) * c.page + off) * 16;
-          *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(from);
-          if (BITS == 8)
-            *reinterpret_cast<uint4*>(w + (BITS == 4 ? 0 : 4)) = *reinterpret_cast<const uint4*>(from + c.page * 16);
-          const uint32_t both =
-              *reinterpret_cast<const uint16_t*>(block + sh.key_scales + off * sh.key_scale_bytes + 2 * part);
-          s0 = both & 255;
-          s1 = both >> 8;
+      const uint32_t sound = __ballot_sync(0xffffffffu, page >= 0);
+      const uint32_t low = T == 32 ? sound : sound & 0xffffu, high = sound >> 16;
+      there = low != 0;
+      there2 = high != 0;
+      const int p0 = __shfl_sync(0xffffffffu, page, low ? __ffs(low) - 1 : 0);
+      const int p1 = __shfl_sync(0xffffffffu, page, high ? 15 + __ffs(high) : 0);
+      const int piece = T * BITS / 8;
+      const uint8_t* rest = plane + (size_t)head * c.head_bytes + sh.values + (32 * part0 + lane) * piece;
+      at = rest + (size_t)max(p0, 0) * c.page_bytes + (size_t)((base & (c.page - 1)) / T) * io.head_dim * piece;
+      at2 = rest + (size_t)max(p1, 0) * c.page_bytes + (size_t)(((base + 16) & (c.page - 1)) / T) * io.head_dim * piece;
+      step = 32 * piece;
+    }
+    const int scale_step = values ? 2 * c.page : 2;
+    const uint8_t* scales =
+        block + (values ? sh.value_scales + 2 * part0 * c.page + off : sh.key_scales + off * sh.key_scale_bytes + 2 * part0);
+    uint4 y[4] = {};
+    uint32_t w[W] = {}, s0 = 0, s1 = 0;
+    auto load = [&]() {  // of 32 channels
+      if constexpr (BITS == 16) {
+        if (there) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) y[k] = __ldg(reinterpret_cast<const uint4*>(at) + k);
         }
       } else {
+        if (BITS == 8) {
+          if (there) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(at);
+          if (there2) *reinterpret_cast<uint4*>(w + W - 4) = *reinterpret_cast<const uint4*>(at2);
+        } else if (!values || T == 32) {
+          if (there) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(at);
+        } else {
+          if (there) *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(at);
+          if (there2) *reinterpret_cast<uint2*>(w + 2) = *reinterpret_cast<const uint2*>(at2);
+        }
         if (page >= 0) {
-          s0 = block[sh.value_scales + 2 * part * c.page + off];
-          s1 = block[sh.value_scales + (2 * part + 1) * c.page + off];
+          s0 = scales[0];
+          s1 = scales[values ? c.page : 1];
         }
-        const int channel = 32 * part + lane;
-        const int T = BITS == 8 || c.page == 16 ? 16 : 32;
-#pragma unroll
-        for (int t = 0; t < 32; t += 16) {
-          if (T == 32 && t) break;
-          // The page of a token of the chunk that is read, if there is one.
-          const uint32_t there = __ballot_sync(0xffffffffu, page >= 0) >> t & (T == 32 ? 0xffffffffu : 0xffffu);
-          const int p = __shfl_sync(0xffffffffu, page, there ? t + __ffs(there) - 1 : 0);
-          if (!there) continue;
-          const int chunk = ((base + t) & (c.page - 1)) / T;
-          const uint8_t* from = plane + (size_t)p * c.page_bytes + (size_t)head * c.head_bytes + sh.values +
-                                ((size_t)chunk * io.head_dim + channel) * (T * BITS / 8);
-          if (BITS == 8 || T == 32)
-            *reinterpret_cast<uint4*>(w + (BITS == 8 && t ? 4 : 0)) = *reinterpret_cast<const uint4*>(from);
-          else
-            *reinterpret_cast<uint2*>(w + (t ? 2 : 0)) = *reinterpret_cast<const uint2*>(from);
-        }
-        transpose_codes<BITS == 4 ? 4 : 8>(w, lane);
       }
-      if (page >= 0) {
+      at += step;
+      at2 += step;
+      scales += scale_step;
+    };
+    load();
+#pragma unroll 1
+    for (int part = part0; part < part_end; ++part) {
+      if constexpr (BITS == 16) {
+        if (row_on) store_row(to, jb.wide, y);
+        if (part + 1 < part_end) load();
+      } else {
+        uint32_t codes[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k) codes[k] = w[k];
+        const uint32_t scale0 = s0, scale1 = s1;
+        if (part + 1 < part_end) load();  // the next channels are on their way meanwhile
+        if (values) transpose_codes<BITS == 8 ? 8 : 4>(codes, lane);
         uint32_t v[8];
-        decode_group<BITS, FP16>(w, s0, v);
+        decode_group<BITS, FP16>(codes, scale0, v);
         y[0] = make_uint4(v[0], v[1], v[2], v[3]);
         y[1] = make_uint4(v[4], v[5], v[6], v[7]);
-        decode_group<BITS, FP16>(w + (BITS == 4 ? 2 : 4), s1, v);
+        decode_group<BITS, FP16>(codes + W / 2, scale1, v);
         y[2] = make_uint4(v[0], v[1], v[2], v[3]);
         y[3] = make_uint4(v[4], v[5], v[6], v[7]);
+        if (page < 0) y[0] = y[1] = y[2] = y[3] = make_uint4(0, 0, 0, 0);
+        if (row_on) store_row(to, jb.wide, y);
       }
-    }
-    if (i >= 0 && i < io.rows) {
-      uint4* to = reinterpret_cast<uint4*>(out + (((size_t)bh * io.rows + i) * io.head_dim + 32 * part) * 2);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) to[k] = y[k];
+      to += 64;
     }
   }
 }
@@ -368,10 +434,24 @@ QuantShape quant_shape(const QuantIo& io) {
   return sh;
 }
 
+// All channels a job while that keeps every SM's warps busy, 32 of them else.
+QuantJobs quant_jobs(const QuantIo& io) {
+  QuantJobs jb;
+  jb.parts = io.head_dim / 32;
+  jb.spans = spans_of(io.rows);
+  jb.jobs = io.batch * io.cache.n_kv_heads * jb.spans;
+  jb.per_job = jb.parts;
+  if (jb.jobs < 16 * io.sm_count) {
+    jb.jobs *= jb.parts;
+    jb.per_job = 1;
+  }
+  jb.wide = ((reinterpret_cast<uintptr_t>(io.K) | reinterpret_cast<uintptr_t>(io.V)) & 31) == 0;
+  return jb;
+}
+
 // Blocks of keys, and as many of values: no more than stay resident.
-int io_blocks(const QuantIo& io) {
-  const long long jobs = (long long)io.batch * io.cache.n_kv_heads * spans_of(io.rows) * (io.head_dim / 32);
-  return (int)std::min<long long>((jobs - 1) / kIoWarps + 1, 4LL * io.sm_count);
+int io_blocks(const QuantIo& io, const QuantJobs& jb) {
+  return std::min((jb.jobs - 1) / kIoWarps + 1, 2 * io.sm_count);
 }
 
 }  // namespace
@@ -385,7 +465,8 @@ cudaError_t launch_kvq_write(const QuantIo& io, cudaStream_t stream) {
         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlots / 32 * 2 * 4);
     if (e != cudaSuccess) return e;
   }
-  kernel<<<dim3(io_blocks(io), 2), kIoThreads, smem, stream>>>(io, quant_shape(io));
+  const QuantJobs jb = quant_jobs(io);
+  kernel<<<dim3(io_blocks(io, jb), 2), kIoThreads, smem, stream>>>(io, quant_shape(io), jb);
   return cudaGetLastError();
 }
 
@@ -393,7 +474,8 @@ cudaError_t launch_kv_read(const QuantIo& io, cudaStream_t stream) {
   auto kernel = io.cache.bits == 4   ? (io.fp16 ? read_kernel<4, true> : read_kernel<4, false>)
                 : io.cache.bits == 8 ? (io.fp16 ? read_kernel<8, true> : read_kernel<8, false>)
                                      : read_kernel<16, true>;
-  kernel<<<dim3(io_blocks(io), 2), kIoThreads, 0, stream>>>(io, quant_shape(io));
+  const QuantJobs jb = quant_jobs(io);
+  kernel<<<dim3(io_blocks(io, jb), 2), kIoThreads, 0, stream>>>(io, quant_shape(io), jb);
   return cudaGetLastError();
 }
 

@@ -72,16 +72,17 @@ __device__ __forceinline__ float q_scale_value(uint32_t byte) {
   return __half2float(__ushort_as_half((unsigned short)(byte << 7)));
 }
 
-// Eight values to one word of e2m1, the first in the lowest bits.  x * (1 / s)
-// may miss a quotient that lies half way between two codes by one unit in the
-// last place, upwards; with the last 8 bits cut off it does not, and other
-// quotients differ from those by more than 2^-12 (x has at most 11 significant
-// bits, a point half way times s at most 7).
+// Eight values to one word of e2m1, the first in the lowest bits; inv is 1 / s
+// rounded up.  A quotient x / s that lies half way between two codes is then
+// hit exactly by x * inv rounded towards zero (the product exceeds it by less
+// than a unit in the last place); other quotients differ from those points by
+// more than 2^-12 (x has at most 11 significant bits, a point half way times s
+// at most 7).
 __device__ __forceinline__ uint32_t q_codes4(const float (&x)[8], float inv) {
   uint32_t w;
   float y[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(__float_as_uint(x[i] * inv) & 0xFFFFFF00u);
+  for (int i = 0; i < 8; ++i) y[i] = __fmul_rz(x[i], inv);
   asm("{\n\t.reg .b8 a, b, c, d;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
