@@ -45,6 +45,10 @@
 
 namespace wise {
 
+// Steps whose S and P are held at a time.  With two, S of a step waited for the
+// softmax of the one before last, and the softmax then for S.
+constexpr int kQaDepth = 3;
+
 template <int D, int BITS, int NMAX>
 struct QaCfg {
   static constexpr int kHalves = NMAX == 16 ? 2 : 1;  // of 128 keys, of a step
@@ -54,10 +58,10 @@ struct QaCfg {
   // Halves of K and of V in tensor memory.  V stays until the softmax has been
   // through its step: with 3 buffers one half of a step had to wait for the
   // products of the step before (32 x 12K tokens: 111 us).
-  static constexpr int kKeyBuffers = 2, kValueBuffers = NMAX == 16 ? 4 : 3;
-  // Columns: K, V, S (two steps), O.
+  static constexpr int kKeyBuffers = 2, kValueBuffers = NMAX == 16 ? 4 : 2;
+  // Columns: K, V, S (of kQaDepth steps), O.
   static constexpr uint32_t kTmemK = 0, kTmemV = 64 * kKeyBuffers, kTmemS = kTmemV + 64 * kValueBuffers,
-                            kTmemO = kTmemS + 2 * kHalves * NMAX;
+                            kTmemO = kTmemS + kQaDepth * kHalves * NMAX;
   static_assert(kTmemO + NMAX <= 512, "tensor memory");
   static constexpr int kBoxes = (D + 63) / 64;
   static constexpr int kBoxBytes = NMAX * 128;
@@ -66,12 +70,12 @@ struct QaCfg {
   static constexpr int kStageBytes = 128 / 16 * q_block_bytes(BITS, D, 16);  // 128 tokens, whatever the page size
   static constexpr int kMaxPlanBytes = 32 * 1024;
   static constexpr int kSumBytes = 2 * (NMAX / 8) * 128 * 8;  // of two steps, a pair of rows' sums for each thread
-  static constexpr int kFixed = 2 * kQBytes + 2 * kPBytes + kSumBytes;
+  static constexpr int kFixed = 2 * kQBytes + kQaDepth * kPBytes + kSumBytes;
   static constexpr int kRoom = (217 * 1024 - 1024 - kMaxPlanBytes - kFixed) / kStageBytes;
   static constexpr int kStages = kRoom < 8 ? kRoom : 8;
   static constexpr int kPlanAt = kFixed + kStages * kStageBytes;
   static constexpr int kSmem = kPlanAt + kMaxPlanBytes + 1024;
-  static_assert(kStages >= 3 && kStageBytes % 128 == 0, "ring");
+  static_assert(kStages >= 2 && kStageBytes % 128 == 0, "ring");
 };
 
 constexpr int kQaSched = 16;
@@ -95,9 +99,9 @@ struct QaShared {
   uint64_t sched_full[kQaSched];
   uint64_t k_ready[NK], k_free[NK];  // 4 warps; products
   uint64_t v_ready[NV], v_free[NV];
-  uint64_t p_ready[2];                // softmax warps
-  uint64_t s_full[2], s_free[2];      // products; softmax warps
-  uint64_t pv_done[2];
+  uint64_t p_ready[kQaDepth];                    // softmax warps
+  uint64_t s_full[kQaDepth], s_free[kQaDepth];   // products; softmax warps
+  uint64_t pv_done[kQaDepth];
   uint64_t q_ready[2], q_free[2];  // q_free: the products and the softmax warps
   uint64_t done[2];
   int4 sched[kQaSched][2];
@@ -598,14 +602,15 @@ __device__ void qa_products_s(const QaParams& p, uint8_t* q_tiles, QA_SHARED& sb
   const uint64_t desc = smem_desc_sw128(0, 16, 1024);
   const uint32_t hi = (uint32_t)(desc >> 32), q_lo = (uint32_t)desc + (smem_u32(q_tiles) >> 4);
   QaRing<C::kKeyBuffers> kb;
+  QaRing<kQaDepth> r;
   int seg = -1;
 #pragma unroll 1
-  for (int t = 0;; ++t) {
+  for (int t = 0;; ++t, r.next()) {
     if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) break;
     const int info = __shfl_sync(0xffffffffu, sb.sched[t % kQaSched][0].x, 0);
-    const int b = t & 1;
-    // (The end too waits for the softmax to have seen the step two before.)
-    if (t >= 2 && !qa_wait(&sb.s_free[b], ((t >> 1) - 1) & 1, wt)) break;
+    const int b = r.at;
+    // (The end too waits for the softmax to have seen the step that had this buffer.)
+    if (t >= kQaDepth && !qa_wait(&sb.s_free[b], r.phase ^ 1, wt)) break;
     if (info & kQaEnd) {
       if (elect_one()) {
         mbar_arrive(&sb.s_full[b]);
@@ -650,13 +655,14 @@ __device__ void qa_products_pv(const QaParams& p, uint8_t* p_tiles, QA_SHARED& s
   const uint64_t desc = smem_desc_sw128(0, 16, 1024);
   const uint32_t hi = (uint32_t)(desc >> 32), p_lo = (uint32_t)desc + (smem_u32(p_tiles) >> 4);
   QaRing<C::kValueBuffers> vb;
+  QaRing<kQaDepth> r;
 #pragma unroll 1
-  for (int t = 0;; ++t) {
+  for (int t = 0;; ++t, r.next()) {
     if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) break;
     const int info = __shfl_sync(0xffffffffu, sb.sched[t % kQaSched][0].x, 0);
     if (info & kQaEnd) break;
-    const int b = t & 1;
-    if (!qa_wait(&sb.p_ready[b], (t >> 1) & 1, wt)) break;
+    const int b = r.at;
+    if (!qa_wait(&sb.p_ready[b], r.phase, wt)) break;
     const uint32_t idesc = qa_idesc(info);
     bool ok = true;
 #pragma unroll 1
@@ -920,7 +926,7 @@ __device__ __noinline__ bool qa_segment_end(const QaParams& p, Shared& sb, const
                                             bool faulty) {
   const QaGroup<NMAX> q;
   const int u = t - 1;
-  if (!qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt)) return false;
+  if (!qa_wait(&sb.pv_done[u % kQaDepth], (u / kQaDepth) & 1, wt)) return false;
   tc_fence_after_sync();
   const int4 e0 = sb.sched[u % kQaSched][0], e1 = sb.sched[u % kQaSched][1];
   const int kind = qa_kind(e0.x), end = q.row0() + q.rows(qa_rows(e0.x));
@@ -977,7 +983,7 @@ __device__ __noinline__ void qa_mask(Shared& sb, int t, int seg, int rows) {
     const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][n0 + 2 * (q.lane & 3)]);
 #pragma unroll 1
     for (int h = 0; h < 2 * H; ++h) {
-      const uint32_t at = q.lanes() + ((uint32_t)(16 * (h & 1)) << 16) + TMEM_S + ((t & 1) * H + (h >> 1)) * NMAX + n0;
+      const uint32_t at = q.lanes() + ((uint32_t)(16 * (h & 1)) << 16) + TMEM_S + (t % kQaDepth * H + (h >> 1)) * NMAX + n0;
       const int key = key0 + 128 * (h >> 1) + 16 * (h & 1);
       uint32_t r[1][1][4];
       qa_load_8(at, r[0][0]);
@@ -1005,7 +1011,7 @@ template <int D, int NMAX, int H, uint32_t TMEM_S, uint32_t TMEM_O, class Shared
 __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait& wt, int t, int seg, bool ok,
                                     bool faulty, float2* sums) {
   const QaGroup<NMAX> q;
-  const int lane = q.lane, b = t & 1;
+  const int lane = q.lane, b = t % kQaDepth;
   const int2 e = ok ? *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]) : make_int2(kQaEnd, 0);
   const int row0 = q.row0(), row_end = row0 + q.rows(qa_rows(e.x));
   const bool end = e.x & kQaEnd, first = e.x & kQaFirst;
@@ -1075,7 +1081,7 @@ __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait&
   }
   if (!first && ok) {  // O in units of the new references
     const int u = t - 1;
-    if ((ok = qa_wait(&sb.pv_done[u & 1], (u >> 1) & 1, wt)) && 32 * q.w < D) {
+    if ((ok = qa_wait(&sb.pv_done[u % kQaDepth], (u / kQaDepth) & 1, wt)) && 32 * q.w < D) {
       tc_fence_after_sync();
 #pragma unroll 1
       for (int n0 = row0; n0 < row_end; n0 += 4) {
@@ -1114,12 +1120,12 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
   constexpr int kSumsStep = NMAX / 8 * 128;
   int seg = -1;
   bool ok = true, faulty = false;
+  QaRing<kQaDepth> r3;
   // Once a wait of a warp has run out, the next vote ends all; every step has one.
 #pragma unroll 1
-  for (int t = 0;; ++t) {
-    const int b = t & 1;
-    ok = ok && qa_wait(&sb.s_full[b], (t >> 1) & 1, wt) &&
-         (t < 2 || qa_wait(&sb.pv_done[b], ((t >> 1) - 1) & 1, wt));
+  for (int t = 0;; ++t, r3.next()) {
+    const int b = r3.at, odd = t & 1;
+    ok = ok && qa_wait(&sb.s_full[b], r3.phase, wt) && (t < kQaDepth || qa_wait(&sb.pv_done[b], r3.phase ^ 1, wt));
     const int2 e = *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]);
     const int info = ok ? e.x : kQaEnd, rows = q.rows(qa_rows(info));
     bool turn = info & (kQaFirst | kQaEnd), turned = false;
@@ -1145,8 +1151,8 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
           }
           const int n = q.row0() + 8 * g2 + 2 * (lane & 3);
           const float *shifts = &sb.shift[seg & 1][n], *scales = &sb.q_scale[seg & 1][n];
-          float2* const from = sums + (b ^ 1) * kSumsStep + g2 * 128;
-          float2* const to = sums + b * kSumsStep + g2 * 128;
+          float2* const from = sums + (odd ^ 1) * kSumsStep + g2 * 128;
+          float2* const to = sums + odd * kSumsStep + g2 * 128;
           float2 scale[kAt], shift[kAt], l[kAt];
 #pragma unroll
           for (int k = 0; k < kAt; ++k) {
@@ -1184,7 +1190,7 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
         turn = top > 15.0f;
       }
       if (!q.vote(turn)) break;
-      const int next = qa_turn<D, NMAX, H, C::kTmemS, C::kTmemO>(p, sb, wt, t, seg, ok, faulty, sums + (b ^ 1) * kSumsStep);
+      const int next = qa_turn<D, NMAX, H, C::kTmemS, C::kTmemO>(p, sb, wt, t, seg, ok, faulty, sums + (odd ^ 1) * kSumsStep);
       if (next == 0) return;
       ok = next == 1;
       if (info & kQaFirst) faulty = false;
@@ -1258,11 +1264,13 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
       mbar_init(&sb.v_ready[i], 4);
       mbar_init(&sb.v_free[i], 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kQaDepth; ++i) {
       mbar_init(&sb.p_ready[i], 4 * C::kGroups);
       mbar_init(&sb.s_full[i], 2);
       mbar_init(&sb.s_free[i], 4 * C::kGroups);
       mbar_init(&sb.pv_done[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
       mbar_init(&sb.q_ready[i], 1);
       mbar_init(&sb.q_free[i], 4 * C::kGroups + 1);
       mbar_init(&sb.done[i], 1);
@@ -1282,7 +1290,7 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
   const QaWait wt = {&sb.abort, p.cache.status, p.wait_ns};
 
   if (warp < 4 * C::kGroups) {
-    qa_softmax<D, BITS, NMAX>(p, p_tiles, reinterpret_cast<float2*>(p_tiles + 2 * C::kPBytes), sb, wt);
+    qa_softmax<D, BITS, NMAX>(p, p_tiles, reinterpret_cast<float2*>(p_tiles + kQaDepth * C::kPBytes), sb, wt);
   } else {
     if (warp < kOther) {
       const int k = warp / 4 - C::kGroups;
