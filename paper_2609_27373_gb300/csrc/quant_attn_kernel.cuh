@@ -637,14 +637,17 @@ __device__ void qa_products_s(const QaParams& p, uint8_t* q_tiles, QA_SHARED& sb
         umma_commit(&sb.k_free[kb.at]);
         if (128 * (h + 1) >= qa_keys_of(info)) {
           umma_commit(&sb.s_full[b]);
-          mbar_arrive(&sb.s_full[b]);  // and what this warp knows of the schedule and the queries
           if (info & kQaLast) umma_commit(&sb.q_free[seg & 1]);
         }
       }
       __syncwarp();
       kb.next();
     }
-    if (!ok) break;
+    // The softmax also learns here what this warp knows: the schedule, the
+    // queries, and that P's buffer has been read (a wait less on its own way).
+    if (!ok || (t >= kQaDepth && !qa_wait(&sb.pv_done[b], r.phase ^ 1, wt))) break;
+    if (elect_one()) mbar_arrive(&sb.s_full[b]);
+    __syncwarp();
   }
   qa_products_done(&sb.done[0]);
 }
@@ -1125,7 +1128,7 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
 #pragma unroll 1
   for (int t = 0;; ++t, r3.next()) {
     const int b = r3.at, odd = t & 1;
-    ok = ok && qa_wait(&sb.s_full[b], r3.phase, wt) && (t < kQaDepth || qa_wait(&sb.pv_done[b], r3.phase ^ 1, wt));
+    ok = ok && qa_wait(&sb.s_full[b], r3.phase, wt);
     const int2 e = *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]);
     const int info = ok ? e.x : kQaEnd, rows = q.rows(qa_rows(info));
     bool turn = info & (kQaFirst | kQaEnd), turned = false;
