@@ -359,6 +359,14 @@ __device__ __forceinline__ bool qa_wait(uint64_t* bar, uint32_t parity, const Qa
   return qa_wait_long(bar, parity, w.abort, w.status, w.limit);
 }
 
+// Two phases, with one latency where both are complete.
+__device__ __forceinline__ bool qa_wait_both(uint64_t* a, uint32_t parity_a, uint64_t* b, uint32_t parity_b,
+                                             const QaWait& w) {
+  const bool first = mbar_test_wait(a, parity_a), second = mbar_test_wait(b, parity_b);
+  if (__builtin_expect(__all_sync(0xffffffffu, first && second), 1)) return true;
+  return qa_wait(a, parity_a, w) && qa_wait(b, parity_b, w);
+}
+
 // A place in a ring of N, and how often the ring has been passed.
 template <int N>
 struct QaRing {
@@ -723,10 +731,10 @@ __device__ void qa_keys(const QaParams& p, int team, uint8_t* ring, QA_SHARED& s
   kb.next(team);
 #pragma unroll 1
   for (int u = team;; u += C::kKeyTeams) {  // halves
-    if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
+    // (A buffer that has not been used yet counts as free: its phase before the first.)
+    if (!qa_wait_both(&sb.full[st.at], st.phase, &sb.k_free[kb.at], kb.phase ^ 1, wt)) return;
     const int keys = sb.half_keys[st.at];
     if (keys == 0) return;
-    if (u >= C::kKeyBuffers && !qa_wait(&sb.k_free[kb.at], kb.phase ^ 1, wt)) return;
     tc_fence_after_sync();
     const uint8_t* data = data_at + st.at * C::kStageBytes;
     const uint8_t* scales = scales_at + st.at * C::kStageBytes;
@@ -798,10 +806,10 @@ __device__ void qa_values(const QaParams& p, int team, uint8_t* ring, QA_SHARED&
   vb.next(team);
 #pragma unroll 1
   for (int u = team;; u += C::kTeams) {  // halves
-    if (!qa_wait(&sb.full[st.at], st.phase, wt)) return;
+    // (A buffer that has not been used yet counts as free: its phase before the first.)
+    if (!qa_wait_both(&sb.full[st.at], st.phase, &sb.v_free[vb.at], vb.phase ^ 1, wt)) return;
     const int keys = sb.half_keys[st.at];
     if (keys == 0) return;
-    if (u >= C::kValueBuffers && !qa_wait(&sb.v_free[vb.at], vb.phase ^ 1, wt)) return;
     tc_fence_after_sync();
     if (on) {
       const uint8_t* stage = ring + st.at * C::kStageBytes;
