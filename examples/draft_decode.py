@@ -2,7 +2,7 @@
 its last step's keys and values go into a paged cache, the samples are forks of it, and every round drafts, verifies
 and drops.
 
-    python examples/draft_decode.py --samples 8 --rounds 12 --draft 4
+    python examples/draft_decode.py --samples 8 --rounds 12 --draft 4 --bits 4
 
 The model is a stand-in (random embeddings and projections, one attention layer, a draft that is the model with noise on
 its logits): it shows the calls in their order of use, not language.
@@ -57,8 +57,8 @@ def prefill(model, prompt, steps=4, discovery=2):
     return K, V
 
 
-def run(samples=8, rounds=12, draft=4, prompt_len=512, vocab=997, share=True, seed=0):
-    """Returns each sample's tokens, and the cache."""
+def run(samples=8, rounds=12, draft=4, prompt_len=512, vocab=997, share=True, seed=0, bits=16):
+    """Returns each sample's tokens, and the cache (of keys and values in 16, 8 or 4 bits)."""
     torch.manual_seed(seed)
     model = StandIn(vocab, 8, 2, 64, seed)
     g = torch.Generator(device="cuda").manual_seed(seed + 1)
@@ -66,7 +66,7 @@ def run(samples=8, rounds=12, draft=4, prompt_len=512, vocab=997, share=True, se
     page = 32
     pages_each = -(-(draft + 1) * (rounds + 1) // page) + 1
     cache = serve.PagedCache(n_layers=1, n_pages=prompt_len // page + 2 + samples * pages_each, n_kv_heads=2, page=page,
-                             head_dim=64, n_slots=samples + 1, max_pages=prompt_len // page + pages_each + 1)
+                             head_dim=64, n_slots=samples + 1, max_pages=prompt_len // page + pages_each + 1, bits=bits)
     i32 = dict(dtype=torch.int32, device="cuda")
 
     # The prompt (all but its last token, which every sample feeds itself) into slot 0, then a fork per sample.
@@ -114,8 +114,9 @@ if __name__ == "__main__":
     ap.add_argument("--samples", type=int, default=8)
     ap.add_argument("--rounds", type=int, default=12)
     ap.add_argument("--draft", type=int, default=4)
+    ap.add_argument("--bits", type=int, default=16, choices=(16, 8, 4))
     args = ap.parse_args()
-    answers, cache, n_live = run(args.samples, args.rounds, args.draft)
+    answers, cache, n_live = run(args.samples, args.rounds, args.draft, bits=args.bits)
     for s, a in enumerate(answers):
         print(f"sample {s}: {len(a)} tokens: {' '.join(map(str, a[:16]))} ...")
     print(f"{n_live} of {cache.n_pages} pages in use after half of the samples ended")

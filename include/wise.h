@@ -509,7 +509,7 @@ int wise_get_status(cudaStream_t stream);
 
 /* Sets the time limit of each internal wait of the attention kernels
  * (wise_full_attn_accumulate, its _noalloc variant, wise_sparse_attn,
- * wise_freeze_a_attn and wise_prefix_attn) for every later launch in this process; ns == 0
+ * wise_freeze_a_attn, wise_prefix_attn and wise_kvq_attn) for every later launch in this process; ns == 0
  * restores the default of 2 s.  A wait that runs out makes the kernel stop
  * issuing work, let the work already in flight finish, and record
  * WISE_ERR_TIMEOUT for wise_get_status(); the outputs of that launch are then

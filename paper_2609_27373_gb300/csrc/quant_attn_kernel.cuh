@@ -63,6 +63,7 @@ struct QaCfg {
   static constexpr uint32_t kTmemK = 0, kTmemV = 64 * kKeyBuffers, kTmemS = kTmemV + 64 * kValueBuffers,
                             kTmemO = kTmemS + kQaDepth * kHalves * NMAX;
   static_assert(kTmemO + NMAX <= 512, "tensor memory");
+  static_assert(kKeyTeams <= kTeams, "the end is told to each team of V");
   static constexpr int kBoxes = (D + 63) / 64;
   static constexpr int kBoxBytes = NMAX * 128;
   static constexpr int kQBytes = kBoxes * kBoxBytes;
@@ -335,27 +336,21 @@ static __device__ __noinline__ void qa_give_up(int* abort, int* status) {
   *reinterpret_cast<volatile int*>(abort) = 1;
   atomicOr(status, kStatusTimeout);
 }
-// Suspends for up to 10 us before it says that the phase is not complete.
-__device__ __forceinline__ bool qa_try_wait(uint64_t* bar, uint32_t parity) {
-  uint32_t done;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}\n"
-      : "=r"(done)
-      : "r"(smem_u32(bar)), "r"(parity), "r"(10000u)
-      : "memory");
-  return done != 0;
-}
-static __device__ __noinline__ bool qa_wait_long(uint64_t* bar, uint32_t parity, int* abort, int* status,
+// After a first try, which the hardware holds for some microseconds.
+static __device__ __noinline__ bool qa_wait_long(uint64_t* bar, uint32_t parity, volatile int* abort, int* status,
                                                  unsigned long long limit) {
-  const bool ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort, limit));
-  if (!ok && (threadIdx.x & 31) == 0) qa_give_up(abort, status);
-  return ok;
+  const uint64_t t0 = global_timer_ns() - 1000;
+  for (;;) {
+    if (__any_sync(0xffffffffu, *abort != 0 || global_timer_ns() - t0 > limit)) {
+      if ((threadIdx.x & 31) == 0) qa_give_up(const_cast<int*>(abort), status);
+      return false;
+    }
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  }
 }
 // All lanes of a warp.
 __device__ __forceinline__ bool qa_wait(uint64_t* bar, uint32_t parity, const QaWait& w) {
-  if (__builtin_expect(__all_sync(0xffffffffu, qa_try_wait(bar, parity)), 1)) return true;
+  if (__builtin_expect(__all_sync(0xffffffffu, mbar_try_wait(bar, parity)), 1)) return true;
   return qa_wait_long(bar, parity, w.abort, w.status, w.limit);
 }
 

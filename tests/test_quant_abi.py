@@ -112,3 +112,48 @@ def test_cache_arguments(monkeypatch):
     assert wise.Cache(plain, *lists).bits == 16
     with pytest.raises(ValueError):
         wise.Cache(plain, *lists, page=32)
+
+
+class Library:
+    """Takes down which calls are made."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append(name)
+            return 64 if name.endswith("workspace") or name.endswith("bytes") else 0
+        return call
+
+
+def test_a_cache_makes_the_calls_of_its_kind(monkeypatch):
+    """PagedCache.write, attend and read with 16 and with fewer bits; keys of another type than the cache's are refused."""
+    from paper_2609_27373_gb300 import serve
+    lib = Library()
+    monkeypatch.setattr(wise, "load", lambda: lib)
+    monkeypatch.setattr(wise, "_check", lambda *a: None)
+    monkeypatch.setattr(wise, "_current_raw", lambda index: 0)
+    monkeypatch.setattr(wise, "_current_device", lambda: -1)
+    monkeypatch.setattr(serve.PagedCache, "_use", lambda self, stream: 0)
+    monkeypatch.setattr(serve, "_empty", lambda shape, dtype, device, stream: torch.empty(shape, dtype=dtype))
+    lists = [torch.zeros((2, 2), dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)]
+    slots = torch.zeros(1, dtype=torch.int32)
+    for bits, write, attn in ((16, "wise_kv_write", "wise_prefix_attn"), (8, "wise_kvq_write", "wise_kvq_attn"),
+                              (4, "wise_kvq_write", "wise_kvq_attn")):
+        if bits == 16:
+            c = serve.PagedCache.over(torch.zeros((2, 3, 2, 16, 64), dtype=torch.float16), *lists)
+        else:
+            c = serve.PagedCache.over(torch.zeros((1, 3, 2, 64), dtype=torch.uint8), *lists, bits=bits, page=16, head_dim=64,
+                                      dtype=torch.float16)
+        x = torch.zeros((1, 2, 1, 64), dtype=torch.float16)
+        lib.calls.clear()
+        c.write(0, slots, None, x, x)
+        c.attend(0, x, x.clone(), slots)
+        c.read(0, x, x.clone(), slots)
+        assert lib.calls == [write, attn + "_workspace", attn, "wise_kv_read"]
+        for call in (lambda y: c.write(0, slots, None, y, y), lambda y: c.attend(0, y, y, slots), lambda y: c.read(0, y, y, slots)):
+            for bad in (x.bfloat16(), torch.zeros((1, 2, 1, 128), dtype=torch.float16)[..., ::2],
+                        torch.zeros((1, 2, 1, 32), dtype=torch.float16)):
+                with pytest.raises(ValueError):
+                    call(bad)
