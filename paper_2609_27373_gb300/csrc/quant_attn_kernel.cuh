@@ -13,16 +13,18 @@
 // to 16 query rows an item), 128 in the wide one (up to 64).  The cache's side
 // moves by halves of 128 keys, one row of the product's M each.
 //
-// Warp roles (768 threads, 640 in the wide instance):
+// Warp roles (768 threads):
 //   4 warps      softmax (8 in the wide instance, each 4 for 32 of the rows): S^T from tensor memory in fragments of 8 keys x 8
 //                rows, running maximum (raised only when a numerator passes
 //                2^15, which the warps vote on), numerators as fp16 to
 //                shared memory (P, the B operand of the second product), O's
-//                rescaling and the end of a segment;
+//                rescaling;
 //   then in turn (two teams of each that take every other half, in the wide
 //                instance one)
 //                K: codes to tensor memory;
 //                V: the same, scales of 8 tokens at a time;
+//   4 warps      results: O, or a partial result, of segments that have ended, while
+//                the softmax goes on with the next (O is held twice);
 //   a warp       producer: page look-ups, one bulk copy a page (codes and scales
 //                of keys and values lie together), the schedule;
 //   a warp       Q: rows of the next segment to shared memory as fp16, each scaled by
@@ -45,24 +47,23 @@
 
 namespace wise {
 
-// Steps whose S and P are held at a time.  With two, S of a step waited for the
-// softmax of the one before last, and the softmax then for S.
-constexpr int kQaDepth = 3;
-
 template <int D, int BITS, int NMAX>
 struct QaCfg {
   static constexpr int kHalves = NMAX == 16 ? 2 : 1;  // of 128 keys, of a step
-  // Warpgroups: softmax, K, V (teams that take the halves in turn), and one for the rest.
+  // Warpgroups: softmax, K, V (teams that take the halves in turn), one that writes
+  // results, and one for the rest.
   static constexpr int kGroups = NMAX == 16 ? 1 : 2, kKeyTeams = 1, kTeams = NMAX == 16 ? 2 : 1;
-  static constexpr int kThreads = 128 * (kGroups + kKeyTeams + kTeams + 1);
+  static constexpr int kThreads = 128 * (kGroups + kKeyTeams + kTeams + 2);
   // Halves of K and of V in tensor memory.  V stays until the softmax has been
   // through its step: with 3 buffers one half of a step had to wait for the
   // products of the step before (32 x 12K tokens: 111 us).
   static constexpr int kKeyBuffers = 2, kValueBuffers = NMAX == 16 ? 4 : 2;
-  // Columns: K, V, S (of kQaDepth steps), O.
+  // Steps whose S and P are held at a time.
+  static constexpr int kDepth = 3, kOuts = NMAX == 16 ? 2 : 1;  // and segments whose O is
+  // Columns: K, V, S, O.
   static constexpr uint32_t kTmemK = 0, kTmemV = 64 * kKeyBuffers, kTmemS = kTmemV + 64 * kValueBuffers,
-                            kTmemO = kTmemS + kQaDepth * kHalves * NMAX;
-  static_assert(kTmemO + NMAX <= 512, "tensor memory");
+                            kTmemO = kTmemS + kDepth * kHalves * NMAX;
+  static_assert(kTmemO + kOuts * NMAX <= 512, "tensor memory");
   static_assert(kKeyTeams <= kTeams, "the end is told to each team of V");
   static constexpr int kBoxes = (D + 63) / 64;
   static constexpr int kBoxBytes = NMAX * 128;
@@ -71,7 +72,7 @@ struct QaCfg {
   static constexpr int kStageBytes = 128 / 16 * q_block_bytes(BITS, D, 16);  // 128 tokens, whatever the page size
   static constexpr int kMaxPlanBytes = 32 * 1024;
   static constexpr int kSumBytes = 2 * (NMAX / 8) * 128 * 8;  // of two steps, a pair of rows' sums for each thread
-  static constexpr int kFixed = 2 * kQBytes + kQaDepth * kPBytes + kSumBytes;
+  static constexpr int kFixed = 2 * kQBytes + kDepth * kPBytes + kSumBytes;
   static constexpr int kRoom = (217 * 1024 - 1024 - kMaxPlanBytes - kFixed) / kStageBytes;
   static constexpr int kStages = kRoom < 8 ? kRoom : 8;
   static constexpr int kPlanAt = kFixed + kStages * kStageBytes;
@@ -94,30 +95,35 @@ __device__ __forceinline__ int qa_rows(int info) { return (info >> 8) & 255; }
 __device__ __forceinline__ int qa_kind(int info) { return (info >> 16) & 1; }
 __device__ __forceinline__ int qa_keys_of(int info) { return info >> 20; }
 
-template <int NS, int NK, int NV, int NT, int NG>
+template <int NS, int NK, int NV, int NT, int NG, int ND>
 struct QaShared {
   uint64_t full[NS], empty[NS];  // empty: 8 warps
-  uint64_t sched_full[kQaSched];
+  uint64_t sched_full[kQaSched], seg_full[kQaSched];
   uint64_t k_ready[NK], k_free[NK];  // 4 warps; products
   uint64_t v_ready[NV], v_free[NV];
-  uint64_t p_ready[kQaDepth];                    // softmax warps
-  uint64_t s_full[kQaDepth], s_free[kQaDepth];   // products; softmax warps
-  uint64_t pv_done[kQaDepth];
+  uint64_t p_ready[ND];              // softmax warps
+  uint64_t s_full[ND], s_free[ND];   // products; softmax warps
+  uint64_t pv_done[ND];
+  uint64_t o_full[2], o_free[2];     // a segment's products; 4 warps that have read O
+  uint64_t end_ready[2];             // softmax warps: what ends a segment is written
   uint64_t q_ready[2], q_free[2];  // q_free: the products and the softmax warps
   uint64_t done[2];
-  int4 sched[kQaSched][2];
+  int4 sched[kQaSched][2], segs[kQaSched][2];
   alignas(16) int lim[2][kQaRows];  // keys that a row sees, 0 for none
   int min_lim[2];            // the least of those that see any
+  int q_from[kQaRows];       // where a row comes from, -1 for a row of 0
   alignas(16) float q_scale[2][kQaRows];  // a row's logits in base-2 units = S * q_scale
-  alignas(16) float warp_max[4 * NG][kQaRows];
+  alignas(16) float warp_max[2][4][kQaRows];
   alignas(16) float shift[2][kQaRows];  // added to a row's logits: 7 minus the reference, 0 where nothing is seen
   alignas(16) float top[2][kQaRows];    // the reference less 7, -inf where nothing is seen
   alignas(16) float factor[kQaRows];    // of O and the sums where the references have moved
-  alignas(16) float sums[4 * NG][kQaRows];
+  // Of a segment that ends: its last step's entry and its rows' sums by warp.
+  int4 last[2][2];
+  alignas(16) float sums[2][4][kQaRows];
   alignas(16) int4 value_scales[4 * NT][32];  // a warp's two groups x 128 tokens as fp16
   int half_keys[NS];  // keys of the half in a stage, 0 at the end
   uint32_t tmem_base;
-  int abort, warp_ok[4 * NG];
+  int abort, failed[NG];  // failed: a wait of one of the group's warps has run out
 };
 
 // ---------------------------------------------------------------------- plan
@@ -395,7 +401,7 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 
 #define QA_SHARED QaShared<QaCfg<D, BITS, NMAX>::kStages, QaCfg<D, BITS, NMAX>::kKeyBuffers, \
                                 QaCfg<D, BITS, NMAX>::kValueBuffers, QaCfg<D, BITS, NMAX>::kTeams, \
-                                QaCfg<D, BITS, NMAX>::kGroups>
+                                QaCfg<D, BITS, NMAX>::kGroups, QaCfg<D, BITS, NMAX>::kDepth>
 
 // ------------------------------------------------------------------ producer
 template <int D, int BITS, int NMAX>
@@ -409,7 +415,7 @@ __device__ void qa_producer(const QaParams& p, const QaPlan& plan, uint8_t* ring
   walk.begin(plan, kQaOwn);
   QaSeg seg;
   QaRing<NS> st;
-  int n = 0, t = 0, bad = 0;
+  int n = 0, t = 0, k = 0, bad = 0;
   bool ok = true;
   while (ok && walk.next(p, plan, seg)) {
     int flags = kQaFirst;
@@ -419,6 +425,12 @@ __device__ void qa_producer(const QaParams& p, const QaPlan& plan, uint8_t* ring
                  : -1;
     };
     int page = look(seg.pos);
+    if (lane == 0) {
+      sb.segs[k % kQaSched][0] = make_int4(seg.req, seg.kvh, seg.row0, seg.rows);
+      sb.segs[k % kQaSched][1] = make_int4(seg.kind, seg.end, 0, 0);
+      mbar_arrive(&sb.seg_full[k % kQaSched]);
+    }
+    ++k;
     for (; ok && seg.left > 0; --seg.left, seg.pos += kKeys, flags = 0) {
       const bool on = at < kKeys && seg.pos + at < seg.end;
       const bool valid = on && valid_page(c, page);
@@ -454,7 +466,11 @@ __device__ void qa_producer(const QaParams& p, const QaPlan& plan, uint8_t* ring
       if (seg.left > 1) page = look(seg.pos + kKeys);
     }
   }
-  // The end, for each of the teams.
+  // The end, for the queries and each of the teams.
+  if (lane == 0) {
+    sb.segs[k % kQaSched][0] = make_int4(0, 0, 0, 0);
+    mbar_arrive(&sb.seg_full[k % kQaSched]);
+  }
 #pragma unroll 1
   for (int k = 0; ok && k < C::kTeams; ++k) {
     if (n + k >= NS && !(ok = qa_wait(&sb.empty[st.at], st.phase ^ 1, wt))) break;
@@ -490,77 +506,82 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
   using C = QaCfg<D, BITS, NMAX>;
   constexpr int kPieces = D / 8;  // of 16 bytes, of a row
   const int lane = threadIdx.x & 31;
-  QaWalk walk;
-  walk.begin(plan, kQaOwn);
-  QaSeg seg;
-  for (int k = 0; walk.next(p, plan, seg); ++k) {
+  for (int k = 0;; ++k) {
     const int buf = k & 1;
+    if (!qa_wait(&sb.seg_full[k % kQaSched], (k / kQaSched) & 1, wt)) break;
+    const int4 a = sb.segs[k % kQaSched][0], e = sb.segs[k % kQaSched][1];
+    struct {
+      int req, kvh, row0, rows, kind, end;
+    } const seg = {a.x, a.y, a.z, a.w, e.x, e.y};
+    if (seg.rows == 0) break;
     if (k >= 2 && !qa_wait(&sb.q_free[buf], ((k >> 1) - 1) & 1, wt)) break;
+    // Loops are left as loops: a segment's code is not in the nearest cache when
+    // it begins, and straight code costs its fetch.
+    const int all = (seg.rows + 15) & ~15;
     int least = INT_MAX;
 #pragma unroll 1
-    for (int n = lane; n < seg.rows; n += 32) {
-      const int r = n / p.rows, row = seg.row0 + n - r * p.rows;  // (own items: r = 0)
-      const int i = row % p.q_len, req = seg.req + r;
-      int lim = 0;
-      if (i < plan.add[req]) lim = max(min(plan.len[req] - plan.add[req] + i + 1, seg.end), 0);
-      sb.lim[buf][n] = lim;
-      if (lim > 0) least = min(least, lim);
+    for (int n = lane; n < all; n += 32) {
+      int lim = 0, r = 0;
+      if (n < seg.rows) {
+        if (seg.kind != kQaOwn) r = n / p.rows;
+        const int row = seg.row0 + n - r * p.rows, i = row % p.q_len, req = seg.req + r;
+        if (i < plan.add[req]) lim = max(min(plan.len[req] - plan.add[req] + i + 1, seg.end), 0);
+        if (lim > 0) least = min(least, lim);
+        sb.lim[buf][n] = lim;
+      }
+      sb.q_scale[buf][n] = fmaxf(p.scale_log2, FLT_MIN);
+      sb.q_from[n] = lim > 0 ? n + r * (p.cache.n_kv_heads - 1) * p.rows : -1;  // in rows
     }
     least = __reduce_min_sync(0xffffffffu, least);
     if (lane == 0) sb.min_lim[buf] = least;
     __syncwarp();
     // Rows of one request are contiguous: Q is [batch][n_kv_heads][rows][D].  A
-    // row takes kPieces lanes; kMany rows of each are on their way at a time.
-    // Rows up to the product's N, and those that see nothing (which may hold
-    // anything), are 0.
-    constexpr int kAtOnce = 32 / kPieces, kMany = 4;
+    // row takes kPieces lanes.  Rows up to the product's N, and those that see
+    // nothing (which may hold anything), are 0.
+    constexpr int kAtOnce = 32 / kPieces;
     const int sub = lane / kPieces, piece = lane - sub * kPieces;
-    const size_t row_bytes = (size_t)D * 2;
     const uint8_t* Q = reinterpret_cast<const uint8_t*>(p.Q) +
-                       (((size_t)seg.req * p.cache.n_kv_heads + seg.kvh) * p.rows + seg.row0) * row_bytes + 16 * piece;
-    const size_t next_req = (size_t)(p.cache.n_kv_heads - 1) * p.rows * row_bytes;  // beyond the rows between
+                       (((size_t)seg.req * p.cache.n_kv_heads + seg.kvh) * p.rows + seg.row0) * (D * 2) + 16 * piece;
     uint8_t* tile = q_tiles + buf * C::kQBytes + (piece >> 3) * C::kBoxBytes;
-    const int all = (seg.rows + 15) & ~15;
 #pragma unroll 1
-    for (int n0 = sub; n0 < all + sub; n0 += kAtOnce * kMany) {
-      uint4 v[kMany];
+    for (int n = sub; n < all && sub < kAtOnce; n += kAtOnce) {
+      const int from = sb.q_from[n];
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                       smem_u32(tile + n * 128 + (((piece & 7) ^ (n & 7)) << 4))),
+                   "l"(Q + (size_t)max(from, 0) * (D * 2)), "r"(from < 0 ? 0 : 16)
+                   : "memory");
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (!p.fp16) {
+#pragma unroll 1
+      for (int n = sub; n < all + sub; n += kAtOnce) {
+        const bool on = sub < kAtOnce && n < all;
+        uint4* const at = reinterpret_cast<uint4*>(tile + min(n, all - 1) * 128 + (((piece & 7) ^ (n & 7)) << 4));
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (on) v = *at;
+        // The row's largest size has exponent field E; times 2^(141 - E) it lies in [2^14, 2^15).
+        uint32_t top = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+        top = max(top & 0xFFFFu, top >> 16);
+        if constexpr (kPieces == 12) {
+          // 12 lanes: those of the other row keep their own maximum.
+          const uint32_t mine = __reduce_max_sync(0xffffffffu, sub == 0 ? top : 0u);
+          const uint32_t other = __reduce_max_sync(0xffffffffu, sub == 1 ? top : 0u);
+          top = sub == 0 ? mine : other;
+        } else {
 #pragma unroll
-      for (int k = 0; k < kMany; ++k) {
-        const int n = n0 + kAtOnce * k;
-        v[k] = make_uint4(0, 0, 0, 0);
-        if (sub < kAtOnce && n < seg.rows && sb.lim[buf][n] > 0)
-          v[k] = __ldg(reinterpret_cast<const uint4*>(Q + n * row_bytes + (seg.kind == kQaOwn ? 0 : n / p.rows) * next_req));
-      }
-#pragma unroll
-      for (int k = 0; k < kMany; ++k) {
-        const int n = n0 + kAtOnce * k;
-        if (!p.fp16) {
-          // The row's largest size has exponent field E; times 2^(141 - E) it lies in [2^14, 2^15).
-          uint32_t top = __vmaxu2(__vmaxu2(v[k].x & 0x7FFF7FFFu, v[k].y & 0x7FFF7FFFu),
-                                  __vmaxu2(v[k].z & 0x7FFF7FFFu, v[k].w & 0x7FFF7FFFu));
-          top = max(top & 0xFFFFu, top >> 16);
-          if constexpr (kPieces == 12) {
-            // 12 lanes: those of the other row keep their own maximum.
-            const uint32_t mine = __reduce_max_sync(0xffffffffu, sub == 0 ? top : 0u);
-            const uint32_t other = __reduce_max_sync(0xffffffffu, sub == 1 ? top : 0u);
-            top = sub == 0 ? mine : other;
-          } else {
-#pragma unroll
-            for (int x = 1; x < kPieces; x <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, x));
-          }
-          const int shift = top == 0 ? 0 : min(141 - (int)(top >> 7), 126);
-          const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
-          uint32_t* w = reinterpret_cast<uint32_t*>(&v[k]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            w[j] = qa_pack_half(__uint_as_float(w[j] << 16) * up, __uint_as_float(w[j] & 0xFFFF0000u) * up);
-          if (piece == 0 && sub < kAtOnce && n < all)
-            sb.q_scale[buf][n] = fmaxf(p.scale_log2 * __uint_as_float((uint32_t)(127 - shift) << 23), FLT_MIN);
-        } else if (piece == 0 && sub < kAtOnce && n < all) {
-          sb.q_scale[buf][n] = fmaxf(p.scale_log2, FLT_MIN);
+          for (int x = 1; x < kPieces; x <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, x));
         }
-        if (sub < kAtOnce && n < all)
-          *reinterpret_cast<uint4*>(tile + n * 128 + (((piece & 7) ^ (n & 7)) << 4)) = v[k];
+        const int shift = top == 0 ? 0 : min(141 - (int)(top >> 7), 126);
+        const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
+        uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          w[j] = qa_pack_half(__uint_as_float(w[j] << 16) * up, __uint_as_float(w[j] & 0xFFFF0000u) * up);
+        if (on) {
+          *at = v;
+          if (piece == 0)
+            sb.q_scale[buf][n] = fmaxf(p.scale_log2 * __uint_as_float((uint32_t)(127 - shift) << 23), FLT_MIN);
+        }
       }
     }
     fence_proxy_async_smem();
@@ -605,7 +626,7 @@ __device__ void qa_products_s(const QaParams& p, uint8_t* q_tiles, QA_SHARED& sb
   const uint64_t desc = smem_desc_sw128(0, 16, 1024);
   const uint32_t hi = (uint32_t)(desc >> 32), q_lo = (uint32_t)desc + (smem_u32(q_tiles) >> 4);
   QaRing<C::kKeyBuffers> kb;
-  QaRing<kQaDepth> r;
+  QaRing<C::kDepth> r;
   int seg = -1;
 #pragma unroll 1
   for (int t = 0;; ++t, r.next()) {
@@ -613,7 +634,7 @@ __device__ void qa_products_s(const QaParams& p, uint8_t* q_tiles, QA_SHARED& sb
     const int info = __shfl_sync(0xffffffffu, sb.sched[t % kQaSched][0].x, 0);
     const int b = r.at;
     // (The end too waits for the softmax to have seen the step that had this buffer.)
-    if (t >= kQaDepth && !qa_wait(&sb.s_free[b], r.phase ^ 1, wt)) break;
+    if (t >= C::kDepth && !qa_wait(&sb.s_free[b], r.phase ^ 1, wt)) break;
     if (info & kQaEnd) {
       if (elect_one()) {
         mbar_arrive(&sb.s_full[b]);
@@ -648,7 +669,7 @@ __device__ void qa_products_s(const QaParams& p, uint8_t* q_tiles, QA_SHARED& sb
     }
     // The softmax also learns here what this warp knows: the schedule, the
     // queries, and that P's buffer has been read (a wait less on its own way).
-    if (!ok || (t >= kQaDepth && !qa_wait(&sb.pv_done[b], r.phase ^ 1, wt))) break;
+    if (!ok || (t >= C::kDepth && !qa_wait(&sb.pv_done[b], r.phase ^ 1, wt))) break;
     if (elect_one()) mbar_arrive(&sb.s_full[b]);
     __syncwarp();
   }
@@ -661,7 +682,8 @@ __device__ void qa_products_pv(const QaParams& p, uint8_t* p_tiles, QA_SHARED& s
   const uint64_t desc = smem_desc_sw128(0, 16, 1024);
   const uint32_t hi = (uint32_t)(desc >> 32), p_lo = (uint32_t)desc + (smem_u32(p_tiles) >> 4);
   QaRing<C::kValueBuffers> vb;
-  QaRing<kQaDepth> r;
+  QaRing<C::kDepth> r;
+  int seg = -1;
 #pragma unroll 1
   for (int t = 0;; ++t, r.next()) {
     if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) break;
@@ -669,7 +691,11 @@ __device__ void qa_products_pv(const QaParams& p, uint8_t* p_tiles, QA_SHARED& s
     if (info & kQaEnd) break;
     const int b = r.at;
     if (!qa_wait(&sb.p_ready[b], r.phase, wt)) break;
-    const uint32_t idesc = qa_idesc(info);
+    if (info & kQaFirst) {
+      ++seg;
+      if (const int old = seg - C::kOuts; old >= 0 && !qa_wait(&sb.o_free[old & 1], (old >> 1) & 1, wt)) break;
+    }
+    const uint32_t idesc = qa_idesc(info), o_at = C::kTmemO + seg % C::kOuts * NMAX;
     bool ok = true;
 #pragma unroll 1
     for (int h = 0; 128 * h < qa_keys_of(info); ++h) {
@@ -680,10 +706,13 @@ __device__ void qa_products_pv(const QaParams& p, uint8_t* p_tiles, QA_SHARED& s
       if (elect_one()) {
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk)
-          umma_ts_split(C::kTmemO, v_at + 8 * kk, p0 + (((kk >> 2) * C::kBoxBytes + (kk & 3) * 32) >> 4), hi, idesc,
+          umma_ts_split(o_at, v_at + 8 * kk, p0 + (((kk >> 2) * C::kBoxBytes + (kk & 3) * 32) >> 4), hi, idesc,
                         kk > 0 ? 1 : more);
         umma_commit(&sb.v_free[vb.at]);
-        if (128 * (h + 1) >= qa_keys_of(info)) umma_commit(&sb.pv_done[b]);
+        if (128 * (h + 1) >= qa_keys_of(info)) {
+          umma_commit(&sb.pv_done[b]);
+          if (info & kQaLast) umma_commit(&sb.o_full[seg & 1]);
+        }
       }
       __syncwarp();
       vb.next();
@@ -926,152 +955,155 @@ struct QaGroup {
 // steps is short: with all of it in one loop the four warps spent more time on
 // fetching instructions than on anything else (2900 clk a step of 256 keys).
 
-// The end of a segment, the step before t: O, or a partial result.
-template <int D, int NMAX, uint32_t TMEM_O, class Shared>
-__device__ __noinline__ bool qa_segment_end(const QaParams& p, Shared& sb, const QaWait& wt, int t, int which,
-                                            bool faulty) {
-  const QaGroup<NMAX> q;
-  const int u = t - 1;
-  if (!qa_wait(&sb.pv_done[u % kQaDepth], (u / kQaDepth) & 1, wt)) return false;
-  tc_fence_after_sync();
-  const int4 e0 = sb.sched[u % kQaSched][0], e1 = sb.sched[u % kQaSched][1];
-  const int kind = qa_kind(e0.x), end = q.row0() + q.rows(qa_rows(e0.x));
-  const bool direct = e0.z < 0;
-  const int slot_rows = kind == kQaPrefix ? kQaRows : min(p.rows, kQaRows);
-  // A lane has the sum and the reference of one row; then four rows at a time.
-  const int mine = min(q.row0() + q.lane, kQaRows - 1);
-  const float l = sb.sums[4 * q.i][mine] + sb.sums[4 * q.i + 1][mine] + sb.sums[4 * q.i + 2][mine] + sb.sums[4 * q.i + 3][mine];
-  const float top = sb.top[which][mine];
-  if (!direct && q.w == 0 && q.row0() + q.lane < end)
-    p.work.ml[kind][(size_t)e0.z * slot_rows + mine] = faulty ? make_float2(0.0f, NAN) : make_float2(top, l);
-  const float inv = l > 0.0f && !faulty && top > -INFINITY ? 1.0f / l : 0.0f;
-  if (32 * q.w < D) {
-    const int d = 32 * q.w + q.lane;
-    float* part = p.work.O[kind] + ((size_t)(direct ? 0 : e0.z) * slot_rows + q.row0()) * D + d;
-    uint16_t* out = reinterpret_cast<uint16_t*>(p.O) +
-                    (((size_t)e0.w * p.cache.n_kv_heads + e1.x) * p.rows + e1.y + q.row0()) * D + d;
+// Four warps that write O, or a partial result, of each segment that has ended.
+template <int D, int BITS, int NMAX>
+__device__ void qa_results(const QaParams& p, QA_SHARED& sb, const QaWait& wt) {
+  using C = QaCfg<D, BITS, NMAX>;
+  const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) & 3, d = 32 * w + lane;
 #pragma unroll 1
-    for (int n0 = 0; n0 < end - q.row0(); n0 += 4, part += 4 * D, out += 4 * D) {
-      uint32_t v[4];
-      asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
-                   : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                   : "r"(q.lanes() + TMEM_O + q.row0() + n0));
-      asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]) : : "memory");
-      const int left = end - q.row0() - n0;
-      if (!direct) {
+  for (int seg = 0;; ++seg) {
+    const int buf = seg & 1;
+    if (!qa_wait(&sb.end_ready[buf], (seg >> 1) & 1, wt)) return;
+    const int4 e0 = sb.last[buf][0], e1 = sb.last[buf][1];
+    if (e0.x & kQaEnd) return;
+    const int rows = qa_rows(e0.x), kind = qa_kind(e0.x);
+    const bool direct = e0.z < 0, faulty = e0.x & kQaFaulty;
+    const int slot_rows = kind == kQaPrefix ? kQaRows : min(p.rows, kQaRows);
+    // A lane has the sums and references of rows `lane` and 32 + lane.
+    float inv[(NMAX + 31) / 32];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (k < left) part[k * D] = __uint_as_float(v[k]);
-      } else {
+    for (int k = 0; 32 * k < NMAX; ++k) {
+      const int n = min(32 * k + lane, NMAX - 1);
+      const float(*from)[kQaRows] = sb.sums[buf];
+      const float l = from[0][n] + from[1][n] + from[2][n] + from[3][n], top = sb.top[buf][n];
+      if (!direct && w == 0 && 32 * k + lane < rows)
+        p.work.ml[kind][(size_t)e0.z * slot_rows + n] = faulty ? make_float2(0.0f, NAN) : make_float2(top, l);
+      inv[k] = l > 0.0f && !faulty && top > -INFINITY ? 1.0f / l : 0.0f;
+    }
+    if (!qa_wait(&sb.o_full[buf], (seg >> 1) & 1, wt)) return;
+    tc_fence_after_sync();
+    if (32 * w < D) {
+      float* part = p.work.O[kind] + (size_t)(direct ? 0 : e0.z) * slot_rows * D + d;
+      uint16_t* out = reinterpret_cast<uint16_t*>(p.O) +
+                      (((size_t)e0.w * p.cache.n_kv_heads + e1.x) * p.rows + e1.y) * D + d;
+#pragma unroll 1
+      for (int n0 = 0; n0 < rows; n0 += 4, part += 4 * D, out += 4 * D) {
+        uint32_t v[4];
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                     : "r"(((uint32_t)(32 * w) << 16) + C::kTmemO + seg % C::kOuts * NMAX + n0));
+        asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]) : : "memory");
+        const int left = rows - n0;
+        if (!direct) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float f = __shfl_sync(0xffffffffu, inv, n0 + k);
-          const float x = f == 0.0f ? 0.0f : __uint_as_float(v[k]) * f;
-          const uint32_t both = p.fp16 ? qa_pack_half(x, x) : pack_bf16x2(x, x);
-          if (k < left) out[k * D] = (uint16_t)both;
+          for (int k = 0; k < 4; ++k)
+            if (k < left) part[k * D] = __uint_as_float(v[k]);
+        } else {
+          const float mine = NMAX == 16 || n0 < 32 ? inv[0] : inv[(NMAX + 31) / 32 - 1];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float f = __shfl_sync(0xffffffffu, mine, (n0 + k) & 31);
+            const float x = f == 0.0f ? 0.0f : __uint_as_float(v[k]) * f;
+            const uint32_t both = p.fp16 ? qa_pack_half(x, x) : pack_bf16x2(x, x);
+            if (k < left) out[k * D] = (uint16_t)both;
+          }
         }
       }
     }
+    tc_fence_before_sync();
+    __syncwarp();
+    qa_arrive(&sb.o_free[buf], lane);
   }
-  tc_fence_before_sync();
-  return true;
 }
 
-// Keys of step t that a row does not see get the logit -inf in tensor memory,
-// whatever S is.
-template <int NMAX, int H, uint32_t TMEM_S, class Shared>
-__device__ __noinline__ void qa_mask(Shared& sb, int t, int seg, int rows) {
+// The largest entry of S of each row among this warp's keys, for new references;
+// with `mask`, keys that a row does not see get the logit -inf in tensor memory
+// first, whatever S is.
+template <int NMAX, int H, class Shared>
+__device__ __noinline__ void qa_look(Shared& sb, uint32_t s_at, int pos, int seg, int rows, bool mask, bool top) {
   const QaGroup<NMAX> q;
-  const int row0 = q.row0(), row_end = row0 + q.rows(rows);
-  const int key0 = sb.sched[t % kQaSched][0].y + 32 * q.w + q.lane / 4;
+  const int row0 = q.row0(), row_end = row0 + q.rows(rows), lane = q.lane;
+  const int key0 = pos + 32 * q.w + lane / 4;
 #pragma unroll 1
   for (int n0 = row0; n0 < row_end; n0 += 8) {
-    const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][n0 + 2 * (q.lane & 3)]);
+    const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][n0 + 2 * (lane & 3)]);
+    float m0 = -INFINITY, m1 = -INFINITY;
+    uint32_t at = q.lanes() + s_at + n0;
 #pragma unroll 1
-    for (int h = 0; h < 2 * H; ++h) {
-      const uint32_t at = q.lanes() + ((uint32_t)(16 * (h & 1)) << 16) + TMEM_S + (t % kQaDepth * H + (h >> 1)) * NMAX + n0;
-      const int key = key0 + 128 * (h >> 1) + 16 * (h & 1);
-      uint32_t r[1][1][4];
-      qa_load_8(at, r[0][0]);
-      qa_load_wait(r);
-      uint32_t* x = r[0][0];
-      if (key >= lim.x) x[0] = 0xFF800000u;
-      if (key >= lim.y) x[1] = 0xFF800000u;
-      if (key + 8 >= lim.x) x[2] = 0xFF800000u;
-      if (key + 8 >= lim.y) x[3] = 0xFF800000u;
-      asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(x[0]), "r"(x[1]), "r"(x[2]),
-                   "r"(x[3])
-                   : "memory");
+    for (int key = key0; key < key0 + 128 * H; key += 128, at += NMAX) {
+#pragma unroll 1
+      for (int k = 0; k < 32; k += 16) {
+        uint32_t r[1][1][4];
+        qa_load_8(at + ((uint32_t)k << 16), r[0][0]);
+        qa_load_wait(r);
+        uint32_t* x = r[0][0];
+        if (mask) {
+          if (key + k >= lim.x) x[0] = 0xFF800000u;
+          if (key + k >= lim.y) x[1] = 0xFF800000u;
+          if (key + k + 8 >= lim.x) x[2] = 0xFF800000u;
+          if (key + k + 8 >= lim.y) x[3] = 0xFF800000u;
+          asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + ((uint32_t)k << 16)),
+                       "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3])
+                       : "memory");
+        }
+        m0 = fmax3(m0, __uint_as_float(x[0]), __uint_as_float(x[2]));
+        m1 = fmax3(m1, __uint_as_float(x[1]), __uint_as_float(x[3]));
+      }
     }
+    if (!top) continue;
+#pragma unroll
+    for (int x = 4; x < 32; x <<= 1) {
+      m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, x));
+      m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, x));
+    }
+    if (lane < 4) *reinterpret_cast<float2*>(&sb.warp_max[seg & 1][q.w][n0 + 2 * lane]) = make_float2(m0, m1);
   }
   tmem_st_wait();
 }
 
-// New references of step t's rows (at the start of a segment, or where a
-// numerator passed 2^15), the end of the segment before, or of everything.
-// All four warps of a group; `ok`: this warp's waits have not run out.
-// `sums`: this thread's entries of its group's rows, as the step before left
-// them.  Returns 0: that is all, 1: go on, 2: a wait has run out, which the next
-// vote will tell.
-template <int D, int NMAX, int H, uint32_t TMEM_S, uint32_t TMEM_O, class Shared>
-__device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait& wt, int t, int seg, bool ok,
-                                    bool faulty, float2* sums) {
+// The reference of row n, from the largest entries of S that the warps have found.
+template <class Shared>
+__device__ __forceinline__ float qa_shift(const Shared& sb, int seg, int n) {
+  const float(*m)[kQaRows] = sb.warp_max[seg & 1];
+  return 7.0f - fmaxf(fmaxf(m[0][n], m[1][n]), fmaxf(m[2][n], m[3][n])) * sb.q_scale[seg & 1][n];
+}
+
+// The references at the start of a segment, once the vote has exchanged the
+// maxima.  Each warp writes them all, the same, and so needs no barrier.
+template <int NMAX, class Shared>
+__device__ __noinline__ bool qa_first(Shared& sb, const QaWait& wt, int seg, int rows, float2* sums) {
   const QaGroup<NMAX> q;
-  const int lane = q.lane, b = t % kQaDepth;
-  const int2 e = ok ? *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]) : make_int2(kQaEnd, 0);
-  const int row0 = q.row0(), row_end = row0 + q.rows(qa_rows(e.x));
-  const bool end = e.x & kQaEnd, first = e.x & kQaFirst;
-  if (ok && t > 0 && (first || end)) {  // the sums of the segment that ended
-    const int before = row0 + q.rows(qa_rows(sb.sched[(t - 1) % kQaSched][0].x));
-#pragma unroll 1
-    for (int n0 = row0; n0 < before; n0 += 8) {
-      float2 l = sums[(n0 - row0) * 16];
-#pragma unroll
-      for (int x = 4; x < 32; x <<= 1) {
-        l.x += __shfl_xor_sync(0xffffffffu, l.x, x);
-        l.y += __shfl_xor_sync(0xffffffffu, l.y, x);
-      }
-      if (lane < 4) *reinterpret_cast<float2*>(&sb.sums[4 * q.i + q.w][n0 + 2 * lane]) = l;
-    }
+  const int own = q.rows(rows), n = q.row0() + q.lane;
+  if (seg >= 2 && !qa_wait(&sb.o_free[seg & 1], ((seg >> 1) - 1) & 1, wt)) return false;
+  if (q.lane < q.kRows) {
+    float moved = INFINITY;
+    if (q.lane < own && sb.lim[seg & 1][n] > 0) moved = qa_shift(sb, seg, n);  // rows that see nothing have queries of 0
+    sb.top[seg & 1][n] = -moved;
+    sb.shift[seg & 1][n] = moved == INFINITY ? 0.0f : moved;
   }
-  if (ok && !end) {
-    // The largest entry of S of each row among this warp's keys.
 #pragma unroll 1
-    for (int n0 = row0; n0 < row_end; n0 += 8) {
-      uint32_t r[2 * H][1][4];
-#pragma unroll
-      for (int h = 0; h < 2 * H; ++h)
-        qa_load_8(q.lanes() + ((uint32_t)(16 * (h & 1)) << 16) + TMEM_S + (b * H + (h >> 1)) * NMAX + n0, r[h][0]);
-      qa_load_wait(r);
-      float m0 = -INFINITY, m1 = -INFINITY;
-#pragma unroll
-      for (int h = 0; h < 2 * H; ++h) {
-        m0 = fmax3(m0, __uint_as_float(r[h][0][0]), __uint_as_float(r[h][0][2]));
-        m1 = fmax3(m1, __uint_as_float(r[h][0][1]), __uint_as_float(r[h][0][3]));
-      }
-#pragma unroll
-      for (int x = 4; x < 32; x <<= 1) {
-        m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, x));
-        m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, x));
-      }
-      if (lane < 4) *reinterpret_cast<float2*>(&sb.warp_max[4 * q.i + q.w][n0 + 2 * lane]) = make_float2(m0, m1);
-    }
-    tc_fence_before_sync();
-  }
-  if (lane == 0) sb.warp_ok[4 * q.i + q.w] = ok;
+  for (int n0 = 0; n0 < own; n0 += 8) sums[n0 * 16] = make_float2(0.0f, 0.0f);
+  __syncwarp();
+  return true;
+}
+
+// New references of step t's rows where a numerator passed 2^15.  All four warps
+// of a group.  `sums`: this thread's entries of its group's rows, as the step
+// before left them.  Returns false when a wait has run out, which the next vote
+// will tell.
+template <int D, int NMAX, int H, int DEPTH, class Shared>
+__device__ __noinline__ bool qa_turn(Shared& sb, const QaWait& wt, uint32_t s_at, uint32_t o_at, int t, int seg, int rows,
+                                     float2* sums) {
+  const QaGroup<NMAX> q;
+  const int row0 = q.row0(), row_end = row0 + q.rows(rows);
+  qa_look<NMAX, H>(sb, s_at, 0, seg, rows, false, true);
   q.sync();
-  const int from = 4 * q.i;
-  if (!(sb.warp_ok[from] && sb.warp_ok[from + 1] && sb.warp_ok[from + 2] && sb.warp_ok[from + 3])) return 0;
-  if (t > 0 && (first || end)) ok = qa_segment_end<D, NMAX, TMEM_O>(p, sb, wt, t, (seg ^ first) & 1, faulty);
-  if (end) return 0;
   const int n = row0 + threadIdx.x % 128;
-  if (n < row0 + q.kRows) {
+  if (n < row_end) {
     float moved = INFINITY, f = 1.0f;
-    if (n < row_end && sb.lim[seg & 1][n] > 0) {  // rows that see nothing anywhere have queries of 0
-      const float m = fmaxf(fmaxf(sb.warp_max[from][n], sb.warp_max[from + 1][n]),
-                            fmaxf(sb.warp_max[from + 2][n], sb.warp_max[from + 3][n]));
-      const float old = first ? INFINITY : -sb.top[seg & 1][n];
-      moved = fminf(old, 7.0f - m * sb.q_scale[seg & 1][n]);
+    if (sb.lim[seg & 1][n] > 0) {
+      const float old = -sb.top[seg & 1][n];
+      moved = fminf(old, qa_shift(sb, seg, n));
       if (moved != INFINITY) f = ex2_approx(moved - old);
     }
     sb.top[seg & 1][n] = -moved;
@@ -1082,31 +1114,58 @@ __device__ __noinline__ int qa_turn(const QaParams& p, Shared& sb, const QaWait&
 #pragma unroll 1
   for (int n0 = row0; n0 < row_end; n0 += 8) {
     float2* l = sums + (n0 - row0) * 16;
-    const float2 f = *reinterpret_cast<const float2*>(&sb.factor[n0 + 2 * (lane & 3)]);
-    *l = first ? make_float2(0.0f, 0.0f) : make_float2(l->x * f.x, l->y * f.y);
+    const float2 f = *reinterpret_cast<const float2*>(&sb.factor[n0 + 2 * (q.lane & 3)]);
+    *l = make_float2(l->x * f.x, l->y * f.y);
   }
-  if (!first && ok) {  // O in units of the new references
-    const int u = t - 1;
-    if ((ok = qa_wait(&sb.pv_done[u % kQaDepth], (u / kQaDepth) & 1, wt)) && 32 * q.w < D) {
-      tc_fence_after_sync();
+  // O in units of the new references.
+  const int u = t - 1;
+  if (!qa_wait(&sb.pv_done[u % DEPTH], (u / DEPTH) & 1, wt)) return false;
+  if (32 * q.w < D) {
+    tc_fence_after_sync();
+    const uint32_t at = q.lanes() + o_at;
 #pragma unroll 1
-      for (int n0 = row0; n0 < row_end; n0 += 4) {
-        uint32_t v[4];
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
-                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                     : "r"(q.lanes() + TMEM_O + n0));
-        asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]) : : "memory");
-        const float4 f = *reinterpret_cast<const float4*>(&sb.factor[n0]);
-        asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(q.lanes() + TMEM_O + n0),
-                     "r"(__float_as_uint(__uint_as_float(v[0]) * f.x)), "r"(__float_as_uint(__uint_as_float(v[1]) * f.y)),
-                     "r"(__float_as_uint(__uint_as_float(v[2]) * f.z)), "r"(__float_as_uint(__uint_as_float(v[3]) * f.w))
-                     : "memory");
-      }
-      tmem_st_wait();
+    for (int n0 = row0; n0 < row_end; n0 += 4) {
+      uint32_t v[4];
+      asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];"
+                   : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                   : "r"(at + n0));
+      asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]) : : "memory");
+      const float4 f = *reinterpret_cast<const float4*>(&sb.factor[n0]);
+      asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + n0),
+                   "r"(__float_as_uint(__uint_as_float(v[0]) * f.x)), "r"(__float_as_uint(__uint_as_float(v[1]) * f.y)),
+                   "r"(__float_as_uint(__uint_as_float(v[2]) * f.z)), "r"(__float_as_uint(__uint_as_float(v[3]) * f.w))
+                   : "memory");
     }
-    tc_fence_before_sync();
+    tmem_st_wait();
   }
-  return ok ? 1 : 2;
+  tc_fence_before_sync();
+  return true;
+}
+
+// After the last step of a segment: what its results need besides O.  `sums` as
+// that step left them.
+template <int NMAX, class Shared>
+__device__ __noinline__ void qa_last(Shared& sb, int t, int seg, bool faulty, const float2* sums) {
+  const QaGroup<NMAX> q;
+  const int buf = seg & 1;
+  const int4 e0 = sb.sched[t % kQaSched][0];
+  const int row0 = q.row0(), row_end = row0 + q.rows(qa_rows(e0.x));
+#pragma unroll 1
+  for (int n0 = row0; n0 < row_end; n0 += 8) {
+    float2 l = sums[(n0 - row0) * 16];
+#pragma unroll
+    for (int x = 4; x < 32; x <<= 1) {
+      l.x += __shfl_xor_sync(0xffffffffu, l.x, x);
+      l.y += __shfl_xor_sync(0xffffffffu, l.y, x);
+    }
+    if (q.lane < 4) *reinterpret_cast<float2*>(&sb.sums[buf][q.w][n0 + 2 * q.lane]) = l;
+  }
+  if (threadIdx.x == 0) {
+    sb.last[buf][0] = make_int4(faulty ? e0.x | kQaFaulty : e0.x, e0.y, e0.z, e0.w);
+    sb.last[buf][1] = sb.sched[t % kQaSched][1];
+  }
+  __syncwarp();
+  qa_arrive(&sb.end_ready[buf], q.lane);
 }
 
 template <int D, int BITS, int NMAX>
@@ -1126,7 +1185,7 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
   constexpr int kSumsStep = NMAX / 8 * 128;
   int seg = -1;
   bool ok = true, faulty = false;
-  QaRing<kQaDepth> r3;
+  QaRing<C::kDepth> r3;
   // Once a wait of a warp has run out, the next vote ends all; every step has one.
 #pragma unroll 1
   for (int t = 0;; ++t, r3.next()) {
@@ -1134,11 +1193,16 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
     ok = ok && qa_wait(&sb.s_full[b], r3.phase, wt);
     const int2 e = *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]);
     const int info = ok ? e.x : kQaEnd, rows = q.rows(qa_rows(info));
+    const bool first = info & kQaFirst;
     bool turn = info & (kQaFirst | kQaEnd), turned = false;
-    if (info & kQaFirst) ++seg;
+    if (first) ++seg;
     tc_fence_after_sync();
-    if (!(info & kQaEnd) && e.y + 128 * H > sb.min_lim[seg & 1])
-      qa_mask<NMAX, H, C::kTmemS>(sb, t, seg, qa_rows(info));
+    if (!(info & kQaEnd)) {
+      const bool mask = e.y + 128 * H > sb.min_lim[seg & 1];
+      if (mask || first) qa_look<NMAX, H>(sb, C::kTmemS + b * H * NMAX, e.y, seg, qa_rows(info), mask, first);
+    } else if (!ok && lane == 0) {
+      sb.failed[q.i] = 1;
+    }
 #pragma unroll 1
     for (;;) {
       if (!turn) {
@@ -1196,10 +1260,22 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
         turn = top > 15.0f;
       }
       if (!q.vote(turn)) break;
-      const int next = qa_turn<D, NMAX, H, C::kTmemS, C::kTmemO>(p, sb, wt, t, seg, ok, faulty, sums + (odd ^ 1) * kSumsStep);
-      if (next == 0) return;
-      ok = next == 1;
-      if (info & kQaFirst) faulty = false;
+      // (A failed warp votes for a turn, and so do all at the start and the end of a segment.)
+      if (*reinterpret_cast<volatile int*>(&sb.failed[q.i])) return;
+      if (info & kQaEnd) {
+        if (seg >= 1 && !qa_wait(&sb.o_free[(seg + 1) & 1], ((seg - 1) >> 1) & 1, wt)) return;
+        if (q.w == 0 && q.i == 0 && lane == 0) sb.last[(seg + 1) & 1][0] = make_int4(kQaEnd, 0, 0, 0);
+        __syncwarp();
+        qa_arrive(&sb.end_ready[(seg + 1) & 1], lane);
+        return;
+      }
+      float2* const from = sums + (odd ^ 1) * kSumsStep;
+      if (first)
+        ok = qa_first<NMAX>(sb, wt, seg, qa_rows(info), from);
+      else
+        ok = qa_turn<D, NMAX, H, C::kDepth>(sb, wt, C::kTmemS + b * H * NMAX, C::kTmemO + seg % C::kOuts * NMAX, t, seg,
+                                            qa_rows(info), from);
+      if (first) faulty = false;
       turn = false;
       turned = true;
     }
@@ -1209,7 +1285,10 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
     __syncwarp();
     qa_arrive(&sb.s_free[b], lane);
     qa_arrive(&sb.p_ready[b], lane);
-    if (info & kQaLast) qa_arrive(&sb.q_free[seg & 1], lane);  // the limits have been read
+    if (info & kQaLast) {
+      qa_arrive(&sb.q_free[seg & 1], lane);  // the limits have been read
+      if (ok) qa_last<NMAX>(sb, t, seg, faulty, sums + odd * kSumsStep);
+    }
   }
 }
 
@@ -1257,11 +1336,15 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
   constexpr int kOther = C::kThreads / 32 - 4;
   if (threadIdx.x == 0) {
     sb.abort = 0;
+    for (int i = 0; i < C::kGroups; ++i) sb.failed[i] = 0;
     for (int i = 0; i < C::kStages; ++i) {
       mbar_init(&sb.full[i], 1);
       mbar_init(&sb.empty[i], 8);
     }
-    for (int i = 0; i < kQaSched; ++i) mbar_init(&sb.sched_full[i], 1);
+    for (int i = 0; i < kQaSched; ++i) {
+      mbar_init(&sb.sched_full[i], 1);
+      mbar_init(&sb.seg_full[i], 1);
+    }
     for (int i = 0; i < C::kKeyBuffers; ++i) {
       mbar_init(&sb.k_ready[i], 4);
       mbar_init(&sb.k_free[i], 1);
@@ -1270,13 +1353,16 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
       mbar_init(&sb.v_ready[i], 4);
       mbar_init(&sb.v_free[i], 1);
     }
-    for (int i = 0; i < kQaDepth; ++i) {
+    for (int i = 0; i < C::kDepth; ++i) {
       mbar_init(&sb.p_ready[i], 4 * C::kGroups);
       mbar_init(&sb.s_full[i], 2);
       mbar_init(&sb.s_free[i], 4 * C::kGroups);
       mbar_init(&sb.pv_done[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
+      mbar_init(&sb.o_full[i], 1);
+      mbar_init(&sb.o_free[i], 4);
+      mbar_init(&sb.end_ready[i], 4 * C::kGroups);
       mbar_init(&sb.q_ready[i], 1);
       mbar_init(&sb.q_free[i], 4 * C::kGroups + 1);
       mbar_init(&sb.done[i], 1);
@@ -1296,14 +1382,16 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
   const QaWait wt = {&sb.abort, p.cache.status, p.wait_ns};
 
   if (warp < 4 * C::kGroups) {
-    qa_softmax<D, BITS, NMAX>(p, p_tiles, reinterpret_cast<float2*>(p_tiles + kQaDepth * C::kPBytes), sb, wt);
+    qa_softmax<D, BITS, NMAX>(p, p_tiles, reinterpret_cast<float2*>(p_tiles + C::kDepth * C::kPBytes), sb, wt);
   } else {
-    if (warp < kOther) {
+    if (warp < kOther - 4) {
       const int k = warp / 4 - C::kGroups;
       if (k < C::kKeyTeams)
         qa_keys<D, BITS, NMAX>(p, k, ring, sb, wt);
       else
         qa_values<D, BITS, NMAX>(p, k - C::kKeyTeams, ring, sb, wt);
+    } else if (warp < kOther) {
+      qa_results<D, BITS, NMAX>(p, sb, wt);
     } else if (warp == kOther) {
       qa_producer<D, BITS, NMAX>(p, plan, ring, sb, wt);
     } else if (warp == kOther + 1) {
