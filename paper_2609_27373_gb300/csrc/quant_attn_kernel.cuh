@@ -1016,41 +1016,38 @@ __device__ void qa_results(const QaParams& p, QA_SHARED& sb, const QaWait& wt) {
   }
 }
 
-// The largest entry of S of each row among this warp's keys, for new references;
-// with `mask`, keys that a row does not see get the logit -inf in tensor memory
-// first, whatever S is.
+// S of keys that a row does not see -> -inf.  `key`: of x[0] and x[1]; x[2] and
+// x[3] are of the key 8 further.
+__device__ __forceinline__ void qa_mask(uint32_t* x, int key, int2 lim) {
+  if (key >= lim.x) x[0] = 0xFF800000u;
+  if (key >= lim.y) x[1] = 0xFF800000u;
+  if (key + 8 >= lim.x) x[2] = 0xFF800000u;
+  if (key + 8 >= lim.y) x[3] = 0xFF800000u;
+}
+
+// The largest entry of S of each row among this warp's keys, for new references.
 template <int NMAX, int H, class Shared>
-__device__ __noinline__ void qa_look(Shared& sb, uint32_t s_at, int pos, int seg, int rows, bool mask, bool top) {
+__device__ __forceinline__ void qa_look(Shared& sb, uint32_t s_at, int pos, int seg, int rows, bool mask) {
   const QaGroup<NMAX> q;
   const int row0 = q.row0(), row_end = row0 + q.rows(rows), lane = q.lane;
-  const int key0 = pos + 32 * q.w + lane / 4;
 #pragma unroll 1
   for (int n0 = row0; n0 < row_end; n0 += 8) {
-    const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][n0 + 2 * (lane & 3)]);
-    float m0 = -INFINITY, m1 = -INFINITY;
-    uint32_t at = q.lanes() + s_at + n0;
-#pragma unroll 1
-    for (int key = key0; key < key0 + 128 * H; key += 128, at += NMAX) {
-#pragma unroll 1
-      for (int k = 0; k < 32; k += 16) {
-        uint32_t r[1][1][4];
-        qa_load_8(at + ((uint32_t)k << 16), r[0][0]);
-        qa_load_wait(r);
-        uint32_t* x = r[0][0];
-        if (mask) {
-          if (key + k >= lim.x) x[0] = 0xFF800000u;
-          if (key + k >= lim.y) x[1] = 0xFF800000u;
-          if (key + k + 8 >= lim.x) x[2] = 0xFF800000u;
-          if (key + k + 8 >= lim.y) x[3] = 0xFF800000u;
-          asm volatile("tcgen05.st.sync.aligned.16x256b.x1.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + ((uint32_t)k << 16)),
-                       "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3])
-                       : "memory");
-        }
-        m0 = fmax3(m0, __uint_as_float(x[0]), __uint_as_float(x[2]));
-        m1 = fmax3(m1, __uint_as_float(x[1]), __uint_as_float(x[3]));
-      }
+    uint32_t r[2 * H][1][4];
+#pragma unroll
+    for (int h = 0; h < 2 * H; ++h)
+      qa_load_8(q.lanes() + ((uint32_t)(16 * (h & 1)) << 16) + s_at + (h >> 1) * NMAX + n0, r[h][0]);
+    qa_load_wait(r);
+    if (mask) {
+      const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][n0 + 2 * (lane & 3)]);
+#pragma unroll
+      for (int h = 0; h < 2 * H; ++h) qa_mask(r[h][0], pos + 32 * q.w + lane / 4 + 128 * (h >> 1) + 16 * (h & 1), lim);
     }
-    if (!top) continue;
+    float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+    for (int h = 0; h < 2 * H; ++h) {
+      m0 = fmax3(m0, __uint_as_float(r[h][0][0]), __uint_as_float(r[h][0][2]));
+      m1 = fmax3(m1, __uint_as_float(r[h][0][1]), __uint_as_float(r[h][0][3]));
+    }
 #pragma unroll
     for (int x = 4; x < 32; x <<= 1) {
       m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, x));
@@ -1058,7 +1055,6 @@ __device__ __noinline__ void qa_look(Shared& sb, uint32_t s_at, int pos, int seg
     }
     if (lane < 4) *reinterpret_cast<float2*>(&sb.warp_max[seg & 1][q.w][n0 + 2 * lane]) = make_float2(m0, m1);
   }
-  tmem_st_wait();
 }
 
 // The reference of row n, from the largest entries of S that the warps have found.
@@ -1071,7 +1067,7 @@ __device__ __forceinline__ float qa_shift(const Shared& sb, int seg, int n) {
 // The references at the start of a segment, once the vote has exchanged the
 // maxima.  Each warp writes them all, the same, and so needs no barrier.
 template <int NMAX, class Shared>
-__device__ __noinline__ bool qa_first(Shared& sb, const QaWait& wt, int seg, int rows, float2* sums) {
+__device__ __forceinline__ bool qa_first(Shared& sb, const QaWait& wt, int seg, int rows, float2* sums) {
   const QaGroup<NMAX> q;
   const int own = q.rows(rows), n = q.row0() + q.lane;
   if (seg >= 2 && !qa_wait(&sb.o_free[seg & 1], ((seg >> 1) - 1) & 1, wt)) return false;
@@ -1092,11 +1088,11 @@ __device__ __noinline__ bool qa_first(Shared& sb, const QaWait& wt, int seg, int
 // before left them.  Returns false when a wait has run out, which the next vote
 // will tell.
 template <int D, int NMAX, int H, int DEPTH, class Shared>
-__device__ __noinline__ bool qa_turn(Shared& sb, const QaWait& wt, uint32_t s_at, uint32_t o_at, int t, int seg, int rows,
-                                     float2* sums) {
+__device__ __noinline__ bool qa_turn(Shared& sb, const QaWait& wt, uint32_t s_at, uint32_t o_at, int t, int pos, int seg, int rows,
+                                     bool mask, float2* sums) {
   const QaGroup<NMAX> q;
   const int row0 = q.row0(), row_end = row0 + q.rows(rows);
-  qa_look<NMAX, H>(sb, s_at, 0, seg, rows, false, true);
+  qa_look<NMAX, H>(sb, s_at, pos, seg, rows, mask);
   q.sync();
   const int n = row0 + threadIdx.x % 128;
   if (n < row_end) {
@@ -1145,7 +1141,7 @@ __device__ __noinline__ bool qa_turn(Shared& sb, const QaWait& wt, uint32_t s_at
 // After the last step of a segment: what its results need besides O.  `sums` as
 // that step left them.
 template <int NMAX, class Shared>
-__device__ __noinline__ void qa_last(Shared& sb, int t, int seg, bool faulty, const float2* sums) {
+__device__ __forceinline__ void qa_last(Shared& sb, int t, int seg, bool faulty, const float2* sums) {
   const QaGroup<NMAX> q;
   const int buf = seg & 1;
   const int4 e0 = sb.sched[t % kQaSched][0];
@@ -1193,16 +1189,15 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
     ok = ok && qa_wait(&sb.s_full[b], r3.phase, wt);
     const int2 e = *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]);
     const int info = ok ? e.x : kQaEnd, rows = q.rows(qa_rows(info));
-    const bool first = info & kQaFirst;
+    const bool first = info & kQaFirst;  // (not where a wait has run out)
     bool turn = info & (kQaFirst | kQaEnd), turned = false;
     if (first) ++seg;
     tc_fence_after_sync();
-    if (!(info & kQaEnd)) {
-      const bool mask = e.y + 128 * H > sb.min_lim[seg & 1];
-      if (mask || first) qa_look<NMAX, H>(sb, C::kTmemS + b * H * NMAX, e.y, seg, qa_rows(info), mask, first);
-    } else if (!ok && lane == 0) {
+    const bool mask = e.y + 128 * H > sb.min_lim[seg & 1];
+    if (first)
+      qa_look<NMAX, H>(sb, C::kTmemS + b * H * NMAX, e.y, seg, qa_rows(info), mask);
+    else if (!ok && lane == 0)
       sb.failed[q.i] = 1;
-    }
 #pragma unroll 1
     for (;;) {
       if (!turn) {
@@ -1231,6 +1226,15 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
             l[k] = from[128 * k];
           }
           qa_load_wait(r);
+          if (__builtin_expect(mask, 0)) {
+#pragma unroll
+            for (int k = 0; k < kAt; ++k) {
+              const int2 lim = *reinterpret_cast<const int2*>(&sb.lim[seg & 1][n + 8 * k]);
+#pragma unroll
+              for (int h = 0; h < 2 * H; ++h)
+                qa_mask(r[h][k], e.y + 32 * q.w + lane / 4 + 128 * (h >> 1) + 16 * (h & 1), lim);
+            }
+          }
 #pragma unroll
           for (int k = 0; k < kAt; ++k) {
             float2 part = make_float2(0.0f, 0.0f);
@@ -1273,8 +1277,8 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
       if (first)
         ok = qa_first<NMAX>(sb, wt, seg, qa_rows(info), from);
       else
-        ok = qa_turn<D, NMAX, H, C::kDepth>(sb, wt, C::kTmemS + b * H * NMAX, C::kTmemO + seg % C::kOuts * NMAX, t, seg,
-                                            qa_rows(info), from);
+        ok = qa_turn<D, NMAX, H, C::kDepth>(sb, wt, C::kTmemS + b * H * NMAX, C::kTmemO + seg % C::kOuts * NMAX, t, e.y,
+                                            seg, qa_rows(info), mask, from);
       if (first) faulty = false;
       turn = false;
       turned = true;
@@ -1390,8 +1394,6 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
         qa_keys<D, BITS, NMAX>(p, k, ring, sb, wt);
       else
         qa_values<D, BITS, NMAX>(p, k - C::kKeyTeams, ring, sb, wt);
-    } else if (warp < kOther) {
-      qa_results<D, BITS, NMAX>(p, sb, wt);
     } else if (warp == kOther) {
       qa_producer<D, BITS, NMAX>(p, plan, ring, sb, wt);
     } else if (warp == kOther + 1) {
@@ -1402,6 +1404,8 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
         qa_sources(p, plan, i, p.work.sources + 2 * (size_t)i);
     } else if (warp == kOther + 2) {
       qa_products_s<D, BITS, NMAX>(p, q_tiles, sb, wt);
+    } else if (warp < kOther) {
+      qa_results<D, BITS, NMAX>(p, sb, wt);
     } else {
       qa_products_pv<D, BITS, NMAX>(p, p_tiles, sb, wt);
     }
