@@ -84,13 +84,18 @@ constexpr int kQaSched = 16;
 constexpr int kQaFirst = 1, kQaLast = 2, kQaEnd = 4, kQaFaulty = 8;
 constexpr int kQaOwn = 0, kQaPrefix = 1;
 
-// Schedule entry of a step, two int4: {flags | rows << 8 | kind << 16 | keys <<
-// 20, position of the first key, workspace slot or -1 (O itself), request}, {kv
-// head, first row of the request, 0, 0}.  The K and V warps go by halves and
-// need no more than half_keys, which comes with the stage.  Entry t % 16 is written again for step
-// t + 16 when the V warps have given back a stage at most 8 halves before that
-// step; they had to wait for the P V product of a half 3 before that one at
-// most, and with it for the softmax and the products to be past step t + 4.
+// Segment entry, two int4: {rows | kind << 8 (0: the end), position of the first
+// key, of the last one + 1, request}, {kv head, first row of the request,
+// workspace slot or -1 (O itself), cache row}, and its first 32 pages, one a lane.
+// Entry k % 16 is written again for segment k + 16, after the queries of segment
+// k + 14 have found a buffer and so after segment k's results.
+//
+// Schedule entry of a step: {flags | rows << 8 | kind << 16 | keys << 20, position
+// of the first key}.  The K and V warps go by halves and need no more than
+// half_keys, which comes with the stage.  Entry t % 16 is written again for step
+// t + 16, whose first stage (of at most 8) the V warps have given back: they are
+// at most 4 halves ahead of the products of P, and so of the softmax, which is
+// past step t then.
 __device__ __forceinline__ int qa_rows(int info) { return (info >> 8) & 255; }
 __device__ __forceinline__ int qa_kind(int info) { return (info >> 16) & 1; }
 __device__ __forceinline__ int qa_keys_of(int info) { return info >> 20; }
@@ -108,7 +113,9 @@ struct QaShared {
   uint64_t end_ready[2];             // softmax warps: what ends a segment is written
   uint64_t q_ready[2], q_free[2];  // q_free: the products and the softmax warps
   uint64_t done[2];
-  int4 sched[kQaSched][2], segs[kQaSched][2];
+  int2 sched[kQaSched];
+  int4 segs[kQaSched][2];
+  int pages[kQaSched][32];
   alignas(16) int lim[2][kQaRows];  // keys that a row sees, 0 for none
   int min_lim[2];            // the least of those that see any
   int q_from[kQaRows];       // where a row comes from, -1 for a row of 0
@@ -117,8 +124,8 @@ struct QaShared {
   alignas(16) float shift[2][kQaRows];  // added to a row's logits: 7 minus the reference, 0 where nothing is seen
   alignas(16) float top[2][kQaRows];    // the reference less 7, -inf where nothing is seen
   alignas(16) float factor[kQaRows];    // of O and the sums where the references have moved
-  // Of a segment that ends: its last step's entry and its rows' sums by warp.
-  int4 last[2][2];
+  // Of a segment that ends: its flags and its rows' sums by warp.
+  int last[2];
   alignas(16) float sums[2][4][kQaRows];
   alignas(16) int4 value_scales[4 * NT][32];  // a warp's two groups x 128 tokens as fp16
   int half_keys[NS];  // keys of the half in a stage, 0 at the end
@@ -254,62 +261,24 @@ __device__ __forceinline__ int qa_find(const int* base, int n, int x) {
 }
 
 struct QaSeg {
-  int kind, req, nreq, kvh;
+  int kind, req, kvh;
   int row0, rows;  // first row of the request (own), rows
-  int slot;        // of the workspace, -1: O itself
-  int seq;         // cache slot whose pages are read
-  int pos, end;    // position of the next tile's first key; one past the item's keys
-  int left;        // tiles left
+  int seq, pos, end;  // cache row, positions of the first key and of the last one + 1
+  int slot;        // workspace slot, -1 for O itself
+  int left;        // tiles
 };
-
-__device__ __forceinline__ QaSeg qa_segment(const QaParams& p, const QaPlan& plan, int kind, int x, int x_end, int run) {
-  QaSeg s;
-  const int kv = p.cache.n_kv_heads;
-  int tiles, t;
-  s.kind = kind;
-  s.row0 = 0;
-  if (kind == kQaPrefix) {
-    const int g = qa_find(plan.base, p.n_groups, x);
-    tiles = plan.tiles[g];
-    const int y = x - plan.base[g], it = y / tiles, n = plan.row_tiles[g];
-    t = y - it * tiles;
-    // kv head outermost: the items of one kv head read the same keys at about the same time.
-    s.kvh = it / n;
-    const int tile = it - s.kvh * n;
-    s.req = plan.start[g] + tile * p.per_tile;
-    s.nreq = min(p.per_tile, plan.start[g + 1] - s.req);
-    s.rows = s.nreq * p.rows;
-    s.slot = plan.item[g] * kv + it + run;
-    const int lead = plan.lead[g];
-    s.seq = plan.slot[lead];
-    s.end = plan.lo[lead];
-    s.pos = t * p.keys;
-  } else {
-    const int per = kv * p.chunks;
-    s.req = qa_find(plan.cum, p.batch, x / per);  // cum[r] * per <= x < cum[r + 1] * per
-    s.nreq = 1;
-    tiles = plan.cum[s.req + 1] - plan.cum[s.req];
-    const int z = x - plan.cum[s.req] * per, unit = z / tiles;
-    t = z - unit * tiles;
-    s.kvh = unit / p.chunks;
-    s.row0 = (unit - s.kvh * p.chunks) * kQaRows;
-    s.rows = min(p.rows - s.row0, kQaRows);
-    s.slot = s.req * per + unit + run;
-    s.seq = plan.slot[s.req];
-    s.end = plan.len[s.req];
-    s.pos = plan.lo[s.req] + t * p.keys;
-    if (t == 0 && tiles <= x_end - x && plan.group[s.req] < 0) s.slot = -1;
-  }
-  s.left = min(tiles - t, x_end - x);
-  return s;
-}
 
 // Walks a CTA's segments: its run of own items, then its run of prefix items.
 // Runs of own items start at the CTA after the last one with prefix items, so
-// that small problems spread out.
+// that small problems spread out.  The first item of a run is found by a search
+// and divisions, the others by steps: short items need a segment every few
+// microseconds.
 struct QaWalk {
-  int kind, run, x, x_end;
-  __device__ void begin(const QaPlan& plan, int k) {
+  int kind = -1, run, x = 0, x_end = 0;
+  int t;           // of the next item: its first tile
+  int req, kvh, row0;  // own: the item
+  int g, it, tile;     // prefix: the group, the item in it, and the item among those of its kv head
+  __device__ __forceinline__ void begin(const QaParams& p, const QaPlan& plan, int k) {
     kind = k;
     const PfxCuts c = k == kQaOwn ? plan.t->own : plan.t->pre;
     run = blockIdx.x;
@@ -318,16 +287,77 @@ struct QaWalk {
       if (run < 0) run += gridDim.x;
     }
     x = x_end = 0;
-    if (run < c.runs) {
-      x = pfx_cut(c, run);
-      x_end = pfx_cut(c, run + 1);
+    if (run >= c.runs) return;
+    x = pfx_cut(c, run);
+    x_end = pfx_cut(c, run + 1);
+    if (k == kQaOwn) {
+      const int per = p.cache.n_kv_heads * p.chunks;
+      req = qa_find(plan.cum, p.batch, x / per);  // cum[r] * per <= x < cum[r + 1] * per
+      const int tiles = plan.cum[req + 1] - plan.cum[req], z = x - plan.cum[req] * per, unit = z / tiles;
+      t = z - unit * tiles;
+      kvh = unit / p.chunks;
+      row0 = (unit - kvh * p.chunks) * kQaRows;
+    } else {
+      g = qa_find(plan.base, p.n_groups, x);
+      const int tiles = plan.tiles[g], y = x - plan.base[g], n = plan.row_tiles[g];
+      it = y / tiles;
+      t = y - it * tiles;
+      // kv head outermost: the items of one kv head read the same keys at about the same time.
+      kvh = it / n;
+      tile = it - kvh * n;
     }
   }
   __device__ __forceinline__ bool next(const QaParams& p, const QaPlan& plan, QaSeg& s) {
-    if (x == x_end && kind == kQaOwn) begin(plan, kQaPrefix);
-    if (x == x_end) return false;
-    s = qa_segment(p, plan, kind, x, x_end, run);
+    while (x == x_end) {
+      if (kind == kQaPrefix) return false;
+      begin(p, plan, kind + 1);
+    }
+    const int kv = p.cache.n_kv_heads;
+    int tiles;
+    s.kind = kind;
+    s.kvh = kvh;
+    if (kind == kQaOwn) {
+      while (plan.cum[req + 1] == plan.cum[req]) ++req;
+      tiles = plan.cum[req + 1] - plan.cum[req];
+      s.req = req;
+      s.row0 = row0;
+      s.rows = min(p.rows - row0, kQaRows);
+      s.slot = (req * kv + kvh) * p.chunks + row0 / kQaRows + run;
+      s.seq = plan.slot[req];
+      s.end = plan.len[req];
+      s.pos = plan.lo[req] + t * p.keys;
+      if (t == 0 && tiles <= x_end - x && plan.group[req] < 0) s.slot = -1;
+      row0 += kQaRows;
+      if (row0 >= p.rows) {
+        row0 = 0;
+        if (++kvh == kv) {
+          kvh = 0;
+          ++req;
+        }
+      }
+    } else {
+      while (plan.base[g + 1] == plan.base[g]) ++g;
+      tiles = plan.tiles[g];
+      s.req = plan.start[g] + tile * p.per_tile;
+      s.row0 = 0;
+      s.rows = min(p.per_tile, plan.start[g + 1] - s.req) * p.rows;
+      s.slot = plan.item[g] * kv + it + run;
+      const int lead = plan.lead[g];
+      s.seq = plan.slot[lead];
+      s.end = plan.lo[lead];
+      s.pos = t * p.keys;
+      ++it;
+      if (++tile == plan.row_tiles[g]) {
+        tile = 0;
+        if (++kvh == kv) {
+          kvh = it = 0;
+          ++g;
+        }
+      }
+    }
+    s.left = min(tiles - t, x_end - x);
     x += s.left;
+    t = 0;
     return true;
   }
 };
@@ -405,78 +435,71 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 
 // ------------------------------------------------------------------ producer
 template <int D, int BITS, int NMAX>
-__device__ void qa_producer(const QaParams& p, const QaPlan& plan, uint8_t* ring, QA_SHARED& sb, const QaWait& wt) {
+__device__ void qa_producer(const QaParams& p, uint8_t* ring, QA_SHARED& sb, const QaWait& wt) {
   using C = QaCfg<D, BITS, NMAX>;
   constexpr int NS = C::kStages, kKeys = 128 * C::kHalves;
   const CacheView& c = p.cache;
   const int lane = threadIdx.x & 31;
-  const int block = c.head_bytes, at = lane << c.page_shift;
-  QaWalk walk;
-  walk.begin(plan, kQaOwn);
-  QaSeg seg;
+  const int block = c.head_bytes, half_pages = 128 >> c.page_shift;
   QaRing<NS> st;
-  int n = 0, t = 0, k = 0, bad = 0;
+  int n = 0, t = 0, bad = 0;
   bool ok = true;
-  while (ok && walk.next(p, plan, seg)) {
-    int flags = kQaFirst;
-    auto look = [&](int pos) {  // this lane's page of a step (up to 16 pages)
-      return at < kKeys && pos + at < seg.end
-                 ? __ldg(c.table + (size_t)seg.seq * c.max_pages + ((pos + at) >> c.page_shift))
-                 : -1;
-    };
-    int page = look(seg.pos);
-    if (lane == 0) {
-      sb.segs[k % kQaSched][0] = make_int4(seg.req, seg.kvh, seg.row0, seg.rows);
-      sb.segs[k % kQaSched][1] = make_int4(seg.kind, seg.end, 0, 0);
-      mbar_arrive(&sb.seg_full[k % kQaSched]);
-    }
-    ++k;
-    for (; ok && seg.left > 0; --seg.left, seg.pos += kKeys, flags = 0) {
-      const bool on = at < kKeys && seg.pos + at < seg.end;
-      const bool valid = on && valid_page(c, page);
-      const uint32_t loads = __ballot_sync(0xffffffffu, valid);
-      if (__any_sync(0xffffffffu, on && !valid)) {
-        flags |= kQaFaulty;
+  for (int k = 0;; ++k) {
+    if (!(ok = qa_wait(&sb.seg_full[k % kQaSched], (k / kQaSched) & 1, wt))) break;
+    const int4 a = sb.segs[k % kQaSched][0], e = sb.segs[k % kQaSched][1];
+    if (a.x == 0) break;
+    int info = a.x << 8 | kQaFirst, at = 0;  // (rows << 8 | kind << 16); the next half's first lane
+    int page = sb.pages[k % kQaSched][lane];
+    uint32_t valid = __ballot_sync(0xffffffffu, valid_page(c, page));
+    const int* table = c.table + (size_t)e.w * c.max_pages;
+    const uint8_t* from = p.plane + (size_t)e.x * block;
+#pragma unroll 1
+    for (int pos = a.y; pos < a.z; pos += kKeys, info &= ~kQaFirst) {
+      if (at == 32) {  // (steps have 1 to 16 pages)
+        const int mine = (pos >> c.page_shift) + lane;
+        page = mine << c.page_shift < a.z ? __ldg(table + mine) : -1;
+        valid = __ballot_sync(0xffffffffu, valid_page(c, page));
+        at = 0;
+      }
+      const int keys = min(kKeys, a.z - pos);
+      const uint32_t step = (1u << ((keys + c.page - 1) >> c.page_shift)) - 1u;
+      if (step & ~(valid >> at)) {
+        info |= kQaFaulty;
         bad = 1;
       }
-      if (seg.left == 1) flags |= kQaLast;
-      const int keys = min(kKeys, seg.end - seg.pos);
-      const uint8_t* from = p.plane + (size_t)max(page, 0) * c.page_bytes + (size_t)seg.kvh * block;
+      if (pos + kKeys >= a.z) info |= kQaLast;
+      bool told = false;
 #pragma unroll 1
-      for (int h = 0; 128 * h < keys; ++h) {
+      for (int h = 0; h < keys; h += 128, at += half_pages) {
         if (n >= NS && !(ok = qa_wait(&sb.empty[st.at], st.phase ^ 1, wt))) break;
-        const int first = (128 * h) >> c.page_shift, pages = 128 >> c.page_shift;  // this half's lanes
         if (lane == 0) {
-          if (h == 0) {
-            sb.sched[t % kQaSched][0] = make_int4(flags | seg.rows << 8 | seg.kind << 16 | keys << 20, seg.pos, seg.slot, seg.req);
-            sb.sched[t % kQaSched][1] = make_int4(seg.kvh, seg.row0, 0, 0);
+          if (!told) {
+            sb.sched[t % kQaSched] = make_int2(info | keys << 20, pos);
             mbar_arrive(&sb.sched_full[t % kQaSched]);
           }
-          sb.half_keys[st.at] = min(128, keys - 128 * h);
-          mbar_arrive_expect_tx(&sb.full[st.at], __popc(loads >> first & ((1u << pages) - 1u)) * block);
+          sb.half_keys[st.at] = min(128, keys - h);
+          mbar_arrive_expect_tx(&sb.full[st.at], __popc(valid >> at & ((1u << half_pages) - 1u)) * block);
         }
         __syncwarp();
-        const int mine = lane - first;
-        if (valid && mine >= 0 && mine < pages)
-          bulk_load(ring + st.at * C::kStageBytes + mine * block, from, block, &sb.full[st.at]);
+        const int mine = lane - at;
+        if (mine >= 0 && mine < half_pages && (valid >> lane & 1u))
+          bulk_load(ring + st.at * C::kStageBytes + mine * block, from + (size_t)page * c.page_bytes, block, &sb.full[st.at]);
+        told = true;
         st.next();
         ++n;
       }
+      if (!ok) break;
       ++t;
-      if (seg.left > 1) page = look(seg.pos + kKeys);
     }
+    if (!ok) break;
   }
-  // The end, for the queries and each of the teams.
-  if (lane == 0) {
-    sb.segs[k % kQaSched][0] = make_int4(0, 0, 0, 0);
-    mbar_arrive(&sb.seg_full[k % kQaSched]);
-  }
+  // The end, for each of the teams.
 #pragma unroll 1
   for (int k = 0; ok && k < C::kTeams; ++k) {
     if (n + k >= NS && !(ok = qa_wait(&sb.empty[st.at], st.phase ^ 1, wt))) break;
     if (lane == 0) {
       if (k == 0) {
-        sb.sched[t % kQaSched][0] = make_int4(kQaEnd, 0, 0, 0);
+        sb.sched[t % kQaSched] = make_int2(kQaEnd, 0);
         mbar_arrive(&sb.sched_full[t % kQaSched]);
       }
       sb.half_keys[st.at] = 0;
@@ -506,26 +529,46 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
   using C = QaCfg<D, BITS, NMAX>;
   constexpr int kPieces = D / 8;  // of 16 bytes, of a row
   const int lane = threadIdx.x & 31;
+  const CacheView& c = p.cache;
+  QaWalk walk;
+  QaSeg seg = {};
+  int page = -1;
+  auto next = [&]() {  // the next segment and its first pages
+    seg.rows = 0;
+    page = -1;
+    if (!walk.next(p, plan, seg)) return;
+    seg.end = min(seg.end, seg.pos + seg.left * p.keys);
+    const int mine = (seg.pos >> c.page_shift) + lane;
+    if (mine << c.page_shift < seg.end) page = __ldg(c.table + (size_t)seg.seq * c.max_pages + mine);
+  };
+  auto tell = [&](int k) {
+    sb.pages[k % kQaSched][lane] = page;
+    if (lane == 0) {
+      sb.segs[k % kQaSched][0] = make_int4(seg.rows | (seg.rows ? seg.kind << 8 : 0), seg.pos, seg.end, seg.req);
+      sb.segs[k % kQaSched][1] = make_int4(seg.kvh, seg.row0, seg.slot, seg.seq);
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sb.seg_full[k % kQaSched]);
+  };
+  next();
+  tell(0);
+#pragma unroll 1
   for (int k = 0;; ++k) {
+    const int kvh = seg.kvh, row0 = seg.row0, rows = seg.rows, kind = seg.kind, req = seg.req, end = seg.end;
+    if (rows == 0) break;
     const int buf = k & 1;
-    if (!qa_wait(&sb.seg_full[k % kQaSched], (k / kQaSched) & 1, wt)) break;
-    const int4 a = sb.segs[k % kQaSched][0], e = sb.segs[k % kQaSched][1];
-    struct {
-      int req, kvh, row0, rows, kind, end;
-    } const seg = {a.x, a.y, a.z, a.w, e.x, e.y};
-    if (seg.rows == 0) break;
     if (k >= 2 && !qa_wait(&sb.q_free[buf], ((k >> 1) - 1) & 1, wt)) break;
     // Loops are left as loops: a segment's code is not in the nearest cache when
     // it begins, and straight code costs its fetch.
-    const int all = (seg.rows + 15) & ~15;
+    const int all = (rows + 15) & ~15;
     int least = INT_MAX;
 #pragma unroll 1
     for (int n = lane; n < all; n += 32) {
       int lim = 0, r = 0;
-      if (n < seg.rows) {
-        if (seg.kind != kQaOwn) r = n / p.rows;
-        const int row = seg.row0 + n - r * p.rows, i = row % p.q_len, req = seg.req + r;
-        if (i < plan.add[req]) lim = max(min(plan.len[req] - plan.add[req] + i + 1, seg.end), 0);
+      if (n < rows) {
+        if (kind != kQaOwn) r = n / p.rows;
+        const int row = row0 + n - r * p.rows, i = row % p.q_len, from = req + r;
+        if (i < plan.add[from]) lim = max(min(plan.len[from] - plan.add[from] + i + 1, end), 0);
         if (lim > 0) least = min(least, lim);
         sb.lim[buf][n] = lim;
       }
@@ -541,7 +584,7 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
     constexpr int kAtOnce = 32 / kPieces;
     const int sub = lane / kPieces, piece = lane - sub * kPieces;
     const uint8_t* Q = reinterpret_cast<const uint8_t*>(p.Q) +
-                       (((size_t)seg.req * p.cache.n_kv_heads + seg.kvh) * p.rows + seg.row0) * (D * 2) + 16 * piece;
+                       (((size_t)req * p.cache.n_kv_heads + kvh) * p.rows + row0) * (D * 2) + 16 * piece;
     uint8_t* tile = q_tiles + buf * C::kQBytes + (piece >> 3) * C::kBoxBytes;
 #pragma unroll 1
     for (int n = sub; n < all && sub < kAtOnce; n += kAtOnce) {
@@ -551,6 +594,7 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
                    "l"(Q + (size_t)max(from, 0) * (D * 2)), "r"(from < 0 ? 0 : 16)
                    : "memory");
     }
+    next();  // the next segment and its pages, while these are on their way
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (!p.fp16) {
 #pragma unroll 1
@@ -587,6 +631,7 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) mbar_arrive(&sb.q_ready[buf]);
+    tell(k + 1);
   }
   __syncwarp();
 }
@@ -631,7 +676,7 @@ __device__ void qa_products_s(const QaParams& p, uint8_t* q_tiles, QA_SHARED& sb
 #pragma unroll 1
   for (int t = 0;; ++t, r.next()) {
     if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) break;
-    const int info = __shfl_sync(0xffffffffu, sb.sched[t % kQaSched][0].x, 0);
+    const int info = __shfl_sync(0xffffffffu, sb.sched[t % kQaSched].x, 0);
     const int b = r.at;
     // (The end too waits for the softmax to have seen the step that had this buffer.)
     if (t >= C::kDepth && !qa_wait(&sb.s_free[b], r.phase ^ 1, wt)) break;
@@ -687,7 +732,7 @@ __device__ void qa_products_pv(const QaParams& p, uint8_t* p_tiles, QA_SHARED& s
 #pragma unroll 1
   for (int t = 0;; ++t, r.next()) {
     if (!qa_wait(&sb.sched_full[t % kQaSched], (t / kQaSched) & 1, wt)) break;
-    const int info = __shfl_sync(0xffffffffu, sb.sched[t % kQaSched][0].x, 0);
+    const int info = __shfl_sync(0xffffffffu, sb.sched[t % kQaSched].x, 0);
     if (info & kQaEnd) break;
     const int b = r.at;
     if (!qa_wait(&sb.p_ready[b], r.phase, wt)) break;
@@ -964,10 +1009,11 @@ __device__ void qa_results(const QaParams& p, QA_SHARED& sb, const QaWait& wt) {
   for (int seg = 0;; ++seg) {
     const int buf = seg & 1;
     if (!qa_wait(&sb.end_ready[buf], (seg >> 1) & 1, wt)) return;
-    const int4 e0 = sb.last[buf][0], e1 = sb.last[buf][1];
-    if (e0.x & kQaEnd) return;
-    const int rows = qa_rows(e0.x), kind = qa_kind(e0.x);
-    const bool direct = e0.z < 0, faulty = e0.x & kQaFaulty;
+    const int info = sb.last[buf];
+    if (info & kQaEnd) return;
+    const int4 e0 = sb.segs[seg % kQaSched][0], e1 = sb.segs[seg % kQaSched][1];
+    const int rows = qa_rows(info), kind = qa_kind(info);
+    const bool direct = e1.z < 0, faulty = info & kQaFaulty;
     const int slot_rows = kind == kQaPrefix ? kQaRows : min(p.rows, kQaRows);
     // A lane has the sums and references of rows `lane` and 32 + lane.
     float inv[(NMAX + 31) / 32];
@@ -977,13 +1023,13 @@ __device__ void qa_results(const QaParams& p, QA_SHARED& sb, const QaWait& wt) {
       const float(*from)[kQaRows] = sb.sums[buf];
       const float l = from[0][n] + from[1][n] + from[2][n] + from[3][n], top = sb.top[buf][n];
       if (!direct && w == 0 && 32 * k + lane < rows)
-        p.work.ml[kind][(size_t)e0.z * slot_rows + n] = faulty ? make_float2(0.0f, NAN) : make_float2(top, l);
+        p.work.ml[kind][(size_t)e1.z * slot_rows + n] = faulty ? make_float2(0.0f, NAN) : make_float2(top, l);
       inv[k] = l > 0.0f && !faulty && top > -INFINITY ? 1.0f / l : 0.0f;
     }
     if (!qa_wait(&sb.o_full[buf], (seg >> 1) & 1, wt)) return;
     tc_fence_after_sync();
     if (32 * w < D) {
-      float* part = p.work.O[kind] + (size_t)(direct ? 0 : e0.z) * slot_rows * D + d;
+      float* part = p.work.O[kind] + (size_t)(direct ? 0 : e1.z) * slot_rows * D + d;
       uint16_t* out = reinterpret_cast<uint16_t*>(p.O) +
                       (((size_t)e0.w * p.cache.n_kv_heads + e1.x) * p.rows + e1.y) * D + d;
 #pragma unroll 1
@@ -1141,11 +1187,10 @@ __device__ __noinline__ bool qa_turn(Shared& sb, const QaWait& wt, uint32_t s_at
 // After the last step of a segment: what its results need besides O.  `sums` as
 // that step left them.
 template <int NMAX, class Shared>
-__device__ __forceinline__ void qa_last(Shared& sb, int t, int seg, bool faulty, const float2* sums) {
+__device__ __forceinline__ void qa_last(Shared& sb, int info, int seg, const float2* sums) {
   const QaGroup<NMAX> q;
   const int buf = seg & 1;
-  const int4 e0 = sb.sched[t % kQaSched][0];
-  const int row0 = q.row0(), row_end = row0 + q.rows(qa_rows(e0.x));
+  const int row0 = q.row0(), row_end = row0 + q.rows(qa_rows(info));
 #pragma unroll 1
   for (int n0 = row0; n0 < row_end; n0 += 8) {
     float2 l = sums[(n0 - row0) * 16];
@@ -1156,10 +1201,7 @@ __device__ __forceinline__ void qa_last(Shared& sb, int t, int seg, bool faulty,
     }
     if (q.lane < 4) *reinterpret_cast<float2*>(&sb.sums[buf][q.w][n0 + 2 * q.lane]) = l;
   }
-  if (threadIdx.x == 0) {
-    sb.last[buf][0] = make_int4(faulty ? e0.x | kQaFaulty : e0.x, e0.y, e0.z, e0.w);
-    sb.last[buf][1] = sb.sched[t % kQaSched][1];
-  }
+  if (threadIdx.x == 0) sb.last[buf] = info;
   __syncwarp();
   qa_arrive(&sb.end_ready[buf], q.lane);
 }
@@ -1187,7 +1229,7 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
   for (int t = 0;; ++t, r3.next()) {
     const int b = r3.at, odd = t & 1;
     ok = ok && qa_wait(&sb.s_full[b], r3.phase, wt);
-    const int2 e = *reinterpret_cast<const int2*>(&sb.sched[t % kQaSched][0]);
+    const int2 e = sb.sched[t % kQaSched];
     const int info = ok ? e.x : kQaEnd, rows = q.rows(qa_rows(info));
     const bool first = info & kQaFirst;  // (not where a wait has run out)
     bool turn = info & (kQaFirst | kQaEnd), turned = false;
@@ -1268,7 +1310,7 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
       if (*reinterpret_cast<volatile int*>(&sb.failed[q.i])) return;
       if (info & kQaEnd) {
         if (seg >= 1 && !qa_wait(&sb.o_free[(seg + 1) & 1], ((seg - 1) >> 1) & 1, wt)) return;
-        if (q.w == 0 && q.i == 0 && lane == 0) sb.last[(seg + 1) & 1][0] = make_int4(kQaEnd, 0, 0, 0);
+        if (q.w == 0 && q.i == 0 && lane == 0) sb.last[(seg + 1) & 1] = kQaEnd;
         __syncwarp();
         qa_arrive(&sb.end_ready[(seg + 1) & 1], lane);
         return;
@@ -1291,7 +1333,7 @@ __device__ void qa_softmax(const QaParams& p, uint8_t* p_tiles, float2* all_sums
     qa_arrive(&sb.p_ready[b], lane);
     if (info & kQaLast) {
       qa_arrive(&sb.q_free[seg & 1], lane);  // the limits have been read
-      if (ok) qa_last<NMAX>(sb, t, seg, faulty, sums + odd * kSumsStep);
+      if (ok) qa_last<NMAX>(sb, faulty ? info | kQaFaulty : info, seg, sums + odd * kSumsStep);
     }
   }
 }
@@ -1395,7 +1437,7 @@ __global__ void __launch_bounds__(QaCfg<D, BITS, NMAX>::kThreads, 1)
       else
         qa_values<D, BITS, NMAX>(p, k - C::kKeyTeams, ring, sb, wt);
     } else if (warp == kOther) {
-      qa_producer<D, BITS, NMAX>(p, plan, ring, sb, wt);
+      qa_producer<D, BITS, NMAX>(p, ring, sb, wt);
     } else if (warp == kOther + 1) {
       qa_queries<D, BITS, NMAX>(p, plan, q_tiles, sb, wt);
       // Where the merge finds its parts.
