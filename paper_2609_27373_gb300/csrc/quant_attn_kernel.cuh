@@ -14,24 +14,36 @@
 // moves by halves of 128 keys, one row of the product's M each.
 //
 // Warp roles (768 threads):
-//   4 warps      softmax (8 in the wide instance, each 4 for 32 of the rows): S^T from tensor memory in fragments of 8 keys x 8
-//                rows, running maximum (raised only when a numerator passes
-//                2^15, which the warps vote on), numerators as fp16 to
-//                shared memory (P, the B operand of the second product), O's
-//                rescaling;
-//   then in turn (two teams of each that take every other half, in the wide
-//                instance one)
-//                K: codes to tensor memory;
-//                V: the same, scales of 8 tokens at a time;
-//   4 warps      results: O, or a partial result, of segments that have ended, while
-//                the softmax goes on with the next (O is held twice);
-//   a warp       producer: page look-ups, one bulk copy a page (codes and scales
-//                of keys and values lie together), the schedule;
-//   a warp       Q: rows of the next segment to shared memory as fp16, each scaled by
-//                a power of two so that its largest is next to 2^15 (exact down
-//                to 2^-28 of it), and how many keys each row sees;
+//   4 warps      softmax (8 in the wide instance, each 4 for 32 of the rows): S^T
+//                from tensor memory in fragments of 8 keys x 8 rows, the mask,
+//                running maximum (raised only when a numerator passes 2^15, which
+//                the warps vote on), numerators as fp16 to shared memory (P, the B
+//                operand of the second product), O's rescaling;
+//   4 warps      K: codes to tensor memory;
+//   8 or 4       V: the same, scales of 8 tokens at a time (in the narrow instance
+//                two teams that take every other half);
+//   4 warps      results: O, or a partial result, of segments that have ended,
+//                while the softmax goes on with the next;
+//   a warp       producer: one bulk copy a page (codes and scales of keys and
+//                values lie together), the schedule;
+//   a warp       the walk over the segments and their page look-ups, and Q: rows of
+//                the next segment to shared memory as fp16, each scaled by a power
+//                of two so that its largest is next to 2^15 (exact down to 2^-28
+//                of it), and how many keys each row sees;
 //   two warps    S products and P V products, each issued by one lane.
 // All of tensor memory is allocated, so that its first column is 0.
+//
+// What bounds it.  With 8 bits the memory: 32 x 4K tokens of 8 kv heads of 128 in
+// 103 us, 5.8 TB/s, 0.85 of a copy.  With 4 bits and long rows the instructions:
+// turning codes into operands and the softmax leave the schedulers idle for 4
+// slots in 10, mostly behind one another's latencies (32 x 12K tokens: 105 us, 4.4
+// TB/s, 2300 clk a step).  With short rows the fetching of instructions: 24 warps
+// in a dozen codes of their own keep little of what a segment does once in the
+// nearest cache, and code that runs once costs 8 to 10 clk an instruction.  So
+// what belongs to a segment is in loops and on warps beside the softmax's: with
+// the results on the softmax's warps, the walk on the producer's and the copying
+// of Q unrolled, a segment of one step took 8800 clk, now 6400 (5500 items of 210
+// tokens: 169 -> 122 us; of 900 tokens: 228 -> 184 us).
 //
 // Every wait is bounded; one that runs out sets the status word and an abort
 // flag, and every role unwinds.
@@ -55,11 +67,12 @@ struct QaCfg {
   static constexpr int kGroups = NMAX == 16 ? 1 : 2, kKeyTeams = 1, kTeams = NMAX == 16 ? 2 : 1;
   static constexpr int kThreads = 128 * (kGroups + kKeyTeams + kTeams + 2);
   // Halves of K and of V in tensor memory.  V stays until the softmax has been
-  // through its step: with 3 buffers one half of a step had to wait for the
-  // products of the step before (32 x 12K tokens: 111 us).
+  // through its step: with 3 buffers one half of a step has to wait for the
+  // products of the step before (32 x 12K tokens: 2 us more).
   static constexpr int kKeyBuffers = 2, kValueBuffers = NMAX == 16 ? 4 : 2;
-  // Steps whose S and P are held at a time.
-  static constexpr int kDepth = 3, kOuts = NMAX == 16 ? 2 : 1;  // and segments whose O is
+  // Steps whose S and P are held at a time (2 in the wide instance: 64 on a shared
+  // 32K prefix 120 -> 128 us), and segments whose O is.
+  static constexpr int kDepth = 3, kOuts = NMAX == 16 ? 2 : 1;
   // Columns: K, V, S, O.
   static constexpr uint32_t kTmemK = 0, kTmemV = 64 * kKeyBuffers, kTmemS = kTmemV + 64 * kValueBuffers,
                             kTmemO = kTmemS + kDepth * kHalves * NMAX;
@@ -995,10 +1008,6 @@ struct QaGroup {
   __device__ __forceinline__ void sync() const { named_barrier_sync(2 + 2 * i, 128); }
   __device__ __forceinline__ uint32_t lanes() const { return (uint32_t)(32 * w) << 16; }
 };
-
-// What a step has to do now and then stands apart, so that the code of most
-// steps is short: with all of it in one loop the four warps spent more time on
-// fetching instructions than on anything else (2900 clk a step of 256 keys).
 
 // Four warps that write O, or a partial result, of each segment that has ended.
 template <int D, int BITS, int NMAX>
