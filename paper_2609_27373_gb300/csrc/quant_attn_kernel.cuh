@@ -87,10 +87,13 @@ struct QaCfg {
   static constexpr int kSumBytes = 2 * (NMAX / 8) * 128 * 8;  // of two steps, a pair of rows' sums for each thread
   static constexpr int kFixed = 2 * kQBytes + kDepth * kPBytes + kSumBytes;
   static constexpr int kRoom = (217 * 1024 - 1024 - kMaxPlanBytes - kFixed) / kStageBytes;
-  static constexpr int kStages = kRoom < 8 ? kRoom : 8;
+  // A multiple of the V teams.  A wait knows the parity of a stage's phase alone,
+  // so whoever waits for a load must have seen the stage's load before it, and a
+  // team sees its own halves only (loads may end out of order).
+  static constexpr int kStages = (kRoom < 8 ? kRoom : 8) / kTeams * kTeams;
   static constexpr int kPlanAt = kFixed + kStages * kStageBytes;
   static constexpr int kSmem = kPlanAt + kMaxPlanBytes + 1024;
-  static_assert(kStages >= 2 && kStageBytes % 128 == 0, "ring");
+  static_assert(kStages >= 2 && kStageBytes % 128 == 0 && kValueBuffers % kTeams == 0, "rings");
 };
 
 constexpr int kQaSched = 16;
