@@ -586,8 +586,10 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
         const int row = row0 + n - r * p.rows, i = row % p.q_len, from = req + r;
         if (i < plan.add[from]) lim = max(min(plan.len[from] - plan.add[from] + i + 1, end), 0);
         if (lim > 0) least = min(least, lim);
-        sb.lim[buf][n] = lim;
       }
+      // 0 behind the rows too: what a step's empty half holds from before must
+      // not look like a numerator there.
+      sb.lim[buf][n] = lim;
       sb.q_scale[buf][n] = fmaxf(p.scale_log2, FLT_MIN);
       sb.q_from[n] = lim > 0 ? n + r * (p.cache.n_kv_heads - 1) * p.rows : -1;  // in rows
     }

@@ -91,3 +91,22 @@ def test_repeats_with_cold_caches(bits, page, head_dim, n_heads):
         cache.attend(0, Q, outs[-1], s)
     assert all(torch.equal(O, first) for O in outs)
     assert wise.wise_get_status() == wise.WISE_OK
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("n_heads", [5, 20])
+def test_other_calls_leave_no_trace(bits, n_heads):
+    """The same bits whatever ran before: items of few rows that end inside a step after calls with more rows and large
+    logits of either sign."""
+    lens = [257 + i % 128 for i in range(200)]
+    cache, twin, slots, gen = build(bits, lens, 64, 1, 64, torch.bfloat16, 3)
+    other, _, theirs, _ = build(bits, [2000] * 200, 64, 1, 64, torch.bfloat16, 4)
+    Q, first = run(cache, twin, slots, gen, n_heads, 1)
+    s, t, X = u32(slots), u32(theirs), torch.empty((200, 16 if n_heads == 5 else 64, 1, 64), dtype=torch.bfloat16, device="cuda")
+    for i in range(12):
+        X.copy_(torch.randn(X.shape, generator=gen, device="cuda") * (0.0, 30.0, 300.0)[i % 3])
+        other.attend(0, X, torch.empty_like(X), t)
+        O = torch.full_like(Q, float("nan"))
+        cache.attend(0, Q, O, s)
+        assert torch.equal(O, first)
+    assert wise.wise_get_status() == wise.WISE_OK
