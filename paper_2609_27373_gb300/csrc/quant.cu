@@ -9,6 +9,12 @@
 // cache that holds for keys too; values lie by channels, so a warp transposes
 // its 32 x 32 codes in registers, exchanging lane bit i with index bit i at a
 // time.
+//
+// Bound by instructions: 2 x 32K tokens of 8 heads of 128 are stored in 4 bits in
+// 65 us (343 MB read and written, 5.3 of a copy's 6.8 TB/s; 62 of 100 issue slots
+// taken: 16 values need their maximum, a quotient, a reciprocal and 16 products and
+// roundings) and read back in 66.  With a warp for 32 channels of a span at any size
+// storing and reading back took 199 us together and reading 103.
 #include <algorithm>
 
 #include "cache_common.cuh"

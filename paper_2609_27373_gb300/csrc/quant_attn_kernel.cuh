@@ -35,9 +35,9 @@
 //
 // What bounds it.  With 8 bits the memory: 32 x 4K tokens of 8 kv heads of 128 in
 // 103 us, 5.8 TB/s, 0.85 of a copy.  With 4 bits and long rows the instructions:
-// turning codes into operands and the softmax leave the schedulers idle for 4
-// slots in 10, mostly behind one another's latencies (32 x 12K tokens: 105 us, 4.4
-// TB/s, 2300 clk a step).  With short rows the fetching of instructions: 24 warps
+// turning codes into operands and the softmax issue in 65 of 100 slots and wait for
+// one another's latencies in the rest (32 x 12K tokens: 105 us, 4.4 TB/s, 2300 clk
+// a step).  With short rows the fetching of instructions: 24 warps
 // in a dozen codes of their own keep little of what a segment does once in the
 // nearest cache, and code that runs once costs 8 to 10 clk an instruction.  So
 // what belongs to a segment is in loops and on warps beside the softmax's: with
