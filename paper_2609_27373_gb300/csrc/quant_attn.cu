@@ -19,6 +19,8 @@ int launch_quant_attn(const PrefixParams& p, void* workspace, int sm_count, cuda
   L.p.group = p.group;
   L.p.n_groups = p.n_groups;
   L.p.rows = p.q_len * p.group;
+  L.p.rows_inv = 65536 / L.p.rows + 1;
+  L.p.q_len_inv = 65536 / p.q_len + 1;
   L.p.chunks = (L.p.rows + kQaRows - 1) / kQaRows;
   L.p.per_tile = p.n_groups > 0 && L.p.rows * 2 <= kQaRows ? kQaRows / L.p.rows : 0;
   L.p.fp16 = p.fp16;

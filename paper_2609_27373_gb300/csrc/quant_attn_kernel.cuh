@@ -582,8 +582,8 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
     for (int n = lane; n < all; n += 32) {
       int lim = 0, r = 0;
       if (n < rows) {
-        if (kind != kQaOwn) r = n / p.rows;
-        const int row = row0 + n - r * p.rows, i = row % p.q_len, from = req + r;
+        if (kind != kQaOwn) r = n * p.rows_inv >> 16;  // n / p.rows
+        const int row = row0 + n - r * p.rows, i = row - (row * p.q_len_inv >> 16) * p.q_len, from = req + r;
         if (i < plan.add[from]) lim = max(min(plan.len[from] - plan.add[from] + i + 1, end), 0);
         if (lim > 0) least = min(least, lim);
       }
