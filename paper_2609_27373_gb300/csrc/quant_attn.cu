@@ -37,7 +37,7 @@ int launch_quant_attn(const PrefixParams& p, void* workspace, int sm_count, cuda
   // The wide instance takes 64 rows at a time, the narrow one half a step's time
   // for at most 16 (32 x 12K tokens, 4 rows: 105 us against 145; 16 x 4K in 8
   // bits 103 against 127).  Sharing prefixes needs the wide one: 64 on a shared
-  // 32K prefix take 118 us in it, 501 each by itself in the narrow one.
+  // 32K prefix take 116 us in it, 501 each by itself in the narrow one.
   L.wide = L.p.rows > 16 || L.p.per_tile > 0;
   L.stream = stream;
   cudaError_t e;

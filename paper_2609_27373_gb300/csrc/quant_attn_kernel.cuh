@@ -43,7 +43,7 @@
 // what belongs to a segment is in loops and on warps beside the softmax's: with
 // the results on the softmax's warps, the walk on the producer's and the copying
 // of Q unrolled, a segment of one step took 8800 clk, now 6400 (5500 items of 210
-// tokens: 169 -> 122 us; of 900 tokens: 228 -> 184 us).
+// tokens: 169 -> 124 us; of 900 tokens: 228 -> 183 us).
 //
 // Every wait is bounded; one that runs out sets the status word and an abort
 // flag, and every role unwinds.
