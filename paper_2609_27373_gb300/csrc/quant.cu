@@ -261,7 +261,8 @@ __global__ void __launch_bounds__(kIoThreads, 4) quant_write_kernel(const QuantI
     // The span's pieces of values in the cache: T tokens each, in one page.
     const int T = BITS == 8 || c.page == 16 ? 16 : 32;
     const int from0 = max(start - base, 0), from1 = max(start - (base + 16), 0);  // first new tokens
-    const int page0 = __shfl_sync(0xffffffffu, page, min(from0, 31)), page1 = __shfl_sync(0xffffffffu, page, min(16 + from1, 31));
+    const int page0 = __shfl_sync(0xffffffffu, page, min(from0, 31));
+    const int page1 = __shfl_sync(0xffffffffu, page, min(16 + from1, 31));
 #pragma unroll 1
     for (int part = part0; part < part0 + jb.per_job; ++part) {
       uint32_t w[BITS];
@@ -307,7 +308,8 @@ __global__ void __launch_bounds__(kIoThreads, 4) quant_write_kernel(const QuantI
 
 // ---------------------------------------------------------------------- read
 template <int BITS, bool FP16>
-__global__ void __launch_bounds__(kIoThreads, 4) read_kernel(const QuantIo io, const QuantShape sh, const QuantJobs jb) {
+__global__ void __launch_bounds__(kIoThreads, 4) read_kernel(const QuantIo io, const QuantShape sh,
+                                                             const QuantJobs jb) {
   constexpr int W = BITS == 8 ? 8 : 4;  // words of a lane's 32 codes
   const CacheView& c = io.cache;
   const int lane = threadIdx.x & 31;
@@ -374,7 +376,8 @@ __global__ void __launch_bounds__(kIoThreads, 4) read_kernel(const QuantIo io, c
     }
     const int scale_step = values ? 2 * c.page : 2;
     const uint8_t* scales =
-        block + (values ? sh.value_scales + 2 * part0 * c.page + off : sh.key_scales + off * sh.key_scale_bytes + 2 * part0);
+        block +
+        (values ? sh.value_scales + 2 * part0 * c.page + off : sh.key_scales + off * sh.key_scale_bytes + 2 * part0);
     uint4 y[4] = {};
     uint32_t w[W] = {}, s0 = 0, s1 = 0;
     auto load = [&]() {  // of 32 channels

@@ -86,7 +86,8 @@ inline QaWork qa_work(void* base, int batch, int n_groups, int n_kv_heads, int r
     return p;
   };
   w.sources = reinterpret_cast<int4*>(take((size_t)units * 2 * sizeof(int4)));
-  for (int k = 0; k < 2; ++k) w.ml[k] = reinterpret_cast<float2*>(take((size_t)slots[k] * slot_rows[k] * sizeof(float2)));
+  for (int k = 0; k < 2; ++k)
+    w.ml[k] = reinterpret_cast<float2*>(take((size_t)slots[k] * slot_rows[k] * sizeof(float2)));
   for (int k = 0; k < 2; ++k) w.O[k] = reinterpret_cast<float*>(take((size_t)slots[k] * slot_rows[k] * head_dim * 4));
   w.bytes = off;
   return w;

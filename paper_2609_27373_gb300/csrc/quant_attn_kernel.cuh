@@ -499,7 +499,8 @@ __device__ void qa_producer(const QaParams& p, uint8_t* ring, QA_SHARED& sb, con
         __syncwarp();
         const int mine = lane - at;
         if (mine >= 0 && mine < half_pages && (valid >> lane & 1u))
-          bulk_load(ring + st.at * C::kStageBytes + mine * block, from + (size_t)page * c.page_bytes, block, &sb.full[st.at]);
+          bulk_load(ring + st.at * C::kStageBytes + mine * block, from + (size_t)page * c.page_bytes, block,
+                    &sb.full[st.at]);
         told = true;
         st.next();
         ++n;
@@ -528,7 +529,8 @@ __device__ void qa_producer(const QaParams& p, uint8_t* ring, QA_SHARED& sb, con
     // Copies already issued land before the CTA's shared memory is released,
     // whoever may have given up.  (Where the end took a stage they have.)
     int never = 0;
-    for (int k = max(0, ok ? n - NS + C::kTeams : n - NS); k < n; ++k) mbar_wait(&sb.full[k % NS], (k / NS) & 1, &never);
+    for (int k = max(0, ok ? n - NS + C::kTeams : n - NS); k < n; ++k)
+      mbar_wait(&sb.full[k % NS], (k / NS) & 1, &never);
   }
   __syncwarp();
 }
@@ -622,7 +624,8 @@ __device__ void qa_queries(const QaParams& p, const QaPlan& plan, uint8_t* q_til
         uint4 v = make_uint4(0, 0, 0, 0);
         if (on) v = *at;
         // The row's largest size has exponent field E; times 2^(141 - E) it lies in [2^14, 2^15).
-        uint32_t top = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+        uint32_t top = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu),
+                                __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
         top = max(top & 0xFFFFu, top >> 16);
         if constexpr (kPieces == 12) {
           // 12 lanes: those of the other row keep their own maximum.
@@ -995,7 +998,8 @@ template <int NMAX>
 struct QaGroup {
   static constexpr int kRows = NMAX == 16 ? 16 : 32;
   int lane, w, i;  // of the warp; warp of the group (TMEM lanes 32 w ..), group
-  __device__ __forceinline__ QaGroup() : lane(threadIdx.x & 31), w((threadIdx.x >> 5) & 3), i(NMAX == 16 ? 0 : threadIdx.x >> 7) {}
+  __device__ __forceinline__ QaGroup()
+      : lane(threadIdx.x & 31), w((threadIdx.x >> 5) & 3), i(NMAX == 16 ? 0 : threadIdx.x >> 7) {}
   __device__ __forceinline__ int row0() const { return kRows * i; }
   __device__ __forceinline__ int rows(int all) const { return NMAX == 16 ? all : min(max(all - kRows * i, 0), kRows); }
   __device__ __forceinline__ bool vote(bool x) const {
@@ -1133,7 +1137,8 @@ __device__ __forceinline__ bool qa_first(Shared& sb, const QaWait& wt, int seg, 
   if (seg >= 2 && !qa_wait(&sb.o_free[seg & 1], ((seg >> 1) - 1) & 1, wt)) return false;
   if (q.lane < q.kRows) {
     float moved = INFINITY;
-    if (q.lane < own && sb.lim[seg & 1][n] > 0) moved = qa_shift(sb, seg, n);  // rows that see nothing have queries of 0
+    // (Rows that see nothing have queries of 0.)
+    if (q.lane < own && sb.lim[seg & 1][n] > 0) moved = qa_shift(sb, seg, n);
     sb.top[seg & 1][n] = -moved;
     sb.shift[seg & 1][n] = moved == INFINITY ? 0.0f : moved;
   }
@@ -1148,8 +1153,8 @@ __device__ __forceinline__ bool qa_first(Shared& sb, const QaWait& wt, int seg, 
 // before left them.  Returns false when a wait has run out, which the next vote
 // will tell.
 template <int D, int NMAX, int H, int DEPTH, class Shared>
-__device__ __noinline__ bool qa_turn(Shared& sb, const QaWait& wt, uint32_t s_at, uint32_t o_at, int t, int pos, int seg, int rows,
-                                     bool mask, float2* sums) {
+__device__ __noinline__ bool qa_turn(Shared& sb, const QaWait& wt, uint32_t s_at, uint32_t o_at, int t, int pos,
+                                     int seg, int rows, bool mask, float2* sums) {
   const QaGroup<NMAX> q;
   const int row0 = q.row0(), row_end = row0 + q.rows(rows);
   qa_look<NMAX, H>(sb, s_at, pos, seg, rows, mask);
