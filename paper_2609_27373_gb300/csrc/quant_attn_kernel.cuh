@@ -513,7 +513,7 @@ __device__ void qa_producer(const QaParams& p, uint8_t* ring, QA_SHARED& sb, con
   // The end, for each of the teams.
 #pragma unroll 1
   for (int k = 0; ok && k < C::kTeams; ++k) {
-    if (n + k >= NS && !(ok = qa_wait(&sb.empty[st.at], st.phase ^ 1, wt))) break;
+    if (n >= NS && !(ok = qa_wait(&sb.empty[st.at], st.phase ^ 1, wt))) break;
     if (lane == 0) {
       if (k == 0) {
         sb.sched[t % kQaSched] = make_int2(kQaEnd, 0);
@@ -523,14 +523,15 @@ __device__ void qa_producer(const QaParams& p, uint8_t* ring, QA_SHARED& sb, con
       mbar_arrive(&sb.full[st.at]);
     }
     st.next();
+    ++n;
   }
   if (bad && lane == 0) atomicOr(c.status, kStatusBadCache);
   if (lane == 0) {
     // Copies already issued land before the CTA's shared memory is released,
-    // whoever may have given up.  (Where the end took a stage they have.)
+    // whoever may have given up: the last phase of each stage is waited for, that
+    // of an end too, as a wait for the phase before it would run out.
     int never = 0;
-    for (int k = max(0, ok ? n - NS + C::kTeams : n - NS); k < n; ++k)
-      mbar_wait(&sb.full[k % NS], (k / NS) & 1, &never);
+    for (int k = max(0, n - NS); k < n; ++k) mbar_wait(&sb.full[k % NS], (k / NS) & 1, &never);
   }
   __syncwarp();
 }
