@@ -12,30 +12,33 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("bits", [4, 8])
-@pytest.mark.parametrize("n_heads,tokens", [(16, 700), (16, 1500), (16, 2600), (80, 1500)])
-def test_a_call_whose_wait_has_run_out_ends_soon(bits, n_heads, tokens):
-    """Ordinary bounded waits with a limit of 1 ns give up at many places, between the two ends of a CTA's work among them
-    (16 heads: two teams for V, an end for each); none of the waits for copies in flight may then last the default 2 s."""
-    lens = [tokens + 37 * i % 500 for i in range(160)]
-    cache, twin, slots, gen = build(bits, lens, 64, 4, 128, torch.bfloat16, n_heads + tokens)
-    Q = torch.randn((160, n_heads, 1, 128), generator=gen, device="cuda").bfloat16()
-    O, s, longest, ran_out = torch.empty_like(Q), u32(slots), 0.0, False
+@pytest.mark.parametrize("n_heads", [4, 20])
+def test_a_call_whose_wait_has_run_out_ends_soon(bits, n_heads):
+    """An item a CTA, of a length at which the first wait to run out (the hardware holds one for some microseconds before
+    its limit is looked at) does so next to the end of the CTA's work, between the two ends that the teams of V get among
+    other places.  None of the waits for copies in flight may then last the default 2 s."""
+    B = torch.cuda.get_device_properties(0).multi_processor_count
+    cache, twin, slots, gen = build(bits, [1700] * B, 64, 1, 128, torch.bfloat16, n_heads)
+    Q = torch.randn((B, n_heads, 1, 128), generator=gen, device="cuda").bfloat16()
+    O, s, longest, ran_out = torch.empty_like(Q), u32(slots), 0.0, 0
     cache.attend(0, Q, O, s)
     torch.cuda.synchronize()
     wise.wise_set_wait_limit_ns(1)
     try:
-        for i in range(100):
-            s.copy_(u32(slots[i % 7:] + slots[:i % 7]))
-            a, b = torch.cuda.Event(True), torch.cuda.Event(True)
-            a.record()
-            cache.attend(0, Q, O, s)
-            b.record()
-            ran_out |= wise.wise_get_status() == wise.WISE_ERR_TIMEOUT
-            longest = max(longest, a.elapsed_time(b))
+        for tokens in range(600, 1700, 20):
+            cache.lens.fill_(tokens)
+            for _ in range(10):
+                a, b = torch.cuda.Event(True), torch.cuda.Event(True)
+                a.record()
+                cache.attend(0, Q, O, s)
+                b.record()
+                ran_out += wise.wise_get_status() == wise.WISE_ERR_TIMEOUT
+                longest = max(longest, a.elapsed_time(b))
             if longest >= 1000.0:
                 break
     finally:
         wise.wise_set_wait_limit_ns(0)
-    assert ran_out and longest < 1000.0, longest
+    assert ran_out > 100 and longest < 1000.0, (ran_out, longest)
+    cache.lens.fill_(1700)
     run(cache, twin, slots, gen, n_heads, 1)
     assert wise.wise_get_status() == wise.WISE_OK
