@@ -613,12 +613,8 @@ def wise_prefix_attn_workspace(cache: Cache, shape: wise_prefix_t) -> int:
     return int(load().wise_prefix_attn_workspace(cache.ref, ctypes.byref(shape)))
 
 
-def wise_prefix_attn(cache: Cache, layer: int, Q, O, slots, n_new=None, group_start=None, prefix_lens=None,
-                     workspace=None, scale: float = 0.0, stream=None, shape: wise_prefix_t = None) -> None:
-    """Attention of new tokens Q over the cached sequences in slots, into O (both [batch, n_heads, q_len,
-    head_dim]); the requests of group g, group_start[g] .. group_start[g + 1] - 1, share their first
-    prefix_lens[g] tokens (both None: nothing is shared).  `shape`: what prefix_shape gives for Q, made anew
-    when absent."""
+def _attn(entry, types, cache, layer, Q, O, slots, n_new, group_start, prefix_lens, workspace, scale, stream, shape):
+    """The call of an attention entry point over a cache; `types`: its arguments between the shape and Q."""
     n_groups = 0 if prefix_lens is None else prefix_lens.shape[0]
     if shape is None:
         shape = prefix_shape(cache, Q, n_groups, scale)
@@ -634,12 +630,22 @@ def wise_prefix_attn(cache: Cache, layer: int, Q, O, slots, n_new=None, group_st
     if workspace is not None:
         ws = _workspace(workspace, 0, cache)
         ws_bytes = workspace.numel() * workspace.element_size()
-    rc = load().wise_prefix_attn(cache.ref, layer, ctypes.byref(shape), _rows16(Q, "Q", full, cache),
-                                 _list32(slots, "slots", batch, cache),
-                                 0 if n_new is None else _list32(n_new, "n_new", batch, cache), starts, lens,
-                                 _rows16(O, "O", full, cache), ws, ws_bytes, _raw_stream(stream, cache.index))
+    rc = getattr(load(), entry)(cache.ref, layer, ctypes.byref(shape), *types, _rows16(Q, "Q", full, cache),
+                                _list32(slots, "slots", batch, cache),
+                                0 if n_new is None else _list32(n_new, "n_new", batch, cache), starts, lens,
+                                _rows16(O, "O", full, cache), ws, ws_bytes, _raw_stream(stream, cache.index))
     if rc != WISE_OK:
-        raise WiseError(rc, "wise_prefix_attn")
+        raise WiseError(rc, entry)
+
+
+def wise_prefix_attn(cache: Cache, layer: int, Q, O, slots, n_new=None, group_start=None, prefix_lens=None,
+                     workspace=None, scale: float = 0.0, stream=None, shape: wise_prefix_t = None) -> None:
+    """Attention of new tokens Q over the cached sequences in slots, into O (both [batch, n_heads, q_len,
+    head_dim]); the requests of group g, group_start[g] .. group_start[g + 1] - 1, share their first
+    prefix_lens[g] tokens (both None: nothing is shared).  `shape`: what prefix_shape gives for Q, made anew
+    when absent."""
+    _attn("wise_prefix_attn", (), cache, layer, Q, O, slots, n_new, group_start, prefix_lens, workspace, scale, stream,
+          shape)
 
 
 def wise_kvq_attn_workspace(cache: Cache, shape: wise_prefix_t) -> int:
@@ -648,31 +654,10 @@ def wise_kvq_attn_workspace(cache: Cache, shape: wise_prefix_t) -> int:
 
 
 def wise_kvq_attn(cache: Cache, layer: int, Q, O, slots, n_new=None, group_start=None, prefix_lens=None,
-                  workspace=None, scale: float = 0.0, stream=None, shape=None) -> None:
+                  workspace=None, scale: float = 0.0, stream=None, shape: wise_prefix_t = None) -> None:
     """wise_prefix_attn over a cache in 8 or 4 bits; Q and O are of the cache's dtype."""
-    if Q is None or Q.dim() != 4:
-        raise ValueError("Q must be [batch, n_heads, q_len, head_dim]")
-    if shape is None:
-        shape = prefix_shape(cache, Q, 0 if prefix_lens is None else prefix_lens.shape[0], scale)
-    batch, full = shape.batch, Q.shape
-    if full[3] != cache.head_dim:
-        raise ValueError(f"Q must have the cache's head_dim {cache.head_dim}")
-    starts = lens = 0
-    if prefix_lens is not None:
-        lens = _list32(prefix_lens, "prefix_lens", shape.n_groups, cache)
-        starts = _list32(group_start, "group_start", shape.n_groups + 1, cache)
-    elif group_start is not None:
-        raise ValueError("group_start needs prefix_lens")
-    ws = ws_bytes = 0
-    if workspace is not None:
-        ws = _workspace(workspace, 0, cache)
-        ws_bytes = workspace.numel() * workspace.element_size()
-    rc = load().wise_kvq_attn(cache.ref, layer, ctypes.byref(shape), cache.type_code, _rows16(Q, "Q", full, cache),
-                              _list32(slots, "slots", batch, cache),
-                              0 if n_new is None else _list32(n_new, "n_new", batch, cache), starts, lens,
-                              _rows16(O, "O", full, cache), ws, ws_bytes, _raw_stream(stream, cache.index))
-    if rc != WISE_OK:
-        raise WiseError(rc, "wise_kvq_attn")
+    _attn("wise_kvq_attn", (cache.type_code,), cache, layer, Q, O, slots, n_new, group_start, prefix_lens, workspace,
+          scale, stream, shape)
 
 
 def _on(t, name, shape, dtype, index):
