@@ -649,7 +649,8 @@ def wise_prefix_attn(cache: Cache, layer: int, Q, O, slots, n_new=None, group_st
 
 
 def wise_kvq_attn_workspace(cache: Cache, shape: wise_prefix_t) -> int:
-    """Bytes of workspace of wise_kvq_attn."""
+    """Bytes of workspace of wise_kvq_attn on the current device."""
+    _on_device(cache.index)
     return int(load().wise_kvq_attn_workspace(cache.ref, ctypes.byref(shape)))
 
 

@@ -59,3 +59,23 @@ def test_queries_of_another_shape_than_the_one_given_are_refused(lib, bits):
     with pytest.raises(ValueError, match="prefix_lens"):
         attn(cache, 0, Q, torch.empty_like(Q), slots, group_start=slots, workspace=ws)
     assert lib.calls == []
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+def test_tensors_of_another_device_than_the_current_one_are_refused(lib, monkeypatch, bits):
+    """Workspaces are of the current device's number of SMs, so they too are asked for on the tensors' own device."""
+    cache, Q, lists = make(bits), queries(), torch.zeros(2, dtype=torch.int32)
+    KV, shape = queries(heads=2), wise.prefix_shape(cache, Q, 0)
+    workspace = wise.wise_prefix_attn_workspace if bits == 16 else wise.wise_kvq_attn_workspace
+    calls = [lambda: cache.attend(0, Q, torch.empty_like(Q), lists), lambda: cache.write(0, lists, None, KV, KV),
+             lambda: cache.read(0, KV, KV.clone(), lists), lambda: workspace(cache, shape)]
+    monkeypatch.setattr(serve.PagedCache, "_use", lambda self, stream: wise._raw_stream(stream, self.index))
+    monkeypatch.setattr(serve, "_empty", lambda shape, dtype, device, stream: torch.empty(shape, dtype=dtype))
+    for call in calls:
+        call()
+    monkeypatch.setattr(wise, "_current_device", lambda: 1)
+    lib.calls.clear()
+    for call in calls:
+        with pytest.raises(ValueError, match="device"):
+            call()
+    assert lib.calls == []
