@@ -15,8 +15,6 @@ int launch_quant_attn(const PrefixParams& p, void* workspace, int sm_count, cuda
   L.p.plane = c.pool + (long long)p.layer * c.plane_bytes;
   L.p.batch = p.batch;
   L.p.q_len = p.q_len;
-  L.p.n_heads = p.n_heads;
-  L.p.group = p.group;
   L.p.n_groups = p.n_groups;
   L.p.rows = p.q_len * p.group;
   L.p.rows_inv = 65536 / L.p.rows + 1;

@@ -96,7 +96,7 @@ inline QaWork qa_work(void* base, int batch, int n_groups, int n_kv_heads, int r
 struct QaParams {
   CacheView cache;
   const uint8_t* plane;  // of the layer
-  int batch, q_len, n_heads, group, n_groups;
+  int batch, q_len, n_groups;
   int rows;      // of a request and kv head
   int rows_inv, q_len_inv;  // 65536 / x + 1: n / x = n * that >> 16 for n <= 128, as 128 / 65536 < 1 / x
   int chunks;    // of up to 64 rows
