@@ -466,10 +466,15 @@ int wise_kv_read(const wise_cache_t* cache, int layer, const int32_t* slots, con
 
 /* wise_prefix_attn over a cache in 8 or 4 bits.  Q and O are of type dtype
  * (WISE_BF16 or WISE_FP16); rows, groups, workspace, limits and faults are as
- * there, but for two things: a shared prefix is read once for every floor(64 /
+ * there, but for three things: a shared prefix is read once for every floor(64 /
  * R) requests of the group (R as there; by each request where that is 1 or 0),
- * and with R above 64 the last limit is 2^29.  Rows at or past lens may hold
- * anything here too. */
+ * with R above 64 the last limit is 2^29, and the softmax's numerators are
+ * rounded to fp16 whatever dtype is (those below 2^-32 of their row's largest
+ * one vanish).  Rows at or past lens may hold anything here too.
+ * With R up to 16, groups are better left out where the prefix is short: they
+ * select a kernel for up to 64 rows at a time, and a call that declares them
+ * takes up to 1.6 times as long as one that does not until about 2K tokens are
+ * shared by 64 requests, 4K to 7K by 32, 16K by 4 (R = 4, head_dim 128). */
 size_t wise_kvq_attn_workspace(const wise_cache_t* cache, const wise_prefix_t* shape);
 
 int wise_kvq_attn(const wise_cache_t* cache, int layer, const wise_prefix_t* shape, int dtype, const void* Q,

@@ -10,11 +10,15 @@
 // its 32 x 32 codes in registers, exchanging lane bit i with index bit i at a
 // time.
 //
-// Bound by instructions: 2 x 32K tokens of 8 heads of 128 are stored in 4 bits in
-// 65 us (343 MB read and written, 5.3 of a copy's 6.8 TB/s; 62 of 100 issue slots
-// taken: 16 values need their maximum, a quotient, a reciprocal and 16 products and
-// roundings) and read back in 66.  With a warp for 32 channels of a span at any size
-// storing and reading back took 199 us together and reading 103.
+// 2 x 32K tokens of 8 heads of 128 are stored in 4 bits in 65 us (343 MB read and
+// written, 5.3 of a copy's 6.8 TB/s) and read back in 66.  Storing is bound by
+// latency: with 64 registers a thread half of the warps that an SM holds are there,
+// and they take 63 of 100 issue slots (16 values need their maximum, a quotient, a
+// reciprocal and 16 products and roundings) and 56 of DRAM's, a third of their time
+// waiting for K and V.  Reading is next to what L1 takes, 86 of 100 of its cycles
+// (41 of the issue slots, 51 of DRAM's): the lanes of a warp write 32 bytes of a row
+// each; in 8 bits 64 of 100, and latency.  With a warp for 32 channels of a span at
+// any size storing and reading back took 199 us together and reading 103.
 #include <algorithm>
 
 #include "cache_common.cuh"

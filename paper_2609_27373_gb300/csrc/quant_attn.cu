@@ -34,8 +34,13 @@ int launch_quant_attn(const PrefixParams& p, void* workspace, int sm_count, cuda
   L.grid = sm_count;
   // The wide instance takes 64 rows at a time, the narrow one half a step's time
   // for at most 16 (32 x 12K tokens, 4 rows: 105 us against 145; 16 x 4K in 8
-  // bits 103 against 127).  Sharing prefixes needs the wide one: 64 on a shared
-  // 32K prefix take 116 us in it, 501 each by itself in the narrow one.
+  // bits 103 against 127).  Prefix items need the wide one, and both lines of the
+  // plan are walked in one launch, so own items run there too as soon as groups are
+  // given: what is shared is known on the device alone.  With 4 rows a request and
+  // 4 bits (us with groups, without): 64 requests of about 256 tokens behind 512
+  // shared ones 51, 33, behind 2K 59, 51, behind 8K 65, 139, behind 32K 106, 496;
+  // 32 of about 8K behind 40 (nothing is shared) 107, 82, behind 2K 116, 91, behind
+  // 8K 126, 135; 4 of about 10K behind 8K 35, 30, behind 32K 43, 53.
   L.wide = L.p.rows > 16 || L.p.per_tile > 0;
   L.stream = stream;
   cudaError_t e;

@@ -18,7 +18,11 @@
 //                from tensor memory in fragments of 8 keys x 8 rows, the mask,
 //                running maximum (raised only when a numerator passes 2^15, which
 //                the warps vote on), numerators as fp16 to shared memory (P, the B
-//                operand of the second product), O's rescaling;
+//                operand of the second product), O's rescaling.  A product takes
+//                both operands in one type, and K and V are exact in fp16: P's
+//                rounding there, 2^-11, is an eighth of bf16's.  fp16 outputs are
+//                off by 2.9e-4 (relative, whole outputs) with it, 2.1e-4 of which
+//                is their own rounding; in 32 bits they would take twice the room;
 //   4 warps      K: codes to tensor memory;
 //   8 or 4       V: the same, scales of 8 tokens at a time (in the narrow instance
 //                two teams that take every other half);
@@ -27,23 +31,27 @@
 //   a warp       producer: one bulk copy a page (codes and scales of keys and
 //                values lie together), the schedule;
 //   a warp       the walk over the segments and their page look-ups, and Q: rows of
-//                the next segment to shared memory as fp16, each scaled by a power
-//                of two so that its largest is next to 2^15 (exact down to 2^-28
-//                of it), and how many keys each row sees;
+//                the next segment to shared memory as fp16, those of bf16 each scaled
+//                by a power of two so that its largest is in [2^14, 2^15) (entries are
+//                exact down to 2^-31 of it), and how many keys each row sees;
 //   two warps    S products and P V products, each issued by one lane.
 // All of tensor memory is allocated, so that its first column is 0.
 //
-// What bounds it.  With 8 bits the memory: 32 x 4K tokens of 8 kv heads of 128 in
-// 103 us, 5.8 TB/s, 0.85 of a copy.  With 4 bits and long rows the instructions:
-// turning codes into operands and the softmax issue in 65 of 100 slots and wait for
-// one another's latencies in the rest (32 x 12K tokens: 105 us, 4.4 TB/s, 2300 clk
-// a step).  With short rows the fetching of instructions: 24 warps
-// in a dozen codes of their own keep little of what a segment does once in the
-// nearest cache, and code that runs once costs 8 to 10 clk an instruction.  So
-// what belongs to a segment is in loops and on warps beside the softmax's: with
-// the results on the softmax's warps, the walk on the producer's and the copying
-// of Q unrolled, a segment of one step took 8800 clk, now 6400 (5500 items of 210
-// tokens: 169 -> 124 us; of 900 tokens: 228 -> 183 us).
+// What bounds it.  With 8 bits the memory: 16 x about 4K tokens of 32 kv heads of
+// 128 in 103 us, 5.8 TB/s, 0.85 of a copy.  With 4 bits and long rows neither the
+// memory nor the issue slots are full (56 and 65 of 100): turning codes into operands
+// and the softmax wait for one another's latencies in the rest (32 x 12K tokens of 8
+// kv heads: 105 us, 4.4 TB/s, 2300 clk a step).  In the wide instance it is the chain
+// S, softmax, P of one step after the other, 1.0 us for 128 keys, which decodes them
+// for at most 64 rows (64 requests of 4 rows on a shared 32K prefix: 116 us, where a
+// cache of 16 bits takes 70: its items have 256 rows).  With short rows the fetching
+// of instructions: 24 warps in a dozen codes of their own keep little of what a
+// segment does once in the nearest cache, and code that runs once costs 8 to 10 clk
+// an instruction.  So what belongs to a segment is in loops and on warps beside the
+// softmax's: with the results on the softmax's warps, the walk on the producer's and
+// the copying of Q unrolled, a segment of one step took 8800 clk, now 6400 (5500 items
+// of 210 tokens: 169 -> 124 us; of 900 tokens: 228 -> 183 us).  6 to 9 us pass from the
+// last step of own keys to the first of a prefix with 64 rows.
 //
 // Every wait is bounded; one that runs out sets the status word and an abort
 // flag, and every role unwinds.

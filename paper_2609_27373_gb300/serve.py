@@ -139,7 +139,8 @@ class PagedCache(wise.Cache):
     def attend(self, layer: int, Q, O, slots, n_new=None, group_start=None, prefix_lens=None, scale: float = 0.0,
                stream=None) -> None:
         """Attention of Q [batch, n_heads, q_len, head_dim] over the sequences in slots, into O; the requests of
-        each group share their first prefix_lens[g] tokens."""
+        each group share their first prefix_lens[g] tokens.  (In 8 and 4 bits short prefixes are better not declared,
+        see include/wise.h.)"""
         raw = self._use(stream)
         plain = self.bits == 16
         key = (Q.shape, 0 if prefix_lens is None else prefix_lens.shape[0], scale)
