@@ -222,3 +222,23 @@ def test_queries_that_nobody_asked_may_hold_anything(bits, dtype, dim, n_heads, 
         assert torch.equal(outs[0], outs[1]) and not outs[1][~asked.expand_as(Q)].any()
         check_attention(outs[1], want, A, 333, float(twin.pool.abs().max()))
     assert wise.wise_get_status() == wise.WISE_OK
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_a_nan_leaves_the_others_of_its_group_alone(bits, dtype):
+    """NaN of either sign in keys and values: every finite value, of the same 16 too, is stored as it would be without it."""
+    c = serve.PagedCache(1, 6, 3, 32, 96, 2, 3, dtype, bits=bits)
+    gen = torch.Generator(device="cuda").manual_seed(bits)
+    x = torch.randn((2, 2, 3, 45, 96), generator=gen, device="cuda").to(dtype)
+    is_nan = torch.rand(x.shape, generator=gen, device="cuda") < 0.1
+    is_nan[..., 3, :16] = True  # a group of nothing else
+    bad = torch.full_like(x, float("nan"))
+    K, V = torch.where(is_nan, torch.where(torch.rand(x.shape, generator=gen, device="cuda") < 0.5, bad, -bad), x)
+    s = u32([1, 0])
+    c.write(0, s, c.extend(s, u32([45, 45])), K.contiguous(), V.contiguous())
+    got = torch.empty_like(x)
+    c.read(0, got[0], got[1], s)
+    want = stored(torch.where(is_nan, 0, x), bits)
+    assert torch.equal(torch.where(is_nan, 0, got.double()), want)
+    assert wise.wise_get_status() == wise.WISE_OK
